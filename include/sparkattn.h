@@ -400,6 +400,118 @@ int sparkattn_select_noalloc(const sparkattn_shape_t* shape, const void* q_bf16,
                              int32_t* kept_idx, int32_t* kept_cnt, void* cuda_stream);
 int sparkattn_select_noalloc_status(void* cuda_stream);
 
+/*
+ * Paged cache of keys and values (Sec. 1's auto-regressive extension: a generator that emits frames, or tokens, one after
+ * another attends to what it has made so far.  The paper has no cache; layout and rules are this library's).
+ *
+ * The cache is a pool of pages; a page holds `page` consecutive tokens of one sequence, for every head that has keys of
+ * its own.  K and V are two pools of the same strides, bf16 or E4M3 codes; with E4M3 every (page, head) has one positive
+ * fp32 scale in k_scale and one in v_scale, [pages, H] contiguous (value = decode(code) * scale).
+ * page_table[b][i] is the page of tokens i * page .. i * page + page - 1 of sequence b.
+ *
+ * A call works on a ragged batch: token rows q_start[b] .. q_start[b+1] - 1 of its row tensors ([T, heads, d], d
+ * contiguous) are the newest tokens of sequence b, which has kv_len[b] tokens in the cache with them; their positions are
+ * kv_len[b] - n_b .. kv_len[b] - 1.  Page table, lengths and starts are device memory and may change from call to call
+ * under a captured graph; the sizes in the structs may not.
+ *
+ * Errors found on the device (SPARKATTN_E_BAD_INDEX in the status word): a page outside [0, pages) among those the call
+ * reaches (its tokens are not stored, or not attended to), a length outside [0, max_pages * page], starts that are not
+ * ascending within [0, T], more new tokens than max_new or than kv_len[b], a rotary position outside the table (the row is left unrotated).
+ */
+typedef struct {
+  uint32_t struct_size; /* sizeof(sparkattn_cache_t)                                          */
+  uint32_t version;     /* SPARKATTN_VERSION                                                  */
+  int32_t dtype;        /* SPARKATTN_BF16 or SPARKATTN_FP8_E4M3                               */
+  int32_t pages;        /* pages in the pool                                                  */
+  int32_t H;            /* heads with keys and values of their own                            */
+  int32_t page;         /* tokens per page: 16, 32, 64 or 128                                 */
+  int32_t d;            /* head dim: 64 or 128                                                */
+  int32_t reserved;     /* must be 0                                                          */
+  int64_t stride_page, stride_h, stride_n; /* element strides of [pages, H, page, d]; d has stride 1; multiples of 16 bytes */
+} sparkattn_cache_t;
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(sparkattn_batch_t)                                          */
+  uint32_t version;     /* SPARKATTN_VERSION                                                  */
+  int32_t B;            /* sequences, at most 4096                                            */
+  int32_t T;            /* token rows of the call                                             */
+  int32_t max_new;      /* no sequence has more new tokens than this                          */
+  int32_t max_pages;    /* columns of page_table                                              */
+  const int32_t* page_table; /* [B, max_pages]                                                */
+  const int32_t* kv_len;     /* [B] tokens of the sequence, the new ones included             */
+  const int32_t* q_start;    /* [B + 1] first row of each sequence, or NULL: T / B rows each  */
+} sparkattn_batch_t;
+
+/* bf16 rows [T, heads, d], d contiguous; strides in elements, multiples of 8; 16-byte aligned */
+typedef struct {
+  void* data;
+  int64_t stride_t, stride_h;
+} sparkattn_rows_t;
+
+/* Rotation of the first `rot` channels: pair m turns by the angle whose cosine and sine are cos[p][m], sin[p][m], with p
+ * = positions[t][axis[m]], or the token's position in its sequence where positions is NULL.  Pairs are the channels
+ * (2m, 2m+1) (interleaved) or (m, m + rot/2):  y1 = x1 cos - x2 sin,  y2 = x1 sin + x2 cos,  every product, sum and
+ * difference rounded to fp32.  The table is the caller's: frequencies, scaling and long-context rules are in it. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(sparkattn_rotary_t)                                    */
+  uint32_t version;          /* SPARKATTN_VERSION                                             */
+  int32_t rot;               /* multiple of 16, at most d                                     */
+  int32_t interleaved;       /* 0 or 1                                                        */
+  int32_t rows;              /* rows of the tables                                            */
+  int32_t axes;              /* columns of positions: 1 to 4; 1 without positions             */
+  const float* cos;          /* [rows, rot/2], 16-byte aligned                                */
+  const float* sin;
+  const int32_t* positions;  /* [T, axes], or NULL                                            */
+  const int32_t* axis;       /* [rot/2], entries in [0, axes); NULL: all 0                    */
+} sparkattn_rotary_t;
+
+/* Bytes of device workspace that sparkattn_cache_fwd needs for H query heads (0: unsupported arguments);
+ * sparkattn_cache_append needs 256. */
+size_t sparkattn_cache_workspace_bytes(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, int32_t H);
+
+/*
+ * Rotates the new tokens' keys (and queries), and stores keys and values in the cache, in one launch.
+ *   bf16 pages: the rotated keys and the values, rounded to nearest even.
+ *   E4M3 pages: the scale of a (page, head) is the smallest power of two s with amax <= 448 s, amax the largest finite
+ *     |x| of the page's tokens, at least 1e-12, and grows with the page: s = max(the page's scale, the new tokens'),
+ *     unless the page's first token is among the new ones.  Where it grows, the codes of the tokens already there are
+ *     encoded again (code * (old * (1/s))), which a power of two leaves exact but for values that fall below 2^-6 s, so
+ *     that a page hardly depends on the steps in which it was filled.  New codes: e4m3_rne_satfinite(x * (1/s)).
+ *     Infinities become +-448 s, NaN stays NaN.
+ * q, q_out : bf16 rows [T, H, d] and where they go rotated (may be the same memory), or both NULL (H is ignored)
+ * k, v     : bf16 rows [T, cache->H, d]
+ * rotary   : NULL: nothing is rotated
+ * workspace: >= 256 bytes, 256-byte aligned; the status word
+ * Two sequences of a call must not append to the same page.
+ */
+int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rotary_t* rotary,
+                           const sparkattn_rows_t* q, int32_t H, const sparkattn_rows_t* k, const sparkattn_rows_t* v,
+                           void* k_cache, void* v_cache, float* k_scale, float* v_scale, const sparkattn_rows_t* q_out,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Softmax attention of the new tokens over the cache.  For the token at position i of its sequence and query head h, over
+ * the keys j of head h / (H / cache->H) with  lo(i) <= j < hi(i):
+ *   out = sum_j softmax_j(softmax_scale * q . k_j) v_j ,   lse = ln sum_j exp(softmax_scale * q . k_j)
+ *   frame_tokens = g >= 1 : hi = min(kv_len, (floor(i/g) + 1) g)   (causal by frames of g tokens; 1: by token)
+ *                  lo = (floor(i/g) - window_frames + 1) g, at least 0; window_frames = 0: lo = 0
+ *   frame_tokens = 0      : all of the sequence's keys (window_frames must be 0)
+ * A row without a key (an empty sequence) gives out = 0, lse = -inf.  What lies in a page behind the sequence's last
+ * token, or in a page that no row reaches, is not looked at, whatever it holds.
+ *
+ * H            : query heads, a multiple of cache->H
+ * q, out       : bf16 rows [T, H, d]; rows that belong to no sequence are not written
+ * softmax_scale: 0 selects 1/sqrt(d)
+ * lse          : fp32 [T, H] contiguous (natural log), or NULL
+ * workspace    : >= sparkattn_cache_workspace_bytes(cache, batch, H), 256-byte aligned; first word = device status
+ * Scores, maxima, sums and the output's accumulation are fp32; the weights are rounded for the second product, to bf16 or (E4M3 pages, few
+ * rows) to fp16.  The same inputs give the same bits.
+ */
+int sparkattn_cache_fwd(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rows_t* q, int32_t H,
+                        const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                        int32_t frame_tokens, int32_t window_frames, float softmax_scale, const sparkattn_rows_t* out,
+                        float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -40,6 +40,7 @@ EXPORTS = (
     "sparkattn_comp_apply", "sparkattn_select_window", "sparkattn_fwd_window", "sparkattn_brick_count",
     "sparkattn_brick_layout", "sparkattn_gather_tokens", "sparkattn_select_padded", "sparkattn_fwd_padded",
     "sparkattn_quant_fp8_pooled", "sparkattn_select_pooled", "sparkattn_fwd_gated_workspace_bytes", "sparkattn_fwd_gated",
+    "sparkattn_cache_workspace_bytes", "sparkattn_cache_append", "sparkattn_cache_fwd",
 )
 
 
@@ -57,6 +58,39 @@ class Shape(ctypes.Structure):
 _SHAPE_BYTES = ctypes.sizeof(Shape)
 
 
+class CacheShape(ctypes.Structure):
+    """Mirror of ``sparkattn_cache_t``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("version", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32), ("pages", ctypes.c_int32), ("H", ctypes.c_int32), ("page", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("stride_page", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_n", ctypes.c_int64),
+    ]
+
+
+class Batch(ctypes.Structure):
+    """Mirror of ``sparkattn_batch_t``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("version", ctypes.c_uint32),
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("max_new", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("page_table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+    ]
+
+
+class Rows(ctypes.Structure):
+    """Mirror of ``sparkattn_rows_t``."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class RotaryShape(ctypes.Structure):
+    """Mirror of ``sparkattn_rotary_t``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("version", ctypes.c_uint32),
+        ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("rows", ctypes.c_int32), ("axes", ctypes.c_int32),
+        ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+    ]
+
+
 class SparkAttnError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -66,7 +100,7 @@ class SparkAttnError(RuntimeError):
 # What the native marshalling of the per-layer calls (csrc/binding.cpp) calls, in its order.
 _BOUND = ("workspace_bytes", "select", "select_window", "select_padded", "select_pooled", "quant_fp8", "quant_fp8_pooled",
           "quant_fp8_per_token", "fwd", "fwd_window", "fwd_padded", "gather_tokens", "comp_workspace_bytes", "comp_state", "comp_apply",
-          "fwd_gated_workspace_bytes", "fwd_gated")
+          "fwd_gated_workspace_bytes", "fwd_gated", "cache_workspace_bytes", "cache_append", "cache_fwd")
 _NO_WORKSPACE = 1        # the library does not serve the shape: the workspace query returned 0
 
 _lib = None
@@ -137,6 +171,13 @@ def lib() -> ctypes.CDLL:
         L.sparkattn_fwd_gated.restype = ctypes.c_int
         L.sparkattn_fwd_gated.argtypes = [sp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp,
                                           vp, vp, sz, vp]
+        cp, bp, rp = ctypes.POINTER(CacheShape), ctypes.POINTER(Batch), ctypes.POINTER(Rows)
+        L.sparkattn_cache_workspace_bytes.restype = sz
+        L.sparkattn_cache_workspace_bytes.argtypes = [cp, bp, i32]
+        L.sparkattn_cache_append.restype = ctypes.c_int
+        L.sparkattn_cache_append.argtypes = [cp, bp, ctypes.POINTER(RotaryShape), rp, i32, rp, rp, vp, vp, vp, vp, rp, vp, sz, vp]
+        L.sparkattn_cache_fwd.restype = ctypes.c_int
+        L.sparkattn_cache_fwd.argtypes = [cp, bp, rp, i32, vp, vp, vp, vp, i32, i32, ctypes.c_float, rp, vp, vp, sz, vp]
         from . import _sparkattn
         _sparkattn.bind(*(ctypes.cast(getattr(L, "sparkattn_" + name), vp).value for name in _BOUND))
         _native = _sparkattn
@@ -409,4 +450,67 @@ def fwd_gated(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kept_idx: torch
     _check(rc, "sparkattn_fwd_gated")
     if check_status:
         _check(read_status(workspace, stream), "sparkattn_fwd_gated (device status)")
+    return (out, lse) if return_lse else out
+
+
+class KVCache(NamedTuple):
+    """Pools of a paged cache: ``k``, ``v`` [pages, H, page, d] of the same strides (d contiguous), bfloat16 or E4M3 codes
+    (float8_e4m3fn or uint8); E4M3 pools have ``k_scale``, ``v_scale`` float32 [pages, H]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+class Rotary(NamedTuple):
+    """Rotation of the first ``2 * cos.shape[1]`` channels of queries and keys: tables ``cos``, ``sin`` float32 [rows, rot/2];
+    pair m of token t turns by the angle of row ``positions[t, axis[m]]`` (int32 [T] or [T, axes]; None: the token's position in
+    its sequence).  Pairs are channels (2m, 2m+1) where ``interleaved``, else (m, m + rot/2)."""
+    cos: torch.Tensor
+    sin: torch.Tensor
+    positions: Optional[torch.Tensor] = None
+    axis: Optional[torch.Tensor] = None
+    interleaved: bool = False
+
+
+def alloc_cache(pages: int, heads: int, page: int, d: int, fp8: bool = True, device="cuda:0") -> KVCache:
+    """A cache of ``pages`` pages of ``page`` tokens (16, 32, 64 or 128) for ``heads`` key heads of ``d`` channels (64 or 128)."""
+    k, v = (torch.zeros((pages, heads, page, d), dtype=torch.uint8 if fp8 else torch.bfloat16, device=device) for _ in range(2))
+    if not fp8:
+        return KVCache(k, v)
+    return KVCache(k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn),
+                   *(torch.ones((pages, heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor, *,
+                 q_start: Optional[torch.Tensor] = None, max_new: int = 0, q: Optional[torch.Tensor] = None,
+                 rotary: Optional[Rotary] = None, q_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None, check_status: bool = False) -> Optional[torch.Tensor]:
+    """``sparkattn_cache_append``: stores k, v bf16 [T, H_kv, d] (k rotated) as the newest tokens of the sequences, and returns
+    q bf16 [T, H, d] rotated (None without q; ``q_out`` may be q).  page_table int32 [B, max_pages]; kv_len int32 [B] with the
+    new tokens; rows q_start[b] .. q_start[b+1] - 1 (int32 [B+1]) belong to sequence b, T / B each without it; max_new:
+    no sequence has more new tokens (0: T, or T / B)."""
+    cos, sin, positions, axis, interleaved = (None, None, None, None, False) if rotary is None else rotary
+    rc, q_out, workspace = _calls().cache_append(*cache, page_table, kv_len, q_start, max_new, k, v, q, q_out, cos, sin, positions, axis,
+                                                 interleaved, workspace, None if stream is None else stream.cuda_stream)
+    if rc != OK:
+        _check(rc, "sparkattn_cache_append")
+    if check_status:
+        _check(read_status(workspace, stream), "sparkattn_cache_append (device status)")
+    return q_out
+
+
+def cache_fwd(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, kv_len: torch.Tensor, *,
+              q_start: Optional[torch.Tensor] = None, max_new: int = 0, frame_tokens: int = 1, window: int = 0,
+              softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, return_lse: bool = False,
+              workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
+    """``sparkattn_cache_fwd``: softmax attention of the newest tokens' queries q bf16 [T, H, d] over the cache, H a multiple of
+    the cache's heads; causal by frames of ``frame_tokens`` tokens (1: by token, 0: not), over the last ``window`` frames (0: all).
+    The batch as in :func:`cache_append`.  Returns out bf16 [T, H, d] (and lse float32 [T, H])."""
+    rc, out, lse, workspace = _calls().cache_fwd(*cache, page_table, kv_len, q_start, max_new, q, frame_tokens, window, softmax_scale, out,
+                                                 return_lse, workspace, None if stream is None else stream.cuda_stream)
+    if rc != OK:
+        _check(rc, "sparkattn_cache_fwd")
+    if check_status:
+        _check(read_status(workspace, stream), "sparkattn_cache_fwd (device status)")
     return (out, lse) if return_lse else out

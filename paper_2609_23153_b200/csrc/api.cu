@@ -540,4 +540,90 @@ int sparkattn_attention_host(const sparkattn_shape_t* shape, int32_t dtype, cons
   return SPARKATTN_OK;
 }
 
+// ---------------------------------------------------------------------------------------------------- paged cache
+namespace {
+int check_cache(const sparkattn_cache_t* c, const sparkattn_batch_t* b) {
+  if (c == nullptr || b == nullptr) return SPARKATTN_E_INVALID_ARG;
+  if (c->struct_size != sizeof(sparkattn_cache_t) || c->version != SPARKATTN_VERSION || c->reserved != 0) return SPARKATTN_E_INVALID_ARG;
+  if (b->struct_size != sizeof(sparkattn_batch_t) || b->version != SPARKATTN_VERSION) return SPARKATTN_E_INVALID_ARG;
+  if (c->dtype != SPARKATTN_BF16 && c->dtype != SPARKATTN_FP8_E4M3) return SPARKATTN_E_INVALID_ARG;
+  if (c->pages < 1 || c->H < 1 || b->B < 1 || b->T < 1 || b->max_new < 1 || b->max_pages < 1) return SPARKATTN_E_INVALID_ARG;
+  if (b->max_new > b->T || (b->q_start == nullptr && (b->T % b->B != 0 || b->max_new != b->T / b->B))) return SPARKATTN_E_INVALID_ARG;
+  if (c->d != 64 && c->d != 128) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  if (b->B > kCacheMaxSequences || c->H > 65535) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  if (c->stride_n < c->d || c->stride_h < c->d || c->stride_page < 1) return SPARKATTN_E_INVALID_ARG;
+  const int per16 = c->dtype == SPARKATTN_BF16 ? 8 : 16;
+  if (c->stride_n % per16 || c->stride_h % per16 || c->stride_page % per16) return SPARKATTN_E_MISALIGNED;
+  return SPARKATTN_OK;
+}
+// strides of 0 stand for rows that are shared (read only)
+int check_rows(const sparkattn_rows_t* r, bool written) {
+  if (r == nullptr || r->data == nullptr || r->stride_t < (written ? 1 : 0) || r->stride_h < (written ? 1 : 0)) return SPARKATTN_E_INVALID_ARG;
+  return !aligned16(r->data) || r->stride_t % 8 || r->stride_h % 8 ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
+}
+int check_rotary(const sparkattn_rotary_t* r, int d) {
+  if (r == nullptr) return SPARKATTN_OK;
+  if (r->struct_size != sizeof(sparkattn_rotary_t) || r->version != SPARKATTN_VERSION) return SPARKATTN_E_INVALID_ARG;
+  if (!r->cos || !r->sin || r->rows < 1 || (r->interleaved != 0 && r->interleaved != 1)) return SPARKATTN_E_INVALID_ARG;
+  if (r->axes < 1 || r->axes > 4 || (r->positions == nullptr && r->axes != 1)) return SPARKATTN_E_INVALID_ARG;
+  if (r->rot < 16 || r->rot > d || r->rot % 16) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  return !aligned16(r->cos) || !aligned16(r->sin) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
+}
+// the pools, the table and the scales
+int check_pools(const sparkattn_cache_t* c, const sparkattn_batch_t* b, const void* k_cache, const void* v_cache, const float* k_scale,
+                const float* v_scale, void* workspace) {
+  if (!k_cache || !v_cache || !b->page_table || !b->kv_len || !workspace) return SPARKATTN_E_INVALID_ARG;
+  const bool fp8 = c->dtype == SPARKATTN_FP8_E4M3;
+  if (fp8 ? (!k_scale || !v_scale) : (k_scale || v_scale)) return SPARKATTN_E_INVALID_ARG;
+  return !aligned16(k_cache) || !aligned16(v_cache) || !aligned256(workspace) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
+}
+int check_heads(const sparkattn_cache_t* c, const sparkattn_batch_t* b, int32_t H) {
+  if (H < 1 || H % c->H) return SPARKATTN_E_INVALID_ARG;
+  return (long long)b->T * H > 0x7fffffffLL ? SPARKATTN_E_UNSUPPORTED_SHAPE : SPARKATTN_OK;
+}
+}  // namespace
+
+size_t sparkattn_cache_workspace_bytes(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, int32_t H) {
+  if (check_cache(cache, batch) != SPARKATTN_OK || check_heads(cache, batch, H) != SPARKATTN_OK) return 0;
+  return cache_fwd_workspace_bytes(*cache, *batch, H);
+}
+
+int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rotary_t* rotary,
+                           const sparkattn_rows_t* q, int32_t H, const sparkattn_rows_t* k, const sparkattn_rows_t* v,
+                           void* k_cache, void* v_cache, float* k_scale, float* v_scale, const sparkattn_rows_t* q_out,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_cache(cache, batch);
+  if (rc == SPARKATTN_OK) rc = check_rotary(rotary, cache->d);
+  if (rc == SPARKATTN_OK) rc = check_rows(k, false);
+  if (rc == SPARKATTN_OK) rc = check_rows(v, false);
+  if (rc == SPARKATTN_OK) rc = check_pools(cache, batch, k_cache, v_cache, k_scale, v_scale, workspace);
+  if (rc != SPARKATTN_OK) return rc;
+  if ((q == nullptr) != (q_out == nullptr)) return SPARKATTN_E_INVALID_ARG;
+  if (q != nullptr) {
+    if (H < 1) return SPARKATTN_E_INVALID_ARG;
+    if ((rc = check_rows(q, false)) != SPARKATTN_OK || (rc = check_rows(q_out, true)) != SPARKATTN_OK) return rc;
+  }
+  if (workspace_bytes < kWorkspaceHeaderBytes) return SPARKATTN_E_WORKSPACE_TOO_SMALL;
+  return launch_cache_append(*cache, *batch, rotary, q, H, *k, *v, k_cache, v_cache, k_scale, v_scale, q_out, workspace,
+                             static_cast<cudaStream_t>(cuda_stream));
+}
+
+int sparkattn_cache_fwd(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rows_t* q, int32_t H,
+                        const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                        int32_t frame_tokens, int32_t window_frames, float softmax_scale, const sparkattn_rows_t* out,
+                        float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_cache(cache, batch);
+  if (rc == SPARKATTN_OK) rc = check_heads(cache, batch, H);
+  if (rc == SPARKATTN_OK) rc = check_rows(q, false);
+  if (rc == SPARKATTN_OK) rc = check_rows(out, true);
+  if (rc == SPARKATTN_OK) rc = check_pools(cache, batch, k_cache, v_cache, k_scale, v_scale, workspace);
+  if (rc != SPARKATTN_OK) return rc;
+  if (frame_tokens < 0 || window_frames < 0 || (frame_tokens == 0 && window_frames != 0)) return SPARKATTN_E_INVALID_ARG;
+  if (!(softmax_scale >= 0.0f) || isinf(softmax_scale)) return SPARKATTN_E_INVALID_ARG;
+  if (workspace_bytes < cache_fwd_workspace_bytes(*cache, *batch, H)) return SPARKATTN_E_WORKSPACE_TOO_SMALL;
+  return launch_cache_fwd(*cache, *batch, *q, H, k_cache, v_cache, k_scale, v_scale, frame_tokens, window_frames, softmax_scale, *out, lse,
+                          workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
 }  // extern "C"

@@ -38,6 +38,9 @@ struct Library {
   decltype(&sparkattn_comp_apply) comp_apply;
   decltype(&sparkattn_fwd_gated_workspace_bytes) fwd_gated_workspace_bytes;
   decltype(&sparkattn_fwd_gated) fwd_gated;
+  decltype(&sparkattn_cache_workspace_bytes) cache_workspace_bytes;
+  decltype(&sparkattn_cache_append) cache_append;
+  decltype(&sparkattn_cache_fwd) cache_fwd;
 };
 Library g_lib{};
 
@@ -429,6 +432,148 @@ PyObject* fwd_gated(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// The paged cache: pools, scales and the batch, as both calls take them.
+struct Cache {
+  at::Tensor k, v, k_scale, v_scale, table, len, start;
+  sparkattn_cache_t c{};
+  sparkattn_batch_t b{};
+  explicit Cache(Args& a) {
+    k = a.tensor();
+    v = a.tensor();
+    k_scale = a.optional_tensor();
+    v_scale = a.optional_tensor();
+    table = a.tensor();
+    len = a.tensor();
+    start = a.optional_tensor();
+    b.max_new = a.i32();
+  }
+  // `rows`: a [T, heads, d] tensor of the call
+  void describe(const at::Tensor& rows) {
+    TORCH_CHECK_VALUE(k.dim() == 4 && k.stride(3) == 1, "expected pools [pages, H, page, d] with a contiguous last dimension");
+    same_layout(k, v);
+    const at::ScalarType type = k.scalar_type();
+    const bool codes = type == at::kByte || type == at::kFloat8_e4m3fn;
+    TORCH_CHECK_VALUE((codes || type == at::kBFloat16) && v.scalar_type() == type, "pools are bfloat16, float8_e4m3fn or uint8 (E4M3 codes)");
+    TORCH_CHECK_VALUE(codes == k_scale.defined() && codes == v_scale.defined(), "E4M3 pools have scales, bf16 pools have none");
+    for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&k_scale, &v_scale})
+      TORCH_CHECK_VALUE(!x->defined() || (x->scalar_type() == at::kFloat && x->dim() == 2 && x->is_contiguous() && x->size(0) == k.size(0) && x->size(1) == k.size(1)),
+                        "scales are contiguous float32 [pages, H]");
+    TORCH_CHECK_VALUE(table.scalar_type() == at::kInt && table.dim() == 2 && table.is_contiguous(), "page_table is a contiguous int32 [B, max_pages]");
+    TORCH_CHECK_VALUE(len.scalar_type() == at::kInt && len.is_contiguous() && len.dim() == 1 && len.size(0) == table.size(0), "kv_len is a contiguous int32 [B]");
+    TORCH_CHECK_VALUE(!start.defined() || (start.scalar_type() == at::kInt && start.is_contiguous() && start.dim() == 1 && start.size(0) == table.size(0) + 1),
+                      "q_start is a contiguous int32 [B + 1]");
+    for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&v, &k_scale, &v_scale, &table, &len, &start, &rows})
+      TORCH_CHECK_VALUE(!x->defined() || x->device() == k.device(), "tensors of one call must be on one device");
+    c.struct_size = sizeof(c);
+    c.version = SPARKATTN_VERSION;
+    c.dtype = codes ? SPARKATTN_FP8_E4M3 : SPARKATTN_BF16;
+    c.pages = (int32_t)k.size(0); c.H = (int32_t)k.size(1); c.page = (int32_t)k.size(2); c.d = (int32_t)k.size(3);
+    c.stride_page = k.stride(0); c.stride_h = k.stride(1); c.stride_n = k.stride(2);
+    b.struct_size = sizeof(b);
+    b.version = SPARKATTN_VERSION;
+    b.B = (int32_t)table.size(0);
+    b.T = (int32_t)rows.size(0);
+    if (b.max_new == 0) b.max_new = start.defined() || b.B == 0 ? b.T : b.T / b.B;
+    b.max_pages = (int32_t)table.size(1);
+    b.page_table = iptr(table); b.kv_len = iptr(len); b.q_start = iptr(start);
+  }
+  // a [T, heads, d] tensor of the call as the library takes it; heads 0: any number
+  sparkattn_rows_t rows(const at::Tensor& x, int64_t heads) const {
+    TORCH_CHECK_VALUE(x.dim() == 3 && x.stride(2) == 1 && x.scalar_type() == at::kBFloat16 && x.size(0) == b.T && x.size(2) == c.d &&
+                          (heads == 0 || x.size(1) == heads) && x.device() == k.device(),
+                      "expected bfloat16 rows [T, heads, d] of the call's T and d with a contiguous last dimension");
+    return {x.data_ptr(), x.stride(0), x.stride(1)};
+  }
+};
+
+// cache_append(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, k, v, q, q_out, cos, sin, positions, axis,
+// interleaved, workspace, stream) -> rc, q_out, workspace
+PyObject* cache_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(19);
+  Cache cache(a);
+  const at::Tensor k = a.tensor(), v = a.tensor(), q = a.optional_tensor();
+  at::Tensor q_out = a.optional_tensor();
+  const at::Tensor cos = a.optional_tensor(), sin = a.optional_tensor(), positions = a.optional_tensor(), axis = a.optional_tensor();
+  const bool interleaved = a.truth();
+  at::Tensor ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  cache.describe(k);
+  const sparkattn_rows_t rk = cache.rows(k, cache.c.H), rv = cache.rows(v, cache.c.H);
+  sparkattn_rotary_t rotary{};
+  if (cos.defined()) {
+    TORCH_CHECK_VALUE(sin.defined() && cos.dim() == 2 && cos.scalar_type() == at::kFloat && sin.scalar_type() == at::kFloat && cos.is_contiguous() &&
+                          sin.is_contiguous() && cos.sizes() == sin.sizes() && cos.device() == k.device() && sin.device() == k.device(),
+                      "rotary tables are contiguous float32 [rows, rot / 2] on the call's device");
+    TORCH_CHECK_VALUE(!positions.defined() || (positions.scalar_type() == at::kInt && positions.is_contiguous() && positions.device() == k.device() &&
+                                               (positions.dim() == 1 || positions.dim() == 2) && positions.size(0) == k.size(0)),
+                      "positions are contiguous int32 [T] or [T, axes] on the call's device");
+    TORCH_CHECK_VALUE(!axis.defined() || (axis.scalar_type() == at::kInt && axis.is_contiguous() && axis.dim() == 1 && axis.size(0) == cos.size(1) &&
+                                          axis.device() == k.device()),
+                      "axis is a contiguous int32 [rot / 2] on the call's device");
+    TORCH_CHECK_VALUE(axis.defined() || !positions.defined() || positions.dim() == 1 || positions.size(1) == 1, "positions over several axes need axis");
+    rotary.struct_size = sizeof(rotary);
+    rotary.version = SPARKATTN_VERSION;
+    rotary.rot = (int32_t)(2 * cos.size(1));
+    rotary.interleaved = interleaved;
+    rotary.rows = (int32_t)cos.size(0);
+    rotary.axes = positions.defined() && positions.dim() == 2 ? (int32_t)positions.size(1) : 1;
+    rotary.cos = fptr(cos); rotary.sin = fptr(sin);
+    rotary.positions = iptr(positions); rotary.axis = iptr(axis);
+  }
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    if (q.defined() && !q_out.defined()) q_out = at::empty(q.sizes(), on(q, at::kBFloat16));
+    if (!ws.defined()) ws = at::empty({256}, on(k, at::kByte));
+    sparkattn_rows_t rq{}, ro{};
+    if (q.defined()) {
+      rq = cache.rows(q, 0);
+      ro = cache.rows(q_out, q.size(1));
+    }
+    rc = g_lib.cache_append(&cache.c, &cache.b, cos.defined() ? &rotary : nullptr, q.defined() ? &rq : nullptr, q.defined() ? (int32_t)q.size(1) : 0, &rk, &rv,
+                            ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), q.defined() ? &ro : nullptr, ptr(ws),
+                            (size_t)ws.numel(), stream);
+  }
+  return result(rc, {q_out, ws});
+  END_HANDLE_TH_ERRORS
+}
+
+// cache_fwd(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, q, frame_tokens, window, softmax_scale, out, return_lse,
+// workspace, stream) -> rc, out, lse, workspace
+PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(16);
+  Cache cache(a);
+  const at::Tensor q = a.tensor();
+  const int32_t frame_tokens = a.i32(), window = a.i32();
+  const float softmax_scale = a.number();
+  at::Tensor out = a.optional_tensor(), lse;
+  const bool return_lse = a.truth();
+  at::Tensor ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  cache.describe(q);
+  const sparkattn_rows_t rq = cache.rows(q, 0);
+  const int32_t H = (int32_t)q.size(1);
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    if (!out.defined()) out = at::empty(q.sizes(), on(q, at::kBFloat16));
+    const sparkattn_rows_t ro = cache.rows(out, H);
+    if (return_lse) lse = at::empty({q.size(0), q.size(1)}, on(q, at::kFloat));
+    if (!ws.defined()) {
+      const size_t bytes = g_lib.cache_workspace_bytes(&cache.c, &cache.b, H);
+      ws = at::empty({(int64_t)(bytes < 256 ? 256 : bytes)}, on(q, at::kByte));      // an unsupported call says why itself
+    }
+    rc = g_lib.cache_fwd(&cache.c, &cache.b, &rq, H, ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), frame_tokens, window,
+                         softmax_scale, &ro, fptr(lse), ptr(ws), (size_t)ws.numel(), stream);
+  }
+  return result(rc, {out, lse, ws});
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(address of each entry point, in the order of Library)
 PyObject* bind(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -448,7 +593,8 @@ PyMethodDef method(const char* name) { return {name, reinterpret_cast<PyCFunctio
 PyMethodDef g_methods[] = {method<bind>("bind"), method<select>("select"), method<select_pooled>("select_pooled"),
                            method<quant_fp8>("quant_fp8"), method<quant_fp8_pooled>("quant_fp8_pooled"),
                            method<quant_fp8_per_token>("quant_fp8_per_token"), method<fwd>("fwd"), method<gather_tokens>("gather_tokens"),
-                           method<comp_state>("comp_state"), method<comp_apply>("comp_apply"), method<fwd_gated>("fwd_gated"), {nullptr, nullptr, 0, nullptr}};
+                           method<comp_state>("comp_state"), method<comp_apply>("comp_apply"), method<fwd_gated>("fwd_gated"),
+                           method<cache_append>("cache_append"), method<cache_fwd>("cache_fwd"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_sparkattn", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -29,17 +29,19 @@ inline EncodeTiledFn encode_tiled_fn() {
 }
 
 // dims[0] is the contiguous dimension (elements); strides are those of dims[1..3], in elements.
+// Rows shorter than a slab (64 bytes: 64 one-byte channels) take the whole box width and the swizzle of that width.
 inline int make_slab_map(CUtensorMap* map, const void* base, int elt_bytes, const uint64_t (&dims)[4],
                          const uint64_t (&strides_elems)[3], uint32_t box_rows) {
+  const bool narrow = dims[0] * elt_bytes == 64;
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return SPARKATTN_E_NO_DEVICE;
   const cuuint64_t d[4] = {dims[0], dims[1], dims[2], dims[3]};
   const cuuint64_t st[3] = {strides_elems[0] * elt_bytes, strides_elems[1] * elt_bytes, strides_elems[2] * elt_bytes};
-  const cuuint32_t box[4] = {(cuuint32_t)(128 / elt_bytes), box_rows, 1u, 1u};
+  const cuuint32_t box[4] = {(cuuint32_t)((narrow ? 64 : 128) / elt_bytes), box_rows, 1u, 1u};
   const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
   const CUresult r = enc(map, elt_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4,
                          const_cast<void*>(base), d, st, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         narrow ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? SPARKATTN_OK : SPARKATTN_E_CUDA;
 }
@@ -48,6 +50,13 @@ inline int make_slab_map(CUtensorMap* map, const void* base, int elt_bytes, cons
 inline int make_token_map(CUtensorMap* map, const void* base, int elt_bytes, const sparkattn_shape_t& s, int box_rows) {
   const uint64_t dims[4] = {(uint64_t)s.d, (uint64_t)s.N, (uint64_t)s.H, (uint64_t)s.B};
   const uint64_t strides[3] = {(uint64_t)s.stride_n, (uint64_t)s.stride_h, (uint64_t)s.stride_b};
+  return make_slab_map(map, base, elt_bytes, dims, strides, (uint32_t)box_rows);
+}
+
+// [pages, H, page, d] pool of a paged cache
+inline int make_page_map(CUtensorMap* map, const void* base, int elt_bytes, const sparkattn_cache_t& c, int box_rows) {
+  const uint64_t dims[4] = {(uint64_t)c.d, (uint64_t)c.page, (uint64_t)c.H, (uint64_t)c.pages};
+  const uint64_t strides[3] = {(uint64_t)c.stride_n, (uint64_t)c.stride_h, (uint64_t)c.stride_page};
   return make_slab_map(map, base, elt_bytes, dims, strides, (uint32_t)box_rows);
 }
 
