@@ -26,122 +26,13 @@
 
 #include <type_traits>
 
-#include "cache.h"
+#include "cache_line.cuh"
 #include "tmap.h"
 
 namespace sparkattn {
 
 constexpr int kTileKeys = 64, kGroupKeys = 16, kGroups = kTileKeys / kGroupKeys;
 constexpr int kComputeWarps = 4, kDecodeThreads = 32 * (kComputeWarps + 1);
-
-// The reference m of a row moves when a weight would pass 2^10 times the one that set it; weights are 2^kBase at the reference, so
-// that fp16 holds them (2^15 < 65504) and loses only what lies 2^-29 below it.
-constexpr float kBase = 5.0f, kLazy = 10.0f;
-
-struct DecodeParams {
-  BatchView batch;
-  Causal causal;
-  const __nv_bfloat16* q;
-  __nv_bfloat16* out;
-  int64_t q_stride_t, q_stride_h, out_stride_t, out_stride_h;
-  const float* k_scale;
-  const float* v_scale;
-  float* lse;
-  int H, Hk, G;
-  float scale_log2;
-  int box_rows, boxes;           // keys of one TMA box, boxes of a tile
-  int least;                     // tiles a CTA takes at least
-  int stages;
-  int32_t* status;
-  int32_t* prefix;               // [B + 2] first tile of every sequence, the total, tiles per CTA
-  float* part_ml;                // [2 workers][rows][2]
-  float* part_o;                 // [2 workers][rows][d]
-};
-
-// ------------------------------------------------------------------------------------------------------------ the line
-// Tiles of a sequence (at least one, so that somebody writes the rows of an empty one), its first tile, its row tiles.
-struct Span {
-  int tiles, first, row_tiles;
-};
-__device__ __forceinline__ Span span_of(const DecodeParams& p, const Sequence& s, int rows_per_tile) {
-  Span r{0, 0, 0};
-  if (s.n == 0) return r;
-  const int2 a = visible_keys(p.causal, s.first_pos(), s.len), z = visible_keys(p.causal, s.len - 1, s.len);
-  r.first = a.x / kTileKeys;
-  r.tiles = max((z.y + kTileKeys - 1) / kTileKeys - r.first, 1);
-  r.row_tiles = (s.n * p.G + rows_per_tile - 1) / rows_per_tile;
-  return r;
-}
-// all threads: s_prefix[b] = tiles in front of sequence b, s_prefix[B] = all
-__device__ __forceinline__ void lay_out(const DecodeParams& p, int rows_per_tile, int* s_prefix, int* s_warp) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  int carry = 0;
-  for (int base = 0; base < p.batch.B; base += blockDim.x) {
-    const int b = base + threadIdx.x;
-    int mine = 0;
-    if (b < p.batch.B) {
-      const Span s = span_of(p, sequence_of(p.batch, b), rows_per_tile);
-      mine = s.tiles * s.row_tiles * p.Hk;
-    }
-    int x = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) s_warp[warp] = x;
-    __syncthreads();
-    int before = carry, all = carry;
-    for (int w = 0; w < warps; ++w) {
-      if (w < warp) before += s_warp[w];
-      all += s_warp[w];
-    }
-    if (b < p.batch.B) s_prefix[b] = before + x - mine;
-    carry = all;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) s_prefix[p.batch.B] = carry;
-  __syncthreads();
-}
-__device__ __forceinline__ int share_of(int total, int workers, int least) { return max((total + workers - 1) / workers, least); }
-// the sequence that tile x belongs to
-__device__ __forceinline__ int owner_of(const int* prefix, int B, int x) {
-  int lo = 0, hi = B;                   // prefix[lo] <= x < prefix[hi]; sequences without tiles have equal entries
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (prefix[mid] <= x) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
-// A stretch of the line, taken item by item.
-struct Segment {
-  Sequence seq;
-  int b, h, row0, rows;        // key head; first row of the tile and how many
-  int t0, t1;                  // tiles of the sequence, counted from the front of its keys
-  int lo, hi;                  // keys that any row of the tile sees
-  bool whole;                  // the item lies in this stretch
-  bool first;                  // the stretch's first segment
-};
-template <int R>
-__device__ __forceinline__ Segment segment_at(const DecodeParams& p, const int* prefix, int x, int end, bool first) {
-  Segment g;
-  g.b = owner_of(prefix, p.batch.B, x);
-  g.seq = sequence_of(p.batch, g.b);
-  const Span s = span_of(p, g.seq, R);
-  const int in = x - prefix[g.b], item = in / s.tiles, at = in - item * s.tiles;
-  g.h = item / s.row_tiles;
-  g.row0 = (item - g.h * s.row_tiles) * R;
-  g.rows = min(R, g.seq.n * p.G - g.row0);
-  const int until = min(s.tiles, at + end - x);
-  g.t0 = s.first + at;
-  g.t1 = s.first + until;
-  g.whole = at == 0 && until == s.tiles;
-  g.first = first;
-  g.lo = visible_keys(p.causal, g.seq.first_pos() + g.row0 / p.G, g.seq.len).x;
-  g.hi = visible_keys(p.causal, g.seq.first_pos() + (g.row0 + g.rows - 1) / p.G, g.seq.len).y;
-  return g;
-}
 
 // ---------------------------------------------------------------------------------------------------------- fragments
 __device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t two) {
@@ -180,14 +71,6 @@ __device__ __forceinline__ uint2 lds8(uint32_t at) {
   return v;
 }
 
-// what the consumer needs to know of 16 keys
-struct GroupInfo {
-  float k;           // factor of the logits
-  float v_log2;      // log2 of the V scale
-  float v_inv;       // its inverse
-  int usable;        // the page exists
-};
-
 template <int D, bool FP8, int NT>
 struct DecodeShape {
   static constexpr int R = 8 * NT;
@@ -205,7 +88,7 @@ struct DecodeShape {
 template <int D, bool FP8, int NT>
 __global__ void __launch_bounds__(kDecodeThreads, 2)
 cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
-                    const __grid_constant__ DecodeParams p) {
+                    const __grid_constant__ CacheFwdParams p) {
   using S = DecodeShape<D, FP8, NT>;
   constexpr int R = S::R, kRowBytes = S::kRowBytes;
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -222,7 +105,6 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
   int* s_warp = s_bad + 2;
   int* s_prefix = s_warp + 8;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int workers = gridDim.x - 1;
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
@@ -233,17 +115,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     *s_abort = 0;
   }
   pdl_wait();
-  lay_out(p, R, s_prefix, s_warp);
-  const int total = s_prefix[p.batch.B], share = share_of(total, workers, p.least);
-  if (blockIdx.x == 0) {           // checks what the others work on, and leaves the line for the combining kernel
-    for (int b = threadIdx.x; b <= p.batch.B; b += kDecodeThreads) p.prefix[b] = s_prefix[b];
-    if (threadIdx.x == 0) p.prefix[p.batch.B + 1] = share;
-    check_batch(p.batch, s_bad, [&](const Sequence& s) {
-      if (s.n == 0) return make_int2(0, 0);
-      const int lo = visible_keys(p.causal, s.first_pos(), s.len).x, hi = visible_keys(p.causal, s.len - 1, s.len).y;
-      return make_int2(lo >> p.batch.page_shift, (hi + (1 << p.batch.page_shift) - 1) >> p.batch.page_shift);
-    });
-    leave_status(p.status, s_bad);
+  Line<R, kTileKeys>::lay_out(p, s_prefix, s_warp);
+  const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys>::share_of(p, total);
+  if (blockIdx.x == 0) {
+    check_and_publish<R, kTileKeys>(p, s_prefix, share, s_bad);
     return;
   }
   const int worker = blockIdx.x - 1;
@@ -255,29 +130,17 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     // ------------------------------------------------------------------------------------------------------ copies
     int stage = 0, use = 0;
     bool ok = true;
-    for (int x = x0; ok && x < x1;) {
-      const Segment g = segment_at<R>(p, s_prefix, x, x1, x == x0);
-      x += g.t1 - g.t0;
-      const int32_t* table = p.batch.page_table + (int64_t)g.b * p.batch.max_pages;
+    Stretch<R, kTileKeys> g;
+    g.begin(p, s_prefix, x0, x1);
+    do {
+      const int32_t* table = p.batch.page_table + (int64_t)g.c.b * p.batch.max_pages;
       constexpr int kBatch = 32 / kGroups;                   // tiles whose groups the lanes look up together
       // lane l looks after group l of a batch: its page and scales, asked for a batch ahead
       int page_n;
       GroupInfo info_n;
       auto look_up = [&](int t) {
-        const int key = t * kTileKeys + lane * kGroupKeys;
-        page_n = -1;
-        info_n = {1.0f, 0.0f, 1.0f, 0};
-        if (key < g.hi && key + kGroupKeys > g.lo && t * kTileKeys + lane * kGroupKeys < g.t1 * kTileKeys) page_n = table[key >> p.batch.page_shift];
-        if ((uint32_t)page_n >= (uint32_t)p.batch.pages) page_n = -1;
-        if (page_n >= 0) {
-          info_n.usable = 1;
-          if constexpr (FP8) {
-            info_n.k = p.k_scale[(int64_t)page_n * p.Hk + g.h];
-            const float v = fmaxf(p.v_scale[(int64_t)page_n * p.Hk + g.h], 5.4e-20f);      // 2^-64: a scale of zero stays finite
-            info_n.v_log2 = log2f(v);
-            info_n.v_inv = 1.0f / v;
-          }
-        }
+        const bool in = t + lane / kGroups < g.t1;
+        page_n = look_up_group<FP8>(p, table, g.c.h, in ? t * kTileKeys + lane * kGroupKeys : 0x7fffff00, g.c.item.lo, g.c.item.hi, info_n);
       };
       look_up(g.t0);
       for (int t = g.t0; ok && t < g.t1; t += kBatch) {
@@ -313,12 +176,12 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
             constexpr int kSlab = kRowBytes > 128 ? 128 : kRowBytes;
 #pragma unroll
             for (int sl = 0; sl < kRowBytes / kSlab; ++sl)
-              tma_load_4d(dst + sl * (kTileKeys * kSlab) + box * p.box_rows * kSlab, map, full + stage, sl * (kSlab / S::kElt), row, g.h, box_page);
+              tma_load_4d(dst + sl * (kTileKeys * kSlab) + box * p.box_rows * kSlab, map, full + stage, sl * (kSlab / S::kElt), row, g.c.h, box_page);
           }
           if (++stage == p.stages) { stage = 0; ++use; }
         }
       }
-    }
+    } while (ok && g.next(p));
     // (nobody leaves before the copies have landed: the computing warps wait for every tile)
   } else {
     // ---------------------------------------------------------------------------------------------------- products
@@ -327,9 +190,9 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     constexpr int kChunkCh = 16 / S::kElt;             // channels of a 16-byte chunk
     int stage = 0, use = 0, segments = 0;
     bool ok = true;
-    for (int x = x0; ok && x < x1;) {
-      const Segment g = segment_at<R>(p, s_prefix, x, x1, x == x0);
-      x += g.t1 - g.t0;
+    Stretch<R, kTileKeys> g;
+    g.begin(p, s_prefix, x0, x1);
+    do {
       // the rows' queries as the first product's B operand: lane (g8, t4) has channels of row g8
       uint32_t qf[NT][kSteps][2];
       float c_row[NT][2];                              // of the accumulators' rows 2 t4 and 2 t4 + 1: logit -> log2 units
@@ -338,8 +201,8 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       for (int nt = 0; nt < NT; ++nt) {
         const int r = nt * 8 + g8, row = g.row0 + r;
         const bool there = r < g.rows;
-        const int token = there ? row / p.G : 0, head = there ? g.h * p.G + (row - token * p.G) : 0;
-        const __nv_bfloat16* src = p.q + (int64_t)(g.seq.start + token) * p.q_stride_t + head * p.q_stride_h;
+        const int token = there ? row / p.G : 0, head = there ? g.c.h * p.G + (row - token * p.G) : 0;
+        const __nv_bfloat16* src = p.q + (int64_t)(g.c.seq.start + token) * p.q_stride_t + head * p.q_stride_h;
         uint2 raw[kSteps];
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
@@ -378,7 +241,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
           for (int j = 0; j < kSteps; ++j) { qf[nt][j][0] = raw[j].x; qf[nt][j][1] = raw[j].y; }
         }
-        const int2 seen = there ? visible_keys(p.causal, g.seq.first_pos() + token, g.seq.len) : make_int2(0, 0);
+        const int2 seen = there ? visible_keys(p.causal, g.c.seq.first_pos() + token, g.c.seq.len) : make_int2(0, 0);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int from = (2 * t4 + i) * 4;
@@ -482,7 +345,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int key = key0 + 4 * t4 + i;
-            if (key < g.lo || key >= g.hi) {
+            if (key < g.c.item.lo || key >= g.c.item.hi) {
 #pragma unroll
               for (int w = 0; w < kVWords; ++w) vw[i][w] = 0u;
             }
@@ -597,7 +460,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           for (int j = 0; j < 8; ++j) acc[j] = fmaf(src[j], f, acc[j]);
         }
         if (g.whole) {
-          const int row = g.row0 + r, token = g.seq.start + row / p.G, head = g.h * p.G + row % p.G;
+          const int row = g.row0 + r, token = g.c.seq.start + row / p.G, head = g.c.h * p.G + row % p.G;
           const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
           uint32_t w[4];
 #pragma unroll
@@ -617,70 +480,39 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       __syncwarp();
       if (lane == 0) mbar_arrive(taken);
       ++segments;
-    }
+    } while (g.next(p));
   }
   if (*s_abort) __nanosleep(200000);      // let copies in flight land before the CTA's memory goes
-}
-
-// Adds up what several stretches have left of an item, in the order of the line.  A CTA per item, a warp per row.
-template <int D, int NT>
-__global__ void __launch_bounds__(128)
-combine_kernel(const __grid_constant__ DecodeParams p, int max_row_tiles) {
-  constexpr int R = 8 * NT, kVec = D / 32;
-  pdl_wait();
-  const int b = blockIdx.x / (p.Hk * max_row_tiles), rest = blockIdx.x % (p.Hk * max_row_tiles);
-  const int h = rest / max_row_tiles, rt = rest % max_row_tiles;
-  const Sequence seq = sequence_of(p.batch, b);
-  const Span s = span_of(p, seq, R);
-  if (rt >= s.row_tiles) return;
-  const int start = p.prefix[b] + (h * s.row_tiles + rt) * s.tiles, share = p.prefix[p.batch.B + 1];
-  const int w0 = start / share, w1 = (start + s.tiles - 1) / share;
-  if (w0 == w1) return;
-  const int lane = threadIdx.x & 31, rows = min(R, seq.n * p.G - rt * R);
-  for (int r = threadIdx.x >> 5; r < rows; r += 4) {
-    auto slot_of = [&](int w) { return 2 * w + (start <= w * share ? 0 : 1); };
-    float top = -INFINITY;
-    for (int w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, p.part_ml[((int64_t)slot_of(w) * R + r) * 2]);
-#pragma unroll
-    for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-    float sum = 0.0f, acc[kVec] = {};
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const int64_t at = (int64_t)slot_of(w) * R + r;
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
-      const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
-      sum = fmaf(ml.y, f, sum);
-      const float* src = p.part_o + at * D + lane * kVec;
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) acc[j] = fmaf(src[j], f, acc[j]);
-    }
-    const int row = rt * R + r, token = seq.start + row / p.G, head = h * p.G + row % p.G;
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + lane * kVec);
-#pragma unroll
-    for (int j = 0; j < kVec / 2; ++j) {
-      const __nv_bfloat162 v = __floats2bfloat162_rn(acc[2 * j] * inv, acc[2 * j + 1] * inv);
-      dst[j] = *reinterpret_cast<const uint32_t*>(&v);
-    }
-    if (p.lse && lane == 0) p.lse[(int64_t)token * p.H + head] = sum == 0.0f ? -INFINITY : (top - kBase + log2f(sum)) * 0.6931471805599453f;
-  }
 }
 
 // ------------------------------------------------------------------------------------------------------------ host side
 namespace {
 constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-// 8-row tiles where they suffice, else 16
-int row_tile(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) { return (long long)(H / c.H) * b.max_new <= 8 ? 8 : 16; }
+// rows of an item, and stretches of the line: up to 16 rows per key head take this file's kernel, more the tensor cores' (cache_chunk.cu)
+struct Plan {
+  int R, workers;
+  size_t prefix, ml, o;        // bytes of the workspace's parts behind the header
+};
+Plan plan_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
+  const long long rows = (long long)(H / c.H) * b.max_new;
+  Plan p;
+  p.R = rows <= 8 ? 8 : rows <= 16 ? 16 : kChunkRows;
+  p.workers = current_sm_count() * (p.R == kChunkRows ? 1 : 2);
+  p.prefix = align256((size_t)(b.B + 2) * 4);
+  p.ml = align256((size_t)2 * p.workers * p.R * 8);
+  p.o = (size_t)2 * p.workers * p.R * c.d * 4;
+  return p;
+}
 }  // namespace
 
 size_t cache_fwd_workspace_bytes(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
-  const int workers = 2 * current_sm_count(), R = row_tile(c, b, H);
-  return kWorkspaceHeaderBytes + align256((size_t)(b.B + 2) * 4) + align256((size_t)2 * workers * R * 8) + (size_t)2 * workers * R * c.d * 4;
+  const Plan p = plan_of(c, b, H);
+  return kWorkspaceHeaderBytes + p.prefix + p.ml + p.o;
 }
 
 template <int D, bool FP8, int NT>
-static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b, DecodeParams& p, const void* k_cache, const void* v_cache,
-                         int workers, cudaStream_t stream) {
+static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b, CacheFwdParams& p, const void* k_cache, const void* v_cache,
+                         cudaStream_t stream) {
   using S = DecodeShape<D, FP8, NT>;
   CUtensorMap mk, mv;
   int rc;
@@ -696,17 +528,14 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   const int smem = p.stages * S::kStageBytes + S::fixed_bytes(b.B, p.stages);
   auto kern = cache_decode_kernel<D, FP8, NT>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
-  if ((rc = launch_kernel(kern, dim3(workers + 1), kDecodeThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
-  const int row_tiles = (int)(((long long)p.G * b.max_new + S::R - 1) / S::R);
-  const long long items = (long long)b.B * c.H * row_tiles;
-  if (items > 0x7fffffffLL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
-  return launch_kernel(combine_kernel<D, NT>, dim3((unsigned)items), 128, 0, true, stream, p, row_tiles);
+  if ((rc = launch_kernel(kern, dim3(p.workers + 1), kDecodeThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
+  return launch_kernel(combine_kernel<D, S::R, kTileKeys>, dim3(p.workers), 128, 0, true, stream, p);
 }
 
 int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rows_t& q, int H, const void* k_cache,
                      const void* v_cache, const float* k_scale, const float* v_scale, int frame_tokens, int window, float softmax_scale,
                      const sparkattn_rows_t& out, float* lse, void* workspace, cudaStream_t stream) {
-  DecodeParams p{};
+  CacheFwdParams p{};
   p.batch = make_batch_view(c, b);
   p.causal = {frame_tokens, window};
   p.q = static_cast<const __nv_bfloat16*>(q.data);
@@ -718,20 +547,22 @@ int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, con
   p.H = H; p.Hk = c.H; p.G = H / c.H;
   p.scale_log2 = (softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf((float)c.d)) * 1.4426950408889634f;
   p.least = 1;
-  const int workers = 2 * current_sm_count(), R = row_tile(c, b, H);
-  if (workers < 2) return SPARKATTN_E_CUDA;
+  const Plan plan = plan_of(c, b, H);
+  if (plan.workers < 1) return SPARKATTN_E_CUDA;
+  p.workers = plan.workers;
   char* base = static_cast<char*>(workspace);
   p.status = reinterpret_cast<int32_t*>(base);
   base += kWorkspaceHeaderBytes;
   p.prefix = reinterpret_cast<int32_t*>(base);
-  base += align256((size_t)(b.B + 2) * 4);
+  base += plan.prefix;
   p.part_ml = reinterpret_cast<float*>(base);
-  base += align256((size_t)2 * workers * R * 8);
+  base += plan.ml;
   p.part_o = reinterpret_cast<float*>(base);
+  if (plan.R == kChunkRows) return launch_cache_chunk(c, b, p, k_cache, v_cache, stream);
   const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;
   auto go = [&](auto d, auto e4m3) {
-    return R == 8 ? launch_decode<decltype(d)::value, decltype(e4m3)::value, 1>(c, b, p, k_cache, v_cache, workers, stream)
-                  : launch_decode<decltype(d)::value, decltype(e4m3)::value, 2>(c, b, p, k_cache, v_cache, workers, stream);
+    return plan.R == 8 ? launch_decode<decltype(d)::value, decltype(e4m3)::value, 1>(c, b, p, k_cache, v_cache, stream)
+                       : launch_decode<decltype(d)::value, decltype(e4m3)::value, 2>(c, b, p, k_cache, v_cache, stream);
   };
   using std::integral_constant;
   if (c.d == 128) return fp8 ? go(integral_constant<int, 128>{}, integral_constant<bool, true>{}) : go(integral_constant<int, 128>{}, integral_constant<bool, false>{});

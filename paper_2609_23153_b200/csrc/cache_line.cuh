@@ -1,0 +1,277 @@
+// The line: the key tiles of all items of a call, one behind the other, cut into equal stretches.
+//
+// An item is R query rows (row = token * G + head in its group) of one (sequence, key head); its tiles of TK keys run from
+// the first to the last key that any of its rows sees, at least one, so that somebody writes the rows of an empty sequence.
+// Stretch w is tiles [w * share, (w + 1) * share).  What a stretch holds of an item is a segment; an item that lies in one
+// stretch is finished there, the others leave partial results that combine_kernel adds up in the line's order.
+// Items stand in the order (sequence, key head, row tile).
+#pragma once
+
+#include "cache.h"
+
+namespace sparkattn {
+
+// The reference m of a row moves when a weight would pass 2^10 times the one that set it; weights are 2^kBase at the reference, so
+// that fp16 holds them (2^15 < 65504) and loses only what lies 2^-29 below it.
+constexpr float kBase = 5.0f, kLazy = 10.0f;
+
+struct CacheFwdParams {
+  BatchView batch;
+  Causal causal;
+  const __nv_bfloat16* q;
+  __nv_bfloat16* out;
+  int64_t q_stride_t, q_stride_h, out_stride_t, out_stride_h;
+  const float* k_scale;
+  const float* v_scale;
+  float* lse;
+  int H, Hk, G;
+  float scale_log2;
+  int box_rows, boxes;           // keys of one TMA box, boxes of a tile
+  int least;                     // tiles a stretch has at least
+  int workers;                   // stretches
+  int stages;
+  int32_t* status;
+  int32_t* prefix;               // [B + 2] first tile of every sequence, the total, tiles per stretch
+  float* part_ml;                // [2 workers][R][2] reference, sum
+  float* part_o;                 // [2 workers][R][d] unnormalised output
+};
+
+// cache_chunk.cu: items of 256 rows
+constexpr int kChunkRows = 256;
+int launch_cache_chunk(const sparkattn_cache_t& c, const sparkattn_batch_t& b, CacheFwdParams& p, const void* k_cache, const void* v_cache,
+                       cudaStream_t stream);
+
+// 16 keys of a tile, as the copying warp has looked them up
+struct GroupInfo {
+  float k;           // factor of the logits
+  float v_log2;      // log2 of the V scale
+  float v_inv;       // its inverse
+  int usable;        // somebody sees keys of it, and the page exists
+};
+
+template <int R, int TK>
+struct Line {
+  struct Item {
+    int first, tiles;            // key tiles, counted from the front of the sequence
+    int lo, hi;                  // keys that any of its rows sees
+  };
+  static __device__ __forceinline__ int row_tiles(const CacheFwdParams& p, const Sequence& s) { return (s.n * p.G + R - 1) / R; }
+  static __device__ __forceinline__ Item item_of(const CacheFwdParams& p, const Sequence& s, int rt) {
+    const int last_row = min((rt + 1) * R, s.n * p.G) - 1;
+    Item it;
+    it.lo = visible_keys(p.causal, s.first_pos() + rt * R / p.G, s.len).x;
+    it.hi = visible_keys(p.causal, s.first_pos() + last_row / p.G, s.len).y;
+    it.first = it.lo / TK;
+    it.tiles = max((it.hi + TK - 1) / TK - it.first, 1);
+    return it;
+  }
+  // tiles of the row tiles of one key head
+  static __device__ __forceinline__ int tiles_of(const CacheFwdParams& p, const Sequence& s) {
+    int sum = 0;
+    for (int rt = 0; rt < row_tiles(p, s); ++rt) sum += item_of(p, s, rt).tiles;
+    return sum;
+  }
+  // all threads: prefix[b] = tiles in front of sequence b, prefix[B] = all (shared memory)
+  static __device__ __forceinline__ void lay_out(const CacheFwdParams& p, int* prefix, int* s_warp) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    int carry = 0;
+    for (int base = 0; base < p.batch.B; base += blockDim.x) {
+      const int b = base + threadIdx.x;
+      const int mine = b < p.batch.B ? tiles_of(p, sequence_of(p.batch, b)) * p.Hk : 0;
+      int x = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (lane == 31) s_warp[warp] = x;
+      __syncthreads();
+      int before = carry, all = carry;
+      for (int w = 0; w < warps; ++w) {
+        if (w < warp) before += s_warp[w];
+        all += s_warp[w];
+      }
+      if (b < p.batch.B) prefix[b] = before + x - mine;
+      carry = all;
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) prefix[p.batch.B] = carry;
+    __syncthreads();
+  }
+  static __device__ __forceinline__ int share_of(const CacheFwdParams& p, int total) { return max((total + p.workers - 1) / p.workers, p.least); }
+
+  // A place in the line, and the walk along it.  Whole warps.
+  struct Place {
+    Sequence seq;
+    Item item;
+    int b, h, rt, row_tiles;
+    int at;                      // tiles of the item in front of the place
+  };
+  static __device__ __forceinline__ Place find(const CacheFwdParams& p, const int* prefix, int x) {
+    Place c;
+    int lo = 0, hi = p.batch.B;                   // prefix[lo] <= x; sequences without tiles have equal entries
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (prefix[mid] <= x) lo = mid; else hi = mid;
+    }
+    c.b = lo;
+    c.seq = sequence_of(p.batch, lo);
+    c.row_tiles = row_tiles(p, c.seq);
+    const int each = (prefix[lo + 1] - prefix[lo]) / p.Hk;
+    int in = x - prefix[lo];
+    c.h = in / each;
+    in -= c.h * each;
+    // the row tile: 32 of them at a time
+    const int lane = threadIdx.x & 31;
+    int rt0 = 0;
+    c.rt = 0;
+    c.at = in;
+    if (c.row_tiles > 1) {
+      for (;; rt0 += 32) {
+        const int mine = rt0 + lane < c.row_tiles ? item_of(p, c.seq, rt0 + lane).tiles : 0;
+        int sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += y;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, sum > in);
+        if (past != 0) {
+          const int l = __ffs(past) - 1;
+          c.rt = rt0 + l;
+          c.at = in - __shfl_sync(0xffffffffu, sum - mine, l);
+          break;
+        }
+        in -= __shfl_sync(0xffffffffu, sum, 31);
+        if (rt0 + 32 >= c.row_tiles) break;       // (never: in is smaller than the sum of all)
+      }
+    }
+    c.item = item_of(p, c.seq, c.rt);
+    return c;
+  }
+  // to the first tile of the next item
+  static __device__ __forceinline__ void next_item(const CacheFwdParams& p, Place& c) {
+    c.at = 0;
+    if (++c.rt == c.row_tiles) {
+      c.rt = 0;
+      if (++c.h == p.Hk) {
+        c.h = 0;
+        do ++c.b, c.seq = sequence_of(p.batch, c.b); while (c.seq.n == 0 && c.b < p.batch.B - 1);
+        c.row_tiles = row_tiles(p, c.seq);
+      }
+    }
+    c.item = item_of(p, c.seq, c.rt);
+  }
+};
+
+// A stretch of the line, taken segment by segment.
+template <int R, int TK>
+struct Stretch {
+  using L = Line<R, TK>;
+  typename L::Place c;
+  int x, end;
+  int t0, t1;                    // the segment's key tiles, counted from the front of the sequence
+  int row0, rows;                // its rows
+  bool whole, first;             // the item lies in this stretch; the stretch's first segment
+  __device__ __forceinline__ void begin(const CacheFwdParams& p, const int* prefix, int from, int to) {
+    x = from;
+    end = to;
+    c = L::find(p, prefix, from);
+    first = true;
+    cut(p);
+  }
+  __device__ __forceinline__ void cut(const CacheFwdParams& p) {
+    const int until = min(c.item.tiles, c.at + end - x);
+    t0 = c.item.first + c.at;
+    t1 = c.item.first + until;
+    whole = c.at == 0 && until == c.item.tiles;
+    row0 = c.rt * R;
+    rows = min(R, c.seq.n * p.G - row0);
+    x += until - c.at;
+  }
+  // false behind the last segment
+  __device__ __forceinline__ bool next(const CacheFwdParams& p) {
+    if (x >= end) return false;
+    L::next_item(p, c);
+    first = false;
+    cut(p);
+    return true;
+  }
+};
+
+// What the lanes of the copying warp look up for a group of 16 keys each: the page and the scales.
+template <bool FP8>
+__device__ __forceinline__ int look_up_group(const CacheFwdParams& p, const int32_t* table, int h, int key, int lo, int hi, GroupInfo& info) {
+  info = {1.0f, 0.0f, 1.0f, 0};
+  int page = -1;
+  if (key < hi && key + 16 > lo) page = table[key >> p.batch.page_shift];
+  if ((uint32_t)page >= (uint32_t)p.batch.pages) return -1;
+  info.usable = 1;
+  if constexpr (FP8) {
+    info.k = p.k_scale[(int64_t)page * p.Hk + h];
+    const float v = fmaxf(p.v_scale[(int64_t)page * p.Hk + h], 5.4e-20f);      // 2^-64: a scale of zero stays finite
+    info.v_log2 = log2f(v);
+    info.v_inv = 1.0f / v;
+  }
+  return page;
+}
+
+// the status of a call, and the line for the combining kernel: the first CTA's work
+template <int R, int TK>
+__device__ __forceinline__ void check_and_publish(const CacheFwdParams& p, const int* prefix, int share, int* s_bad) {
+  for (int b = threadIdx.x; b <= p.batch.B; b += blockDim.x) p.prefix[b] = prefix[b];
+  if (threadIdx.x == 0) p.prefix[p.batch.B + 1] = share;
+  check_batch(p.batch, s_bad, [&](const Sequence& s) {
+    if (s.n == 0) return make_int2(0, 0);
+    const int lo = visible_keys(p.causal, s.first_pos(), s.len).x, hi = visible_keys(p.causal, s.len - 1, s.len).y;
+    return make_int2(lo >> p.batch.page_shift, (hi + (1 << p.batch.page_shift) - 1) >> p.batch.page_shift);
+  });
+  leave_status(p.status, s_bad);
+}
+
+// Adds up what several stretches have left of an item, in the order of the line.  CTA w looks at the border in front of
+// stretch w + 1 and does the item if that is the first border inside it; gridDim.y CTAs share its rows, a warp each.
+template <int D, int R, int TK>
+__global__ void __launch_bounds__(128)
+combine_kernel(const __grid_constant__ CacheFwdParams p) {
+  using L = Line<R, TK>;
+  constexpr int kVec = D / 32;
+  pdl_wait();
+  const int total = p.prefix[p.batch.B], share = p.prefix[p.batch.B + 1];
+  const long long border = (long long)(blockIdx.x + 1) * share;
+  if (border >= total) return;
+  const typename L::Place c = L::find(p, p.prefix, (int)border);
+  const int start = (int)border - c.at;
+  if (c.at == 0 || start < (int)border - share) return;
+  const int w0 = start / share, w1 = (start + c.item.tiles - 1) / share;
+  const int lane = threadIdx.x & 31, rows = min(R, c.seq.n * p.G - c.rt * R);
+  for (int r = blockIdx.y * 4 + (threadIdx.x >> 5); r < rows; r += 4 * gridDim.y) {
+    auto slot_of = [&](int w) { return 2 * w + (start <= w * share ? 0 : 1); };
+    float top = -INFINITY;
+    for (int w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, p.part_ml[((int64_t)slot_of(w) * R + r) * 2]);
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    float sum = 0.0f, acc[kVec] = {};
+#pragma unroll 4
+    for (int w = w0; w <= w1; ++w) {
+      const int64_t at = (int64_t)slot_of(w) * R + r;
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
+      const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
+      sum = fmaf(ml.y, f, sum);
+      const float* src = p.part_o + at * D + lane * kVec;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) acc[j] = fmaf(src[j], f, acc[j]);
+    }
+    const int row = c.rt * R + r, token = c.seq.start + row / p.G, head = c.h * p.G + row % p.G;
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + lane * kVec);
+#pragma unroll
+    for (int j = 0; j < kVec / 2; ++j) {
+      const __nv_bfloat162 v = __floats2bfloat162_rn(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+      dst[j] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    if (p.lse && lane == 0) p.lse[(int64_t)token * p.H + head] = sum == 0.0f ? -INFINITY : (top - kBase + log2f(sum)) * 0.6931471805599453f;
+  }
+}
+
+}  // namespace sparkattn

@@ -351,18 +351,11 @@ __device__ __forceinline__ void pipe_tma_store_4d(const void* tmap, const void* 
       : "memory");
 }
 
-// One thread of a converged warp; and a value that is the same in all its threads, told to the compiler as such.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t one;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-  return one != 0;
-}
 // a truth value that is known when it is compiled
 template <bool V>
 struct Const {
   __device__ constexpr operator bool() const { return V; }
 };
-__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // PAIR: 64-token blocks; a work item is a pair of query blocks, a tile two key blocks (see pair_list).
 // GATE (bf16, 128-token blocks, no window): the closing warpgroup of an item also computes the low-rank branch

@@ -125,6 +125,13 @@ CASES = [
     ([77, 500], [20, 300], 8, 8, 128, 32, True, 1, 33),
     ([5000], [1], 8, 1, 128, 128, True, 1, 0),
     ([40000, 100], [1, 1], 2, 2, 128, 64, True, 1, 0),
+    ([600, 129, 1], [129, 128, 1], 1, 1, 128, 64, True, 1, 0),
+    ([2000, 0, 515], [300, 4, 257], 8, 2, 128, 16, True, 1, 0),
+    ([2000, 1600, 40], [40, 90, 17], 16, 1, 64, 128, True, 0, 0),
+    ([1300, 900], [700, 300], 4, 4, 128, 128, True, 100, 3),
+    ([1300, 900], [700, 300], 5, 5, 128, 32, False, 1, 256),
+    ([7000], [40], 3, 1, 64, 64, False, 1, 0),
+    ([9000, 8], [33, 8], 40, 8, 128, 64, True, 1, 0),
     ([3, 130, 513], [7, 130, 1], 7, 7, 128, 64, True, 1, 0),         # more new tokens than the first sequence holds
 ]
 
@@ -142,7 +149,7 @@ def test_attention_over_pages(case, general):
     kv_len, q_start = batch_of(lens, news)
     q = (1.5 * torch.randn((sum(news), H, d), generator=gen, device=DEV)).bfloat16()
     over = any(n > length for length, n in zip(lens, news))
-    ws = torch.full((1 << 24,), 0xA5, dtype=torch.uint8, device=DEV)
+    ws = torch.full((1 << 26,), 0xA5, dtype=torch.uint8, device=DEV)
     out, lse = sa.cache_fwd(q, cache, table, kv_len, q_start=q_start, max_new=max(news), frame_tokens=frame, window=window,
                             return_lse=True, workspace=ws)
     assert sa.read_status(ws) == (sa.E_BAD_INDEX if over else sa.OK)
