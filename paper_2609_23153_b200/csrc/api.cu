@@ -567,7 +567,7 @@ int check_rotary(const sparkattn_rotary_t* r, int d) {
   if (r->struct_size != sizeof(sparkattn_rotary_t) || r->version != SPARKATTN_VERSION) return SPARKATTN_E_INVALID_ARG;
   if (!r->cos || !r->sin || r->rows < 1 || (r->interleaved != 0 && r->interleaved != 1)) return SPARKATTN_E_INVALID_ARG;
   if (r->axes < 1 || r->axes > 4 || (r->positions == nullptr && r->axes != 1)) return SPARKATTN_E_INVALID_ARG;
-  if (r->rot < 16 || r->rot > d || r->rot % 16) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  if (r->rot < 16 || r->rot > d || r->rot % 16 || (long long)r->rows * (r->rot / 2) > 0x7fffffffLL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   return !aligned16(r->cos) || !aligned16(r->sin) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
 }
 // the pools, the table and the scales

@@ -3,15 +3,18 @@
 //
 // The rotation is a 2 x 2 product per channel pair; the quantisation of a page needs the largest |x| of its new tokens
 // before the first code, so a page's tokens of one head stay in registers between the two: HBM sees every row once.
-// A unit is the new tokens of one (sequence, page, head) of K or of V; 2 threads per token row (at least a warp) hold it.
-// The queries, which nothing is reduced over, go row by row: a thread keeps its channels' phases for all heads of a token.
+// A unit is the new tokens of one (sequence, page) and some of its lines; a line is one head of K, of V or of the queries.  Four threads
+// per token (at least a warp) work on a unit.  The tokens' cosines and sines, which all heads share, go to shared memory
+// once; then the lines are taken one after the other, the next one's rows on their way (asynchronous copies, each thread's own)
+// while this one is encoded.
 #include <cuda_fp8.h>
 
+#include <algorithm>
+
 #include "cache.h"
+#include "tmap.h"
 
 namespace sparkattn {
-
-constexpr int kAppendThreads = 256;
 
 struct RowsView {
   __nv_bfloat16* data;
@@ -35,118 +38,100 @@ struct AppendParams {
   int64_t stride_page, stride_h, stride_n;
   int H, Hk;
   int pages_each;                // pages of a sequence that max_new tokens can reach
-  long long units;
-  int unit_ctas;                 // CTAs 1 .. unit_ctas work on units, those behind them on query rows
-  int q_tokens;                  // tokens per query CTA
+  FastDiv by_pages_each, by_groups;
+  int lines;                     // of a (sequence, page): K and V of every key head, then the queries
+  int groups;                    // units that share them: unit g takes lines g, g + groups, ...
+  int units;
   int32_t* status;
 };
 
-// eight fp32 channels
+// eight fp32 channels, in pairs for the packed instructions
 struct Chunk {
-  float x[8];
+  uint64_t x[4];
 };
-__device__ __forceinline__ Chunk widen(uint4 v) {
-  const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
-  Chunk c;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float2 f = __bfloat1622float2(p[j]);
-    c.x[2 * j] = f.x;
-    c.x[2 * j + 1] = f.y;
-  }
-  return c;
+__device__ __forceinline__ uint64_t widen2(uint32_t w) { return pack_f32x2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t narrow2(uint64_t x) {
+  const float2 f = unpack_f32x2(x);
+  const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ uint4 narrow(const Chunk& c) {
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(c.x[2 * j], c.x[2 * j + 1]);
-    w[j] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
+__device__ __forceinline__ Chunk widen(uint4 v) { return {{widen2(v.x), widen2(v.y), widen2(v.z), widen2(v.w)}}; }
+__device__ __forceinline__ uint4 narrow(const Chunk& c) { return make_uint4(narrow2(c.x[0]), narrow2(c.x[1]), narrow2(c.x[2]), narrow2(c.x[3])); }
 
-// The phases of the channels 8c .. 8c+7 of a token.  Interleaved: cosines and sines of its four pairs.  Halves: of
-// the eight pairs of which the chunk holds one side.
+// The phases of the channels 8c .. 8c+7 of a token: a channel becomes x c + y s, y the other side of its pair, and s negative for a
+// first side (a - b and a + (-b) round alike).
 struct Phases {
-  float c[8], s[8];
-  bool on;
+  uint64_t c[4], s[4];
 };
-__device__ __forceinline__ Phases phases_of(const RotaryView& r, int t, int pos, int chunk) {
-  Phases p;
-  p.on = chunk * 8 < r.rot;
-  if (!p.on) return p;
-  const int pairs = r.rot / 2;
-  const int n = r.interleaved ? 4 : 8;
-  const int m0 = r.interleaved ? chunk * 4 : (chunk * 8) % pairs;
-  if (r.axis == nullptr) {
-    const int at = r.positions ? r.positions[(int64_t)t * r.axes] : pos;
-    p.on = (uint32_t)at < (uint32_t)r.rows;
-    if (!p.on) return p;
-    const float4* c = reinterpret_cast<const float4*>(r.cos + (int64_t)at * pairs + m0);
-    const float4* s = reinterpret_cast<const float4*>(r.sin + (int64_t)at * pairs + m0);
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (4 * j < n) {
-        const float4 a = c[j], b = s[j];
-        p.c[4 * j] = a.x; p.c[4 * j + 1] = a.y; p.c[4 * j + 2] = a.z; p.c[4 * j + 3] = a.w;
-        p.s[4 * j] = b.x; p.s[4 * j + 1] = b.y; p.s[4 * j + 2] = b.z; p.s[4 * j + 3] = b.w;
+// cosines and sines of a unit's tokens as [rows][pairs], from the tables; a pair outside them is turned by nothing
+__device__ __forceinline__ void gather_phases(const RotaryView& r, int rows, int t0, int pos0, float* s_cos, float* s_sin, int tid, int threads) {
+  const int quads = r.rot / 8;                             // of four pairs
+  for (int i = tid; i < rows * quads; i += threads) {
+    const int row = i / quads, m = (i - row * quads) * 4;
+    const int32_t* at = r.positions + (int64_t)(t0 + row) * r.axes;
+    float4 c = make_float4(1.0f, 1.0f, 1.0f, 1.0f), s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (r.axis == nullptr) {
+      const uint32_t e = r.positions ? at[0] : pos0 + row;
+      if (e < (uint32_t)r.rows) {
+        c = *reinterpret_cast<const float4*>(r.cos + (e * (r.rot / 2) + m));
+        s = *reinterpret_cast<const float4*>(r.sin + (e * (r.rot / 2) + m));
       }
-    return p;
-  }
-  // a pair whose position lies outside the table is left as it is: turned by nothing
+    } else {
+      float* cc = &c.x;
+      float* ss = &s.x;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    p.c[j] = 1.0f;
-    p.s[j] = 0.0f;
-    if (j < n) {
-      const int ax = r.axis[m0 + j];
-      const int at = (uint32_t)ax >= (uint32_t)r.axes ? -1 : r.positions ? r.positions[(int64_t)t * r.axes + ax] : pos;
-      if ((uint32_t)at < (uint32_t)r.rows) {
-        p.c[j] = r.cos[(int64_t)at * pairs + m0 + j];
-        p.s[j] = r.sin[(int64_t)at * pairs + m0 + j];
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t ax = r.axis[m + j];
+        const uint32_t e = ax >= (uint32_t)r.axes ? 0xffffffffu : r.positions ? (uint32_t)at[ax] : (uint32_t)(pos0 + row);
+        if (e < (uint32_t)r.rows) {
+          cc[j] = r.cos[e * (r.rot / 2) + m + j];
+          ss[j] = r.sin[e * (r.rot / 2) + m + j];
+        }
       }
     }
+    *reinterpret_cast<float4*>(s_cos + row * (r.rot / 2) + m) = c;
+    *reinterpret_cast<float4*>(s_sin + row * (r.rot / 2) + m) = s;
+  }
+}
+// a chunk's share of a row of them
+__device__ __forceinline__ Phases phases_of(const RotaryView& r, const float* c, const float* s, bool second) {
+  Phases p;
+  const float4 c0 = *reinterpret_cast<const float4*>(c), s0 = *reinterpret_cast<const float4*>(s);
+  if (r.interleaved) {
+    p.c[0] = pack_f32x2(c0.x, c0.x); p.c[1] = pack_f32x2(c0.y, c0.y); p.c[2] = pack_f32x2(c0.z, c0.z); p.c[3] = pack_f32x2(c0.w, c0.w);
+    p.s[0] = pack_f32x2(-s0.x, s0.x); p.s[1] = pack_f32x2(-s0.y, s0.y); p.s[2] = pack_f32x2(-s0.z, s0.z); p.s[3] = pack_f32x2(-s0.w, s0.w);
+  } else {
+    const float4 c1 = *reinterpret_cast<const float4*>(c + 4), s1 = *reinterpret_cast<const float4*>(s + 4);
+    const float f = second ? 1.0f : -1.0f;
+    p.c[0] = pack_f32x2(c0.x, c0.y); p.c[1] = pack_f32x2(c0.z, c0.w); p.c[2] = pack_f32x2(c1.x, c1.y); p.c[3] = pack_f32x2(c1.z, c1.w);
+    const uint64_t f2 = pack_f32x2(f, f);
+    p.s[0] = fmul2(pack_f32x2(s0.x, s0.y), f2); p.s[1] = fmul2(pack_f32x2(s0.z, s0.w), f2);
+    p.s[2] = fmul2(pack_f32x2(s1.x, s1.y), f2); p.s[3] = fmul2(pack_f32x2(s1.z, s1.w), f2);
   }
   return p;
 }
-// The chunk turned, given the raw chunk that holds the other side of its pairs (halves; its own where interleaved).  Each product
-// and sum is rounded by itself, so that a cache filled by any route holds the same bits.
-__device__ __forceinline__ Chunk turn(const RotaryView& r, const Phases& p, int chunk, const Chunk& x, const Chunk& other) {
-  Chunk y = x;
-  if (!p.on) return y;
-  if (r.interleaved) {
+// The chunk turned, given the other sides of its channels' pairs.  Each product and sum is rounded by itself, so that a cache
+// filled by any route holds the same bits.
+// (The sum is not a packed instruction: behind packed products it was fused with one of them, which rounds once.)
+__device__ __forceinline__ uint64_t turn2(uint64_t c, uint64_t s, uint64_t x, uint64_t y) {
+  const float2 a = unpack_f32x2(fmul2(x, c)), b = unpack_f32x2(fmul2(y, s));
+  return pack_f32x2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
+}
+__device__ __forceinline__ Chunk turn(const Phases& p, uint4 x, uint4 y) {
+  return {{turn2(p.c[0], p.s[0], widen2(x.x), widen2(y.x)), turn2(p.c[1], p.s[1], widen2(x.y), widen2(y.y)),
+           turn2(p.c[2], p.s[2], widen2(x.z), widen2(y.z)), turn2(p.c[3], p.s[3], widen2(x.w), widen2(y.w))}};
+}
+// largest |x| as bits: of all values, or of the finite ones
+template <bool FINITE>
+__device__ __forceinline__ uint32_t largest_bits(const Chunk& c, uint32_t top) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float a = x.x[2 * j], b = x.x[2 * j + 1];
-      y.x[2 * j] = __fsub_rn(__fmul_rn(a, p.c[j]), __fmul_rn(b, p.s[j]));
-      y.x[2 * j + 1] = __fadd_rn(__fmul_rn(a, p.s[j]), __fmul_rn(b, p.c[j]));
-    }
-  } else if (chunk * 8 < r.rot / 2) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y.x[j] = __fsub_rn(__fmul_rn(x.x[j], p.c[j]), __fmul_rn(other.x[j], p.s[j]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y.x[j] = __fadd_rn(__fmul_rn(other.x[j], p.s[j]), __fmul_rn(x.x[j], p.c[j]));
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = unpack_f32x2(c.x[j]);
+    uint32_t a = __float_as_uint(f.x) & 0x7fffffffu, b = __float_as_uint(f.y) & 0x7fffffffu;
+    if constexpr (FINITE) { a = a < 0x7f800000u ? a : 0u; b = b < 0x7f800000u ? b : 0u; }
+    top = max(top, max(a, b));
   }
-  return y;
-}
-// the lanes of a row hold its chunks in order: the lane with the other side of this lane's pairs
-template <int D>
-__device__ __forceinline__ uint4 other_side(const RotaryView& r, int chunk, uint4 v) {
-  const int half = r.rot / 16;                             // chunks per side
-  const int partner = chunk < half ? chunk + half : chunk < 2 * half ? chunk - half : chunk;
-  const int src = (threadIdx.x & 31 & ~(D / 8 - 1)) + partner;
-  v.x = __shfl_sync(0xffffffffu, v.x, src);
-  v.y = __shfl_sync(0xffffffffu, v.y, src);
-  v.z = __shfl_sync(0xffffffffu, v.z, src);
-  v.w = __shfl_sync(0xffffffffu, v.w, src);
-  return v;
-}
-
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
+  return top;
 }
 // smallest power of two s with amax <= 448 s (448 = 1.75 * 2^8), from the bits of amax >= 1e-12
 __device__ __forceinline__ float power_scale(uint32_t amax_bits) {
@@ -154,10 +139,10 @@ __device__ __forceinline__ float power_scale(uint32_t amax_bits) {
   return __uint_as_float(((u >> 23) - 8u + ((u & 0x7fffffu) > 0x600000u ? 1u : 0u)) << 23);
 }
 __device__ __forceinline__ uint2 encode(const Chunk& c, float inv) {
+  const uint64_t by = pack_f32x2(inv, inv);
   uint32_t w[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    w[j] = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(c.x[2 * j], inv), __fmul_rn(c.x[2 * j + 1], inv)), __NV_SATFINITE, __NV_E4M3);
+  for (int j = 0; j < 4; ++j) w[j] = __nv_cvt_float2_to_fp8x2(unpack_f32x2(fmul2(c.x[j], by)), __NV_SATFINITE, __NV_E4M3);
   return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 __device__ __forceinline__ Chunk decode(uint2 codes) {
@@ -166,157 +151,175 @@ __device__ __forceinline__ Chunk decode(uint2 codes) {
   for (int j = 0; j < 4; ++j) {
     const uint32_t pair = (j < 2 ? codes.x : codes.y) >> (16 * (j & 1));
     const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
-    c.x[2 * j] = f.x;
-    c.x[2 * j + 1] = f.y;
+    c.x[j] = pack_f32x2(f.x, f.y);
   }
   return c;
 }
 
-// U threads hold the up to ROWS new rows of a unit, 16 bytes of a row each at a time.
-template <int D, bool FP8, int ROWS>
-__device__ __forceinline__ void append_units(const AppendParams& p, uint32_t* s_max) {
-  constexpr int kLanes = D / 8;                                    // threads of a row
-  constexpr int U = ROWS * 2 < 32 ? 32 : ROWS * 2;
-  constexpr int kRowsAtOnce = U / kLanes;
-  constexpr int C = (ROWS + kRowsAtOnce - 1) / kRowsAtOnce;
-  constexpr int kElt = FP8 ? 1 : 2;
-  const int group = threadIdx.x / U, tid = threadIdx.x % U;
-  const long long unit = (long long)(blockIdx.x - 1) * (kAppendThreads / U) + group;
-  const int chunk = tid % kLanes, row0 = tid / kLanes;
-  const bool is_v = unit & 1;
-  const long long rest = unit >> 1;
-  const int h = (int)(rest % p.Hk);
-  const int bj = (int)(rest / p.Hk);
-  const int b = bj / p.pages_each;
-  const int P = 1 << p.batch.page_shift;
-  int rows = 0, held = 0, pos0 = 0, t0 = 0, page = -1;
-  if (unit < p.units) {
-    const Sequence s = sequence_of(p.batch, b);
-    const int first = max(s.first_pos(), 0);
-    const int number = (first >> p.batch.page_shift) + bj % p.pages_each;
-    pos0 = max(number << p.batch.page_shift, first);
-    rows = min((number + 1) << p.batch.page_shift, s.len) - pos0;
-    if (rows > 0 && number < p.batch.max_pages) {
-      held = pos0 & (P - 1);
-      t0 = s.start + pos0 - s.first_pos();
-      page = p.batch.page_table[(int64_t)b * p.batch.max_pages + number];
-    }
-    if ((uint32_t)page >= (uint32_t)p.batch.pages) rows = 0;
-  }
-  const RowsView& from = is_v ? p.v : p.k;
-  const __nv_bfloat16* src = from.data + h * from.stride_h + chunk * 8;
-  unsigned char* dst = (is_v ? p.v_cache : p.k_cache) + ((int64_t)page * p.stride_page + h * p.stride_h + chunk * 8) * kElt;
-  uint4 raw[C];
-#pragma unroll
-  for (int i = 0; i < C; ++i) {
-    const int r = row0 + i * kRowsAtOnce;
-    raw[i] = r < rows ? *reinterpret_cast<const uint4*>(src + (int64_t)(t0 + r) * from.stride_t) : make_uint4(0u, 0u, 0u, 0u);
-  }
-  float* scale_at = FP8 && rows > 0 ? (is_v ? p.v_scale : p.k_scale) + (int64_t)page * p.Hk + h : nullptr;
-  const float old = FP8 && rows > 0 && held > 0 ? *scale_at : 0.0f;
-  const bool rotate = !is_v && p.rotary.rot > 0;
-  Chunk x[C];
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < C; ++i) {
-    const int r = row0 + i * kRowsAtOnce;
-    x[i] = widen(raw[i]);
-    if (__any_sync(0xffffffffu, rotate)) {
-      const uint4 far = other_side<D>(p.rotary, chunk, raw[i]);
-      if (rotate && r < rows) x[i] = turn(p.rotary, phases_of(p.rotary, t0 + r, pos0 + r, chunk), chunk, x[i], widen(far));
-    }
-    if constexpr (FP8) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) amax = max(amax, finite_bits(x[i].x[j]));
-    }
-  }
-  if constexpr (!FP8) {
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      const int r = row0 + i * kRowsAtOnce;
-      if (r < rows) *reinterpret_cast<uint4*>(dst + (int64_t)(held + r) * p.stride_n * kElt) = narrow(x[i]);
-    }
-  } else {
-    amax = __reduce_max_sync(0xffffffffu, amax);
-    if constexpr (U > 32) {
-      if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = amax;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < U / 32; ++w) amax = max(amax, s_max[group * (U / 32) + w]);
-    }
-    float scale = power_scale(amax);
-    if (held > 0 && old >= scale) scale = old;
-    const float inv = 1.0f / scale;
-    if (rows > 0 && held > 0 && scale > old) {
-      const float again = __fmul_rn(old, inv);
-      for (int r = row0; r < held; r += kRowsAtOnce) {
-        uint2* at = reinterpret_cast<uint2*>(dst + (int64_t)r * p.stride_n);
-        *at = encode(decode(*at), again);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      const int r = row0 + i * kRowsAtOnce;
-      if (r < rows) *reinterpret_cast<uint2*>(dst + (int64_t)(held + r) * p.stride_n) = encode(x[i], inv);
-    }
-    // (every thread of a larger unit has read the old scale: the barrier above is behind that read)
-    __syncwarp();
-    if (rows > 0 && tid == 0) *scale_at = scale;
-  }
+// The new tokens of a (sequence, page).
+struct Part {
+  int page, held;              // the page, -1: nothing to do; tokens there before
+  int rows, t0, pos0;          // new tokens; row of the call and position of the first
+};
+__device__ __forceinline__ Part part_of(const AppendParams& p, int bj) {
+  Part u{-1, 0, 0, 0, 0};
+  const int b = fast_div(bj, p.by_pages_each);
+  const Sequence s = sequence_of(p.batch, b);
+  const int first = max(s.first_pos(), 0), number = (first >> p.batch.page_shift) + bj - b * p.pages_each;
+  u.pos0 = max(number << p.batch.page_shift, first);
+  u.rows = min((number + 1) << p.batch.page_shift, s.len) - u.pos0;
+  if (u.rows <= 0 || number >= p.batch.max_pages) { u.rows = 0; return u; }
+  u.held = u.pos0 & ((1 << p.batch.page_shift) - 1);
+  u.t0 = s.start + u.pos0 - s.first_pos();
+  u.page = p.batch.page_table[(int64_t)b * p.batch.max_pages + number];
+  if ((uint32_t)u.page >= (uint32_t)p.batch.pages) u.page = -1;
+  return u;
 }
 
-template <int D>
-__device__ __forceinline__ void rotate_queries(const AppendParams& p) {
-  constexpr int kLanes = D / 8, kHeadsAtOnce = kAppendThreads / kLanes, kAhead = 4;
-  const int chunk = threadIdx.x % kLanes, h0 = threadIdx.x / kLanes;
-  const int first = (blockIdx.x - 1 - p.unit_ctas) * p.q_tokens;
-  for (int t = first; t < min(first + p.q_tokens, p.batch.T); ++t) {
-    // the token's sequence, for its position there
-    int pos = 0;
-    bool owned = true;
-    if (p.rotary.positions == nullptr) {
-      int b = 0;
-      if (p.batch.q_start == nullptr) {
-        b = t / (p.batch.T / p.batch.B);
-      } else {
-        int hi = p.batch.B;                               // the last sequence that starts at or before t
-        while (hi - b > 1) {
-          const int mid = (b + hi) >> 1;
-          if (p.batch.q_start[mid] <= t) b = mid; else hi = mid;
+template <int D, int ROWS>
+struct UnitShape {
+  static constexpr int kLanes = D / 8;                             // threads of a row
+  static constexpr int U = ROWS * 4 < 32 ? 32 : ROWS * 4;          // threads of a unit
+  static constexpr int kThreads = U < 256 ? 256 : U;               // of a CTA
+  static constexpr int kRowsAtOnce = U / kLanes;
+  static constexpr int C = (ROWS + kRowsAtOnce - 1) / kRowsAtOnce;
+  // rows on their way, then cosines and sines
+  static constexpr int kRowBytes = kThreads * C * 16;
+  static size_t smem(int rot) { return kRowBytes + (size_t)(kThreads / U) * ROWS * rot * sizeof(float); }
+};
+
+// Lines first, first + step, ... of a unit: the threads hold its up to ROWS new rows of one of them, 16 bytes of a row each at a time.
+template <int D, bool FP8, int ROWS>
+__device__ __forceinline__ void append_lines(const AppendParams& p, const Part& u, int first, int step, int group, uint32_t* s_max,
+                                             const float* s_cos, const float* s_sin) {
+  using S = UnitShape<D, ROWS>;
+  constexpr int U = S::U, C = S::C, kElt = FP8 ? 1 : 2;
+  const int tid = threadIdx.x % U, chunk = tid % S::kLanes, row0 = tid / S::kLanes;
+  const RotaryView& rot = p.rotary;
+  const int pairs = rot.rot / 2, half = rot.rot / 16;            // chunks per side
+  const bool on = chunk * 8 < rot.rot, second = chunk >= half;
+  // where this chunk's pairs lie, and (halves) the lane with their other sides: the lanes of a row hold its chunks in order
+  const int m0 = rot.interleaved ? chunk * 4 : (second ? chunk - half : chunk) * 8;
+  const int partner = (threadIdx.x & 31 & ~(S::kLanes - 1)) + (!on ? chunk : second ? chunk - half : chunk + half);
+  auto other_side = [&](uint4 v) {
+    if (rot.interleaved) return make_uint4(__byte_perm(v.x, 0, 0x1032), __byte_perm(v.y, 0, 0x1032), __byte_perm(v.z, 0, 0x1032), __byte_perm(v.w, 0, 0x1032));
+    v.x = __shfl_sync(0xffffffffu, v.x, partner);
+    v.y = __shfl_sync(0xffffffffu, v.y, partner);
+    v.z = __shfl_sync(0xffffffffu, v.z, partner);
+    v.w = __shfl_sync(0xffffffffu, v.w, partner);
+    return v;
+  };
+  extern __shared__ __align__(16) unsigned char s_raw[];
+  const uint32_t mine = smem_u32(s_raw) + threadIdx.x * 16;      // the thread's places, kThreads * 16 bytes apart
+  float old = 0.0f;                                              // E4M3: the scale of the line's page, if it held tokens
+  auto scale_of = [&](int n) { return (n < p.Hk ? p.k_scale + n : p.v_scale + n - p.Hk) + (int64_t)u.page * p.Hk; };
+  auto fetch = [&](int n) {
+    const bool key = n < p.Hk, query = n >= 2 * p.Hk;
+    const RowsView& from = key ? p.k : query ? p.q : p.v;
+    const int h = key ? n : query ? n - 2 * p.Hk : n - p.Hk;
+    const int rows = query || u.page >= 0 ? u.rows : 0;
+    const __nv_bfloat16* src = from.data + h * from.stride_h + (int64_t)(u.t0 + row0) * from.stride_t + chunk * 8;
+    const int64_t by = S::kRowsAtOnce * from.stride_t;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      if (row0 + i * S::kRowsAtOnce < rows) cp_async16(mine + i * S::kThreads * 16, src);
+      src += by;
+    }
+    cp_async_commit();
+    if constexpr (FP8) old = !query && rows > 0 && u.held > 0 ? *scale_of(n) : 0.0f;
+  };
+  fetch(first);
+  int turn_of = 0;                                               // which half of s_max this line takes
+#pragma unroll 1
+  for (int n = first; n < p.lines; n += step) {
+    const bool query = n >= 2 * p.Hk, rotate = (n < p.Hk || query) && rot.rot > 0;
+    const int h = n < p.Hk ? n : query ? n - 2 * p.Hk : n - p.Hk;
+    const int rows = query || u.page >= 0 ? u.rows : 0;
+    uint4 raw[C];
+    cp_async_wait<0>();
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      raw[i] = row0 + i * S::kRowsAtOnce < rows ? *reinterpret_cast<const uint4*>(s_raw + (threadIdx.x + i * S::kThreads) * 16) : make_uint4(0u, 0u, 0u, 0u);
+    const float before = old;
+    if (n + step < p.lines) fetch(n + step);
+    if (!FP8 || query) {
+      // bf16 to bf16
+      unsigned char* at = query ? reinterpret_cast<unsigned char*>(p.q_out.data + h * p.q_out.stride_h + (int64_t)(u.t0 + row0) * p.q_out.stride_t + chunk * 8)
+                                : (n < p.Hk ? p.k_cache : p.v_cache) + ((int64_t)u.page * p.stride_page + h * p.stride_h + (int64_t)(u.held + row0) * p.stride_n + chunk * 8) * 2;
+      const int64_t by = 2 * S::kRowsAtOnce * (query ? p.q_out.stride_t : p.stride_n);
+      uint4 y[C];
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        y[i] = raw[i];
+        if (rotate) {
+          const int r = row0 + i * S::kRowsAtOnce;
+          const uint4 far = other_side(raw[i]);
+          if (on && r < rows) y[i] = narrow(turn(phases_of(rot, s_cos + r * pairs + m0, s_sin + r * pairs + m0, second), raw[i], far));
         }
       }
-      const Sequence s = sequence_of(p.batch, b);
-      owned = t >= s.start && t < s.start + s.n;
-      pos = s.first_pos() + t - s.start;
-    }
-    Phases ph = phases_of(p.rotary, t, pos, chunk);
-    if (!owned) ph.on = false;
-    const __nv_bfloat16* src = p.q.data + (int64_t)t * p.q.stride_t + chunk * 8;
-    __nv_bfloat16* dst = p.q_out.data + (int64_t)t * p.q_out.stride_t + chunk * 8;
-    for (int base = 0; base < p.H; base += kHeadsAtOnce * kAhead) {
-      uint4 raw[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int h = base + h0 + i * kHeadsAtOnce;
-        if (h < p.H) raw[i] = *reinterpret_cast<const uint4*>(src + h * p.q.stride_h);
+      for (int i = 0; i < C; ++i) {
+        if (row0 + i * S::kRowsAtOnce < rows) *reinterpret_cast<uint4*>(at) = y[i];
+        at += by;
       }
+    } else {
+      unsigned char* page = (n < p.Hk ? p.k_cache : p.v_cache) + (int64_t)u.page * p.stride_page + h * p.stride_h + chunk * 8;
+      Chunk x[C];
+      uint32_t amax = 0;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int h = base + h0 + i * kHeadsAtOnce;
-        if (base + i * kHeadsAtOnce >= p.H) break;
-        if (h >= p.H) raw[i] = make_uint4(0u, 0u, 0u, 0u);
-        const Chunk far = widen(other_side<D>(p.rotary, chunk, raw[i]));
-        const uint4 y = narrow(turn(p.rotary, ph, chunk, widen(raw[i]), far));
-        if (h < p.H) *reinterpret_cast<uint4*>(dst + h * p.q_out.stride_h) = y;
+      for (int i = 0; i < C; ++i) {
+        x[i] = widen(raw[i]);
+        if (rotate) {
+          const int r = row0 + i * S::kRowsAtOnce;
+          const uint4 far = other_side(raw[i]);
+          if (on && r < rows) x[i] = turn(phases_of(rot, s_cos + r * pairs + m0, s_sin + r * pairs + m0, second), raw[i], far);
+        }
+        amax = largest_bits<false>(x[i], amax);
       }
+      float* scale_at = scale_of(n);
+      amax = __reduce_max_sync(0xffffffffu, amax);
+      if (amax >= 0x7f800000u) {                                 // infinities or NaN among them: the finite ones count
+        amax = 0;
+#pragma unroll
+        for (int i = 0; i < C; ++i) amax = largest_bits<true>(x[i], amax);
+        amax = __reduce_max_sync(0xffffffffu, amax);
+      }
+      if constexpr (U > 32) {
+        uint32_t* s = s_max + turn_of * (S::kThreads / 32);
+        turn_of ^= 1;
+        if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = amax;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(U) : "memory");
+        amax = __reduce_max_sync(0xffffffffu, s[group * (U / 32) + (threadIdx.x & 31) % (U / 32)]);
+      }
+      float scale = power_scale(amax);
+      if (u.held > 0 && before >= scale) scale = before;
+      const float inv = 1.0f / scale;
+      if (rows > 0 && u.held > 0 && scale > before) {
+        const float again = __fmul_rn(before, inv);
+        for (int r = row0; r < u.held; r += S::kRowsAtOnce) {
+          uint2* codes = reinterpret_cast<uint2*>(page + (int64_t)r * p.stride_n);
+          *codes = encode(decode(*codes), again);
+        }
+      }
+      unsigned char* at = page + (int64_t)(u.held + row0) * p.stride_n;
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        if (row0 + i * S::kRowsAtOnce < rows) *reinterpret_cast<uint2*>(at) = encode(x[i], inv);
+        at += S::kRowsAtOnce * p.stride_n;
+      }
+      // (every thread of a larger unit has the page's scale of before: it arrived in front of the barrier above)
+      __syncwarp();
+      if (rows > 0 && tid == 0) *scale_at = scale;
     }
   }
 }
 
 template <int D, bool FP8, int ROWS>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(UnitShape<D, ROWS>::kThreads, 1024 / UnitShape<D, ROWS>::kThreads)
 cache_append_kernel(const __grid_constant__ AppendParams p) {
-  __shared__ uint32_t s_max[kAppendThreads / 32];
+  constexpr int kThreads = UnitShape<D, ROWS>::kThreads;
+  __shared__ uint32_t s_max[2 * kThreads / 32];
+  extern __shared__ __align__(16) unsigned char s_raw[];
   __shared__ int s_bad[2];
   pdl_wait();
   if (blockIdx.x == 0) {
@@ -326,41 +329,70 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
       const RotaryView& r = p.rotary;
       auto bad = [&](int detail) { if (atomicExch(s_bad, 1) == 0) s_bad[1] = detail; };
       if (r.positions) {
-        for (long long i = threadIdx.x; i < (long long)p.batch.T * r.axes; i += kAppendThreads)
-          if ((uint32_t)r.positions[i] >= (uint32_t)r.rows) bad(r.positions[i]);
+        const long long n = (long long)p.batch.T * r.axes;
+        for (long long first = threadIdx.x; first < n; first += 8 * kThreads) {
+          int at[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) at[i] = first + i * kThreads < n ? r.positions[first + i * kThreads] : 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if ((uint32_t)at[i] >= (uint32_t)r.rows) bad(at[i]);
+        }
       } else {
-        for (int b = threadIdx.x; b < p.batch.B; b += kAppendThreads) {
+        for (int b = threadIdx.x; b < p.batch.B; b += kThreads) {
           const Sequence s = sequence_of(p.batch, b);
           if (s.n > 0 && s.len > r.rows) bad(s.len - 1);
         }
       }
       if (r.axis)
-        for (int m = threadIdx.x; m < r.rot / 2; m += kAppendThreads)
+        for (int m = threadIdx.x; m < r.rot / 2; m += kThreads)
           if ((uint32_t)r.axis[m] >= (uint32_t)r.axes) bad(r.axis[m]);
     }
     leave_status(p.status, s_bad);
-  } else if ((int)blockIdx.x <= p.unit_ctas) {
-    append_units<D, FP8, ROWS>(p, s_max);
-  } else {
-    rotate_queries<D>(p);
+    return;
   }
+  constexpr int U = UnitShape<D, ROWS>::U;
+  const int group = threadIdx.x / U;
+  const int unit = (int)(blockIdx.x - 1) * (kThreads / U) + group;
+  if (unit >= p.units) return;
+  const int bj = fast_div(unit, p.by_groups), first = unit - bj * p.groups;
+  const Part u = part_of(p, bj);
+  if (u.rows <= 0) return;
+  float* s_cos = reinterpret_cast<float*>(s_raw + UnitShape<D, ROWS>::kRowBytes) + group * ROWS * p.rotary.rot;
+  float* s_sin = s_cos + ROWS * (p.rotary.rot / 2);
+  if (p.rotary.rot > 0) {
+    gather_phases(p.rotary, u.rows, u.t0, u.pos0, s_cos, s_sin, threadIdx.x % U, U);
+    if constexpr (U > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(U) : "memory");
+    else __syncwarp();
+  }
+  append_lines<D, FP8, ROWS>(p, u, first, p.groups, group, s_max, s_cos, s_sin);
 }
 
 template <int D, bool FP8>
-static int launch_rows(const AppendParams& p, int rows, cudaStream_t stream) {
-  auto go = [&](auto kern, int unit_threads) {
-    AppendParams q = p;
-    const int per = kAppendThreads / unit_threads;
-    const long long ctas = (p.units + per - 1) / per, q_ctas = p.q.data ? ((long long)p.batch.T + p.q_tokens - 1) / p.q_tokens : 0;
-    if (1 + ctas + q_ctas > 0x7fffffffLL) return (int)SPARKATTN_E_UNSUPPORTED_SHAPE;
-    q.unit_ctas = (int)ctas;
-    return launch_kernel(kern, dim3((unsigned)(1 + ctas + q_ctas)), kAppendThreads, 0, true, stream, q);
+static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream) {
+  auto go = [&](auto kern, auto shape) {
+    constexpr int kThreads = decltype(shape)::kThreads, per = kThreads / decltype(shape)::U;
+    AppendParams p = given;
+    p.lines = 2 * p.Hk + (p.q.data ? p.H : 0);
+    // One wave of CTAs where that leaves a unit at most sixteen lines, else units of eight
+    const long long parts = (long long)p.batch.B * p.pages_each, slots = (long long)per * (1024 / kThreads) * current_sm_count();
+    p.groups = (int)std::min<long long>(std::max<long long>(slots / parts, 1), p.lines);
+    if (p.lines > 16 * p.groups) p.groups = (p.lines + 7) / 8;
+    const long long units = parts * p.groups;
+    if (units > 0x7fffff00LL) return (int)SPARKATTN_E_UNSUPPORTED_SHAPE;
+    p.units = (int)units;
+    p.by_pages_each = make_fast_div(p.pages_each);
+    p.by_groups = make_fast_div(p.groups);
+    const unsigned ctas = 1 + (unsigned)((units + per - 1) / per);
+    const size_t smem = decltype(shape)::smem(p.rotary.rot);
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)decltype(shape)::smem(D)) != cudaSuccess) return (int)SPARKATTN_E_CUDA;
+    return launch_kernel(kern, dim3(ctas), kThreads, smem, true, stream, p);
   };
-  if (rows <= 4) return go(cache_append_kernel<D, FP8, 4>, 32);
-  if (rows <= 16) return go(cache_append_kernel<D, FP8, 16>, 32);
-  if (rows <= 32) return go(cache_append_kernel<D, FP8, 32>, 64);
-  if (rows <= 64) return go(cache_append_kernel<D, FP8, 64>, 128);
-  return go(cache_append_kernel<D, FP8, 128>, 256);
+  if (rows <= 4) return go(cache_append_kernel<D, FP8, 4>, UnitShape<D, 4>{});
+  if (rows <= 16) return go(cache_append_kernel<D, FP8, 16>, UnitShape<D, 16>{});
+  if (rows <= 32) return go(cache_append_kernel<D, FP8, 32>, UnitShape<D, 32>{});
+  if (rows <= 64) return go(cache_append_kernel<D, FP8, 64>, UnitShape<D, 64>{});
+  return go(cache_append_kernel<D, FP8, 128>, UnitShape<D, 128>{});
 }
 
 int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rotary_t* rotary, const sparkattn_rows_t* q,
@@ -379,8 +411,6 @@ int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, 
   p.stride_page = c.stride_page; p.stride_h = c.stride_h; p.stride_n = c.stride_n;
   p.H = H; p.Hk = c.H;
   p.pages_each = (b.max_new - 1 + c.page - 1) / c.page + 1;
-  p.units = 2LL * b.B * p.pages_each * c.H;
-  p.q_tokens = 1;
   p.status = static_cast<int32_t*>(workspace);
   const int rows = c.page < b.max_new ? c.page : b.max_new;
   const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;

@@ -381,6 +381,19 @@ __device__ __forceinline__ bool elect_one() {
   return one != 0;
 }
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+// x / d for 0 <= x < 2^31 without the division's twenty-odd instructions at every place that takes an item apart: division
+// by an invariant integer through multiplication, after Granlund and Montgomery
+struct FastDiv {
+  uint32_t mul, shift;
+};
+inline FastDiv make_fast_div(uint32_t d) {
+  FastDiv f{0, 0};
+  while ((1ull << f.shift) < d) ++f.shift;
+  f.mul = (uint32_t)(((1ull << 32) * ((1ull << f.shift) - d)) / d + 1);
+  return f;
+}
+__device__ __forceinline__ int fast_div(int x, FastDiv f) { return (int)((__umulhi((uint32_t)x, f.mul) + (uint32_t)x) >> f.shift); }
+
 // Register re-balancing between warpgroups (all warps of a warpgroup execute it).
 template <int N>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }

@@ -90,19 +90,6 @@ constexpr int kTileRing = 8;                               // tile descriptors t
 constexpr int kPipeSmem = kOffMisc + 512 /*barriers*/ + 2 * 128 * 4 /*reference maxima*/ + 128 * 8 /*row sums*/ + 64 +
                           kTileRing * 32 /*tile descriptors*/;
 
-// x / d for 0 <= x < 2^31 without the division's twenty-odd instructions at every place that takes an item apart: division
-// by an invariant integer through multiplication, after Granlund and Montgomery
-struct FastDiv {
-  uint32_t mul, shift;
-};
-static FastDiv make_fast_div(uint32_t d) {
-  FastDiv f{0, 0};
-  while ((1ull << f.shift) < d) ++f.shift;
-  f.mul = (uint32_t)(((1ull << 32) * ((1ull << f.shift) - d)) / d + 1);
-  return f;
-}
-__device__ __forceinline__ int fast_div(int x, FastDiv f) { return (int)((__umulhi((uint32_t)x, f.mul) + (uint32_t)x) >> f.shift); }
-
 struct PipeParams {
   int32_t* clean_cnt;          // [items] valid kept blocks per item
   int32_t* clean_list;         // [items][kmax] their indices, compacted in list order
