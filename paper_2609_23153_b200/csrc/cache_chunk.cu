@@ -94,12 +94,13 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
   const int total = s_prefix[p.batch.B], share = L::share_of(p, total);
-  if (blockIdx.x == 0) check_and_publish<kChunkRows, kChunkKeys>(p, s_prefix, share, s_bad);
+  if (blockIdx.x == 0) check_call(p, s_bad);
   const long long begin = (long long)((int)blockIdx.x - 1) * share;
   const bool works = blockIdx.x > 0 && begin < total;
   const int x0 = works ? (int)begin : 0, x1 = works ? (int)min(begin + share, (long long)total) : 0;
   Stretch<kChunkRows, kChunkKeys> g;
   if (works) g.begin(p, s_prefix, x0, x1);
+  if (blockIdx.x > 0 && threadIdx.x == 0) note_border(p, (int)blockIdx.x - 1, works, share, g);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // tiles go where the line's beginnings lie
   __syncthreads();
   if (warp < 4) reg_dec<kCtrlRegs>();
@@ -524,7 +525,7 @@ static int launch_chunk(const sparkattn_cache_t& c, const sparkattn_batch_t& b, 
   auto kern = cache_chunk_kernel<D, FP8>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kChunkThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
-  return launch_kernel(combine_kernel<D, kChunkRows, kChunkKeys>, dim3(p.workers, 16), 128, 0, true, stream, p);
+  return launch_kernel(combine_kernel<D, kChunkRows>, dim3(p.workers - 1, 16), kCombineThreads, 0, true, stream, p);
 }
 
 int launch_cache_chunk(const sparkattn_cache_t& c, const sparkattn_batch_t& b, CacheFwdParams& p, const void* k_cache, const void* v_cache,

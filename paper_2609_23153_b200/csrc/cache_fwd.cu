@@ -71,6 +71,9 @@ __device__ __forceinline__ uint2 lds8(uint32_t at) {
   return v;
 }
 
+// CTAs per SM, as registers and the rings allow
+constexpr int decode_ctas_per_sm(int D, bool fp8, int R) { return R == 8 ? (fp8 ? 4 : D == 64 ? 3 : 2) : D == 64 ? 3 : 2; }
+
 template <int D, bool FP8, int NT>
 struct DecodeShape {
   static constexpr int R = 8 * NT;
@@ -79,6 +82,7 @@ struct DecodeShape {
   static constexpr int kTileBytes = kTileKeys * kRowBytes;
   static constexpr int kStageBytes = 2 * kTileBytes;
   static constexpr int kOPitch = D + 4;
+  static constexpr int kPerSM = decode_ctas_per_sm(D, FP8, R);
   static constexpr int kMergeBytes = kComputeWarps * R * (kOPitch + 2) * 4;
   static constexpr int fixed_bytes(int B, int stages) {
     return kMergeBytes + stages * (kGroups * (int)sizeof(GroupInfo) + 16) + 64 + (B + 1) * 4 + 64;
@@ -86,7 +90,7 @@ struct DecodeShape {
 };
 
 template <int D, bool FP8, int NT>
-__global__ void __launch_bounds__(kDecodeThreads, 2)
+__global__ void __launch_bounds__(kDecodeThreads, DecodeShape<D, FP8, NT>::kPerSM)
 cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                     const __grid_constant__ CacheFwdParams p) {
   using S = DecodeShape<D, FP8, NT>;
@@ -108,7 +112,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
-    for (int i = 0; i < p.stages; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, kComputeWarps); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(full + i, 2); mbar_init(empty + i, kComputeWarps); }
     mbar_init(merged, kComputeWarps);
     mbar_init(taken, kComputeWarps);
     mbar_fence_init();
@@ -118,20 +122,22 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
   Line<R, kTileKeys>::lay_out(p, s_prefix, s_warp);
   const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys>::share_of(p, total);
   if (blockIdx.x == 0) {
-    check_and_publish<R, kTileKeys>(p, s_prefix, share, s_bad);
+    check_call(p, s_bad);
     return;
   }
   const int worker = blockIdx.x - 1;
   const long long begin = (long long)worker * share;
-  if (begin >= total) return;
+  const bool works = begin < total;
   const int x0 = (int)begin, x1 = (int)min(begin + share, (long long)total);
+  Stretch<R, kTileKeys> g;
+  if (works) g.begin(p, s_prefix, x0, x1);
+  if (threadIdx.x == 0) note_border(p, worker, works, share, g);
+  if (!works) return;
 
   if (warp == kComputeWarps) {
     // ------------------------------------------------------------------------------------------------------ copies
     int stage = 0, use = 0;
     bool ok = true;
-    Stretch<R, kTileKeys> g;
-    g.begin(p, s_prefix, x0, x1);
     do {
       const int32_t* table = p.batch.page_table + (int64_t)g.c.b * p.batch.max_pages;
       constexpr int kBatch = 32 / kGroups;                   // tiles whose groups the lanes look up together
@@ -151,7 +157,6 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           if (use > 0) ok = mbar_wait(empty + stage, (use - 1) & 1, s_abort, p.status, 1);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
-          if (lane / kGroups == u) s_info[stage * kGroups + lane % kGroups] = info;
           // lane i copies box i of K, lane i + boxes box i of V: as many of them as have a page
           const int box = lane & (p.boxes - 1);
           const int src = u * kGroups + box * (kGroups / p.boxes);
@@ -161,7 +166,6 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           for (int i = 1; i < kGroups / p.boxes; ++i) box_page = max(box_page, __shfl_sync(0xffffffffu, page, src + i));
           const bool copies = lane < 2 * p.boxes && box_page >= 0;
           const uint32_t going = __ballot_sync(0xffffffffu, copies);
-          __syncwarp();                                      // the groups' notes are written
           if (lane == 0) {
             if (going) mbar_expect_tx(full + stage, __popc(going) * p.box_rows * kRowBytes);
             else mbar_arrive(full + stage);
@@ -178,6 +182,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
             for (int sl = 0; sl < kRowBytes / kSlab; ++sl)
               tma_load_4d(dst + sl * (kTileKeys * kSlab) + box * p.box_rows * kSlab, map, full + stage, sl * (kSlab / S::kElt), row, g.c.h, box_page);
           }
+          // the groups' notes follow, so that the first copies do not wait for the first scales
+          if (lane / kGroups == u) s_info[stage * kGroups + lane % kGroups] = info;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(full + stage);
           if (++stage == p.stages) { stage = 0; ++use; }
         }
       }
@@ -190,8 +198,6 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     constexpr int kChunkCh = 16 / S::kElt;             // channels of a 16-byte chunk
     int stage = 0, use = 0, segments = 0;
     bool ok = true;
-    Stretch<R, kTileKeys> g;
-    g.begin(p, s_prefix, x0, x1);
     do {
       // the rows' queries as the first product's B operand: lane (g8, t4) has channels of row g8
       uint32_t qf[NT][kSteps][2];
@@ -491,14 +497,15 @@ constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 // rows of an item, and stretches of the line: up to 16 rows per key head take this file's kernel, more the tensor cores' (cache_chunk.cu)
 struct Plan {
   int R, workers;
-  size_t prefix, ml, o;        // bytes of the workspace's parts behind the header
+  size_t borders, ml, o;       // bytes of the workspace's parts behind the header
 };
 Plan plan_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
   const long long rows = (long long)(H / c.H) * b.max_new;
   Plan p;
   p.R = rows <= 8 ? 8 : rows <= 16 ? 16 : kChunkRows;
-  p.workers = current_sm_count() * (p.R == kChunkRows ? 1 : 2);
-  p.prefix = align256((size_t)(b.B + 2) * 4);
+  const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;
+  p.workers = current_sm_count() * (p.R == kChunkRows ? 1 : decode_ctas_per_sm(c.d, fp8, p.R));
+  p.borders = align256((size_t)p.workers * sizeof(Border));
   p.ml = align256((size_t)2 * p.workers * p.R * 8);
   p.o = (size_t)2 * p.workers * p.R * c.d * 4;
   return p;
@@ -507,7 +514,7 @@ Plan plan_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
 
 size_t cache_fwd_workspace_bytes(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
   const Plan p = plan_of(c, b, H);
-  return kWorkspaceHeaderBytes + p.prefix + p.ml + p.o;
+  return kWorkspaceHeaderBytes + p.borders + p.ml + p.o;
 }
 
 template <int D, bool FP8, int NT>
@@ -520,16 +527,18 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   p.boxes = kTileKeys / p.box_rows;
   if ((rc = make_page_map(&mk, k_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
   if ((rc = make_page_map(&mv, v_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
-  // two CTAs per SM, or one where the list of a great many sequences leaves no room for two rings
-  p.stages = (113 * 1024 - S::fixed_bytes(b.B, 12)) / S::kStageBytes;
-  if (p.stages < 2) p.stages = (226 * 1024 - S::fixed_bytes(b.B, 12)) / S::kStageBytes;
+  // as deep a ring as the CTAs of an SM leave each other; fewer CTAs where a great many sequences leave no room for two tiles
+  for (int per = S::kPerSM; per > 0; --per) {
+    p.stages = (227 * 1024 / per - 1024 - S::fixed_bytes(b.B, 12)) / S::kStageBytes;
+    if (p.stages >= 2) break;
+  }
   if (p.stages > 12) p.stages = 12;
   if (p.stages < 2) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   const int smem = p.stages * S::kStageBytes + S::fixed_bytes(b.B, p.stages);
   auto kern = cache_decode_kernel<D, FP8, NT>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kDecodeThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
-  return launch_kernel(combine_kernel<D, S::R, kTileKeys>, dim3(p.workers), 128, 0, true, stream, p);
+  return launch_kernel(combine_kernel<D, S::R>, dim3(p.workers - 1), kCombineThreads, 0, true, stream, p);
 }
 
 int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rows_t& q, int H, const void* k_cache,
@@ -553,8 +562,8 @@ int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, con
   char* base = static_cast<char*>(workspace);
   p.status = reinterpret_cast<int32_t*>(base);
   base += kWorkspaceHeaderBytes;
-  p.prefix = reinterpret_cast<int32_t*>(base);
-  base += plan.prefix;
+  p.borders = reinterpret_cast<Border*>(base);
+  base += plan.borders;
   p.part_ml = reinterpret_cast<float*>(base);
   base += plan.ml;
   p.part_o = reinterpret_cast<float*>(base);

@@ -31,9 +31,17 @@ struct CacheFwdParams {
   int workers;                   // stretches
   int stages;
   int32_t* status;
-  int32_t* prefix;               // [B + 2] first tile of every sequence, the total, tiles per stretch
+  struct Border* borders;        // [workers]
   float* part_ml;                // [2 workers][R][2] reference, sum
   float* part_o;                 // [2 workers][R][d] unnormalised output
+};
+
+// What the combining kernel needs to know of the border in front of a stretch: the item that it cuts, if it does.
+struct Border {
+  int before;                    // tiles of the item in front of the border; 0: the border cuts none
+  int tiles, share;              // of the item; of a stretch
+  int token0, row0, rows, h;     // row r is head h * G + (row0 + r) % G of token token0 + (row0 + r) / G
+  int pad;
 };
 
 // cache_chunk.cu: items of 256 rows
@@ -216,11 +224,8 @@ __device__ __forceinline__ int look_up_group(const CacheFwdParams& p, const int3
   return page;
 }
 
-// the status of a call, and the line for the combining kernel: the first CTA's work
-template <int R, int TK>
-__device__ __forceinline__ void check_and_publish(const CacheFwdParams& p, const int* prefix, int share, int* s_bad) {
-  for (int b = threadIdx.x; b <= p.batch.B; b += blockDim.x) p.prefix[b] = prefix[b];
-  if (threadIdx.x == 0) p.prefix[p.batch.B + 1] = share;
+// the status of a call: the first CTA's work
+__device__ __forceinline__ void check_call(const CacheFwdParams& p, int* s_bad) {
   check_batch(p.batch, s_bad, [&](const Sequence& s) {
     if (s.n == 0) return make_int2(0, 0);
     const int lo = visible_keys(p.causal, s.first_pos(), s.len).x, hi = visible_keys(p.causal, s.len - 1, s.len).y;
@@ -228,41 +233,72 @@ __device__ __forceinline__ void check_and_publish(const CacheFwdParams& p, const
   });
   leave_status(p.status, s_bad);
 }
+template <int R, int TK>
+__device__ __forceinline__ void note_border(const CacheFwdParams& p, int worker, bool works, int share, const Stretch<R, TK>& g) {
+  Border b{};
+  if (works) b = {g.c.at, g.c.item.tiles, share, g.c.seq.start, g.row0, g.rows, g.c.h, 0};
+  reinterpret_cast<int4*>(p.borders + worker)[0] = reinterpret_cast<const int4*>(&b)[0];
+  reinterpret_cast<int4*>(p.borders + worker)[1] = reinterpret_cast<const int4*>(&b)[1];
+}
 
-// Adds up what several stretches have left of an item, in the order of the line.  CTA w looks at the border in front of
-// stretch w + 1 and does the item if that is the first border inside it; gridDim.y CTAs share its rows, a warp each.
-template <int D, int R, int TK>
-__global__ void __launch_bounds__(128)
+// Adds up what several stretches have left of an item, in the order of the line.  CTA w looks at the border in front of stretch
+// w + 1 and does the item if that is the first border inside it; gridDim.y CTAs share its rows.  A warp takes a row, or, of an item
+// of few rows, every n-th part of a row, since what this kernel spends is the time of a few loads one after the other.
+constexpr int kCombineThreads = 512;
+template <int D, int R>
+__global__ void __launch_bounds__(kCombineThreads)
 combine_kernel(const __grid_constant__ CacheFwdParams p) {
-  using L = Line<R, TK>;
-  constexpr int kVec = D / 32;
+  constexpr int kVec = D / 32, kWarps = kCombineThreads / 32;
+  __shared__ float s_acc[kWarps][D + 2];
   pdl_wait();
-  const int total = p.prefix[p.batch.B], share = p.prefix[p.batch.B + 1];
-  const long long border = (long long)(blockIdx.x + 1) * share;
-  if (border >= total) return;
-  const typename L::Place c = L::find(p, p.prefix, (int)border);
-  const int start = (int)border - c.at;
-  if (c.at == 0 || start < (int)border - share) return;
-  const int w0 = start / share, w1 = (start + c.item.tiles - 1) / share;
-  const int lane = threadIdx.x & 31, rows = min(R, c.seq.n * p.G - c.rt * R);
-  for (int r = blockIdx.y * 4 + (threadIdx.x >> 5); r < rows; r += 4 * gridDim.y) {
-    auto slot_of = [&](int w) { return 2 * w + (start <= w * share ? 0 : 1); };
-    float top = -INFINITY;
-    for (int w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, p.part_ml[((int64_t)slot_of(w) * R + r) * 2]);
+  const int4 b0 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[0], b1 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[1];
+  const int before = b0.x, tiles = b0.y, share = b0.z, token0 = b0.w, row0 = b1.x, rows = b1.y, h = b1.z;
+  if (before == 0 || before > share) return;
+  const int w0 = blockIdx.x, parts = 1 + (tiles - before + share - 1) / share;
+  // the stretch in front holds the item's beginning as its last segment (its only one where it begins with it), the others as their first
+  auto slot_of = [&](int i) { return 2 * (w0 + i) + (i > 0 || before == share ? 0 : 1); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int split = rows >= kWarps ? 1 : kWarps / rows;           // warps of a row
+  const int share_of_row = warp % split;
+  for (int r = blockIdx.y * (kWarps / split) + warp / split; r - warp / split < rows; r += gridDim.y * (kWarps / split)) {
+    const bool there = r < rows && warp / split < kWarps / split;
+    float top = -INFINITY, sum = 0.0f, acc[kVec] = {};
+    if (there) {
+      for (int i = lane; i < parts; i += 32) top = fmaxf(top, p.part_ml[((int64_t)slot_of(i) * R + r) * 2]);
+    }
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-    float sum = 0.0f, acc[kVec] = {};
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const int64_t at = (int64_t)slot_of(w) * R + r;
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
-      const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
-      sum = fmaf(ml.y, f, sum);
-      const float* src = p.part_o + at * D + lane * kVec;
+    if (there) {
+#pragma unroll 8
+      for (int i = share_of_row; i < parts; i += split) {
+        const int64_t at = (int64_t)slot_of(i) * R + r;
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
+        const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
+        sum = fmaf(ml.y, f, sum);
+        const float* src = p.part_o + at * D + lane * kVec;
+        float v[kVec];
+        if constexpr (kVec == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
+        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) acc[j] = fmaf(src[j], f, acc[j]);
+        for (int j = 0; j < kVec; ++j) acc[j] = fmaf(v[j], f, acc[j]);
+      }
     }
-    const int row = c.rt * R + r, token = c.seq.start + row / p.G, head = c.h * p.G + row % p.G;
+    if (split > 1) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) s_acc[warp][lane * kVec + j] = acc[j];
+      if (lane == 0) s_acc[warp][D] = sum;
+      __syncthreads();
+      if (there && share_of_row == 0) {
+        for (int i = 1; i < split; ++i) {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) acc[j] += s_acc[warp + i][lane * kVec + j];
+          sum += s_acc[warp + i][D];
+        }
+      }
+      __syncthreads();
+    }
+    if (!there || share_of_row != 0) continue;
+    const int row = row0 + r, token = token0 + row / p.G, head = h * p.G + row % p.G;
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + lane * kVec);
 #pragma unroll
