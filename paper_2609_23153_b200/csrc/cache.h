@@ -77,19 +77,20 @@ __device__ __forceinline__ void check_batch(const BatchView& v, int* s_bad /* [2
       bad(b);
     }
   }
-  // a warp per sequence, so that the pages of a long one are asked for 32 at a time
-  for (int b = threadIdx.x >> 5; b < v.B; b += blockDim.x >> 5) {
+  // eight lanes per sequence, eight pages each at a time
+  const int lanes = 8, lane = threadIdx.x & (lanes - 1);
+  for (int b = threadIdx.x / lanes; b < v.B; b += blockDim.x / lanes) {
     const Sequence s = sequence_of(v, b);
     const int2 pages = reach(s);
     const int32_t* row = v.page_table + (int64_t)b * v.max_pages;
     const int last = min(pages.y, v.max_pages);
-    for (int i = pages.x + (threadIdx.x & 31); i < last; i += 32 * 4) {
+    for (int i = pages.x + lane; i < last; i += lanes * 8) {
+      int page[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int at = i + 32 * u;
-        const int page = at < last ? row[at] : 0;
-        if ((uint32_t)page >= (uint32_t)v.pages) bad(page);
-      }
+      for (int u = 0; u < 8; ++u) page[u] = i + lanes * u < last ? row[i + lanes * u] : 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if ((uint32_t)page[u] >= (uint32_t)v.pages) bad(page[u]);
     }
   }
 }

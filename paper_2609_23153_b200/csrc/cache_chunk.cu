@@ -256,12 +256,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               const uint32_t w[4] = {v.x, v.y, v.z, v.w};
               uint32_t h[8];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i] & 0xffffu), __NV_E4M3);
-                const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i] >> 16), __NV_E4M3);
-                h[2 * i] = (uint32_t)lo.x | (uint32_t)lo.y << 16;
-                h[2 * i + 1] = (uint32_t)hi.x | (uint32_t)hi.y << 16;
-              }
+              for (int i = 0; i < 4; ++i) e4m3_to_half(w[i], h[2 * i], h[2 * i + 1]);
               const uint32_t dst = to + (c >> 2) * kSlab + r * 128;
               const int ck = (c & 3) * 2;
               asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + ((ck ^ (r & 7)) << 4)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");

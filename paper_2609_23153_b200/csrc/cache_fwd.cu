@@ -8,15 +8,16 @@
 //     stretches, one per CTA, two CTAs per SM.  A CTA's stretch is a sequence of segments (parts of items); an item that
 //     lies in one stretch is finished there, one that several stretches share leaves partial results (maximum, sum,
 //     unnormalised output) in the workspace, which combine_kernel, launched behind, adds up in a fixed order.
-//   Copies: one warp requests the tiles with TMA (boxes of up to 64 rows of a page), as far ahead as the ring is deep, across
+//   Copies: one warp requests the tiles with TMA (boxes of whole pages, or what a tile takes of one), as far ahead as the ring is deep, across
 //     segment borders.  It also fetches page numbers and scales, 32 groups of 16 keys at a time, one batch ahead.
 //   Products: four warps, each with 16 keys of every tile and online-softmax state of its own (merged when a segment
 //     ends), so that nothing in the loop waits for another warp.  S^T = K Q^T and O^T = V^T P^T as m16n8k16 products with the
 //     rows as the N side: eight rows fill an instruction, where rows on the M side would leave half of it empty.
 //     The channel order of the first product and the key order of the second are free, so every lane takes its
-//     operands from shared memory 16 bytes at a time: 16 channels of a key, of which four make a fragment.  E4M3 becomes
-//     fp16 (exact) on the way, V's bytes of two keys interleaved by a byte permutation; the queries are fp16, scaled by
-//     a power of two per row.  P^T is S^T's accumulator transposed by movmatrix.
+//     operands from shared memory 16 bytes at a time: 16 channels of a key, of which eight make a fragment.
+//     E4M3: K's codes are the first product's operand as they are, against the queries in two E4M3 parts (split_queries), which
+//     hold all eight of a bf16's digits; V's bytes of two keys are interleaved by a byte permutation and become fp16 (exact), as the
+//     weights do.  P^T is S^T's accumulator transposed by movmatrix.
 //   Scales: k's multiplies the logits.  v's goes into the exponent: with t = logit + log2(v_scale), the weights of the second
 //     product are 2^(t - m), m a running reference of t, and the row sum adds weight / v_scale.  So neither costs a
 //     multiplication per element.
@@ -24,6 +25,7 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "cache_line.cuh"
@@ -31,34 +33,35 @@
 
 namespace sparkattn {
 
-constexpr int kTileKeys = 64, kGroupKeys = 16, kGroups = kTileKeys / kGroupKeys;
+constexpr int kGroupKeys = 16;
+constexpr int kInfoRing = 32;      // tiles whose groups' notes are kept: a batch of up to 8 and a ring of up to 8 at a time
 constexpr int kComputeWarps = 4, kDecodeThreads = 32 * (kComputeWarps + 1);
 
 // ---------------------------------------------------------------------------------------------------------- fragments
-__device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t two) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
-}
 template <bool FP8>
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (FP8)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_16832(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 
 // Shared memory of a tile as TMA leaves it: slabs of at most 128 bytes a row, 16-byte chunks swizzled within 8 rows.
-template <int ROW_BYTES>
+template <int ROW_BYTES, int TILE_KEYS>
 __device__ __forceinline__ uint32_t chunk_offset(int row, int chunk) {
   if constexpr (ROW_BYTES == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
-  else return (chunk >> 3) * (kTileKeys * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+  else return (chunk >> 3) * (TILE_KEYS * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
 }
 __device__ __forceinline__ uint4 lds16(uint32_t at) {
   uint4 v;
@@ -72,135 +75,202 @@ __device__ __forceinline__ uint2 lds8(uint32_t at) {
 }
 
 // CTAs per SM, as registers and the rings allow
-constexpr int decode_ctas_per_sm(int D, bool fp8, int R) { return R == 8 ? (fp8 ? 4 : D == 64 ? 3 : 2) : D == 64 ? 3 : 2; }
+constexpr int decode_ctas_per_sm(int D, bool fp8, int R) { return 2; }
 
 template <int D, bool FP8, int NT>
 struct DecodeShape {
   static constexpr int R = 8 * NT;
   static constexpr int kElt = FP8 ? 1 : 2;
   static constexpr int kRowBytes = D * kElt;
-  static constexpr int kTileBytes = kTileKeys * kRowBytes;
-  static constexpr int kStageBytes = 2 * kTileBytes;
+  // groups of 16 keys that a warp takes of a tile: two where a K or V tile stays within 16 KB, so that their chains of dependent
+  // steps run side by side and the steps that a tile needs once are spread over 32 keys
+  static constexpr int kPerWarp = kRowBytes <= 128 ? 2 : 1;
+  static constexpr int kGroups = kComputeWarps * kPerWarp, kTileKeys = kGroups * kGroupKeys;
+  static constexpr int kTileBytes = kTileKeys * kRowBytes;       // of K or of V
   static constexpr int kOPitch = D + 4;
   static constexpr int kPerSM = decode_ctas_per_sm(D, FP8, R);
   static constexpr int kMergeBytes = kComputeWarps * R * (kOPitch + 2) * 4;
-  static constexpr int fixed_bytes(int B, int stages) {
-    return kMergeBytes + stages * (kGroups * (int)sizeof(GroupInfo) + 16) + 64 + (B + 1) * 4 + 64;
+  static constexpr int fixed_bytes(int B, int slots) {
+    return kMergeBytes + kInfoRing * kGroups * (int)sizeof(GroupInfo) + slots * 16 + 64 + ((B + 1) * 4 > R * 8 ? (B + 1) * 4 : R * 8) + 64;
   }
 };
 
-template <int D, bool FP8, int NT>
+// CLUSTER: an item (it has one row tile) belongs to a cluster of CTAs, each takes an equal run of its key tiles, and the CTAs' results
+// are added up through distributed shared memory.  Otherwise the line, see cache_line.cuh; cluster_of has the rule.
+template <int D, bool FP8, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(kDecodeThreads, DecodeShape<D, FP8, NT>::kPerSM)
 cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                     const __grid_constant__ CacheFwdParams p) {
   using S = DecodeShape<D, FP8, NT>;
-  constexpr int R = S::R, kRowBytes = S::kRowBytes;
+  constexpr int R = S::R, kRowBytes = S::kRowBytes, kTileKeys = S::kTileKeys, kGroups = S::kGroups, kPerWarp = S::kPerWarp;
   extern __shared__ __align__(1024) unsigned char smem[];
-  unsigned char* after = smem + p.stages * S::kStageBytes;
+  unsigned char* after = smem + p.slots * S::kTileBytes;
   float* s_o = reinterpret_cast<float*>(after);                                      // [warps][R][pitch]
   float2* s_ml = reinterpret_cast<float2*>(s_o + kComputeWarps * R * S::kOPitch);    // [warps][R]
-  GroupInfo* s_info = reinterpret_cast<GroupInfo*>(s_ml + kComputeWarps * R);        // [stages][groups]
-  uint64_t* full = reinterpret_cast<uint64_t*>(s_info + p.stages * kGroups);
-  uint64_t* empty = full + p.stages;
-  uint64_t* merged = empty + p.stages;                                               // a segment's parts are in shared memory
+  GroupInfo* s_info = reinterpret_cast<GroupInfo*>(s_ml + kComputeWarps * R);        // [ring][groups]
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_info + kInfoRing * kGroups);
+  uint64_t* empty = full + p.slots;
+  uint64_t* merged = empty + p.slots;                                               // a segment's parts are in shared memory
   uint64_t* taken = merged + 1;                                                      // ... and have been read
   volatile int* s_abort = reinterpret_cast<volatile int*>(taken + 1);
   int* s_bad = const_cast<int*>(s_abort) + 1;
   int* s_warp = s_bad + 2;
-  int* s_prefix = s_warp + 8;
+  int* s_prefix = s_warp + 8;                                                        // the line's
+  float2* s_cta = reinterpret_cast<float2*>(s_warp + 9);                             // [R], a cluster's CTA: reference and sum of its rows
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
-    for (int i = 0; i < p.stages; ++i) { mbar_init(full + i, 2); mbar_init(empty + i, kComputeWarps); }
+    for (int i = 0; i < p.slots; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, kComputeWarps); }
     mbar_init(merged, kComputeWarps);
     mbar_init(taken, kComputeWarps);
     mbar_fence_init();
     *s_abort = 0;
   }
   pdl_wait();
+  Stretch<R, kTileKeys> g;
+  int worker = 0;
+  if constexpr (CLUSTER) {
+    __syncthreads();
+    const int cluster = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x - cluster * p.cluster;
+    if (cluster == 0) {
+      if (rank == 0) check_call(p, s_bad);
+      return;
+    }
+    const int b = (cluster - 1) / p.Hk;
+    if (!g.run_of(p, b, cluster - 1 - b * p.Hk, rank, p.cluster)) return;
+  } else {
   Line<R, kTileKeys>::lay_out(p, s_prefix, s_warp);
   const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys>::share_of(p, total);
   if (blockIdx.x == 0) {
     check_call(p, s_bad);
     return;
   }
-  const int worker = blockIdx.x - 1;
+  worker = blockIdx.x - 1;
   const long long begin = (long long)worker * share;
   const bool works = begin < total;
   const int x0 = (int)begin, x1 = (int)min(begin + share, (long long)total);
-  Stretch<R, kTileKeys> g;
   if (works) g.begin(p, s_prefix, x0, x1);
   if (threadIdx.x == 0) note_border(p, worker, works, share, g);
   if (!works) return;
+  }
 
   if (warp == kComputeWarps) {
     // ------------------------------------------------------------------------------------------------------ copies
-    int stage = 0, use = 0;
-    bool ok = true;
-    do {
-      const int32_t* table = p.batch.page_table + (int64_t)g.c.b * p.batch.max_pages;
-      constexpr int kBatch = 32 / kGroups;                   // tiles whose groups the lanes look up together
-      // lane l looks after group l of a batch: its page and scales, asked for a batch ahead
-      int page_n;
-      GroupInfo info_n;
-      auto look_up = [&](int t) {
-        const bool in = t + lane / kGroups < g.t1;
-        page_n = look_up_group<FP8>(p, table, g.c.h, in ? t * kTileKeys + lane * kGroupKeys : 0x7fffff00, g.c.item.lo, g.c.item.hi, info_n);
-      };
-      look_up(g.t0);
-      for (int t = g.t0; ok && t < g.t1; t += kBatch) {
-        const int page = page_n;
-        const GroupInfo info = info_n;
-        if (t + kBatch < g.t1) look_up(t + kBatch);
-        for (int u = 0; u < kBatch && t + u < g.t1; ++u) {
-          if (use > 0) ok = mbar_wait(empty + stage, (use - 1) & 1, s_abort, p.status, 1);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          // lane i copies box i of K, lane i + boxes box i of V: as many of them as have a page
-          const int box = lane & (p.boxes - 1);
-          const int src = u * kGroups + box * (kGroups / p.boxes);
-          const int at_page = __shfl_sync(0xffffffffu, page, src);
-          // (a box may begin before the first visible key and still hold some: any group of it will do)
-          int box_page = at_page;
-          for (int i = 1; i < kGroups / p.boxes; ++i) box_page = max(box_page, __shfl_sync(0xffffffffu, page, src + i));
-          const bool copies = lane < 2 * p.boxes && box_page >= 0;
-          const uint32_t going = __ballot_sync(0xffffffffu, copies);
-          if (lane == 0) {
-            if (going) mbar_expect_tx(full + stage, __popc(going) * p.box_rows * kRowBytes);
-            else mbar_arrive(full + stage);
-          }
-          __syncwarp();
-          if (copies) {
-            const bool is_v = lane >= p.boxes;
-            const int key = (t + u) * kTileKeys + box * p.box_rows;
-            unsigned char* dst = smem + stage * S::kStageBytes + (is_v ? S::kTileBytes : 0);
-            const CUtensorMap* map = is_v ? &tmap_v : &tmap_k;
-            const int row = key & ((1 << p.batch.page_shift) - 1);
-            constexpr int kSlab = kRowBytes > 128 ? 128 : kRowBytes;
-#pragma unroll
-            for (int sl = 0; sl < kRowBytes / kSlab; ++sl)
-              tma_load_4d(dst + sl * (kTileKeys * kSlab) + box * p.box_rows * kSlab, map, full + stage, sl * (kSlab / S::kElt), row, g.c.h, box_page);
-          }
-          // the groups' notes follow, so that the first copies do not wait for the first scales
-          if (lane / kGroups == u) s_info[stage * kGroups + lane % kGroups] = info;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(full + stage);
-          if (++stage == p.stages) { stage = 0; ++use; }
+    // The stretch goes by in batches of a few tiles of a segment, of whose groups of 16 keys every lane looks after one.  Pages are
+    // asked for two batches ahead and scales one, across segments, so that only the first batch waits for them.
+    struct Batch {
+      int t, n, h;                 // first tile, tiles; key head
+      int page;                    // of the lane's group, -1: nobody sees it, or there is no such page
+      float k_scale, v_scale;
+    };
+    constexpr int kBatch = 32 / kGroups;
+    int t_next = g.t0;
+    bool live = true;
+    auto ask_pages = [&] {
+      Batch b{t_next, 0, 0, -1, 1.0f, 1.0f};
+      if (!live) return b;
+      b.n = min(kBatch, g.t1 - b.t);
+      b.h = g.c.h;
+      const int key = b.t * kTileKeys + lane * kGroupKeys;
+      if (lane / kGroups < b.n && key < g.c.item.hi && key + kGroupKeys > g.c.item.lo)
+        b.page = p.batch.page_table[(int64_t)g.c.b * p.batch.max_pages + (key >> p.batch.page_shift)];
+      t_next += b.n;
+      if (t_next >= g.t1) {
+        live = g.next(p);
+        t_next = g.t0;
+      }
+      return b;
+    };
+    auto ask_scales = [&](Batch& b) {
+      if ((uint32_t)b.page >= (uint32_t)p.batch.pages) b.page = -1;
+      if constexpr (FP8) {
+        if (b.page >= 0) {
+          b.k_scale = p.k_scale[(int64_t)b.page * p.Hk + b.h];
+          b.v_scale = p.v_scale[(int64_t)b.page * p.Hk + b.h];
         }
       }
-    } while (ok && g.next(p));
+    };
+    int slot = 0, use = 0, n = 0;        // K and V tiles take turns in the ring; tiles so far
+    bool ok = true;
+    const int per_box = kGroups / p.boxes;               // groups of a box
+    Batch now = ask_pages(), next = ask_pages();
+    ask_scales(now);
+    while (ok && now.n > 0) {
+      // a box is copied if somebody sees one of its groups; the lane of its first group copies it
+      int page = now.page;
+      if (per_box > 1) page = max(page, __shfl_xor_sync(0xffffffffu, page, 1));
+      if (per_box > 2) page = max(page, __shfl_xor_sync(0xffffffffu, page, 2));
+      if (per_box > 4) page = max(page, __shfl_xor_sync(0xffffffffu, page, 4));
+      const bool copies = page >= 0 && lane % per_box == 0;
+      const uint32_t going = __ballot_sync(0xffffffffu, copies);
+      const int key = now.t * kTileKeys + lane * kGroupKeys, row = key & ((1 << p.batch.page_shift) - 1);
+      // (a copy may finish before the barrier has been told to expect it: the phase is not over without that arrival)
+      auto copy = [&](int u, int kv, int slot) {
+        if (lane / kGroups == u && copies) {
+          constexpr int kSlab = kRowBytes > 128 ? 128 : kRowBytes;
+          unsigned char* dst = smem + slot * S::kTileBytes + (lane % kGroups) * kGroupKeys * kSlab;
+#pragma unroll
+          for (int sl = 0; sl < kRowBytes / kSlab; ++sl)
+            tma_load_4d(dst + sl * (kTileKeys * kSlab), kv ? &tmap_v : &tmap_k, full + slot, sl * (kSlab / S::kElt), row, now.h, page);
+        }
+      };
+      auto arrive = [&](int u, int slot) {
+        if (lane == 0) {
+          const int boxes = __popc((going >> (u * kGroups)) & ((1u << kGroups) - 1u));
+          if (boxes) mbar_expect_tx(full + slot, boxes * p.box_rows * kRowBytes);
+          else mbar_arrive(full + slot);
+        }
+      };
+      // the ring is empty at first: its copies do not wait for the first scales
+      const int ahead = n == 0 ? min(now.n, p.slots / 2) : 0;
+      for (int u = 0; u < ahead; ++u) {
+        copy(u, 0, 2 * u);
+        copy(u, 1, 2 * u + 1);
+      }
+      // the groups' notes (what they write over belongs to tiles that left the ring long ago)
+      {
+        GroupInfo info{1.0f, 0.0f, 1.0f, now.page >= 0};
+        if constexpr (FP8) {
+          const float v = fmaxf(now.v_scale, 5.4e-20f);    // 2^-64: a scale of zero stays finite
+          info.k = now.k_scale;
+          info.v_log2 = log2f(v);
+          info.v_inv = 1.0f / v;
+        }
+        s_info[(n * kGroups + lane) & (kInfoRing * kGroups - 1)] = info;
+      }
+      __syncwarp();
+      ask_scales(next);
+      const Batch after_next = ask_pages();
+      for (int u = 0; ok && u < now.n; ++u) {
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          if (u >= ahead) {
+            if (use > 0) ok = __all_sync(0xffffffffu, pipe_wait(empty + slot, (use - 1) & 1, s_abort, 1));
+            if (!ok) break;
+            copy(u, kv, slot);
+          }
+          arrive(u, slot);
+          if (++slot == p.slots) { slot = 0; ++use; }
+        }
+      }
+      n += now.n;
+      now = next;
+      next = after_next;
+    }
     // (nobody leaves before the copies have landed: the computing warps wait for every tile)
   } else {
     // ---------------------------------------------------------------------------------------------------- products
     const int g8 = lane >> 2, t4 = lane & 3;
     constexpr int kSteps = D / 16;                     // k-steps of the first product, m-tiles of the second
     constexpr int kChunkCh = 16 / S::kElt;             // channels of a 16-byte chunk
-    int stage = 0, use = 0, segments = 0;
+    int slot = 0, use = 0, segments = 0;
+    int at_info = warp * kPerWarp;                                // of the tile whose scores come next
     bool ok = true;
     do {
       // the rows' queries as the first product's B operand: lane (g8, t4) has channels of row g8
-      uint32_t qf[NT][kSteps][2];
+      constexpr int kQ = FP8 ? D / 32 * 4 : kSteps * 2;
+      uint32_t qf[NT][kQ];                             // bf16: k-step j has words 2j, 2j + 1; E4M3: step j's high parts 4j, 4j + 1, low parts 4j + 2, 4j + 3
       float c_row[NT][2];                              // of the accumulators' rows 2 t4 and 2 t4 + 1: logit -> log2 units
       int lo[NT][2], hi[NT][2];
 #pragma unroll
@@ -209,43 +279,37 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         const bool there = r < g.rows;
         const int token = there ? row / p.G : 0, head = there ? g.c.h * p.G + (row - token * p.G) : 0;
         const __nv_bfloat16* src = p.q + (int64_t)(g.c.seq.start + token) * p.q_stride_t + head * p.q_stride_h;
-        uint2 raw[kSteps];
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j) {
-          const int chunk = t4 + 4 * (j / (kChunkCh / 4));
-          raw[j] = there ? *reinterpret_cast<const uint2*>(src + chunk * kChunkCh + (j % (kChunkCh / 4)) * 4) : make_uint2(0u, 0u);
-        }
         float back = 1.0f;
         if constexpr (FP8) {
-          // fp16 queries: the row times the power of two that brings its largest entry to [1, 2)
-          uint32_t top = 0;
+          uint4 raw[D / 32];
 #pragma unroll
-          for (int j = 0; j < kSteps; ++j) {
-            const uint32_t w[2] = {raw[j].x, raw[j].y};
+          for (int j = 0; j < D / 32; ++j)
+            raw[j] = there ? *reinterpret_cast<const uint4*>(src + (t4 + 4 * (j / 2)) * 16 + (j & 1) * 8) : make_uint4(0u, 0u, 0u, 0u);
+          float top = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t a = (w[i] & 0x7fffu) << 16, b = w[i] & 0x7fff0000u;
-              if (a < 0x7f800000u) top = max(top, a);
-              if (b < 0x7f800000u) top = max(top, b);
-            }
+          for (int j = 0; j < D / 32; ++j) {
+            const uint32_t x[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = largest(top, x[i]);
           }
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const int e = min(max((int)(top >> 23), 1), 253);
-          back = __uint_as_float((uint32_t)e << 23);
-          const float to = __uint_as_float((uint32_t)(254 - e) << 23);
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const QueryScale s = query_scale(top);
+          back = s.back;
 #pragma unroll
-          for (int j = 0; j < kSteps; ++j) {
-            const uint32_t w[2] = {raw[j].x, raw[j].y};
+          for (int j = 0; j < D / 32; ++j) {
+            const uint32_t x[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const __half2 h = __floats2half2_rn(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xffff0000u) * to);
-              qf[nt][j][i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
+            for (int i = 0; i < 2; ++i) split_queries(x[2 * i], x[2 * i + 1], s.to, qf[nt][4 * j + i], qf[nt][4 * j + 2 + i]);
           }
         } else {
 #pragma unroll
-          for (int j = 0; j < kSteps; ++j) { qf[nt][j][0] = raw[j].x; qf[nt][j][1] = raw[j].y; }
+          for (int j = 0; j < kSteps; ++j) {
+            const int chunk = t4 + 4 * (j / (kChunkCh / 4));
+            const uint2 x = there ? *reinterpret_cast<const uint2*>(src + chunk * kChunkCh + (j % (kChunkCh / 4)) * 4) : make_uint2(0u, 0u);
+            qf[nt][2 * j] = x.x;
+            qf[nt][2 * j + 1] = x.y;
+          }
         }
         const int2 seen = there ? visible_keys(p.causal, g.c.seq.first_pos() + token, g.c.seq.len) : make_int2(0, 0);
 #pragma unroll
@@ -274,104 +338,110 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) o[i][nt][0] = o[i][nt][1] = o[i][nt][2] = o[i][nt][3] = 0.0f;
       }
-      for (int t = g.t0; t < g.t1; ++t) {
-        ok = __all_sync(0xffffffffu, mbar_wait(full + stage, use & 1, s_abort, p.status, 2));
-        if (!ok) break;
-        const GroupInfo info = s_info[stage * kGroups + warp];
-        const int key0 = t * kTileKeys + warp * kGroupKeys;
-        if (!info.usable) {                            // nothing here for any row
-          __syncwarp();
-          if (lane == 0) mbar_arrive(empty + stage);
-          if (++stage == p.stages) { stage = 0; ++use; }
-          continue;
-        }
-        const uint32_t s_k = smem_u32(smem + stage * S::kStageBytes), s_v = s_k + S::kTileBytes;
-        const int row0 = warp * kGroupKeys;
-        // S^T: the product's row 2 t + e (of 0..7) is key 4 t + e of the group, row 8 + 2 t + e key 4 t + 2 + e
-        float s[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
-        {
-          const int ka = row0 + 4 * (g8 >> 1) + (g8 & 1), kb = ka + 2;
-#pragma unroll
-          for (int c = 0; c < kRowBytes / 64; ++c) {
-            const uint4 va = lds16(s_k + chunk_offset<kRowBytes>(ka, t4 + 4 * c)), vb = lds16(s_k + chunk_offset<kRowBytes>(kb, t4 + 4 * c));
-            const uint32_t wa[4] = {va.x, va.y, va.z, va.w}, wb[4] = {vb.x, vb.y, vb.z, vb.w};
-#pragma unroll
-            for (int j = 0; j < kChunkCh / 4; ++j) {
-              uint32_t a[4];
-              if constexpr (FP8) {
-                a[0] = e4m3_to_half2(wa[j] & 0xffffu); a[2] = e4m3_to_half2(wa[j] >> 16);
-                a[1] = e4m3_to_half2(wb[j] & 0xffffu); a[3] = e4m3_to_half2(wb[j] >> 16);
-              } else {
-                a[0] = wa[2 * j]; a[2] = wa[2 * j + 1];
-                a[1] = wb[2 * j]; a[3] = wb[2 * j + 1];
-              }
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_16816<FP8>(s[nt], a, qf[nt][c * (kChunkCh / 4) + j][0], qf[nt][c * (kChunkCh / 4) + j][1]);
-            }
-          }
-        }
-        // V of keys 4 t4 .. 4 t4 + 3, channels D/8 g8 ..
-        constexpr int kVWords = D / 8 * S::kElt / 4;    // 32-bit words of a lane's channels: 2, 4 or 8
-        uint32_t vw[4][kVWords];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = row0 + 4 * t4 + i;
-          if constexpr (kVWords == 2) {
-            const uint2 w = lds8(s_v + chunk_offset<kRowBytes>(key, g8 >> 1) + (g8 & 1) * 8);
-            vw[i][0] = w.x; vw[i][1] = w.y;
-          } else {
-#pragma unroll
-            for (int c = 0; c < kVWords / 4; ++c) {
-              const uint4 w = lds16(s_v + chunk_offset<kRowBytes>(key, g8 * (kVWords / 4) + c));
-              vw[i][4 * c] = w.x; vw[i][4 * c + 1] = w.y; vw[i][4 * c + 2] = w.z; vw[i][4 * c + 3] = w.w;
-            }
-          }
-        }
+      constexpr int kVWords = D / 8 * S::kElt / 4;      // 32-bit words of a lane's channels: 2, 4 or 8
+      const int row0 = warp * (kPerWarp * kGroupKeys);
+      auto wait_full = [&] { return __all_sync(0xffffffffu, pipe_wait(full + slot, use & 1, s_abort, 2)) != 0; };
+      auto release = [&] {
         __syncwarp();
-        if (lane == 0) mbar_arrive(empty + stage);
-        if (++stage == p.stages) { stage = 0; ++use; }
+        if (lane == 0) mbar_arrive(empty + slot);
+        if (++slot == p.slots) { slot = 0; ++use; }
+      };
+      for (int t = g.t0; t < g.t1; ++t) {
+        ok = wait_full();
+        if (!ok) break;
+        GroupInfo info[kPerWarp];
+        float s[kPerWarp][NT][4];
+        {
+          // S^T: the product's row 2 t + e (of 0..7) is key 4 t + e of the group, row 8 + 2 t + e key 4 t + 2 + e
+          const uint32_t at = smem_u32(smem + slot * S::kTileBytes);
+          uint4 ka[kPerWarp][kRowBytes / 64], kb[kPerWarp][kRowBytes / 64];
+#pragma unroll
+          for (int u = 0; u < kPerWarp; ++u) {
+            const int key = row0 + u * kGroupKeys + 4 * (g8 >> 1) + (g8 & 1);
+#pragma unroll
+            for (int c = 0; c < kRowBytes / 64; ++c) {
+              ka[u][c] = lds16(at + chunk_offset<kRowBytes, kTileKeys>(key, t4 + 4 * c));
+              kb[u][c] = lds16(at + chunk_offset<kRowBytes, kTileKeys>(key + 2, t4 + 4 * c));
+            }
+            info[u] = s_info[at_info + u];
+          }
+          at_info = (at_info + kGroups) & (kInfoRing * kGroups - 1);
+          release();
+          [[maybe_unused]] float s_low[kPerWarp][NT][4];
+#pragma unroll
+          for (int u = 0; u < kPerWarp; ++u)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[u][nt][i] = s_low[u][nt][i] = 0.0f;
+#pragma unroll
+          for (int c = 0; c < kRowBytes / 64; ++c)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int u = 0; u < kPerWarp; ++u) {
+                const uint32_t a[4] = {j ? ka[u][c].z : ka[u][c].x, j ? kb[u][c].z : kb[u][c].x, j ? ka[u][c].w : ka[u][c].y, j ? kb[u][c].w : kb[u][c].y};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  if constexpr (FP8) {
+                    const uint32_t* q = qf[nt] + 4 * (2 * c + j);
+                    mma_16832(s[u][nt], a, q[0], q[1]);
+                    mma_16832(s_low[u][nt], a, q[2], q[3]);
+                  } else {
+                    mma_16816<false>(s[u][nt], a, qf[nt][2 * (2 * c + j)], qf[nt][2 * (2 * c + j) + 1]);
+                  }
+                }
+              }
+          if constexpr (FP8) {
+#pragma unroll
+            for (int u = 0; u < kPerWarp; ++u)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[u][nt][i] += s_low[u][nt][i];
+          }
+        }
         // t = logit + log2(v scale); keys a row does not see get -inf
-        float tt[NT][4];
+        const int key0 = t * kTileKeys + row0;
+        bool edge = key0 < all_lo || key0 + kPerWarp * kGroupKeys > all_hi;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) tt[nt][i] = fmaf(s[nt][i], c_row[nt][i & 1] * info.k, info.v_log2);
-        if (key0 < all_lo || key0 + kGroupKeys > all_hi) {
-          const int ka = key0 + 4 * (g8 >> 1) + (g8 & 1);
+        for (int u = 0; u < kPerWarp; ++u) {
+          edge = edge || !info[u].usable;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = ka + (i & 2);
-              if (key < lo[nt][i & 1] || key >= hi[nt][i & 1]) tt[nt][i] = -INFINITY;
-            }
-          // what no row sees may be anything, and 0 times that need not be 0
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = key0 + 4 * t4 + i;
-            if (key < g.c.item.lo || key >= g.c.item.hi) {
-#pragma unroll
-              for (int w = 0; w < kVWords; ++w) vw[i][w] = 0u;
-            }
-          }
+            for (int i = 0; i < 4; ++i) s[u][nt][i] = fmaf(s[u][nt][i], c_row[nt][i & 1] * info[u].k, info[u].v_log2);
         }
+        if (edge) {
+#pragma unroll
+          for (int u = 0; u < kPerWarp; ++u)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int key = key0 + u * kGroupKeys + 4 * (g8 >> 1) + (g8 & 1) + (i & 2);
+                if (key < lo[nt][i & 1] || key >= hi[nt][i & 1] || !info[u].usable) s[u][nt][i] = -INFINITY;
+              }
+        }
+        float top[NT][2];
         bool moves = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) moves = moves || tt[nt][i] > m[nt][i & 1] + kLazy;
+          for (int i = 0; i < 2; ++i) {
+            top[nt][i] = fmaxf(s[0][nt][i], s[0][nt][i + 2]);
+            if constexpr (kPerWarp > 1) top[nt][i] = fmaxf(top[nt][i], fmaxf(s[1][nt][i], s[1][nt][i + 2]));
+            moves = moves || top[nt][i] > m[nt][i] + kLazy;
+          }
         if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             float f[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              float top = fmaxf(tt[nt][i], tt[nt][i + 2]);
 #pragma unroll
-              for (int k = 4; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-              const float to = fmaxf(m[nt][i], top);
+              for (int k = 4; k < 32; k <<= 1) top[nt][i] = fmaxf(top[nt][i], __shfl_xor_sync(0xffffffffu, top[nt][i], k));
+              const float to = fmaxf(m[nt][i], top[nt][i]);
               f[i] = to == -INFINITY ? 1.0f : fast_exp2(m[nt][i] - to);
               m[nt][i] = to;
               l[nt][i] *= f[i];
@@ -382,54 +452,95 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
               for (int i = 0; i < 4; ++i) o[k][nt][i] *= f[i & 1];
           }
         }
-        uint32_t pf[NT][2];
+        uint32_t pf[kPerWarp][NT][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float w[4];
+        for (int u = 0; u < kPerWarp; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float ref = m[nt][i & 1];
-            w[i] = fast_exp2(tt[nt][i] - (ref == -INFINITY ? 0.0f : ref - kBase));
-          }
-          l[nt][0] = fmaf(w[0] + w[2], info.v_inv, l[nt][0]);
-          l[nt][1] = fmaf(w[1] + w[3], info.v_inv, l[nt][1]);
-          if constexpr (FP8) {
-            const __half2 a = __floats2half2_rn(w[0], w[1]), b = __floats2half2_rn(w[2], w[3]);
-            pf[nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
-            pf[nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
-          } else {
-            const __nv_bfloat162 a = __floats2bfloat162_rn(w[0], w[1]), b = __floats2bfloat162_rn(w[2], w[3]);
-            pf[nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
-            pf[nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
-          }
-        }
-        // O^T: m-tile i has channels D/8 g8 + 2i (rows g8) and + 2i + 1 (rows 8 + g8)
-        if constexpr (FP8) {
+          for (int nt = 0; nt < NT; ++nt) {
+            float w[4];
 #pragma unroll
-          for (int w = 0; w < kVWords; ++w) {
-            const uint32_t e01 = __byte_perm(vw[0][w], vw[1][w], 0x5140), f01 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
-            const uint32_t e23 = __byte_perm(vw[2][w], vw[3][w], 0x5140), f23 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
-            uint32_t a[4] = {e4m3_to_half2(e01 & 0xffffu), e4m3_to_half2(e01 >> 16), e4m3_to_half2(e23 & 0xffffu), e4m3_to_half2(e23 >> 16)};
-            uint32_t b[4] = {e4m3_to_half2(f01 & 0xffffu), e4m3_to_half2(f01 >> 16), e4m3_to_half2(f23 & 0xffffu), e4m3_to_half2(f23 >> 16)};
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_16816<true>(o[2 * w][nt], a, pf[nt][0], pf[nt][1]);
-              mma_16816<true>(o[2 * w + 1][nt], b, pf[nt][0], pf[nt][1]);
+            for (int i = 0; i < 4; ++i) {
+              const float ref = m[nt][i & 1];
+              w[i] = fast_exp2(s[u][nt][i] - (ref == -INFINITY ? 0.0f : ref - kBase));
+            }
+            l[nt][0] = fmaf(w[0] + w[2], info[u].v_inv, l[nt][0]);
+            l[nt][1] = fmaf(w[1] + w[3], info[u].v_inv, l[nt][1]);
+            if constexpr (FP8) {
+              const __half2 a = __floats2half2_rn(w[0], w[1]), b = __floats2half2_rn(w[2], w[3]);
+              pf[u][nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
+              pf[u][nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
+            } else {
+              const __nv_bfloat162 a = __floats2bfloat162_rn(w[0], w[1]), b = __floats2bfloat162_rn(w[2], w[3]);
+              pf[u][nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
+              pf[u][nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
             }
           }
-        } else {
+        // V of keys 4 t4 .. 4 t4 + 3 of each group, channels D/8 g8 ..
+        ok = wait_full();
+        if (!ok) break;
+        const uint32_t s_v = smem_u32(smem + slot * S::kTileBytes);
+        uint32_t vw[kPerWarp][4][kVWords];
+#pragma unroll
+        for (int u = 0; u < kPerWarp; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = row0 + u * kGroupKeys + 4 * t4 + i;
+            if constexpr (kVWords == 2) {
+              const uint2 w = lds8(s_v + chunk_offset<kRowBytes, kTileKeys>(key, g8 >> 1) + (g8 & 1) * 8);
+              vw[u][i][0] = w.x; vw[u][i][1] = w.y;
+            } else {
+#pragma unroll
+              for (int c = 0; c < kVWords / 4; ++c) {
+                const uint4 w = lds16(s_v + chunk_offset<kRowBytes, kTileKeys>(key, g8 * (kVWords / 4) + c));
+                vw[u][i][4 * c] = w.x; vw[u][i][4 * c + 1] = w.y; vw[u][i][4 * c + 2] = w.z; vw[u][i][4 * c + 3] = w.w;
+              }
+            }
+          }
+        if (edge) {
+          // what no row sees may be anything, and 0 times that need not be 0
+#pragma unroll
+          for (int u = 0; u < kPerWarp; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = key0 + u * kGroupKeys + 4 * t4 + i;
+              if (key < g.c.item.lo || key >= g.c.item.hi || !info[u].usable) {
+#pragma unroll
+                for (int w = 0; w < kVWords; ++w) vw[u][i][w] = 0u;
+              }
+            }
+        }
+        release();
+        // O^T: m-tile i has channels D/8 g8 + 2i (rows g8) and + 2i + 1 (rows 8 + g8)
+#pragma unroll
+        for (int u = 0; u < kPerWarp; ++u)
 #pragma unroll
           for (int w = 0; w < kVWords; ++w) {
-            uint32_t a[4] = {__byte_perm(vw[0][w], vw[1][w], 0x5410), __byte_perm(vw[0][w], vw[1][w], 0x7632),
-                             __byte_perm(vw[2][w], vw[3][w], 0x5410), __byte_perm(vw[2][w], vw[3][w], 0x7632)};
+            const uint32_t* v0 = vw[u][0];
+            const uint32_t* v1 = vw[u][1];
+            const uint32_t* v2 = vw[u][2];
+            const uint32_t* v3 = vw[u][3];
+            if constexpr (FP8) {
+              uint32_t a[4], b[4];
+              e4m3_to_half(__byte_perm(v0[w], v1[w], 0x5140), a[0], a[1]);
+              e4m3_to_half(__byte_perm(v2[w], v3[w], 0x5140), a[2], a[3]);
+              e4m3_to_half(__byte_perm(v0[w], v1[w], 0x7362), b[0], b[1]);
+              e4m3_to_half(__byte_perm(v2[w], v3[w], 0x7362), b[2], b[3]);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_16816<false>(o[w][nt], a, pf[nt][0], pf[nt][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                mma_16816<true>(o[2 * w][nt], a, pf[u][nt][0], pf[u][nt][1]);
+                mma_16816<true>(o[2 * w + 1][nt], b, pf[u][nt][0], pf[u][nt][1]);
+              }
+            } else {
+              const uint32_t a[4] = {__byte_perm(v0[w], v1[w], 0x5410), __byte_perm(v0[w], v1[w], 0x7632),
+                                     __byte_perm(v2[w], v3[w], 0x5410), __byte_perm(v2[w], v3[w], 0x7632)};
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_16816<false>(o[w][nt], a, pf[u][nt][0], pf[u][nt][1]);
+            }
           }
-        }
       }
       if (!ok) break;
       // ------------------------------------------------------------------------------------- the warps' parts together
-      if (segments > 0) ok = __all_sync(0xffffffffu, mbar_wait(taken, (segments - 1) & 1, s_abort, p.status, 3));
+      if (segments > 0) ok = __all_sync(0xffffffffu, pipe_wait(taken, (segments - 1) & 1, s_abort, 3));
       if (!ok) break;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -446,7 +557,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         }
       __syncwarp();
       if (lane == 0) mbar_arrive(merged);
-      ok = __all_sync(0xffffffffu, mbar_wait(merged, segments & 1, s_abort, p.status, 4));
+      ok = __all_sync(0xffffffffu, pipe_wait(merged, segments & 1, s_abort, 4));
       if (!ok) break;
       const int slot = 2 * worker + (g.first ? 0 : 1);
       constexpr int kPer = D / 8;                            // threads of a row, eight channels each
@@ -465,7 +576,12 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
           for (int j = 0; j < 8; ++j) acc[j] = fmaf(src[j], f, acc[j]);
         }
-        if (g.whole) {
+        if (CLUSTER && p.cluster > 1) {
+          float4* dst = reinterpret_cast<float4*>(s_o + r * S::kOPitch + ch);       // (in place of the first warp's, which this thread alone reads)
+          dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+          dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+          if (ch == 0) s_cta[r] = make_float2(top, sum);
+        } else if (CLUSTER || g.whole) {
           const int row = g.row0 + r, token = g.c.seq.start + row / p.G, head = g.c.h * p.G + row % p.G;
           const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
           uint32_t w[4];
@@ -483,17 +599,76 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           if (ch == 0) *reinterpret_cast<float2*>(p.part_ml + ((int64_t)slot * R + r) * 2) = make_float2(top, sum);
         }
       }
+      if constexpr (CLUSTER) break;
       __syncwarp();
       if (lane == 0) mbar_arrive(taken);
       ++segments;
     } while (g.next(p));
   }
+  if constexpr (CLUSTER) {
+    if (p.cluster > 1) {
+      // (every thread of the cluster comes here, whatever happened to it)
+      cluster_arrive();
+      cluster_wait();
+      const int rank = (int)blockIdx.x % p.cluster;
+      constexpr int kPer = D / 4;                            // threads of a row, four channels each
+      if (warp < kComputeWarps) {
+        for (int task = rank + p.cluster * (int)threadIdx.x; task < g.rows * kPer; task += p.cluster * 32 * kComputeWarps) {
+          const int r = task / kPer, ch = (task % kPer) * 4;
+          const uint32_t at_ml = smem_u32(s_cta + r), at_o = smem_u32(s_o + r * S::kOPitch + ch);
+          float top = -INFINITY, sum = 0.0f, acc[4] = {};
+#pragma unroll 8
+          for (int c = 0; c < p.cluster; ++c) {
+            const float2 ml = cluster_ld2(at_ml, c);
+            const float4 v = cluster_ld4(at_o, c);
+            const float to = fmaxf(top, ml.x), f = to == -INFINITY ? 0.0f : fast_exp2(ml.x - to), keep = to == -INFINITY ? 0.0f : fast_exp2(top - to);
+            sum = fmaf(ml.y, f, sum * keep);
+            acc[0] = fmaf(v.x, f, acc[0] * keep);
+            acc[1] = fmaf(v.y, f, acc[1] * keep);
+            acc[2] = fmaf(v.z, f, acc[2] * keep);
+            acc[3] = fmaf(v.w, f, acc[3] * keep);
+            top = to;
+          }
+          const int row = g.row0 + r, token = g.c.seq.start + row / p.G, head = g.c.h * p.G + row % p.G;
+          const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+          const __nv_bfloat162 a = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), b = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
+          *reinterpret_cast<uint2*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + ch) =
+              make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+          if (p.lse && ch == 0) p.lse[(int64_t)token * p.H + head] = sum == 0.0f ? -INFINITY : (top - kBase + log2f(sum)) * 0.6931471805599453f;
+        }
+      }
+      cluster_arrive();
+      cluster_wait();                                        // nobody leaves while others read its memory
+    }
+  }
+  if (threadIdx.x == 0) report_abort(p.status, *s_abort);
   if (*s_abort) __nanosleep(200000);      // let copies in flight land before the CTA's memory goes
 }
 
 // ------------------------------------------------------------------------------------------------------------ host side
 namespace {
 constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+// Who splits an item: a cluster of the returned number of CTAs, or (0) the line.
+//   A cluster adds up its parts at once (128-key tiles, 8 key heads, one sequence of 500 / 4000 / 16,000 keys: 6.2 / 8.4 / 15.1 us, line 9.3 / 11.7 /
+//   17.7), as many CTAs as one wave of two per SM holds, of up to sixteen where that leaves SMs to spare (16 of 8 items: 4000 keys 8.4 us, 8: 8.7;
+//   16,000 keys 15.1 and 17.8; more than a wave: 16 sequences of 1000 keys by 2 CTAs an item 10.5 us, by 4 16.1).
+//   Two of a long item's where one each would fill a wave: sequences seldom have one length (16 sequences of up to 4000 keys, 12 heads, E4M3:
+//   26.6 us, by one CTA 32.4, the line 33.6; all of one length 49.4, 41.3, 42.6).
+//   The line takes over where clusters leave SMs idle for long (32,000 keys: 21.4 us, clusters of 16 24.0) and where the
+//   items are more than a wave and long, whose lengths may differ (64 sequences of up to 8191 keys, 8 heads: 105 us, clusters of
+//   1 / 2 121 / 107; all of one length 179 and 169 / 184; of 2000 keys 55 and 50).
+int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame_tokens, int window, int tile_keys, int sms) {
+  const long long items = (long long)b.B * c.H;
+  long long keys = (long long)b.max_pages * c.page;                       // that an item may have
+  if (window > 0) keys = std::min(keys, (long long)(window + 1) * frame_tokens + b.max_new);
+  const long long tiles = (keys + tile_keys - 1) / tile_keys;
+  int n = items * 16 <= sms ? 16 : 8;
+  while (n > 1 && (items * n > std::max(2 * sms, 16) || n / 2 >= tiles)) n /= 2;
+  if (n == 1 && items <= 2 * sms && tiles >= 16) n = 2;
+  if (items > 2 * sms ? tiles >= 32 : items * n < sms && tiles > 12 * n) return 0;
+  return n;
+}
+
 // rows of an item, and stretches of the line: up to 16 rows per key head take this file's kernel, more the tensor cores' (cache_chunk.cu)
 struct Plan {
   int R, workers;
@@ -523,20 +698,29 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   using S = DecodeShape<D, FP8, NT>;
   CUtensorMap mk, mv;
   int rc;
-  p.box_rows = c.page < kTileKeys ? c.page : kTileKeys;
-  p.boxes = kTileKeys / p.box_rows;
+  p.box_rows = c.page < S::kTileKeys ? c.page : S::kTileKeys;
+  p.boxes = S::kTileKeys / p.box_rows;
   if ((rc = make_page_map(&mk, k_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
   if ((rc = make_page_map(&mv, v_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
+  const long long items = (long long)b.B * c.H;
+  p.cluster = cluster_of(c, b, p.causal.frame, p.causal.window, S::kTileKeys, p.workers / S::kPerSM);
+  const bool cluster = p.cluster > 0;
   // as deep a ring as the CTAs of an SM leave each other; fewer CTAs where a great many sequences leave no room for two tiles
+  // (the CTAs of an SM differ by a ring's depth at most: one alone on its SM could not be kept busier by more than twelve tiles)
+  const int listed = cluster ? 0 : b.B;
   for (int per = S::kPerSM; per > 0; --per) {
-    p.stages = (227 * 1024 / per - 1024 - S::fixed_bytes(b.B, 12)) / S::kStageBytes;
-    if (p.stages >= 2) break;
+    p.slots = (227 * 1024 / per - 1024 - S::fixed_bytes(listed, 16)) / S::kTileBytes;
+    if (p.slots >= 3) break;
   }
-  if (p.stages > 12) p.stages = 12;
-  if (p.stages < 2) return SPARKATTN_E_UNSUPPORTED_SHAPE;
-  const int smem = p.stages * S::kStageBytes + S::fixed_bytes(b.B, p.stages);
-  auto kern = cache_decode_kernel<D, FP8, NT>;
+  if (p.slots > 16) p.slots = 16;
+  if (p.slots < 3) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  const int smem = p.slots * S::kTileBytes + S::fixed_bytes(listed, p.slots);
+  auto kern = cluster ? cache_decode_kernel<D, FP8, NT, true> : cache_decode_kernel<D, FP8, NT, false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
+  if (cluster) {
+    if (p.cluster > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SPARKATTN_E_CUDA;
+    return launch_clustered(kern, dim3((unsigned)((items + 1) * p.cluster)), kDecodeThreads, smem, true, p.cluster, stream, mk, mv, p);
+  }
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kDecodeThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
   return launch_kernel(combine_kernel<D, S::R>, dim3(p.workers - 1), kCombineThreads, 0, true, stream, p);
 }

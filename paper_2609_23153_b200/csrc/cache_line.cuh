@@ -7,6 +7,9 @@
 // Items stand in the order (sequence, key head, row tile).
 #pragma once
 
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
 #include "cache.h"
 
 namespace sparkattn {
@@ -29,7 +32,8 @@ struct CacheFwdParams {
   int box_rows, boxes;           // keys of one TMA box, boxes of a tile
   int least;                     // tiles a stretch has at least
   int workers;                   // stretches
-  int stages;
+  int slots;                     // K and V tiles that a CTA's ring holds
+  int cluster;                   // CTAs of an item's cluster; 0: the line
   int32_t* status;
   struct Border* borders;        // [workers]
   float* part_ml;                // [2 workers][R][2] reference, sum
@@ -197,6 +201,25 @@ struct Stretch {
     rows = min(R, c.seq.n * p.G - row0);
     x += until - c.at;
   }
+  // instead: run `rank` of `ranks` equal runs of the item (b, h), which has all its rows in one tile; false if it has none
+  __device__ __forceinline__ bool run_of(const CacheFwdParams& p, int b, int h, int rank, int ranks) {
+    c.b = b;
+    c.h = h;
+    c.rt = c.at = 0;
+    c.row_tiles = 1;
+    c.seq = sequence_of(p.batch, b);
+    if (c.seq.n == 0) return false;
+    c.item = L::item_of(p, c.seq, 0);
+    const int each = (c.item.tiles + ranks - 1) / ranks, end_tile = c.item.first + c.item.tiles;
+    t0 = min(c.item.first + rank * each, end_tile);
+    t1 = min(t0 + each, end_tile);
+    row0 = 0;
+    rows = c.seq.n * p.G;
+    x = end = 0;
+    first = true;
+    whole = false;
+    return true;
+  }
   // false behind the last segment
   __device__ __forceinline__ bool next(const CacheFwdParams& p) {
     if (x >= end) return false;
@@ -206,6 +229,38 @@ struct Stretch {
     return true;
   }
 };
+
+// Queries against E4M3 keys: a row times the power of two that brings its largest entry to [128, 256), as two E4M3 parts,
+// high = rne(x) and low = rne(x - high).  A bf16 has eight significant digits and an E4M3 four, so x - high has at most four and
+// the sum of the parts is x, but for entries below 2^-9 of the row's largest, whose low part falls into E4M3's subnormal
+// numbers: off by at most 2^-18 of the largest.  Products of two E4M3 numbers are exact in the tensor core and their sums were found to be
+// fp32's (off by at most 2^-25 of the sum of the magnitudes, m16n8k32 over 128 channels).  Keys stay codes, and the two products
+// take as long as one with 16-bit operands.  A row with an infinity or a NaN in it gives NaN.
+struct QueryScale {
+  float to, back;
+};
+__device__ __forceinline__ float largest(float top, uint32_t two_bf16) {
+  // (integer order: NaN above infinity above the finite)
+  const uint32_t a = (two_bf16 & 0x7fffu) << 16, b = two_bf16 & 0x7fff0000u;
+  return __uint_as_float(max(max(a, b), __float_as_uint(top)));
+}
+__device__ __forceinline__ QueryScale query_scale(float top) {
+  const int e = min(max((int)(__float_as_uint(top) >> 23), 8), 254);
+  return {__uint_as_float((uint32_t)(261 - e) << 23), __float_as_uint(top) < 0x7f800000u ? __uint_as_float((uint32_t)(e - 7) << 23) : __uint_as_float(0x7fffffffu)};
+}
+// four channels (two bf16 pairs) as four codes of high parts and four of low parts
+__device__ __forceinline__ void split_queries(uint32_t x, uint32_t y, float to, uint32_t& high, uint32_t& low) {
+  const float v[4] = {__uint_as_float(x << 16) * to, __uint_as_float(x & 0xffff0000u) * to, __uint_as_float(y << 16) * to, __uint_as_float(y & 0xffff0000u) * to};
+  uint32_t h[2], l[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    h[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * i], v[2 * i + 1]), __NV_SATFINITE, __NV_E4M3);
+    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h[i], __NV_E4M3)));
+    l[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * i] - f.x, v[2 * i + 1] - f.y), __NV_SATFINITE, __NV_E4M3);
+  }
+  high = h[0] | h[1] << 16;
+  low = l[0] | l[1] << 16;
+}
 
 // What the lanes of the copying warp look up for a group of 16 keys each: the page and the scales.
 template <bool FP8>

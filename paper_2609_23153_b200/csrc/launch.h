@@ -11,23 +11,35 @@
 namespace sparkattn {
 
 // Launches a kernel; with `overlap` it may start while the kernel before it on the stream is draining (it then calls
-// pdl_wait, common.cuh, before it touches memory).
+// pdl_wait, common.cuh, before it touches memory); `cluster` CTAs form a thread-block cluster.
 template <typename... Params, typename... Args>
-inline int launch_kernel(void (*kern)(Params...), dim3 grid, unsigned threads, size_t smem, bool overlap, cudaStream_t stream,
-                         const Args&... args) {
+inline int launch_clustered(void (*kern)(Params...), dim3 grid, unsigned threads, size_t smem, bool overlap, int cluster, cudaStream_t stream,
+                            const Args&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = overlap ? 1 : 0;
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
+    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
   if (cudaLaunchKernelEx(&cfg, kern, Params(args)...) == cudaSuccess) return SPARKATTN_OK;
   cudaGetLastError();          // reported here: a later call's own check must not find it again
   return SPARKATTN_E_CUDA;
+}
+
+template <typename... Params, typename... Args>
+inline int launch_kernel(void (*kern)(Params...), dim3 grid, unsigned threads, size_t smem, bool overlap, cudaStream_t stream,
+                         const Args&... args) {
+  return launch_clustered(kern, grid, threads, smem, overlap, 1, stream, args...);
 }
 
 // quant.cu
