@@ -452,7 +452,8 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
               for (int i = 0; i < 4; ++i) o[k][nt][i] *= f[i & 1];
           }
         }
-        uint32_t pf[kPerWarp][NT][2];
+        // bf16 pages: the weights in two bf16 parts, since one (2^-8) would add as much to the result's error as its own rounding does
+        uint32_t pf[kPerWarp][NT][FP8 ? 2 : 4];
 #pragma unroll
         for (int u = 0; u < kPerWarp; ++u)
 #pragma unroll
@@ -471,8 +472,12 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
               pf[u][nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
             } else {
               const __nv_bfloat162 a = __floats2bfloat162_rn(w[0], w[1]), b = __floats2bfloat162_rn(w[2], w[3]);
+              const float2 fa = __bfloat1622float2(a), fb = __bfloat1622float2(b);
+              const __nv_bfloat162 la = __floats2bfloat162_rn(w[0] - fa.x, w[1] - fa.y), lb = __floats2bfloat162_rn(w[2] - fb.x, w[3] - fb.y);
               pf[u][nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
               pf[u][nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
+              pf[u][nt][2] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&la));
+              pf[u][nt][3] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&lb));
             }
           }
         // V of keys 4 t4 .. 4 t4 + 3 of each group, channels D/8 g8 ..
@@ -534,7 +539,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
               const uint32_t a[4] = {__byte_perm(v0[w], v1[w], 0x5410), __byte_perm(v0[w], v1[w], 0x7632),
                                      __byte_perm(v2[w], v3[w], 0x5410), __byte_perm(v2[w], v3[w], 0x7632)};
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_16816<false>(o[w][nt], a, pf[u][nt][0], pf[u][nt][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                mma_16816<false>(o[w][nt], a, pf[u][nt][0], pf[u][nt][1]);
+                mma_16816<false>(o[w][nt], a, pf[u][nt][2], pf[u][nt][3]);
+              }
             }
           }
       }
