@@ -2,19 +2,24 @@
 // cache on the tensor cores, bf16 or E4M3 pages.
 //
 // The products, 4 d flops per (row, key), bound it, so an item is 256 query rows of one (sequence, key head): two M = 128
-// tiles that share every key tile, since fetching a tile and turning its codes into operands costs shared-memory
+// tiles that share every key tile, since fetching a tile and turning codes into operands costs shared-memory
 // bandwidth, which the products themselves use to three quarters (Q and K from shared memory: 64 KB per 128 x 128 x 128).
+// SPLIT: where no sequence has more than 128 rows, an item is one M tile, and the two halves of the pipeline take its key tiles in
+// turns and add up at the end; each would otherwise wait for itself most of the time.
 // The line of all items' key tiles (cache_line.cuh) is cut evenly over one CTA per SM.  Roles:
 //   warp 0       TMA producer: pages of K and of V, scales, one descriptor per 16 keys
-//   warp 1       issues S_g = Q_g K^T and O_g += P_g V (tcgen05, accumulators in TMEM: S0 | S1 | O0 | O1)
-//   warps 4-7    E4M3: codes -> fp16 operand tiles (exact).  Both: V rows that no row of the item sees become zeros, since
-//                a page holds anything behind its sequence's last token, and 0 times that need not be 0
-//   warps 8-11, 12-15   softmax of tile 0 / 1, a thread per row: S from TMEM, weights back over the same columns as the second product's
+//   warp 1       issues S_g = Q K^T and O_g += P_g V (tcgen05, accumulators in TMEM: S0 | S1 | O0 | O1)
+//   warps 4-7    E4M3: V's codes -> fp16 operand tiles (exact), 64-channel heads K's as well.  Both: V rows that no row of the item
+//                sees become zeros, since a page holds anything behind its sequence's last token, and 0 times that need not be 0
+//   warps 8-11, 12-15   softmax of half 0 / 1, a thread per row: S from TMEM, weights back over the same columns as the second product's
 //                operand, running reference (lazy: O is rescaled only when a weight would pass 2^10), output
 // While one softmax warpgroup works on its S, the tensor core runs the other one's PV and next S; tcgen05.mma of one thread
 // run in the order of issue, so S_g of the next tile may overwrite the columns that PV_g has read its P from.
-// E4M3: Q, P and V are fp16 (the queries scaled by a power of two per row, the weights by 2^5 at the reference), and V's scale
-// is part of the exponent: t = logit + log2(v_scale), the row sum adds weight / v_scale.  bf16 pages: bf16 throughout.
+// E4M3, 128 channels: K's codes are the first product's operand as they are, against the queries in two E4M3 parts
+// (split_queries): twice as many products at twice the rate.  P and V are fp16 (the weights 2^5 at the reference), and V's scale is part of the
+// exponent: t = logit + log2(v_scale), the row sum adds weight / v_scale.  bf16 pages: bf16 throughout.
+// (A quarter of the exponentials as a polynomial of degree 4 on the FMA pipe, to spare the special-function unit: 870 us
+// either way for three frames of 1560 tokens over 32,760 keys, 710 instead of 672 for four prompts.)
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -27,45 +32,59 @@
 namespace sparkattn {
 
 constexpr int kChunkKeys = 128, kChunkThreads = 512;
+constexpr int kChunkOver = 3;                                   // tiles that the beginning and the end of an item take as long as
 constexpr int kChunkGroups = kChunkKeys / 16;
 constexpr int kSoftRegs = 192, kConvRegs = 72, kCtrlRegs = 56;      // 2 x 128 x 192 + 128 x 72 + 128 x 56 = 512 x 128
-constexpr int kInfoRing = 4;
+constexpr int kChunkInfoRing = 8;                                   // tiles whose descriptors are kept: the K ring and what is still worked on
 
 template <int D, bool FP8>
 struct ChunkShape {
+  static constexpr bool kRawK = FP8 && D == 128;            // K's codes are an operand
+  static constexpr bool kConvK = FP8 && !kRawK;
   static constexpr int kOperand = kChunkKeys * D * 2;       // a 128 x D tile of 16-bit operands: slabs of 64 channels
-  static constexpr int kRaw = kChunkKeys * D;               // the same as E4M3 codes
-  static constexpr int kOffK = 2 * kOperand, kOffV = 4 * kOperand, kOffRaw = 6 * kOperand;
-  static constexpr int kOffMisc = kOffRaw + (FP8 ? 2 * kRaw : 0);
-  static constexpr int kMisc = 256 /* barriers */ + kInfoRing * kChunkGroups * (int)sizeof(GroupInfo) + 128;
+  static constexpr int kCodes = kChunkKeys * D;             // the same as E4M3 codes
+  static constexpr int kQ = kOperand;                       // of one M tile (kRawK: high parts, then low parts)
+  static constexpr int kK = kRawK ? kCodes : kOperand;
+  static constexpr int RK = kRawK ? 3 : 2, RV = 2;          // rings: K operands, V operands (and V codes)
+  static constexpr int kOffK = 2 * kQ, kOffV = kOffK + RK * kK, kOffRaw = kOffV + RV * kOperand;      // raw: V codes, then (kConvK) K codes
+  static constexpr int kOffMisc = kOffRaw + (FP8 ? RV * kCodes : 0) + (kConvK ? kCodes : 0);
+  static constexpr int kMisc = 256 /* barriers */ + kChunkInfoRing * kChunkGroups * (int)sizeof(GroupInfo) + 128 + 128 * 8 /* SPLIT: row sums */;
   static constexpr int kBytes = kOffMisc + kMisc;
 };
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool SPLIT>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                    const __grid_constant__ CacheFwdParams p) {
   using C = ChunkShape<D, FP8>;
-  using L = Line<kChunkRows, kChunkKeys>;
-  constexpr int kSlab = kChunkKeys * 128;                    // bytes of 64 operand channels
+  constexpr int R = SPLIT ? 128 : 256;
+  using L = Line<R, kChunkKeys, kChunkOver>;
+  constexpr int kSlab = kChunkKeys * 128;                    // bytes of 64 16-bit channels, or of 128 codes
+  constexpr int RK = C::RK, RV = C::RV;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* sQ = smem;
   unsigned char* sK = smem + C::kOffK;
   unsigned char* sV = smem + C::kOffV;
   unsigned char* sRaw = smem + C::kOffRaw;
+  unsigned char* sRawK = sRaw + RV * C::kCodes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kOffMisc);
-  uint64_t* q_full = bars;            // [2] 128 arrivals: the item's queries are in shared memory
-  uint64_t* k_full = bars + 2;        // [2] operand K tile (E4M3: 128 arrivals; bf16: its copies)
-  uint64_t* k_free = bars + 4;        // [2] the S products that read it are complete
-  uint64_t* v_full = bars + 6;        // [2] 128 arrivals
-  uint64_t* v_free = bars + 8;        // [2] the PV products that read it are complete
-  uint64_t* raw_full = bars + 10;     // [2] E4M3: codes of a K (0) or V (1) tile; bf16: [slot] the copies of a V tile
-  uint64_t* raw_free = bars + 12;     // [2] E4M3, 128 arrivals
-  uint64_t* s_full = bars + 14;       // [2] S_g complete: the product's arrival and its issuer's (who has seen the tile's descriptor)
-  uint64_t* p_full = bars + 16;       // [2] 128 arrivals: weights written, S_g read
-  uint64_t* pv_done = bars + 18;      // [2]
+  uint64_t* q_full = bars;            // [2] the item's queries are in shared memory (SPLIT: [0], both warpgroups')
+  uint64_t* k_full = bars + 2;        // [RK] operand K tile (its copies; kConvK: 128 arrivals)
+  uint64_t* k_free = bars + 5;        // [RK] the S products that read it are complete
+  uint64_t* v_full = bars + 8;        // [RV] 128 arrivals
+  uint64_t* v_free = bars + 10;       // [RV] the PV products that read it are complete
+  uint64_t* raw_full = bars + 12;     // [RV] the copies of a V tile (E4M3: as codes)
+  uint64_t* raw_free = bars + 14;     // [RV] E4M3, 128 arrivals
+  uint64_t* rawk_full = bars + 16;    // kConvK: the copies of a K tile
+  uint64_t* rawk_free = bars + 17;
+  uint64_t* s_full = bars + 18;       // [2] S_g complete: the product's arrival and its issuer's (who has seen the tile's descriptor)
+  uint64_t* p_full = bars + 20;       // [2] 128 arrivals: weights written, S_g read
+  uint64_t* pv_done = bars + 22;      // [2]
+  uint64_t* sums_full = bars + 24;    // SPLIT, 128 arrivals: warpgroup 1 has left its row sums, and its O is complete
+  uint64_t* sums_free = bars + 25;    // SPLIT, 128 arrivals: they have been taken
   GroupInfo* s_info = reinterpret_cast<GroupInfo*>(bars + 32);          // [ring][groups]
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_info + kInfoRing * kChunkGroups);
+  float2* s_sums = reinterpret_cast<float2*>(s_info + kChunkInfoRing * kChunkGroups);      // [128]
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_sums + 128);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int* s_bad = reinterpret_cast<int*>(s_tmem + 2);
   int* s_warp = s_bad + 2;            // [16]
@@ -75,12 +94,14 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(q_full + i, 128);
-      mbar_init(k_full + i, FP8 ? 128 : 1); mbar_init(k_free + i, 1);
+      mbar_init(q_full + i, SPLIT ? 256 : 128);
       mbar_init(v_full + i, 128); mbar_init(v_free + i, 1);
       mbar_init(raw_full + i, 1); mbar_init(raw_free + i, 128);
       mbar_init(s_full + i, 2); mbar_init(p_full + i, 128); mbar_init(pv_done + i, 1);
     }
+    for (int i = 0; i < RK; ++i) { mbar_init(k_full + i, C::kConvK ? 128 : 1); mbar_init(k_free + i, 1); }
+    mbar_init(rawk_full, 1); mbar_init(rawk_free, 128);
+    mbar_init(sums_full, 128); mbar_init(sums_free, 128);
     mbar_fence_init();
     *s_abort = 0;
   }
@@ -98,7 +119,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const long long begin = (long long)((int)blockIdx.x - 1) * share;
   const bool works = blockIdx.x > 0 && begin < total;
   const int x0 = works ? (int)begin : 0, x1 = works ? (int)min(begin + share, (long long)total) : 0;
-  Stretch<kChunkRows, kChunkKeys> g;
+  Stretch<R, kChunkKeys, kChunkOver> g;
   if (works) g.begin(p, s_prefix, x0, x1);
   if (blockIdx.x > 0 && threadIdx.x == 0) note_border(p, (int)blockIdx.x - 1, works, share, g);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // tiles go where the line's beginnings lie
@@ -126,7 +147,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const GroupInfo info = info_n;
         if (t + kBatch < g.t1) look_up(t + kBatch);
         for (int u = 0; ok && u < kBatch && t + u < g.t1; ++u, ++n) {
-          const int slot = n & 1;
           const int per = kChunkGroups / p.boxes;
           const int box = lane % p.boxes, src = u * kChunkGroups + box * per;
           int box_page = -1;
@@ -134,16 +154,16 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           const bool copies = lane < p.boxes && box_page >= 0;
           const int going = __popc(__ballot_sync(0xffffffffu, copies));
           const int key = (t + u) * kChunkKeys + box * p.box_rows, row = key & ((1 << p.batch.page_shift) - 1);
-          // K, then V.  E4M3: both have one slot of codes; bf16: they land where the products read them
+          // K, then V: as codes that are an operand or become one, or (bf16) where the products read them
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
-            uint64_t* freed = FP8 ? raw_free + kv : (kv ? v_free : k_free) + slot;
-            const int uses = FP8 ? n : n >> 1;               // how often the slot has been filled
+            const int slot = kv ? n % RV : C::kConvK ? 0 : n % RK, uses = kv ? n / RV : C::kConvK ? n : n / RK;
+            uint64_t* freed = kv ? (FP8 ? raw_free : v_free) + slot : C::kConvK ? rawk_free : k_free + slot;
+            uint64_t* full = kv ? raw_full + slot : C::kConvK ? rawk_full : k_full + slot;
             if (uses > 0) ok = __all_sync(0xffffffffu, pipe_wait(freed, (uses - 1) & 1, s_abort, 1 + kv));
             if (!ok) break;
-            if (kv == 0 && lane / kChunkGroups == u) s_info[(n & (kInfoRing - 1)) * kChunkGroups + lane % kChunkGroups] = info;
+            if (kv == 0 && lane / kChunkGroups == u) s_info[(n & (kChunkInfoRing - 1)) * kChunkGroups + lane % kChunkGroups] = info;
             __syncwarp();
-            uint64_t* full = FP8 ? raw_full + kv : (kv ? raw_full : k_full) + slot;
             if (lane == 0) {
               if (going) mbar_expect_tx(full, going * p.box_rows * D * (FP8 ? 1 : 2));
               else mbar_arrive(full);
@@ -152,7 +172,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (copies) {
               const CUtensorMap* map = kv ? &tmap_v : &tmap_k;
               if constexpr (FP8) {
-                tma_load_4d(sRaw + kv * C::kRaw + box * p.box_rows * D, map, full, 0, row, g.c.h, box_page);
+                unsigned char* dst = kv ? sRaw + slot * C::kCodes : C::kConvK ? sRawK : sK + slot * C::kK;
+                tma_load_4d(dst + box * p.box_rows * D, map, full, 0, row, g.c.h, box_page);
               } else {
 #pragma unroll
                 for (int sl = 0; sl < D / 64; ++sl)
@@ -165,121 +186,156 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     } while (ok && g.next(p));
   } else if (warp == 1) {
     // ------------------------------------------------------------------------------------------------- products
-    constexpr uint32_t idesc_s = make_idesc(FP8 ? 0u : 1u, 128, kChunkKeys, false);
+    constexpr uint32_t idesc_s = make_idesc(FP8 ? 0u : 1u, 128, kChunkKeys, false);       // (E4M3 and fp16 are both 0, each in its kind)
     constexpr uint32_t idesc_o = make_idesc(FP8 ? 0u : 1u, 128, D, true);
     const uint32_t k_hi = (uint32_t)(make_smem_desc_sw128(0, 16) >> 32);
     const uint32_t q_lo = (uint32_t)make_smem_desc_sw128(smem_u32(sQ), 16), k_lo = (uint32_t)make_smem_desc_sw128(smem_u32(sK), 16);
     const uint32_t v_hi = (uint32_t)(make_smem_desc_sw128(0, kSlab) >> 32);
     const uint32_t v_lo = (uint32_t)make_smem_desc_sw128(smem_u32(sV), kSlab);
-    int n = 0;
-    uint32_t done[2] = {0, 0};                                // tiles of warpgroup 0, 1 so far (the second sits out items of up to 128 rows)
-    uint32_t seg[2] = {0, 0};
+    int n = 0;                                                // tiles in front of the segment
+    uint32_t done[2] = {0, 0}, loaded[2] = {0, 0};            // weights taken and queries seen of half 0, 1
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity, int id) { return __all_sync(0xffffffffu, pipe_wait(bar, parity, s_abort, id)) != 0; };
-    do {
-      const int tiles = g.t1 - g.t0, groups = g.rows > 128 ? 2 : 1;
-      auto s_product = [&](int w, int at) {                   // S_w of tile `at`
-        if (elect_one()) {
-          const uint32_t qa = q_lo + ((w * C::kOperand) >> 4), ka = k_lo + (((at & 1) * C::kOperand) >> 4);
+    // S of tile `at` for half w; `last`: nothing else reads the K tile
+    auto s_product = [&](int w, int at, bool last) {
+      tc_fence_after();
+      if (elect_one()) {
+        const uint32_t qa = q_lo + (((SPLIT ? 0 : w) * C::kQ) >> 4), ka = k_lo + (((at % RK) * C::kK) >> 4);
+        if constexpr (C::kRawK) {
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              mma_ss<true>(tmem + w * 128, make_desc(qa + ((part * kSlab + kk * 32) >> 4), k_hi), make_desc(ka + ((kk * 32) >> 4), k_hi), idesc_s,
+                           (part | kk) != 0 ? 1u : 0u);
+        } else {
 #pragma unroll
           for (int sl = 0; sl < D / 64; ++sl)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
               mma_ss<false>(tmem + w * 128, make_desc(qa + ((sl * kSlab + kk * 32) >> 4), k_hi), make_desc(ka + ((sl * kSlab + kk * 32) >> 4), k_hi),
                             idesc_s, (sl | kk) != 0 ? 1u : 0u);
-          tc_commit(s_full + w);
-          mbar_arrive(s_full + w);
-          if (w == groups - 1) tc_commit(k_free + (at & 1));
         }
-        __syncwarp();
-      };
-      ok = wait(k_full + (n & 1), (n >> 1) & 1, 3);
-      for (int w = 0; ok && w < groups; ++w) {
-        ok = wait(q_full + w, seg[w] & 1, 4);
-        if (!ok) break;
-        ++seg[w];
-        tc_fence_after();
-        s_product(w, n);
+        tc_commit(s_full + w);
+        mbar_arrive(s_full + w);
+        if (last) tc_commit(k_free + at % RK);
       }
-      for (int i = 0; ok && i < tiles; ++i, ++n) {
-        ok = wait(v_full + (n & 1), (n >> 1) & 1, 5);
-        for (int w = 0; ok && w < groups; ++w) {
-          ok = wait(p_full + w, done[w] & 1, 6);
-          if (!ok) break;
-          ++done[w];
-          tc_fence_after();
-          if (elect_one()) {
-            const uint32_t va = v_lo + (((n & 1) * C::kOperand) >> 4);
+      __syncwarp();
+    };
+    // O of half w plus the weights times tile `at` (first: instead of what O held)
+    auto o_product = [&](int w, int at, bool first, bool last) {
+      tc_fence_after();
+      if (elect_one()) {
+        const uint32_t va = v_lo + (((at % RV) * C::kOperand) >> 4);
 #pragma unroll
-            for (int kk = 0; kk < kChunkKeys / 16; ++kk)
-              mma_ts<false>(tmem + 256 + w * 128, tmem + w * 128 + kk * 8, make_desc(va + ((kk * 16 * 128) >> 4), v_hi), idesc_o,
-                            (i == 0 && kk == 0) ? 0u : 1u);
-            tc_commit(pv_done + w);
-            if (w == groups - 1) tc_commit(v_free + (n & 1));
+        for (int kk = 0; kk < kChunkKeys / 16; ++kk)
+          mma_ts<false>(tmem + 256 + w * 128, tmem + w * 128 + kk * 8, make_desc(va + ((kk * 16 * 128) >> 4), v_hi), idesc_o, first && kk == 0 ? 0u : 1u);
+        tc_commit(pv_done + w);
+        if (last) tc_commit(v_free + at % RV);
+      }
+      __syncwarp();
+    };
+    do {
+      const int tiles = g.t1 - g.t0;
+      if (tiles == 0) continue;
+      if constexpr (SPLIT) {
+        // half i & 1 takes tile i
+        ok = wait(q_full, loaded[0]++ & 1, 4);
+        for (int i = 0; ok && i < min(tiles, 2); ++i) {
+          ok = wait(k_full + (n + i) % RK, ((n + i) / RK) & 1, 3);
+          if (ok) s_product(i, n + i, true);
+        }
+        for (int i = 0; ok && i < tiles; ++i) {
+          const int w = i & 1;
+          ok = wait(v_full + (n + i) % RV, ((n + i) / RV) & 1, 5) && wait(p_full + w, done[w]++ & 1, 6);
+          if (!ok) break;
+          o_product(w, n + i, i < 2, true);
+          if (i + 2 < tiles) {
+            ok = wait(k_full + (n + i + 2) % RK, ((n + i + 2) / RK) & 1, 7);
+            if (ok) s_product(w, n + i + 2, true);
           }
-          __syncwarp();
-          if (i + 1 < tiles) {
-            if (w == 0) ok = wait(k_full + ((n + 1) & 1), ((n + 1) >> 1) & 1, 7);
+        }
+      } else {
+        const int halves = g.rows > 128 ? 2 : 1;
+        ok = wait(k_full + n % RK, (n / RK) & 1, 3);
+        for (int w = 0; ok && w < halves; ++w) {
+          ok = wait(q_full + w, loaded[w]++ & 1, 4);
+          if (ok) s_product(w, n, w == halves - 1);
+        }
+        for (int i = 0; ok && i < tiles; ++i) {
+          ok = wait(v_full + (n + i) % RV, ((n + i) / RV) & 1, 5);
+          for (int w = 0; ok && w < halves; ++w) {
+            ok = wait(p_full + w, done[w]++ & 1, 6);
             if (!ok) break;
-            tc_fence_after();
-            s_product(w, n + 1);
+            o_product(w, n + i, i == 0, w == halves - 1);
+            if (i + 1 < tiles) {
+              if (w == 0) ok = wait(k_full + (n + i + 1) % RK, ((n + i + 1) / RK) & 1, 7);
+              if (ok) s_product(w, n + i + 1, w == halves - 1);
+            }
           }
         }
       }
+      n += tiles;
     } while (ok && g.next(p));
   } else if (warp >= 4 && warp < 8) {
     // -------------------------------------------------------------------------------------------------- operands
     const int tid = threadIdx.x - 128;
     int n = 0;
     bool ok = true;
+    // a tile of codes as fp16 operands; rows outside [lo, hi) and of groups that nobody sees as zeros
+    auto convert = [&](const unsigned char* codes, unsigned char* operand, const GroupInfo* info, int lo, int hi) {
+      const uint32_t raw = smem_u32(codes), to = smem_u32(operand);
+      constexpr int kCh = D / 16, kRowsAtOnce = 128 / kCh;                // 16-code chunks of a row
+      const int c = tid % kCh;
+      const bool swap = D == 128 && c >= 4;                               // (the lanes of a row write eight different banks at a time)
+#pragma unroll 4
+      for (int r0 = 0; r0 < kChunkKeys; r0 += kRowsAtOnce) {
+        const int r = r0 + tid / kCh;
+        const uint32_t from = D == 128 ? raw + r * 128 + ((c ^ (r & 7)) << 4) : raw + r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from));
+        if (info != nullptr && (r < lo || r >= hi || !info[r / 16].usable)) v = make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t x[4] = {swap ? v.z : v.x, swap ? v.w : v.y, swap ? v.x : v.z, swap ? v.y : v.w};
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e4m3_to_half(x[i], h[2 * i], h[2 * i + 1]);
+        const uint32_t dst = to + (c >> 2) * kSlab + r * 128;
+        const int ck = (c & 3) * 2;
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + (((ck + swap) ^ (r & 7)) << 4)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + (((ck + !swap) ^ (r & 7)) << 4)), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+      }
+    };
     do {
       for (int t = g.t0; ok && t < g.t1; ++t, ++n) {
-        const int slot = n & 1;
-        // rows of the V tile that may be anything
+        // rows of the V tile that may be anything lie outside these
         const int z_lo = g.c.item.lo - t * kChunkKeys, z_hi = g.c.item.hi - t * kChunkKeys;
-        if constexpr (FP8) {
-#pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) {
-            ok = __all_sync(0xffffffffu, pipe_wait(raw_full + kv, n & 1, s_abort, 8 + kv));
-            if (ok && n >= 2) ok = __all_sync(0xffffffffu, pipe_wait((kv ? v_free : k_free) + slot, ((n >> 1) - 1) & 1, s_abort, 10 + kv));
-            if (!ok) break;
-            const uint32_t raw = smem_u32(sRaw + kv * C::kRaw), to = smem_u32((kv ? sV : sK) + slot * C::kOperand);
-            constexpr int kCh = D / 16, kRowsAtOnce = 128 / kCh;                // 16-code chunks of a row
-            const int c = tid % kCh;
-#pragma unroll 4
-            for (int r0 = 0; r0 < kChunkKeys; r0 += kRowsAtOnce) {
-              const int r = r0 + tid / kCh;
-              const uint32_t from = D == 128 ? raw + r * 128 + ((c ^ (r & 7)) << 4) : raw + r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
-              uint4 v;
-              asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from));
-              if (kv == 1 && (r < z_lo || r >= z_hi || !s_info[(n & (kInfoRing - 1)) * kChunkGroups + r / 16].usable)) v = make_uint4(0u, 0u, 0u, 0u);
-              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-              uint32_t h[8];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) e4m3_to_half(w[i], h[2 * i], h[2 * i + 1]);
-              const uint32_t dst = to + (c >> 2) * kSlab + r * 128;
-              const int ck = (c & 3) * 2;
-              asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + ((ck ^ (r & 7)) << 4)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-              asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + (((ck + 1) ^ (r & 7)) << 4)), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
-            }
-            mbar_arrive(raw_free + kv);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            mbar_arrive((kv ? v_full : k_full) + slot);
-          }
-        } else {
-          ok = __all_sync(0xffffffffu, pipe_wait(raw_full + slot, (n >> 1) & 1, s_abort, 9));
+        const GroupInfo* info = s_info + (n & (kChunkInfoRing - 1)) * kChunkGroups;
+        if constexpr (C::kConvK) {
+          ok = __all_sync(0xffffffffu, pipe_wait(rawk_full, n & 1, s_abort, 8));
+          if (ok && n >= RK) ok = __all_sync(0xffffffffu, pipe_wait(k_free + n % RK, (n / RK - 1) & 1, s_abort, 10));
           if (!ok) break;
-          const GroupInfo* info = s_info + (n & (kInfoRing - 1)) * kChunkGroups;
-          const int r = tid;
-          if (r < z_lo || r >= z_hi || !info[r / 16].usable) {
-            const uint32_t to = smem_u32(sV + slot * C::kOperand);
-#pragma unroll 1
-            for (int i = 0; i < D / 8; ++i)
-              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(to + (i >> 3) * kSlab + r * 128 + ((i & 7) << 4)), "r"(0u) : "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          }
-          mbar_arrive(v_full + slot);
+          convert(sRawK, sK + (n % RK) * C::kK, nullptr, 0, 0);
+          mbar_arrive(rawk_free);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_arrive(k_full + n % RK);
         }
+        const int slot = n % RV;
+        ok = __all_sync(0xffffffffu, pipe_wait(raw_full + slot, (n / RV) & 1, s_abort, 9));
+        if (FP8 && ok && n >= RV) ok = __all_sync(0xffffffffu, pipe_wait(v_free + slot, (n / RV - 1) & 1, s_abort, 11));
+        if (!ok) break;
+        if constexpr (FP8) {
+          const bool edge = z_lo > 0 || z_hi < kChunkKeys || __any_sync(0xffffffffu, lane < kChunkGroups && !info[lane % kChunkGroups].usable);
+          convert(sRaw + slot * C::kCodes, sV + slot * C::kOperand, edge ? info : nullptr, z_lo, z_hi);
+          mbar_arrive(raw_free + slot);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        } else if (tid < z_lo || tid >= z_hi || !info[tid / 16].usable) {
+          const uint32_t to = smem_u32(sV + slot * C::kOperand);
+#pragma unroll 1
+          for (int i = 0; i < D / 8; ++i)
+            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(to + (i >> 3) * kSlab + tid * 128 + ((i & 7) << 4)), "r"(0u) : "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        mbar_arrive(v_full + slot);
       }
     } while (ok && g.next(p));
   } else if (warp >= 8) {
@@ -288,68 +344,103 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const int w = (warp >> 2) - 2, row = threadIdx.x & 127;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + w * 128 + lane_off, tO = tmem + 256 + w * 128 + lane_off;
-    int n = 0;                      // tiles so far
-    int mine = 0;                   // ... of this warpgroup
+    int n = 0;                      // tiles in front of the segment
+    int mine = 0;                   // tiles of this warpgroup so far
+    [[maybe_unused]] int segments = 0;
     bool ok = true;
-    do {
-      if (w == 1 && g.rows <= 128) {
-        n += g.t1 - g.t0;
-        continue;
-      }
-      const int r = w * 128 + row;                           // the item's row
-      const bool there = r < g.rows;
-      const int token = there ? (g.row0 + r) / p.G : 0, head = there ? g.c.h * p.G + (g.row0 + r) - token * p.G : 0;
-      const int2 seen = there ? visible_keys(p.causal, g.c.seq.first_pos() + token, g.c.seq.len) : make_int2(0, 0);
-      // the row's queries as an operand row (the last item's S products, which read this place, are complete: their S has been read)
+    // A row of the segment at hand: where its output goes, the keys it sees, its logits' factor
+    struct Row {
+      int there, token, head;       // whether there is such a row; row of the call
+      int2 seen;
+      float c;
+    } at;
+    const int r = (SPLIT ? 0 : w * 128) + row;               // the item's row
+    // whether this warpgroup has work in the segment (the second one sits out items of up to 128 rows)
+    auto idle = [&] { return !SPLIT && w == 1 && g.rows <= 128; };
+    // The segment's queries as operand rows.  The S products of the segment before have read this place: their S has been read.
+    auto take_queries = [&] {
+      at.there = r < g.rows;
+      const int in = at.there ? (g.row0 + r) / p.G : 0;
+      at.head = at.there ? g.c.h * p.G + (g.row0 + r) - in * p.G : 0;
+      at.token = g.c.seq.start + in;
+      at.seen = at.there ? visible_keys(p.causal, g.c.seq.first_pos() + in, g.c.seq.len) : make_int2(0, 0);
+      if (g.t0 == g.t1) return;
       float back = 1.0f;
       {
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)(g.c.seq.start + token) * p.q_stride_t + head * p.q_stride_h);
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)at.token * p.q_stride_t + at.head * p.q_stride_h);
         uint4 v[D / 8];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) v[i] = there ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < D / 8; ++i) v[i] = at.there ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+        unsigned char* tile = sQ + (SPLIT ? 0 : w * C::kQ);
+        auto put = [&](int i, uint4 x) {                     // 16-byte chunk i of the row, in slabs of eight
+          *reinterpret_cast<uint4*>(tile + (i >> 3) * kSlab + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = x;
+        };
+        float top = 0.0f;
         if constexpr (FP8) {
-          uint32_t top = 0;
 #pragma unroll
           for (int i = 0; i < D / 8; ++i) {
             const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t a = (x[j] & 0x7fffu) << 16, b = x[j] & 0x7fff0000u;
-              if (a < 0x7f800000u) top = max(top, a);
-              if (b < 0x7f800000u) top = max(top, b);
+            for (int j = 0; j < 4; ++j) top = largest(top, x[j]);
+          }
+          const QueryScale s = query_scale(top);
+          back = s.back;
+          if constexpr (C::kRawK) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+              uint32_t high[4], low[4];
+              split_queries(v[2 * i].x, v[2 * i].y, s.to, high[0], low[0]);
+              split_queries(v[2 * i].z, v[2 * i].w, s.to, high[1], low[1]);
+              split_queries(v[2 * i + 1].x, v[2 * i + 1].y, s.to, high[2], low[2]);
+              split_queries(v[2 * i + 1].z, v[2 * i + 1].w, s.to, high[3], low[3]);
+              if (!SPLIT || w == 0) put(i, make_uint4(high[0], high[1], high[2], high[3]));
+              if (!SPLIT || w == 1) put(8 + i, make_uint4(low[0], low[1], low[2], low[3]));
+            }
+          } else {
+            // fp16: the row's largest entry lies in [128, 256), what is below 2^-32 of it is rounded to fp16's subnormal numbers
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+              uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(x[j] << 16) * s.to, __uint_as_float(x[j] & 0xffff0000u) * s.to);
+                x[j] = *reinterpret_cast<const uint32_t*>(&h);
+              }
+              if (!SPLIT || (i & 1) == w) put(i, make_uint4(x[0], x[1], x[2], x[3]));
             }
           }
-          const int e = min(max((int)(top >> 23), 1), 253);
-          back = __uint_as_float((uint32_t)e << 23);
-          const float to = __uint_as_float((uint32_t)(254 - e) << 23);
+        } else {
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const __half2 h = __floats2half2_rn(__uint_as_float(x[j] << 16) * to, __uint_as_float(x[j] & 0xffff0000u) * to);
-              x[j] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            v[i] = make_uint4(x[0], x[1], x[2], x[3]);
-          }
+          for (int i = 0; i < D / 8; ++i)
+            if (!SPLIT || (i & 1) == w) put(i, v[i]);
         }
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-          *reinterpret_cast<uint4*>(sQ + w * C::kOperand + (i >> 3) * kSlab + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = v[i];
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(q_full + w);
+        mbar_arrive(q_full + (SPLIT ? 0 : w));
       }
-      const float c_row = back * p.scale_log2;
+      at.c = back * p.scale_log2;
+    };
+    bool live = true;
+    while (live && idle()) {
+      n += g.t1 - g.t0;
+      live = g.next(p);
+    }
+    if (live) take_queries();
+    while (live) {
+      const int tiles = g.t1 - g.t0;
+      const float c_row = at.c;
+      const int2 seen = at.seen;
       float m = -INFINITY, l = 0.0f;
-      for (int t = g.t0; t < g.t1; ++t, ++n, ++mine) {
+      int took = 0;                                          // tiles of this segment
+#pragma unroll 1
+      for (int i = SPLIT ? w : 0; i < tiles; i += SPLIT ? 2 : 1, ++mine, ++took) {
         ok = __all_sync(0xffffffffu, pipe_wait(s_full + w, mine & 1, s_abort, 12 + w));
         if (!ok) break;
         tc_fence_after();
         uint32_t sr[kChunkKeys];
 #pragma unroll
         for (int ch = 0; ch < kChunkKeys / 32; ++ch) tmem_ld32(tS + ch * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[ch * 32]));
-        const GroupInfo* info = s_info + (n & (kInfoRing - 1)) * kChunkGroups;
-        const int c_lo = seen.x - t * kChunkKeys, c_hi = seen.y - t * kChunkKeys;
+        const GroupInfo* info = s_info + ((n + i) & (kChunkInfoRing - 1)) * kChunkGroups;
+        const int c_lo = seen.x - (g.t0 + i) * kChunkKeys, c_hi = seen.y - (g.t0 + i) * kChunkKeys;
         bool masked = c_lo > 0 || c_hi < kChunkKeys;
         if (lane < kChunkGroups) masked = masked || !info[lane].usable;
         masked = __any_sync(0xffffffffu, masked);
@@ -363,8 +454,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (!info[2 * ch + 1].usable) keep &= 0x0000ffffu;
             if (keep != 0xffffffffu) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!(keep & (1u << i))) sr[ch * 32 + i] = 0xff800000u;
+              for (int j = 0; j < 32; ++j)
+                if (!(keep & (1u << j))) sr[ch * 32 + j] = 0xff800000u;
             }
           }
         }
@@ -375,18 +466,18 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           for (int q = 0; q < kChunkGroups; ++q) {
             float a = fmaxf(__uint_as_float(sr[16 * q]), __uint_as_float(sr[16 * q + 1])), b = fmaxf(__uint_as_float(sr[16 * q + 2]), __uint_as_float(sr[16 * q + 3]));
 #pragma unroll
-            for (int i = 4; i < 16; i += 4) {
-              a = fmax3(a, __uint_as_float(sr[16 * q + i]), __uint_as_float(sr[16 * q + i + 1]));
-              b = fmax3(b, __uint_as_float(sr[16 * q + i + 2]), __uint_as_float(sr[16 * q + i + 3]));
+            for (int j = 4; j < 16; j += 4) {
+              a = fmax3(a, __uint_as_float(sr[16 * q + j]), __uint_as_float(sr[16 * q + j + 1]));
+              b = fmax3(b, __uint_as_float(sr[16 * q + j + 2]), __uint_as_float(sr[16 * q + j + 3]));
             }
             top = fmaxf(top, fmaf(fmaxf(a, b), c_row * info[q].k, info[q].v_log2));
           }
         } else {
           float mx[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mx[i] = __uint_as_float(sr[i]);
+          for (int j = 0; j < 4; ++j) mx[j] = __uint_as_float(sr[j]);
 #pragma unroll
-          for (int i = 4; i < kChunkKeys; i += 2) mx[(i >> 1) & 3] = fmax3(mx[(i >> 1) & 3], __uint_as_float(sr[i]), __uint_as_float(sr[i + 1]));
+          for (int j = 4; j < kChunkKeys; j += 2) mx[(j >> 1) & 3] = fmax3(mx[(j >> 1) & 3], __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
           top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c_row;
         }
         const bool moves = top > m + kLazy;                   // (always for the first key that the row sees)
@@ -395,7 +486,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           const float f = moves ? fast_exp2(m - to) : 1.0f;   // 0 where nothing has been added up yet
           m = to;
           l *= f;
-          if (t > g.t0) {
+          if (took > 0) {
             // O is complete up to the tile before
             ok = __all_sync(0xffffffffu, pipe_wait(pv_done + w, (mine - 1) & 1, s_abort, 14 + w));
             if (!ok) break;
@@ -407,10 +498,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               tmem_ld16(tO + ch * 16, o);
               tc_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 16; i += 2) {
-                const float2 x = unpack_f32x2(fmul2(pack_f32x2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), f2));
-                o[i] = __float_as_uint(x.x);
-                o[i + 1] = __float_as_uint(x.y);
+              for (int j = 0; j < 16; j += 2) {
+                const float2 x = unpack_f32x2(fmul2(pack_f32x2(__uint_as_float(o[j]), __uint_as_float(o[j + 1])), f2));
+                o[j] = __float_as_uint(x.x);
+                o[j + 1] = __float_as_uint(x.y);
               }
               tmem_st16(tO + ch * 16, o);
             }
@@ -434,17 +525,19 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const uint64_t c2 = pack_f32x2(c, c), off2 = pack_f32x2(off, off);
             uint64_t sum = pack_f32x2(0.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              const int at = ch * 32 + q * 16 + i;
-              const float2 e = unpack_f32x2(ffma2(pack_f32x2(__uint_as_float(sr[at]), __uint_as_float(sr[at + 1])), c2, off2));
-              const float a = fast_exp2(e.x), b = fast_exp2(e.y);
-              sum = fadd2(sum, pack_f32x2(a, b));
+            for (int j = 0; j < 16; j += 2) {
+              const int at = ch * 32 + q * 16 + j;
+              const uint64_t e2 = ffma2(pack_f32x2(__uint_as_float(sr[at]), __uint_as_float(sr[at + 1])), c2, off2);
+              float2 e = unpack_f32x2(e2);
+              e.x = fast_exp2(e.x);
+              e.y = fast_exp2(e.y);
+              sum = fadd2(sum, pack_f32x2(e.x, e.y));
               if constexpr (FP8) {
-                const __half2 h = __floats2half2_rn(a, b);
-                pk[q * 8 + i / 2] = *reinterpret_cast<const uint32_t*>(&h);
+                const __half2 h = __floats2half2_rn(e.x, e.y);
+                pk[q * 8 + j / 2] = *reinterpret_cast<const uint32_t*>(&h);
               } else {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-                pk[q * 8 + i / 2] = *reinterpret_cast<const uint32_t*>(&h);
+                const __nv_bfloat162 h = __floats2bfloat162_rn(e.x, e.y);
+                pk[q * 8 + j / 2] = *reinterpret_cast<const uint32_t*>(&h);
               }
             }
             const float2 s2 = unpack_f32x2(sum);
@@ -458,41 +551,90 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
       if (!ok) break;
       // ------------------------------------------------------------------------------------- the segment's end
-      ok = __all_sync(0xffffffffu, pipe_wait(pv_done + w, (mine - 1) & 1, s_abort, 16 + w));
+      // The next segment's queries go first (not where the two halves share them): its first product then runs while this output is read.
+      const bool there = at.there, whole = g.whole;
+      const int token = at.token, head = at.head, slot = 2 * ((int)blockIdx.x - 1) + (g.first ? 0 : 1);
+      n += tiles;
+      auto go_on = [&] {
+        live = g.next(p);
+        while (live && idle()) {
+          n += g.t1 - g.t0;
+          live = g.next(p);
+        }
+        if (live) take_queries();
+      };
+      if constexpr (!SPLIT) go_on();
+      if (took > 0) ok = __all_sync(0xffffffffu, pipe_wait(pv_done + w, (mine - 1) & 1, s_abort, 16 + w));
       if (!ok) break;
+      float f_own = 1.0f, f_other = 0.0f;                     // SPLIT: factors of the two halves' O
+      bool other = false;
+      if constexpr (SPLIT) {
+        if (w == 1) {
+          s_sums[row] = make_float2(m, l);
+          tc_fence_before();
+          mbar_arrive(sums_full);
+          ok = __all_sync(0xffffffffu, pipe_wait(sums_free, segments++ & 1, s_abort, 18));
+          if (!ok) break;
+          go_on();
+          continue;
+        }
+        ok = __all_sync(0xffffffffu, pipe_wait(sums_full, segments++ & 1, s_abort, 19));
+        if (!ok) break;
+        const float2 its = s_sums[row];
+        other = tiles > 1;
+        const float to = fmaxf(m, its.x);
+        f_own = to == -INFINITY ? 1.0f : fast_exp2(m - to);
+        f_other = to == -INFINITY ? 1.0f : fast_exp2(its.x - to);
+        l = l * f_own + its.y * f_other;
+        m = to;
+      }
       tc_fence_after();
-      const int slot = 2 * ((int)blockIdx.x - 1) + (g.first ? 0 : 1);
-      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      const bool empty = m == -INFINITY && l == l;            // the row sees no key
+      const float inv = empty ? 0.0f : 1.0f / l;
 #pragma unroll 1
       for (int ch = 0; ch < D / 32; ++ch) {
         uint32_t o[32];
         tmem_ld32(tO + ch * 32, o);
         tc_wait_ld();
-        if (there && g.whole) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + (int64_t)(g.c.seq.start + token) * p.out_stride_t + head * p.out_stride_h + ch * 32);
+        if constexpr (SPLIT) {
+          if (other) {
+            uint32_t x[32];
+            tmem_ld32(tO + 128 + ch * 32, x);
+            tc_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(__uint_as_float(x[j]), f_other, __uint_as_float(o[j]) * f_own));
+          }
+        }
+        if (there && whole) {
+          uint4* dst = reinterpret_cast<uint4*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + ch * 32);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
             uint32_t x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(o[8 * i + 2 * j]) * inv, __uint_as_float(o[8 * i + 2 * j + 1]) * inv);
-              x[j] = *reinterpret_cast<const uint32_t*>(&h);
+            for (int k = 0; k < 4; ++k) {
+              const __nv_bfloat162 h = empty ? __floats2bfloat162_rn(0.0f, 0.0f)
+                                             : __floats2bfloat162_rn(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
+              x[k] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            dst[i] = make_uint4(x[0], x[1], x[2], x[3]);
+            dst[j] = make_uint4(x[0], x[1], x[2], x[3]);
           }
-        } else if (there) {
-          uint4* dst = reinterpret_cast<uint4*>(p.part_o + ((int64_t)slot * kChunkRows + r) * D + ch * 32);
+        } else if (there && tiles > 0) {
+          uint4* dst = reinterpret_cast<uint4*>(p.part_o + ((int64_t)slot * R + r) * D + ch * 32);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          for (int j = 0; j < 8; ++j) dst[j] = empty ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
         }
       }
       tc_fence_before();
-      if (there && g.whole) {
-        if (p.lse) p.lse[(int64_t)(g.c.seq.start + token) * p.H + head] = l == 0.0f ? -INFINITY : (m - kBase + log2f(l)) * 0.6931471805599453f;
+      if (there && whole) {
+        if (p.lse) p.lse[(int64_t)token * p.H + head] = empty ? -INFINITY : (m - kBase + log2f(l)) * 0.6931471805599453f;
       } else if (there) {
-        *reinterpret_cast<float2*>(p.part_ml + ((int64_t)slot * kChunkRows + r) * 2) = make_float2(m, l);
+        *reinterpret_cast<float2*>(p.part_ml + ((int64_t)slot * R + r) * 2) = make_float2(m, empty ? 0.0f : l);
       }
-    } while (g.next(p));
+      if constexpr (SPLIT) {
+        mbar_arrive(sums_free);
+        go_on();
+      }
+    }
   }
   // -------------------------------------------------------------------------------------------------------- teardown
   tc_fence_before();
@@ -505,29 +647,34 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   }
 }
 
-template <int D, bool FP8>
-static int launch_chunk(const sparkattn_cache_t& c, const sparkattn_batch_t& b, CacheFwdParams& p, const void* k_cache, const void* v_cache,
-                        cudaStream_t stream) {
+template <int D, bool FP8, bool SPLIT>
+static int launch_chunk(const sparkattn_cache_t& c, CacheFwdParams& p, const void* k_cache, const void* v_cache, cudaStream_t stream) {
   using C = ChunkShape<D, FP8>;
+  constexpr int R = SPLIT ? 128 : 256;
   CUtensorMap mk, mv;
   int rc;
   p.box_rows = c.page;
   p.boxes = kChunkKeys / p.box_rows;
   if ((rc = make_page_map(&mk, k_cache, FP8 ? 1 : 2, c, p.box_rows)) != SPARKATTN_OK) return rc;
   if ((rc = make_page_map(&mv, v_cache, FP8 ? 1 : 2, c, p.box_rows)) != SPARKATTN_OK) return rc;
-  static_assert(C::kBytes <= 232448 && (kCacheMaxSequences + 1) * 4 <= 2 * C::kOperand, "fits an SM");
+  static_assert(C::kBytes <= 232448 && (kCacheMaxSequences + 1) * 4 <= 2 * C::kQ, "fits an SM");
   constexpr int smem = C::kBytes;
-  auto kern = cache_chunk_kernel<D, FP8>;
+  auto kern = cache_chunk_kernel<D, FP8, SPLIT>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kChunkThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
-  return launch_kernel(combine_kernel<D, kChunkRows>, dim3(p.workers - 1, 16), kCombineThreads, 0, true, stream, p);
+  return launch_kernel(combine_kernel<D, R>, dim3(p.workers - 1, R / 16), kCombineThreads, 0, true, stream, p);
 }
 
-int launch_cache_chunk(const sparkattn_cache_t& c, const sparkattn_batch_t& b, CacheFwdParams& p, const void* k_cache, const void* v_cache,
-                       cudaStream_t stream) {
+int launch_cache_chunk(const sparkattn_cache_t& c, int rows, CacheFwdParams& p, const void* k_cache, const void* v_cache, cudaStream_t stream) {
+  auto go = [&](auto d, auto e4m3) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool FP8 = decltype(e4m3)::value;
+    return rows == 128 ? launch_chunk<D, FP8, true>(c, p, k_cache, v_cache, stream) : launch_chunk<D, FP8, false>(c, p, k_cache, v_cache, stream);
+  };
+  using std::integral_constant;
   if (c.dtype == SPARKATTN_FP8_E4M3)
-    return c.d == 128 ? launch_chunk<128, true>(c, b, p, k_cache, v_cache, stream) : launch_chunk<64, true>(c, b, p, k_cache, v_cache, stream);
-  return c.d == 128 ? launch_chunk<128, false>(c, b, p, k_cache, v_cache, stream) : launch_chunk<64, false>(c, b, p, k_cache, v_cache, stream);
+    return c.d == 128 ? go(integral_constant<int, 128>{}, integral_constant<bool, true>{}) : go(integral_constant<int, 64>{}, integral_constant<bool, true>{});
+  return c.d == 128 ? go(integral_constant<int, 128>{}, integral_constant<bool, false>{}) : go(integral_constant<int, 64>{}, integral_constant<bool, false>{});
 }
 
 }  // namespace sparkattn

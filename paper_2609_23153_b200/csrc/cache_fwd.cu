@@ -34,6 +34,7 @@
 namespace sparkattn {
 
 constexpr int kGroupKeys = 16;
+constexpr int kDecodeOver = 2;      // tiles that the beginning and the end of an item take as long as
 constexpr int kInfoRing = 32;      // tiles whose groups' notes are kept: a batch of up to 8 and a ring of up to 8 at a time
 constexpr int kComputeWarps = 4, kDecodeThreads = 32 * (kComputeWarps + 1);
 
@@ -128,7 +129,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     *s_abort = 0;
   }
   pdl_wait();
-  Stretch<R, kTileKeys> g;
+  Stretch<R, kTileKeys, kDecodeOver> g;
   int worker = 0;
   if constexpr (CLUSTER) {
     __syncthreads();
@@ -140,8 +141,8 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     const int b = (cluster - 1) / p.Hk;
     if (!g.run_of(p, b, cluster - 1 - b * p.Hk, rank, p.cluster)) return;
   } else {
-  Line<R, kTileKeys>::lay_out(p, s_prefix, s_warp);
-  const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys>::share_of(p, total);
+  Line<R, kTileKeys, kDecodeOver>::lay_out(p, s_prefix, s_warp);
+  const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys, kDecodeOver>::share_of(p, total);
   if (blockIdx.x == 0) {
     check_call(p, s_bad);
     return;
@@ -168,6 +169,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     int t_next = g.t0;
     bool live = true;
     auto ask_pages = [&] {
+      while (live && t_next >= g.t1) {
+        live = g.next(p);
+        t_next = g.t0;
+      }
       Batch b{t_next, 0, 0, -1, 1.0f, 1.0f};
       if (!live) return b;
       b.n = min(kBatch, g.t1 - b.t);
@@ -176,10 +181,6 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       if (lane / kGroups < b.n && key < g.c.item.hi && key + kGroupKeys > g.c.item.lo)
         b.page = p.batch.page_table[(int64_t)g.c.b * p.batch.max_pages + (key >> p.batch.page_shift)];
       t_next += b.n;
-      if (t_next >= g.t1) {
-        live = g.next(p);
-        t_next = g.t0;
-      }
       return b;
     };
     auto ask_scales = [&](Batch& b) {
@@ -685,9 +686,9 @@ struct Plan {
 Plan plan_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
   const long long rows = (long long)(H / c.H) * b.max_new;
   Plan p;
-  p.R = rows <= 8 ? 8 : rows <= 16 ? 16 : kChunkRows;
+  p.R = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 128 ? 128 : 256;
   const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;
-  p.workers = current_sm_count() * (p.R == kChunkRows ? 1 : decode_ctas_per_sm(c.d, fp8, p.R));
+  p.workers = current_sm_count() * (p.R >= 128 ? 1 : decode_ctas_per_sm(c.d, fp8, p.R));
   p.borders = align256((size_t)p.workers * sizeof(Border));
   p.ml = align256((size_t)2 * p.workers * p.R * 8);
   p.o = (size_t)2 * p.workers * p.R * c.d * 4;
@@ -759,7 +760,7 @@ int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, con
   p.part_ml = reinterpret_cast<float*>(base);
   base += plan.ml;
   p.part_o = reinterpret_cast<float*>(base);
-  if (plan.R == kChunkRows) return launch_cache_chunk(c, b, p, k_cache, v_cache, stream);
+  if (plan.R >= 128) return launch_cache_chunk(c, plan.R, p, k_cache, v_cache, stream);
   const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;
   auto go = [&](auto d, auto e4m3) {
     return plan.R == 8 ? launch_decode<decltype(d)::value, decltype(e4m3)::value, 1>(c, b, p, k_cache, v_cache, stream)

@@ -1,8 +1,10 @@
-// The line: the key tiles of all items of a call, one behind the other, cut into equal stretches.
+// The line: the key tiles of all items of a call, one behind the other, cut into stretches of equal work.
 //
 // An item is R query rows (row = token * G + head in its group) of one (sequence, key head); its tiles of TK keys run from
 // the first to the last key that any of its rows sees, at least one, so that somebody writes the rows of an empty sequence.
-// Stretch w is tiles [w * share, (w + 1) * share).  What a stretch holds of an item is a segment; an item that lies in one
+// Every item stands for OVER units more than it has tiles, in front of them: what it takes to begin and to finish one, without which the
+// stretches with many short items would take longest (prompts of four different lengths: FIGURE).
+// Stretch w is units [w * share, (w + 1) * share).  What a stretch holds of an item is a segment; an item that lies in one
 // stretch is finished there, the others leave partial results that combine_kernel adds up in the line's order.
 // Items stand in the order (sequence, key head, row tile).
 #pragma once
@@ -30,7 +32,7 @@ struct CacheFwdParams {
   int H, Hk, G;
   float scale_log2;
   int box_rows, boxes;           // keys of one TMA box, boxes of a tile
-  int least;                     // tiles a stretch has at least
+  int least;                     // units a stretch has at least
   int workers;                   // stretches
   int slots;                     // K and V tiles that a CTA's ring holds
   int cluster;                   // CTAs of an item's cluster; 0: the line
@@ -42,16 +44,14 @@ struct CacheFwdParams {
 
 // What the combining kernel needs to know of the border in front of a stretch: the item that it cuts, if it does.
 struct Border {
-  int before;                    // tiles of the item in front of the border; 0: the border cuts none
-  int tiles, share;              // of the item; of a stretch
+  int before;                    // units of the item in front of the border; 0: the border cuts none
+  int units, share;              // of the item; of a stretch
   int token0, row0, rows, h;     // row r is head h * G + (row0 + r) % G of token token0 + (row0 + r) / G
   int pad;
 };
 
-// cache_chunk.cu: items of 256 rows
-constexpr int kChunkRows = 256;
-int launch_cache_chunk(const sparkattn_cache_t& c, const sparkattn_batch_t& b, CacheFwdParams& p, const void* k_cache, const void* v_cache,
-                       cudaStream_t stream);
+// cache_chunk.cu: items of 128 or 256 rows
+int launch_cache_chunk(const sparkattn_cache_t& c, int rows, CacheFwdParams& p, const void* k_cache, const void* v_cache, cudaStream_t stream);
 
 // 16 keys of a tile, as the copying warp has looked them up
 struct GroupInfo {
@@ -61,11 +61,12 @@ struct GroupInfo {
   int usable;        // somebody sees keys of it, and the page exists
 };
 
-template <int R, int TK>
+template <int R, int TK, int OVER>
 struct Line {
   struct Item {
     int first, tiles;            // key tiles, counted from the front of the sequence
     int lo, hi;                  // keys that any of its rows sees
+    __device__ __forceinline__ int units() const { return tiles + OVER; }
   };
   static __device__ __forceinline__ int row_tiles(const CacheFwdParams& p, const Sequence& s) { return (s.n * p.G + R - 1) / R; }
   static __device__ __forceinline__ Item item_of(const CacheFwdParams& p, const Sequence& s, int rt) {
@@ -77,19 +78,19 @@ struct Line {
     it.tiles = max((it.hi + TK - 1) / TK - it.first, 1);
     return it;
   }
-  // tiles of the row tiles of one key head
-  static __device__ __forceinline__ int tiles_of(const CacheFwdParams& p, const Sequence& s) {
+  // units of the row tiles of one key head
+  static __device__ __forceinline__ int units_of(const CacheFwdParams& p, const Sequence& s) {
     int sum = 0;
-    for (int rt = 0; rt < row_tiles(p, s); ++rt) sum += item_of(p, s, rt).tiles;
+    for (int rt = 0; rt < row_tiles(p, s); ++rt) sum += item_of(p, s, rt).units();
     return sum;
   }
-  // all threads: prefix[b] = tiles in front of sequence b, prefix[B] = all (shared memory)
+  // all threads: prefix[b] = units in front of sequence b, prefix[B] = all (shared memory)
   static __device__ __forceinline__ void lay_out(const CacheFwdParams& p, int* prefix, int* s_warp) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     int carry = 0;
     for (int base = 0; base < p.batch.B; base += blockDim.x) {
       const int b = base + threadIdx.x;
-      const int mine = b < p.batch.B ? tiles_of(p, sequence_of(p.batch, b)) * p.Hk : 0;
+      const int mine = b < p.batch.B ? units_of(p, sequence_of(p.batch, b)) * p.Hk : 0;
       int x = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -117,11 +118,11 @@ struct Line {
     Sequence seq;
     Item item;
     int b, h, rt, row_tiles;
-    int at;                      // tiles of the item in front of the place
+    int at;                      // units of the item in front of the place
   };
   static __device__ __forceinline__ Place find(const CacheFwdParams& p, const int* prefix, int x) {
     Place c;
-    int lo = 0, hi = p.batch.B;                   // prefix[lo] <= x; sequences without tiles have equal entries
+    int lo = 0, hi = p.batch.B;                   // prefix[lo] <= x; sequences without new tokens have equal entries
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (prefix[mid] <= x) lo = mid; else hi = mid;
@@ -140,7 +141,7 @@ struct Line {
     c.at = in;
     if (c.row_tiles > 1) {
       for (;; rt0 += 32) {
-        const int mine = rt0 + lane < c.row_tiles ? item_of(p, c.seq, rt0 + lane).tiles : 0;
+        const int mine = rt0 + lane < c.row_tiles ? item_of(p, c.seq, rt0 + lane).units() : 0;
         int sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -161,7 +162,7 @@ struct Line {
     c.item = item_of(p, c.seq, c.rt);
     return c;
   }
-  // to the first tile of the next item
+  // to the front of the next item
   static __device__ __forceinline__ void next_item(const CacheFwdParams& p, Place& c) {
     c.at = 0;
     if (++c.rt == c.row_tiles) {
@@ -177,12 +178,12 @@ struct Line {
 };
 
 // A stretch of the line, taken segment by segment.
-template <int R, int TK>
+template <int R, int TK, int OVER>
 struct Stretch {
-  using L = Line<R, TK>;
+  using L = Line<R, TK, OVER>;
   typename L::Place c;
   int x, end;
-  int t0, t1;                    // the segment's key tiles, counted from the front of the sequence
+  int t0, t1;                    // the segment's key tiles, counted from the front of the sequence (none, where it is all beginning)
   int row0, rows;                // its rows
   bool whole, first;             // the item lies in this stretch; the stretch's first segment
   __device__ __forceinline__ void begin(const CacheFwdParams& p, const int* prefix, int from, int to) {
@@ -193,10 +194,10 @@ struct Stretch {
     cut(p);
   }
   __device__ __forceinline__ void cut(const CacheFwdParams& p) {
-    const int until = min(c.item.tiles, c.at + end - x);
-    t0 = c.item.first + c.at;
-    t1 = c.item.first + until;
-    whole = c.at == 0 && until == c.item.tiles;
+    const int until = min(c.item.units(), c.at + end - x);
+    t0 = c.item.first + max(c.at - OVER, 0);
+    t1 = c.item.first + max(until - OVER, 0);
+    whole = c.at == 0 && until == c.item.units();
     row0 = c.rt * R;
     rows = min(R, c.seq.n * p.G - row0);
     x += until - c.at;
@@ -288,10 +289,10 @@ __device__ __forceinline__ void check_call(const CacheFwdParams& p, int* s_bad) 
   });
   leave_status(p.status, s_bad);
 }
-template <int R, int TK>
-__device__ __forceinline__ void note_border(const CacheFwdParams& p, int worker, bool works, int share, const Stretch<R, TK>& g) {
+template <int R, int TK, int OVER>
+__device__ __forceinline__ void note_border(const CacheFwdParams& p, int worker, bool works, int share, const Stretch<R, TK, OVER>& g) {
   Border b{};
-  if (works) b = {g.c.at, g.c.item.tiles, share, g.c.seq.start, g.row0, g.rows, g.c.h, 0};
+  if (works) b = {g.c.at, g.c.item.units(), share, g.c.seq.start, g.row0, g.rows, g.c.h, 0};
   reinterpret_cast<int4*>(p.borders + worker)[0] = reinterpret_cast<const int4*>(&b)[0];
   reinterpret_cast<int4*>(p.borders + worker)[1] = reinterpret_cast<const int4*>(&b)[1];
 }
@@ -307,9 +308,9 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
   __shared__ float s_acc[kWarps][D + 2];
   pdl_wait();
   const int4 b0 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[0], b1 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[1];
-  const int before = b0.x, tiles = b0.y, share = b0.z, token0 = b0.w, row0 = b1.x, rows = b1.y, h = b1.z;
+  const int before = b0.x, units = b0.y, share = b0.z, token0 = b0.w, row0 = b1.x, rows = b1.y, h = b1.z;
   if (before == 0 || before > share) return;
-  const int w0 = blockIdx.x, parts = 1 + (tiles - before + share - 1) / share;
+  const int w0 = blockIdx.x, parts = 1 + (units - before + share - 1) / share;
   // the stretch in front holds the item's beginning as its last segment (its only one where it begins with it), the others as their first
   auto slot_of = [&](int i) { return 2 * (w0 + i) + (i > 0 || before == share ? 0 : 1); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -335,7 +336,7 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
         if constexpr (kVec == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
         else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) acc[j] = fmaf(v[j], f, acc[j]);
+        for (int j = 0; j < kVec; ++j) acc[j] = f == 0.0f ? acc[j] : fmaf(v[j], f, acc[j]);      // (a part without keys has left no output)
       }
     }
     if (split > 1) {
