@@ -45,24 +45,30 @@ struct AppendParams {
   int32_t* status;
 };
 
-// eight fp32 channels, in pairs for the packed instructions
+// eight fp32 channels
 struct Chunk {
-  uint64_t x[4];
+  float x[8];
 };
-__device__ __forceinline__ uint64_t widen2(uint32_t w) { return pack_f32x2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ uint32_t narrow2(uint64_t x) {
-  const float2 f = unpack_f32x2(x);
-  const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
-  return *reinterpret_cast<const uint32_t*>(&h);
+__device__ __forceinline__ Chunk widen(uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  Chunk c;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    c.x[2 * j] = __uint_as_float(w[j] << 16);
+    c.x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+  }
+  return c;
 }
-__device__ __forceinline__ Chunk widen(uint4 v) { return {{widen2(v.x), widen2(v.y), widen2(v.z), widen2(v.w)}}; }
-__device__ __forceinline__ uint4 narrow(const Chunk& c) { return make_uint4(narrow2(c.x[0]), narrow2(c.x[1]), narrow2(c.x[2]), narrow2(c.x[3])); }
+__device__ __forceinline__ uint4 narrow(const Chunk& c) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(c.x[2 * j], c.x[2 * j + 1]);
+    w[j] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 
-// The phases of the channels 8c .. 8c+7 of a token: a channel becomes x c + y s, y the other side of its pair, and s negative for a
-// first side (a - b and a + (-b) round alike).
-struct Phases {
-  uint64_t c[4], s[4];
-};
 // cosines and sines of a unit's tokens as [rows][pairs], from the tables; a pair outside them is turned by nothing
 __device__ __forceinline__ void gather_phases(const RotaryView& r, int rows, int t0, int pos0, float* s_cos, float* s_sin, int tid, int threads) {
   const int quads = r.rot / 8;                             // of four pairs
@@ -93,45 +99,44 @@ __device__ __forceinline__ void gather_phases(const RotaryView& r, int rows, int
     *reinterpret_cast<float4*>(s_sin + row * (r.rot / 2) + m) = s;
   }
 }
-// a chunk's share of a row of them
-__device__ __forceinline__ Phases phases_of(const RotaryView& r, const float* c, const float* s, bool second) {
-  Phases p;
-  const float4 c0 = *reinterpret_cast<const float4*>(c), s0 = *reinterpret_cast<const float4*>(s);
-  if (r.interleaved) {
-    p.c[0] = pack_f32x2(c0.x, c0.x); p.c[1] = pack_f32x2(c0.y, c0.y); p.c[2] = pack_f32x2(c0.z, c0.z); p.c[3] = pack_f32x2(c0.w, c0.w);
-    p.s[0] = pack_f32x2(-s0.x, s0.x); p.s[1] = pack_f32x2(-s0.y, s0.y); p.s[2] = pack_f32x2(-s0.z, s0.z); p.s[3] = pack_f32x2(-s0.w, s0.w);
-  } else {
-    const float4 c1 = *reinterpret_cast<const float4*>(c + 4), s1 = *reinterpret_cast<const float4*>(s + 4);
-    const float f = second ? 1.0f : -1.0f;
-    p.c[0] = pack_f32x2(c0.x, c0.y); p.c[1] = pack_f32x2(c0.z, c0.w); p.c[2] = pack_f32x2(c1.x, c1.y); p.c[3] = pack_f32x2(c1.z, c1.w);
-    const uint64_t f2 = pack_f32x2(f, f);
-    p.s[0] = fmul2(pack_f32x2(s0.x, s0.y), f2); p.s[1] = fmul2(pack_f32x2(s0.z, s0.w), f2);
-    p.s[2] = fmul2(pack_f32x2(s1.x, s1.y), f2); p.s[3] = fmul2(pack_f32x2(s1.z, s1.w), f2);
-  }
-  return p;
-}
-// The chunk turned, given the other sides of its channels' pairs.  Each product and sum is rounded by itself, so that a cache
-// filled by any route holds the same bits.
-// (The sum is not a packed instruction: behind packed products it was fused with one of them, which rounds once.)
-__device__ __forceinline__ uint64_t turn2(uint64_t c, uint64_t s, uint64_t x, uint64_t y) {
-  const float2 a = unpack_f32x2(fmul2(x, c)), b = unpack_f32x2(fmul2(y, s));
-  return pack_f32x2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y));
-}
-__device__ __forceinline__ Chunk turn(const Phases& p, uint4 x, uint4 y) {
-  return {{turn2(p.c[0], p.s[0], widen2(x.x), widen2(y.x)), turn2(p.c[1], p.s[1], widen2(x.y), widen2(y.y)),
-           turn2(p.c[2], p.s[2], widen2(x.z), widen2(y.z)), turn2(p.c[3], p.s[3], widen2(x.w), widen2(y.w))}};
-}
-// largest |x| as bits: of all values, or of the finite ones
-template <bool FINITE>
-__device__ __forceinline__ uint32_t largest_bits(const Chunk& c, uint32_t top) {
+// The chunk turned by its share c, s of a row of them.  Interleaved: its own four pairs.  Halves: `y` holds the other sides of its
+// eight channels.  Each product and sum is rounded by itself, so that a cache filled by any route holds the same bits.  (Scalar
+// instructions: the packed ones want their pairs in neighbouring registers and spend more on moves than they save, and a packed sum
+// behind packed products was fused with one of them, which rounds once.)
+__device__ __forceinline__ Chunk turn_pairs(const float* c, const float* s, const Chunk& x) {
+  const float4 cc = *reinterpret_cast<const float4*>(c), ss = *reinterpret_cast<const float4*>(s);
+  const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
+  Chunk r;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 f = unpack_f32x2(c.x[j]);
-    uint32_t a = __float_as_uint(f.x) & 0x7fffffffu, b = __float_as_uint(f.y) & 0x7fffffffu;
-    if constexpr (FINITE) { a = a < 0x7f800000u ? a : 0u; b = b < 0x7f800000u ? b : 0u; }
-    top = max(top, max(a, b));
+    r.x[2 * j] = __fsub_rn(__fmul_rn(x.x[2 * j], cv[j]), __fmul_rn(x.x[2 * j + 1], sv[j]));
+    r.x[2 * j + 1] = __fadd_rn(__fmul_rn(x.x[2 * j], sv[j]), __fmul_rn(x.x[2 * j + 1], cv[j]));
   }
-  return top;
+  return r;
+}
+__device__ __forceinline__ Chunk turn_halves(const float* c, const float* s, const Chunk& x, const Chunk& y, float sign) {
+  Chunk r;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const float4 cc = reinterpret_cast<const float4*>(c)[g], ss = reinterpret_cast<const float4*>(s)[g];
+    const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)      // a first side takes away what a second side adds: x c - y s and x c + y s round alike
+      r.x[4 * g + j] = __fadd_rn(__fmul_rn(x.x[4 * g + j], cv[j]), __fmul_rn(y.x[4 * g + j], __fmul_rn(sv[j], sign)));
+  }
+  return r;
+}
+
+// bits of the largest |x|, NaN aside; or of the finite ones
+template <bool FINITE>
+__device__ __forceinline__ uint32_t largest_bits(const Chunk& c, uint32_t top) {
+  float m = __uint_as_float(top);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float a = fabsf(c.x[j]);
+    m = fmaxf(m, FINITE && !(a < INFINITY) ? 0.0f : a);
+  }
+  return __float_as_uint(m);
 }
 // smallest power of two s with amax <= 448 s (448 = 1.75 * 2^8), from the bits of amax >= 1e-12
 __device__ __forceinline__ float power_scale(uint32_t amax_bits) {
@@ -139,10 +144,10 @@ __device__ __forceinline__ float power_scale(uint32_t amax_bits) {
   return __uint_as_float(((u >> 23) - 8u + ((u & 0x7fffffu) > 0x600000u ? 1u : 0u)) << 23);
 }
 __device__ __forceinline__ uint2 encode(const Chunk& c, float inv) {
-  const uint64_t by = pack_f32x2(inv, inv);
   uint32_t w[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) w[j] = __nv_cvt_float2_to_fp8x2(unpack_f32x2(fmul2(c.x[j], by)), __NV_SATFINITE, __NV_E4M3);
+  for (int j = 0; j < 4; ++j)
+    w[j] = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(c.x[2 * j], inv), __fmul_rn(c.x[2 * j + 1], inv)), __NV_SATFINITE, __NV_E4M3);
   return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 __device__ __forceinline__ Chunk decode(uint2 codes) {
@@ -151,7 +156,8 @@ __device__ __forceinline__ Chunk decode(uint2 codes) {
   for (int j = 0; j < 4; ++j) {
     const uint32_t pair = (j < 2 ? codes.x : codes.y) >> (16 * (j & 1));
     const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
-    c.x[j] = pack_f32x2(f.x, f.y);
+    c.x[2 * j] = f.x;
+    c.x[2 * j + 1] = f.y;
   }
   return c;
 }
@@ -201,13 +207,15 @@ __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& 
   // where this chunk's pairs lie, and (halves) the lane with their other sides: the lanes of a row hold its chunks in order
   const int m0 = rot.interleaved ? chunk * 4 : (second ? chunk - half : chunk) * 8;
   const int partner = (threadIdx.x & 31 & ~(S::kLanes - 1)) + (!on ? chunk : second ? chunk - half : chunk + half);
-  auto other_side = [&](uint4 v) {
-    if (rot.interleaved) return make_uint4(__byte_perm(v.x, 0, 0x1032), __byte_perm(v.y, 0, 0x1032), __byte_perm(v.z, 0, 0x1032), __byte_perm(v.w, 0, 0x1032));
-    v.x = __shfl_sync(0xffffffffu, v.x, partner);
-    v.y = __shfl_sync(0xffffffffu, v.y, partner);
-    v.z = __shfl_sync(0xffffffffu, v.z, partner);
-    v.w = __shfl_sync(0xffffffffu, v.w, partner);
-    return v;
+  const float sign = second ? 1.0f : -1.0f;
+  // row r's chunk turned (lanes of a row together: halves pass their chunks on)
+  auto turned = [&](uint4 v, int r, bool there) {
+    const float* c = s_cos + r * pairs + m0;
+    const float* s = s_sin + r * pairs + m0;
+    if (rot.interleaved) return on && there ? turn_pairs(c, s, widen(v)) : widen(v);
+    const uint4 far = make_uint4(__shfl_sync(0xffffffffu, v.x, partner), __shfl_sync(0xffffffffu, v.y, partner), __shfl_sync(0xffffffffu, v.z, partner),
+                                 __shfl_sync(0xffffffffu, v.w, partner));
+    return on && there ? turn_halves(c, s, widen(v), widen(far), sign) : widen(v);
   };
   extern __shared__ __align__(16) unsigned char s_raw[];
   const uint32_t mine = smem_u32(s_raw) + threadIdx.x * 16;      // the thread's places, kThreads * 16 bytes apart
@@ -250,12 +258,8 @@ __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& 
       uint4 y[C];
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        y[i] = raw[i];
-        if (rotate) {
-          const int r = row0 + i * S::kRowsAtOnce;
-          const uint4 far = other_side(raw[i]);
-          if (on && r < rows) y[i] = narrow(turn(phases_of(rot, s_cos + r * pairs + m0, s_sin + r * pairs + m0, second), raw[i], far));
-        }
+        const int r = row0 + i * S::kRowsAtOnce;
+        y[i] = rotate ? narrow(turned(raw[i], r, r < rows)) : raw[i];
       }
 #pragma unroll
       for (int i = 0; i < C; ++i) {
@@ -268,17 +272,13 @@ __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& 
       uint32_t amax = 0;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        x[i] = widen(raw[i]);
-        if (rotate) {
-          const int r = row0 + i * S::kRowsAtOnce;
-          const uint4 far = other_side(raw[i]);
-          if (on && r < rows) x[i] = turn(phases_of(rot, s_cos + r * pairs + m0, s_sin + r * pairs + m0, second), raw[i], far);
-        }
+        const int r = row0 + i * S::kRowsAtOnce;
+        x[i] = rotate ? turned(raw[i], r, r < rows) : widen(raw[i]);
         amax = largest_bits<false>(x[i], amax);
       }
       float* scale_at = scale_of(n);
       amax = __reduce_max_sync(0xffffffffu, amax);
-      if (amax >= 0x7f800000u) {                                 // infinities or NaN among them: the finite ones count
+      if (amax >= 0x7f800000u) {                                 // infinities among them: the finite ones count
         amax = 0;
 #pragma unroll
         for (int i = 0; i < C; ++i) amax = largest_bits<true>(x[i], amax);

@@ -34,7 +34,7 @@
 namespace sparkattn {
 
 constexpr int kGroupKeys = 16;
-constexpr int kDecodeOver = 2;      // tiles that the beginning and the end of an item take as long as
+constexpr int kDecodeOver = 4;      // tiles that the beginning and the end of an item take as long as
 constexpr int kInfoRing = 32;      // tiles whose groups' notes are kept: a batch of up to 8 and a ring of up to 8 at a time
 constexpr int kComputeWarps = 4, kDecodeThreads = 32 * (kComputeWarps + 1);
 
