@@ -130,60 +130,76 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // fall through to the teardown
   } else if (warp == 0) {
     // --------------------------------------------------------------------------------------------------- copies
+    // The stretch goes by in batches of four tiles of a segment, of whose groups of 16 keys every lane looks after one.  Pages are
+    // asked for two batches ahead and scales one, across segments.
+    constexpr int kBatch = 32 / kChunkGroups;
+    GroupBatch now, next, after;
+    int t_next = g.t0;
+    bool live = true;
+    auto ask_pages = [&](GroupBatch& b) {
+      while (live && t_next >= g.t1) {
+        live = g.next(p);
+        t_next = g.t0;
+      }
+      b = {t_next, live ? min(kBatch, g.t1 - t_next) : 0, g.c.h, -1, 1.0f, 1.0f};
+      const int key = b.t * kChunkKeys + lane * 16;
+      if (lane / kChunkGroups < b.n && key < g.c.item.hi && key + 16 > g.c.item.lo)
+        b.page = p.batch.page_table[(int64_t)g.c.b * p.batch.max_pages + (key >> p.batch.page_shift)];
+      t_next += b.n;
+    };
     int n = 0;                                               // tiles so far
     bool ok = true;
-    do {
-      const int32_t* table = p.batch.page_table + (int64_t)g.c.b * p.batch.max_pages;
-      constexpr int kBatch = 32 / kChunkGroups;
-      int page_n;
-      GroupInfo info_n;
-      auto look_up = [&](int t) {
-        const bool in = t + lane / kChunkGroups < g.t1;
-        page_n = look_up_group<FP8>(p, table, g.c.h, in ? t * kChunkKeys + lane * 16 : 0x7fffff00, g.c.item.lo, g.c.item.hi, info_n);
-      };
-      look_up(g.t0);
-      for (int t = g.t0; ok && t < g.t1; t += kBatch) {
-        const int page = page_n;
-        const GroupInfo info = info_n;
-        if (t + kBatch < g.t1) look_up(t + kBatch);
-        for (int u = 0; ok && u < kBatch && t + u < g.t1; ++u, ++n) {
-          const int per = kChunkGroups / p.boxes;
-          const int box = lane % p.boxes, src = u * kChunkGroups + box * per;
-          int box_page = -1;
-          for (int i = 0; i < per; ++i) box_page = max(box_page, __shfl_sync(0xffffffffu, page, src + i));
-          const bool copies = lane < p.boxes && box_page >= 0;
-          const int going = __popc(__ballot_sync(0xffffffffu, copies));
-          const int key = (t + u) * kChunkKeys + box * p.box_rows, row = key & ((1 << p.batch.page_shift) - 1);
-          // K, then V: as codes that are an operand or become one, or (bf16) where the products read them
+    const int per_box = kChunkGroups / p.boxes;              // groups of a box
+    ask_pages(now);
+    ask_pages(next);
+    ask_scales<FP8>(p, now);
+    while (ok && now.n > 0) {
+      // a box is copied if somebody sees one of its groups; the lane of its first group copies it
+      int page = now.page;
+      if (per_box > 1) page = max(page, __shfl_xor_sync(0xffffffffu, page, 1));
+      if (per_box > 2) page = max(page, __shfl_xor_sync(0xffffffffu, page, 2));
+      if (per_box > 4) page = max(page, __shfl_xor_sync(0xffffffffu, page, 4));
+      const bool copies = page >= 0 && lane % per_box == 0;
+      const uint32_t going = __ballot_sync(0xffffffffu, copies);
+      const int key = now.t * kChunkKeys + lane * 16, row = key & ((1 << p.batch.page_shift) - 1), at_row = (lane % kChunkGroups) * 16;
+      const GroupInfo info = info_of<FP8>(now);
+      ask_scales<FP8>(p, next);
+      ask_pages(after);
+      for (int u = 0; ok && u < now.n; ++u, ++n) {
+        const bool my_tile = lane / kChunkGroups == u;
+        const int boxes = __popc((going >> (u * kChunkGroups)) & ((1u << kChunkGroups) - 1u));
+        // K, then V: as codes that are an operand or become one, or (bf16) where the products read them
 #pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            const int slot = kv ? n % RV : C::kConvK ? 0 : n % RK, uses = kv ? n / RV : C::kConvK ? n : n / RK;
-            uint64_t* freed = kv ? (FP8 ? raw_free : v_free) + slot : C::kConvK ? rawk_free : k_free + slot;
-            uint64_t* full = kv ? raw_full + slot : C::kConvK ? rawk_full : k_full + slot;
-            if (uses > 0) ok = __all_sync(0xffffffffu, pipe_wait(freed, (uses - 1) & 1, s_abort, 1 + kv));
-            if (!ok) break;
-            if (kv == 0 && lane / kChunkGroups == u) s_info[(n & (kChunkInfoRing - 1)) * kChunkGroups + lane % kChunkGroups] = info;
-            __syncwarp();
-            if (lane == 0) {
-              if (going) mbar_expect_tx(full, going * p.box_rows * D * (FP8 ? 1 : 2));
-              else mbar_arrive(full);
-            }
-            __syncwarp();
-            if (copies) {
-              const CUtensorMap* map = kv ? &tmap_v : &tmap_k;
-              if constexpr (FP8) {
-                unsigned char* dst = kv ? sRaw + slot * C::kCodes : C::kConvK ? sRawK : sK + slot * C::kK;
-                tma_load_4d(dst + box * p.box_rows * D, map, full, 0, row, g.c.h, box_page);
-              } else {
+        for (int kv = 0; kv < 2; ++kv) {
+          const int slot = kv ? n % RV : C::kConvK ? 0 : n % RK, uses = kv ? n / RV : C::kConvK ? n : n / RK;
+          uint64_t* freed = kv ? (FP8 ? raw_free : v_free) + slot : C::kConvK ? rawk_free : k_free + slot;
+          uint64_t* full = kv ? raw_full + slot : C::kConvK ? rawk_full : k_full + slot;
+          if (uses > 0) ok = __all_sync(0xffffffffu, pipe_wait(freed, (uses - 1) & 1, s_abort, 1 + kv));
+          if (!ok) break;
+          if (my_tile && copies) {
+            const CUtensorMap* map = kv ? &tmap_v : &tmap_k;
+            if constexpr (FP8) {
+              unsigned char* dst = kv ? sRaw + slot * C::kCodes : C::kConvK ? sRawK : sK + slot * C::kK;
+              tma_load_4d(dst + at_row * D, map, full, 0, row, now.h, page);
+            } else {
 #pragma unroll
-                for (int sl = 0; sl < D / 64; ++sl)
-                  tma_load_4d((kv ? sV : sK) + slot * C::kOperand + sl * kSlab + box * p.box_rows * 128, map, full, sl * 64, row, g.c.h, box_page);
-              }
+              for (int sl = 0; sl < D / 64; ++sl)
+                tma_load_4d((kv ? sV : sK) + slot * C::kOperand + sl * kSlab + at_row * 128, map, full, sl * 64, row, now.h, page);
             }
+          }
+          if (kv == 0) {
+            if (my_tile) s_info[(n & (kChunkInfoRing - 1)) * kChunkGroups + lane % kChunkGroups] = info;
+            __syncwarp();
+          }
+          if (lane == 0) {
+            if (boxes) mbar_expect_tx(full, boxes * p.box_rows * D * (FP8 ? 1 : 2));
+            else mbar_arrive(full);
           }
         }
       }
-    } while (ok && g.next(p));
+      now = next;
+      next = after;
+    }
   } else if (warp == 1) {
     // ------------------------------------------------------------------------------------------------- products
     constexpr uint32_t idesc_s = make_idesc(FP8 ? 0u : 1u, 128, kChunkKeys, false);       // (E4M3 and fp16 are both 0, each in its kind)

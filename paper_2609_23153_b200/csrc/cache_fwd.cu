@@ -160,11 +160,6 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     // ------------------------------------------------------------------------------------------------------ copies
     // The stretch goes by in batches of a few tiles of a segment, of whose groups of 16 keys every lane looks after one.  Pages are
     // asked for two batches ahead and scales one, across segments, so that only the first batch waits for them.
-    struct Batch {
-      int t, n, h;                 // first tile, tiles; key head
-      int page;                    // of the lane's group, -1: nobody sees it, or there is no such page
-      float k_scale, v_scale;
-    };
     constexpr int kBatch = 32 / kGroups;
     int t_next = g.t0;
     bool live = true;
@@ -173,7 +168,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         live = g.next(p);
         t_next = g.t0;
       }
-      Batch b{t_next, 0, 0, -1, 1.0f, 1.0f};
+      GroupBatch b{t_next, 0, 0, -1, 1.0f, 1.0f};
       if (!live) return b;
       b.n = min(kBatch, g.t1 - b.t);
       b.h = g.c.h;
@@ -183,20 +178,11 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       t_next += b.n;
       return b;
     };
-    auto ask_scales = [&](Batch& b) {
-      if ((uint32_t)b.page >= (uint32_t)p.batch.pages) b.page = -1;
-      if constexpr (FP8) {
-        if (b.page >= 0) {
-          b.k_scale = p.k_scale[(int64_t)b.page * p.Hk + b.h];
-          b.v_scale = p.v_scale[(int64_t)b.page * p.Hk + b.h];
-        }
-      }
-    };
     int slot = 0, use = 0, n = 0;        // K and V tiles take turns in the ring; tiles so far
     bool ok = true;
     const int per_box = kGroups / p.boxes;               // groups of a box
-    Batch now = ask_pages(), next = ask_pages();
-    ask_scales(now);
+    GroupBatch now = ask_pages(), next = ask_pages();
+    ask_scales<FP8>(p, now);
     while (ok && now.n > 0) {
       // a box is copied if somebody sees one of its groups; the lane of its first group copies it
       int page = now.page;
@@ -230,19 +216,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         copy(u, 1, 2 * u + 1);
       }
       // the groups' notes (what they write over belongs to tiles that left the ring long ago)
-      {
-        GroupInfo info{1.0f, 0.0f, 1.0f, now.page >= 0};
-        if constexpr (FP8) {
-          const float v = fmaxf(now.v_scale, 5.4e-20f);    // 2^-64: a scale of zero stays finite
-          info.k = now.k_scale;
-          info.v_log2 = log2f(v);
-          info.v_inv = 1.0f / v;
-        }
-        s_info[(n * kGroups + lane) & (kInfoRing * kGroups - 1)] = info;
-      }
+      s_info[(n * kGroups + lane) & (kInfoRing * kGroups - 1)] = info_of<FP8>(now);
       __syncwarp();
-      ask_scales(next);
-      const Batch after_next = ask_pages();
+      ask_scales<FP8>(p, next);
+      const GroupBatch after_next = ask_pages();
       for (int u = 0; ok && u < now.n; ++u) {
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {

@@ -263,21 +263,32 @@ __device__ __forceinline__ void split_queries(uint32_t x, uint32_t y, float to, 
   low = l[0] | l[1] << 16;
 }
 
-// What the lanes of the copying warp look up for a group of 16 keys each: the page and the scales.
+// A batch of tiles as the copying warp asks for it: every lane looks after one group of 16 keys, its page and its scales.
+struct GroupBatch {
+  int t, n, h;                   // first tile, tiles; key head
+  int page;                      // of the lane's group, -1: nobody sees it, or there is no such page
+  float k_scale, v_scale;
+};
 template <bool FP8>
-__device__ __forceinline__ int look_up_group(const CacheFwdParams& p, const int32_t* table, int h, int key, int lo, int hi, GroupInfo& info) {
-  info = {1.0f, 0.0f, 1.0f, 0};
-  int page = -1;
-  if (key < hi && key + 16 > lo) page = table[key >> p.batch.page_shift];
-  if ((uint32_t)page >= (uint32_t)p.batch.pages) return -1;
-  info.usable = 1;
+__device__ __forceinline__ void ask_scales(const CacheFwdParams& p, GroupBatch& b) {
+  if ((uint32_t)b.page >= (uint32_t)p.batch.pages) b.page = -1;
   if constexpr (FP8) {
-    info.k = p.k_scale[(int64_t)page * p.Hk + h];
-    const float v = fmaxf(p.v_scale[(int64_t)page * p.Hk + h], 5.4e-20f);      // 2^-64: a scale of zero stays finite
+    if (b.page >= 0) {
+      b.k_scale = p.k_scale[(int64_t)b.page * p.Hk + b.h];
+      b.v_scale = p.v_scale[(int64_t)b.page * p.Hk + b.h];
+    }
+  }
+}
+template <bool FP8>
+__device__ __forceinline__ GroupInfo info_of(const GroupBatch& b) {
+  GroupInfo info{1.0f, 0.0f, 1.0f, b.page >= 0};
+  if constexpr (FP8) {
+    const float v = fmaxf(b.v_scale, 5.4e-20f);      // 2^-64: a scale of zero stays finite
+    info.k = b.k_scale;
     info.v_log2 = log2f(v);
     info.v_inv = 1.0f / v;
   }
-  return page;
+  return info;
 }
 
 // the status of a call: the first CTA's work
