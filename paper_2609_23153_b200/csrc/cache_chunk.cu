@@ -48,8 +48,7 @@ struct ChunkShape {
   static constexpr int RK = kRawK ? 3 : 2, RV = 2;          // rings: K operands, V operands (and V codes)
   static constexpr int kOffK = 2 * kQ, kOffV = kOffK + RK * kK, kOffRaw = kOffV + RV * kOperand;      // raw: V codes, then (kConvK) K codes
   static constexpr int kOffMisc = kOffRaw + (FP8 ? RV * kCodes : 0) + (kConvK ? kCodes : 0);
-  static constexpr int kMisc = 256 /* barriers */ + kChunkInfoRing * kChunkGroups * (int)sizeof(GroupInfo) + 128 + 128 * 8 /* SPLIT: row sums */;
-  static constexpr int kBytes = kOffMisc + kMisc;
+  static constexpr int kFixed = kOffMisc + 256 /* barriers */ + kChunkInfoRing * kChunkGroups * (int)sizeof(GroupInfo) + 128 + 128 * 8 /* SPLIT: row sums */;
 };
 
 template <int D, bool FP8, bool SPLIT>
@@ -79,7 +78,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   uint64_t* rawk_free = bars + 17;
   uint64_t* s_full = bars + 18;       // [2] S_g complete: the product's arrival and its issuer's (who has seen the tile's descriptor)
   uint64_t* p_full = bars + 20;       // [2] 128 arrivals: weights written, S_g read
-  uint64_t* pv_done = bars + 22;      // [2]
+  uint64_t* pv_done = bars + 22;      // [2] O_g complete up to a tile: the product's arrival and its issuer's (who has seen V's operand)
   uint64_t* sums_full = bars + 24;    // SPLIT, 128 arrivals: warpgroup 1 has left its row sums, and its O is complete
   uint64_t* sums_free = bars + 25;    // SPLIT, 128 arrivals: they have been taken
   GroupInfo* s_info = reinterpret_cast<GroupInfo*>(bars + 32);          // [ring][groups]
@@ -89,7 +88,9 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   int* s_bad = reinterpret_cast<int*>(s_tmem + 2);
   int* s_warp = s_bad + 2;            // [16]
   int* s_prefix = reinterpret_cast<int*>(smem);       // [B + 1], until every warp has found its place in the line
+  const Marks<D, R, FP8> marks{reinterpret_cast<uint32_t*>(smem + C::kFixed)};
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  marks.clear_all();
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
@@ -97,7 +98,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       mbar_init(q_full + i, SPLIT ? 256 : 128);
       mbar_init(v_full + i, 128); mbar_init(v_free + i, 1);
       mbar_init(raw_full + i, 1); mbar_init(raw_free + i, 128);
-      mbar_init(s_full + i, 2); mbar_init(p_full + i, 128); mbar_init(pv_done + i, 1);
+      mbar_init(s_full + i, 2); mbar_init(p_full + i, 128); mbar_init(pv_done + i, 2);
     }
     for (int i = 0; i < RK; ++i) { mbar_init(k_full + i, C::kConvK ? 128 : 1); mbar_init(k_free + i, 1); }
     mbar_init(rawk_full, 1); mbar_init(rawk_free, 128);
@@ -247,6 +248,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         for (int kk = 0; kk < kChunkKeys / 16; ++kk)
           mma_ts<false>(tmem + 256 + w * 128, tmem + w * 128 + kk * 8, make_desc(va + ((kk * 16 * 128) >> 4), v_hi), idesc_o, first && kk == 0 ? 0u : 1u);
         tc_commit(pv_done + w);
+        mbar_arrive(pv_done + w);
         if (last) tc_commit(v_free + at % RV);
       }
       __syncwarp();
@@ -296,10 +298,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   } else if (warp >= 4 && warp < 8) {
     // -------------------------------------------------------------------------------------------------- operands
     const int tid = threadIdx.x - 128;
-    int n = 0;
+    int n = 0, segment = 0;
     bool ok = true;
-    // a tile of codes as fp16 operands; rows outside [lo, hi) and of groups that nobody sees as zeros
-    auto convert = [&](const unsigned char* codes, unsigned char* operand, const GroupInfo* info, int lo, int hi) {
+    // a tile of codes as fp16 operands
+    auto convert = [&](const unsigned char* codes, unsigned char* operand) {
       const uint32_t raw = smem_u32(codes), to = smem_u32(operand);
       constexpr int kCh = D / 16, kRowsAtOnce = 128 / kCh;                // 16-code chunks of a row
       const int c = tid % kCh;
@@ -310,7 +312,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const uint32_t from = D == 128 ? raw + r * 128 + ((c ^ (r & 7)) << 4) : raw + r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
         uint4 v;
         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from));
-        if (info != nullptr && (r < lo || r >= hi || !info[r / 16].usable)) v = make_uint4(0u, 0u, 0u, 0u);
         const uint32_t x[4] = {swap ? v.z : v.x, swap ? v.w : v.y, swap ? v.x : v.z, swap ? v.y : v.w};
         uint32_t h[8];
 #pragma unroll
@@ -322,15 +323,18 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
     };
     do {
+      // keys that every row of the item sees
+      const int all_lo = visible_keys(p.causal, g.c.seq.first_pos() + (g.row0 + g.rows - 1) / p.G, g.c.seq.len).x;
+      const int all_hi = visible_keys(p.causal, g.c.seq.first_pos() + g.row0 / p.G, g.c.seq.len).y;
+      const bool parts = all_lo > g.c.item.lo || all_hi < g.c.item.hi;
       for (int t = g.t0; ok && t < g.t1; ++t, ++n) {
-        // rows of the V tile that may be anything lie outside these
-        const int z_lo = g.c.item.lo - t * kChunkKeys, z_hi = g.c.item.hi - t * kChunkKeys;
+        const int key0 = t * kChunkKeys;
         const GroupInfo* info = s_info + (n & (kChunkInfoRing - 1)) * kChunkGroups;
         if constexpr (C::kConvK) {
           ok = __all_sync(0xffffffffu, pipe_wait(rawk_full, n & 1, s_abort, 8));
           if (ok && n >= RK) ok = __all_sync(0xffffffffu, pipe_wait(k_free + n % RK, (n / RK - 1) & 1, s_abort, 10));
           if (!ok) break;
-          convert(sRawK, sK + (n % RK) * C::kK, nullptr, 0, 0);
+          convert(sRawK, sK + (n % RK) * C::kK);
           mbar_arrive(rawk_free);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           mbar_arrive(k_full + n % RK);
@@ -339,20 +343,33 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         ok = __all_sync(0xffffffffu, pipe_wait(raw_full + slot, (n / RV) & 1, s_abort, 9));
         if (FP8 && ok && n >= RV) ok = __all_sync(0xffffffffu, pipe_wait(v_free + slot, (n / RV - 1) & 1, s_abort, 11));
         if (!ok) break;
-        if constexpr (FP8) {
-          const bool edge = z_lo > 0 || z_hi < kChunkKeys || __any_sync(0xffffffffu, lane < kChunkGroups && !info[lane % kChunkGroups].usable);
-          convert(sRaw + slot * C::kCodes, sV + slot * C::kOperand, edge ? info : nullptr, z_lo, z_hi);
-          mbar_arrive(raw_free + slot);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        } else if (tid < z_lo || tid >= z_hi || !info[tid / 16].usable) {
-          const uint32_t to = smem_u32(sV + slot * C::kOperand);
+        const bool edge = key0 < all_lo || key0 + kChunkKeys > all_hi || __any_sync(0xffffffffu, lane < kChunkGroups && !info[lane % kChunkGroups].usable);
+        if (edge) {
+          // V's words: zeros for keys that nobody sees; and see Marks.  (E4M3: every thread what it converts next)
+          constexpr int kLanes = FP8 ? D / 16 : 1, kRowsAtOnce = 128 / kLanes, kWords = FP8 ? 4 : D / 2;
+          unsigned char* tile = FP8 ? sRaw + slot * C::kCodes : sV + slot * C::kOperand;
 #pragma unroll 1
-          for (int i = 0; i < D / 8; ++i)
-            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(to + (i >> 3) * kSlab + tid * 128 + ((i & 7) << 4)), "r"(0u) : "memory");
+          for (int i = 0; i < kChunkKeys / kRowsAtOnce * kWords; ++i) {
+            const int r = i / kWords * kRowsAtOnce + tid / kLanes, ch = FP8 ? tid % kLanes * 16 + i % kWords * 4 : i * 2;
+            uint32_t at;
+            if constexpr (!FP8) at = (ch >> 6) * kSlab + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4) + (ch & 7) * 2;
+            else if constexpr (D == 128) at = r * 128 + (((ch >> 4) ^ (r & 7)) << 4) + (ch & 15);
+            else at = r * 64 + (((ch >> 4) ^ ((r >> 1) & 3)) << 4) + (ch & 15);
+            uint32_t* word = reinterpret_cast<uint32_t*>(tile + at);
+            const uint32_t x = *word;
+            if (key0 + r < g.c.item.lo || key0 + r >= g.c.item.hi || !info[r / 16].usable) *word = 0u;
+            else if (parts && word_not_finite<FP8>(x)) *word = mark_word<D, R, FP8>(p, marks, segment, g.c.seq, g.row0, g.rows, key0 + r, ch, x);
+          }
+          if constexpr (!FP8) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        if constexpr (FP8) {
+          convert(sRaw + slot * C::kCodes, sV + slot * C::kOperand);
+          mbar_arrive(raw_free + slot);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         mbar_arrive(v_full + slot);
       }
+      ++segment;
     } while (ok && g.next(p));
   } else if (warp >= 8) {
     // --------------------------------------------------------------------------------------------------- softmax
@@ -362,7 +379,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const uint32_t tS = tmem + w * 128 + lane_off, tO = tmem + 256 + w * 128 + lane_off;
     int n = 0;                      // tiles in front of the segment
     int mine = 0;                   // tiles of this warpgroup so far
-    [[maybe_unused]] int segments = 0;
+    int segment = 0;                // of the stretch
+    [[maybe_unused]] int merges = 0;
     bool ok = true;
     // A row of the segment at hand: where its output goes, the keys it sees, its logits' factor
     struct Row {
@@ -439,6 +457,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     while (live && idle()) {
       n += g.t1 - g.t0;
       live = g.next(p);
+      ++segment;
     }
     if (live) take_queries();
     while (live) {
@@ -570,12 +589,15 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       // The next segment's queries go first (not where the two halves share them): its first product then runs while this output is read.
       const bool there = at.there, whole = g.whole;
       const int token = at.token, head = at.head, slot = 2 * ((int)blockIdx.x - 1) + (g.first ? 0 : 1);
+      const int set = segment;
       n += tiles;
       auto go_on = [&] {
         live = g.next(p);
+        ++segment;
         while (live && idle()) {
           n += g.t1 - g.t0;
           live = g.next(p);
+          ++segment;
         }
         if (live) take_queries();
       };
@@ -589,12 +611,12 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           s_sums[row] = make_float2(m, l);
           tc_fence_before();
           mbar_arrive(sums_full);
-          ok = __all_sync(0xffffffffu, pipe_wait(sums_free, segments++ & 1, s_abort, 18));
+          ok = __all_sync(0xffffffffu, pipe_wait(sums_free, merges++ & 1, s_abort, 18));
           if (!ok) break;
           go_on();
           continue;
         }
-        ok = __all_sync(0xffffffffu, pipe_wait(sums_full, segments++ & 1, s_abort, 19));
+        ok = __all_sync(0xffffffffu, pipe_wait(sums_full, merges++ & 1, s_abort, 19));
         if (!ok) break;
         const float2 its = s_sums[row];
         other = tiles > 1;
@@ -605,6 +627,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         m = to;
       }
       tc_fence_after();
+      const bool marked = tiles > 0 && *reinterpret_cast<volatile uint32_t*>(marks.any(set)) != 0u;
       const bool empty = m == -INFINITY && l == l;            // the row sees no key
       const float inv = empty ? 0.0f : 1.0f / l;
 #pragma unroll 1
@@ -620,6 +643,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
             for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(__uint_as_float(x[j]), f_other, __uint_as_float(o[j]) * f_own));
           }
+        }
+        if (marked && there) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(marks.add(set, r, ch * 32 + j, __uint_as_float(o[j])));
         }
         if (there && whole) {
           uint4* dst = reinterpret_cast<uint4*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + ch * 32);
@@ -645,6 +672,11 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (p.lse) p.lse[(int64_t)token * p.H + head] = empty ? -INFINITY : (m - kBase + log2f(l)) * 0.6931471805599453f;
       } else if (there) {
         *reinterpret_cast<float2*>(p.part_ml + ((int64_t)slot * R + r) * 2) = make_float2(m, empty ? 0.0f : l);
+      }
+      if (marked) {
+        // this row's marks are taken; the flag stays up for the other rows, and for whoever uses the set next, where it finds nothing
+#pragma unroll 1
+        for (int j = 0; j < Marks<D, R, FP8>::kSigns * Marks<D, R, FP8>::kWords; ++j) marks.row(set, r)[j] = 0u;
       }
       if constexpr (SPLIT) {
         mbar_arrive(sums_free);
@@ -673,8 +705,8 @@ static int launch_chunk(const sparkattn_cache_t& c, CacheFwdParams& p, const voi
   p.boxes = kChunkKeys / p.box_rows;
   if ((rc = make_page_map(&mk, k_cache, FP8 ? 1 : 2, c, p.box_rows)) != SPARKATTN_OK) return rc;
   if ((rc = make_page_map(&mv, v_cache, FP8 ? 1 : 2, c, p.box_rows)) != SPARKATTN_OK) return rc;
-  static_assert(C::kBytes <= 232448 && (kCacheMaxSequences + 1) * 4 <= 2 * C::kQ, "fits an SM");
-  constexpr int smem = C::kBytes;
+  constexpr int smem = C::kFixed + Marks<D, R, FP8>::kBytes;
+  static_assert(smem <= 232448 && (kCacheMaxSequences + 1) * 4 <= 2 * C::kQ, "fits an SM");
   auto kern = cache_chunk_kernel<D, FP8, SPLIT>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kChunkThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;

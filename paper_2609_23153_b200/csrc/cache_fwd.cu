@@ -92,7 +92,7 @@ struct DecodeShape {
   static constexpr int kPerSM = decode_ctas_per_sm(D, FP8, R);
   static constexpr int kMergeBytes = kComputeWarps * R * (kOPitch + 2) * 4;
   static constexpr int fixed_bytes(int B, int slots) {
-    return kMergeBytes + kInfoRing * kGroups * (int)sizeof(GroupInfo) + slots * 16 + 64 + ((B + 1) * 4 > R * 8 ? (B + 1) * 4 : R * 8) + 64;
+    return Marks<D, R, FP8>::kBytes + kMergeBytes + kInfoRing * kGroups * (int)sizeof(GroupInfo) + slots * 16 + 64 + ((B + 1) * 4 > R * 8 ? (B + 1) * 4 : R * 8) + 64;
   }
 };
 
@@ -106,7 +106,8 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
   constexpr int R = S::R, kRowBytes = S::kRowBytes, kTileKeys = S::kTileKeys, kGroups = S::kGroups, kPerWarp = S::kPerWarp;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* after = smem + p.slots * S::kTileBytes;
-  float* s_o = reinterpret_cast<float*>(after);                                      // [warps][R][pitch]
+  const Marks<D, R, FP8> marks{reinterpret_cast<uint32_t*>(after)};
+  float* s_o = reinterpret_cast<float*>(after + Marks<D, R, FP8>::kBytes);           // [warps][R][pitch]
   float2* s_ml = reinterpret_cast<float2*>(s_o + kComputeWarps * R * S::kOPitch);    // [warps][R]
   GroupInfo* s_info = reinterpret_cast<GroupInfo*>(s_ml + kComputeWarps * R);        // [ring][groups]
   uint64_t* full = reinterpret_cast<uint64_t*>(s_info + kInfoRing * kGroups);
@@ -128,6 +129,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     mbar_fence_init();
     *s_abort = 0;
   }
+  marks.clear_all();
   pdl_wait();
   Stretch<R, kTileKeys, kDecodeOver> g;
   int worker = 0;
@@ -449,11 +451,18 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
               pf[u][nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
               pf[u][nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
             } else {
-              const __nv_bfloat162 a = __floats2bfloat162_rn(w[0], w[1]), b = __floats2bfloat162_rn(w[2], w[3]);
-              const float2 fa = __bfloat1622float2(a), fb = __bfloat1622float2(b);
-              const __nv_bfloat162 la = __floats2bfloat162_rn(w[0] - fa.x, w[1] - fa.y), lb = __floats2bfloat162_rn(w[2] - fb.x, w[3] - fb.y);
-              pf[u][nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
-              pf[u][nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
+              // (the first cut off, so that the second is positive, and at least 2^-100: an infinite value then gives its infinity twice)
+              uint32_t high[4];
+              float low[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                high[i] = __float_as_uint(w[i]) & 0xffff0000u;
+                low[i] = fmaxf(w[i] - __uint_as_float(high[i]), 7.9e-31f);
+              }
+              const uint32_t a = __byte_perm(high[0], high[1], 0x7632), b = __byte_perm(high[2], high[3], 0x7632);
+              const __nv_bfloat162 la = __floats2bfloat162_rn(low[0], low[1]), lb = __floats2bfloat162_rn(low[2], low[3]);
+              pf[u][nt][0] = transpose_8x8(a);
+              pf[u][nt][1] = transpose_8x8(b);
               pf[u][nt][2] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&la));
               pf[u][nt][3] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&lb));
             }
@@ -462,6 +471,17 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         ok = wait_full();
         if (!ok) break;
         const uint32_t s_v = smem_u32(smem + slot * S::kTileBytes);
+        if (edge && (all_lo > g.c.item.lo || all_hi < g.c.item.hi)) {
+          // some rows see some of these keys and others do not: see Marks.  A lane looks at the words that it loads next
+#pragma unroll 1
+          for (int i = 0; i < kPerWarp * 4 * kVWords; ++i) {
+            const int in = (i / kVWords >> 2) * kGroupKeys + 4 * t4 + (i / kVWords & 3), key = key0 + in, channel = g8 * (D / 8) + i % kVWords * (4 / S::kElt);
+            const uint32_t at = chunk_offset<kRowBytes, kTileKeys>(row0 + in, channel * S::kElt / 16) + channel * S::kElt % 16;
+            uint32_t* word = reinterpret_cast<uint32_t*>(smem + slot * S::kTileBytes + at);
+            if (key >= g.c.item.lo && key < g.c.item.hi && info[i / kVWords / 4 % kPerWarp].usable && word_not_finite<FP8>(*word))
+              *word = mark_word<D, R, FP8>(p, marks, segments, g.c.seq, g.row0, g.rows, key, channel, *word);
+          }
+        }
         uint32_t vw[kPerWarp][4][kVWords];
 #pragma unroll
         for (int u = 0; u < kPerWarp; ++u)
@@ -546,6 +566,8 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       ok = __all_sync(0xffffffffu, pipe_wait(merged, segments & 1, s_abort, 4));
       if (!ok) break;
       const int slot = 2 * worker + (g.first ? 0 : 1);
+      const bool marked = *reinterpret_cast<volatile uint32_t*>(marks.any(segments)) != 0u;
+      if (!CLUSTER && warp == 0) marks.clear(segments + 2);    // (last read two segments ago, marked again behind the next segment's end)
       constexpr int kPer = D / 8;                            // threads of a row, eight channels each
       for (int task = threadIdx.x; task < g.rows * kPer; task += 32 * kComputeWarps) {
         const int r = task / kPer, ch = (task % kPer) * 8;
@@ -561,6 +583,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           const float* src = s_o + (w * R + r) * S::kOPitch + ch;
 #pragma unroll
           for (int j = 0; j < 8; ++j) acc[j] = fmaf(src[j], f, acc[j]);
+        }
+        if (marked) {
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) acc[j] = marks.add(segments, r, ch + j, acc[j]);
         }
         if (CLUSTER && p.cluster > 1) {
           float4* dst = reinterpret_cast<float4*>(s_o + r * S::kOPitch + ch);       // (in place of the first warp's, which this thread alone reads)

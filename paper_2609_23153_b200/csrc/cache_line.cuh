@@ -291,6 +291,68 @@ __device__ __forceinline__ GroupInfo info_of(const GroupBatch& b) {
   return info;
 }
 
+// Values that are not finite, under a mask.  In a tile that some rows of an item see only in part, a key has weight 0 for rows that do
+// not see it, and 0 times an infinity or a NaN is NaN.  There such a value becomes 0 in the product's operand, and the rows
+// that do see its key get it back at the end: a bit per row and channel for what has +infinity (or NaN) and one for -infinity (or NaN)
+// coming.  (Tiles that every row sees whole need none of this, nor do keys that no row sees: their values become zeros.)
+constexpr int kMarkSets = 4;             // of segments: whoever marks is at most two ahead of who reads
+template <int D, int R, bool FP8>
+struct Marks {
+  static constexpr int kSigns = FP8 ? 1 : 2;         // E4M3 has no infinities
+  static constexpr int kWords = D / 32;
+  static constexpr int kBytes = kMarkSets * (R * kSigns * kWords + 4) * 4;
+  uint32_t* at;
+  __device__ __forceinline__ uint32_t* any(int set) const { return at + (set & (kMarkSets - 1)) * (R * kSigns * kWords + 4); }
+  __device__ __forceinline__ uint32_t* row(int set, int r) const { return any(set) + 4 + r * kSigns * kWords; }
+  // nothing marked: all of a CTA's threads for all sets, a warp for one
+  __device__ __forceinline__ void clear_all() const {
+    for (int i = threadIdx.x; i < kBytes / 4; i += blockDim.x) at[i] = 0u;
+  }
+  __device__ __forceinline__ void clear(int set) const {
+    for (int i = threadIdx.x & 31; i < R * kSigns * kWords + 4; i += 32) any(set)[i] = 0u;
+  }
+  // x plus what is marked for it
+  __device__ __forceinline__ float add(int set, int r, int channel, float x) const {
+    const uint32_t* w = row(set, r) + channel / 32;
+    const bool up = w[0] >> (channel % 32) & 1u, down = FP8 ? up : w[(kSigns - 1) * kWords] >> (channel % 32) & 1u;
+    return x + (up ? INFINITY : 0.0f) + (down ? -INFINITY : 0.0f);
+  }
+};
+// Whether some value of a word (four E4M3 codes, or two bf16) is not finite.
+template <bool FP8>
+__device__ __forceinline__ bool word_not_finite(uint32_t w) {
+  if constexpr (FP8) return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u;
+  else return (w & 0x7f800000u) == 0x7f800000u || (w & 0x7f80u) == 0x7f80u;
+}
+// Such a word of key `key`, channels from `channel` on: its values that are not finite are marked for the rows that see the key, and
+// become zeros.  (Inlined, and in loops that stay loops: the operand warps have few registers, and no call may take more.)
+template <int D, int R, bool FP8>
+__device__ __forceinline__ uint32_t mark_word(const CacheFwdParams& p, const Marks<D, R, FP8> marks, int set, const Sequence seq, int row0, int rows, int key,
+                                           int channel, uint32_t w) {
+  constexpr int kPer = FP8 ? 4 : 2, kBits = 32 / kPer;
+  uint32_t up = 0u, down = 0u, out = w;
+#pragma unroll 1
+  for (int i = 0; i < kPer; ++i) {
+    const uint32_t v = w >> (i * kBits) & (FP8 ? 0xffu : 0xffffu);
+    const bool bad = FP8 ? (v & 0x7fu) == 0x7fu : (v & 0x7f80u) == 0x7f80u;
+    if (!bad) continue;
+    const bool nan = FP8 || (v & 0x7fu) != 0u;
+    if (nan || !(v & 0x8000u)) up |= 1u << ((channel + i) % 32);
+    if (nan || (v & 0x8000u)) down |= 1u << ((channel + i) % 32);
+    out &= ~((FP8 ? 0xffu : 0xffffu) << (i * kBits));
+  }
+#pragma unroll 1
+  for (int r = 0; r < rows; ++r) {
+    const int2 seen = visible_keys(p.causal, seq.first_pos() + (row0 + r) / p.G, seq.len);
+    if (key < seen.x || key >= seen.y) continue;
+    uint32_t* to = marks.row(set, r) + channel / 32;
+    if (up) atomicOr(to, up);
+    if (!FP8 && down) atomicOr(to + (Marks<D, R, FP8>::kSigns - 1) * Marks<D, R, FP8>::kWords, down);
+    *reinterpret_cast<volatile uint32_t*>(marks.any(set)) = 1u;
+  }
+  return out;
+}
+
 // the status of a call: the first CTA's work
 __device__ __forceinline__ void check_call(const CacheFwdParams& p, int* s_bad) {
   check_batch(p.batch, s_bad, [&](const Sequence& s) {

@@ -280,3 +280,318 @@ def test_append_bits(case, layout):
     assert again.data_ptr() == q.data_ptr() and same_bits(again, want_q)         # in place, and appending again changes nothing
     for got, ref in zip(cache, want):
         assert got is None or same_bits(got, ref)
+
+
+# ------------------------------------------------------------------------------------------------- what must not be looked at
+
+def poisoned(cache, table, lens, page):
+    """The cache with NaN, infinities and the type's largest values wherever no sequence has a token: behind the last token of a page,
+    and in pages of nobody."""
+    fp8 = cache.k_scale is not None
+    owned = torch.zeros((cache.k.shape[0], page), dtype=torch.bool, device=DEV)
+    for b, n in enumerate(lens):
+        for i in range(-(-n // page)):
+            owned[int(table[b, i]), :min(page, n - i * page)] = True
+    junk = torch.tensor([0x7f, 0xff, 0x7e, 0xfe] if fp8 else [0x7fc0, -0x0080, 0x7f80, 0x7f7f], device=DEV)
+    out = []
+    for x in (cache.k, cache.v):
+        bits = x.view(torch.uint8 if fp8 else torch.int16).clone(memory_format=torch.preserve_format)
+        pattern = junk[torch.arange(bits.numel(), device=DEV) % 4].view(bits.shape).to(bits.dtype)
+        bits = torch.where(owned[:, None, :, None], bits, pattern)
+        out.append(bits.view(x.dtype))
+    scales = []
+    for s in (cache.k_scale, cache.v_scale):
+        if s is not None:
+            s = s.clone()
+            s[~owned.any(1)] = math.nan
+        scales.append(s)
+    return sa.KVCache(*out, *scales)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("d,page,G,news", [(128, 64, 1, [1, 1, 1]), (128, 16, 4, [3, 2, 4]), (64, 128, 2, [1, 1, 1]), (128, 128, 2, [60, 1, 17]),
+                                           (64, 32, 3, [200, 5, 90]), (128, 32, 4, [150, 31, 2])])
+def test_nothing_behind_the_last_token(fp8, d, page, G, news):
+    gen = torch.Generator(device=DEV).manual_seed(page + G)
+    lens, Hk = [517, 33, 260], 3
+    pages = sum(-(-n // page) for n in lens) + 4
+    cache = make_cache(gen, pages, Hk, page, d, fp8, general=fp8)
+    table = make_table(gen, lens, page, pages, spare=3)
+    kv_len, q_start = batch_of(lens, news)
+    q = torch.randn((sum(news), Hk * G, d), generator=gen, device=DEV).bfloat16()
+    for frame, window in ((1, 0), (1, 70), (0, 0), (40, 2)):
+        want = sa.cache_fwd(q, cache, table, kv_len, q_start=q_start, max_new=max(news), frame_tokens=frame, window=window, return_lse=True)
+        got = sa.cache_fwd(q, poisoned(cache, table, lens, page), table, kv_len, q_start=q_start, max_new=max(news), frame_tokens=frame,
+                           window=window, return_lse=True, check_status=True)
+        assert all(torch.isfinite(x).all() for x in want)
+        assert all(same_bits(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("d,G,n,length", [(128, 2, 4, 300), (64, 4, 4, 150), (128, 1, 200, 500), (128, 4, 100, 257), (64, 1, 300, 300), (128, 2, 40, 128)])
+@pytest.mark.parametrize("frame,window", [(1, 0), (1, 40), (16, 2)])
+def test_values_that_are_not_finite_reach_only_who_sees_them(fp8, d, G, n, length, frame, window):
+    """NaN and infinities in keys and values: the rows that see such a key have what the formula gives (NaN in the channels of a value,
+    everywhere for a key), all others are bit for bit what they are without."""
+    gen = torch.Generator(device=DEV).manual_seed(n + d)
+    page, Hk = 32, 2
+    pages = -(-length // page)
+    cache = make_cache(gen, pages, Hk, page, d, fp8)
+    table = make_table(gen, [length], page, pages)
+    kv_len, q_start = batch_of([length], [n])
+    q = torch.randn((n, Hk * G, d), generator=gen, device=DEV).bfloat16()
+    kw = dict(q_start=q_start, max_new=n, frame_tokens=frame, window=window, return_lse=True)
+    clean, clean_lse = sa.cache_fwd(q, cache, table, kv_len, **kw)
+    marks = [(length - 1, 3, math.nan), (length - n // 2, 5, math.nan), (length - n // 2, 9, math.inf), (max(0, length - n - 20), 1, -math.inf),
+             (length - n // 2 - 1, 9, -math.inf)]
+    bad_key = length - n // 3 - 1
+    k, v = (x.clone(memory_format=torch.preserve_format) for x in cache[:2])
+
+    def put(x, j, h, c, value):
+        at = (int(table[0, j // page]), h, j % page, c)
+        if fp8:
+            x.view(torch.uint8)[at] = 0x7f                    # E4M3 has no infinity
+        else:
+            x[at] = value
+    for j, c, value in marks:
+        put(v, j, 0, c, value)
+    put(k, bad_key, 1, 7, math.nan)
+    got, lse = sa.cache_fwd(q, sa.KVCache(k, v, *cache[2:]), table, kv_len, **kw)
+    want, want_lse = clean.float(), clean_lse.clone()
+    for i in range(n):
+        lo, hi = visible(length - n + i, length, frame, window)
+        for j, c, value in marks:
+            if lo <= j < hi:
+                want[i, :G, c] += math.nan if fp8 else value
+        if lo <= bad_key < hi:
+            want[i, G:] = math.nan
+            want_lse[i, G:] = math.nan
+    want = want.bfloat16()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isnan(lse), torch.isnan(want_lse))
+    assert same_bits(torch.where(torch.isnan(want), 0.0, got), torch.where(torch.isnan(want), 0.0, want))
+    fine = ~torch.isnan(want_lse)
+    assert same_bits(lse[fine], want_lse[fine])
+
+
+def test_pages_that_do_not_exist():
+    """A page number outside the pool: reported, its tokens are not attended to and not stored."""
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    for n, H in ((1, 4), (40, 4)):
+        lens = [300, 200]
+        cache = make_cache(gen, 12, 2, 64, 128, True)
+        table = make_table(gen, lens, 64, 12)
+        kv_len, q_start = batch_of(lens, [n, n])
+        q = torch.randn((2 * n, H, 128), generator=gen, device=DEV).bfloat16()
+        broken = table.clone()
+        broken[0, 1], broken[1, 0] = 12, -1
+        ws = torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+        out, lse = sa.cache_fwd(q, cache, broken, kv_len, q_start=q_start, max_new=n, frame_tokens=0, return_lse=True, workspace=ws)
+        assert sa.read_status(ws) == sa.E_BAD_INDEX
+        # the same without those keys: they become the last ones, behind the length
+        for b, gone in ((0, 1), (1, 0)):
+            keep = [i for i in range(-(-lens[b] // 64)) if i != gone]
+            t2 = table[b:b + 1, keep].contiguous()
+            want, want_lse = sa.cache_fwd(q[b * n:(b + 1) * n], cache, t2, kv_len[b:b + 1] - 64, max_new=n, frame_tokens=0, return_lse=True, workspace=ws)
+            assert sa.read_status(ws) == sa.OK
+            assert (out[b * n:(b + 1) * n].float() - want.float()).abs().max() <= 2 ** -7 * want.float().abs().max()
+            assert (lse[b * n:(b + 1) * n] - want_lse).abs().max() <= 1e-4
+        before = [x.clone() for x in cache]
+        k = torch.randn((2 * n, 2, 128), generator=gen, device=DEV).bfloat16()
+        broken[:] = 99
+        sa.cache_append(cache, k, k, broken, kv_len, q_start=q_start, max_new=n, workspace=ws)
+        assert sa.read_status(ws) == sa.E_BAD_INDEX
+        assert all(same_bits(x, y) for x, y in zip(cache, before))
+
+
+@pytest.mark.parametrize("what", ["negative length", "length beyond the table", "starts descend", "starts beyond the rows", "more than max_new"])
+def test_numbers_that_do_not_fit_stay_inside(what):
+    """Device-side numbers of a broken caller: reported, and nothing outside the tensors is touched (the call ends, its neighbours' pages
+    keep their bits)."""
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    cache = make_cache(gen, 8, 2, 16, 64, True)
+    table = make_table(gen, [40, 50], 16, 8, spare=0)
+    lens, starts = [40, 50], [0, 3, 6]
+    if what == "negative length":
+        lens[0] = -5
+    elif what == "length beyond the table":
+        lens[1] = 100000
+    elif what == "starts descend":
+        starts = [4, 2, 6]
+    elif what == "starts beyond the rows":
+        starts = [0, 3, 900]
+    kv_len = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    q_start = torch.tensor(starts, dtype=torch.int32, device=DEV)
+    q = torch.randn((6, 4, 64), generator=gen, device=DEV).bfloat16()
+    max_new = 2 if what == "more than max_new" else 3
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+    sa.cache_fwd(q, cache, table, kv_len, q_start=q_start, max_new=max_new, workspace=ws)
+    assert sa.read_status(ws) == sa.E_BAD_INDEX
+    k = q[:, :2].contiguous()
+    sa.cache_append(cache, k, k, table, kv_len, q_start=q_start, max_new=max_new, q=q, workspace=ws)
+    assert sa.read_status(ws) == sa.E_BAD_INDEX
+
+
+# --------------------------------------------------------------------------------------------------------- shapes of memory
+
+@pytest.mark.parametrize("news", [[1], [30]])
+def test_offsets_beyond_32_bits(news):
+    """A pool of 2.7 billion entries per side, whose last pages hold the sequence."""
+    pages, Hk, page, d = 41000, 8, 64, 128
+    pools = [torch.empty((pages, Hk, page, d), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.ones((pages, Hk), device=DEV) for _ in range(2)]
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    lens = [333]
+    table = torch.arange(pages - 6, pages, device=DEV, dtype=torch.int32)[None].contiguous()
+    kv_len, q_start = batch_of(lens, lens)
+    k, v = (torch.randn((333, Hk, d), generator=gen, device=DEV).bfloat16() for _ in range(2))
+    cache = sa.KVCache(*pools, *scales)
+    sa.cache_append(cache, k, v, table, kv_len, q_start=q_start, max_new=333, check_status=True)
+    small = sa.KVCache(*(x[-6:].clone() for x in cache))
+    check_k = small.k.view(torch.uint8).view(torch.float8_e4m3fn).float() * small.k_scale[:, :, None, None]
+    got = check_k.transpose(1, 2).reshape(-1, Hk, d)[:333]
+    assert (got - k.float()).abs().max() <= 2 ** -4 * k.float().abs().max()
+    q = torch.randn((news[0], 16, d), generator=gen, device=DEV).bfloat16()
+    a = sa.cache_fwd(q, cache, table, kv_len, check_status=True)
+    b = sa.cache_fwd(q, small, table - (pages - 6), kv_len, check_status=True)
+    assert same_bits(a, b)
+
+
+@pytest.mark.parametrize("n", [1, 3, 50])
+def test_views_streams_and_defaults(n):
+    """Rows of fused projections, an output inside a larger tensor, equal shares without q_start, another stream, a captured graph
+    whose lengths change between replays: the same bits every time."""
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    B, Hk, G, page, d = 3, 2, 3, 32, 128
+    lens = [200, 77, 130]
+    cache = make_cache(gen, 30, Hk, page, d, True)
+    table = make_table(gen, [256] * 3, page, 30)
+    kv_len, q_start = batch_of(lens, [n] * B)
+    rows = torch.randn((B * n, 20, d), generator=gen, device=DEV).bfloat16()
+    q = rows[:, 4:4 + Hk * G]
+    want, want_lse = sa.cache_fwd(q.contiguous(), cache, table, kv_len, q_start=q_start, max_new=n, return_lse=True)
+    room = torch.zeros((B * n, 3, Hk * G, d), dtype=torch.bfloat16, device=DEV)
+    got = sa.cache_fwd(q, cache, table, kv_len, out=room[:, 1])
+    assert got.data_ptr() == room[:, 1].data_ptr() and same_bits(got, want)
+    assert (room[:, 0] == 0).all() and (room[:, 2] == 0).all()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    x, lse = sa.cache_fwd(q, cache, table, kv_len, stream=side, return_lse=True, max_new=n)
+    side.synchronize()
+    assert same_bits(x, want) and same_bits(lse, want_lse)
+    graph = torch.cuda.CUDAGraph()
+    length = kv_len.clone()
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(want)
+    with torch.cuda.graph(graph):
+        sa.cache_fwd(q, cache, table, length, out=out, workspace=ws)
+    for lens2 in ([200, 77, 130], [60, 256, 51], [200, 77, 130]):
+        length.copy_(torch.tensor(lens2, dtype=torch.int32, device=DEV))
+        graph.replay()
+        want2 = sa.cache_fwd(q, cache, table, length)
+        assert same_bits(out, want2) and sa.read_status(ws) == sa.OK
+
+
+def test_many_short_sequences():
+    """More sequences than CTAs, lengths from zero on, one to three new tokens."""
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    B = 700
+    news = [1 + i % 3 for i in range(B)]
+    lens = [max(news[i], (i * 7) % 40) if i % 11 else 0 for i in range(B)]
+    news = [min(n, max(length, 1)) for n, length in zip(news, lens)]
+    pages = sum(-(-n // 16) for n in lens) + 1
+    cache = make_cache(gen, pages, 2, 16, 64, True)
+    table = make_table(gen, lens, 16, pages)
+    kv_len, q_start = batch_of(lens, news)
+    for H in (2, 12, 64):
+        q = torch.randn((sum(news), H, 64), generator=gen, device=DEV).bfloat16()
+        out, lse = sa.cache_fwd(q, cache, table, kv_len, q_start=q_start, max_new=3, return_lse=True)
+        want, want_lse = reference(q, cache, table, lens, news, 1, 0)
+        check(out, lse, want, want_lse)
+
+
+@pytest.mark.parametrize("scale", [0.02, 1.7])
+def test_softmax_scale_and_sharp_rows(scale):
+    """A scale of the caller's, and logits far apart: one key takes nearly everything, others underflow."""
+    gen = torch.Generator(device=DEV).manual_seed(13)
+    for n in (1, 20):
+        cache = make_cache(gen, 40, 2, 32, 128, True, general=True)
+        lens, news = [900], [n]
+        table = make_table(gen, lens, 32, 40)
+        kv_len, q_start = batch_of(lens, news)
+        q = (3 * torch.randn((n, 4, 128), generator=gen, device=DEV)).bfloat16()
+        out, lse = sa.cache_fwd(q, cache, table, kv_len, softmax_scale=scale, return_lse=True, check_status=True)
+        want, want_lse = reference(q, cache, table, lens, news, 1, 0, scale)
+        rms = (out.double() - want).square().mean().sqrt() / want.square().mean().sqrt()
+        # logits of up to a few thousand carry fp32's rounding: 2^-22 of the largest
+        tol = 2 ** -22 * float(want_lse.abs().max()) * 16
+        print(float(rms), float((lse - want_lse).abs().max()), tol)
+        assert rms <= OUT_RELRMS + 2 * tol and (lse - want_lse).abs().max() <= LSE_ABS + tol
+
+
+# --------------------------------------------------------------------------------------------------- how a page fills up
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("steps", [[1] * 40, [7, 1, 20, 3, 9], [40]])
+def test_a_page_hardly_depends_on_its_steps(fp8, steps):
+    """Token by token or at once: each way is the restatement's bits, and with power-of-two scales what they hold differs only where
+    small values had been rounded to a larger scale's subnormal numbers before."""
+    gen = torch.Generator(device=DEV).manual_seed(21)
+    Hk, page, d, total = 3, 16, 64, 40
+    k, v = (torch.randn((total, Hk, d), generator=gen, device=DEV) * torch.exp(torch.randn((total, Hk, 1), generator=gen, device=DEV) * 1.5) for _ in range(2))
+    k, v = k.bfloat16(), v.bfloat16()
+    k[5, 0, 3], k[6, 1, 0], v[11, 2, 1] = math.inf, math.nan, -math.inf
+    cache = sa.alloc_cache(4, Hk, page, d, fp8=fp8)
+    table = torch.tensor([[2, 0, 3]], dtype=torch.int32, device=DEV)
+    want = sa.KVCache(*(None if x is None else x.clone() for x in cache))
+    at = 0
+    for n in steps:
+        at += n
+        kv_len = torch.tensor([at], dtype=torch.int32, device=DEV)
+        sa.cache_append(cache, k[at - n:at], v[at - n:at], table, kv_len, check_status=True)
+        want, _ = append_reference(want, k[at - n:at], v[at - n:at], table, [at], [n], None, None)
+        for got, ref in zip(cache, want):
+            if got is not None and got.dtype == torch.float32:
+                assert same_bits(got, ref)
+            elif got is not None:      # NaN is NaN, whichever
+                a, b = got.cpu().float(), ref.float()
+                assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a, 0.0), torch.nan_to_num(b, 0.0))
+    if fp8:
+        whole = sa.alloc_cache(4, Hk, page, d)
+        sa.cache_append(whole, k, v, table, torch.tensor([total], dtype=torch.int32, device=DEV))
+        for a, b, s, t in ((cache.k, whole.k, cache.k_scale, whole.k_scale), (cache.v, whole.v, cache.v_scale, whole.v_scale)):
+            assert torch.equal(s[[2, 0, 3]], t[[2, 0, 3]])
+            x, y = (torch.nan_to_num(z.float(), 0.0) * s[:, :, None, None] for z in (a, b))
+            # (an infinity became the largest number of the scale at its time)
+            x, y = (torch.where(b.float().abs() == 448, 0.0, z) for z in (x, y))
+            assert ((x - y).abs() <= s[:, :, None, None] * 2.0 ** -9).all()          # half a subnormal step twice
+
+
+def test_append_then_attend_is_attention():
+    """The two calls together, token by token, against softmax attention in 64 bits over the rotated bf16 values: bf16 pages exactly those
+    values, E4M3 pages within the codes' rounding."""
+    gen = torch.Generator(device=DEV).manual_seed(31)
+    H, Hk, d, page, total = 4, 2, 128, 16, 50
+    rotary = make_rotary(gen, d, d, total, total, 0, False)
+    q, k, v = (torch.randn((total, h, d), generator=gen, device=DEV).bfloat16() for h in (H, Hk, Hk))
+    m = torch.arange(total, device=DEV)
+    turn = lambda x: torch.stack([turned(x[i].float(), rotary.cos[i], rotary.sin[i], False) for i in m.tolist()]).bfloat16()
+    qr, kr = turn(q).double(), turn(k).double()
+    want = torch.zeros((total, H, d), dtype=torch.float64, device=DEV)
+    for i in range(total):
+        for h in range(H):
+            a = torch.softmax(kr[:i + 1, h // 2] @ qr[i, h] * d ** -0.5, 0)
+            want[i, h] = a @ v[:i + 1, h // 2].double()
+    for fp8, bar in ((False, OUT_RELRMS), (True, 5e-2)):
+        cache = sa.alloc_cache(5, Hk, page, d, fp8=fp8)
+        table = torch.tensor([[4, 1, 0, 2]], dtype=torch.int32, device=DEV)
+        outs, at = [], 0
+        for n in [3, 1, 1, 20, 1, 24]:
+            at += n
+            kv_len = torch.tensor([at], dtype=torch.int32, device=DEV)
+            part = slice(at - n, at)
+            rq = sa.cache_append(cache, k[part], v[part], table, kv_len, q=q[part], rotary=rotary, check_status=True)
+            outs.append(sa.cache_fwd(rq, cache, table, kv_len, check_status=True))
+        got = torch.cat(outs).double()
+        rms = (got - want).square().mean().sqrt() / want.square().mean().sqrt()
+        print(fp8, float(rms))
+        assert rms <= bar
