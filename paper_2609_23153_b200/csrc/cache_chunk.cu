@@ -346,19 +346,24 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const bool edge = key0 < all_lo || key0 + kChunkKeys > all_hi || __any_sync(0xffffffffu, lane < kChunkGroups && !info[lane % kChunkGroups].usable);
         if (edge) {
           // V's words: zeros for keys that nobody sees; and see Marks.  (E4M3: every thread what it converts next)
-          constexpr int kLanes = FP8 ? D / 16 : 1, kRowsAtOnce = 128 / kLanes, kWords = FP8 ? 4 : D / 2;
+          constexpr int kPer = FP8 ? 16 : 8, kLanes = FP8 ? D / 16 : 1, kRowsAtOnce = 128 / kLanes, kChunks = FP8 ? 1 : D / 8;      // 16-byte chunks
           unsigned char* tile = FP8 ? sRaw + slot * C::kCodes : sV + slot * C::kOperand;
 #pragma unroll 1
-          for (int i = 0; i < kChunkKeys / kRowsAtOnce * kWords; ++i) {
-            const int r = i / kWords * kRowsAtOnce + tid / kLanes, ch = FP8 ? tid % kLanes * 16 + i % kWords * 4 : i * 2;
-            uint32_t at;
-            if constexpr (!FP8) at = (ch >> 6) * kSlab + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4) + (ch & 7) * 2;
-            else if constexpr (D == 128) at = r * 128 + (((ch >> 4) ^ (r & 7)) << 4) + (ch & 15);
-            else at = r * 64 + (((ch >> 4) ^ ((r >> 1) & 3)) << 4) + (ch & 15);
-            uint32_t* word = reinterpret_cast<uint32_t*>(tile + at);
-            const uint32_t x = *word;
-            if (key0 + r < g.c.item.lo || key0 + r >= g.c.item.hi || !info[r / 16].usable) *word = 0u;
-            else if (parts && word_not_finite<FP8>(x)) *word = mark_word<D, R, FP8>(p, marks, segment, g.c.seq, g.row0, g.rows, key0 + r, ch, x);
+          for (int i = 0; i < kChunkKeys / kRowsAtOnce * kChunks; ++i) {
+            const int r = i / kChunks * kRowsAtOnce + tid / kLanes, c = FP8 ? tid % kLanes : i % kChunks;
+            uint4* chunk = reinterpret_cast<uint4*>(tile + (FP8 && D == 64 ? r * 64 + ((c ^ ((r >> 1) & 3)) << 4) : (c >> 3) * kSlab + r * 128 + (((c & 7) ^ (r & 7)) << 4)));
+            if (key0 + r < g.c.item.lo || key0 + r >= g.c.item.hi || !info[r / 16].usable) {
+              *chunk = make_uint4(0u, 0u, 0u, 0u);
+            } else if (parts) {
+              const uint4 x = *chunk;
+              if (word_not_finite<FP8>(x.x) || word_not_finite<FP8>(x.y) || word_not_finite<FP8>(x.z) || word_not_finite<FP8>(x.w)) {
+                uint32_t* word = reinterpret_cast<uint32_t*>(chunk);
+#pragma unroll 1
+                for (int j = 0; j < 4; ++j)
+                  if (word_not_finite<FP8>(word[j]))
+                    word[j] = mark_word<D, R, FP8>(p, marks, segment, g.c.seq, g.row0, g.rows, key0 + r, c * kPer + j * (kPer / 4), word[j]);
+              }
+            }
           }
           if constexpr (!FP8) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }

@@ -96,6 +96,24 @@ struct DecodeShape {
   }
 };
 
+// Some rows see some of a warp's keys of a tile and others do not: see Marks.  A lane looks at the words of V that it loads next.  (A
+// function of its own: in the tile loop its code cost the smallest call 0.7 us.)
+template <int D, bool FP8, int NT>
+__device__ __noinline__ void mark_tile(const CacheFwdParams& p, const Marks<D, 8 * NT, FP8> marks, int set, const Sequence seq, int row0, int rows, int2 seen,
+                                       int key0, int tile_row0, int usable, unsigned char* tile) {
+  using S = DecodeShape<D, FP8, NT>;
+  constexpr int kVWords = D / 8 * S::kElt / 4;
+  const int g8 = (threadIdx.x & 31) >> 2, t4 = threadIdx.x & 3;
+#pragma unroll 1
+  for (int i = 0; i < S::kPerWarp * 4 * kVWords; ++i) {
+    const int u = i / kVWords >> 2, in = u * kGroupKeys + 4 * t4 + (i / kVWords & 3), key = key0 + in, channel = g8 * (D / 8) + i % kVWords * (4 / S::kElt);
+    const uint32_t at = chunk_offset<S::kRowBytes, S::kTileKeys>(tile_row0 + in, channel * S::kElt / 16) + channel * S::kElt % 16;
+    uint32_t* word = reinterpret_cast<uint32_t*>(tile + at);
+    if (key >= seen.x && key < seen.y && (usable >> u & 1) && word_not_finite<FP8>(*word))
+      *word = mark_word<D, S::R, FP8>(p, marks, set, seq, row0, rows, key, channel, *word);
+  }
+}
+
 // CLUSTER: an item (it has one row tile) belongs to a cluster of CTAs, each takes an equal run of its key tiles, and the CTAs' results
 // are added up through distributed shared memory.  Otherwise the line, see cache_line.cuh; cluster_of has the rule.
 template <int D, bool FP8, int NT, bool CLUSTER>
@@ -471,17 +489,9 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         ok = wait_full();
         if (!ok) break;
         const uint32_t s_v = smem_u32(smem + slot * S::kTileBytes);
-        if (edge && (all_lo > g.c.item.lo || all_hi < g.c.item.hi)) {
-          // some rows see some of these keys and others do not: see Marks.  A lane looks at the words that it loads next
-#pragma unroll 1
-          for (int i = 0; i < kPerWarp * 4 * kVWords; ++i) {
-            const int in = (i / kVWords >> 2) * kGroupKeys + 4 * t4 + (i / kVWords & 3), key = key0 + in, channel = g8 * (D / 8) + i % kVWords * (4 / S::kElt);
-            const uint32_t at = chunk_offset<kRowBytes, kTileKeys>(row0 + in, channel * S::kElt / 16) + channel * S::kElt % 16;
-            uint32_t* word = reinterpret_cast<uint32_t*>(smem + slot * S::kTileBytes + at);
-            if (key >= g.c.item.lo && key < g.c.item.hi && info[i / kVWords / 4 % kPerWarp].usable && word_not_finite<FP8>(*word))
-              *word = mark_word<D, R, FP8>(p, marks, segments, g.c.seq, g.row0, g.rows, key, channel, *word);
-          }
-        }
+        if (edge && (all_lo > g.c.item.lo || all_hi < g.c.item.hi))
+          mark_tile<D, FP8, NT>(p, marks, segments, g.c.seq, g.row0, g.rows, make_int2(g.c.item.lo, g.c.item.hi), key0, row0,
+                                info[0].usable | info[kPerWarp - 1].usable << 1, smem + slot * S::kTileBytes);
         uint32_t vw[kPerWarp][4][kVWords];
 #pragma unroll
         for (int u = 0; u < kPerWarp; ++u)
