@@ -34,7 +34,7 @@ namespace sparkattn {
 constexpr int kChunkKeys = 128, kChunkThreads = 512;
 constexpr int kChunkOver = 6;                                   // tiles that the beginning and the end of an item take as long as
 constexpr int kChunkGroups = kChunkKeys / 16;
-constexpr int kSoftRegs = 192, kConvRegs = 72, kCtrlRegs = 56;      // 2 x 128 x 192 + 128 x 72 + 128 x 56 = 512 x 128
+constexpr int kSoftRegs = 208, kConvRegs = 48, kCtrlRegs = 48;      // 2 x 128 x 208 + 2 x 128 x 48 = 512 x 128
 constexpr int kChunkInfoRing = 8;                                   // tiles whose descriptors are kept: the K ring and what is still worked on
 
 template <int D, bool FP8>

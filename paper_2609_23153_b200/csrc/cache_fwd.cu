@@ -595,7 +595,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           for (int j = 0; j < 8; ++j) acc[j] = fmaf(src[j], f, acc[j]);
         }
         if (marked) {
-#pragma unroll 1
+#pragma unroll
           for (int j = 0; j < 8; ++j) acc[j] = marks.add(segments, r, ch + j, acc[j]);
         }
         if (CLUSTER && p.cluster > 1) {
