@@ -580,7 +580,7 @@ int check_pools(const sparkattn_cache_t* c, const sparkattn_batch_t* b, const vo
 }
 int check_heads(const sparkattn_cache_t* c, const sparkattn_batch_t* b, int32_t H) {
   if (H < 1 || H % c->H) return SPARKATTN_E_INVALID_ARG;
-  return (long long)b->T * H > 0x7fffffffLL ? SPARKATTN_E_UNSUPPORTED_SHAPE : SPARKATTN_OK;
+  return (long long)b->T * H > 0x7fffffffLL || !cache_work_fits(*c, *b, H) ? SPARKATTN_E_UNSUPPORTED_SHAPE : SPARKATTN_OK;
 }
 }  // namespace
 
@@ -602,6 +602,7 @@ int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch
   if ((q == nullptr) != (q_out == nullptr)) return SPARKATTN_E_INVALID_ARG;
   if (q != nullptr) {
     if (H < 1) return SPARKATTN_E_INVALID_ARG;
+    if ((long long)batch->T * H > 0x7fffffffLL - 2 * 65535) return SPARKATTN_E_UNSUPPORTED_SHAPE;
     if ((rc = check_rows(q, false)) != SPARKATTN_OK || (rc = check_rows(q_out, true)) != SPARKATTN_OK) return rc;
   }
   if (workspace_bytes < kWorkspaceHeaderBytes) return SPARKATTN_E_WORKSPACE_TOO_SMALL;

@@ -477,6 +477,8 @@ struct Cache {
     b.max_pages = (int32_t)table.size(1);
     b.page_table = iptr(table); b.kv_len = iptr(len); b.q_start = iptr(start);
   }
+  void check_device() const { TORCH_CHECK_VALUE(k.is_cuda(), "tensors of a call must be on a CUDA device"); }
+  void check_workspace(const at::Tensor& ws) const { TORCH_CHECK_VALUE(ws.device() == k.device() && ws.is_contiguous() && ws.element_size() == 1, "the workspace is contiguous bytes on the call's device"); }
   // a [T, heads, d] tensor of the call as the library takes it; heads 0: any number
   sparkattn_rows_t rows(const at::Tensor& x, int64_t heads) const {
     TORCH_CHECK_VALUE(x.dim() == 3 && x.stride(2) == 1 && x.scalar_type() == at::kBFloat16 && x.size(0) == b.T && x.size(2) == c.d &&
@@ -522,11 +524,13 @@ PyObject* cache_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     rotary.cos = fptr(cos); rotary.sin = fptr(sin);
     rotary.positions = iptr(positions); rotary.axis = iptr(axis);
   }
+  cache.check_device();
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
     if (q.defined() && !q_out.defined()) q_out = at::empty(q.sizes(), on(q, at::kBFloat16));
     if (!ws.defined()) ws = at::empty({256}, on(k, at::kByte));
+    cache.check_workspace(ws);
     sparkattn_rows_t rq{}, ro{};
     if (q.defined()) {
       rq = cache.rows(q, 0);
@@ -557,6 +561,7 @@ PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   cache.describe(q);
   const sparkattn_rows_t rq = cache.rows(q, 0);
   const int32_t H = (int32_t)q.size(1);
+  cache.check_device();
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
@@ -567,6 +572,7 @@ PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
       const size_t bytes = g_lib.cache_workspace_bytes(&cache.c, &cache.b, H);
       ws = at::empty({(int64_t)(bytes < 256 ? 256 : bytes)}, on(q, at::kByte));      // an unsupported call says why itself
     }
+    cache.check_workspace(ws);
     rc = g_lib.cache_fwd(&cache.c, &cache.b, &rq, H, ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), frame_tokens, window,
                          softmax_scale, &ro, fptr(lse), ptr(ws), (size_t)ws.numel(), stream);
   }

@@ -18,6 +18,12 @@
 // E4M3, 128 channels: K's codes are the first product's operand as they are, against the queries in two E4M3 parts
 // (split_queries): twice as many products at twice the rate.  P and V are fp16 (the weights 2^5 at the reference), and V's scale is part of the
 // exponent: t = logit + log2(v_scale), the row sum adds weight / v_scale.  bf16 pages: bf16 throughout.
+// Measured (E4M3, 128 channels; a library product of bf16 matrices reaches 1704 TFLOP/s in a burst, 1439 for seconds): 4680 new tokens,
+// three frames, over 32,760, 12 heads, 897 GFLOP in 865 us = 1040 TFLOP/s, at 1.6 GHz under the power limit: tensor cores and special-function unit are busy 52 % of the
+// clocks each, the rest is the chain that a half goes through once a tile, S, maximum, exponentials, P V.
+// Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 545 us = 930 TFLOP/s; a causal
+// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 77 us;
+// 1.3 us a tile per SM, a chain of copy, conversion, product, softmax and product that only two tiles at a time share.
 // (A quarter of the exponentials as a polynomial of degree 4 on the FMA pipe, to spare the special-function unit: 870 us
 // either way for three frames of 1560 tokens over 32,760 keys, 710 instead of 672 for four prompts.)
 #include <cuda.h>

@@ -4,13 +4,15 @@
 // A (sequence, key head) with G query heads and n new tokens has G n query rows over the same keys.  The work is reading
 // the keys and values once: 2 d bytes (E4M3) a token against 4 d G n flops, far below the tensor cores' rate, so what
 // counts is that every SM always has copies in flight, and that long and short sequences come out even.
-//   Work split: the tiles of 64 keys of all (sequence, key head, row tile) stand in one line, which is cut into equal
-//     stretches, one per CTA, two CTAs per SM.  A CTA's stretch is a sequence of segments (parts of items); an item that
-//     lies in one stretch is finished there, one that several stretches share leaves partial results (maximum, sum,
-//     unnormalised output) in the workspace, which combine_kernel, launched behind, adds up in a fixed order.
+//   Work split: an item is a (sequence, key head); a tile is 128 of its keys (bf16 with 128 channels: 64).  Two CTAs per SM.  Either
+//     each item belongs to a thread-block cluster, whose CTAs take equal runs of its tiles and add up maximum, sum and
+//     unnormalised output through distributed shared memory; or the tiles of all items stand in one line (cache_line.cuh), which is
+//     cut into equal stretches, one per CTA: an item that lies in one stretch is finished there, one that several share leaves partial
+//     results in the workspace, which combine_kernel, launched behind, adds up in a fixed order.  cluster_of has the rule and
+//     the figures of both.
 //   Copies: one warp requests the tiles with TMA (boxes of whole pages, or what a tile takes of one), as far ahead as the ring is deep, across
-//     segment borders.  It also fetches page numbers and scales, 32 groups of 16 keys at a time, one batch ahead.
-//   Products: four warps, each with 16 keys of every tile and online-softmax state of its own (merged when a segment
+//     segment borders.  It also fetches page numbers two batches of up to 32 groups of 16 keys ahead, and their scales one.
+//   Products: four warps, each with 16 or 32 keys of every tile and online-softmax state of its own (merged when a segment
 //     ends), so that nothing in the loop waits for another warp.  S^T = K Q^T and O^T = V^T P^T as m16n8k16 products with the
 //     rows as the N side: eight rows fill an instruction, where rows on the M side would leave half of it empty.
 //     The channel order of the first product and the key order of the second are free, so every lane takes its
@@ -21,6 +23,11 @@
 //   Scales: k's multiplies the logits.  v's goes into the exponent: with t = logit + log2(v_scale), the weights of the second
 //     product are 2^(t - m), m a running reference of t, and the row sum adds weight / v_scale.  So neither costs a
 //     multiplication per element.
+// Measured (one new token per sequence; bytes of keys, values and scales that must be read; E4M3, 128 channels and 8 key heads where nothing
+// else is said): 64 sequences of up to 8191 keys, 555 MB in 96 us = 5.8 TB/s, 0.90 of a copy's rate, which bounds it; one sequence
+// of 131,071 keys, 269 MB in 53 us = 5.0 TB/s, where the second launch and the way of the first tiles, 5 us each, have nothing to
+// hide behind; one of 1001 keys 7.3 us, of one key 4.8: latency.  16 sequences of up to 4095 keys, 12 heads, bf16: 206 MB in 42 us = 5.0 TB/s.
+// 32 sequences, a window of 1000 keys, 4 heads of 64 channels, pages of 16 keys: 16 MB in 11 us, latency again.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -36,6 +43,9 @@ namespace sparkattn {
 constexpr int kGroupKeys = 16;
 constexpr int kDecodeOver = 4;      // tiles that the beginning and the end of an item take as long as
 constexpr int kInfoRing = 32;      // tiles whose groups' notes are kept: a batch of up to 8 and a ring of up to 8 at a time
+// CTAs per SM: two, so that one's items begin and end while the other's copies run (64 sequences of up to 8191 keys, 8 key heads, E4M3:
+// 96 us, by one 110, by three 98; one sequence of 1001 keys 7.3, 12.5, 7.3; 64 of 1000 keys 31.9, 44.0, 37.4).
+constexpr int kDecodePerSM = 2;
 constexpr int kComputeWarps = 4, kDecodeThreads = 32 * (kComputeWarps + 1);
 
 // ---------------------------------------------------------------------------------------------------------- fragments
@@ -75,9 +85,6 @@ __device__ __forceinline__ uint2 lds8(uint32_t at) {
   return v;
 }
 
-// CTAs per SM, as registers and the rings allow
-constexpr int decode_ctas_per_sm(int D, bool fp8, int R) { return 2; }
-
 template <int D, bool FP8, int NT>
 struct DecodeShape {
   static constexpr int R = 8 * NT;
@@ -89,7 +96,6 @@ struct DecodeShape {
   static constexpr int kGroups = kComputeWarps * kPerWarp, kTileKeys = kGroups * kGroupKeys;
   static constexpr int kTileBytes = kTileKeys * kRowBytes;       // of K or of V
   static constexpr int kOPitch = D + 4;
-  static constexpr int kPerSM = decode_ctas_per_sm(D, FP8, R);
   static constexpr int kMergeBytes = kComputeWarps * R * (kOPitch + 2) * 4;
   static constexpr int fixed_bytes(int B, int slots) {
     return Marks<D, R, FP8>::kBytes + kMergeBytes + kInfoRing * kGroups * (int)sizeof(GroupInfo) + slots * 16 + 64 + ((B + 1) * 4 > R * 8 ? (B + 1) * 4 : R * 8) + 64;
@@ -117,7 +123,7 @@ __device__ __noinline__ void mark_tile(const CacheFwdParams& p, const Marks<D, 8
 // CLUSTER: an item (it has one row tile) belongs to a cluster of CTAs, each takes an equal run of its key tiles, and the CTAs' results
 // are added up through distributed shared memory.  Otherwise the line, see cache_line.cuh; cluster_of has the rule.
 template <int D, bool FP8, int NT, bool CLUSTER>
-__global__ void __launch_bounds__(kDecodeThreads, DecodeShape<D, FP8, NT>::kPerSM)
+__global__ void __launch_bounds__(kDecodeThreads, kDecodePerSM)
 cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                     const __grid_constant__ CacheFwdParams p) {
   using S = DecodeShape<D, FP8, NT>;
@@ -696,18 +702,28 @@ struct Plan {
   int R, workers;
   size_t borders, ml, o;       // bytes of the workspace's parts behind the header
 };
-Plan plan_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
+int plan_rows(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
   const long long rows = (long long)(H / c.H) * b.max_new;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 128 ? 128 : 256;
+}
+Plan plan_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
   Plan p;
-  p.R = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 128 ? 128 : 256;
-  const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;
-  p.workers = current_sm_count() * (p.R >= 128 ? 1 : decode_ctas_per_sm(c.d, fp8, p.R));
+  p.R = plan_rows(c, b, H);
+  p.workers = current_sm_count() * (p.R >= 128 ? 1 : kDecodePerSM);
   p.borders = align256((size_t)p.workers * sizeof(Border));
   p.ml = align256((size_t)2 * p.workers * p.R * 8);
   p.o = (size_t)2 * p.workers * p.R * c.d * 4;
   return p;
 }
 }  // namespace
+
+// The kernels count key tiles of all items in 32 bits.  What the struct allows at most, whatever the lengths are: a sixteenth of this for
+// 32,000 tokens of 64 query heads, eight key heads and a million keys.
+bool cache_work_fits(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
+  const int R = plan_rows(c, b, H);
+  const double items = ((double)b.T * (H / c.H) / R + b.B) * c.H, tiles = (double)b.max_pages * c.page / 64 + 1;
+  return items * (tiles + std::max(kDecodeOver, 6)) < 2147418112.0;
+}
 
 size_t cache_fwd_workspace_bytes(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H) {
   const Plan p = plan_of(c, b, H);
@@ -725,12 +741,11 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   if ((rc = make_page_map(&mk, k_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
   if ((rc = make_page_map(&mv, v_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
   const long long items = (long long)b.B * c.H;
-  p.cluster = cluster_of(c, b, p.causal.frame, p.causal.window, S::kTileKeys, p.workers / S::kPerSM);
+  p.cluster = cluster_of(c, b, p.causal.frame, p.causal.window, S::kTileKeys, p.workers / kDecodePerSM);
   const bool cluster = p.cluster > 0;
-  // as deep a ring as the CTAs of an SM leave each other; fewer CTAs where a great many sequences leave no room for two tiles
-  // (the CTAs of an SM differ by a ring's depth at most: one alone on its SM could not be kept busier by more than twelve tiles)
+  // as deep a ring as the CTAs of an SM leave each other, sixteen tiles at most; fewer CTAs where a great many sequences leave no room
   const int listed = cluster ? 0 : b.B;
-  for (int per = S::kPerSM; per > 0; --per) {
+  for (int per = kDecodePerSM; per > 0; --per) {
     p.slots = (227 * 1024 / per - 1024 - S::fixed_bytes(listed, 16)) / S::kTileBytes;
     if (p.slots >= 3) break;
   }

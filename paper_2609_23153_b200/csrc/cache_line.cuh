@@ -3,7 +3,8 @@
 // An item is R query rows (row = token * G + head in its group) of one (sequence, key head); its tiles of TK keys run from
 // the first to the last key that any of its rows sees, at least one, so that somebody writes the rows of an empty sequence.
 // Every item stands for OVER units more than it has tiles, in front of them: what it takes to begin and to finish one, without which the
-// stretches with many short items would take longest (prompts of four different lengths: FIGURE).
+// stretches with many short items would take longest (a piece of 2048 tokens of each of four prompts of up to 8000, 32 heads over 8: 540 us
+// with six, 660 without; 64 sequences of up to 8191 keys, one token each, 8 heads: 96 us with four, 107 without).
 // Stretch w is units [w * share, (w + 1) * share).  What a stretch holds of an item is a segment; an item that lies in one
 // stretch is finished there, the others leave partial results that combine_kernel adds up in the line's order.
 // Items stand in the order (sequence, key head, row tile).

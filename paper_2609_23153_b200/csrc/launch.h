@@ -112,6 +112,7 @@ constexpr int kCacheMaxSequences = 4096;   // their lengths are laid out in shar
 int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rotary_t* rotary, const sparkattn_rows_t* q,
                         int H, const sparkattn_rows_t& k, const sparkattn_rows_t& v, void* k_cache, void* v_cache, float* k_scale,
                         float* v_scale, const sparkattn_rows_t* q_out, void* workspace, cudaStream_t stream);
+bool cache_work_fits(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);
 size_t cache_fwd_workspace_bytes(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);
 int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rows_t& q, int H, const void* k_cache,
                      const void* v_cache, const float* k_scale, const float* v_scale, int frame_tokens, int window, float softmax_scale,

@@ -595,3 +595,14 @@ def test_append_then_attend_is_attention():
         rms = (got - want).square().mean().sqrt() / want.square().mean().sqrt()
         print(fp8, float(rms))
         assert rms <= bar
+
+
+@pytest.mark.parametrize("kw", [dict(grid=(6, 11), heads=4, kv_heads=2), dict(grid=(9, 20), heads=2, kv_heads=2, fp8=False, page=128),
+                                dict(grid=(1, 1), frames=70, heads=8, kv_heads=1, page=16, d=64)], ids=["frames", "bf16", "tokens"])
+def test_example(kw):
+    """The example's steps of streams of different ages, one of which pauses; its bound is this file's."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    from examples import generate_frames
+    assert generate_frames.run(**dict(dict(streams=3, frames=5, device=DEV), **kw)) <= OUT_RELRMS
