@@ -22,8 +22,8 @@
 // three frames, over 32,760, 12 heads, 897 GFLOP in 865 us = 1040 TFLOP/s, at 1.6 GHz under the power limit: tensor cores and special-function unit are busy 52 % of the
 // clocks each, the rest is the chain that a half goes through once a tile, S, maximum, exponentials, P V.
 // Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 545 us = 930 TFLOP/s; a causal
-// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 77 us;
-// 1.3 us a tile per SM, a chain of copy, conversion, product, softmax and product that only two tiles at a time share.
+// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 67 us;
+// 1 us a tile per SM, a chain of copy, conversion, product, softmax and product that only two tiles at a time share.
 // (A quarter of the exponentials as a polynomial of degree 4 on the FMA pipe, to spare the special-function unit: 870 us
 // either way for three frames of 1560 tokens over 32,760 keys, 710 instead of 672 for four prompts.)
 #include <cuda.h>
@@ -408,75 +408,173 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const int in = at.there ? (g.row0 + r) / p.G : 0;
       at.head = at.there ? g.c.h * p.G + (g.row0 + r) - in * p.G : 0;
       at.token = g.c.seq.start + in;
-      at.seen = at.there ? visible_keys(p.causal, g.c.seq.first_pos() + in, g.c.seq.len) : make_int2(0, 0);
+      at.seen = at.there ? visible_keys(p.causal, g.c.seq.first_pos() + in, g.c.seq.len) : make_int2(0, 0x7fffffff);      // (rows that are none need no mask)
       if (g.t0 == g.t1) return;
       float back = 1.0f;
       {
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)at.token * p.q_stride_t + at.head * p.q_stride_h);
-        uint4 v[D / 8];
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) v[i] = at.there ? src[i] : make_uint4(0u, 0u, 0u, 0u);
-        unsigned char* tile = sQ + (SPLIT ? 0 : w * C::kQ);
-        auto put = [&](int i, uint4 x) {                     // 16-byte chunk i of the row, in slabs of eight
-          *reinterpret_cast<uint4*>(tile + (i >> 3) * kSlab + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = x;
-        };
-        float top = 0.0f;
+        // A warp's 32 rows, D / 8 lanes a row and 16 bytes a lane, copied to where they will be operands and turned into them there.  In
+        // short loops: code that runs once an item comes from memory, and a thread's whole row unrolled took longer than what it does (five
+        // drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 72 us, unrolled 79; queries and output at one place each: 67).
+        constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
+        const uint64_t src = at.there ? reinterpret_cast<uint64_t>(p.q + (int64_t)at.token * p.q_stride_t + at.head * p.q_stride_h) : 0ull;
+        const int c = lane % kLanes, first = (row & ~31) + lane / kLanes;
+        unsigned char* tile = sQ + w * C::kQ;                // (SPLIT: the products read half 0's)
+        auto place = [&](int to, int chunk) { return tile + (chunk >> 3) * kSlab + to * 128 + (((chunk & 7) ^ (to & 7)) << 4); };
+#pragma unroll 1
+        for (int k = 0; k < 32; k += kRowsAtOnce) {
+          const uint64_t from = __shfl_sync(0xffffffffu, src, k + lane / kLanes);
+          if (from) cp_async16(smem_u32(place(first + k, c)), reinterpret_cast<const uint4*>(from) + c);
+          else *reinterpret_cast<uint4*>(place(first + k, c)) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
         if constexpr (FP8) {
+#pragma unroll 1
+          for (int k = 0; k < 32; k += kRowsAtOnce) {
+            const uint4 x = *reinterpret_cast<const uint4*>(place(first + k, c));
+            float top = largest(largest(largest(largest(0.0f, x.x), x.y), x.z), x.w);
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            for (int i = 1; i < kLanes; i <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+            const QueryScale s = query_scale(top);
+            const float its = __shfl_sync(0xffffffffu, s.back, lane % kRowsAtOnce * kLanes);
+            if (lane / kRowsAtOnce == k / kRowsAtOnce) back = its;
+            if constexpr (C::kRawK) {
+              uint32_t high[2], low[2];
+              split_queries(x.x, x.y, s.to, high[0], low[0]);
+              split_queries(x.z, x.w, s.to, high[1], low[1]);
+              unsigned char* to = place(first + k, c >> 1) + (c & 1) * 8;
+              *reinterpret_cast<uint2*>(to) = make_uint2(high[0], high[1]);
+              *reinterpret_cast<uint2*>(to + kSlab) = make_uint2(low[0], low[1]);
+            } else {
+              // fp16: the row's largest entry lies in [128, 256), what is below 2^-32 of it is rounded to fp16's subnormal numbers
+              uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = largest(top, x[j]);
-          }
-          const QueryScale s = query_scale(top);
-          back = s.back;
-          if constexpr (C::kRawK) {
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-              uint32_t high[4], low[4];
-              split_queries(v[2 * i].x, v[2 * i].y, s.to, high[0], low[0]);
-              split_queries(v[2 * i].z, v[2 * i].w, s.to, high[1], low[1]);
-              split_queries(v[2 * i + 1].x, v[2 * i + 1].y, s.to, high[2], low[2]);
-              split_queries(v[2 * i + 1].z, v[2 * i + 1].w, s.to, high[3], low[3]);
-              if (!SPLIT || w == 0) put(i, make_uint4(high[0], high[1], high[2], high[3]));
-              if (!SPLIT || w == 1) put(8 + i, make_uint4(low[0], low[1], low[2], low[3]));
-            }
-          } else {
-            // fp16: the row's largest entry lies in [128, 256), what is below 2^-32 of it is rounded to fp16's subnormal numbers
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-              uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const __half2 h = __floats2half2_rn(__uint_as_float(x[j] << 16) * s.to, __uint_as_float(x[j] & 0xffff0000u) * s.to);
-                x[j] = *reinterpret_cast<const uint32_t*>(&h);
+              for (int i = 0; i < 4; ++i) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(y[i] << 16) * s.to, __uint_as_float(y[i] & 0xffff0000u) * s.to);
+                y[i] = *reinterpret_cast<const uint32_t*>(&h);
               }
-              if (!SPLIT || (i & 1) == w) put(i, make_uint4(x[0], x[1], x[2], x[3]));
+              *reinterpret_cast<uint4*>(place(first + k, c)) = make_uint4(y[0], y[1], y[2], y[3]);
             }
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i)
-            if (!SPLIT || (i & 1) == w) put(i, v[i]);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(q_full + (SPLIT ? 0 : w));
       }
       at.c = back * p.scale_log2;
     };
-    bool live = true;
-    while (live && idle()) {
-      n += g.t1 - g.t0;
-      live = g.next(p);
-      ++segment;
-    }
-    if (live) take_queries();
-    while (live) {
-      const int tiles = g.t1 - g.t0;
+    bool live = true, begun = false;
+    int tiles = 0, took = 0;        // of the segment: tiles, and those that this warpgroup has taken
+    float m = -INFINITY, l = 0.0f;
+    struct Past {                   // a segment whose output has not been written
+      int there, token, head, slot, set;
+      bool whole;
+    } past{};
+    auto finish = [&] {
+      if (took > 0) ok = __all_sync(0xffffffffu, pipe_wait(pv_done + w, (mine - 1) & 1, s_abort, 16 + w));
+      if (!ok) return;
+      float f_own = 1.0f, f_other = 0.0f;                     // SPLIT: factors of the two halves' O
+      bool other = false;
+      if constexpr (SPLIT) {
+        if (w == 1) {
+          s_sums[row] = make_float2(m, l);
+          tc_fence_before();
+          mbar_arrive(sums_full);
+          ok = __all_sync(0xffffffffu, pipe_wait(sums_free, merges++ & 1, s_abort, 18));
+          return;
+        }
+        ok = __all_sync(0xffffffffu, pipe_wait(sums_full, merges++ & 1, s_abort, 19));
+        if (!ok) return;
+        const float2 its = s_sums[row];
+        other = tiles > 1;
+        const float to = fmaxf(m, its.x);
+        f_own = to == -INFINITY ? 1.0f : fast_exp2(m - to);
+        f_other = to == -INFINITY ? 1.0f : fast_exp2(its.x - to);
+        l = l * f_own + its.y * f_other;
+        m = to;
+      }
+      tc_fence_after();
+      const bool marked = tiles > 0 && *reinterpret_cast<volatile uint32_t*>(marks.any(past.set)) != 0u;
+      const bool empty = m == -INFINITY && l == l;            // the row sees no key
+      const float inv = empty ? 0.0f : 1.0f / l;
+#pragma unroll 1
+      for (int ch = 0; ch < D / 32; ++ch) {
+        uint32_t o[32];
+        tmem_ld32(tO + ch * 32, o);
+        tc_wait_ld();
+        if constexpr (SPLIT) {
+          if (other) {
+            uint32_t x[32];
+            tmem_ld32(tO + 128 + ch * 32, x);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(__uint_as_float(x[j]), f_other, __uint_as_float(o[j]) * f_own));
+          }
+        }
+        if (marked && past.there) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(marks.add(past.set, r, ch * 32 + j, __uint_as_float(o[j])));
+        }
+        if (past.there && past.whole) {
+          uint4* dst = reinterpret_cast<uint4*>(p.out + (int64_t)past.token * p.out_stride_t + past.head * p.out_stride_h + ch * 32);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const __nv_bfloat162 h = empty ? __floats2bfloat162_rn(0.0f, 0.0f)
+                                             : __floats2bfloat162_rn(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
+              x[k] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            dst[j] = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        } else if (past.there && tiles > 0) {
+          uint4* dst = reinterpret_cast<uint4*>(p.part_o + ((int64_t)past.slot * R + r) * D + ch * 32);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dst[j] = empty ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+        }
+      }
+      tc_fence_before();
+      if (past.there && past.whole) {
+        if (p.lse) p.lse[(int64_t)past.token * p.H + past.head] = empty ? -INFINITY : (m - kBase + log2f(l)) * 0.6931471805599453f;
+      } else if (past.there) {
+        *reinterpret_cast<float2*>(p.part_ml + ((int64_t)past.slot * R + r) * 2) = make_float2(m, empty ? 0.0f : l);
+      }
+      if (marked) {
+        // this row's marks are taken; the flag stays up for the other rows, and for whoever uses the past.set next, where it finds nothing
+#pragma unroll 1
+        for (int j = 0; j < Marks<D, R, FP8>::kSigns * Marks<D, R, FP8>::kWords; ++j) marks.row(past.set, r)[j] = 0u;
+      }
+      if constexpr (SPLIT) mbar_arrive(sums_free);
+    };
+    // (one place for the queries and one for the output, see take_queries)
+    while (true) {
+      if constexpr (SPLIT) {
+        if (begun) finish();                                 // (the two halves share the queries' place)
+        if (!ok) break;
+      }
+      if (begun) {
+        n += tiles;
+        live = g.next(p);
+        ++segment;
+      }
+      while (live && idle()) {
+        n += g.t1 - g.t0;
+        live = g.next(p);
+        ++segment;
+      }
+      // The next segment's queries go first: its first product then runs while the output is read.
+      if (live) take_queries();
+      if constexpr (!SPLIT) {
+        if (begun) finish();
+        if (!ok) break;
+      }
+      if (!live) break;
+      tiles = g.t1 - g.t0;
+      m = -INFINITY;
+      l = 0.0f;
+      took = 0;
       const float c_row = at.c;
       const int2 seen = at.seen;
-      float m = -INFINITY, l = 0.0f;
-      int took = 0;                                          // tiles of this segment
 #pragma unroll 1
       for (int i = SPLIT ? w : 0; i < tiles; i += SPLIT ? 2 : 1, ++mine, ++took) {
         ok = __all_sync(0xffffffffu, pipe_wait(s_full + w, mine & 1, s_abort, 12 + w));
@@ -596,103 +694,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         mbar_arrive(p_full + w);
       }
       if (!ok) break;
-      // ------------------------------------------------------------------------------------- the segment's end
-      // The next segment's queries go first (not where the two halves share them): its first product then runs while this output is read.
-      const bool there = at.there, whole = g.whole;
-      const int token = at.token, head = at.head, slot = 2 * ((int)blockIdx.x - 1) + (g.first ? 0 : 1);
-      const int set = segment;
-      n += tiles;
-      auto go_on = [&] {
-        live = g.next(p);
-        ++segment;
-        while (live && idle()) {
-          n += g.t1 - g.t0;
-          live = g.next(p);
-          ++segment;
-        }
-        if (live) take_queries();
-      };
-      if constexpr (!SPLIT) go_on();
-      if (took > 0) ok = __all_sync(0xffffffffu, pipe_wait(pv_done + w, (mine - 1) & 1, s_abort, 16 + w));
-      if (!ok) break;
-      float f_own = 1.0f, f_other = 0.0f;                     // SPLIT: factors of the two halves' O
-      bool other = false;
-      if constexpr (SPLIT) {
-        if (w == 1) {
-          s_sums[row] = make_float2(m, l);
-          tc_fence_before();
-          mbar_arrive(sums_full);
-          ok = __all_sync(0xffffffffu, pipe_wait(sums_free, merges++ & 1, s_abort, 18));
-          if (!ok) break;
-          go_on();
-          continue;
-        }
-        ok = __all_sync(0xffffffffu, pipe_wait(sums_full, merges++ & 1, s_abort, 19));
-        if (!ok) break;
-        const float2 its = s_sums[row];
-        other = tiles > 1;
-        const float to = fmaxf(m, its.x);
-        f_own = to == -INFINITY ? 1.0f : fast_exp2(m - to);
-        f_other = to == -INFINITY ? 1.0f : fast_exp2(its.x - to);
-        l = l * f_own + its.y * f_other;
-        m = to;
-      }
-      tc_fence_after();
-      const bool marked = tiles > 0 && *reinterpret_cast<volatile uint32_t*>(marks.any(set)) != 0u;
-      const bool empty = m == -INFINITY && l == l;            // the row sees no key
-      const float inv = empty ? 0.0f : 1.0f / l;
-#pragma unroll 1
-      for (int ch = 0; ch < D / 32; ++ch) {
-        uint32_t o[32];
-        tmem_ld32(tO + ch * 32, o);
-        tc_wait_ld();
-        if constexpr (SPLIT) {
-          if (other) {
-            uint32_t x[32];
-            tmem_ld32(tO + 128 + ch * 32, x);
-            tc_wait_ld();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(__uint_as_float(x[j]), f_other, __uint_as_float(o[j]) * f_own));
-          }
-        }
-        if (marked && there) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(marks.add(set, r, ch * 32 + j, __uint_as_float(o[j])));
-        }
-        if (there && whole) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + ch * 32);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const __nv_bfloat162 h = empty ? __floats2bfloat162_rn(0.0f, 0.0f)
-                                             : __floats2bfloat162_rn(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
-              x[k] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            dst[j] = make_uint4(x[0], x[1], x[2], x[3]);
-          }
-        } else if (there && tiles > 0) {
-          uint4* dst = reinterpret_cast<uint4*>(p.part_o + ((int64_t)slot * R + r) * D + ch * 32);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) dst[j] = empty ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-        }
-      }
-      tc_fence_before();
-      if (there && whole) {
-        if (p.lse) p.lse[(int64_t)token * p.H + head] = empty ? -INFINITY : (m - kBase + log2f(l)) * 0.6931471805599453f;
-      } else if (there) {
-        *reinterpret_cast<float2*>(p.part_ml + ((int64_t)slot * R + r) * 2) = make_float2(m, empty ? 0.0f : l);
-      }
-      if (marked) {
-        // this row's marks are taken; the flag stays up for the other rows, and for whoever uses the set next, where it finds nothing
-#pragma unroll 1
-        for (int j = 0; j < Marks<D, R, FP8>::kSigns * Marks<D, R, FP8>::kWords; ++j) marks.row(set, r)[j] = 0u;
-      }
-      if constexpr (SPLIT) {
-        mbar_arrive(sums_free);
-        go_on();
-      }
+      past = {at.there, at.token, at.head, 2 * ((int)blockIdx.x - 1) + (g.first ? 0 : 1), segment, g.whole};
+      begun = true;
     }
   }
   // -------------------------------------------------------------------------------------------------------- teardown
