@@ -477,7 +477,7 @@ size_t sparkattn_cache_workspace_bytes(const sparkattn_cache_t* cache, const spa
  *     unless the page's first token is among the new ones.  Where it grows, the codes of the tokens already there are
  *     encoded again (code * (old * (1/s))), which a power of two leaves exact but for values that fall below 2^-6 s, so
  *     that a page hardly depends on the steps in which it was filled.  New codes: e4m3_rne_satfinite(x * (1/s)).
- *     Infinities become +-448 s, NaN stays NaN.
+ *     Infinities become the largest code, +-448 of the scale at that time, NaN stays NaN.
  * q, q_out : bf16 rows [T, H, d] and where they go rotated (may be the same memory), or both NULL (H is ignored)
  * k, v     : bf16 rows [T, cache->H, d]
  * rotary   : NULL: nothing is rotated
@@ -504,8 +504,13 @@ int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch
  * softmax_scale: 0 selects 1/sqrt(d)
  * lse          : fp32 [T, H] contiguous (natural log), or NULL
  * workspace    : >= sparkattn_cache_workspace_bytes(cache, batch, H), 256-byte aligned; first word = device status
- * Scores, maxima, sums and the output's accumulation are fp32; the weights are rounded for the second product, to bf16 or (E4M3 pages, few
- * rows) to fp16.  The same inputs give the same bits.
+ * A key or value that is not finite reaches the rows that see its key, and no others.
+ * Scores, maxima, sums and the output's accumulation are fp32.  The weights of the second product are rounded to fp16 over
+ * E4M3 pages; over bf16 pages to two bf16 parts (16 digits together) for up to 16 rows per key head (H / cache->H * max_new), to
+ * one for more.  Queries over E4M3 pages are used as bf16 holds them, but for entries below 2^-9 of their row's largest, which
+ * are off by 2^-18 of that at most (d = 128; d = 64: fp16 scaled by the row's largest, for more than 16 rows); a query row with
+ * an infinity or a NaN in it gives NaN.  The same inputs give the same bits.
+ * A batch whose structs allow more than 2^31 key tiles of 64 in all is SPARKATTN_E_UNSUPPORTED_SHAPE.
  */
 int sparkattn_cache_fwd(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rows_t* q, int32_t H,
                         const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
