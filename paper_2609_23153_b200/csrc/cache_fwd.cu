@@ -91,8 +91,9 @@ struct DecodeShape {
   static constexpr int kElt = FP8 ? 1 : 2;
   static constexpr int kRowBytes = D * kElt;
   // groups of 16 keys that a warp takes of a tile: two where a K or V tile stays within 16 KB, so that their chains of dependent
-  // steps run side by side and the steps that a tile needs once are spread over 32 keys
-  static constexpr int kPerWarp = kRowBytes <= 128 ? 2 : 1;
+  // steps run side by side and the steps that a tile needs once are spread over 32 keys, and where the registers hold it (16 rows of 128
+  // channels: 16 sequences of 8000 keys, 64 heads over 4, 42.8 us by one group a warp, 46.2 by two; of 64 channels 28.1 and 23.5)
+  static constexpr int kPerWarp = kRowBytes <= 128 && D * NT <= 128 ? 2 : 1;
   static constexpr int kGroups = kComputeWarps * kPerWarp, kTileKeys = kGroups * kGroupKeys;
   static constexpr int kTileBytes = kTileKeys * kRowBytes;       // of K or of V
   static constexpr int kOPitch = D + 4;
@@ -684,7 +685,11 @@ constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 //   26.6 us, by one CTA 32.4, the line 33.6; all of one length 49.4, 41.3, 42.6).
 //   The line takes over where clusters leave SMs idle for long (32,000 keys: 21.4 us, clusters of 16 24.0) and where the
 //   items are more than a wave and long, whose lengths may differ (64 sequences of up to 8191 keys, 8 heads: 105 us, clusters of
-//   1 / 2 121 / 107; all of one length 179 and 169 / 184; of 2000 keys 55 and 50).
+//   1 / 2 121 / 107; all of one length 179 and 169 / 184; of 2000 keys 55 and 50).  So it does between, from 2304 keys a CTA on: lengths up to
+//   the stated one, in parentheses all of it, line / cluster of two, E4M3: 10 sequences of 8 heads, 4000 keys 19.0 / 20.0 us (21.8 / 23.8), 16,000
+//   42.7 / 63.6 (63.2 / 76.3); 16 of 8, 4000 21.8 / 20.3 (34.7 / 27.5), 16,000 54.2 / 65.2 (91.8 / 83.0); 16 of 12, 8000 43.7 / 46.2 (71.4 / 87.2); cluster
+//   of four: 5 of 8, 16,000 26.7 / 35.5 (37.7 / 42.9).  bf16: 16 of 8, 4000 33.1 / 31.3 (51.3 / 44.5); 8 of 12, 16,000 74.2 / 96.3 (127 / 118); 32 of 8, 8000
+//   92.5 / 100 (168 / 152).
 int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame_tokens, int window, int tile_keys, int sms) {
   const long long items = (long long)b.B * c.H;
   long long keys = (long long)b.max_pages * c.page;                       // that an item may have
@@ -693,7 +698,7 @@ int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame
   int n = items * 16 <= sms ? 16 : 8;
   while (n > 1 && (items * n > std::max(2 * sms, 16) || n / 2 >= tiles)) n /= 2;
   if (n == 1 && items <= 2 * sms && tiles >= 16) n = 2;
-  if (items > 2 * sms ? tiles >= 32 : items * n < sms && tiles > 12 * n) return 0;
+  if (items > 2 * sms ? tiles >= 32 : items * n < sms ? tiles > 12 * n : keys > 2304LL * n) return 0;
   return n;
 }
 
