@@ -50,11 +50,12 @@ __device__ __forceinline__ Sequence sequence_of(const BatchView& v, int b) {
 // [lo, hi) of the keys that the token at position pos of a sequence of len tokens sees
 struct Causal {
   int frame, window;      // frame 0: every key; window 0: from the first key on
+  FastDiv by_frame;
 };
 __device__ __forceinline__ int2 visible_keys(const Causal& c, int pos, int len) {
   if (c.frame == 0) return make_int2(0, len);
   if (pos < 0) return make_int2(0, 0);
-  const int f = pos / c.frame;
+  const int f = fast_div(pos, c.by_frame);
   const long long hi = ((long long)f + 1) * c.frame;
   const long long lo = c.window == 0 ? 0 : max((long long)(f - c.window + 1) * c.frame, 0LL);
   return make_int2((int)min(lo, (long long)len), (int)min(hi, (long long)len));

@@ -19,10 +19,10 @@
 // (split_queries): twice as many products at twice the rate.  P and V are fp16 (the weights 2^5 at the reference), and V's scale is part of the
 // exponent: t = logit + log2(v_scale), the row sum adds weight / v_scale.  bf16 pages: bf16 throughout.
 // Measured (E4M3, 128 channels; a library product of bf16 matrices reaches 1704 TFLOP/s in a burst, 1439 for seconds): 4680 new tokens,
-// three frames, over 32,760, 12 heads, 897 GFLOP in 865 us = 1040 TFLOP/s, at 1.6 GHz under the power limit: tensor cores and special-function unit are busy 52 % of the
+// three frames, over 32,760, 12 heads, 897 GFLOP in 860 us = 1040 TFLOP/s, at 1.6 GHz under the power limit: tensor cores and special-function unit are busy 52 % of the
 // clocks each, the rest is the chain that a half goes through once a tile, S, maximum, exponentials, P V.
-// Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 545 us = 930 TFLOP/s; a causal
-// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 67 us;
+// Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 560 us = 910 TFLOP/s; a causal
+// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 64 us;
 // 1 us a tile per SM, a chain of copy, conversion, product, softmax and product that only two tiles at a time share.
 // (A quarter of the exponentials as a polynomial of degree 4 on the FMA pipe, to spare the special-function unit: 870 us
 // either way for three frames of 1560 tokens over 32,760 keys, 710 instead of 672 for four prompts.)
@@ -330,8 +330,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     };
     do {
       // keys that every row of the item sees
-      const int all_lo = visible_keys(p.causal, g.c.seq.first_pos() + (g.row0 + g.rows - 1) / p.G, g.c.seq.len).x;
-      const int all_hi = visible_keys(p.causal, g.c.seq.first_pos() + g.row0 / p.G, g.c.seq.len).y;
+      const int all_lo = visible_keys(p.causal, g.c.seq.first_pos() + fast_div(g.row0 + g.rows - 1, p.by_G), g.c.seq.len).x;
+      const int all_hi = visible_keys(p.causal, g.c.seq.first_pos() + fast_div(g.row0, p.by_G), g.c.seq.len).y;
       const bool parts = all_lo > g.c.item.lo || all_hi < g.c.item.hi;
       for (int t = g.t0; ok && t < g.t1; ++t, ++n) {
         const int key0 = t * kChunkKeys;
@@ -405,7 +405,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // The segment's queries as operand rows.  The S products of the segment before have read this place: their S has been read.
     auto take_queries = [&] {
       at.there = r < g.rows;
-      const int in = at.there ? (g.row0 + r) / p.G : 0;
+      const int in = at.there ? fast_div(g.row0 + r, p.by_G) : 0;
       at.head = at.there ? g.c.h * p.G + (g.row0 + r) - in * p.G : 0;
       at.token = g.c.seq.start + in;
       at.seen = at.there ? visible_keys(p.causal, g.c.seq.first_pos() + in, g.c.seq.len) : make_int2(0, 0x7fffffff);      // (rows that are none need no mask)

@@ -26,8 +26,8 @@
 // Measured (one new token per sequence; bytes of keys, values and scales that must be read; E4M3, 128 channels and 8 key heads where nothing
 // else is said): 64 sequences of up to 8191 keys, 555 MB in 96 us = 5.8 TB/s, 0.90 of a copy's rate, which bounds it; one sequence
 // of 131,071 keys, 269 MB in 53 us = 5.0 TB/s, where the second launch and the way of the first tiles, 5 us each, have nothing to
-// hide behind; one of 1001 keys 7.3 us, of one key 4.8: latency.  16 sequences of up to 4095 keys, 12 heads, bf16: 206 MB in 42 us = 5.0 TB/s.
-// 32 sequences, a window of 1000 keys, 4 heads of 64 channels, pages of 16 keys: 16 MB in 11 us, latency again.
+// hide behind; one of 1001 keys 7.1 us, of one key 4.8: latency.  16 sequences of up to 4095 keys, 12 heads, bf16: 206 MB in 42 us = 5.0 TB/s.
+// 32 sequences, a window of 1000 keys, 4 heads of 64 channels, pages of 16 keys: 16 MB in 10.5 us, latency again.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -165,7 +165,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       if (rank == 0) check_call(p, s_bad);
       return;
     }
-    const int b = (cluster - 1) / p.Hk;
+    const int b = fast_div(cluster - 1, p.by_Hk);
     if (!g.run_of(p, b, cluster - 1 - b * p.Hk, rank, p.cluster)) return;
   } else {
   Line<R, kTileKeys, kDecodeOver>::lay_out(p, s_prefix, s_warp);
@@ -282,7 +282,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       for (int nt = 0; nt < NT; ++nt) {
         const int r = nt * 8 + g8, row = g.row0 + r;
         const bool there = r < g.rows;
-        const int token = there ? row / p.G : 0, head = there ? g.c.h * p.G + (row - token * p.G) : 0;
+        const int token = there ? fast_div(row, p.by_G) : 0, head = there ? g.c.h * p.G + (row - token * p.G) : 0;
         const __nv_bfloat16* src = p.q + (int64_t)(g.c.seq.start + token) * p.q_stride_t + head * p.q_stride_h;
         float back = 1.0f;
         if constexpr (FP8) {
@@ -611,7 +611,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
           if (ch == 0) s_cta[r] = make_float2(top, sum);
         } else if (CLUSTER || g.whole) {
-          const int row = g.row0 + r, token = g.c.seq.start + row / p.G, head = g.c.h * p.G + row % p.G;
+          const int row = g.row0 + r, of = fast_div(row, p.by_G), token = g.c.seq.start + of, head = g.c.h * p.G + row - of * p.G;
           const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
           uint32_t w[4];
 #pragma unroll
@@ -658,7 +658,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
             acc[3] = fmaf(v.w, f, acc[3] * keep);
             top = to;
           }
-          const int row = g.row0 + r, token = g.c.seq.start + row / p.G, head = g.c.h * p.G + row % p.G;
+          const int row = g.row0 + r, of = fast_div(row, p.by_G), token = g.c.seq.start + of, head = g.c.h * p.G + row - of * p.G;
           const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
           const __nv_bfloat162 a = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), b = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
           *reinterpret_cast<uint2*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + ch) =
@@ -772,7 +772,7 @@ int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, con
                      const sparkattn_rows_t& out, float* lse, void* workspace, cudaStream_t stream) {
   CacheFwdParams p{};
   p.batch = make_batch_view(c, b);
-  p.causal = {frame_tokens, window};
+  p.causal = {frame_tokens, window, make_fast_div(std::max(frame_tokens, 1))};
   p.q = static_cast<const __nv_bfloat16*>(q.data);
   p.out = static_cast<__nv_bfloat16*>(out.data);
   p.q_stride_t = q.stride_t; p.q_stride_h = q.stride_h;
@@ -780,6 +780,8 @@ int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, con
   p.k_scale = k_scale; p.v_scale = v_scale;
   p.lse = lse;
   p.H = H; p.Hk = c.H; p.G = H / c.H;
+  p.by_Hk = make_fast_div(p.Hk);
+  p.by_G = make_fast_div(p.G);
   p.scale_log2 = (softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf((float)c.d)) * 1.4426950408889634f;
   p.least = 1;
   const Plan plan = plan_of(c, b, H);

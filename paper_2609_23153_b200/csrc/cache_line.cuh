@@ -31,6 +31,7 @@ struct CacheFwdParams {
   const float* v_scale;
   float* lse;
   int H, Hk, G;
+  FastDiv by_Hk, by_G;           // (divisions took 4 us of the 67 of five drafted tokens of 8 sequences, 64 heads over 8: every role has them in code of its own)
   float scale_log2;
   int box_rows, boxes;           // keys of one TMA box, boxes of a tile
   int least;                     // units a stretch has at least
@@ -71,10 +72,10 @@ struct Line {
   };
   static __device__ __forceinline__ int row_tiles(const CacheFwdParams& p, const Sequence& s) { return (s.n * p.G + R - 1) / R; }
   static __device__ __forceinline__ Item item_of(const CacheFwdParams& p, const Sequence& s, int rt) {
-    const int last_row = min((rt + 1) * R, s.n * p.G) - 1;
+    const int last_row = max(min((rt + 1) * R, s.n * p.G) - 1, 0);
     Item it;
-    it.lo = visible_keys(p.causal, s.first_pos() + rt * R / p.G, s.len).x;
-    it.hi = visible_keys(p.causal, s.first_pos() + last_row / p.G, s.len).y;
+    it.lo = visible_keys(p.causal, s.first_pos() + fast_div(rt * R, p.by_G), s.len).x;
+    it.hi = visible_keys(p.causal, s.first_pos() + fast_div(last_row, p.by_G), s.len).y;
     it.first = it.lo / TK;
     it.tiles = max((it.hi + TK - 1) / TK - it.first, 1);
     return it;
@@ -131,7 +132,7 @@ struct Line {
     c.b = lo;
     c.seq = sequence_of(p.batch, lo);
     c.row_tiles = row_tiles(p, c.seq);
-    const int each = (prefix[lo + 1] - prefix[lo]) / p.Hk;
+    const int each = fast_div(prefix[lo + 1] - prefix[lo], p.by_Hk);
     int in = x - prefix[lo];
     c.h = in / each;
     in -= c.h * each;
@@ -344,7 +345,7 @@ __device__ __forceinline__ uint32_t mark_word(const CacheFwdParams& p, const Mar
   }
 #pragma unroll 1
   for (int r = 0; r < rows; ++r) {
-    const int2 seen = visible_keys(p.causal, seq.first_pos() + (row0 + r) / p.G, seq.len);
+    const int2 seen = visible_keys(p.causal, seq.first_pos() + fast_div(row0 + r, p.by_G), seq.len);
     if (key < seen.x || key >= seen.y) continue;
     uint32_t* to = marks.row(set, r) + channel / 32;
     if (up) atomicOr(to, up);
@@ -428,7 +429,7 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
       __syncthreads();
     }
     if (!there || share_of_row != 0) continue;
-    const int row = row0 + r, token = token0 + row / p.G, head = h * p.G + row % p.G;
+    const int row = row0 + r, of = fast_div(row, p.by_G), token = token0 + of, head = h * p.G + row - of * p.G;
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + (int64_t)token * p.out_stride_t + head * p.out_stride_h + lane * kVec);
 #pragma unroll
