@@ -375,8 +375,9 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         if constexpr (FP8) {
           convert(sRaw + slot * C::kCodes, sV + slot * C::kOperand);
-          mbar_arrive(raw_free + slot);
+          // in front of both arrivals: the codes' zeros (edge) before the next copy into their place, the operand before the product
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_arrive(raw_free + slot);
         }
         mbar_arrive(v_full + slot);
       }

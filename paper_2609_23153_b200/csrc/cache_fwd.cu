@@ -119,6 +119,7 @@ __device__ __noinline__ void mark_tile(const CacheFwdParams& p, const Marks<D, 8
     if (key >= seen.x && key < seen.y && (usable >> u & 1) && word_not_finite<FP8>(*word))
       *word = mark_word<D, S::R, FP8>(p, marks, set, seq, row0, rows, key, channel, *word);
   }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the tile is released to the next copy
 }
 
 // CLUSTER: an item (it has one row tile) belongs to a cluster of CTAs, each takes an equal run of its key tiles, and the CTAs' results

@@ -3,6 +3,7 @@ serve is refused before anything is enqueued."""
 import ctypes
 import math
 import os
+import re
 
 import pytest
 import torch
@@ -173,3 +174,16 @@ def test_alloc_cache(page, d, fp8):
     assert c.k.shape == c.v.shape == (3, 2, page, d) and c.k.data_ptr() != c.v.data_ptr()
     assert c.k.dtype == (torch.float8_e4m3fn if fp8 else torch.bfloat16)
     assert (c.k_scale is not None and c.k_scale.shape == (3, 2) and c.k_scale.dtype == torch.float32) if fp8 else c.k_scale is None
+
+
+def test_what_threads_write_into_a_tile_is_fenced_before_the_next_copy():
+    """The operand warps put zeros among V's codes, and both kernels marks' zeros among values: ordinary stores where TMA writes next.  Between them and the
+    arrival that frees the place stands the fence that orders the two."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    chunk, decode = (re.sub(r"//[^\n]*", "", open(os.path.join(root, "paper_2609_23153_b200", "csrc", f)).read()) for f in ("cache_chunk.cu", "cache_fwd.cu"))
+    codes = chunk[chunk.index("convert(sRaw + slot"):]
+    assert codes.index("fence.proxy.async") < codes.index("mbar_arrive(raw_free") < codes.index("mbar_arrive(v_full")
+    edge = chunk[chunk.index("*chunk = make_uint4"):chunk.index("convert(sRaw + slot")]
+    assert re.search(r"if constexpr \(!FP8\) asm volatile\(.fence\.proxy\.async", edge)
+    mark = decode[decode.index("mark_tile("):decode.index("cache_decode_kernel(")]
+    assert mark.index("mark_word<") < mark.index("fence.proxy.async")

@@ -606,3 +606,40 @@ def test_example(kw):
     sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     from examples import generate_frames
     assert generate_frames.run(**dict(dict(streams=3, frames=5, device=DEV), **kw)) <= OUT_RELRMS
+
+
+# ------------------------------------------------------------------------------------- memory that threads and copies share
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("d,page,H,n", [(128, 64, 2, 20), (64, 16, 4, 9), (128, 32, 2, 4), (64, 128, 8, 2)])
+def test_tiles_that_threads_write_between_copies(fp8, d, page, H, n):
+    """Many items, nearly all of which end inside a tile and hold values that are not finite: their zeros and marks are written where the
+    next item's copies go.  Every call gives the same bits, and 64-bit attention's values where nothing is broken."""
+    gen = torch.Generator(device=DEV).manual_seed(d + n)
+    B, Hk = 150, 2
+    lens = [n + (b * 37) % 290 for b in range(B)]
+    pages = sum(-(-x // page) for x in lens) + 1
+    cache = make_cache(gen, pages, Hk, page, d, fp8)
+    table = make_table(gen, lens, page, pages, spare=4200 // page)      # (as wide as makes a line of all items, several to a CTA)
+    kv_len, q_start = batch_of(lens, [n] * B)
+    q = torch.randn((B * n, H, d), generator=gen, device=DEV).bfloat16()
+    kw = dict(q_start=q_start, max_new=n, return_lse=True)
+    want, want_lse = reference(q[:12 * n], cache, table, lens[:12], [n] * 12, 1, 0)
+    clean = sa.cache_fwd(q, cache, table, kv_len, **kw)
+    check(clean[0][:12 * n], clean[1][:12 * n], want, want_lse)
+    # the newest token's value is broken: the row that sees it has NaN in that channel, all others have what they had
+    v = cache.v.clone(memory_format=torch.preserve_format)
+    for b in range(B):
+        at = (int(table[b, (lens[b] - 1) // page]), 0, (lens[b] - 1) % page, b % d)
+        if fp8:
+            v.view(torch.uint8)[at] = 0x7f
+        else:
+            v[at] = math.nan
+    expected = clean[0].clone()
+    for b in range(B):
+        expected[(b + 1) * n - 1, :H // Hk, b % d] = math.nan
+    broken = poisoned(cache._replace(v=v), table, lens, page)
+    for _ in range(20):
+        out, lse = sa.cache_fwd(q, broken, table, kv_len, **kw)
+        assert torch.equal(torch.isnan(out), torch.isnan(expected)) and same_bits(lse, clean[1])
+        assert same_bits(torch.nan_to_num(out), torch.nan_to_num(expected))
