@@ -57,6 +57,14 @@ struct ChunkShape {
   static constexpr int kFixed = kOffMisc + 256 /* barriers */ + kChunkInfoRing * kChunkGroups * (int)sizeof(GroupInfo) + 128 + 128 * 8 /* SPLIT: row sums */;
 };
 
+// What the logits of a row and 16 keys are multiplied by, kept from 0: a row of zeros has 2^-126 here and a page of zeros 2^-48, whose product
+// underflows, and a masked logit, -inf, times 0 would be NaN.  Logits that this changes are below 2^-100.  A NaN, of a broken row, stays.
+__device__ __forceinline__ float logit_factor(float row, float key) {
+  float c = row * key;
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(c) : "f"(1.17549435e-38f));
+  return c;
+}
+
 template <int D, bool FP8, bool SPLIT>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
@@ -615,7 +623,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               a = fmax3(a, __uint_as_float(sr[16 * q + j]), __uint_as_float(sr[16 * q + j + 1]));
               b = fmax3(b, __uint_as_float(sr[16 * q + j + 2]), __uint_as_float(sr[16 * q + j + 3]));
             }
-            top = fmaxf(top, fmaf(fmaxf(a, b), c_row * info[q].k, info[q].v_log2));
+            top = fmaxf(top, fmaf(fmaxf(a, b), logit_factor(c_row, info[q].k), info[q].v_log2));
           }
         } else {
           float mx[4];
@@ -663,7 +671,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             float c = c_row, off = ref, inv = 1.0f;
             if constexpr (FP8) {
               const GroupInfo gi = info[2 * ch + q];
-              c *= gi.k;
+              c = logit_factor(c, gi.k);
               off += gi.v_log2;
               inv = gi.v_inv;
             }

@@ -643,3 +643,46 @@ def test_tiles_that_threads_write_between_copies(fp8, d, page, H, n):
         out, lse = sa.cache_fwd(q, broken, table, kv_len, **kw)
         assert torch.equal(torch.isnan(out), torch.isnan(expected)) and same_bits(lse, clean[1])
         assert same_bits(torch.nan_to_num(out), torch.nan_to_num(expected))
+
+
+# ------------------------------------------------------------------------------------------------- zeros, and what underflows
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 4, 8, 9, 70, 300])
+@pytest.mark.parametrize("size", [0.0, 1e-5, 1e-30])
+def test_rows_and_keys_of_zeros(d, n, size):
+    """Queries of zeros (padding, a first step with zeroed projections) over keys of zeros, or tiny ones: every key that a row sees weighs the same,
+    on both sides of the 16 rows per key head that take one kernel or the other."""
+    gen = torch.Generator(device=DEV).manual_seed(n + d)
+    Hk, G, page = 2, 2, 32
+    lens, news = [n + 150, n], [n, n]
+    k = (size * torch.randn((sum(lens), Hk, d), generator=gen, device=DEV)).bfloat16()
+    v = torch.randn((sum(lens), Hk, d), generator=gen, device=DEV).bfloat16()
+    for fp8 in (True, False):
+        cache = sa.alloc_cache(40, Hk, page, d, fp8=fp8)
+        table = make_table(gen, lens, page, 40)
+        kv_len, start = batch_of(lens, lens)
+        sa.cache_append(cache, k, v, table, kv_len, q_start=start, max_new=max(lens), check_status=True)
+        q = torch.zeros((2 * n, Hk * G, d), dtype=torch.bfloat16, device=DEV)
+        q[::3, 1] = torch.randn((len(q[::3]), d), generator=gen, device=DEV).bfloat16()      # some rows are not zeros
+        _, start = batch_of(lens, news)
+        for frame, window in ((1, 0), (1, 40), (7, 0), (0, 0)):
+            out, lse = sa.cache_fwd(q, cache, table, kv_len, q_start=start, max_new=n, frame_tokens=frame, window=window, return_lse=True, check_status=True)
+            want, want_lse = reference(q, cache, table, lens, news, frame, window)
+            check(out, lse, want, want_lse)
+
+
+@pytest.mark.parametrize("n", [2, 40])
+def test_a_tiny_softmax_scale_is_a_mean(n):
+    """A scale that all but vanishes, with masks: the mean of what a row sees."""
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    for fp8 in (True, False):
+        cache = make_cache(gen, 12, 2, 32, 128, fp8)
+        lens, news = [200, 90], [n, n]
+        table = make_table(gen, lens, 32, 12)
+        kv_len, q_start = batch_of(lens, news)
+        q = torch.randn((2 * n, 4, 128), generator=gen, device=DEV).bfloat16()
+        for scale in (1e-30, 1e-44):
+            out, lse = sa.cache_fwd(q, cache, table, kv_len, q_start=q_start, max_new=n, softmax_scale=scale, return_lse=True)
+            want, want_lse = reference(q, cache, table, lens, news, 1, 0, scale)
+            check(out, lse, want, want_lse)
