@@ -46,6 +46,7 @@ constexpr int kInfoRing = 32;      // tiles whose groups' notes are kept: a batc
 // CTAs per SM: two, so that one's items begin and end while the other's copies run (64 sequences of up to 8191 keys, 8 key heads, E4M3:
 // 96 us, by one 110, by three 98; one sequence of 1001 keys 7.3, 12.5, 7.3; 64 of 1000 keys 31.9, 44.0, 37.4).
 constexpr int kDecodePerSM = 2;
+constexpr int kSmemOfSM = 227 * 1024;      // that CTAs can have, 1 KB of each taken by the system
 constexpr int kComputeWarps = 4, kDecodeThreads = 32 * (kComputeWarps + 1);
 
 // ---------------------------------------------------------------------------------------------------------- fragments
@@ -752,14 +753,15 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   // as deep a ring as the CTAs of an SM leave each other, sixteen tiles at most; fewer CTAs where a great many sequences leave no room
   const int listed = cluster ? 0 : b.B;
   for (int per = kDecodePerSM; per > 0; --per) {
-    p.slots = (227 * 1024 / per - 1024 - S::fixed_bytes(listed, 16)) / S::kTileBytes;
+    p.slots = (kSmemOfSM / per - 1024 - S::fixed_bytes(listed, 16)) / S::kTileBytes;
     if (p.slots >= 3) break;
   }
   if (p.slots > 16) p.slots = 16;
   if (p.slots < 3) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   const int smem = p.slots * S::kTileBytes + S::fixed_bytes(listed, p.slots);
   auto kern = cluster ? cache_decode_kernel<D, FP8, NT, true> : cache_decode_kernel<D, FP8, NT, false>;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
+  // (the kernel's, not the call's: the most that any call asks for, since host threads with other batches set it too)
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemOfSM - 1024) != cudaSuccess) return SPARKATTN_E_CUDA;
   if (cluster) {
     if (p.cluster > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SPARKATTN_E_CUDA;
     return launch_clustered(kern, dim3((unsigned)((items + 1) * p.cluster)), kDecodeThreads, smem, true, p.cluster, stream, mk, mv, p);

@@ -686,3 +686,42 @@ def test_a_tiny_softmax_scale_is_a_mean(n):
             out, lse = sa.cache_fwd(q, cache, table, kv_len, q_start=q_start, max_new=n, softmax_scale=scale, return_lse=True)
             want, want_lse = reference(q, cache, table, lens, news, 1, 0, scale)
             check(out, lse, want, want_lse)
+
+
+def test_host_threads_with_batches_of_different_sizes():
+    """Two host threads, each with a stream of its own, call the same kernel for 64 and for 1024 sequences: no call is refused, and each gives the
+    bits that it gives alone."""
+    import threading
+    gen = torch.Generator(device=DEV).manual_seed(15)
+    Hk, page, d, columns = 8, 64, 128, 80
+    calls = []
+    for B in (64, 1024):
+        lens = [1 + i % 60 for i in range(B)]
+        cache = make_cache(gen, B + 1, Hk, page, d, True)
+        table = torch.zeros((B, columns), dtype=torch.int32, device=DEV)
+        table[:, 0] = torch.randperm(B, generator=gen, device=DEV).int()
+        kv_len, _ = batch_of(lens, [1] * B)
+        q = torch.randn((B, 2 * Hk, d), generator=gen, device=DEV).bfloat16()
+        want = sa.cache_fwd(q, cache, table, kv_len, check_status=True)
+        calls.append((q, cache, table, kv_len, torch.empty_like(want), want, torch.empty(1 << 26, dtype=torch.uint8, device=DEV), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(q, cache, table, kv_len, out, want, ws, stream):
+        try:
+            stream.synchronize()                                # (the thread's context is there)
+            for i in range(3000):
+                sa.cache_fwd(q, cache, table, kv_len, out=out, workspace=ws, stream=stream)
+                if i % 100 == 99:
+                    stream.synchronize()
+        except Exception as e:      # (a refusal must not stay in its thread)
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=c) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for c in calls:
+        assert same_bits(c[4], c[5])
