@@ -725,3 +725,38 @@ def test_host_threads_with_batches_of_different_sizes():
     assert not errors
     for c in calls:
         assert same_bits(c[4], c[5])
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_host_threads_first_call(n):
+    """A host thread whose first use of the GPU is one of these calls, with nothing left to allocate, is served as any other."""
+    import threading
+    gen = torch.Generator(device=DEV).manual_seed(19)
+    cache = make_cache(gen, 12, 2, 64, 128, True)
+    table = make_table(gen, [700], 64, 12)
+    kv_len = torch.tensor([700], dtype=torch.int32, device=DEV)
+    q, k = (torch.randn((n, h, 128), generator=gen, device=DEV).bfloat16() for h in (4, 2))
+    want = sa.cache_fwd(q, cache, table, kv_len)
+    out, ws, stream = torch.zeros_like(want), torch.empty(1 << 26, dtype=torch.uint8, device=DEV), torch.cuda.current_stream()
+    dense = [torch.randn((1, 2, 512, 128), generator=gen, device=DEV).bfloat16() for _ in range(3)]
+    kept, count = sa.select(*dense[:2], 128, 2)
+    dense_want = sa.fwd(*dense, kept, count, 128)
+    dense_out = torch.zeros_like(dense_want)
+    torch.cuda.synchronize()
+    calls = {"cache_fwd": lambda: sa.cache_fwd(q, cache, table, kv_len, out=out, workspace=ws, stream=stream),
+             "fwd": lambda: sa.fwd(*dense, kept, count, 128, out=dense_out, workspace=ws, stream=stream),
+             "cache_append": lambda: sa.cache_append(cache, k, k, table, kv_len, workspace=ws, stream=stream)}
+    errors = []
+
+    def work(name):
+        try:
+            calls[name]()
+        except Exception as e:
+            errors.append((name, e))
+    for name in calls:
+        thread = threading.Thread(target=work, args=(name,))
+        thread.start()
+        thread.join()
+    torch.cuda.synchronize()
+    assert not errors
+    assert same_bits(out, want) and same_bits(dense_out, dense_want)
