@@ -411,7 +411,7 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
         if constexpr (kVec == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
         else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) acc[j] = f == 0.0f ? acc[j] : fmaf(v[j], f, acc[j]);      // (a part without keys has left no output)
+        for (int j = 0; j < kVec; ++j) acc[j] = ml.x == -INFINITY ? acc[j] : fmaf(v[j], f, acc[j]);      // (a part without keys has left no output)
       }
     }
     if (split > 1) {

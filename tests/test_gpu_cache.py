@@ -760,3 +760,35 @@ def test_a_host_threads_first_call(n):
     torch.cuda.synchronize()
     assert not errors
     assert same_bits(out, want) and same_bits(dense_out, dense_want)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("length,n", [(3000, 1), (40000, 1), (40000, 2), (40000, 30), (40000, 150)])
+def test_broken_values_of_keys_far_below(fp8, length, n):
+    """A value that is not finite, of a key whose logit lies 226 below the row's largest (its weight underflows), reaches every row that sees it, however
+    the keys were dealt out: to one thread-block cluster, or to stretches of the line that hold nothing but such keys."""
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    page, d, G = 64, 128, 2
+    cache = make_cache(gen, -(-length // page), 1, page, d, False)
+    cache.k[:] = -10.0
+    first = length // 3
+    table = torch.arange(-(-length // page), dtype=torch.int32, device=DEV)[None].contiguous()
+    cache.k[:first // page] = 10.0
+    if fp8:
+        cache = sa.KVCache(*(x.to(torch.float8_e4m3fn) for x in cache[:2]), *(torch.ones((cache.k.shape[0], 1), device=DEV) for _ in range(2)))
+    q = torch.ones((n, G, d), dtype=torch.bfloat16, device=DEV)
+    kv_len = torch.tensor([length], dtype=torch.int32, device=DEV)
+    kw = dict(max_new=n, frame_tokens=0, return_lse=True)
+    clean, clean_lse = sa.cache_fwd(q, cache, table, kv_len, **kw)
+    assert torch.isfinite(clean).all()
+    v = cache.v.clone()
+    for key, c in ((first + 100, 5), (length // 2, 77), (length - 1, 8)):
+        if fp8:
+            v.view(torch.uint8)[key // page, 0, key % page, c] = 0x7f
+        else:
+            v[key // page, 0, key % page, c] = math.nan if c != 77 else math.inf
+    out, lse = sa.cache_fwd(q, cache._replace(v=v), table, kv_len, **kw)
+    broken = torch.zeros(d, dtype=torch.bool, device=DEV)
+    broken[[5, 77, 8]] = True
+    assert (~torch.isfinite(out[..., broken])).all()
+    assert same_bits(out[..., ~broken], clean[..., ~broken]) and same_bits(lse, clean_lse)
