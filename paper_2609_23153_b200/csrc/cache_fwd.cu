@@ -478,13 +478,14 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
               pf[u][nt][0] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&a));
               pf[u][nt][1] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&b));
             } else {
-              // (the first cut off, so that the second is positive, and at least 2^-100: an infinite value then gives its infinity twice)
+              // (the first cut off, so that the second is positive, and at least 2^-18 of the weight: an infinite value then gives its infinity
+              // twice, and the weight 0 of a key that the row does not see stays 0)
               uint32_t high[4];
               float low[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 high[i] = __float_as_uint(w[i]) & 0xffff0000u;
-                low[i] = fmaxf(w[i] - __uint_as_float(high[i]), 7.9e-31f);
+                low[i] = fmaxf(w[i] - __uint_as_float(high[i]), w[i] * 3.8e-6f);
               }
               const uint32_t a = __byte_perm(high[0], high[1], 0x7632), b = __byte_perm(high[2], high[3], 0x7632);
               const __nv_bfloat162 la = __floats2bfloat162_rn(low[0], low[1]), lb = __floats2bfloat162_rn(low[2], low[3]);

@@ -792,3 +792,57 @@ def test_broken_values_of_keys_far_below(fp8, length, n):
     broken[[5, 77, 8]] = True
     assert (~torch.isfinite(out[..., broken])).all()
     assert same_bits(out[..., ~broken], clean[..., ~broken]) and same_bits(lse, clean_lse)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("d,G,n", [(128, 1, 5), (128, 4, 4), (64, 2, 4), (64, 4, 3), (128, 4, 20), (64, 2, 150)])
+def test_large_values_stay_with_who_sees_them(fp8, d, G, n):
+    """Values near the type's largest among the newest tokens: the rows in front of them keep their bits, and where all that a row sees is zero, so is
+    its output."""
+    gen = torch.Generator(device=DEV).manual_seed(n + G)
+    page, Hk, length = 32, 2, 100 + n
+    cache = make_cache(gen, 12, Hk, page, d, fp8)
+    table = make_table(gen, [length], page, 12)
+    kv_len = torch.tensor([length], dtype=torch.int32, device=DEV)
+    q = torch.randn((n, Hk * G, d), generator=gen, device=DEV).bfloat16()
+    kw = dict(max_new=n, return_lse=True)
+    seen = length - n + n // 2                                  # keys of the rows in front of row n // 2
+    for zeros, large in ((False, 1e30), (True, 1e30), (False, 3e38), (True, 3e38)):
+        v = cache.v.clone(memory_format=torch.preserve_format)
+        bits = v.view(torch.uint8) if fp8 else v
+        if zeros:
+            bits.zero_()
+        clean, clean_lse = sa.cache_fwd(q, cache._replace(v=v), table, kv_len, **kw)
+        for j in range(seen, length):
+            bits[int(table[0, j // page]), :, j % page] = 0x7e if fp8 else large
+        out, lse = sa.cache_fwd(q, cache._replace(v=v), table, kv_len, **kw)
+        assert same_bits(lse, clean_lse)
+        assert same_bits(out[:n // 2], clean[:n // 2])
+        assert not zeros or (out[:n // 2] == 0).all()
+        if large == 3e38:                                       # (sums of weights up to 2^15 times such values pass fp32)
+            continue
+        want, _ = reference(q, cache._replace(v=v), table, [length], [n], 1, 0)
+        assert ((out.double() - want).abs() <= OUT_MAX_OF_ROW * want.abs().amax(-1, keepdim=True)).all()
+
+
+@pytest.mark.parametrize("n", [1, 2, 30])
+def test_small_weights_of_large_values(n):
+    """bf16 pages: a key of weight 2^-120 with values of 2^126 beside one of weight 1 with values of 1."""
+    page, d = 16, 128
+    cache = sa.alloc_cache(2, 1, page, d, fp8=False)
+    cache.k[0, 0, 0] = 0.0
+    cache.k[0, 0, 1] = -120 * math.log(2.0) / math.sqrt(d)
+    cache.v[0, 0, 0], cache.v[0, 0, 1] = 1.0, 2.0 ** 126
+    q = torch.ones((n, 1, d), dtype=torch.bfloat16, device=DEV)
+    table = torch.zeros((1, 1), dtype=torch.int32, device=DEV)
+    kv_len = torch.tensor([2], dtype=torch.int32, device=DEV)
+    if n > 2:
+        kv_len += n - 2
+        cache.k[0, 0, 2:] = cache.k[0, 0, 1]
+        cache.k[1, 0] = cache.k[0, 0, 1]
+        table = torch.tensor([[0, 1]], dtype=torch.int32, device=DEV)
+    lens = [int(kv_len)]
+    out = sa.cache_fwd(q, cache, table, kv_len, max_new=n, frame_tokens=0, check_status=True)
+    want, _ = reference(q, cache, table, lens, [n], 0, 0)
+    # (the logit's own rounding: 2^-23 of 83, times the exponential)
+    assert ((out.double() - want).abs() <= OUT_MAX_OF_ROW * want.abs().amax(-1, keepdim=True)).all()
