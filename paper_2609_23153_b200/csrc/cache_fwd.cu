@@ -696,7 +696,7 @@ constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame_tokens, int window, int tile_keys, int sms) {
   const long long items = (long long)b.B * c.H;
   long long keys = (long long)b.max_pages * c.page;                       // that an item may have
-  if (window > 0) keys = std::min(keys, (long long)(window + 1) * frame_tokens + b.max_new);
+  if (window > 0) keys = std::min(keys, ((long long)window + 1) * frame_tokens + b.max_new);
   const long long tiles = (keys + tile_keys - 1) / tile_keys;
   int n = items * 16 <= sms ? 16 : 8;
   while (n > 1 && (items * n > std::max(2 * sms, 16) || n / 2 >= tiles)) n /= 2;

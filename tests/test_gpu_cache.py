@@ -846,3 +846,18 @@ def test_small_weights_of_large_values(n):
     want, _ = reference(q, cache, table, lens, [n], 0, 0)
     # (the logit's own rounding: 2^-23 of 83, times the exponential)
     assert ((out.double() - want).abs() <= OUT_MAX_OF_ROW * want.abs().amax(-1, keepdim=True)).all()
+
+
+@pytest.mark.parametrize("frame,n", [(1, 1), (50, 3), (7, 30)])
+def test_a_window_of_any_size(frame, n):
+    """The widest window that an int holds is no window: the same keys, dealt out in the same way, the same bits."""
+    gen = torch.Generator(device=DEV).manual_seed(frame)
+    lens, news = [3001, 700], [n, n]
+    cache = make_cache(gen, 60, 2, 64, 128, True)
+    table = make_table(gen, lens, 64, 60, spare=0)
+    kv_len, q_start = batch_of(lens, news)
+    q = torch.randn((2 * n, 4, 128), generator=gen, device=DEV).bfloat16()
+    want, want_lse = sa.cache_fwd(q, cache, table, kv_len, max_new=n, frame_tokens=frame, return_lse=True)
+    for window in (2 ** 31 - 1, 2 ** 31 - 2, 10 ** 6):
+        out, lse = sa.cache_fwd(q, cache, table, kv_len, max_new=n, frame_tokens=frame, window=window, return_lse=True, check_status=True)
+        assert same_bits(out, want) and same_bits(lse, want_lse)
