@@ -6,6 +6,9 @@ step of the path (block selection, FP8 quantisation, block-sparse attention)
 runs in the CUDA kernels behind the ``extern "C"`` entry points declared in
 ``include/sparkattn.h``.  PyTorch is used for device memory and streams.  There
 is no CPU fallback: if the shared library is missing or cannot be loaded, every call raises.
+
+Without ``stream`` a per-layer call uses the current stream.  With it, outputs and workspace that the call allocates come from that
+stream's memory; an output is read on the current stream once that has waited for the other.
 """
 from __future__ import annotations
 
@@ -351,9 +354,13 @@ def brick_layout(grid, brick, block: int, device="cuda:0", stream: Optional[torc
     if bricks == 0:
         raise SparkAttnError(E_INVALID_ARG, "sparkattn_brick_count")
     n = int(grid[0]) * int(grid[1]) * int(grid[2])
-    gather = torch.empty(bricks * block, dtype=torch.int32, device=device)
-    valid = torch.empty(bricks, dtype=torch.int32, device=device)
-    scatter = torch.empty(n, dtype=torch.int32, device=device)
+    with torch.cuda.stream(stream):      # (None: the current one)
+        gather = torch.empty(bricks * block, dtype=torch.int32, device=device)
+        valid = torch.empty(bricks, dtype=torch.int32, device=device)
+        scatter = torch.empty(n, dtype=torch.int32, device=device)
+    if stream is not None:
+        for x in (gather, valid, scatter):
+            x.record_stream(torch.cuda.current_stream(x.device))
     rc = lib().sparkattn_brick_layout(ctypes.cast(g, ctypes.c_void_p), ctypes.cast(b, ctypes.c_void_p), block, _ptr(gather),
                                       _ptr(valid), _ptr(scatter), _stream_ptr(stream))
     _check(rc, "sparkattn_brick_layout")
@@ -389,7 +396,8 @@ def attention_host(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, block: int
     if out is None:
         out = torch.empty_like(q).pin_memory()
     if arena is None:
-        arena = torch.empty(arena_bytes(shape, dtype, topk), dtype=torch.uint8, device=device)
+        with torch.cuda.stream(stream):      # (None: the current one)
+            arena = torch.empty(arena_bytes(shape, dtype, topk), dtype=torch.uint8, device=device)
     rc = lib().sparkattn_attention_host(ctypes.byref(shape), dtype, _ptr(q), _ptr(k), _ptr(v), topk, _ptr(out),
                                         _ptr(kept_idx), _ptr(arena), arena.numel(), _stream_ptr(stream))
     _check(rc, "sparkattn_attention_host")

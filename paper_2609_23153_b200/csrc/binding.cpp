@@ -7,6 +7,7 @@
 // workspace query and the tuples of sizes and strides behind each check.  Now 8.1, and the call takes what the device takes:
 // 16.5 -> 12.6 us; selection + forward of 3 heads of 1,200 tokens 36.4 -> 19.0.
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -49,6 +50,30 @@ struct Stream {
   void* handle = nullptr;
   bool given = false;
   operator void*() const { return given ? handle : c10::cuda::getCurrentCUDAStream().stream(); }
+  // Memory that a call allocates for a stream of the caller's comes from that stream's: the current stream's may still be read
+  // or written there, and would be handed out again before this one is through with it (a workspace: at the call's return).
+  at::Tensor scratch(int64_t bytes, const at::Tensor& like) const {
+    return allocate(like, [&] { return at::empty({bytes}, like.options().dtype(at::kByte)); });
+  }
+  // An output is read on the current stream, too: not handed out again before that one is through with it either.
+  at::Tensor output(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& like) const {
+    return read_here(allocate(like, [&] { return at::empty(sizes, like.options().dtype(type)); }));
+  }
+  at::Tensor output_like(const at::Tensor& like, at::ScalarType type) const {      // its strides as well
+    return read_here(allocate(like, [&] { return at::empty_strided(like.sizes(), like.strides(), like.options().dtype(type)); }));
+  }
+
+ private:
+  template <typename Make>
+  at::Tensor allocate(const at::Tensor& like, Make make) const {
+    if (!given || !like.is_cuda()) return make();
+    c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(handle), like.device().index()));
+    return make();
+  }
+  at::Tensor read_here(at::Tensor x) const {
+    if (given && x.is_cuda()) x.record_stream(c10::cuda::getCurrentCUDAStream(x.device().index()));
+    return x;
+  }
 };
 
 // The arguments of one call, taken in order; the first one of a wrong kind raises.
@@ -115,16 +140,15 @@ void same_layout(const at::Tensor& a, const at::Tensor& b) {
 void* ptr(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 int32_t* iptr(const at::Tensor& t) { return static_cast<int32_t*>(ptr(t)); }
 float* fptr(const at::Tensor& t) { return static_cast<float*>(ptr(t)); }
-at::TensorOptions on(const at::Tensor& x, at::ScalarType type) { return at::TensorOptions().dtype(type).device(x.device()); }
 // Token blocks of a head.  Outputs are sized with it before the library has looked at the shape: a block size below 1,
 // which the library refuses, has none.
 int64_t blocks(const sparkattn_shape_t& s) { return s.block < 1 ? 0 : ((int64_t)s.N + s.block - 1) / s.block; }
 
 // The caller's workspace, or a new one; undefined when the library does not serve the shape.
-at::Tensor workspace_for(at::Tensor given, const sparkattn_shape_t& s, int32_t which, int32_t k, const at::Tensor& x) {
+at::Tensor workspace_for(at::Tensor given, const sparkattn_shape_t& s, int32_t which, int32_t k, const at::Tensor& x, const Stream& stream) {
   if (given.defined()) return given;
   const size_t n = g_lib.workspace_bytes(&s, which, k);
-  return n == 0 ? at::Tensor() : at::empty({(int64_t)n}, on(x, at::kByte));
+  return n == 0 ? at::Tensor() : stream.scratch((int64_t)n, x);
 }
 
 PyObject* result(int rc, std::initializer_list<at::Tensor> tensors) {
@@ -161,9 +185,9 @@ PyObject* select(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    if (!idx.defined()) idx = at::empty({s.B, s.H, blocks(s), std::max(topk, 1)}, on(q, at::kInt));
-    if (!cnt.defined()) cnt = at::empty({s.B, s.H, blocks(s)}, on(q, at::kInt));
-    ws = workspace_for(ws, s, 0, topk, q);
+    if (!idx.defined()) idx = stream.output({s.B, s.H, blocks(s), std::max(topk, 1)}, at::kInt, q);
+    if (!cnt.defined()) cnt = stream.output({s.B, s.H, blocks(s)}, at::kInt, q);
+    ws = workspace_for(ws, s, 0, topk, q, stream);
     if (!ws.defined()) rc = kNoWorkspace;
     else if (valid.defined())
       rc = g_lib.select_padded(&s, ptr(q), ptr(k), topk, iptr(valid), iptr(idx), iptr(cnt), ptr(ws), (size_t)ws.numel(), stream);
@@ -190,8 +214,8 @@ PyObject* select_pooled(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    if (!idx.defined()) idx = at::empty({s.B, s.H, blocks(s), std::max(topk, 1)}, on(ref, at::kInt));
-    if (!cnt.defined()) cnt = at::empty({s.B, s.H, blocks(s)}, on(ref, at::kInt));
+    if (!idx.defined()) idx = stream.output({s.B, s.H, blocks(s), std::max(topk, 1)}, at::kInt, ref);
+    if (!cnt.defined()) cnt = stream.output({s.B, s.H, blocks(s)}, at::kInt, ref);
     rc = g_lib.select_pooled(&s, topk, iptr(idx), iptr(cnt), ptr(ws), (size_t)ws.numel(), stream);
   }
   return result(rc, {idx, cnt});
@@ -200,12 +224,12 @@ PyObject* select_pooled(PyObject*, PyObject* const* argv, Py_ssize_t n) {
 
 // What the three quantisation calls share: codes (laid out like x) and scales [B, H, per_head] where the caller brings none.
 template <typename Call>
-PyObject* quantise(const at::Tensor& x, const sparkattn_shape_t& s, int64_t per_head, at::Tensor codes, at::Tensor scales, Call call) {
+PyObject* quantise(const at::Tensor& x, const sparkattn_shape_t& s, int64_t per_head, at::Tensor codes, at::Tensor scales, const Stream& stream, Call call) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    if (!codes.defined()) codes = at::empty_strided(x.sizes(), x.strides(), on(x, at::kByte));
-    if (!scales.defined()) scales = at::empty({s.B, s.H, per_head}, on(x, at::kFloat));
+    if (!codes.defined()) codes = stream.output_like(x, at::kByte);
+    if (!scales.defined()) scales = stream.output({s.B, s.H, per_head}, at::kFloat, x);
     rc = call(&s, ptr(x), static_cast<uint8_t*>(ptr(codes)), fptr(scales));
   }
   return result(rc, {codes, scales});
@@ -220,7 +244,7 @@ PyObject* quant_fp8(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const sparkattn_shape_t s = make_shape(x, a.i32());
   const at::Tensor codes = a.optional_tensor(), scales = a.optional_tensor();
   const Stream stream = a.stream();
-  return quantise(x, s, blocks(s), codes, scales, [&](auto... to) { return g_lib.quant_fp8(to..., 0, stream); });
+  return quantise(x, s, blocks(s), codes, scales, stream, [&](auto... to) { return g_lib.quant_fp8(to..., 0, stream); });
   END_HANDLE_TH_ERRORS
 }
 
@@ -234,7 +258,7 @@ PyObject* quant_fp8_pooled(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const bool key_side = a.truth();
   const at::Tensor ws = a.tensor(), codes = a.optional_tensor(), scales = a.optional_tensor();
   const Stream stream = a.stream();
-  return quantise(x, s, blocks(s), codes, scales,
+  return quantise(x, s, blocks(s), codes, scales, stream,
                   [&](auto... to) { return g_lib.quant_fp8_pooled(to..., key_side, ptr(ws), (size_t)ws.numel(), stream); });
   END_HANDLE_TH_ERRORS
 }
@@ -248,7 +272,7 @@ PyObject* quant_fp8_per_token(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const sparkattn_shape_t s = make_shape(x, x.size(-1) == 64 ? 64 : 128);
   const at::Tensor codes = a.optional_tensor(), scales = a.optional_tensor();
   const Stream stream = a.stream();
-  return quantise(x, s, s.N, codes, scales, [&](auto... to) { return g_lib.quant_fp8_per_token(to..., stream); });
+  return quantise(x, s, s.N, codes, scales, stream, [&](auto... to) { return g_lib.quant_fp8_per_token(to..., stream); });
   END_HANDLE_TH_ERRORS
 }
 
@@ -275,9 +299,9 @@ PyObject* fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    if (!out.defined()) out = at::empty_strided(q.sizes(), q.strides(), on(q, at::kBFloat16));
-    if (return_lse) lse = at::empty({s.B, s.H, s.N}, on(q, at::kFloat));
-    ws = workspace_for(ws, s, 1, kmax, q);
+    if (!out.defined()) out = stream.output_like(q, at::kBFloat16);
+    if (return_lse) lse = stream.output({s.B, s.H, s.N}, at::kFloat, q);
+    ws = workspace_for(ws, s, 1, kmax, q, stream);
     const size_t bytes = ws.defined() ? (size_t)ws.numel() : 0;
     if (!ws.defined()) rc = kNoWorkspace;
     else if (valid.defined())
@@ -309,9 +333,9 @@ PyObject* gather_tokens(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    if (!out.defined()) out = at::empty({src.B, src.H, index.numel(), src.d}, on(x, x.scalar_type()));
+    if (!out.defined()) out = stream.output({src.B, src.H, index.numel(), src.d}, x.scalar_type(), x);
     const sparkattn_shape_t dst = make_shape(out, block);
-    if (!ws.defined()) ws = at::empty({256}, on(x, at::kByte));
+    if (!ws.defined()) ws = stream.scratch(256, x);
     rc = g_lib.gather_tokens(&src, ptr(x), &dst, iptr(index), ptr(out), ptr(ws), (size_t)ws.numel(), stream);
   }
   return result(rc, {out, ws});
@@ -345,7 +369,7 @@ void check_gate_operands(const at::Tensor& state, const at::Tensor& gate, const 
                     "state must be contiguous fp32 [B, H, rank, d]");
   TORCH_CHECK_VALUE(is_contiguous(gate, {s.B, s.H, s.N}) && gate.scalar_type() == at::kFloat, "gate must be contiguous fp32 [B, H, N]");
 }
-at::Tensor at_least_256(size_t bytes, const at::Tensor& x) { return at::empty({(int64_t)std::max(bytes, (size_t)256)}, on(x, at::kByte)); }
+int64_t at_least_256(size_t bytes) { return (int64_t)std::max(bytes, (size_t)256); }
 
 // comp_state(k, v, pk, T, Hg, Wg, axis, freq, state, workspace, stream) -> rc, state, workspace
 PyObject* comp_state(PyObject*, PyObject* const* argv, Py_ssize_t n) {
@@ -363,8 +387,8 @@ PyObject* comp_state(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   {
     pybind11::gil_scoped_release no_gil;
     rope.to_host();
-    if (!state.defined()) state = at::empty({s.B, s.H, rank, s.d}, on(k, at::kFloat));
-    if (!ws.defined()) ws = at_least_256(g_lib.comp_workspace_bytes(&s, rope.grid), k);
+    if (!state.defined()) state = stream.output({s.B, s.H, rank, s.d}, at::kFloat, k);
+    if (!ws.defined()) ws = stream.scratch(at_least_256(g_lib.comp_workspace_bytes(&s, rope.grid)), k);
     rc = g_lib.comp_state(&s, ptr(k), ptr(v), ptr(pk), rank, rope.grid, iptr(rope.axis), fptr(rope.freq), fptr(state), ptr(ws),
                           (size_t)ws.numel(), stream);
   }
@@ -390,8 +414,8 @@ PyObject* comp_apply(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   {
     pybind11::gil_scoped_release no_gil;
     rope.to_host();
-    if (!out.defined()) out = at::empty_strided(q.sizes(), q.strides(), on(q, at::kBFloat16));
-    if (!ws.defined()) ws = at_least_256(g_lib.comp_workspace_bytes(&s, rope.grid), q);
+    if (!out.defined()) out = stream.output_like(q, at::kBFloat16);
+    if (!ws.defined()) ws = stream.scratch(at_least_256(g_lib.comp_workspace_bytes(&s, rope.grid)), q);
     rc = g_lib.comp_apply(&s, ptr(q), ptr(pq), rank, rope.grid, iptr(rope.axis), fptr(rope.freq), fptr(state), fptr(gate),
                           ptr(o_sparse), ptr(out), eps, ptr(ws), (size_t)ws.numel(), stream);
   }
@@ -422,9 +446,9 @@ PyObject* fwd_gated(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   {
     pybind11::gil_scoped_release no_gil;
     rope.to_host();
-    if (!out.defined()) out = at::empty_strided(q.sizes(), q.strides(), on(q, at::kBFloat16));
-    if (return_lse) lse = at::empty({s.B, s.H, s.N}, on(q, at::kFloat));
-    if (!ws.defined()) ws = at_least_256(g_lib.fwd_gated_workspace_bytes(&s, kmax, rope.grid), q);
+    if (!out.defined()) out = stream.output_like(q, at::kBFloat16);
+    if (return_lse) lse = stream.output({s.B, s.H, s.N}, at::kFloat, q);
+    if (!ws.defined()) ws = stream.scratch(at_least_256(g_lib.fwd_gated_workspace_bytes(&s, kmax, rope.grid)), q);
     rc = g_lib.fwd_gated(&s, ptr(q), ptr(k), ptr(v), iptr(idx), iptr(cnt), kmax, ptr(pq), rank, rope.grid, iptr(rope.axis),
                          fptr(rope.freq), fptr(state), fptr(gate), eps, ptr(out), fptr(lse), ptr(ws), (size_t)ws.numel(), stream);
   }
@@ -528,8 +552,8 @@ PyObject* cache_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    if (q.defined() && !q_out.defined()) q_out = at::empty(q.sizes(), on(q, at::kBFloat16));
-    if (!ws.defined()) ws = at::empty({256}, on(k, at::kByte));
+    if (q.defined() && !q_out.defined()) q_out = stream.output(q.sizes(), at::kBFloat16, q);
+    if (!ws.defined()) ws = stream.scratch(256, k);
     cache.check_workspace(ws);
     sparkattn_rows_t rq{}, ro{};
     if (q.defined()) {
@@ -565,12 +589,12 @@ PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    if (!out.defined()) out = at::empty(q.sizes(), on(q, at::kBFloat16));
+    if (!out.defined()) out = stream.output(q.sizes(), at::kBFloat16, q);
     const sparkattn_rows_t ro = cache.rows(out, H);
-    if (return_lse) lse = at::empty({q.size(0), q.size(1)}, on(q, at::kFloat));
+    if (return_lse) lse = stream.output({q.size(0), q.size(1)}, at::kFloat, q);
     if (!ws.defined()) {
       const size_t bytes = g_lib.cache_workspace_bytes(&cache.c, &cache.b, H);
-      ws = at::empty({(int64_t)(bytes < 256 ? 256 : bytes)}, on(q, at::kByte));      // an unsupported call says why itself
+      ws = stream.scratch((int64_t)(bytes < 256 ? 256 : bytes), q);      // an unsupported call says why itself
     }
     cache.check_workspace(ws);
     rc = g_lib.cache_fwd(&cache.c, &cache.b, &rq, H, ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), frame_tokens, window,

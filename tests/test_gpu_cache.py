@@ -861,3 +861,60 @@ def test_a_window_of_any_size(frame, n):
     for window in (2 ** 31 - 1, 2 ** 31 - 2, 10 ** 6):
         out, lse = sa.cache_fwd(q, cache, table, kv_len, max_new=n, frame_tokens=frame, window=window, return_lse=True, check_status=True)
         assert same_bits(out, want) and same_bits(lse, want_lse)
+
+
+def test_memory_of_calls_on_another_stream():
+    """What a call allocates itself for a stream of the caller's is neither memory that the current stream may still use, nor handed out to the
+    current stream while the other has yet to use it."""
+    gen = torch.Generator(device=DEV).manual_seed(17)
+    cache = make_cache(gen, 40, 2, 64, 128, True)
+    table = make_table(gen, [2000], 64, 40)
+    kv_len = torch.tensor([2000], dtype=torch.int32, device=DEV)
+    q = torch.randn((1, 4, 128), generator=gen, device=DEV).bfloat16()
+    k = torch.randn((1, 2, 128), generator=gen, device=DEV).bfloat16()
+    x = torch.randn((1, 2, 512, 128), generator=gen, device=DEV).bfloat16()
+    kept, count = sa.select(x, x, 128, 2)
+    index = torch.arange(512, device=DEV, dtype=torch.int32)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    to, native = side.cuda_stream, sa._calls()
+    calls = {"cache_fwd": lambda: native.cache_fwd(*cache, table, kv_len, None, 0, q, 1, 0, 0.0, None, True, None, to),
+             "cache_append": lambda: native.cache_append(*cache, table, kv_len, None, 0, k, k, q, None, None, None, None, None, False, None, to),
+             "select": lambda: native.select(x, x, 128, 2, None, None, None, to, 0, 0, None),
+             "quant_fp8": lambda: native.quant_fp8(x, 128, None, None, to),
+             "fwd": lambda: native.fwd(x, x, x, kept, count, 128, sa.BF16, None, None, None, 0.0, None, True, None, to, 0, 0, None),
+             "gather_tokens": lambda: native.gather_tokens(x, index, None, None, to)}
+    places = lambda tensors: [(y.data_ptr(), y.data_ptr() + y.numel() * y.element_size()) for y in tensors if y is not None]
+    apart = lambda a, b: all(hi <= x0 or x1 <= lo for lo, hi in a for x0, x1 in b)
+    for name, call in calls.items():
+        rc, *made = call()
+        assert rc == sa.OK
+        sizes = [hi - lo for lo, hi in places(made)]
+        del made
+        torch.cuda.synchronize()
+        # memory that the current stream has given back, and may still be working on
+        freed = [torch.empty(size, dtype=torch.uint8, device=DEV) for size in sizes for _ in range(4)]
+        torch.cuda._sleep(20_000_000)
+        used = places(freed)
+        del freed
+        rc, *made = call()
+        assert apart(places(made), used), name
+        torch.cuda.synchronize()
+        # the other stream has not begun when what the call made is dropped
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        rc, *made = call()
+        used = places(made)
+        del made
+        others = [torch.empty(size, dtype=torch.uint8, device=DEV) for size in sizes for _ in range(4)]
+        assert apart(places(others), used), name
+        torch.cuda.synchronize()
+        # an output that the current stream reads is not overwritten by the other's next call
+        rc, *made = call()
+        out = places(made[:1])
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda._sleep(20_000_000)
+        del made
+        rc, *made = call()
+        assert apart(places(made), out), name
+        torch.cuda.synchronize()
