@@ -506,10 +506,14 @@ int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch
  * workspace    : >= sparkattn_cache_workspace_bytes(cache, batch, H), 256-byte aligned; first word = device status
  * A key or value that is not finite reaches the rows that see its key, and no others.
  * Scores, maxima, sums and the output's accumulation are fp32.  The weights of the second product are rounded to fp16 over
- * E4M3 pages; over bf16 pages to two bf16 parts (16 digits together) for up to 16 rows per key head (H / cache->H * max_new), to
- * one for more.  Queries over E4M3 pages are used as bf16 holds them, but for entries below 2^-9 of their row's largest, which
- * are off by 2^-18 of that at most (d = 128; d = 64: fp16 scaled by the row's largest, for more than 16 rows); a query row with
- * an infinity or a NaN in it gives NaN.  The same inputs give the same bits.
+ * E4M3 pages, where what lies below 2^-30 of a row's largest (weight times value scale) is lost to the output, not to lse; over bf16
+ * pages to two bf16 parts (16 digits together) for up to 16 rows per key head (H / cache->H * max_new), to one for more.  A value
+ * scale below 2^-64 counts as 2^-64.  Queries over E4M3 pages are used as bf16 holds them, but for entries below 2^-9 of their row's
+ * largest, which are off by 2^-17 of that at most (d = 64 and more than 16 rows: below 2^-24, by 2^-32); a query row with
+ * an infinity or a NaN in it gives NaN.  The same inputs give the same bits, however often and beside whatever they are computed, as
+ * long as the structs are the same: the work is split by max_new and by max_pages * page, the longest sequence that the table allows, not
+ * by the lengths.  So both cost time where they are far above what the batch has (one sequence of 1000 keys under a table of 131,072: three
+ * microseconds more; single tokens under a max_new of more than 16 rows take the kernel for prompts).
  * A batch whose structs allow more than 2^31 key tiles of 64 in all is SPARKATTN_E_UNSUPPORTED_SHAPE.
  */
 int sparkattn_cache_fwd(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rows_t* q, int32_t H,

@@ -455,7 +455,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
               *reinterpret_cast<uint2*>(to) = make_uint2(high[0], high[1]);
               *reinterpret_cast<uint2*>(to + kSlab) = make_uint2(low[0], low[1]);
             } else {
-              // fp16: the row's largest entry lies in [128, 256), what is below 2^-32 of it is rounded to fp16's subnormal numbers
+              // fp16: the row's largest entry lies in [128, 256); entries below 2^-24 of it are subnormal numbers, off by at most 2^-32 of it
               uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
               for (int i = 0; i < 4; ++i) {

@@ -18,7 +18,7 @@
 namespace sparkattn {
 
 // The reference m of a row moves when a weight would pass 2^10 times the one that set it; weights are 2^kBase at the reference, so
-// that fp16 holds them (2^15 < 65504) and loses only what lies 2^-29 below it.
+// that fp16 holds them (2^15 < 65504) and loses only what lies below 2^-30 of it, half of the smallest subnormal number.
 constexpr float kBase = 5.0f, kLazy = 10.0f;
 
 struct CacheFwdParams {
@@ -236,7 +236,7 @@ struct Stretch {
 // Queries against E4M3 keys: a row times the power of two that brings its largest entry to [128, 256), as two E4M3 parts,
 // high = rne(x) and low = rne(x - high).  A bf16 has eight significant digits and an E4M3 four, so x - high has at most four and
 // the sum of the parts is x, but for entries below 2^-9 of the row's largest, whose low part falls into E4M3's subnormal
-// numbers: off by at most 2^-18 of the largest.  Products of two E4M3 numbers are exact in the tensor core and their sums were found to be
+// numbers: off by at most 2^-10, half of their step, which is 2^-17 of the largest.  Products of two E4M3 numbers are exact in the tensor core and their sums were found to be
 // fp32's (off by at most 2^-25 of the sum of the magnitudes, m16n8k32 over 128 channels).  Keys stay codes, and the two products
 // take as long as one with 16-bit operands.  A row with an infinity or a NaN in it gives NaN.
 struct QueryScale {
@@ -285,7 +285,7 @@ template <bool FP8>
 __device__ __forceinline__ GroupInfo info_of(const GroupBatch& b) {
   GroupInfo info{1.0f, 0.0f, 1.0f, b.page >= 0};
   if constexpr (FP8) {
-    const float v = fmaxf(b.v_scale, 5.4e-20f);      // 2^-64: a scale of zero stays finite
+    const float v = fmaxf(b.v_scale, 0x1p-64f);      // a scale of zero stays finite, and so do sums of weights over it
     info.k = b.k_scale;
     info.v_log2 = log2f(v);
     info.v_inv = 1.0f / v;

@@ -187,3 +187,16 @@ def test_what_threads_write_into_a_tile_is_fenced_before_the_next_copy():
     assert re.search(r"if constexpr \(!FP8\) asm volatile\(.fence\.proxy\.async", edge)
     mark = decode[decode.index("mark_tile("):decode.index("cache_decode_kernel(")]
     assert mark.index("mark_word<") < mark.index("fence.proxy.async")
+
+
+def test_queries_in_parts_are_as_exact_as_the_header_says():
+    """Every bf16 of a row whose largest entry lies in [128, 256): as two E4M3 parts exact from 2^-9 of the largest on and off by 2^-17 of it at most
+    below, as fp16 from 2^-24 on and by 2^-32."""
+    x = torch.arange(1, 0x7f80, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).double()
+    x = x[x < 256]
+    e4m3 = lambda y: y.float().to(torch.float8_e4m3fn).double()
+    high = e4m3(x)
+    off = (x - high - e4m3(x - high)).abs()
+    assert off.max() == 128 * 2.0 ** -17 and (off[x >= 128 * 2.0 ** -9] == 0).all()
+    off = (x - x.float().half().double()).abs()
+    assert off.max() == 128 * 2.0 ** -32 and (off[x >= 128 * 2.0 ** -24] == 0).all()

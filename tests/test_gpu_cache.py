@@ -918,3 +918,139 @@ def test_memory_of_calls_on_another_stream():
         rc, *made = call()
         assert apart(places(made), out), name
         torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------------------ inside the tensors
+
+def margined(x):
+    """x's bits as a view into a larger buffer, and the buffer: one of a known byte, on both sides, and between rows of the last dimension but two."""
+    outer = list(x.shape)
+    outer[0] += 2                                               # a whole block in front and behind
+    if x.dim() > 2:
+        outer[-2] += 1                                          # and a row behind each block's rows
+    buf = torch.empty(outer, dtype=x.dtype, device=DEV)
+    buf.view(torch.uint8).fill_(0xA5)
+    inner = buf[1:-1, ..., :-1, :] if x.dim() > 2 else buf[1:-1]
+    inner.copy_(x)
+    return inner, buf
+
+
+def margins_kept(inner, buf):
+    bits = buf.view(torch.uint8).clone()
+    same = torch.full_like(bits, 0xA5)
+    inside = (lambda x: x[1:-1, ..., :-1, :]) if buf.dim() > 2 else (lambda x: x[1:-1])
+    inside(bits).copy_(inside(same))
+    return torch.equal(bits, same)
+
+
+@pytest.mark.parametrize("what", ["nothing", "negative length", "length beyond the table", "starts descend", "starts beyond the rows", "more than max_new",
+                                  "more new tokens than tokens", "pages that do not exist"])
+@pytest.mark.parametrize("fp8,G", [(True, 2), (False, 2), (True, 9), (False, 9)])
+def test_a_broken_callers_numbers_touch_nothing_else(what, fp8, G):
+    """Pools, scales, rows and outputs inside larger buffers: whatever the device-side numbers are, the margins, pages of nobody and the tokens in front of
+    the new ones keep their bits."""
+    gen = torch.Generator(device=DEV).manual_seed(16)
+    Hk, page, d, n = 2, 16, 64, 3
+    cache = make_cache(gen, 9, Hk, page, d, fp8)
+    held = [None if x is None else margined(x) for x in cache]
+    cache = sa.KVCache(*(None if x is None else x[0] for x in held))
+    if cache.k_scale is not None:                               # (scales are contiguous: rows in front and behind)
+        assert cache.k_scale.is_contiguous()
+    lens, starts = [40, 50], [0, 3, 6]
+    table = make_table(gen, lens, page, 9, spare=0)
+    table[0, 3] = table[0, 0]                                   # (a column that a length of 40 does not reach)
+    owned = {b: set(table[b, :-(-x // page)].tolist()) for b, x in enumerate(lens)}
+    max_new = n
+    if what == "negative length":
+        lens[0] = -5
+    elif what == "length beyond the table":
+        lens[1] = 100000
+    elif what == "starts descend":
+        starts = [4, 2, 6]
+    elif what == "starts beyond the rows":
+        starts = [0, 3, 900]
+    elif what == "more than max_new":
+        max_new = 2
+    elif what == "more new tokens than tokens":
+        lens[0] = 2
+    elif what == "pages that do not exist":
+        table[0, 2], table[1, 1] = 9, -1
+    kv_len = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    q_start = torch.tensor(starts, dtype=torch.int32, device=DEV)
+    q = torch.randn((6, Hk * G, d), generator=gen, device=DEV).bfloat16()
+    k, v = (torch.randn((6, Hk, d), generator=gen, device=DEV).bfloat16() for _ in range(2))
+    outs = [margined(torch.zeros_like(q)) for _ in range(2)]
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+    before = [None if x is None else x.clone() for x in cache]
+    status = sa.OK if what == "nothing" else sa.E_BAD_INDEX
+    sa.cache_fwd(q, cache, table, kv_len, q_start=q_start, max_new=max_new, out=outs[0][0], workspace=ws)
+    assert sa.read_status(ws) == status
+    for x, y in zip(cache, before):
+        assert x is None or same_bits(x, y)                     # (it reads)
+    sa.cache_append(cache, k, v, table, kv_len, q_start=q_start, max_new=max_new, q=q, q_out=outs[1][0], workspace=ws)
+    assert sa.read_status(ws) == status
+    for x in (*held, *outs):
+        assert x is None or margins_kept(*x)
+    nobodys = [p for p in range(9) if p not in owned[0] | owned[1]]
+    for x, y in zip(cache, before):
+        assert x is None or same_bits(x[nobodys], y[nobodys])
+    # pages that a sequence has filled before: all but the one where its new tokens begin, where the numbers are its own
+    for b, first in ((0, 37 // page), (1, 47 // page)):
+        if what in ("nothing", "more than max_new", "pages that do not exist"):
+            full = [p for p in table[b, :first].tolist() if 0 <= p < 9]
+            for x, y in zip(cache, before):
+                assert x is None or same_bits(x[full], y[full])
+
+
+# ------------------------------------------------------------------------------------- forms that the cases above leave out
+
+@pytest.mark.parametrize("case", [
+    ([1000, 130], [10, 9], 16, 4, 128, 64, False, 1, 0),       # 40 rows of 128 channels, bf16
+    ([700], [100], 1, 1, 128, 16, False, 1, 90),
+    ([3000, 20], [16, 3], 8, 1, 128, 128, False, 30, 2),
+    ([500, 0, 300], [16, 2, 16], 8, 8, 128, 32, False, 1, 0),  # 16 rows, one group of keys a warp
+    ([600], [8], 8, 4, 64, 32, False, 1, 0),
+    ([1, 4000, 17], [1, 500, 1], 4, 2, 64, 16, True, 1, 0),    # a prompt's piece beside single tokens
+    ([1, 900, 17], [1, 300, 1], 8, 8, 128, 64, False, 1, 0),
+], ids=lambda c: "-".join(str(x) for x in c[2:]) + f"-{len(c[0])}x{max(c[0])}")
+def test_attention_over_pages_of_other_forms(case):
+    test_attention_over_pages(case, False)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("n", [1, 2, 30])
+def test_a_table_wider_than_the_lengths(fp8, n):
+    """A serving loop's table has columns for the longest context allowed: the result is attention's, whatever the width."""
+    gen = torch.Generator(device=DEV).manual_seed(18)
+    lens, news = [1000, 77], [n, n]
+    cache = make_cache(gen, 40, 2, 32, 128, fp8)
+    kv_len, q_start = batch_of(lens, news)
+    q = torch.randn((2 * n, 16, 128), generator=gen, device=DEV).bfloat16()
+    table = make_table(gen, lens, 32, 40)
+    want, want_lse = reference(q, cache, table, lens, news, 1, 0)
+    for columns in (32, 128, 1000, 4096):
+        wide = torch.full((2, columns), -7, dtype=torch.int32, device=DEV)
+        wide[:, :32] = table[:, :32]
+        out, lse = sa.cache_fwd(q, cache, wide, kv_len, q_start=q_start, max_new=n, return_lse=True, check_status=True)
+        check(out, lse, want, want_lse)
+
+
+@pytest.mark.parametrize("n", [1, 30])
+def test_scales_of_any_size(n):
+    """Scales of a page and head anywhere from 2^-64 to 2^60, side by side; a value scale below 2^-64 counts as that."""
+    gen = torch.Generator(device=DEV).manual_seed(20)
+    lens, page, d = [300], 32, 64
+    cache = make_cache(gen, 12, 2, page, d, True)
+    table = make_table(gen, lens, page, 12)
+    kv_len = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    q = torch.randn((n, 4, d), generator=gen, device=DEV).bfloat16()
+    for low, high in ((-64, -60), (-8, 60), (-64, 0), (20, 60)):
+        scale = torch.exp2(torch.randint(low, high + 1, (12, 2), generator=gen, device=DEV).float())
+        c = cache._replace(v_scale=scale)
+        out, lse = sa.cache_fwd(q, c, table, kv_len, max_new=n, return_lse=True, check_status=True)
+        want, want_lse = reference(q, c, table, lens, [n], 1, 0)
+        size = want.abs().amax(-1, keepdim=True)
+        assert ((out.double() - want).abs() <= OUT_MAX_OF_ROW * size).all() and (lse - want_lse).abs().max() <= LSE_ABS
+    tiny = sa.cache_fwd(q, cache._replace(v_scale=torch.full_like(scale, 2.0 ** -100)), table, kv_len, max_new=n)
+    least = sa.cache_fwd(q, cache._replace(v_scale=torch.full_like(scale, 2.0 ** -64)), table, kv_len, max_new=n)
+    assert same_bits(tiny, least)
