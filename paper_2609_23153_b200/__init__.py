@@ -497,7 +497,7 @@ def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, page_table: t
     """``sparkattn_cache_append``: stores k, v bf16 [T, H_kv, d] (k rotated) as the newest tokens of the sequences, and returns
     q bf16 [T, H, d] rotated (None without q; ``q_out`` may be q).  page_table int32 [B, max_pages]; kv_len int32 [B] with the
     new tokens; rows q_start[b] .. q_start[b+1] - 1 (int32 [B+1]) belong to sequence b, T / B each without it; max_new:
-    no sequence has more new tokens (0: T, or T / B)."""
+    no sequence has more new tokens (0: T with q_start, which is slow where many sequences share the rows, else T / B)."""
     cos, sin, positions, axis, interleaved = (None, None, None, None, False) if rotary is None else rotary
     rc, q_out, workspace = _calls().cache_append(*cache, page_table, kv_len, q_start, max_new, k, v, q, q_out, cos, sin, positions, axis,
                                                  interleaved, workspace, None if stream is None else stream.cuda_stream)
@@ -514,7 +514,8 @@ def cache_fwd(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, kv_len:
               workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
     """``sparkattn_cache_fwd``: softmax attention of the newest tokens' queries q bf16 [T, H, d] over the cache, H a multiple of
     the cache's heads; causal by frames of ``frame_tokens`` tokens (1: by token, 0: not), over the last ``window`` frames (0: all).
-    The batch as in :func:`cache_append`.  Returns out bf16 [T, H, d] (and lse float32 [T, H])."""
+    The batch as in :func:`cache_append`; kernel and split go by ``max_new`` and the width of ``page_table``, so both should be what the
+    batch needs.  Returns out bf16 [T, H, d] (and lse float32 [T, H])."""
     rc, out, lse, workspace = _calls().cache_fwd(*cache, page_table, kv_len, q_start, max_new, q, frame_tokens, window, softmax_scale, out,
                                                  return_lse, workspace, None if stream is None else stream.cuda_stream)
     if rc != OK:

@@ -17,12 +17,15 @@
 // run in the order of issue, so S_g of the next tile may overwrite the columns that PV_g has read its P from.
 // E4M3, 128 channels: K's codes are the first product's operand as they are, against the queries in two E4M3 parts
 // (split_queries): twice as many products at twice the rate.  P and V are fp16 (the weights 2^5 at the reference), and V's scale is part of the
-// exponent: t = logit + log2(v_scale), the row sum adds weight / v_scale.  bf16 pages: bf16 throughout.
+// exponent: t = logit + log2(v_scale), the row sum adds weight / v_scale.  bf16 pages: bf16 throughout, the weights too, since A and B of a
+// product have one type: out is then 2.0-2.3e-3 from the result in 64 bits, where its own rounding is 1.7e-3.  Weights in two bf16 parts,
+// the second one in the other half of S's columns, give 1.7e-3, and half as many products again: three frames of 1560 tokens 851 -> 1184 us, four
+// prompts 550 -> 774, five drafted tokens of 8 sequences 69 -> 78.  So one part here, two with few rows, where the memory's time hides the second.
 // Measured (E4M3, 128 channels; a library product of bf16 matrices reaches 1704 TFLOP/s in a burst, 1439 for seconds): 4680 new tokens,
-// three frames, over 32,760, 12 heads, 897 GFLOP in 860 us = 1040 TFLOP/s, at 1.6 GHz under the power limit: tensor cores and special-function unit are busy 52 % of the
-// clocks each, the rest is the chain that a half goes through once a tile, S, maximum, exponentials, P V.
-// Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 560 us = 910 TFLOP/s; a causal
-// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 64 us;
+// three frames, over 32,760, 12 heads, 897 GFLOP in 835-860 us = 1040-1070 TFLOP/s, called for seconds, at 1.6 GHz and less under the power limit, 938: tensor cores and
+// special-function unit are busy 52 % of the clocks each, the rest is the chain that a half goes through once a tile, S, maximum, exponentials, P V.
+// Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 550-590 us = 860-920 TFLOP/s; a causal
+// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 64-66 us;
 // 1 us a tile per SM, a chain of copy, conversion, product, softmax and product that only two tiles at a time share.
 // (A quarter of the exponentials as a polynomial of degree 4 on the FMA pipe, to spare the special-function unit: 870 us
 // either way for three frames of 1560 tokens over 32,760 keys, 710 instead of 672 for four prompts.)
@@ -422,8 +425,9 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       float back = 1.0f;
       {
         // A warp's 32 rows, D / 8 lanes a row and 16 bytes a lane, copied to where they will be operands and turned into them there.  In
-        // short loops: code that runs once an item comes from memory, and a thread's whole row unrolled took longer than what it does (five
-        // drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 72 us, unrolled 79; queries and output at one place each: 67).
+        // short loops: code that runs once an item comes from memory, and a thread's whole row unrolled took longer than what it does (when this
+        // was built, five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 72 us, unrolled 79; queries and output at one place each
+        // then 67, and 64 with the divisions as multiplications).
         constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
         const uint64_t src = at.there ? reinterpret_cast<uint64_t>(p.q + (int64_t)at.token * p.q_stride_t + at.head * p.q_stride_h) : 0ull;
         const int c = lane % kLanes, first = (row & ~31) + lane / kLanes;

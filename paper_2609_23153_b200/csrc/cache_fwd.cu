@@ -681,18 +681,20 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 namespace {
 constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 // Who splits an item: a cluster of the returned number of CTAs, or (0) the line.
-//   A cluster adds up its parts at once (128-key tiles, 8 key heads, one sequence of 500 / 4000 / 16,000 keys: 6.2 / 8.4 / 15.1 us, line 9.3 / 11.7 /
-//   17.7), as many CTAs as one wave of two per SM holds, of up to sixteen where that leaves SMs to spare (16 of 8 items: 4000 keys 8.4 us, 8: 8.7;
-//   16,000 keys 15.1 and 17.8; more than a wave: 16 sequences of 1000 keys by 2 CTAs an item 10.5 us, by 4 16.1).
+//   A cluster adds up its parts at once (128-key tiles, 8 key heads, one sequence of 500 / 4000 / 16,000 keys: 6.2 / 8.5 / 15.3 us, line 9.4 / 12.1 /
+//   16.0), as many CTAs as one wave of two per SM holds, of up to sixteen where that leaves SMs to spare (16 of 8 items: 4000 keys 8.5 us, 8: 9.0;
+//   16,000 keys 15.3 and 18.2; more than a wave: 16 sequences of 1000 keys by 2 CTAs an item 10.6 us, by 4 16.0).
 //   Two of a long item's where one each would fill a wave: sequences seldom have one length (16 sequences of up to 4000 keys, 12 heads, E4M3:
-//   26.6 us, by one CTA 32.4, the line 33.6; all of one length 49.4, 41.3, 42.6).
-//   The line takes over where clusters leave SMs idle for long (32,000 keys: 21.4 us, clusters of 16 24.0) and where the
-//   items are more than a wave and long, whose lengths may differ (64 sequences of up to 8191 keys, 8 heads: 105 us, clusters of
-//   1 / 2 121 / 107; all of one length 179 and 169 / 184; of 2000 keys 55 and 50).  So it does between, from 2304 keys a CTA on: lengths up to
-//   the stated one, in parentheses all of it, line / cluster of two, E4M3: 10 sequences of 8 heads, 4000 keys 19.0 / 20.0 us (21.8 / 23.8), 16,000
-//   42.7 / 63.6 (63.2 / 76.3); 16 of 8, 4000 21.8 / 20.3 (34.7 / 27.5), 16,000 54.2 / 65.2 (91.8 / 83.0); 16 of 12, 8000 43.7 / 46.2 (71.4 / 87.2); cluster
-//   of four: 5 of 8, 16,000 26.7 / 35.5 (37.7 / 42.9).  bf16: 16 of 8, 4000 33.1 / 31.3 (51.3 / 44.5); 8 of 12, 16,000 74.2 / 96.3 (127 / 118); 32 of 8, 8000
-//   92.5 / 100 (168 / 152).
+//   27.0 us, by one CTA 33.1, the line 26.7; all of one length 50.4, 42.5, 42.8).
+//   The line takes over where clusters leave SMs idle for long (32,000 keys: 19.2 us, clusters of 16 24.2) and where the
+//   items are more than a wave and long, whose lengths may differ (64 sequences of up to 8191 keys, 8 heads: 95 us, clusters of
+//   1 / 2 120 / 109; all of one length 171 and 167 / 184; of 2000 keys 56 and 52).  So it does between, from 2304 keys a CTA on: lengths up to
+//   the stated one, in parentheses all of it, line / cluster of two, E4M3: 10 sequences of 8 heads, 4000 keys 18.1 / 20.2 us (22.1 / 24.6), 16,000
+//   41.8 / 64.7 (61.5 / 78.2); 16 of 8, 4000 20.5 / 20.3 (32.7 / 27.6), 16,000 52.7 / 65.7 (89.2 / 83.2); 16 of 12, 8000 43.0 / 46.1 (71.4 / 87.9); cluster
+//   of four: 5 of 8, 16,000 26.0 / 36.1 (36.3 / 43.4).  bf16: 16 of 8, 4000 31.8 / 30.4 (51.5 / 44.1); 8 of 12, 16,000 73.3 / 94.9 (129 / 118); 32 of 8, 8000
+//   93.0 / one CTA 105 (169 / 150).
+//   Lengths are known on the device only: the table's width stands for them, and one sequence of 1000 keys under a table of 131,072 takes the
+//   line (9.8 us; under its own width a cluster, 6.2).  Sixteen CTAs take eight SMs of one GPC: 148 SMs in eight GPCs always leave one with that many.
 int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame_tokens, int window, int tile_keys, int sms) {
   const long long items = (long long)b.B * c.H;
   long long keys = (long long)b.max_pages * c.page;                       // that an item may have
