@@ -913,7 +913,7 @@ def test_memory_of_calls_on_another_stream():
         rc, *made = call()
         out = places(made[:1])
         torch.cuda.current_stream().wait_stream(side)
-        torch.cuda._sleep(20_000_000)
+        torch.cuda._sleep(200_000_000)                          # (0.1 s: the host is back in time)
         del made
         rc, *made = call()
         assert apart(places(made), out), name
