@@ -522,6 +522,20 @@ int sparkattn_cache_fwd(const sparkattn_cache_t* cache, const sparkattn_batch_t*
                         int32_t frame_tokens, int32_t window_frames, float softmax_scale, const sparkattn_rows_t* out,
                         float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * The same through a window and with the sequence's first tokens, which stay visible however far it has gone on: the token at
+ * position i sees the keys j < hi(i) with  lo(i) <= j  or  j < sink_tokens.
+ * What a generator without end attends to: what has left the window is not read, its pages may be gone (any number, -1 among them, may
+ * stand in the table there; sparkattn_pages_trim gives them back), and the first tokens or the first frame go on being seen.  Positions
+ * are those of the sequence; keys keep the rotation they were stored with.
+ * sink_tokens  : >= 0; without a window (window_frames = 0) and with 0 the call is sparkattn_cache_fwd
+ * Everything else, the workspace among it, as in sparkattn_cache_fwd.
+ */
+int sparkattn_cache_fwd_sink(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rows_t* q, int32_t H,
+                             const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                             int32_t frame_tokens, int32_t window_frames, int32_t sink_tokens, float softmax_scale,
+                             const sparkattn_rows_t* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

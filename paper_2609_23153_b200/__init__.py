@@ -43,7 +43,7 @@ EXPORTS = (
     "sparkattn_comp_apply", "sparkattn_select_window", "sparkattn_fwd_window", "sparkattn_brick_count",
     "sparkattn_brick_layout", "sparkattn_gather_tokens", "sparkattn_select_padded", "sparkattn_fwd_padded",
     "sparkattn_quant_fp8_pooled", "sparkattn_select_pooled", "sparkattn_fwd_gated_workspace_bytes", "sparkattn_fwd_gated",
-    "sparkattn_cache_workspace_bytes", "sparkattn_cache_append", "sparkattn_cache_fwd",
+    "sparkattn_cache_workspace_bytes", "sparkattn_cache_append", "sparkattn_cache_fwd", "sparkattn_cache_fwd_sink",
 )
 
 
@@ -103,7 +103,8 @@ class SparkAttnError(RuntimeError):
 # What the native marshalling of the per-layer calls (csrc/binding.cpp) calls, in its order.
 _BOUND = ("workspace_bytes", "select", "select_window", "select_padded", "select_pooled", "quant_fp8", "quant_fp8_pooled",
           "quant_fp8_per_token", "fwd", "fwd_window", "fwd_padded", "gather_tokens", "comp_workspace_bytes", "comp_state", "comp_apply",
-          "fwd_gated_workspace_bytes", "fwd_gated", "cache_workspace_bytes", "cache_append", "cache_fwd")
+          "fwd_gated_workspace_bytes", "fwd_gated", "cache_workspace_bytes", "cache_append", "cache_fwd",
+          "cache_fwd_sink")
 _NO_WORKSPACE = 1        # the library does not serve the shape: the workspace query returned 0
 
 _lib = None
@@ -181,6 +182,8 @@ def lib() -> ctypes.CDLL:
         L.sparkattn_cache_append.argtypes = [cp, bp, ctypes.POINTER(RotaryShape), rp, i32, rp, rp, vp, vp, vp, vp, rp, vp, sz, vp]
         L.sparkattn_cache_fwd.restype = ctypes.c_int
         L.sparkattn_cache_fwd.argtypes = [cp, bp, rp, i32, vp, vp, vp, vp, i32, i32, ctypes.c_float, rp, vp, vp, sz, vp]
+        L.sparkattn_cache_fwd_sink.restype = ctypes.c_int
+        L.sparkattn_cache_fwd_sink.argtypes = [cp, bp, rp, i32, vp, vp, vp, vp, i32, i32, i32, ctypes.c_float, rp, vp, vp, sz, vp]
         from . import _sparkattn
         _sparkattn.bind(*(ctypes.cast(getattr(L, "sparkattn_" + name), vp).value for name in _BOUND))
         _native = _sparkattn
@@ -509,14 +512,15 @@ def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, page_table: t
 
 
 def cache_fwd(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, kv_len: torch.Tensor, *,
-              q_start: Optional[torch.Tensor] = None, max_new: int = 0, frame_tokens: int = 1, window: int = 0,
+              q_start: Optional[torch.Tensor] = None, max_new: int = 0, frame_tokens: int = 1, window: int = 0, sink: int = 0,
               softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, return_lse: bool = False,
               workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
-    """``sparkattn_cache_fwd``: softmax attention of the newest tokens' queries q bf16 [T, H, d] over the cache, H a multiple of
-    the cache's heads; causal by frames of ``frame_tokens`` tokens (1: by token, 0: not), over the last ``window`` frames (0: all).
+    """``sparkattn_cache_fwd`` (``sparkattn_cache_fwd_sink`` where ``sink`` > 0): softmax attention of the newest tokens' queries
+    q bf16 [T, H, d] over the cache, H a multiple of the cache's heads; causal by frames of ``frame_tokens`` tokens (1: by token,
+    0: not), over the last ``window`` frames (0: all) and the sequence's first ``sink`` tokens.
     The batch as in :func:`cache_append`; kernel and split go by ``max_new`` and the width of ``page_table``, so both should be what the
     batch needs.  Returns out bf16 [T, H, d] (and lse float32 [T, H])."""
-    rc, out, lse, workspace = _calls().cache_fwd(*cache, page_table, kv_len, q_start, max_new, q, frame_tokens, window, softmax_scale, out,
+    rc, out, lse, workspace = _calls().cache_fwd(*cache, page_table, kv_len, q_start, max_new, q, frame_tokens, window, sink, softmax_scale, out,
                                                  return_lse, workspace, None if stream is None else stream.cuda_stream)
     if rc != OK:
         _check(rc, "sparkattn_cache_fwd")

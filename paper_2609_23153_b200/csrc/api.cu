@@ -614,17 +614,25 @@ int sparkattn_cache_fwd(const sparkattn_cache_t* cache, const sparkattn_batch_t*
                         const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                         int32_t frame_tokens, int32_t window_frames, float softmax_scale, const sparkattn_rows_t* out,
                         float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return sparkattn_cache_fwd_sink(cache, batch, q, H, k_cache, v_cache, k_scale, v_scale, frame_tokens, window_frames, 0, softmax_scale, out, lse,
+                                  workspace, workspace_bytes, cuda_stream);
+}
+
+int sparkattn_cache_fwd_sink(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rows_t* q, int32_t H,
+                             const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                             int32_t frame_tokens, int32_t window_frames, int32_t sink_tokens, float softmax_scale,
+                             const sparkattn_rows_t* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   int rc = check_cache(cache, batch);
   if (rc == SPARKATTN_OK) rc = check_heads(cache, batch, H);
   if (rc == SPARKATTN_OK) rc = check_rows(q, false);
   if (rc == SPARKATTN_OK) rc = check_rows(out, true);
   if (rc == SPARKATTN_OK) rc = check_pools(cache, batch, k_cache, v_cache, k_scale, v_scale, workspace);
   if (rc != SPARKATTN_OK) return rc;
-  if (frame_tokens < 0 || window_frames < 0 || (frame_tokens == 0 && window_frames != 0)) return SPARKATTN_E_INVALID_ARG;
+  if (frame_tokens < 0 || window_frames < 0 || sink_tokens < 0 || (frame_tokens == 0 && window_frames != 0)) return SPARKATTN_E_INVALID_ARG;
   if (!(softmax_scale >= 0.0f) || isinf(softmax_scale)) return SPARKATTN_E_INVALID_ARG;
   if (workspace_bytes < cache_fwd_workspace_bytes(*cache, *batch, H)) return SPARKATTN_E_WORKSPACE_TOO_SMALL;
-  return launch_cache_fwd(*cache, *batch, *q, H, k_cache, v_cache, k_scale, v_scale, frame_tokens, window_frames, softmax_scale, *out, lse,
-                          workspace, static_cast<cudaStream_t>(cuda_stream));
+  return launch_cache_fwd(*cache, *batch, *q, H, k_cache, v_cache, k_scale, v_scale, frame_tokens, window_frames, sink_tokens, softmax_scale, *out,
+                          lse, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
 }  // extern "C"

@@ -42,6 +42,7 @@ struct Library {
   decltype(&sparkattn_cache_workspace_bytes) cache_workspace_bytes;
   decltype(&sparkattn_cache_append) cache_append;
   decltype(&sparkattn_cache_fwd) cache_fwd;
+  decltype(&sparkattn_cache_fwd_sink) cache_fwd_sink;
 };
 Library g_lib{};
 
@@ -568,15 +569,15 @@ PyObject* cache_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// cache_fwd(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, q, frame_tokens, window, softmax_scale, out, return_lse,
-// workspace, stream) -> rc, out, lse, workspace
+// cache_fwd(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, q, frame_tokens, window, sink, softmax_scale, out,
+// return_lse, workspace, stream) -> rc, out, lse, workspace
 PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Args a(argv, n);
-  a.expect(16);
+  a.expect(17);
   Cache cache(a);
   const at::Tensor q = a.tensor();
-  const int32_t frame_tokens = a.i32(), window = a.i32();
+  const int32_t frame_tokens = a.i32(), window = a.i32(), sink = a.i32();
   const float softmax_scale = a.number();
   at::Tensor out = a.optional_tensor(), lse;
   const bool return_lse = a.truth();
@@ -597,8 +598,8 @@ PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
       ws = stream.scratch((int64_t)(bytes < 256 ? 256 : bytes), q);      // an unsupported call says why itself
     }
     cache.check_workspace(ws);
-    rc = g_lib.cache_fwd(&cache.c, &cache.b, &rq, H, ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), frame_tokens, window,
-                         softmax_scale, &ro, fptr(lse), ptr(ws), (size_t)ws.numel(), stream);
+    rc = g_lib.cache_fwd_sink(&cache.c, &cache.b, &rq, H, ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), frame_tokens, window,
+                              sink, softmax_scale, &ro, fptr(lse), ptr(ws), (size_t)ws.numel(), stream);
   }
   return result(rc, {out, lse, ws});
   END_HANDLE_TH_ERRORS

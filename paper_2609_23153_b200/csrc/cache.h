@@ -47,10 +47,12 @@ __device__ __forceinline__ Sequence sequence_of(const BatchView& v, int b) {
   return s;
 }
 
-// [lo, hi) of the keys that the token at position pos of a sequence of len tokens sees
+// [lo, hi) of the keys that the token at position pos of a sequence of len tokens sees; in kernels with SINK those of its window, in
+// front of which it sees the first `sink` keys
 struct Causal {
   int frame, window;      // frame 0: every key; window 0: from the first key on
   FastDiv by_frame;
+  int sink;               // more than 0 only where there is a window
 };
 __device__ __forceinline__ int2 visible_keys(const Causal& c, int pos, int len) {
   if (c.frame == 0) return make_int2(0, len);
@@ -61,10 +63,16 @@ __device__ __forceinline__ int2 visible_keys(const Causal& c, int pos, int len) 
   return make_int2((int)min(lo, (long long)len), (int)min(hi, (long long)len));
 }
 
+template <bool SINK>
+__device__ __forceinline__ bool sees(const Causal& c, int2 seen, int key) {
+  return key < seen.y && (key >= seen.x || (SINK && key < c.sink));
+}
+
 // One CTA looks through the numbers a call was given and leaves the status word: nobody else writes it but a wait that has run
-// out, seconds later, so that nothing has to be cleared in front.  first, last: pages of the sequence that the call reaches.
+// out, seconds later, so that nothing has to be cleared in front.  reach: pages of the sequence that the call reaches, from the
+// first to behind the last; and those of the first `sink` tokens.
 template <typename Reach>
-__device__ __forceinline__ void check_batch(const BatchView& v, int* s_bad /* [2], shared */, Reach reach) {
+__device__ __forceinline__ void check_batch(const BatchView& v, int* s_bad /* [2], shared */, Reach reach, int sink = 0) {
   if (threadIdx.x == 0) { s_bad[0] = 0; s_bad[1] = 0; }
   __syncthreads();
   auto bad = [&](int detail) { if (atomicExch(s_bad, 1) == 0) s_bad[1] = detail; };
@@ -85,10 +93,15 @@ __device__ __forceinline__ void check_batch(const BatchView& v, int* s_bad /* [2
     const int2 pages = reach(s);
     const int32_t* row = v.page_table + (int64_t)b * v.max_pages;
     const int last = min(pages.y, v.max_pages);
-    for (int i = pages.x + lane; i < last; i += lanes * 8) {
+    // (the first tokens' pages stand in front of the others, `gap` pages nearer to them than they are)
+    const int front = sink > 0 ? min(((sink - 1) >> v.page_shift) + 1, pages.x) : 0, gap = pages.x - front;
+    for (int i = pages.x - front + lane; i < last; i += lanes * 8) {
       int page[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) page[u] = i + lanes * u < last ? row[i + lanes * u] : 0;
+      for (int u = 0; u < 8; ++u) {
+        const int at = i + lanes * u;
+        page[u] = at < last ? row[at < pages.x ? at - gap : at] : 0;
+      }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
         if ((uint32_t)page[u] >= (uint32_t)v.pages) bad(page[u]);

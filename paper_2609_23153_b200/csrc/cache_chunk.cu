@@ -68,13 +68,13 @@ __device__ __forceinline__ float logit_factor(float row, float key) {
   return c;
 }
 
-template <int D, bool FP8, bool SPLIT>
+template <int D, bool FP8, bool SPLIT, bool SINK>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                    const __grid_constant__ CacheFwdParams p) {
   using C = ChunkShape<D, FP8>;
   constexpr int R = SPLIT ? 128 : 256;
-  using L = Line<R, kChunkKeys, kChunkOver>;
+  using L = Line<R, kChunkKeys, kChunkOver, SINK>;
   constexpr int kSlab = kChunkKeys * 128;                    // bytes of 64 16-bit channels, or of 128 codes
   constexpr int RK = C::RK, RV = C::RV;
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -133,11 +133,11 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
   const int total = s_prefix[p.batch.B], share = L::share_of(p, total);
-  if (blockIdx.x == 0) check_call(p, s_bad);
+  if (blockIdx.x == 0) check_call<SINK>(p, s_bad);
   const long long begin = (long long)((int)blockIdx.x - 1) * share;
   const bool works = blockIdx.x > 0 && begin < total;
   const int x0 = works ? (int)begin : 0, x1 = works ? (int)min(begin + share, (long long)total) : 0;
-  Stretch<R, kChunkKeys, kChunkOver> g;
+  Stretch<R, kChunkKeys, kChunkOver, SINK> g;
   if (works) g.begin(p, s_prefix, x0, x1);
   if (blockIdx.x > 0 && threadIdx.x == 0) note_border(p, (int)blockIdx.x - 1, works, share, g);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // tiles go where the line's beginnings lie
@@ -159,9 +159,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         live = g.next(p);
         t_next = g.t0;
       }
-      b = {t_next, live ? min(kBatch, g.t1 - t_next) : 0, g.c.h, -1, 1.0f, 1.0f};
-      const int key = b.t * kChunkKeys + lane * 16;
-      if (lane / kChunkGroups < b.n && key < g.c.item.hi && key + 16 > g.c.item.lo)
+      b = {t_next, live ? min(kBatch, g.t1 - t_next) : 0, g.c.h, 0, -1, 1.0f, 1.0f};
+      const int key = SINK ? g.c.item.tile_of(b.t + lane / kChunkGroups) * kChunkKeys + lane % kChunkGroups * 16 : b.t * kChunkKeys + lane * 16;
+      if constexpr (SINK) b.key = key;
+      if (lane / kChunkGroups < b.n && key < g.c.item.hi && (key + 16 > g.c.item.lo || (SINK && key < p.causal.sink)))
         b.page = p.batch.page_table[(int64_t)g.c.b * p.batch.max_pages + (key >> p.batch.page_shift)];
       t_next += b.n;
     };
@@ -179,7 +180,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (per_box > 4) page = max(page, __shfl_xor_sync(0xffffffffu, page, 4));
       const bool copies = page >= 0 && lane % per_box == 0;
       const uint32_t going = __ballot_sync(0xffffffffu, copies);
-      const int key = now.t * kChunkKeys + lane * 16, row = key & ((1 << p.batch.page_shift) - 1), at_row = (lane % kChunkGroups) * 16;
+      const int key = SINK ? now.key : now.t * kChunkKeys + lane * 16, row = key & ((1 << p.batch.page_shift) - 1), at_row = (lane % kChunkGroups) * 16;
       const GroupInfo info = info_of<FP8>(now);
       ask_scales<FP8>(p, next);
       ask_pages(after);
@@ -345,7 +346,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const int all_hi = visible_keys(p.causal, g.c.seq.first_pos() + fast_div(g.row0, p.by_G), g.c.seq.len).y;
       const bool parts = all_lo > g.c.item.lo || all_hi < g.c.item.hi;
       for (int t = g.t0; ok && t < g.t1; ++t, ++n) {
-        const int key0 = t * kChunkKeys;
+        const int key0 = g.c.item.tile_of(t) * kChunkKeys;
         const GroupInfo* info = s_info + (n & (kChunkInfoRing - 1)) * kChunkGroups;
         if constexpr (C::kConvK) {
           ok = __all_sync(0xffffffffu, pipe_wait(rawk_full, n & 1, s_abort, 8));
@@ -360,7 +361,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         ok = __all_sync(0xffffffffu, pipe_wait(raw_full + slot, (n / RV) & 1, s_abort, 9));
         if (FP8 && ok && n >= RV) ok = __all_sync(0xffffffffu, pipe_wait(v_free + slot, (n / RV - 1) & 1, s_abort, 11));
         if (!ok) break;
-        const bool edge = key0 < all_lo || key0 + kChunkKeys > all_hi || __any_sync(0xffffffffu, lane < kChunkGroups && !info[lane % kChunkGroups].usable);
+        const bool edge = (key0 < all_lo && !(SINK && key0 + kChunkKeys <= p.causal.sink)) || key0 + kChunkKeys > all_hi || __any_sync(0xffffffffu, lane < kChunkGroups && !info[lane % kChunkGroups].usable);
         if (edge) {
           // V's words: zeros for keys that nobody sees; and see Marks.  (E4M3: every thread what it converts next)
           constexpr int kPer = FP8 ? 16 : 8, kLanes = FP8 ? D / 16 : 1, kRowsAtOnce = 128 / kLanes, kChunks = FP8 ? 1 : D / 8;      // 16-byte chunks
@@ -369,7 +370,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           for (int i = 0; i < kChunkKeys / kRowsAtOnce * kChunks; ++i) {
             const int r = i / kChunks * kRowsAtOnce + tid / kLanes, c = FP8 ? tid % kLanes : i % kChunks;
             uint4* chunk = reinterpret_cast<uint4*>(tile + (FP8 && D == 64 ? r * 64 + ((c ^ ((r >> 1) & 3)) << 4) : (c >> 3) * kSlab + r * 128 + (((c & 7) ^ (r & 7)) << 4)));
-            if (key0 + r < g.c.item.lo || key0 + r >= g.c.item.hi || !info[r / 16].usable) {
+            if (!sees<SINK>(p.causal, make_int2(g.c.item.lo, g.c.item.hi), key0 + r) || !info[r / 16].usable) {
               *chunk = make_uint4(0u, 0u, 0u, 0u);
             } else if (parts) {
               const uint4 x = *chunk;
@@ -378,7 +379,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll 1
                 for (int j = 0; j < 4; ++j)
                   if (word_not_finite<FP8>(word[j]))
-                    word[j] = mark_word<D, R, FP8>(p, marks, segment, g.c.seq, g.row0, g.rows, key0 + r, c * kPer + j * (kPer / 4), word[j]);
+                    word[j] = mark_word<D, R, FP8, SINK>(p, marks, segment, g.c.seq, g.row0, g.rows, key0 + r, c * kPer + j * (kPer / 4), word[j]);
               }
             }
           }
@@ -597,8 +598,9 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
         for (int ch = 0; ch < kChunkKeys / 32; ++ch) tmem_ld32(tS + ch * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[ch * 32]));
         const GroupInfo* info = s_info + ((n + i) & (kChunkInfoRing - 1)) * kChunkGroups;
-        const int c_lo = seen.x - (g.t0 + i) * kChunkKeys, c_hi = seen.y - (g.t0 + i) * kChunkKeys;
-        bool masked = c_lo > 0 || c_hi < kChunkKeys;
+        const int key0 = g.c.item.tile_of(g.t0 + i) * kChunkKeys, c_lo = seen.x - key0, c_hi = seen.y - key0;
+        const int c_sink = SINK ? p.causal.sink - key0 : 0;
+        bool masked = (c_lo > 0 && !(SINK && c_sink >= kChunkKeys)) || c_hi < kChunkKeys;
         if (lane < kChunkGroups) masked = masked || !info[lane].usable;
         masked = __any_sync(0xffffffffu, masked);
         tc_wait_ld();
@@ -606,7 +608,9 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           auto below = [](int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; };
 #pragma unroll
           for (int ch = 0; ch < kChunkKeys / 32; ++ch) {
-            uint32_t keep = below(c_hi - ch * 32) & ~below(c_lo - ch * 32);
+            uint32_t keep = ~below(c_lo - ch * 32);
+            if constexpr (SINK) keep |= below(c_sink - ch * 32);
+            keep &= below(c_hi - ch * 32);
             if (!info[2 * ch].usable) keep &= 0xffff0000u;
             if (!info[2 * ch + 1].usable) keep &= 0x0000ffffu;
             if (keep != 0xffffffffu) {
@@ -734,7 +738,7 @@ static int launch_chunk(const sparkattn_cache_t& c, CacheFwdParams& p, const voi
   if ((rc = make_page_map(&mv, v_cache, FP8 ? 1 : 2, c, p.box_rows)) != SPARKATTN_OK) return rc;
   constexpr int smem = C::kFixed + Marks<D, R, FP8>::kBytes;
   static_assert(smem <= 232448 && (kCacheMaxSequences + 1) * 4 <= 2 * C::kQ, "fits an SM");
-  auto kern = cache_chunk_kernel<D, FP8, SPLIT>;
+  auto kern = p.causal.sink > 0 ? cache_chunk_kernel<D, FP8, SPLIT, true> : cache_chunk_kernel<D, FP8, SPLIT, false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kChunkThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
   return launch_kernel(combine_kernel<D, R>, dim3(p.workers - 1, R / 16), kCombineThreads, 0, true, stream, p);

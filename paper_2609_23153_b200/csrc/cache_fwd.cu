@@ -106,7 +106,7 @@ struct DecodeShape {
 
 // Some rows see some of a warp's keys of a tile and others do not: see Marks.  A lane looks at the words of V that it loads next.  (A
 // function of its own: in the tile loop its code cost the smallest call 0.7 us.)
-template <int D, bool FP8, int NT>
+template <int D, bool FP8, int NT, bool SINK>
 __device__ __noinline__ void mark_tile(const CacheFwdParams& p, const Marks<D, 8 * NT, FP8> marks, int set, const Sequence seq, int row0, int rows, int2 seen,
                                        int key0, int tile_row0, int usable, unsigned char* tile) {
   using S = DecodeShape<D, FP8, NT>;
@@ -117,15 +117,15 @@ __device__ __noinline__ void mark_tile(const CacheFwdParams& p, const Marks<D, 8
     const int u = i / kVWords >> 2, in = u * kGroupKeys + 4 * t4 + (i / kVWords & 3), key = key0 + in, channel = g8 * (D / 8) + i % kVWords * (4 / S::kElt);
     const uint32_t at = chunk_offset<S::kRowBytes, S::kTileKeys>(tile_row0 + in, channel * S::kElt / 16) + channel * S::kElt % 16;
     uint32_t* word = reinterpret_cast<uint32_t*>(tile + at);
-    if (key >= seen.x && key < seen.y && (usable >> u & 1) && word_not_finite<FP8>(*word))
-      *word = mark_word<D, S::R, FP8>(p, marks, set, seq, row0, rows, key, channel, *word);
+    if (sees<SINK>(p.causal, seen, key) && (usable >> u & 1) && word_not_finite<FP8>(*word))
+      *word = mark_word<D, S::R, FP8, SINK>(p, marks, set, seq, row0, rows, key, channel, *word);
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the tile is released to the next copy
 }
 
 // CLUSTER: an item (it has one row tile) belongs to a cluster of CTAs, each takes an equal run of its key tiles, and the CTAs' results
 // are added up through distributed shared memory.  Otherwise the line, see cache_line.cuh; cluster_of has the rule.
-template <int D, bool FP8, int NT, bool CLUSTER>
+template <int D, bool FP8, int NT, bool CLUSTER, bool SINK>
 __global__ void __launch_bounds__(kDecodeThreads, kDecodePerSM)
 cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                     const __grid_constant__ CacheFwdParams p) {
@@ -158,22 +158,22 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
   }
   marks.clear_all();
   pdl_wait();
-  Stretch<R, kTileKeys, kDecodeOver> g;
+  Stretch<R, kTileKeys, kDecodeOver, SINK> g;
   int worker = 0;
   if constexpr (CLUSTER) {
     __syncthreads();
     const int cluster = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x - cluster * p.cluster;
     if (cluster == 0) {
-      if (rank == 0) check_call(p, s_bad);
+      if (rank == 0) check_call<SINK>(p, s_bad);
       return;
     }
     const int b = fast_div(cluster - 1, p.by_Hk);
     if (!g.run_of(p, b, cluster - 1 - b * p.Hk, rank, p.cluster)) return;
   } else {
-  Line<R, kTileKeys, kDecodeOver>::lay_out(p, s_prefix, s_warp);
-  const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys, kDecodeOver>::share_of(p, total);
+  Line<R, kTileKeys, kDecodeOver, SINK>::lay_out(p, s_prefix, s_warp);
+  const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys, kDecodeOver, SINK>::share_of(p, total);
   if (blockIdx.x == 0) {
-    check_call(p, s_bad);
+    check_call<SINK>(p, s_bad);
     return;
   }
   worker = blockIdx.x - 1;
@@ -197,12 +197,13 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         live = g.next(p);
         t_next = g.t0;
       }
-      GroupBatch b{t_next, 0, 0, -1, 1.0f, 1.0f};
+      GroupBatch b{t_next, 0, 0, 0, -1, 1.0f, 1.0f};
       if (!live) return b;
       b.n = min(kBatch, g.t1 - b.t);
       b.h = g.c.h;
-      const int key = b.t * kTileKeys + lane * kGroupKeys;
-      if (lane / kGroups < b.n && key < g.c.item.hi && key + kGroupKeys > g.c.item.lo)
+      const int key = SINK ? g.c.item.tile_of(b.t + lane / kGroups) * kTileKeys + lane % kGroups * kGroupKeys : b.t * kTileKeys + lane * kGroupKeys;
+      if constexpr (SINK) b.key = key;
+      if (lane / kGroups < b.n && key < g.c.item.hi && (key + kGroupKeys > g.c.item.lo || (SINK && key < p.causal.sink)))
         b.page = p.batch.page_table[(int64_t)g.c.b * p.batch.max_pages + (key >> p.batch.page_shift)];
       t_next += b.n;
       return b;
@@ -220,7 +221,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       if (per_box > 4) page = max(page, __shfl_xor_sync(0xffffffffu, page, 4));
       const bool copies = page >= 0 && lane % per_box == 0;
       const uint32_t going = __ballot_sync(0xffffffffu, copies);
-      const int key = now.t * kTileKeys + lane * kGroupKeys, row = key & ((1 << p.batch.page_shift) - 1);
+      const int key = SINK ? now.key : now.t * kTileKeys + lane * kGroupKeys, row = key & ((1 << p.batch.page_shift) - 1);
       // (a copy may finish before the barrier has been told to expect it: the phase is not over without that arrival)
       auto copy = [&](int u, int kv, int slot) {
         if (lane / kGroups == u && copies) {
@@ -409,8 +410,8 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           }
         }
         // t = logit + log2(v scale); keys a row does not see get -inf
-        const int key0 = t * kTileKeys + row0;
-        bool edge = key0 < all_lo || key0 + kPerWarp * kGroupKeys > all_hi;
+        const int key0 = g.c.item.tile_of(t) * kTileKeys + row0;
+        bool edge = (key0 < all_lo && !(SINK && key0 + kPerWarp * kGroupKeys <= p.causal.sink)) || key0 + kPerWarp * kGroupKeys > all_hi;
 #pragma unroll
         for (int u = 0; u < kPerWarp; ++u) {
           edge = edge || !info[u].usable;
@@ -427,7 +428,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const int key = key0 + u * kGroupKeys + 4 * (g8 >> 1) + (g8 & 1) + (i & 2);
-                if (key < lo[nt][i & 1] || key >= hi[nt][i & 1] || !info[u].usable) s[u][nt][i] = -INFINITY;
+                if ((key < lo[nt][i & 1] && !(SINK && key < p.causal.sink)) || key >= hi[nt][i & 1] || !info[u].usable) s[u][nt][i] = -INFINITY;
               }
         }
         float top[NT][2];
@@ -500,7 +501,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         if (!ok) break;
         const uint32_t s_v = smem_u32(smem + slot * S::kTileBytes);
         if (edge && (all_lo > g.c.item.lo || all_hi < g.c.item.hi))
-          mark_tile<D, FP8, NT>(p, marks, segments, g.c.seq, g.row0, g.rows, make_int2(g.c.item.lo, g.c.item.hi), key0, row0,
+          mark_tile<D, FP8, NT, SINK>(p, marks, segments, g.c.seq, g.row0, g.rows, make_int2(g.c.item.lo, g.c.item.hi), key0, row0,
                                 info[0].usable | info[kPerWarp - 1].usable << 1, smem + slot * S::kTileBytes);
         uint32_t vw[kPerWarp][4][kVWords];
 #pragma unroll
@@ -526,7 +527,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int key = key0 + u * kGroupKeys + 4 * t4 + i;
-              if (key < g.c.item.lo || key >= g.c.item.hi || !info[u].usable) {
+              if (!sees<SINK>(p.causal, make_int2(g.c.item.lo, g.c.item.hi), key) || !info[u].usable) {
 #pragma unroll
                 for (int w = 0; w < kVWords; ++w) vw[u][i][w] = 0u;
               }
@@ -695,10 +696,10 @@ constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 //   93.0 / one CTA 105 (169 / 150).
 //   Lengths are known on the device only: the table's width stands for them, and one sequence of 1000 keys under a table of 131,072 takes the
 //   line (9.8 us; under its own width a cluster, 6.2).  Sixteen CTAs take eight SMs of one GPC: 148 SMs in eight GPCs always leave one with that many.
-int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame_tokens, int window, int tile_keys, int sms) {
+int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame_tokens, int window, int sink, int tile_keys, int sms) {
   const long long items = (long long)b.B * c.H;
   long long keys = (long long)b.max_pages * c.page;                       // that an item may have
-  if (window > 0) keys = std::min(keys, ((long long)window + 1) * frame_tokens + b.max_new);
+  if (window > 0) keys = std::min(keys, ((long long)window + 1) * frame_tokens + b.max_new + sink);
   const long long tiles = (keys + tile_keys - 1) / tile_keys;
   int n = items * 16 <= sms ? 16 : 8;
   while (n > 1 && (items * n > std::max(2 * sms, 16) || n / 2 >= tiles)) n /= 2;
@@ -751,7 +752,7 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   if ((rc = make_page_map(&mk, k_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
   if ((rc = make_page_map(&mv, v_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
   const long long items = (long long)b.B * c.H;
-  p.cluster = cluster_of(c, b, p.causal.frame, p.causal.window, S::kTileKeys, p.workers / kDecodePerSM);
+  p.cluster = cluster_of(c, b, p.causal.frame, p.causal.window, p.causal.sink, S::kTileKeys, p.workers / kDecodePerSM);
   const bool cluster = p.cluster > 0;
   // as deep a ring as the CTAs of an SM leave each other, sixteen tiles at most; fewer CTAs where a great many sequences leave no room
   const int listed = cluster ? 0 : b.B;
@@ -762,7 +763,8 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   if (p.slots > 16) p.slots = 16;
   if (p.slots < 3) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   const int smem = p.slots * S::kTileBytes + S::fixed_bytes(listed, p.slots);
-  auto kern = cluster ? cache_decode_kernel<D, FP8, NT, true> : cache_decode_kernel<D, FP8, NT, false>;
+  auto kern = p.causal.sink > 0 ? cluster ? cache_decode_kernel<D, FP8, NT, true, true> : cache_decode_kernel<D, FP8, NT, false, true>
+                                : cluster ? cache_decode_kernel<D, FP8, NT, true, false> : cache_decode_kernel<D, FP8, NT, false, false>;
   // (the kernel's, not the call's: the most that any call asks for, since host threads with other batches set it too)
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemOfSM - 1024) != cudaSuccess) return SPARKATTN_E_CUDA;
   if (cluster) {
@@ -774,11 +776,11 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
 }
 
 int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rows_t& q, int H, const void* k_cache,
-                     const void* v_cache, const float* k_scale, const float* v_scale, int frame_tokens, int window, float softmax_scale,
+                     const void* v_cache, const float* k_scale, const float* v_scale, int frame_tokens, int window, int sink, float softmax_scale,
                      const sparkattn_rows_t& out, float* lse, void* workspace, cudaStream_t stream) {
   CacheFwdParams p{};
   p.batch = make_batch_view(c, b);
-  p.causal = {frame_tokens, window, make_fast_div(std::max(frame_tokens, 1))};
+  p.causal = {frame_tokens, window, make_fast_div(std::max(frame_tokens, 1)), window > 0 ? sink : 0};
   p.q = static_cast<const __nv_bfloat16*>(q.data);
   p.out = static_cast<__nv_bfloat16*>(out.data);
   p.q_stride_t = q.stride_t; p.q_stride_h = q.stride_h;

@@ -8,6 +8,8 @@
 // Stretch w is units [w * share, (w + 1) * share).  What a stretch holds of an item is a segment; an item that lies in one
 // stretch is finished there, the others leave partial results that combine_kernel adds up in the line's order.
 // Items stand in the order (sequence, key head, row tile).
+// SINK: an item's rows also see the sequence's first tokens.  The tiles of these stand in front of the window's in the item's run of tiles, with
+// the numbers right below theirs (Item::tile_of), so that everything that counts tiles counts on; the keys between take no part.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -63,12 +65,15 @@ struct GroupInfo {
   int usable;        // somebody sees keys of it, and the page exists
 };
 
-template <int R, int TK, int OVER>
+template <int R, int TK, int OVER, bool SINK>
 struct Line {
   struct Item {
-    int first, tiles;            // key tiles, counted from the front of the sequence
-    int lo, hi;                  // keys that any of its rows sees
+    int first, tiles;            // key tiles, counted from the front of the sequence (SINK: see tile_of)
+    int lo, hi;                  // keys that any of its rows sees (SINK: besides the first ones)
+    int window;                  // SINK: the window's first tile
     __device__ __forceinline__ int units() const { return tiles + OVER; }
+    // where tile number t lies in the sequence
+    __device__ __forceinline__ int tile_of(int t) const { return SINK && t < window ? t - first : t; }
   };
   static __device__ __forceinline__ int row_tiles(const CacheFwdParams& p, const Sequence& s) { return (s.n * p.G + R - 1) / R; }
   static __device__ __forceinline__ Item item_of(const CacheFwdParams& p, const Sequence& s, int rt) {
@@ -78,6 +83,12 @@ struct Line {
     it.hi = visible_keys(p.causal, s.first_pos() + fast_div(last_row, p.by_G), s.len).y;
     it.first = it.lo / TK;
     it.tiles = max((it.hi + TK - 1) / TK - it.first, 1);
+    if constexpr (SINK) {
+      it.window = it.first;
+      const int front = min((p.causal.sink - 1) / TK + 1, it.first);
+      it.first -= front;
+      it.tiles += front;
+    }
     return it;
   }
   // units of the row tiles of one key head
@@ -180,12 +191,12 @@ struct Line {
 };
 
 // A stretch of the line, taken segment by segment.
-template <int R, int TK, int OVER>
+template <int R, int TK, int OVER, bool SINK>
 struct Stretch {
-  using L = Line<R, TK, OVER>;
+  using L = Line<R, TK, OVER, SINK>;
   typename L::Place c;
   int x, end;
-  int t0, t1;                    // the segment's key tiles, counted from the front of the sequence (none, where it is all beginning)
+  int t0, t1;                    // the segment's key tiles, numbered as the item's (none, where it is all beginning)
   int row0, rows;                // its rows
   bool whole, first;             // the item lies in this stretch; the stretch's first segment
   __device__ __forceinline__ void begin(const CacheFwdParams& p, const int* prefix, int from, int to) {
@@ -268,6 +279,7 @@ __device__ __forceinline__ void split_queries(uint32_t x, uint32_t y, float to, 
 // A batch of tiles as the copying warp asks for it: every lane looks after one group of 16 keys, its page and its scales.
 struct GroupBatch {
   int t, n, h;                   // first tile, tiles; key head
+  int key;                       // SINK: the group's first
   int page;                      // of the lane's group, -1: nobody sees it, or there is no such page
   float k_scale, v_scale;
 };
@@ -328,7 +340,7 @@ __device__ __forceinline__ bool word_not_finite(uint32_t w) {
 }
 // Such a word of key `key`, channels from `channel` on: its values that are not finite are marked for the rows that see the key, and
 // become zeros.  (Inlined, and in loops that stay loops: the operand warps have few registers, and no call may take more.)
-template <int D, int R, bool FP8>
+template <int D, int R, bool FP8, bool SINK>
 __device__ __forceinline__ uint32_t mark_word(const CacheFwdParams& p, const Marks<D, R, FP8> marks, int set, const Sequence seq, int row0, int rows, int key,
                                            int channel, uint32_t w) {
   constexpr int kPer = FP8 ? 4 : 2, kBits = 32 / kPer;
@@ -346,7 +358,7 @@ __device__ __forceinline__ uint32_t mark_word(const CacheFwdParams& p, const Mar
 #pragma unroll 1
   for (int r = 0; r < rows; ++r) {
     const int2 seen = visible_keys(p.causal, seq.first_pos() + fast_div(row0 + r, p.by_G), seq.len);
-    if (key < seen.x || key >= seen.y) continue;
+    if (!sees<SINK>(p.causal, seen, key)) continue;
     uint32_t* to = marks.row(set, r) + channel / 32;
     if (up) atomicOr(to, up);
     if (!FP8 && down) atomicOr(to + (Marks<D, R, FP8>::kSigns - 1) * Marks<D, R, FP8>::kWords, down);
@@ -356,16 +368,17 @@ __device__ __forceinline__ uint32_t mark_word(const CacheFwdParams& p, const Mar
 }
 
 // the status of a call: the first CTA's work
+template <bool SINK>
 __device__ __forceinline__ void check_call(const CacheFwdParams& p, int* s_bad) {
   check_batch(p.batch, s_bad, [&](const Sequence& s) {
     if (s.n == 0) return make_int2(0, 0);
     const int lo = visible_keys(p.causal, s.first_pos(), s.len).x, hi = visible_keys(p.causal, s.len - 1, s.len).y;
     return make_int2(lo >> p.batch.page_shift, (hi + (1 << p.batch.page_shift) - 1) >> p.batch.page_shift);
-  });
+  }, SINK ? p.causal.sink : 0);
   leave_status(p.status, s_bad);
 }
-template <int R, int TK, int OVER>
-__device__ __forceinline__ void note_border(const CacheFwdParams& p, int worker, bool works, int share, const Stretch<R, TK, OVER>& g) {
+template <int R, int TK, int OVER, bool SINK>
+__device__ __forceinline__ void note_border(const CacheFwdParams& p, int worker, bool works, int share, const Stretch<R, TK, OVER, SINK>& g) {
   Border b{};
   if (works) b = {g.c.at, g.c.item.units(), share, g.c.seq.start, g.row0, g.rows, g.c.h, 0};
   reinterpret_cast<int4*>(p.borders + worker)[0] = reinterpret_cast<const int4*>(&b)[0];

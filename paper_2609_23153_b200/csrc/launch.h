@@ -115,7 +115,7 @@ int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, 
 bool cache_work_fits(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);
 size_t cache_fwd_workspace_bytes(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);
 int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rows_t& q, int H, const void* k_cache,
-                     const void* v_cache, const float* k_scale, const float* v_scale, int frame_tokens, int window, float softmax_scale,
+                     const void* v_cache, const float* k_scale, const float* v_scale, int frame_tokens, int window, int sink, float softmax_scale,
                      const sparkattn_rows_t& out, float* lse, void* workspace, cudaStream_t stream);
 
 }  // namespace sparkattn
