@@ -63,7 +63,7 @@ typedef enum {
   SPARKATTN_E_NO_DEVICE = -8          /* no CUDA device / driver entry point unavailable               */
 } sparkattn_status;
 
-typedef enum { SPARKATTN_BF16 = 0, SPARKATTN_FP8_E4M3 = 1 } sparkattn_dtype;
+typedef enum { SPARKATTN_BF16 = 0, SPARKATTN_FP8_E4M3 = 1, SPARKATTN_FP32 = 2 /* weights of norms only */ } sparkattn_dtype;
 
 /* Problem shape.  Caller fills it; the library reads it during the call only. */
 typedef struct {
@@ -465,6 +465,20 @@ typedef struct {
   const int32_t* axis;       /* [rot/2], entries in [0, axes); NULL: all 0                    */
 } sparkattn_rotary_t;
 
+/* RMS norm over the d channels of each head, in front of the rotation:  y_c = x_c / sqrt(mean(x^2) + eps) * weight_c.
+ * fp32 throughout (squares, their sum, the root, both products), no rounding between norm and rotation.  A row whose sum of squares passes
+ * fp32's range, which takes entries of 1e18, comes out as zeros; one with an infinity or a NaN gives NaN there. */
+typedef struct {
+  uint32_t struct_size;   /* sizeof(sparkattn_norm_t)                                         */
+  uint32_t version;       /* SPARKATTN_VERSION                                                */
+  int32_t weight_dtype;   /* SPARKATTN_BF16 or SPARKATTN_FP32                                 */
+  int32_t per_head;       /* 0: weights [d], shared by the heads; 1: [heads, d] contiguous    */
+  float eps;              /* > 0                                                              */
+  uint32_t pad;           /* must be 0                                                        */
+  const void* q_weight;   /* 16-byte aligned, or NULL: ones                                   */
+  const void* k_weight;
+} sparkattn_norm_t;
+
 /* Bytes of device workspace that sparkattn_cache_fwd needs for H query heads (0: unsupported arguments);
  * sparkattn_cache_append needs 256. */
 size_t sparkattn_cache_workspace_bytes(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, int32_t H);
@@ -488,6 +502,28 @@ int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch
                            const sparkattn_rows_t* q, int32_t H, const sparkattn_rows_t* k, const sparkattn_rows_t* v,
                            void* k_cache, void* v_cache, float* k_scale, float* v_scale, const sparkattn_rows_t* q_out,
                            void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The same with the norm of keys and queries (not of values) in front of their rotation.  norm: NULL is sparkattn_cache_append. */
+int sparkattn_cache_append_norm(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_norm_t* norm,
+                                const sparkattn_rotary_t* rotary, const sparkattn_rows_t* q, int32_t H, const sparkattn_rows_t* k,
+                                const sparkattn_rows_t* v, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                                const sparkattn_rows_t* q_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Norm and rotation of the queries and keys of whole sequences, in front of sparkattn_select, sparkattn_quant_fp8 and sparkattn_fwd,
+ * which take them as the model's normalisation left them.  One launch; every row is read and written once.
+ * q, k       : in,  bf16 [B, H, N, d]; B, N and d are the same, the heads may differ.  k_shape, k, k_out_shape, k_out NULL: queries alone
+ * q_out, k_out : out, the same sizes with the strides of their own shape; may be q and k themselves with their strides, and overlap the inputs in
+ *              no other way
+ * norm, rotary : either may be NULL, not both.  Positions are [N, axes], the same for every sample; NULL: the token's index
+ * workspace  : >= 256 bytes, 256-byte aligned; the status word: SPARKATTN_E_BAD_INDEX for a position or axis outside the tables, whose pairs
+ *              are left unrotated
+ * `block` and `softmax_scale` of the shapes are validated, not used.
+ */
+int sparkattn_norm_rotate(const sparkattn_shape_t* q_shape, const void* q, const sparkattn_shape_t* q_out_shape, void* q_out,
+                          const sparkattn_shape_t* k_shape, const void* k, const sparkattn_shape_t* k_out_shape, void* k_out,
+                          const sparkattn_norm_t* norm, const sparkattn_rotary_t* rotary, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream);
 
 /*
  * Softmax attention of the new tokens over the cache.  For the token at position i of its sequence and query head h, over

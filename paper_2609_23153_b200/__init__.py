@@ -34,6 +34,7 @@ E_NO_DEVICE = -8
 
 BF16 = 0
 FP8_E4M3 = 1
+FP32 = 2
 
 EXPORTS = (
     "sparkattn_version", "sparkattn_status_string", "sparkattn_workspace_bytes", "sparkattn_select",
@@ -44,6 +45,7 @@ EXPORTS = (
     "sparkattn_brick_layout", "sparkattn_gather_tokens", "sparkattn_select_padded", "sparkattn_fwd_padded",
     "sparkattn_quant_fp8_pooled", "sparkattn_select_pooled", "sparkattn_fwd_gated_workspace_bytes", "sparkattn_fwd_gated",
     "sparkattn_cache_workspace_bytes", "sparkattn_cache_append", "sparkattn_cache_fwd", "sparkattn_cache_fwd_sink",
+    "sparkattn_cache_append_norm", "sparkattn_norm_rotate",
 )
 
 
@@ -94,6 +96,15 @@ class RotaryShape(ctypes.Structure):
     ]
 
 
+class NormShape(ctypes.Structure):
+    """Mirror of ``sparkattn_norm_t``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("version", ctypes.c_uint32),
+        ("weight_dtype", ctypes.c_int32), ("per_head", ctypes.c_int32), ("eps", ctypes.c_float), ("pad", ctypes.c_uint32),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+    ]
+
+
 class SparkAttnError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -104,7 +115,7 @@ class SparkAttnError(RuntimeError):
 _BOUND = ("workspace_bytes", "select", "select_window", "select_padded", "select_pooled", "quant_fp8", "quant_fp8_pooled",
           "quant_fp8_per_token", "fwd", "fwd_window", "fwd_padded", "gather_tokens", "comp_workspace_bytes", "comp_state", "comp_apply",
           "fwd_gated_workspace_bytes", "fwd_gated", "cache_workspace_bytes", "cache_append", "cache_fwd",
-          "cache_fwd_sink")
+          "cache_fwd_sink", "cache_append_norm", "norm_rotate")
 _NO_WORKSPACE = 1        # the library does not serve the shape: the workspace query returned 0
 
 _lib = None
@@ -182,6 +193,11 @@ def lib() -> ctypes.CDLL:
         L.sparkattn_cache_append.argtypes = [cp, bp, ctypes.POINTER(RotaryShape), rp, i32, rp, rp, vp, vp, vp, vp, rp, vp, sz, vp]
         L.sparkattn_cache_fwd.restype = ctypes.c_int
         L.sparkattn_cache_fwd.argtypes = [cp, bp, rp, i32, vp, vp, vp, vp, i32, i32, ctypes.c_float, rp, vp, vp, sz, vp]
+        np = ctypes.POINTER(NormShape)
+        L.sparkattn_cache_append_norm.restype = ctypes.c_int
+        L.sparkattn_cache_append_norm.argtypes = [cp, bp, np, ctypes.POINTER(RotaryShape), rp, i32, rp, rp, vp, vp, vp, vp, rp, vp, sz, vp]
+        L.sparkattn_norm_rotate.restype = ctypes.c_int
+        L.sparkattn_norm_rotate.argtypes = [sp, vp, sp, vp, sp, vp, sp, vp, np, ctypes.POINTER(RotaryShape), vp, sz, vp]
         L.sparkattn_cache_fwd_sink.restype = ctypes.c_int
         L.sparkattn_cache_fwd_sink.argtypes = [cp, bp, rp, i32, vp, vp, vp, vp, i32, i32, i32, ctypes.c_float, rp, vp, vp, sz, vp]
         from . import _sparkattn
@@ -484,6 +500,34 @@ class Rotary(NamedTuple):
     interleaved: bool = False
 
 
+class Norm(NamedTuple):
+    """RMS norm over the channels of each head of queries and keys, in front of their rotation: x / sqrt(mean(x^2) + eps) * weight.  Weights
+    ``q``, ``k`` float32 or bfloat16, [d] or [heads, d], both alike; None: ones."""
+    q: Optional[torch.Tensor] = None
+    k: Optional[torch.Tensor] = None
+    eps: float = 1e-6
+
+
+_NO_ROTARY = (None, None, None, None, False)
+_NO_NORM = (False, None, None, 1.0)
+
+
+def norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, norm: Optional[Norm] = None, rotary: Optional[Rotary] = None,
+                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
+    """``sparkattn_norm_rotate``: q, k bf16 [B, H, N, d] (k with heads of its own number) normalised head by head and rotated, in one pass;
+    ``rotary.positions`` are int32 [N] or [N, axes] (None: the token's index).  Returns (q, k), or q alone, with the strides of the inputs;
+    ``q_out`` may be q, ``k_out`` k."""
+    rc, q_out, k_out, workspace = _calls().norm_rotate(q, k, q_out, k_out, *(_NO_ROTARY if rotary is None else rotary),
+                                                       *(_NO_NORM if norm is None else (True, *norm)), workspace,
+                                                       None if stream is None else stream.cuda_stream)
+    if rc != OK:
+        _check(rc, "sparkattn_norm_rotate")
+    if check_status:
+        _check(read_status(workspace, stream), "sparkattn_norm_rotate (device status)")
+    return q_out if k is None else (q_out, k_out)
+
+
 def alloc_cache(pages: int, heads: int, page: int, d: int, fp8: bool = True, device="cuda:0") -> KVCache:
     """A cache of ``pages`` pages of ``page`` tokens (16, 32, 64 or 128) for ``heads`` key heads of ``d`` channels (64 or 128)."""
     k, v = (torch.zeros((pages, heads, page, d), dtype=torch.uint8 if fp8 else torch.bfloat16, device=device) for _ in range(2))
@@ -495,15 +539,15 @@ def alloc_cache(pages: int, heads: int, page: int, d: int, fp8: bool = True, dev
 
 def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor, *,
                  q_start: Optional[torch.Tensor] = None, max_new: int = 0, q: Optional[torch.Tensor] = None,
-                 rotary: Optional[Rotary] = None, q_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 norm: Optional[Norm] = None, rotary: Optional[Rotary] = None, q_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                  stream: Optional[torch.cuda.Stream] = None, check_status: bool = False) -> Optional[torch.Tensor]:
-    """``sparkattn_cache_append``: stores k, v bf16 [T, H_kv, d] (k rotated) as the newest tokens of the sequences, and returns
-    q bf16 [T, H, d] rotated (None without q; ``q_out`` may be q).  page_table int32 [B, max_pages]; kv_len int32 [B] with the
+    """``sparkattn_cache_append`` (``sparkattn_cache_append_norm`` with ``norm``): stores k, v bf16 [T, H_kv, d] (k normalised and rotated)
+    as the newest tokens of the sequences, and returns q bf16 [T, H, d] normalised and rotated (None without q; ``q_out`` may be q).  page_table int32 [B, max_pages]; kv_len int32 [B] with the
     new tokens; rows q_start[b] .. q_start[b+1] - 1 (int32 [B+1]) belong to sequence b, T / B each without it; max_new:
     no sequence has more new tokens (0: T with q_start, which is slow where many sequences share the rows, else T / B)."""
-    cos, sin, positions, axis, interleaved = (None, None, None, None, False) if rotary is None else rotary
-    rc, q_out, workspace = _calls().cache_append(*cache, page_table, kv_len, q_start, max_new, k, v, q, q_out, cos, sin, positions, axis,
-                                                 interleaved, workspace, None if stream is None else stream.cuda_stream)
+    rc, q_out, workspace = _calls().cache_append(*cache, page_table, kv_len, q_start, max_new, k, v, q, q_out, *(_NO_ROTARY if rotary is None else rotary),
+                                                 *(_NO_NORM if norm is None else (True, *norm)), workspace,
+                                                 None if stream is None else stream.cuda_stream)
     if rc != OK:
         _check(rc, "sparkattn_cache_append")
     if check_status:

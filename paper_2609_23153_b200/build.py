@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libsparkattn.so")
 BINDING = os.path.join(HERE, "_sparkattn.so")
 OBJDIR = os.path.join(HERE, "build")
 BINDING_FOR = os.path.join(OBJDIR, "_sparkattn.for")      # what the binding was built against
-SOURCES = ["api.cu", "select.cu", "quant.cu", "fwd.cu", "noalloc.cu", "comp.cu", "fwd_pipe.cu", "reorder.cu", "cache_append.cu",
+SOURCES = ["api.cu", "select.cu", "quant.cu", "fwd.cu", "noalloc.cu", "comp.cu", "fwd_pipe.cu", "reorder.cu", "norm.cu", "cache_append.cu",
            "cache_fwd.cu", "cache_chunk.cu"]
 NVCC_FLAGS = [
     "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",

@@ -570,6 +570,21 @@ int check_rotary(const sparkattn_rotary_t* r, int d) {
   if (r->rot < 16 || r->rot > d || r->rot % 16 || (long long)r->rows * (r->rot / 2) > 0x7fffffffLL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   return !aligned16(r->cos) || !aligned16(r->sin) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
 }
+int check_norm(const sparkattn_norm_t* n) {
+  if (n == nullptr) return SPARKATTN_OK;
+  if (n->struct_size != sizeof(sparkattn_norm_t) || n->version != SPARKATTN_VERSION || n->pad != 0) return SPARKATTN_E_INVALID_ARG;
+  if ((n->weight_dtype != SPARKATTN_BF16 && n->weight_dtype != SPARKATTN_FP32) || (n->per_head != 0 && n->per_head != 1)) return SPARKATTN_E_INVALID_ARG;
+  if (!(n->eps > 0.0f) || isinf(n->eps)) return SPARKATTN_E_INVALID_ARG;
+  return !aligned16(n->q_weight) || !aligned16(n->k_weight) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
+}
+// one tensor of sparkattn_norm_rotate
+int check_head_rows(const sparkattn_shape_t* s, const void* in, const sparkattn_shape_t* o, const void* out) {
+  int rc = check_shape(s);
+  if (rc == SPARKATTN_OK) rc = check_shape(o);
+  if (rc != SPARKATTN_OK) return rc;
+  if (!in || !out || s->B != o->B || s->H != o->H || s->N != o->N || s->d != o->d) return SPARKATTN_E_INVALID_ARG;
+  return !aligned16(in) || !aligned16(out) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
+}
 // the pools, the table and the scales
 int check_pools(const sparkattn_cache_t* c, const sparkattn_batch_t* b, const void* k_cache, const void* v_cache, const float* k_scale,
                 const float* v_scale, void* workspace) {
@@ -593,7 +608,16 @@ int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch
                            const sparkattn_rows_t* q, int32_t H, const sparkattn_rows_t* k, const sparkattn_rows_t* v,
                            void* k_cache, void* v_cache, float* k_scale, float* v_scale, const sparkattn_rows_t* q_out,
                            void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return sparkattn_cache_append_norm(cache, batch, nullptr, rotary, q, H, k, v, k_cache, v_cache, k_scale, v_scale, q_out, workspace, workspace_bytes,
+                                     cuda_stream);
+}
+
+int sparkattn_cache_append_norm(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_norm_t* norm,
+                                const sparkattn_rotary_t* rotary, const sparkattn_rows_t* q, int32_t H, const sparkattn_rows_t* k,
+                                const sparkattn_rows_t* v, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                                const sparkattn_rows_t* q_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   int rc = check_cache(cache, batch);
+  if (rc == SPARKATTN_OK) rc = check_norm(norm);
   if (rc == SPARKATTN_OK) rc = check_rotary(rotary, cache->d);
   if (rc == SPARKATTN_OK) rc = check_rows(k, false);
   if (rc == SPARKATTN_OK) rc = check_rows(v, false);
@@ -606,8 +630,26 @@ int sparkattn_cache_append(const sparkattn_cache_t* cache, const sparkattn_batch
     if ((rc = check_rows(q, false)) != SPARKATTN_OK || (rc = check_rows(q_out, true)) != SPARKATTN_OK) return rc;
   }
   if (workspace_bytes < kWorkspaceHeaderBytes) return SPARKATTN_E_WORKSPACE_TOO_SMALL;
-  return launch_cache_append(*cache, *batch, rotary, q, H, *k, *v, k_cache, v_cache, k_scale, v_scale, q_out, workspace,
+  return launch_cache_append(*cache, *batch, norm, rotary, q, H, *k, *v, k_cache, v_cache, k_scale, v_scale, q_out, workspace,
                              static_cast<cudaStream_t>(cuda_stream));
+}
+
+int sparkattn_norm_rotate(const sparkattn_shape_t* q_shape, const void* q, const sparkattn_shape_t* q_out_shape, void* q_out,
+                          const sparkattn_shape_t* k_shape, const void* k, const sparkattn_shape_t* k_out_shape, void* k_out,
+                          const sparkattn_norm_t* norm, const sparkattn_rotary_t* rotary, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream) {
+  int rc = check_head_rows(q_shape, q, q_out_shape, q_out);
+  const bool keys = k_shape || k || k_out_shape || k_out;
+  if (rc == SPARKATTN_OK && keys) rc = check_head_rows(k_shape, k, k_out_shape, k_out);
+  if (rc != SPARKATTN_OK) return rc;
+  if (keys && (k_shape->B != q_shape->B || k_shape->N != q_shape->N || k_shape->d != q_shape->d)) return SPARKATTN_E_INVALID_ARG;
+  if ((norm == nullptr && rotary == nullptr) || workspace == nullptr) return SPARKATTN_E_INVALID_ARG;
+  if ((rc = check_norm(norm)) != SPARKATTN_OK || (rc = check_rotary(rotary, q_shape->d)) != SPARKATTN_OK) return rc;
+  if (!aligned256(workspace)) return SPARKATTN_E_MISALIGNED;
+  if (workspace_bytes < kWorkspaceHeaderBytes) return SPARKATTN_E_WORKSPACE_TOO_SMALL;
+  if ((long long)q_shape->B * q_shape->H + (keys ? (long long)k_shape->B * k_shape->H : 0) > 0x7fffff00LL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  const HeadRows rq{q_shape, q, q_out_shape, q_out}, rk{k_shape, k, k_out_shape, k_out};
+  return launch_norm_rotate(rq, keys ? &rk : nullptr, norm, rotary, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int sparkattn_cache_fwd(const sparkattn_cache_t* cache, const sparkattn_batch_t* batch, const sparkattn_rows_t* q, int32_t H,

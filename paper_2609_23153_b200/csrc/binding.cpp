@@ -43,6 +43,8 @@ struct Library {
   decltype(&sparkattn_cache_append) cache_append;
   decltype(&sparkattn_cache_fwd) cache_fwd;
   decltype(&sparkattn_cache_fwd_sink) cache_fwd_sink;
+  decltype(&sparkattn_cache_append_norm) cache_append_norm;
+  decltype(&sparkattn_norm_rotate) norm_rotate;
 };
 Library g_lib{};
 
@@ -513,42 +515,88 @@ struct Cache {
   }
 };
 
+// The rotation and the norm of queries and keys, as the calls that take them do.
+struct Rotation {
+  at::Tensor cos, sin, positions, axis;
+  sparkattn_rotary_t r{};
+  explicit Rotation(Args& a) {
+    cos = a.optional_tensor();
+    sin = a.optional_tensor();
+    positions = a.optional_tensor();
+    axis = a.optional_tensor();
+    r.interleaved = a.truth();
+  }
+  // for `tokens` tokens; NULL where nothing is rotated
+  const sparkattn_rotary_t* describe(int64_t tokens, const at::Device& device) {
+    if (!cos.defined()) return nullptr;
+    TORCH_CHECK_VALUE(sin.defined() && cos.dim() == 2 && cos.scalar_type() == at::kFloat && sin.scalar_type() == at::kFloat && cos.is_contiguous() &&
+                          sin.is_contiguous() && cos.sizes() == sin.sizes() && cos.device() == device && sin.device() == device,
+                      "rotary tables are contiguous float32 [rows, rot / 2] on the call's device");
+    TORCH_CHECK_VALUE(!positions.defined() || (positions.scalar_type() == at::kInt && positions.is_contiguous() && positions.device() == device &&
+                                               (positions.dim() == 1 || positions.dim() == 2) && positions.size(0) == tokens),
+                      "positions are contiguous int32 [T] or [T, axes] on the call's device");
+    TORCH_CHECK_VALUE(!axis.defined() || (axis.scalar_type() == at::kInt && axis.is_contiguous() && axis.dim() == 1 && axis.size(0) == cos.size(1) &&
+                                          axis.device() == device),
+                      "axis is a contiguous int32 [rot / 2] on the call's device");
+    TORCH_CHECK_VALUE(axis.defined() || !positions.defined() || positions.dim() == 1 || positions.size(1) == 1, "positions over several axes need axis");
+    r.struct_size = sizeof(r);
+    r.version = SPARKATTN_VERSION;
+    r.rot = (int32_t)(2 * cos.size(1));
+    r.rows = (int32_t)cos.size(0);
+    r.axes = positions.defined() && positions.dim() == 2 ? (int32_t)positions.size(1) : 1;
+    r.cos = fptr(cos); r.sin = fptr(sin);
+    r.positions = iptr(positions); r.axis = iptr(axis);
+    return &r;
+  }
+};
+struct HeadNorm {
+  at::Tensor q, k;
+  bool on;
+  sparkattn_norm_t n{};
+  explicit HeadNorm(Args& a) {
+    on = a.truth();
+    q = a.optional_tensor();
+    k = a.optional_tensor();
+    n.eps = a.number();
+  }
+  // heads -1: the call has no such tensor
+  const sparkattn_norm_t* describe(int64_t q_heads, int64_t k_heads, int64_t d, const at::Device& device) {
+    if (!on) return nullptr;
+    n.struct_size = sizeof(n);
+    n.version = SPARKATTN_VERSION;
+    const at::Tensor& any = q.defined() ? q : k;
+    n.weight_dtype = any.defined() && any.scalar_type() == at::kBFloat16 ? SPARKATTN_BF16 : SPARKATTN_FP32;
+    n.per_head = any.defined() && any.dim() == 2;
+    auto check = [&](const at::Tensor& w, int64_t heads) {
+      TORCH_CHECK_VALUE(!w.defined() || ((w.scalar_type() == at::kFloat || w.scalar_type() == at::kBFloat16) && w.scalar_type() == any.scalar_type() &&
+                                         w.is_contiguous() && w.dim() == any.dim() && (w.dim() == 1 || (w.dim() == 2 && (heads < 0 || w.size(0) == heads))) &&
+                                         w.size(-1) == d && w.device() == device),
+                        "norm weights are contiguous float32 or bfloat16 [d] or [heads, d], both alike, on the call's device");
+    };
+    check(q, q_heads);
+    check(k, k_heads);
+    n.q_weight = ptr(q); n.k_weight = ptr(k);
+    return &n;
+  }
+};
+
 // cache_append(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, k, v, q, q_out, cos, sin, positions, axis,
-// interleaved, workspace, stream) -> rc, q_out, workspace
+// interleaved, norm, q_weight, k_weight, eps, workspace, stream) -> rc, q_out, workspace
 PyObject* cache_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Args a(argv, n);
-  a.expect(19);
+  a.expect(23);
   Cache cache(a);
   const at::Tensor k = a.tensor(), v = a.tensor(), q = a.optional_tensor();
   at::Tensor q_out = a.optional_tensor();
-  const at::Tensor cos = a.optional_tensor(), sin = a.optional_tensor(), positions = a.optional_tensor(), axis = a.optional_tensor();
-  const bool interleaved = a.truth();
+  Rotation rotation(a);
+  HeadNorm norm(a);
   at::Tensor ws = a.optional_tensor();
   const Stream stream = a.stream();
   cache.describe(k);
   const sparkattn_rows_t rk = cache.rows(k, cache.c.H), rv = cache.rows(v, cache.c.H);
-  sparkattn_rotary_t rotary{};
-  if (cos.defined()) {
-    TORCH_CHECK_VALUE(sin.defined() && cos.dim() == 2 && cos.scalar_type() == at::kFloat && sin.scalar_type() == at::kFloat && cos.is_contiguous() &&
-                          sin.is_contiguous() && cos.sizes() == sin.sizes() && cos.device() == k.device() && sin.device() == k.device(),
-                      "rotary tables are contiguous float32 [rows, rot / 2] on the call's device");
-    TORCH_CHECK_VALUE(!positions.defined() || (positions.scalar_type() == at::kInt && positions.is_contiguous() && positions.device() == k.device() &&
-                                               (positions.dim() == 1 || positions.dim() == 2) && positions.size(0) == k.size(0)),
-                      "positions are contiguous int32 [T] or [T, axes] on the call's device");
-    TORCH_CHECK_VALUE(!axis.defined() || (axis.scalar_type() == at::kInt && axis.is_contiguous() && axis.dim() == 1 && axis.size(0) == cos.size(1) &&
-                                          axis.device() == k.device()),
-                      "axis is a contiguous int32 [rot / 2] on the call's device");
-    TORCH_CHECK_VALUE(axis.defined() || !positions.defined() || positions.dim() == 1 || positions.size(1) == 1, "positions over several axes need axis");
-    rotary.struct_size = sizeof(rotary);
-    rotary.version = SPARKATTN_VERSION;
-    rotary.rot = (int32_t)(2 * cos.size(1));
-    rotary.interleaved = interleaved;
-    rotary.rows = (int32_t)cos.size(0);
-    rotary.axes = positions.defined() && positions.dim() == 2 ? (int32_t)positions.size(1) : 1;
-    rotary.cos = fptr(cos); rotary.sin = fptr(sin);
-    rotary.positions = iptr(positions); rotary.axis = iptr(axis);
-  }
+  const sparkattn_rotary_t* rotary = rotation.describe(k.size(0), k.device());
+  const sparkattn_norm_t* normed = norm.describe(q.defined() && q.dim() == 3 ? q.size(1) : -1, cache.c.H, cache.c.d, k.device());
   cache.check_device();
   int rc;
   {
@@ -561,11 +609,50 @@ PyObject* cache_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
       rq = cache.rows(q, 0);
       ro = cache.rows(q_out, q.size(1));
     }
-    rc = g_lib.cache_append(&cache.c, &cache.b, cos.defined() ? &rotary : nullptr, q.defined() ? &rq : nullptr, q.defined() ? (int32_t)q.size(1) : 0, &rk, &rv,
-                            ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), q.defined() ? &ro : nullptr, ptr(ws),
-                            (size_t)ws.numel(), stream);
+    rc = g_lib.cache_append_norm(&cache.c, &cache.b, normed, rotary, q.defined() ? &rq : nullptr, q.defined() ? (int32_t)q.size(1) : 0, &rk, &rv,
+                                 ptr(cache.k), ptr(cache.v), fptr(cache.k_scale), fptr(cache.v_scale), q.defined() ? &ro : nullptr, ptr(ws),
+                                 (size_t)ws.numel(), stream);
   }
   return result(rc, {q_out, ws});
+  END_HANDLE_TH_ERRORS
+}
+
+// norm_rotate(q, k, q_out, k_out, cos, sin, positions, axis, interleaved, norm, q_weight, k_weight, eps, workspace, stream)
+// -> rc, q_out, k_out, workspace
+PyObject* norm_rotate(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(15);
+  const at::Tensor q = a.tensor(), k = a.optional_tensor();
+  at::Tensor q_out = a.optional_tensor(), k_out = a.optional_tensor();
+  Rotation rotation(a);
+  HeadNorm norm(a);
+  at::Tensor ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  const int32_t block = q.dim() == 4 && q.size(3) == 64 ? 64 : 128;
+  const sparkattn_shape_t qs = make_shape(q, block);
+  sparkattn_shape_t ks{};
+  if (k.defined()) ks = make_shape(k, block);
+  TORCH_CHECK_VALUE(k.defined() || !k_out.defined(), "k_out without k");
+  const sparkattn_rotary_t* rotary = rotation.describe(qs.N, q.device());
+  const sparkattn_norm_t* normed = norm.describe(qs.H, k.defined() ? ks.H : -1, qs.d, q.device());
+  for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&q, &k, &q_out, &k_out})
+    TORCH_CHECK_VALUE(!x->defined() || (x->scalar_type() == at::kBFloat16 && x->device() == q.device()), "expected bfloat16 tensors on one device");
+  TORCH_CHECK_VALUE(q.is_cuda(), "tensors of a call must be on a CUDA device");
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    if (!q_out.defined()) q_out = stream.output_like(q, at::kBFloat16);
+    if (k.defined() && !k_out.defined()) k_out = stream.output_like(k, at::kBFloat16);
+    if (!ws.defined()) ws = stream.scratch(256, q);
+    TORCH_CHECK_VALUE(ws.device() == q.device() && ws.is_contiguous() && ws.element_size() == 1, "the workspace is contiguous bytes on the call's device");
+    const sparkattn_shape_t qo = make_shape(q_out, block);
+    sparkattn_shape_t ko{};
+    if (k.defined()) ko = make_shape(k_out, block);
+    rc = g_lib.norm_rotate(&qs, ptr(q), &qo, ptr(q_out), k.defined() ? &ks : nullptr, ptr(k), k.defined() ? &ko : nullptr, ptr(k_out), normed, rotary, ptr(ws),
+                           (size_t)ws.numel(), stream);
+  }
+  return result(rc, {q_out, k_out, ws});
   END_HANDLE_TH_ERRORS
 }
 
@@ -625,7 +712,8 @@ PyMethodDef g_methods[] = {method<bind>("bind"), method<select>("select"), metho
                            method<quant_fp8>("quant_fp8"), method<quant_fp8_pooled>("quant_fp8_pooled"),
                            method<quant_fp8_per_token>("quant_fp8_per_token"), method<fwd>("fwd"), method<gather_tokens>("gather_tokens"),
                            method<comp_state>("comp_state"), method<comp_apply>("comp_apply"), method<fwd_gated>("fwd_gated"),
-                           method<cache_append>("cache_append"), method<cache_fwd>("cache_fwd"), {nullptr, nullptr, 0, nullptr}};
+                           method<cache_append>("cache_append"), method<cache_fwd>("cache_fwd"),
+                           method<norm_rotate>("norm_rotate"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_sparkattn", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -15,8 +15,10 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
+#include "rows.cuh"
 #include "tmap.h"
 
 namespace sparkattn {
@@ -25,16 +27,10 @@ struct RowsView {
   __nv_bfloat16* data;
   int64_t stride_t, stride_h;
 };
-struct RotaryView {
-  const float* cos;
-  const float* sin;
-  const int32_t* positions;
-  const int32_t* axis;
-  int rot, interleaved, rows, axes;
-};
 struct AppendParams {
   BatchView batch;
   RotaryView rotary;             // rot = 0: nothing is rotated
+  NormView norm;
   RowsView q, k, v, q_out;       // q.data NULL: no queries
   unsigned char* k_cache;
   unsigned char* v_cache;
@@ -49,30 +45,6 @@ struct AppendParams {
   int units;
   int32_t* status;
 };
-
-// eight fp32 channels
-struct Chunk {
-  float x[8];
-};
-__device__ __forceinline__ Chunk widen(uint4 v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  Chunk c;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    c.x[2 * j] = __uint_as_float(w[j] << 16);
-    c.x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-  }
-  return c;
-}
-__device__ __forceinline__ uint4 narrow(const Chunk& c) {
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(c.x[2 * j], c.x[2 * j + 1]);
-    w[j] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // cosines and sines of a unit's tokens as [rows][pairs], from the tables; a pair outside them is turned by nothing
 __device__ __forceinline__ void gather_phases(const RotaryView& r, int rows, int t0, int pos0, float* s_cos, float* s_sin, int tid, int threads) {
@@ -104,34 +76,6 @@ __device__ __forceinline__ void gather_phases(const RotaryView& r, int rows, int
     *reinterpret_cast<float4*>(s_sin + row * (r.rot / 2) + m) = s;
   }
 }
-// The chunk turned by its share c, s of a row of them.  Interleaved: its own four pairs.  Halves: `y` holds the other sides of its
-// eight channels.  Each product and sum is rounded by itself, so that a cache filled by any route holds the same bits.  (Scalar
-// instructions: the packed ones want their pairs in neighbouring registers and spend more on moves than they save, and a packed sum
-// behind packed products was fused with one of them, which rounds once.)
-__device__ __forceinline__ Chunk turn_pairs(const float* c, const float* s, const Chunk& x) {
-  const float4 cc = *reinterpret_cast<const float4*>(c), ss = *reinterpret_cast<const float4*>(s);
-  const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
-  Chunk r;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    r.x[2 * j] = __fsub_rn(__fmul_rn(x.x[2 * j], cv[j]), __fmul_rn(x.x[2 * j + 1], sv[j]));
-    r.x[2 * j + 1] = __fadd_rn(__fmul_rn(x.x[2 * j], sv[j]), __fmul_rn(x.x[2 * j + 1], cv[j]));
-  }
-  return r;
-}
-__device__ __forceinline__ Chunk turn_halves(const float* c, const float* s, const Chunk& x, const Chunk& y, float sign) {
-  Chunk r;
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    const float4 cc = reinterpret_cast<const float4*>(c)[g], ss = reinterpret_cast<const float4*>(s)[g];
-    const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)      // a first side takes away what a second side adds: x c - y s and x c + y s round alike
-      r.x[4 * g + j] = __fadd_rn(__fmul_rn(x.x[4 * g + j], cv[j]), __fmul_rn(y.x[4 * g + j], __fmul_rn(sv[j], sign)));
-  }
-  return r;
-}
-
 // bits of the largest |x|, NaN aside; or of the finite ones
 template <bool FINITE>
 __device__ __forceinline__ uint32_t largest_bits(const Chunk& c, uint32_t top) {
@@ -200,7 +144,8 @@ struct UnitShape {
 };
 
 // Lines first, first + step, ... of a unit: the threads hold its up to ROWS new rows of one of them, 16 bytes of a row each at a time.
-template <int D, bool FP8, int ROWS>
+// NORM: keys and queries are normalised first.
+template <int D, bool FP8, int ROWS, bool NORM>
 __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& u, int first, int step, int group, uint32_t* s_max,
                                              const float* s_cos, const float* s_sin) {
   using S = UnitShape<D, ROWS>;
@@ -213,10 +158,18 @@ __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& 
   const int m0 = rot.interleaved ? chunk * 4 : (second ? chunk - half : chunk) * 8;
   const int partner = (threadIdx.x & 31 & ~(S::kLanes - 1)) + (!on ? chunk : second ? chunk - half : chunk + half);
   const float sign = second ? 1.0f : -1.0f;
+  [[maybe_unused]] Chunk weight;                                 // NORM: of the line's head
   // row r's chunk turned (lanes of a row together: halves pass their chunks on)
   auto turned = [&](uint4 v, int r, bool there) {
     const float* c = s_cos + r * pairs + m0;
     const float* s = s_sin + r * pairs + m0;
+    if constexpr (NORM) {
+      const Chunk x = normed<D>(widen(v), weight, p.norm.eps);
+      if (rot.rot == 0) return x;
+      if (rot.interleaved) return on && there ? turn_pairs(c, s, x) : x;
+      const Chunk far = chunk_of(x, partner);
+      return on && there ? turn_halves(c, s, x, far, sign) : x;
+    }
     if (rot.interleaved) return on && there ? turn_pairs(c, s, widen(v)) : widen(v);
     const uint4 far = make_uint4(__shfl_sync(0xffffffffu, v.x, partner), __shfl_sync(0xffffffffu, v.y, partner), __shfl_sync(0xffffffffu, v.z, partner),
                                  __shfl_sync(0xffffffffu, v.w, partner));
@@ -242,11 +195,22 @@ __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& 
     if constexpr (FP8) old = !query && rows > 0 && u.held > 0 ? *scale_of(n) : 0.0f;
   };
   fetch(first);
+  [[maybe_unused]] const void* weight_of = nullptr;
+  [[maybe_unused]] bool weighted = false;
   int turn_of = 0;                                               // which half of s_max this line takes
 #pragma unroll 1
   for (int n = first; n < p.lines; n += step) {
-    const bool query = n >= 2 * p.Hk, rotate = (n < p.Hk || query) && rot.rot > 0;
+    const bool query = n >= 2 * p.Hk, rotate = (n < p.Hk || query) && (NORM || rot.rot > 0);
     const int h = n < p.Hk ? n : query ? n - 2 * p.Hk : n - p.Hk;
+    if constexpr (NORM) {
+      // (one head's weights serve the other heads' lines where all heads share them)
+      const void* from = query ? p.norm.q_weight : p.norm.k_weight;
+      if (rotate && (!weighted || p.norm.stride != 0 || from != weight_of)) {
+        weight = norm_weights(p.norm, from, h, chunk * 8);
+        weight_of = from;
+        weighted = true;
+      }
+    }
     const int rows = query || u.page >= 0 ? u.rows : 0;
     uint4 raw[C];
     cp_async_wait<0>();
@@ -319,7 +283,7 @@ __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& 
   }
 }
 
-template <int D, bool FP8, int ROWS>
+template <int D, bool FP8, int ROWS, bool NORM>
 __global__ void __launch_bounds__(UnitShape<D, ROWS>::kThreads, 1024 / UnitShape<D, ROWS>::kThreads)
 cache_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kThreads = UnitShape<D, ROWS>::kThreads;
@@ -370,10 +334,10 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
     if constexpr (U > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(U) : "memory");
     else __syncwarp();
   }
-  append_lines<D, FP8, ROWS>(p, u, first, p.groups, group, s_max, s_cos, s_sin);
+  append_lines<D, FP8, ROWS, NORM>(p, u, first, p.groups, group, s_max, s_cos, s_sin);
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool NORM>
 static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream) {
   auto go = [&](auto kern, auto shape) {
     constexpr int kThreads = decltype(shape)::kThreads, per = kThreads / decltype(shape)::U;
@@ -393,19 +357,20 @@ static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream)
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)decltype(shape)::smem(D)) != cudaSuccess) return (int)SPARKATTN_E_CUDA;
     return launch_kernel(kern, dim3(ctas), kThreads, smem, true, stream, p);
   };
-  if (rows <= 4) return go(cache_append_kernel<D, FP8, 4>, UnitShape<D, 4>{});
-  if (rows <= 16) return go(cache_append_kernel<D, FP8, 16>, UnitShape<D, 16>{});
-  if (rows <= 32) return go(cache_append_kernel<D, FP8, 32>, UnitShape<D, 32>{});
-  if (rows <= 64) return go(cache_append_kernel<D, FP8, 64>, UnitShape<D, 64>{});
-  return go(cache_append_kernel<D, FP8, 128>, UnitShape<D, 128>{});
+  if (rows <= 4) return go(cache_append_kernel<D, FP8, 4, NORM>, UnitShape<D, 4>{});
+  if (rows <= 16) return go(cache_append_kernel<D, FP8, 16, NORM>, UnitShape<D, 16>{});
+  if (rows <= 32) return go(cache_append_kernel<D, FP8, 32, NORM>, UnitShape<D, 32>{});
+  if (rows <= 64) return go(cache_append_kernel<D, FP8, 64, NORM>, UnitShape<D, 64>{});
+  return go(cache_append_kernel<D, FP8, 128, NORM>, UnitShape<D, 128>{});
 }
 
-int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rotary_t* rotary, const sparkattn_rows_t* q,
-                        int H, const sparkattn_rows_t& k, const sparkattn_rows_t& v, void* k_cache, void* v_cache, float* k_scale,
+int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_norm_t* norm, const sparkattn_rotary_t* rotary,
+                        const sparkattn_rows_t* q, int H, const sparkattn_rows_t& k, const sparkattn_rows_t& v, void* k_cache, void* v_cache, float* k_scale,
                         float* v_scale, const sparkattn_rows_t* q_out, void* workspace, cudaStream_t stream) {
   AppendParams p{};
   p.batch = make_batch_view(c, b);
-  if (rotary) p.rotary = {rotary->cos, rotary->sin, rotary->positions, rotary->axis, rotary->rot, rotary->interleaved, rotary->rows, rotary->axes};
+  p.rotary = make_rotary_view(rotary);
+  p.norm = make_norm_view(norm, c.d);
   auto view = [](const sparkattn_rows_t& r) { return RowsView{static_cast<__nv_bfloat16*>(r.data), r.stride_t, r.stride_h}; };
   if (q) { p.q = view(*q); p.q_out = view(*q_out); }
   p.k = view(k);
@@ -419,8 +384,12 @@ int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, 
   p.status = static_cast<int32_t*>(workspace);
   const int rows = c.page < b.max_new ? c.page : b.max_new;
   const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;
-  if (c.d == 128) return fp8 ? launch_rows<128, true>(p, rows, stream) : launch_rows<128, false>(p, rows, stream);
-  return fp8 ? launch_rows<64, true>(p, rows, stream) : launch_rows<64, false>(p, rows, stream);
+  auto go = [&](auto normed) {
+    constexpr bool NORM = decltype(normed)::value;
+    if (c.d == 128) return fp8 ? launch_rows<128, true, NORM>(p, rows, stream) : launch_rows<128, false, NORM>(p, rows, stream);
+    return fp8 ? launch_rows<64, true, NORM>(p, rows, stream) : launch_rows<64, false, NORM>(p, rows, stream);
+  };
+  return norm ? go(std::true_type{}) : go(std::false_type{});
 }
 
 }  // namespace sparkattn

@@ -107,10 +107,20 @@ int launch_brick_layout(const int32_t* grid, const int32_t* brick, int block, in
 int launch_gather_tokens(const sparkattn_shape_t& src, const void* x, const sparkattn_shape_t& dst, const int32_t* index,
                          void* out, void* workspace, cudaStream_t stream);
 
+// norm.cu: norms and rotation of queries and keys of whole sequences (k_in NULL: of queries alone)
+struct HeadRows {
+  const sparkattn_shape_t* in_shape;
+  const void* in;
+  const sparkattn_shape_t* out_shape;
+  void* out;
+};
+int launch_norm_rotate(const HeadRows& q, const HeadRows* k, const sparkattn_norm_t* norm, const sparkattn_rotary_t* rotary, void* workspace,
+                       cudaStream_t stream);
+
 // cache_append.cu, cache_fwd.cu: the paged cache
 constexpr int kCacheMaxSequences = 4096;   // their lengths are laid out in shared memory
-int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rotary_t* rotary, const sparkattn_rows_t* q,
-                        int H, const sparkattn_rows_t& k, const sparkattn_rows_t& v, void* k_cache, void* v_cache, float* k_scale,
+int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_norm_t* norm, const sparkattn_rotary_t* rotary,
+                        const sparkattn_rows_t* q, int H, const sparkattn_rows_t& k, const sparkattn_rows_t& v, void* k_cache, void* v_cache, float* k_scale,
                         float* v_scale, const sparkattn_rows_t* q_out, void* workspace, cudaStream_t stream);
 bool cache_work_fits(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);
 size_t cache_fwd_workspace_bytes(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);

@@ -1,0 +1,183 @@
+// sparkattn_norm_rotate: RMS norm of each head's queries and keys and their rotation, whole sequences at a time.
+//
+// y = R(x / sqrt(mean x^2 + eps) * w), row by row; nothing is used twice but the tokens' cosines and sines, which all heads share, and the
+// weights, which all tokens share.  So a thread stays with 16 bytes of one token's rows: its pairs' phases and (per tensor) its weights are in
+// registers once, and it goes through the heads, kUnroll rows asked for at a time.  The sum of squares goes through the D / 8 lanes of a row.
+// A CTA is 256 threads: 16 tokens (32 of 64 channels) by a run of the (sample, head) lines of both tensors.
+#include <algorithm>
+
+#include "rows.cuh"
+#include "tmap.h"
+
+namespace sparkattn {
+
+constexpr int kNormThreads = 256, kNormUnroll = 4;
+
+struct HeadRowsView {
+  const __nv_bfloat16* in;
+  __nv_bfloat16* out;
+  int64_t in_b, in_h, in_n, out_b, out_h, out_n;      // strides
+  const void* weight;
+  int H, lines;                                       // heads; samples * heads
+  FastDiv by_H;
+};
+struct NormRotateParams {
+  HeadRowsView x[2];             // queries, keys (lines 0: none)
+  RotaryView rotary;             // rot = 0: nothing is rotated
+  NormView norm;
+  int N;
+  int tiles, each;               // tiles of tokens; lines of a CTA
+  FastDiv by_tiles;
+  int32_t* status;
+};
+
+// Whether a pair of token n is turned by an angle of the tables.  (A pair that is not stays as it is and is reported.)
+__device__ __forceinline__ uint32_t angle_row(const RotaryView& r, int n, int m) {
+  uint32_t axis = 0;
+  if (r.axis != nullptr) {
+    axis = (uint32_t)r.axis[m];
+    if (axis >= (uint32_t)r.axes) return 0xffffffffu;
+  }
+  return r.positions != nullptr ? (uint32_t)r.positions[(int64_t)n * r.axes + axis] : (uint32_t)n;
+}
+
+template <int D, bool INTERLEAVED, bool NORM>
+__global__ void __launch_bounds__(kNormThreads, 4)
+norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
+  constexpr int kLanes = D / 8, kRows = kNormThreads / kLanes, kPairs = INTERLEAVED ? 4 : 8;
+  const RotaryView& r = p.rotary;
+  const int group = fast_div((int)blockIdx.x, p.by_tiles), tile = (int)blockIdx.x - group * p.tiles;
+  const int chunk = threadIdx.x % kLanes, n = tile * kRows + threadIdx.x / kLanes;
+  const bool there = n < p.N, on = chunk * 8 < r.rot;
+  const int half = r.rot / 16;                                    // halves: chunks of a side
+  const bool second = chunk >= half;
+  const int m0 = INTERLEAVED ? chunk * 4 : (second ? chunk - half : chunk) * 8;
+  const int partner = (threadIdx.x & 31 & ~(kLanes - 1)) + (!on ? chunk : second ? chunk - half : chunk + half);
+  pdl_wait();
+  bool code_there = false;
+  if (blockIdx.x == 0 && threadIdx.x == 0) code_there = take_header(p.status);
+  float c[kPairs], s[kPairs];
+  int bad = 0;
+  bool any_bad = false;
+#pragma unroll
+  for (int j = 0; j < kPairs; ++j) {
+    c[j] = 1.0f;
+    s[j] = 0.0f;
+    if (there && on) {
+      const uint32_t e = angle_row(r, n, m0 + j);
+      if (e < (uint32_t)r.rows) {
+        c[j] = r.cos[e * (r.rot / 2) + m0 + j];
+        s[j] = r.sin[e * (r.rot / 2) + m0 + j];
+      } else {
+        any_bad = true;
+        bad = (int)e;
+      }
+    }
+    if (!INTERLEAVED && !second) s[j] = -s[j];                    // a first side takes away what a second side adds
+  }
+  auto turned = [&](const Chunk& x) {
+    Chunk y;
+    if constexpr (INTERLEAVED) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        y.x[2 * j] = __fsub_rn(__fmul_rn(x.x[2 * j], c[j]), __fmul_rn(x.x[2 * j + 1], s[j]));
+        y.x[2 * j + 1] = __fadd_rn(__fmul_rn(x.x[2 * j], s[j]), __fmul_rn(x.x[2 * j + 1], c[j]));
+      }
+    } else {
+      const Chunk far = chunk_of(x, partner);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y.x[j] = __fadd_rn(__fmul_rn(x.x[j], c[j]), __fmul_rn(far.x[j], s[j]));
+    }
+    return y;
+  };
+  const int from = group * p.each, to = from + p.each;
+#pragma unroll 1
+  for (int t = 0, base = 0; t < 2; base += p.x[t].lines, ++t) {
+    const HeadRowsView& v = p.x[t];
+    const int first = max(from - base, 0), last = min(to - base, v.lines);
+    if (first >= last) continue;
+    Chunk weight;
+    if constexpr (NORM) {
+      if (p.norm.stride == 0) weight = norm_weights(p.norm, v.weight, 0, chunk * 8);
+    }
+    const __nv_bfloat16* in = v.in + (int64_t)n * v.in_n + chunk * 8;
+    __nv_bfloat16* out = v.out + (int64_t)n * v.out_n + chunk * 8;
+#pragma unroll 1
+    for (int l0 = first; l0 < last; l0 += kNormUnroll) {
+      uint4 raw[kNormUnroll];
+#pragma unroll
+      for (int u = 0; u < kNormUnroll; ++u) {
+        const int l = l0 + u, b = fast_div(l, v.by_H), h = l - b * v.H;
+        raw[u] = l < last && there ? *reinterpret_cast<const uint4*>(in + (b * v.in_b + h * v.in_h)) : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int u = 0; u < kNormUnroll; ++u) {
+        const int l = l0 + u, b = fast_div(l, v.by_H), h = l - b * v.H;
+        Chunk x = widen(raw[u]);
+        if constexpr (NORM) {
+          if (p.norm.stride != 0 && l < last) weight = norm_weights(p.norm, v.weight, h, chunk * 8);
+          x = normed<D>(x, weight, p.norm.eps);
+        }
+        if (r.rot > 0) {
+          const Chunk y = turned(x);
+          if (on) x = y;
+        }
+        if (l < last && there) *reinterpret_cast<uint4*>(out + (b * v.out_b + h * v.out_h)) = narrow(x);
+      }
+    }
+  }
+  if (r.rot == 0) return;
+  if (group == 0 && any_bad) report_early(p.status, SPARKATTN_E_BAD_INDEX, bad);
+  if (blockIdx.x == 0 && __syncthreads_or(code_there)) {
+    // the word held a code, which may have been one of this call's: see take_header
+    any_bad = false;
+    const long long all = (long long)p.N * (r.rot / 2);
+#pragma unroll 1
+    for (long long i = threadIdx.x; i < all; i += kNormThreads) {
+      const int row = (int)(i / (r.rot / 2));
+      const uint32_t e = angle_row(r, row, (int)(i - (long long)row * (r.rot / 2)));
+      if (e >= (uint32_t)r.rows) {
+        any_bad = true;
+        bad = (int)e;
+      }
+    }
+    if (any_bad) report_early(p.status, SPARKATTN_E_BAD_INDEX, bad);
+  }
+}
+
+int launch_norm_rotate(const HeadRows& q, const HeadRows* k, const sparkattn_norm_t* norm, const sparkattn_rotary_t* rotary, void* workspace,
+                       cudaStream_t stream) {
+  NormRotateParams p{};
+  auto view = [](const HeadRows& x, const void* weight) {
+    const sparkattn_shape_t &i = *x.in_shape, &o = *x.out_shape;
+    return HeadRowsView{static_cast<const __nv_bfloat16*>(x.in), static_cast<__nv_bfloat16*>(x.out), i.stride_b, i.stride_h, i.stride_n, o.stride_b,
+                        o.stride_h, o.stride_n, weight, i.H, i.B * i.H, make_fast_div(i.H)};
+  };
+  const sparkattn_shape_t& s = *q.in_shape;
+  p.rotary = make_rotary_view(rotary);
+  p.norm = make_norm_view(norm, s.d);
+  p.x[0] = view(q, p.norm.q_weight);
+  if (k) p.x[1] = view(*k, p.norm.k_weight);
+  p.N = s.N;
+  p.status = static_cast<int32_t*>(workspace);
+  const int rows = kNormThreads / (s.d / 8), sms = current_sm_count();
+  if (sms < 1) return SPARKATTN_E_CUDA;
+  p.tiles = (s.N + rows - 1) / rows;
+  p.by_tiles = make_fast_div(p.tiles);
+  // runs of lines: as many as give four CTAs for every place on the SMs, of at least two batches of rows each
+  const long long lines = (long long)p.x[0].lines + p.x[1].lines;
+  long long groups = std::min<long long>((16LL * sms + p.tiles - 1) / p.tiles, (lines + 2 * kNormUnroll - 1) / (2 * kNormUnroll));
+  p.each = (int)((lines + groups - 1) / groups);
+  groups = (lines + p.each - 1) / p.each;
+  if (groups * p.tiles > 0x7fffff00LL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  auto go = [&](auto kern) { return launch_kernel(kern, dim3((unsigned)(groups * p.tiles)), kNormThreads, 0, true, stream, p); };
+  const bool inter = p.rotary.interleaved != 0;
+  if (s.d == 128) {
+    if (norm) return inter ? go(norm_rotate_kernel<128, true, true>) : go(norm_rotate_kernel<128, false, true>);
+    return inter ? go(norm_rotate_kernel<128, true, false>) : go(norm_rotate_kernel<128, false, false>);
+  }
+  if (norm) return inter ? go(norm_rotate_kernel<64, true, true>) : go(norm_rotate_kernel<64, false, true>);
+  return inter ? go(norm_rotate_kernel<64, true, false>) : go(norm_rotate_kernel<64, false, false>);
+}
+
+}  // namespace sparkattn

@@ -1,0 +1,125 @@
+// Rows of bf16 channels, eight to a thread, as the calls that normalise and rotate queries and keys take them: the norm of a row and the
+// rotation of its channel pairs.  D / 8 neighbouring lanes of a warp hold a row.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "launch.h"
+
+namespace sparkattn {
+
+struct RotaryView {
+  const float* cos;
+  const float* sin;
+  const int32_t* positions;
+  const int32_t* axis;
+  int rot, interleaved, rows, axes;
+};
+inline RotaryView make_rotary_view(const sparkattn_rotary_t* r) {
+  return r ? RotaryView{r->cos, r->sin, r->positions, r->axis, r->rot, r->interleaved, r->rows, r->axes} : RotaryView{};
+}
+// Weights of the norms: [D], or [heads, D] where stride is D; NULL: ones
+struct NormView {
+  const void* q_weight;
+  const void* k_weight;
+  int stride, bf16;
+  float eps;
+};
+inline NormView make_norm_view(const sparkattn_norm_t* n, int d) {
+  return n ? NormView{n->q_weight, n->k_weight, n->per_head ? d : 0, n->weight_dtype == SPARKATTN_BF16, n->eps} : NormView{};
+}
+
+// eight fp32 channels
+struct Chunk {
+  float x[8];
+};
+__device__ __forceinline__ Chunk widen(uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  Chunk c;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    c.x[2 * j] = __uint_as_float(w[j] << 16);
+    c.x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+  }
+  return c;
+}
+__device__ __forceinline__ uint4 narrow(const Chunk& c) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(c.x[2 * j], c.x[2 * j + 1]);
+    w[j] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// the weights of eight channels of a head
+__device__ __forceinline__ Chunk norm_weights(const NormView& n, const void* weight, int head, int channel) {
+  Chunk w;
+  const int at = head * n.stride + channel;
+  if (weight == nullptr) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w.x[j] = 1.0f;
+  } else if (n.bf16) {
+    w = widen(*reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(weight) + at));
+  } else {
+    const float4* from = reinterpret_cast<const float4*>(static_cast<const float*>(weight) + at);
+    const float4 a = from[0], b = from[1];
+    w = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+  }
+  return w;
+}
+// x / sqrt(mean x^2 + eps) * weight of a row whose chunks the D / 8 lanes hold.  Squares, their sum and both products are fp32; the order of the sum
+// is that of the lanes, so a row has the same bits whatever call it goes through.
+template <int D>
+__device__ __forceinline__ Chunk normed(const Chunk& x, const Chunk& weight, float eps) {
+  float sum = __fmul_rn(x.x[0], x.x[0]);
+#pragma unroll
+  for (int j = 1; j < 8; ++j) sum = __fmaf_rn(x.x[j], x.x[j], sum);
+#pragma unroll
+  for (int o = 1; o < D / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const float by = rsqrtf(__fmaf_rn(sum, 1.0f / D, eps));
+  Chunk r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r.x[j] = __fmul_rn(__fmul_rn(x.x[j], by), weight.x[j]);
+  return r;
+}
+
+// The chunk turned by its share c, s of a row of them.  Interleaved: its own four pairs.  Halves: `y` holds the other sides of its
+// eight channels.  Each product and sum is rounded by itself, so that a cache filled by any route holds the same bits.  (Scalar
+// instructions: the packed ones want their pairs in neighbouring registers and spend more on moves than they save, and a packed sum
+// behind packed products was fused with one of them, which rounds once.)
+__device__ __forceinline__ Chunk turn_pairs(const float* c, const float* s, const Chunk& x) {
+  const float4 cc = *reinterpret_cast<const float4*>(c), ss = *reinterpret_cast<const float4*>(s);
+  const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
+  Chunk r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    r.x[2 * j] = __fsub_rn(__fmul_rn(x.x[2 * j], cv[j]), __fmul_rn(x.x[2 * j + 1], sv[j]));
+    r.x[2 * j + 1] = __fadd_rn(__fmul_rn(x.x[2 * j], sv[j]), __fmul_rn(x.x[2 * j + 1], cv[j]));
+  }
+  return r;
+}
+__device__ __forceinline__ Chunk turn_halves(const float* c, const float* s, const Chunk& x, const Chunk& y, float sign) {
+  Chunk r;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const float4 cc = reinterpret_cast<const float4*>(c)[g], ss = reinterpret_cast<const float4*>(s)[g];
+    const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)      // a first side takes away what a second side adds: x c - y s and x c + y s round alike
+      r.x[4 * g + j] = __fadd_rn(__fmul_rn(x.x[4 * g + j], cv[j]), __fmul_rn(y.x[4 * g + j], __fmul_rn(sv[j], sign)));
+  }
+  return r;
+}
+
+// the chunk that another lane holds
+__device__ __forceinline__ Chunk chunk_of(const Chunk& x, int lane) {
+  Chunk r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r.x[j] = __shfl_sync(0xffffffffu, x.x[j], lane);
+  return r;
+}
+
+}  // namespace sparkattn
