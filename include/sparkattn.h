@@ -60,7 +60,8 @@ typedef enum {
   SPARKATTN_E_CUDA = -5,              /* launch or driver error; cudaGetLastError has the detail       */
   SPARKATTN_E_DEVICE_TIMEOUT = -6,    /* a bounded device-side wait expired (device status word)       */
   SPARKATTN_E_BAD_INDEX = -7,         /* a kept block index outside [0, nb) (device status word)       */
-  SPARKATTN_E_NO_DEVICE = -8          /* no CUDA device / driver entry point unavailable               */
+  SPARKATTN_E_NO_DEVICE = -8,         /* no CUDA device / driver entry point unavailable               */
+  SPARKATTN_E_OUT_OF_PAGES = -9       /* fewer free pages than a reservation asks for (device status word) */
 } sparkattn_status;
 
 typedef enum { SPARKATTN_BF16 = 0, SPARKATTN_FP8_E4M3 = 1, SPARKATTN_FP32 = 2 /* weights of norms only */ } sparkattn_dtype;
@@ -571,6 +572,94 @@ int sparkattn_cache_fwd_sink(const sparkattn_cache_t* cache, const sparkattn_bat
                              const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                              int32_t frame_tokens, int32_t window_frames, int32_t sink_tokens, float softmax_scale,
                              const sparkattn_rows_t* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The book of a paged cache: which sequence holds which pages of the pool.  The tables name the pages, refs counts for every page how many entries
+ * of tables name it (0: free); whoever keeps a page for another reason, a prompt that is asked for again for instance, adds 1 of its own.
+ * Every layer has pools of its own; the book is one for all, and the calls that move pages leave (from, to) pairs that
+ * sparkattn_cache_copy_pages takes once for each layer.  Nothing here waits for the host: a captured graph can reserve, append,
+ * attend and trim step after step.
+ *
+ * An entry of a table is a page, or -1 where a sequence has none.  The calls write table, counts and lengths to where they are told, which
+ * may be where they come from (but for sparkattn_pages_fork's tables and lengths); entries that name no page of the pool count as none.
+ * Free pages are handed out in ascending order, in the order of the sequences: the same call gives the same book.
+ */
+typedef struct {
+  uint32_t struct_size; /* sizeof(sparkattn_book_t)                                           */
+  uint32_t version;     /* SPARKATTN_VERSION                                                  */
+  int32_t B;            /* sequences, at most 4096                                            */
+  int32_t max_pages;    /* columns of page_table; B * max_pages < 2^31                        */
+  int32_t pages;        /* pages in the pool, at most 2^30                                    */
+  int32_t page;         /* tokens per page: 16, 32, 64 or 128                                 */
+  const int32_t* page_table; /* [B, max_pages]                                                */
+  const int32_t* refs;       /* [pages]                                                       */
+} sparkattn_book_t;
+
+/* Bytes of device workspace, 256-byte aligned, that each of the four calls needs (0: unsupported arguments); first word = device status. */
+size_t sparkattn_pages_workspace_bytes(const sparkattn_book_t* book);
+
+/*
+ * Sequence b of the new batch goes on from sequence parent[b] of the old one: fork (the same parent several times), reorder, and drop (a sequence
+ * that is nobody's parent gives its pages back).  Children share their parent's pages, the partly filled last one too, until
+ * sparkattn_pages_reserve finds that both go on in it.
+ * kv_len     : in,  int32 [B]
+ * parent     : in,  int32 [B_out], entries in [-1, B); -1: an empty sequence (so does any other number, which is reported)
+ * B_out      : sequences of the new batch, at most 4096
+ * table_out  : out, int32 [B_out, max_pages];  kv_len_out : out, int32 [B_out];  refs_out : out, int32 [pages], may be refs
+ * Device errors (SPARKATTN_E_BAD_INDEX): a parent outside [-1, B); in rows whose number of users changes, an entry outside [-1, pages) or a page
+ * whose count falls below 0.
+ */
+int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* parent, int32_t B_out, int32_t* table_out,
+                         int32_t* kv_len_out, int32_t* refs_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Pages for the tokens kv_len[b] .. kv_new[b] - 1 of every sequence, in front of sparkattn_cache_append: the columns that these tokens begin get
+ * free pages (those that have one keep it).  Where the token kv_len[b] falls into a page that others hold as well, it is replaced
+ * by a free one, and the pair (src, dst) says what has to be copied; of the sequences that go on in one page the first keeps it if nobody
+ * else holds it.  All or nothing: where the pool has fewer free pages than that, the book stays as it was, and the status is
+ * SPARKATTN_E_OUT_OF_PAGES, its detail the number of pages that are missing.  Nothing may be appended then.
+ * kv_len, kv_new : in,  int32 [B], 0 <= kv_len <= kv_new <= max_pages * page
+ * src, dst   : out, int32 [B]: pages to copy for sequence b, or -1 and -1
+ * table_out, refs_out : out, may be page_table and refs
+ * Device errors (SPARKATTN_E_BAD_INDEX): lengths that are not so (the sequence is left out), a partly filled page that is none.
+ */
+int sparkattn_pages_reserve(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out,
+                            int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Gives back the pages that no token from position kv_len[b] on reads, under the rules of sparkattn_cache_fwd_sink: those that lie
+ * between the first sink_tokens tokens and the window of the next token, and those behind the sequence's length (tokens that were
+ * drafted and not taken; kv_len 0: all of the sequence's).  Their entries become -1.
+ * kv_len     : in,  int32 [B]
+ * frame_tokens, window_frames, sink_tokens : as in that call; window_frames 0: every token reads all earlier ones
+ * Device errors (SPARKATTN_E_BAD_INDEX): a length outside [0, max_pages * page] (the sequence stays as it is), an entry among those given back that
+ * names no page, a page whose count falls below 0.
+ */
+int sparkattn_pages_trim(const sparkattn_book_t* book, const int32_t* kv_len, int32_t frame_tokens, int32_t window_frames, int32_t sink_tokens,
+                         int32_t* table_out, int32_t* refs_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Moves the pages in use to the front of the pool: with n of them, the pages from n on go, in ascending order, to the free ones below n.
+ * The book has to hold every table that names pages of the pool.  The pages themselves move with sparkattn_cache_copy_pages, which has to
+ * come before anything reads or appends by the new table.
+ * src, dst   : out, int32 [pages / 2]: the pairs, then -1
+ * Device errors (SPARKATTN_E_BAD_INDEX): an entry that names no page, or one that nobody holds (it becomes -1).
+ */
+int sparkattn_pages_compact(const sparkattn_book_t* book, int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Pages src[i] of one pool to pages dst[i] of another, or of the same (the same pointers and the same struct): keys, values and scales.
+ * from, to   : dtype, H, page and d alike; pages and strides of their own
+ * src, dst   : in,  int32 [n], n >= 0; pairs of -1 and -1 are passed over
+ * workspace  : >= 256 bytes, 256-byte aligned; the status word
+ * Device errors (SPARKATTN_E_BAD_INDEX): a number outside its pool (that pair is passed over); a page that is written twice, or written and
+ * read (what such a page then holds is undefined).
+ */
+int sparkattn_cache_copy_pages(const sparkattn_cache_t* from, const void* k_from, const void* v_from, const float* k_scale_from,
+                               const float* v_scale_from, const sparkattn_cache_t* to, void* k_to, void* v_to, float* k_scale_to,
+                               float* v_scale_to, const int32_t* src, const int32_t* dst, int32_t n, void* workspace, size_t workspace_bytes,
+                               void* cuda_stream);
 
 #ifdef __cplusplus
 }

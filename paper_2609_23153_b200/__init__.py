@@ -31,6 +31,7 @@ E_CUDA = -5
 E_DEVICE_TIMEOUT = -6
 E_BAD_INDEX = -7
 E_NO_DEVICE = -8
+E_OUT_OF_PAGES = -9
 
 BF16 = 0
 FP8_E4M3 = 1
@@ -45,7 +46,8 @@ EXPORTS = (
     "sparkattn_brick_layout", "sparkattn_gather_tokens", "sparkattn_select_padded", "sparkattn_fwd_padded",
     "sparkattn_quant_fp8_pooled", "sparkattn_select_pooled", "sparkattn_fwd_gated_workspace_bytes", "sparkattn_fwd_gated",
     "sparkattn_cache_workspace_bytes", "sparkattn_cache_append", "sparkattn_cache_fwd", "sparkattn_cache_fwd_sink",
-    "sparkattn_cache_append_norm", "sparkattn_norm_rotate",
+    "sparkattn_cache_append_norm", "sparkattn_norm_rotate", "sparkattn_pages_workspace_bytes", "sparkattn_pages_fork",
+    "sparkattn_pages_reserve", "sparkattn_pages_trim", "sparkattn_pages_compact", "sparkattn_cache_copy_pages",
 )
 
 
@@ -96,6 +98,15 @@ class RotaryShape(ctypes.Structure):
     ]
 
 
+class BookShape(ctypes.Structure):
+    """Mirror of ``sparkattn_book_t``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("version", ctypes.c_uint32),
+        ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("pages", ctypes.c_int32), ("page", ctypes.c_int32),
+        ("page_table", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+    ]
+
+
 class NormShape(ctypes.Structure):
     """Mirror of ``sparkattn_norm_t``."""
     _fields_ = [
@@ -115,7 +126,8 @@ class SparkAttnError(RuntimeError):
 _BOUND = ("workspace_bytes", "select", "select_window", "select_padded", "select_pooled", "quant_fp8", "quant_fp8_pooled",
           "quant_fp8_per_token", "fwd", "fwd_window", "fwd_padded", "gather_tokens", "comp_workspace_bytes", "comp_state", "comp_apply",
           "fwd_gated_workspace_bytes", "fwd_gated", "cache_workspace_bytes", "cache_append", "cache_fwd",
-          "cache_fwd_sink", "cache_append_norm", "norm_rotate")
+          "cache_fwd_sink", "cache_append_norm", "norm_rotate", "pages_workspace_bytes", "pages_fork", "pages_reserve", "pages_trim",
+          "pages_compact", "cache_copy_pages")
 _NO_WORKSPACE = 1        # the library does not serve the shape: the workspace query returned 0
 
 _lib = None
@@ -198,6 +210,16 @@ def lib() -> ctypes.CDLL:
         L.sparkattn_cache_append_norm.argtypes = [cp, bp, np, ctypes.POINTER(RotaryShape), rp, i32, rp, rp, vp, vp, vp, vp, rp, vp, sz, vp]
         L.sparkattn_norm_rotate.restype = ctypes.c_int
         L.sparkattn_norm_rotate.argtypes = [sp, vp, sp, vp, sp, vp, sp, vp, np, ctypes.POINTER(RotaryShape), vp, sz, vp]
+        kp = ctypes.POINTER(BookShape)
+        L.sparkattn_pages_workspace_bytes.restype = sz
+        L.sparkattn_pages_workspace_bytes.argtypes = [kp]
+        for name, args in (("fork", [vp, vp, i32, vp, vp, vp]), ("reserve", [vp, vp, vp, vp, vp, vp]), ("trim", [vp, i32, i32, i32, vp, vp]),
+                           ("compact", [vp, vp, vp, vp])):
+            call = getattr(L, "sparkattn_pages_" + name)
+            call.restype = ctypes.c_int
+            call.argtypes = [kp, *args, vp, sz, vp]
+        L.sparkattn_cache_copy_pages.restype = ctypes.c_int
+        L.sparkattn_cache_copy_pages.argtypes = [cp, vp, vp, vp, vp, cp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
         L.sparkattn_cache_fwd_sink.restype = ctypes.c_int
         L.sparkattn_cache_fwd_sink.argtypes = [cp, bp, rp, i32, vp, vp, vp, vp, i32, i32, i32, ctypes.c_float, rp, vp, vp, sz, vp]
         from . import _sparkattn
@@ -571,3 +593,64 @@ def cache_fwd(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, kv_len:
     if check_status:
         _check(read_status(workspace, stream), "sparkattn_cache_fwd (device status)")
     return (out, lse) if return_lse else out
+
+
+def _book(rc: int, what: str, workspace: torch.Tensor, stream: Optional[torch.cuda.Stream], check_status: bool) -> None:
+    if rc != OK:
+        _check(rc, what)
+    if check_status:
+        _check(read_status(workspace, stream), what + " (device status)")
+
+
+def pages_fork(page_table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, parent: torch.Tensor, *,
+               page_table_out: Optional[torch.Tensor] = None, kv_len_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
+    """``sparkattn_pages_fork``: sequence b of the new batch goes on from sequence ``parent[b]`` of the old one (int32; -1: empty); what is nobody's
+    parent gives its pages back.  page_table int32 [B, max_pages] (-1: none), kv_len int32 [B], refs int32 [pages] (users of each page).
+    Returns (page_table, kv_len, refs); ``refs_out`` may be refs."""
+    rc, table, length, refs, workspace = _calls().pages_fork(page_table, kv_len, refs, parent, page_table_out, kv_len_out, refs_out, workspace,
+                                                             None if stream is None else stream.cuda_stream)
+    _book(rc, "sparkattn_pages_fork", workspace, stream, check_status)
+    return table, length, refs
+
+
+def pages_reserve(page_table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, kv_new: torch.Tensor, page: int, *,
+                  page_table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, src: Optional[torch.Tensor] = None,
+                  dst: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                  check_status: bool = False):
+    """``sparkattn_pages_reserve``: pages for the tokens kv_len[b] .. kv_new[b] - 1 of every sequence, pages of ``page`` tokens, in front of
+    :func:`cache_append`.  Returns (page_table, refs, src, dst): src, dst int32 [B] go to :func:`cache_copy_pages`, for every layer's cache.  All
+    or nothing: with too few free pages the status is E_OUT_OF_PAGES and the book stays as it was.  The outputs may be the inputs."""
+    rc, table, refs, src, dst, workspace = _calls().pages_reserve(page_table, kv_len, refs, kv_new, page, page_table_out, refs_out, src, dst, workspace,
+                                                                  None if stream is None else stream.cuda_stream)
+    _book(rc, "sparkattn_pages_reserve", workspace, stream, check_status)
+    return table, refs, src, dst
+
+
+def pages_trim(page_table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, page: int, *, frame_tokens: int = 1, window: int = 0, sink: int = 0,
+               page_table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
+    """``sparkattn_pages_trim``: gives back the pages that no token from position kv_len[b] on reads through :func:`cache_fwd` with the same
+    ``frame_tokens``, ``window`` and ``sink``, and those behind kv_len[b].  Returns (page_table, refs); they may be the inputs."""
+    rc, table, refs, workspace = _calls().pages_trim(page_table, kv_len, refs, page, frame_tokens, window, sink, page_table_out, refs_out, workspace,
+                                                     None if stream is None else stream.cuda_stream)
+    _book(rc, "sparkattn_pages_trim", workspace, stream, check_status)
+    return table, refs
+
+
+def pages_compact(page_table: torch.Tensor, refs: torch.Tensor, *, page_table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None,
+                  src: Optional[torch.Tensor] = None, dst: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
+    """``sparkattn_pages_compact``: the pages in use become the pool's first.  Returns (page_table, refs, src, dst): src, dst int32 [pages // 2] go
+    to :func:`cache_copy_pages`, for every layer's cache, before the new table is used.  The outputs may be the inputs."""
+    rc, table, refs, src, dst, workspace = _calls().pages_compact(page_table, refs, page_table_out, refs_out, src, dst, workspace,
+                                                                  None if stream is None else stream.cuda_stream)
+    _book(rc, "sparkattn_pages_compact", workspace, stream, check_status)
+    return table, refs, src, dst
+
+
+def cache_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, *, to: Optional[KVCache] = None, workspace: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None, check_status: bool = False) -> None:
+    """``sparkattn_cache_copy_pages``: page src[i] of the cache to page dst[i] of it, or of the cache ``to`` (int32; pairs of -1 are passed over)."""
+    rc, workspace = _calls().cache_copy_pages(*cache, *(cache if to is None else to), src, dst, workspace, None if stream is None else stream.cuda_stream)
+    _book(rc, "sparkattn_cache_copy_pages", workspace, stream, check_status)

@@ -50,6 +50,7 @@ const char* sparkattn_status_string(int status) {
     case SPARKATTN_E_DEVICE_TIMEOUT: return "device-side wait timed out";
     case SPARKATTN_E_BAD_INDEX: return "kept block index out of range";
     case SPARKATTN_E_NO_DEVICE: return "no CUDA device or driver entry point";
+    case SPARKATTN_E_OUT_OF_PAGES: return "fewer free pages than asked for";
     default: return "unknown status";
   }
 }
@@ -675,6 +676,87 @@ int sparkattn_cache_fwd_sink(const sparkattn_cache_t* cache, const sparkattn_bat
   if (workspace_bytes < cache_fwd_workspace_bytes(*cache, *batch, H)) return SPARKATTN_E_WORKSPACE_TOO_SMALL;
   return launch_cache_fwd(*cache, *batch, *q, H, k_cache, v_cache, k_scale, v_scale, frame_tokens, window_frames, sink_tokens, softmax_scale, *out,
                           lse, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// ------------------------------------------------------------------------------------------------ the cache's pages
+namespace {
+int check_book(const sparkattn_book_t* b) {
+  if (b == nullptr || b->struct_size != sizeof(sparkattn_book_t) || b->version != SPARKATTN_VERSION) return SPARKATTN_E_INVALID_ARG;
+  if (b->B < 1 || b->max_pages < 1 || b->pages < 1) return SPARKATTN_E_INVALID_ARG;
+  if (b->B > kCacheMaxSequences || (long long)b->B * b->max_pages > 0x7fffffffLL || b->pages > 1 << 30) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  if (b->page != 16 && b->page != 32 && b->page != 64 && b->page != 128) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  return SPARKATTN_OK;
+}
+int check_book_call(const sparkattn_book_t* b, const void* table_out, const void* refs_out, const void* workspace, size_t workspace_bytes) {
+  const int rc = check_book(b);
+  if (rc != SPARKATTN_OK) return rc;
+  if (!b->page_table || !b->refs || !table_out || !refs_out || !workspace) return SPARKATTN_E_INVALID_ARG;
+  if (!aligned256(workspace)) return SPARKATTN_E_MISALIGNED;
+  return workspace_bytes < pages_workspace_bytes(*b) ? SPARKATTN_E_WORKSPACE_TOO_SMALL : SPARKATTN_OK;
+}
+// a pool by itself
+int check_pool(const sparkattn_cache_t* c, const void* k, const void* v, const float* k_scale, const float* v_scale) {
+  const sparkattn_batch_t one{sizeof(sparkattn_batch_t), SPARKATTN_VERSION, 1, 1, 1, 1, nullptr, nullptr, nullptr};
+  const int rc = check_cache(c, &one);
+  if (rc != SPARKATTN_OK) return rc;
+  if (!k || !v || (c->dtype == SPARKATTN_FP8_E4M3 ? !k_scale || !v_scale : k_scale || v_scale)) return SPARKATTN_E_INVALID_ARG;
+  return !aligned16(k) || !aligned16(v) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
+}
+}  // namespace
+
+size_t sparkattn_pages_workspace_bytes(const sparkattn_book_t* book) { return check_book(book) == SPARKATTN_OK ? pages_workspace_bytes(*book) : 0; }
+
+int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* parent, int32_t B_out, int32_t* table_out,
+                         int32_t* kv_len_out, int32_t* refs_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const int rc = check_book_call(book, table_out, refs_out, workspace, workspace_bytes);
+  if (rc != SPARKATTN_OK) return rc;
+  if (!kv_len || !parent || !kv_len_out || B_out < 1 || table_out == book->page_table || kv_len_out == kv_len) return SPARKATTN_E_INVALID_ARG;
+  if (B_out > kCacheMaxSequences || (long long)B_out * book->max_pages > 0x7fffffffLL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  return launch_pages_fork(*book, kv_len, parent, B_out, table_out, kv_len_out, refs_out, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int sparkattn_pages_reserve(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out,
+                            int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const int rc = check_book_call(book, table_out, refs_out, workspace, workspace_bytes);
+  if (rc != SPARKATTN_OK) return rc;
+  if (!kv_len || !kv_new || !src || !dst) return SPARKATTN_E_INVALID_ARG;
+  return launch_pages_reserve(*book, kv_len, kv_new, table_out, refs_out, src, dst, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int sparkattn_pages_trim(const sparkattn_book_t* book, const int32_t* kv_len, int32_t frame_tokens, int32_t window_frames, int32_t sink_tokens,
+                         int32_t* table_out, int32_t* refs_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const int rc = check_book_call(book, table_out, refs_out, workspace, workspace_bytes);
+  if (rc != SPARKATTN_OK) return rc;
+  if (!kv_len || frame_tokens < 0 || window_frames < 0 || sink_tokens < 0 || (frame_tokens == 0 && window_frames != 0)) return SPARKATTN_E_INVALID_ARG;
+  return launch_pages_trim(*book, kv_len, frame_tokens, window_frames, sink_tokens, table_out, refs_out, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int sparkattn_pages_compact(const sparkattn_book_t* book, int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream) {
+  const int rc = check_book_call(book, table_out, refs_out, workspace, workspace_bytes);
+  if (rc != SPARKATTN_OK) return rc;
+  if (book->pages > 1 && (!src || !dst)) return SPARKATTN_E_INVALID_ARG;
+  return launch_pages_compact(*book, table_out, refs_out, src, dst, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int sparkattn_cache_copy_pages(const sparkattn_cache_t* from, const void* k_from, const void* v_from, const float* k_scale_from,
+                               const float* v_scale_from, const sparkattn_cache_t* to, void* k_to, void* v_to, float* k_scale_to,
+                               float* v_scale_to, const int32_t* src, const int32_t* dst, int32_t n, void* workspace, size_t workspace_bytes,
+                               void* cuda_stream) {
+  int rc = check_pool(from, k_from, v_from, k_scale_from, v_scale_from);
+  if (rc == SPARKATTN_OK) rc = check_pool(to, k_to, v_to, k_scale_to, v_scale_to);
+  if (rc != SPARKATTN_OK) return rc;
+  if (from->dtype != to->dtype || from->H != to->H || from->page != to->page || from->d != to->d) return SPARKATTN_E_INVALID_ARG;
+  // one pool, or two
+  const bool same = k_from == k_to;
+  if (same != (v_from == v_to) || (same && memcmp(from, to, sizeof(*from)) != 0)) return SPARKATTN_E_INVALID_ARG;
+  if (from->dtype == SPARKATTN_FP8_E4M3 && (same != (k_scale_from == k_scale_to) || same != (v_scale_from == v_scale_to))) return SPARKATTN_E_INVALID_ARG;
+  if (n < 0 || (n > 0 && (!src || !dst)) || !workspace) return SPARKATTN_E_INVALID_ARG;
+  if (!aligned256(workspace)) return SPARKATTN_E_MISALIGNED;
+  if (workspace_bytes < kWorkspaceHeaderBytes) return SPARKATTN_E_WORKSPACE_TOO_SMALL;
+  const PagePools in{const_cast<void*>(k_from), const_cast<void*>(v_from), const_cast<float*>(k_scale_from), const_cast<float*>(v_scale_from)};
+  const PagePools out{k_to, v_to, k_scale_to, v_scale_to};
+  return launch_copy_pages(*from, in, *to, out, src, dst, n, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
 }  // extern "C"

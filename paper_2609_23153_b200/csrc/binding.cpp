@@ -45,6 +45,12 @@ struct Library {
   decltype(&sparkattn_cache_fwd_sink) cache_fwd_sink;
   decltype(&sparkattn_cache_append_norm) cache_append_norm;
   decltype(&sparkattn_norm_rotate) norm_rotate;
+  decltype(&sparkattn_pages_workspace_bytes) pages_workspace_bytes;
+  decltype(&sparkattn_pages_fork) pages_fork;
+  decltype(&sparkattn_pages_reserve) pages_reserve;
+  decltype(&sparkattn_pages_trim) pages_trim;
+  decltype(&sparkattn_pages_compact) pages_compact;
+  decltype(&sparkattn_cache_copy_pages) cache_copy_pages;
 };
 Library g_lib{};
 
@@ -459,23 +465,16 @@ PyObject* fwd_gated(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// The paged cache: pools, scales and the batch, as both calls take them.
-struct Cache {
-  at::Tensor k, v, k_scale, v_scale, table, len, start;
-  sparkattn_cache_t c{};
-  sparkattn_batch_t b{};
-  explicit Cache(Args& a) {
+// The pools of a paged cache.
+struct Pools {
+  at::Tensor k, v, k_scale, v_scale;
+  explicit Pools(Args& a) {
     k = a.tensor();
     v = a.tensor();
     k_scale = a.optional_tensor();
     v_scale = a.optional_tensor();
-    table = a.tensor();
-    len = a.tensor();
-    start = a.optional_tensor();
-    b.max_new = a.i32();
   }
-  // `rows`: a [T, heads, d] tensor of the call
-  void describe(const at::Tensor& rows) {
+  void describe(sparkattn_cache_t& c) const {
     TORCH_CHECK_VALUE(k.dim() == 4 && k.stride(3) == 1, "expected pools [pages, H, page, d] with a contiguous last dimension");
     same_layout(k, v);
     const at::ScalarType type = k.scalar_type();
@@ -485,17 +484,36 @@ struct Cache {
     for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&k_scale, &v_scale})
       TORCH_CHECK_VALUE(!x->defined() || (x->scalar_type() == at::kFloat && x->dim() == 2 && x->is_contiguous() && x->size(0) == k.size(0) && x->size(1) == k.size(1)),
                         "scales are contiguous float32 [pages, H]");
-    TORCH_CHECK_VALUE(table.scalar_type() == at::kInt && table.dim() == 2 && table.is_contiguous(), "page_table is a contiguous int32 [B, max_pages]");
-    TORCH_CHECK_VALUE(len.scalar_type() == at::kInt && len.is_contiguous() && len.dim() == 1 && len.size(0) == table.size(0), "kv_len is a contiguous int32 [B]");
-    TORCH_CHECK_VALUE(!start.defined() || (start.scalar_type() == at::kInt && start.is_contiguous() && start.dim() == 1 && start.size(0) == table.size(0) + 1),
-                      "q_start is a contiguous int32 [B + 1]");
-    for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&v, &k_scale, &v_scale, &table, &len, &start, &rows})
+    for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&v, &k_scale, &v_scale})
       TORCH_CHECK_VALUE(!x->defined() || x->device() == k.device(), "tensors of one call must be on one device");
     c.struct_size = sizeof(c);
     c.version = SPARKATTN_VERSION;
     c.dtype = codes ? SPARKATTN_FP8_E4M3 : SPARKATTN_BF16;
     c.pages = (int32_t)k.size(0); c.H = (int32_t)k.size(1); c.page = (int32_t)k.size(2); c.d = (int32_t)k.size(3);
     c.stride_page = k.stride(0); c.stride_h = k.stride(1); c.stride_n = k.stride(2);
+  }
+};
+
+// The paged cache: pools, scales and the batch, as both calls take them.
+struct Cache : Pools {
+  at::Tensor table, len, start;
+  sparkattn_cache_t c{};
+  sparkattn_batch_t b{};
+  explicit Cache(Args& a) : Pools(a) {
+    table = a.tensor();
+    len = a.tensor();
+    start = a.optional_tensor();
+    b.max_new = a.i32();
+  }
+  // `rows`: a [T, heads, d] tensor of the call
+  void describe(const at::Tensor& rows) {
+    Pools::describe(c);
+    TORCH_CHECK_VALUE(table.scalar_type() == at::kInt && table.dim() == 2 && table.is_contiguous(), "page_table is a contiguous int32 [B, max_pages]");
+    TORCH_CHECK_VALUE(len.scalar_type() == at::kInt && len.is_contiguous() && len.dim() == 1 && len.size(0) == table.size(0), "kv_len is a contiguous int32 [B]");
+    TORCH_CHECK_VALUE(!start.defined() || (start.scalar_type() == at::kInt && start.is_contiguous() && start.dim() == 1 && start.size(0) == table.size(0) + 1),
+                      "q_start is a contiguous int32 [B + 1]");
+    for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&table, &len, &start, &rows})
+      TORCH_CHECK_VALUE(!x->defined() || x->device() == k.device(), "tensors of one call must be on one device");
     b.struct_size = sizeof(b);
     b.version = SPARKATTN_VERSION;
     b.B = (int32_t)table.size(0);
@@ -692,6 +710,178 @@ PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// The book of a pool of pages, as its calls take it.
+struct Book {
+  at::Tensor table, len, refs, table_out, refs_out, ws;
+  sparkattn_book_t b{};
+  bool needs_len;
+  explicit Book(Args& a, bool len_too) : needs_len(len_too) {
+    table = a.tensor();
+    if (len_too) len = a.tensor();
+    refs = a.tensor();
+  }
+  // int32 words [n] of the call
+  void words(const at::Tensor& x, int64_t n, const char* what) const {
+    TORCH_CHECK_VALUE(x.scalar_type() == at::kInt && x.dim() == 1 && x.is_contiguous() && x.size(0) == n && x.device() == table.device(), what);
+  }
+  void describe(int32_t page) {
+    TORCH_CHECK_VALUE(table.scalar_type() == at::kInt && table.dim() == 2 && table.is_contiguous(), "page_table is a contiguous int32 [B, max_pages]");
+    TORCH_CHECK_VALUE(refs.scalar_type() == at::kInt && refs.dim() == 1 && refs.is_contiguous() && refs.device() == table.device(),
+                      "refs is a contiguous int32 [pages] on the table's device");
+    if (needs_len) words(len, table.size(0), "kv_len is a contiguous int32 [B] on the table's device");
+    TORCH_CHECK_VALUE(table.is_cuda(), "tensors of a call must be on a CUDA device");
+    b.struct_size = sizeof(b);
+    b.version = SPARKATTN_VERSION;
+    b.B = (int32_t)table.size(0); b.max_pages = (int32_t)table.size(1); b.pages = (int32_t)refs.size(0); b.page = page;
+    b.page_table = iptr(table); b.refs = iptr(refs);
+  }
+  void outputs(at::Tensor given_table, at::Tensor given_refs, at::Tensor given_ws, int64_t rows, const Stream& stream) {
+    table_out = given_table.defined() ? given_table : stream.output({rows, table.size(1)}, at::kInt, table);
+    refs_out = given_refs.defined() ? given_refs : stream.output({refs.size(0)}, at::kInt, refs);
+    TORCH_CHECK_VALUE(table_out.scalar_type() == at::kInt && table_out.dim() == 2 && table_out.is_contiguous() && table_out.size(0) == rows &&
+                          table_out.size(1) == table.size(1) && table_out.device() == table.device(), "the new table is a contiguous int32 [sequences, max_pages]");
+    words(refs_out, refs.size(0), "the new refs are a contiguous int32 [pages]");
+    if (given_ws.defined()) {
+      ws = given_ws;
+    } else {
+      const size_t bytes = g_lib.pages_workspace_bytes(&b);
+      ws = stream.scratch((int64_t)(bytes < 256 ? 256 : bytes), table);      // an unsupported call says why itself
+    }
+    TORCH_CHECK_VALUE(ws.device() == table.device() && ws.is_contiguous() && ws.element_size() == 1, "the workspace is contiguous bytes on the call's device");
+  }
+  at::Tensor pairs(at::Tensor given, int64_t n, const Stream& stream) const {
+    if (!given.defined()) return stream.output({n}, at::kInt, table);
+    words(given, n, "src and dst are contiguous int32 of the call's length");
+    return given;
+  }
+};
+
+// pages_fork(page_table, kv_len, refs, parent, table_out, kv_len_out, refs_out, workspace, stream) -> rc, table, kv_len, refs, workspace
+PyObject* pages_fork(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(9);
+  Book book(a, true);
+  const at::Tensor parent = a.tensor(), table_out = a.optional_tensor();
+  at::Tensor len_out = a.optional_tensor();
+  const at::Tensor refs_out = a.optional_tensor(), ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  book.describe(16);      // (the call does not look at tokens)
+  TORCH_CHECK_VALUE(parent.dim() == 1, "parent is a contiguous int32 [sequences] on the table's device");
+  book.words(parent, parent.size(0), "parent is a contiguous int32 [sequences] on the table's device");
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    book.outputs(table_out, refs_out, ws, parent.size(0), stream);
+    if (!len_out.defined()) len_out = stream.output({parent.size(0)}, at::kInt, parent);
+    book.words(len_out, parent.size(0), "the new lengths are a contiguous int32 [sequences]");
+    rc = g_lib.pages_fork(&book.b, iptr(book.len), iptr(parent), (int32_t)parent.size(0), iptr(book.table_out), iptr(len_out), iptr(book.refs_out), ptr(book.ws),
+                          (size_t)book.ws.numel(), stream);
+  }
+  return result(rc, {book.table_out, len_out, book.refs_out, book.ws});
+  END_HANDLE_TH_ERRORS
+}
+
+// pages_reserve(page_table, kv_len, refs, kv_new, page, table_out, refs_out, src, dst, workspace, stream) -> rc, table, refs, src, dst, workspace
+PyObject* pages_reserve(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(11);
+  Book book(a, true);
+  const at::Tensor kv_new = a.tensor();
+  const int32_t page = a.i32();
+  const at::Tensor table_out = a.optional_tensor(), refs_out = a.optional_tensor();
+  at::Tensor src = a.optional_tensor(), dst = a.optional_tensor();
+  const at::Tensor ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  book.describe(page);
+  book.words(kv_new, book.b.B, "kv_new is a contiguous int32 [B] on the table's device");
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    book.outputs(table_out, refs_out, ws, book.b.B, stream);
+    src = book.pairs(src, book.b.B, stream);
+    dst = book.pairs(dst, book.b.B, stream);
+    rc = g_lib.pages_reserve(&book.b, iptr(book.len), iptr(kv_new), iptr(book.table_out), iptr(book.refs_out), iptr(src), iptr(dst), ptr(book.ws),
+                             (size_t)book.ws.numel(), stream);
+  }
+  return result(rc, {book.table_out, book.refs_out, src, dst, book.ws});
+  END_HANDLE_TH_ERRORS
+}
+
+// pages_trim(page_table, kv_len, refs, page, frame_tokens, window, sink, table_out, refs_out, workspace, stream) -> rc, table, refs, workspace
+PyObject* pages_trim(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(11);
+  Book book(a, true);
+  const int32_t page = a.i32(), frame_tokens = a.i32(), window = a.i32(), sink = a.i32();
+  const at::Tensor table_out = a.optional_tensor(), refs_out = a.optional_tensor(), ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  book.describe(page);
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    book.outputs(table_out, refs_out, ws, book.b.B, stream);
+    rc = g_lib.pages_trim(&book.b, iptr(book.len), frame_tokens, window, sink, iptr(book.table_out), iptr(book.refs_out), ptr(book.ws), (size_t)book.ws.numel(),
+                          stream);
+  }
+  return result(rc, {book.table_out, book.refs_out, book.ws});
+  END_HANDLE_TH_ERRORS
+}
+
+// pages_compact(page_table, refs, table_out, refs_out, src, dst, workspace, stream) -> rc, table, refs, src, dst, workspace
+PyObject* pages_compact(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(8);
+  Book book(a, false);
+  const at::Tensor table_out = a.optional_tensor(), refs_out = a.optional_tensor();
+  at::Tensor src = a.optional_tensor(), dst = a.optional_tensor();
+  const at::Tensor ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  book.describe(16);
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    book.outputs(table_out, refs_out, ws, book.b.B, stream);
+    src = book.pairs(src, book.b.pages / 2, stream);
+    dst = book.pairs(dst, book.b.pages / 2, stream);
+    rc = g_lib.pages_compact(&book.b, iptr(book.table_out), iptr(book.refs_out), iptr(src), iptr(dst), ptr(book.ws), (size_t)book.ws.numel(), stream);
+  }
+  return result(rc, {book.table_out, book.refs_out, src, dst, book.ws});
+  END_HANDLE_TH_ERRORS
+}
+
+// cache_copy_pages(k, v, k_scale, v_scale, k_to, v_to, k_scale_to, v_scale_to, src, dst, workspace, stream) -> rc, workspace
+PyObject* cache_copy_pages(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(argv, n);
+  a.expect(12);
+  Pools from(a), to(a);
+  const at::Tensor src = a.tensor(), dst = a.tensor();
+  at::Tensor ws = a.optional_tensor();
+  const Stream stream = a.stream();
+  sparkattn_cache_t c_from{}, c_to{};
+  from.describe(c_from);
+  to.describe(c_to);
+  TORCH_CHECK_VALUE(src.scalar_type() == at::kInt && src.dim() == 1 && src.is_contiguous() && dst.scalar_type() == at::kInt && dst.is_contiguous() &&
+                        src.sizes() == dst.sizes(), "src and dst are contiguous int32 of one length");
+  for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&to.k, &src, &dst})
+    TORCH_CHECK_VALUE(x->device() == from.k.device(), "tensors of one call must be on one device");
+  TORCH_CHECK_VALUE(from.k.is_cuda(), "tensors of a call must be on a CUDA device");
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    if (!ws.defined()) ws = stream.scratch(256, src);
+    TORCH_CHECK_VALUE(ws.device() == src.device() && ws.is_contiguous() && ws.element_size() == 1, "the workspace is contiguous bytes on the call's device");
+    rc = g_lib.cache_copy_pages(&c_from, ptr(from.k), ptr(from.v), fptr(from.k_scale), fptr(from.v_scale), &c_to, ptr(to.k), ptr(to.v), fptr(to.k_scale),
+                                fptr(to.v_scale), iptr(src), iptr(dst), (int32_t)src.numel(), ptr(ws), (size_t)ws.numel(), stream);
+  }
+  return result(rc, {ws});
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(address of each entry point, in the order of Library)
 PyObject* bind(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -713,7 +903,9 @@ PyMethodDef g_methods[] = {method<bind>("bind"), method<select>("select"), metho
                            method<quant_fp8_per_token>("quant_fp8_per_token"), method<fwd>("fwd"), method<gather_tokens>("gather_tokens"),
                            method<comp_state>("comp_state"), method<comp_apply>("comp_apply"), method<fwd_gated>("fwd_gated"),
                            method<cache_append>("cache_append"), method<cache_fwd>("cache_fwd"),
-                           method<norm_rotate>("norm_rotate"), {nullptr, nullptr, 0, nullptr}};
+                           method<norm_rotate>("norm_rotate"), method<pages_fork>("pages_fork"), method<pages_reserve>("pages_reserve"),
+                           method<pages_trim>("pages_trim"), method<pages_compact>("pages_compact"), method<cache_copy_pages>("cache_copy_pages"),
+                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_sparkattn", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

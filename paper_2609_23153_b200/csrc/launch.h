@@ -122,6 +122,24 @@ constexpr int kCacheMaxSequences = 4096;   // their lengths are laid out in shar
 int launch_cache_append(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_norm_t* norm, const sparkattn_rotary_t* rotary,
                         const sparkattn_rows_t* q, int H, const sparkattn_rows_t& k, const sparkattn_rows_t& v, void* k_cache, void* v_cache, float* k_scale,
                         float* v_scale, const sparkattn_rows_t* q_out, void* workspace, cudaStream_t stream);
+// pages.cu: the book of a pool of pages, and the pages themselves
+size_t pages_workspace_bytes(const sparkattn_book_t& b);
+int launch_pages_fork(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* parent, int B_out, int32_t* table_out, int32_t* kv_len_out,
+                      int32_t* refs_out, void* workspace, cudaStream_t stream);
+int launch_pages_trim(const sparkattn_book_t& book, const int32_t* kv_len, int frame, int window, int sink, int32_t* table_out, int32_t* refs_out,
+                      void* workspace, cudaStream_t stream);
+int launch_pages_reserve(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out, int32_t* src,
+                         int32_t* dst, void* workspace, cudaStream_t stream);
+int launch_pages_compact(const sparkattn_book_t& book, int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace, cudaStream_t stream);
+struct PagePools {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+};
+int launch_copy_pages(const sparkattn_cache_t& from, const PagePools& in, const sparkattn_cache_t& to, const PagePools& out, const int32_t* src,
+                      const int32_t* dst, int n, void* workspace, cudaStream_t stream);
+
 bool cache_work_fits(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);
 size_t cache_fwd_workspace_bytes(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int H);
 int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const sparkattn_rows_t& q, int H, const void* k_cache,

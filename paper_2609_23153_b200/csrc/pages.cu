@@ -1,0 +1,739 @@
+// The book of a paged cache: who holds which pages.  sparkattn_pages_fork, _reserve, _trim, _compact keep it, sparkattn_cache_copy_pages moves
+// what the pages hold.
+//
+// The book is a few hundred thousand words at most, so what a step costs is launches and chains of loads.  Each call is one launch (compact: two).
+// What has to happen in order, counting, handing out, adjusting counts, is the work of one thread-block cluster of up to sixteen CTAs, whose
+// barrier stands between the steps and through whose shared memory the counts go; a chain of launches would take 2 us a step.  Tables that go
+// to another place are copied meanwhile by the grid's other clusters.  Counts change by integer additions, so their order does not matter, and free
+// pages are handed out in ascending order: the same call gives the same book.
+#include <algorithm>
+
+#include "cache.h"
+#include "tmap.h"
+
+namespace sparkattn {
+
+constexpr int kBookThreads = 512, kBookWarps = kBookThreads / 32, kBookClusterMax = 16;
+
+struct BookView {
+  const int32_t* table;        // [B, max_pages]
+  const int32_t* refs;         // [pages]
+  int32_t* table_out;
+  int32_t* refs_out;
+  int B, max_pages, pages, shift;
+};
+inline BookView make_book_view(const sparkattn_book_t& b, int32_t* table_out, int32_t* refs_out) {
+  int shift = 0;
+  while ((1 << shift) < b.page) ++shift;
+  return {b.page_table, b.refs, table_out, refs_out, b.B, b.max_pages, b.pages, shift};
+}
+__device__ __forceinline__ int pages_of(const BookView& v, int tokens) { return (int)(((long long)tokens + (1 << v.shift) - 1) >> v.shift); }
+__device__ __forceinline__ bool fits_table(const BookView& v, int tokens) { return tokens >= 0 && tokens <= (long long)v.max_pages << v.shift; }
+
+// What one cluster knows together
+struct BookShared {
+  int status[kBookClusterMax][2];      // of the first CTA: what every CTA has found
+  int bad[2];                          // what this CTA has found: a code, a number
+  int count[kBookWarps];               // per warp
+  int scan[kBookWarps];
+};
+__device__ __forceinline__ int cluster_ld_int(const int* at, int rank) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_map(smem_u32(at), rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_st_int(const int* at, int rank, int v) {
+  asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_map(smem_u32(at), rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void found(BookShared& s, int code, int detail) {
+  if (atomicCAS(&s.bad[0], 0, code) == 0) s.bad[1] = detail;
+}
+__device__ __forceinline__ void book_barrier() {
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
+}
+__device__ __forceinline__ void book_begin(BookShared& s) {
+  if (threadIdx.x == 0) s.bad[0] = s.bad[1] = 0;
+  __syncthreads();
+}
+// The end of the first cluster's work: its first CTA writes the status word, which nobody else does.  (The barriers before this one say
+// that the first CTA is there.)
+__device__ __forceinline__ void book_end(BookShared& s, int rank, int ranks, int32_t* status) {
+  __syncthreads();
+  if (threadIdx.x < 2) cluster_st_int(&s.status[rank][threadIdx.x], 0, s.bad[threadIdx.x]);
+  book_barrier();
+  if (rank == 0 && threadIdx.x == 0) {
+    unsigned long long word = 0;
+    for (int i = ranks - 1; i >= 0; --i)
+      if (s.status[i][0] != 0) word = (unsigned long long)(uint32_t)s.status[i][1] << 32 | (uint32_t)s.status[i][0];
+    *reinterpret_cast<unsigned long long*>(status) = word;
+  }
+}
+// The pool in runs of the cluster's warps, so that ranks within it need one exchange of counts and no further barriers.
+struct PoolRun {
+  int first, last;
+};
+__device__ __forceinline__ int run_length(int pages, int ranks) {
+  const int warps = ranks * kBookWarps;
+  return ((pages + warps - 1) / warps + 31) & ~31;
+}
+__device__ __forceinline__ PoolRun run_of_warp(int pages, int ranks, int rank) {
+  const int each = run_length(pages, ranks), w = rank * kBookWarps + (threadIdx.x >> 5);
+  const int first = (int)min((long long)w * each, (long long)pages);
+  return {first, (int)min((long long)first + each, (long long)pages)};
+}
+// Counts of the runs, s.count of every CTA (behind a cluster barrier): (those in front of this warp's run, all).  Whole CTA.
+__device__ __forceinline__ int2 in_front(BookShared& s, int rank, int ranks) {
+  int mine = 0, all = 0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int i = lane; i < ranks * kBookWarps; i += 32) {
+    const int n = cluster_ld_int(&s.count[i % kBookWarps], i / kBookWarps);
+    all += n;
+    if (i < rank * kBookWarps + warp) mine += n;
+  }
+  return make_int2((int)__reduce_add_sync(0xffffffffu, (unsigned)mine), (int)__reduce_add_sync(0xffffffffu, (unsigned)all));
+}
+// refs -> refs_out (or where they are), and the number of pages of the warp's run for which `counts` holds
+template <typename Counts>
+__device__ __forceinline__ int count_run(const BookView& v, const PoolRun& run, Counts counts) {
+  int n = 0;
+  const int lane = threadIdx.x & 31;
+  const bool copy = v.refs_out != v.refs;
+#pragma unroll 1
+  for (int p0 = run.first + lane; p0 < run.last; p0 += 32 * 8) {
+    int r[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) r[u] = p0 + 32 * u < run.last ? v.refs[p0 + 32 * u] : 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (p0 + 32 * u < run.last) {
+        n += counts(r[u]);
+        if (copy) v.refs_out[p0 + 32 * u] = r[u];
+      }
+  }
+  return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+}
+
+// Table rows to their other place, a warp taking up to 256 columns of a row: row b from row from(b) (-1: none), an entry of column i as
+// entry(b, i, e); keep(b, i): it is not this function's.
+constexpr int kCopyColumns = 256;
+template <typename From, typename Entry, typename Keep>
+__device__ __forceinline__ void copy_table(const BookView& v, int rows, int cta, int ctas, From from, Entry entry, Keep keep) {
+  const int segments = (v.max_pages + kCopyColumns - 1) / kCopyColumns, lane = threadIdx.x & 31;
+  const long long items = (long long)rows * segments;
+  for (long long item = (long long)cta * kBookWarps + (threadIdx.x >> 5); item < items; item += (long long)ctas * kBookWarps) {
+    const int b = (int)(item / segments), c0 = (int)(item - (long long)b * segments) * kCopyColumns + lane, source = from(b);
+    const int32_t* in = v.table + (int64_t)source * v.max_pages;
+    int32_t* out = v.table_out + (int64_t)b * v.max_pages;
+    int e[kCopyColumns / 32];
+#pragma unroll
+    for (int u = 0; u < kCopyColumns / 32; ++u) {
+      const int i = c0 + 32 * u;
+      e[u] = source >= 0 && i < v.max_pages ? in[i] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyColumns / 32; ++u) {
+      const int i = c0 + 32 * u;
+      if (i < v.max_pages && !keep(b, i)) out[i] = entry(b, i, e[u]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- fork
+struct ForkParams {
+  BookView v;
+  const int32_t* kv_len;
+  const int32_t* parent;
+  int32_t* kv_len_out;
+  int B_out, ranks;
+  int32_t* status;
+};
+// Every row's number of users changes by the sequences that go on from it less one; its pages' counts do with it.
+__global__ void __launch_bounds__(kBookThreads)
+pages_fork_kernel(const __grid_constant__ ForkParams p) {
+  __shared__ BookShared s;
+  __shared__ int uses[kCacheMaxSequences];
+  const int cluster = (int)blockIdx.x / p.ranks, rank = (int)blockIdx.x - cluster * p.ranks;
+  const BookView& v = p.v;
+  pdl_wait();
+  if (cluster > 0) {
+    copy_table(v, p.B_out, (int)blockIdx.x - p.ranks, (int)gridDim.x - p.ranks,
+               [&](int b) { const int f = p.parent[b]; return (uint32_t)f < (uint32_t)v.B ? f : -1; }, [](int, int, int e) { return e; },
+               [](int, int) { return false; });
+    return;
+  }
+  for (int b = threadIdx.x; b < v.B; b += kBookThreads) uses[b] = -1;
+  book_begin(s);
+  for (int b = threadIdx.x; b < p.B_out; b += kBookThreads) {
+    const int f = p.parent[b];
+    const bool there = (uint32_t)f < (uint32_t)v.B;
+    if (there) atomicAdd(&uses[f], 1);
+    else if (f != -1) found(s, SPARKATTN_E_BAD_INDEX, f);
+    if (rank == 0) p.kv_len_out[b] = there ? p.kv_len[f] : 0;
+  }
+  if (v.refs_out != v.refs) count_run(v, run_of_warp(v.pages, p.ranks, rank), [](int) { return 0; });
+  book_barrier();
+  const int segments = (v.max_pages + kCopyColumns - 1) / kCopyColumns, lane = threadIdx.x & 31;
+  const long long items = (long long)v.B * segments;
+  for (long long item = rank * kBookWarps + (threadIdx.x >> 5); item < items; item += p.ranks * kBookWarps) {
+    const int b = (int)(item / segments), c0 = (int)(item - (long long)b * segments) * kCopyColumns + lane, change = uses[b];
+    if (change == 0) continue;
+    int e[kCopyColumns / 32];
+#pragma unroll
+    for (int u = 0; u < kCopyColumns / 32; ++u) e[u] = c0 + 32 * u < v.max_pages ? v.table[(int64_t)b * v.max_pages + c0 + 32 * u] : -1;
+#pragma unroll
+    for (int u = 0; u < kCopyColumns / 32; ++u) {
+      if ((uint32_t)e[u] < (uint32_t)v.pages) {
+        if (atomicAdd(v.refs_out + e[u], change) <= 0 && change < 0) found(s, SPARKATTN_E_BAD_INDEX, e[u]);
+      } else if (e[u] != -1) {
+        found(s, SPARKATTN_E_BAD_INDEX, e[u]);
+      }
+    }
+  }
+  book_end(s, rank, p.ranks, p.status);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- trim
+struct TrimParams {
+  BookView v;
+  const int32_t* kv_len;
+  int frame, window, sink, ranks;
+  int32_t* status;
+};
+// Columns of a sequence that no later token reads: [from, to) between the first tokens and the window, and from `end` on
+struct Dead {
+  int from, to, end;
+};
+__device__ __forceinline__ Dead dead_of(const TrimParams& p, int b) {
+  const int len = p.kv_len[b];
+  if (!fits_table(p.v, len)) return {0, 0, p.v.max_pages};
+  Dead d{0, 0, pages_of(p.v, len)};
+  if (p.window > 0) {
+    const long long lo = max(((long long)(len / p.frame) - p.window + 1) * p.frame, 0LL);
+    d.from = (int)min((long long)pages_of(p.v, p.sink), (long long)p.v.max_pages);
+    d.to = (int)(lo >> p.v.shift);
+  }
+  return d;
+}
+__device__ __forceinline__ bool is_dead(const Dead& d, int i) { return i >= d.end || (i >= d.from && i < d.to); }
+
+__global__ void __launch_bounds__(kBookThreads)
+pages_trim_kernel(const __grid_constant__ TrimParams p) {
+  __shared__ BookShared s;
+  const int cluster = (int)blockIdx.x / p.ranks, rank = (int)blockIdx.x - cluster * p.ranks;
+  const BookView& v = p.v;
+  pdl_wait();
+  if (cluster > 0) {
+    Dead d{};
+    int of = -1;
+    copy_table(v, v.B, (int)blockIdx.x - p.ranks, (int)gridDim.x - p.ranks, [&](int b) {
+      if (b != of) { of = b; d = dead_of(p, b); }
+      return b; }, [&](int, int i, int e) { return is_dead(d, i) ? -1 : e; }, [](int, int) { return false; });
+    return;
+  }
+  book_begin(s);
+  for (int b = rank * kBookThreads + threadIdx.x; b < v.B; b += p.ranks * kBookThreads)
+    if (!fits_table(v, p.kv_len[b])) found(s, SPARKATTN_E_BAD_INDEX, p.kv_len[b]);
+  if (v.refs_out != v.refs) count_run(v, run_of_warp(v.pages, p.ranks, rank), [](int) { return 0; });
+  book_barrier();
+  const int segments = (v.max_pages + kCopyColumns - 1) / kCopyColumns, lane = threadIdx.x & 31;
+  const bool in_place = v.table_out == v.table;
+  const long long items = (long long)v.B * segments;
+  for (long long item = rank * kBookWarps + (threadIdx.x >> 5); item < items; item += p.ranks * kBookWarps) {
+    const int b = (int)(item / segments), first = (int)(item - (long long)b * segments) * kCopyColumns, c0 = first + lane;
+    const Dead d = dead_of(p, b);
+    if (first + kCopyColumns <= d.end && (first >= d.to || first + kCopyColumns <= d.from)) continue;
+    const int64_t row = (int64_t)b * v.max_pages;
+    int e[kCopyColumns / 32];
+#pragma unroll
+    for (int u = 0; u < kCopyColumns / 32; ++u) {
+      const int i = c0 + 32 * u;
+      e[u] = i < v.max_pages && is_dead(d, i) ? v.table[row + i] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyColumns / 32; ++u) {
+      if (e[u] == -1) continue;
+      if ((uint32_t)e[u] >= (uint32_t)v.pages || atomicSub(v.refs_out + e[u], 1) <= 0) found(s, SPARKATTN_E_BAD_INDEX, e[u]);
+      if (in_place) v.table_out[row + c0 + 32 * u] = -1;
+    }
+  }
+  book_end(s, rank, p.ranks, p.status);
+}
+
+// ------------------------------------------------------------------------------------------------------------- reserve
+struct ReserveParams {
+  BookView v;
+  const int32_t* kv_len;
+  const int32_t* kv_new;
+  int32_t* src;
+  int32_t* dst;
+  int32_t* list;                 // workspace: the free pages that are handed out, in order
+  int ranks, slots;              // slots of the hash table: a power of two, twice the sequences or more
+  int32_t* status;
+};
+// What a sequence asks for: pages for the columns [first, last) that have none, and another page in place of a partly filled one, `tail`, that
+// others hold as well.
+struct Asks {
+  int tail, first, last;         // tail: column of the partly filled page, or first where there is none
+  bool fine;                     // the numbers make sense
+  __device__ __forceinline__ bool partly() const { return tail < first; }
+};
+__device__ __forceinline__ Asks asks_of(const ReserveParams& p, int b) {
+  const int old = p.kv_len[b], len = p.kv_new[b];
+  Asks a{0, 0, 0, old >= 0 && len >= old && fits_table(p.v, len)};
+  if (a.fine && len > old) a = {old >> p.v.shift, pages_of(p.v, old), pages_of(p.v, len), true};
+  return a;
+}
+// Shared memory behind BookShared: prefix[B + 1], then the hash table of partly filled pages that several hold: page, sequences that write to it, the
+// first of them.
+__global__ void __launch_bounds__(kBookThreads)
+pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
+  __shared__ BookShared s;
+  extern __shared__ int s_dynamic[];
+  int* prefix = s_dynamic;
+  int* h_page = prefix + p.v.B + 1;
+  int* h_writers = h_page + p.slots;
+  int* h_first = h_writers + p.slots;
+  const int cluster = (int)blockIdx.x / p.ranks, rank = (int)blockIdx.x - cluster * p.ranks;
+  const BookView& v = p.v;
+  pdl_wait();
+  if (cluster > 0) {
+    Asks a{};
+    int of = -1;
+    copy_table(v, v.B, (int)blockIdx.x - p.ranks, (int)gridDim.x - p.ranks, [&](int b) {
+      if (b != of) { of = b; a = asks_of(p, b); }
+      return b; }, [](int, int, int e) { return e; }, [&](int, int i) { return i >= a.tail && i < a.last; });
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < p.slots; i += kBookThreads) { h_page[i] = -1; h_writers[i] = 0; h_first[i] = 0x7fffffff; }
+  book_begin(s);
+  // every CTA for itself: who writes to pages that several hold
+  const PoolRun run = run_of_warp(v.pages, p.ranks, rank);
+  const int free_here = count_run(v, run, [](int r) { return r == 0 ? 1 : 0; });
+  if (lane == 0) s.count[warp] = free_here;
+  auto slot_of = [&](int page, bool insert) {
+    uint32_t at = (uint32_t)page * 2654435761u >> 7;
+    for (int tries = 0; tries < p.slots; ++tries, ++at) {           // (it always ends earlier: there are more slots than pages in it)
+      int* k = h_page + (at & (p.slots - 1));
+      const int there = insert ? atomicCAS(k, -1, page) : *k;
+      if (there == page || (insert && there == -1)) break;
+    }
+    return (int)(at & (p.slots - 1));
+  };
+  auto tail_page = [&](const Asks& a, int b) {       // the partly filled page, if others hold it, or -1
+    if (!a.partly()) return -1;
+    const int e = v.table[(int64_t)b * v.max_pages + a.tail];
+    if ((uint32_t)e >= (uint32_t)v.pages) return -2;
+    return v.refs[e] > 1 ? e : -1;
+  };
+  for (int b = threadIdx.x; b < v.B; b += kBookThreads) {
+    const Asks a = asks_of(p, b);
+    if (!a.fine) found(s, SPARKATTN_E_BAD_INDEX, b);
+    const int page = tail_page(a, b);
+    if (page == -2) found(s, SPARKATTN_E_BAD_INDEX, v.table[(int64_t)b * v.max_pages + a.tail]);
+    if (page >= 0) {
+      const int at = slot_of(page, true);
+      atomicAdd(h_writers + at, 1);
+      atomicMin(h_first + at, b);
+    }
+  }
+  __syncthreads();
+  // the first of the sequences that write to a page keeps it, if nobody else holds it
+  auto copies = [&](const Asks& a, int b) {
+    const int page = tail_page(a, b);
+    if (page < 0) return -1;
+    const int at = slot_of(page, false);
+    return h_writers[at] == v.refs[page] && h_first[at] == b ? -1 : page;
+  };
+  int carry = 0;
+  for (int base = 0; base < v.B; base += kBookThreads) {
+    const int b = base + threadIdx.x;
+    int mine = 0;
+    if (b < v.B) {
+      const Asks a = asks_of(p, b);
+      mine = copies(a, b) >= 0 ? 1 : 0;
+      const int32_t* row = v.table + (int64_t)b * v.max_pages;
+#pragma unroll 4
+      for (int i = a.first; i < a.last; ++i) mine += row[i] == -1 ? 1 : 0;
+    }
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) s.scan[warp] = x;
+    __syncthreads();
+    int before = carry;
+    for (int w = 0; w < kBookWarps; ++w) {
+      if (w < warp) before += s.scan[w];
+      carry += s.scan[w];
+    }
+    if (b < v.B) prefix[b] = before + x - mine;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) prefix[v.B] = carry;
+  book_barrier();
+  const int2 free = in_front(s, rank, p.ranks);
+  const bool enough = carry <= free.y;
+  if (!enough && rank == 0 && threadIdx.x == 0) found(s, SPARKATTN_E_OUT_OF_PAGES, carry - free.y);
+  if (enough) {
+    int k = free.x;
+    for (int p0 = run.first; p0 < run.last && k < carry; p0 += 32) {
+      const bool is = p0 + lane < run.last && v.refs[p0 + lane] == 0;
+      const uint32_t all = __ballot_sync(0xffffffffu, is);
+      const int mine = k + __popc(all & ((1u << lane) - 1u));
+      if (is && mine < carry) {
+        p.list[mine] = p0 + lane;
+        v.refs_out[p0 + lane] = 1;
+      }
+      k += __popc(all);
+    }
+  }
+  // (who copies is asked before counts change under the question)
+  for (int b = rank * kBookWarps + warp; b < v.B; b += p.ranks * kBookWarps) {
+    const int from = copies(asks_of(p, b), b);
+    if (lane == 0) p.src[b] = enough ? from : -1;
+  }
+  book_barrier();
+  for (int b = rank * kBookWarps + warp; b < v.B; b += p.ranks * kBookWarps) {
+    const Asks a = asks_of(p, b);
+    const int from = p.src[b];
+    int at = prefix[b];
+    const int32_t* row = v.table + (int64_t)b * v.max_pages;
+    int32_t* out = v.table_out + (int64_t)b * v.max_pages;
+    int to = -1;
+    if (from >= 0) {
+      to = p.list[at++];
+      if (lane == 0) atomicSub(v.refs_out + from, 1);
+    }
+    if (lane == 0) p.dst[b] = to;
+    if (a.partly() && lane == 0) out[a.tail] = from >= 0 ? to : row[a.tail];
+    for (int i0 = a.first; i0 < a.last; i0 += 32) {
+      const int i = i0 + lane;
+      const int e = i < a.last ? row[i] : 0;
+      const uint32_t missing = __ballot_sync(0xffffffffu, i < a.last && e == -1);
+      if (i < a.last) out[i] = e == -1 && enough ? p.list[at + __popc(missing & ((1u << lane) - 1u))] : e;
+      at += __popc(missing);
+    }
+  }
+  book_end(s, rank, p.ranks, p.status);
+}
+
+// ------------------------------------------------------------------------------------------------------------- compact
+struct CompactParams {
+  BookView v;
+  int32_t* src;
+  int32_t* dst;                  // [pages / 2]
+  int32_t* to;                   // workspace [pages]: where a page goes, -1: nobody holds it
+  int ranks;
+  int32_t* status;
+};
+// With n pages in use, those from n on move, the i-th of them to the i-th free page below n.  A free page at x has x - used(x) free ones in
+// front of it, a moving one used(x) - used(n) moving ones.
+__global__ void __launch_bounds__(kBookThreads)
+pages_compact_kernel(const __grid_constant__ CompactParams p) {
+  __shared__ BookShared s;
+  __shared__ int s_part;
+  const int rank = (int)blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const BookView& v = p.v;
+  pdl_wait();
+  book_begin(s);
+  const PoolRun run = run_of_warp(v.pages, p.ranks, rank);
+  int n = 0;
+#pragma unroll 4
+  for (int i = run.first + lane; i < run.last; i += 32) n += v.refs[i] > 0 ? 1 : 0;
+  n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+  if (lane == 0) s.count[warp] = n;
+  if (threadIdx.x == 0) s_part = 0;
+  book_barrier();
+  const int2 used = in_front(s, rank, p.ranks);
+  // used(n): the runs in front of n's, and a part of that one
+  const int border = used.y, each = run_length(v.pages, p.ranks), border_run = border / each;
+  int front = 0;
+  for (int i = lane; i < min(border_run, p.ranks * kBookWarps); i += 32) front += cluster_ld_int(&s.count[i % kBookWarps], i / kBookWarps);
+  front = (int)__reduce_add_sync(0xffffffffu, (unsigned)front);
+  int part = 0;
+  for (long long i = (long long)border_run * each + threadIdx.x; i < border; i += kBookThreads) part += v.refs[i] > 0 ? 1 : 0;
+  part = (int)__reduce_add_sync(0xffffffffu, (unsigned)part);
+  if (lane == 0) atomicAdd(&s_part, part);
+  __syncthreads();
+  const int below = front + s_part, moves = border - below;
+  int k = used.x;                                                   // used pages in front
+  for (int p0 = run.first; p0 < run.last; p0 += 32) {
+    const int at = p0 + lane;
+    const bool there = at < run.last, is = there && v.refs[at] > 0;
+    const uint32_t all = __ballot_sync(0xffffffffu, is);
+    const int in_use = k + __popc(all & ((1u << lane) - 1u));
+    if (there) {
+      if (is && at >= border) p.src[in_use - below] = at;
+      else p.to[at] = is ? at : -1;
+      if (!is && at < border) p.dst[at - in_use] = at;
+    }
+    k += __popc(all);
+  }
+  for (int i = moves + rank * kBookThreads + threadIdx.x; i < v.pages / 2; i += p.ranks * kBookThreads) p.src[i] = p.dst[i] = -1;
+  book_barrier();
+  if (v.refs_out != v.refs) {
+    // every page's count where it ends up: what stays, then what moves (whose new places nobody held)
+    for (int p0 = run.first + lane; p0 < run.last; p0 += 32) {
+      const int r = v.refs[p0];
+      if (p0 < border ? r > 0 : true) v.refs_out[p0] = p0 < border ? r : 0;
+    }
+  }
+  for (int i = rank * kBookThreads + threadIdx.x; i < moves; i += p.ranks * kBookThreads) {
+    const int from = p.src[i], to = p.dst[i];
+    p.to[from] = to;
+    v.refs_out[to] = v.refs[from];
+    if (v.refs_out == v.refs) v.refs_out[from] = 0;
+  }
+  book_end(s, rank, p.ranks, p.status);
+}
+__global__ void __launch_bounds__(kBookThreads)
+pages_remap_kernel(const __grid_constant__ CompactParams p) {
+  pdl_wait();
+  const long long entries = (long long)p.v.B * p.v.max_pages, step = (long long)gridDim.x * kBookThreads;
+#pragma unroll 4
+  for (long long i = (long long)blockIdx.x * kBookThreads + threadIdx.x; i < entries; i += step) {
+    const int e = p.v.table[i];
+    const int to = (uint32_t)e < (uint32_t)p.v.pages ? p.to[e] : -1;
+    if (to < 0 && e != -1) report_status(p.status, SPARKATTN_E_BAD_INDEX, e);
+    p.v.table_out[i] = to;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- copy
+constexpr int kCopyThreads = 256, kCopyUnroll = 8, kCopyPieces = kCopyThreads * kCopyUnroll;      // 16-byte pieces of a unit: 32 KB
+constexpr int kCheckPages = 1 << 17;      // pages that a checking CTA looks after: a bit each in 16 KB
+
+struct CopyPagesParams {
+  const uint4* from[2];          // K, V
+  uint4* to[2];
+  const float* scale_from[2];    // NULL: bf16
+  float* scale_to[2];
+  int64_t page_from, page_to;    // strides in 16-byte pieces
+  int64_t outer_from[2], outer_to[2];      // of a run: (j / runs) * outer[0] + (j % runs) * outer[1]
+  FastDiv by_run, by_runs;
+  int run, runs, pieces;         // contiguous pieces; runs of the inner dimension; pieces of a page
+  int H, pages_from, pages_to, same;       // same: one pool
+  const int32_t* src;
+  const int32_t* dst;
+  int n, split;                  // pairs; units of a page's K or V
+  FastDiv by_split;
+  long long units;
+  int checkers;
+  int32_t* status;
+};
+
+// Looks through the pairs: numbers outside the pools, a page that is written twice, and one that is written and read.
+__device__ __forceinline__ bool check_pairs(const CopyPagesParams& p, int range, uint32_t* bits, int* s_bad) {
+  const int first = range * kCheckPages;
+  for (int i = threadIdx.x; i < kCheckPages / 32; i += kCopyThreads) bits[i] = 0u;
+  if (threadIdx.x == 0) { s_bad[0] = 0; s_bad[1] = 0; }
+  __syncthreads();
+  auto bad = [&](int page) { if (atomicExch(s_bad, 1) == 0) s_bad[1] = page; };
+#pragma unroll 1
+  for (int pass = 0; pass < 1 + p.same; ++pass) {
+#pragma unroll 1
+    for (long long i0 = threadIdx.x; i0 < p.n; i0 += 8 * kCopyThreads) {
+      int a[8], b[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const long long i = i0 + (long long)u * kCopyThreads;
+        a[u] = i < p.n ? p.src[i] : -1;
+        b[u] = i < p.n ? p.dst[i] : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (a[u] == -1 && b[u] == -1) continue;
+        if ((uint32_t)a[u] >= (uint32_t)p.pages_from || (uint32_t)b[u] >= (uint32_t)p.pages_to) {
+          bad((uint32_t)a[u] >= (uint32_t)p.pages_from ? a[u] : b[u]);
+          continue;
+        }
+        const uint32_t at = (uint32_t)(pass == 0 ? b[u] : a[u]) - (uint32_t)first;
+        if (at >= (uint32_t)kCheckPages) continue;
+        const uint32_t bit = 1u << (at & 31);
+        const uint32_t before = pass == 0 ? atomicOr(bits + (at >> 5), bit) : bits[at >> 5];
+        if (before & bit) bad(pass == 0 ? b[u] : a[u]);
+      }
+    }
+    __syncthreads();
+  }
+  const bool is = s_bad[0] != 0;
+  if (threadIdx.x == 0 && is) report_early(p.status, SPARKATTN_E_BAD_INDEX, s_bad[1]);
+  __syncthreads();
+  return is;
+}
+
+__global__ void __launch_bounds__(kCopyThreads, 4)
+cache_copy_pages_kernel(const __grid_constant__ CopyPagesParams p) {
+  __shared__ uint32_t bits[kCheckPages / 32];
+  __shared__ int s_bad[2];
+  __shared__ int s_pair[kCopyThreads], s_part[kCopyThreads], s_n;
+  pdl_wait();
+  if ((int)blockIdx.x < p.checkers) {
+    bool code_there = false;
+    if (blockIdx.x == 0 && threadIdx.x == 0) code_there = take_header(p.status);
+    check_pairs(p, blockIdx.x, bits, s_bad);
+    if (blockIdx.x == 0 && __syncthreads_or(code_there))
+      // the word held a code, which may have been another checker's: see take_header
+      for (int range = 1; range < p.checkers; ++range) check_pairs(p, range, bits, s_bad);
+    return;
+  }
+  const long long cta = (int)blockIdx.x - p.checkers, ctas = (int)gridDim.x - p.checkers;
+#pragma unroll 1
+  for (long long round = 0; cta + ctas * kCopyThreads * round < p.units; ++round) {
+    // 256 units at a time: which of them have a page to copy
+    if (threadIdx.x == 0) s_n = 0;
+    __syncthreads();
+    const long long unit = cta + ctas * (kCopyThreads * round + threadIdx.x);
+    if (unit < p.units) {
+      const int pair = (int)(unit / (2 * p.split)), part = (int)(unit - (long long)pair * 2 * p.split);
+      if ((uint32_t)p.src[pair] < (uint32_t)p.pages_from && (uint32_t)p.dst[pair] < (uint32_t)p.pages_to) {
+        const int at = atomicAdd(&s_n, 1);
+        s_pair[at] = pair;
+        s_part[at] = part;
+      }
+    }
+    __syncthreads();
+    const int found = s_n;
+#pragma unroll 1
+    for (int i = 0; i < found; ++i) {
+      const int pair = s_pair[i], part = s_part[i], kv = part >= p.split, first = (part - kv * p.split) * kCopyPieces + threadIdx.x;
+      const int from = p.src[pair], to = p.dst[pair];
+      const uint4* in = p.from[kv] + from * p.page_from;
+      uint4* out = p.to[kv] + to * p.page_to;
+      uint4 x[kCopyUnroll];
+      int64_t at[kCopyUnroll];
+#pragma unroll
+      for (int u = 0; u < kCopyUnroll; ++u) {
+        const int piece = first + u * kCopyThreads, run = fast_div(piece, p.by_run), in_run = piece - run * p.run;
+        const int outer = fast_div(run, p.by_runs), inner = run - outer * p.runs;
+        at[u] = outer * p.outer_to[0] + inner * p.outer_to[1] + in_run;
+        if (piece < p.pieces) x[u] = in[outer * p.outer_from[0] + inner * p.outer_from[1] + in_run];
+      }
+#pragma unroll
+      for (int u = 0; u < kCopyUnroll; ++u)
+        if (first + u * kCopyThreads < p.pieces) out[at[u]] = x[u];
+      if (p.scale_from[kv] != nullptr && part == kv * p.split)
+        for (int h = threadIdx.x; h < p.H; h += kCopyThreads) p.scale_to[kv][(int64_t)to * p.H + h] = p.scale_from[kv][(int64_t)from * p.H + h];
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ host side
+namespace {
+// CTAs of the first cluster: by the words that it goes through, some 4000 a CTA
+int ranks_for(long long words) {
+  int n = 1;
+  while (n < kBookClusterMax && (long long)n * 4096 < words) n *= 2;
+  return n;
+}
+// clusters that copy the tables meanwhile
+int copiers_for(long long rows, int max_pages, int ranks, int sms) {
+  const long long warps = rows * ((max_pages + kCopyColumns - 1) / kCopyColumns), ctas = (warps + kBookWarps - 1) / kBookWarps;
+  return (int)std::max<long long>(1, std::min<long long>((ctas + ranks - 1) / ranks, 2LL * sms / ranks));
+}
+template <typename Params>
+int launch_book(void (*kern)(Params), int clusters, int ranks, size_t smem, cudaStream_t stream, const Params& p) {
+  if (ranks > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SPARKATTN_E_CUDA;
+  return launch_clustered(kern, dim3((unsigned)(clusters * ranks)), kBookThreads, smem, true, ranks, stream, p);
+}
+}  // namespace
+
+size_t pages_workspace_bytes(const sparkattn_book_t& b) { return kWorkspaceHeaderBytes + ((size_t)b.pages * 4 + 255) / 256 * 256; }
+
+int launch_pages_fork(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* parent, int B_out, int32_t* table_out, int32_t* kv_len_out,
+                      int32_t* refs_out, void* workspace, cudaStream_t stream) {
+  ForkParams p{make_book_view(book, table_out, refs_out), kv_len, parent, kv_len_out, B_out, 1, static_cast<int32_t*>(workspace)};
+  const int sms = current_sm_count();
+  if (sms < 1) return SPARKATTN_E_CUDA;
+  p.ranks = ranks_for((long long)book.B * book.max_pages + book.pages);
+  return launch_book(pages_fork_kernel, 1 + copiers_for(B_out, book.max_pages, p.ranks, sms), p.ranks, 0, stream, p);
+}
+
+int launch_pages_trim(const sparkattn_book_t& book, const int32_t* kv_len, int frame, int window, int sink, int32_t* table_out, int32_t* refs_out,
+                      void* workspace, cudaStream_t stream) {
+  TrimParams p{make_book_view(book, table_out, refs_out), kv_len, std::max(frame, 1), window, sink, 1, static_cast<int32_t*>(workspace)};
+  const int sms = current_sm_count();
+  if (sms < 1) return SPARKATTN_E_CUDA;
+  p.ranks = ranks_for((long long)book.B * book.max_pages + book.pages);
+  const int copiers = table_out != book.page_table ? copiers_for(book.B, book.max_pages, p.ranks, sms) : 0;
+  return launch_book(pages_trim_kernel, 1 + copiers, p.ranks, 0, stream, p);
+}
+
+int launch_pages_reserve(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out, int32_t* src,
+                         int32_t* dst, void* workspace, cudaStream_t stream) {
+  int32_t* status = static_cast<int32_t*>(workspace);
+  ReserveParams p{make_book_view(book, table_out, refs_out), kv_len, kv_new, src, dst, status + kWorkspaceHeaderBytes / 4, 1, 64, status};
+  const int sms = current_sm_count();
+  if (sms < 1) return SPARKATTN_E_CUDA;
+  while (p.slots < 2 * book.B) p.slots *= 2;
+  p.ranks = ranks_for((long long)book.pages + 64LL * book.B);
+  const size_t smem = ((size_t)book.B + 1 + 3 * (size_t)p.slots) * 4;
+  // (the most that any call asks for: host threads with other batches set it too)
+  if (cudaFuncSetAttribute(pages_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kCacheMaxSequences + 1 + 3 * 2 * kCacheMaxSequences) * 4) != cudaSuccess)
+    return SPARKATTN_E_CUDA;
+  const int copiers = table_out != book.page_table ? copiers_for(book.B, book.max_pages, p.ranks, sms) : 0;
+  return launch_book(pages_reserve_kernel, 1 + copiers, p.ranks, smem, stream, p);
+}
+
+int launch_pages_compact(const sparkattn_book_t& book, int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace, cudaStream_t stream) {
+  int32_t* status = static_cast<int32_t*>(workspace);
+  CompactParams p{make_book_view(book, table_out, refs_out), src, dst, status + kWorkspaceHeaderBytes / 4, ranks_for(book.pages), status};
+  const int sms = current_sm_count();
+  if (sms < 1) return SPARKATTN_E_CUDA;
+  const int rc = launch_book(pages_compact_kernel, 1, p.ranks, 0, stream, p);
+  if (rc != SPARKATTN_OK) return rc;
+  const long long entries = (long long)book.B * book.max_pages, ctas = (entries + 4 * kBookThreads - 1) / (4 * kBookThreads);
+  return launch_kernel(pages_remap_kernel, dim3((unsigned)std::min<long long>(ctas, 2 * sms)), kBookThreads, 0, true, stream, p);
+}
+
+int launch_copy_pages(const sparkattn_cache_t& from, const PagePools& in, const sparkattn_cache_t& to, const PagePools& out, const int32_t* src,
+                      const int32_t* dst, int n, void* workspace, cudaStream_t stream) {
+  CopyPagesParams p{};
+  const int per16 = from.dtype == SPARKATTN_BF16 ? 8 : 16;
+  for (int i = 0; i < 2; ++i) {
+    p.from[i] = static_cast<const uint4*>(i ? in.v : in.k);
+    p.to[i] = static_cast<uint4*>(i ? out.v : out.k);
+    p.scale_from[i] = i ? in.v_scale : in.k_scale;
+    p.scale_to[i] = i ? out.v_scale : out.k_scale;
+  }
+  p.page_from = from.stride_page / per16;
+  p.page_to = to.stride_page / per16;
+  // the page as runs of contiguous bytes: rows, with the tokens of a head or the heads of a token where these lie side by side in both pools, or all
+  struct Dim {
+    long long count, from, to;
+  } token{from.page, from.stride_n, to.stride_n}, head{from.H, from.stride_h, to.stride_h}, in_dim = token, out_dim = head;
+  if (!(token.from == from.d && token.to == from.d) && head.from == from.d && head.to == from.d) { in_dim = head; out_dim = token; }
+  long long run = from.d;
+  auto join = [&](Dim& d) { if (d.from == run && d.to == run) { run *= d.count; d.count = 1; } };
+  join(in_dim);
+  if (in_dim.count == 1) join(out_dim);
+  if (run / per16 > 0x3fffffffLL || (long long)from.H * from.page * from.d / per16 > 0x3fffffffLL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  p.run = (int)(run / per16);
+  p.runs = (int)in_dim.count;
+  p.outer_from[0] = out_dim.from / per16; p.outer_from[1] = in_dim.from / per16;
+  p.outer_to[0] = out_dim.to / per16; p.outer_to[1] = in_dim.to / per16;
+  p.by_run = make_fast_div(p.run);
+  p.by_runs = make_fast_div(p.runs);
+  p.pieces = (int)((long long)from.H * from.page * from.d / per16);
+  p.H = from.H;
+  p.pages_from = from.pages;
+  p.pages_to = to.pages;
+  p.same = in.k == out.k;
+  p.src = src; p.dst = dst; p.n = n;
+  p.split = (p.pieces + kCopyPieces - 1) / kCopyPieces;
+  p.units = 2LL * p.split * n;
+  p.checkers = (to.pages + kCheckPages - 1) / kCheckPages;
+  p.status = static_cast<int32_t*>(workspace);
+  const int sms = current_sm_count();
+  if (sms < 1) return SPARKATTN_E_CUDA;
+  const unsigned ctas = p.checkers + (unsigned)std::min<long long>(p.units, 4LL * sms);
+  return launch_kernel(cache_copy_pages_kernel, dim3(ctas), kCopyThreads, 0, true, stream, p);
+}
+
+}  // namespace sparkattn
