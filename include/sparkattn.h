@@ -467,14 +467,15 @@ typedef struct {
 } sparkattn_rotary_t;
 
 /* RMS norm over the d channels of each head, in front of the rotation:  y_c = x_c / sqrt(mean(x^2) + eps) * weight_c.
- * fp32 throughout (squares, their sum, the root, both products), no rounding between norm and rotation.  A row whose sum of squares passes
+ * fp32 throughout (squares, their sum, the root, the products); no rounding to 16 bits between norm and rotation, whose products and sums may be
+ * fused here.  A row whose sum of squares passes
  * fp32's range, which takes entries of 1e18, comes out as zeros; one with an infinity or a NaN gives NaN there. */
 typedef struct {
   uint32_t struct_size;   /* sizeof(sparkattn_norm_t)                                         */
   uint32_t version;       /* SPARKATTN_VERSION                                                */
   int32_t weight_dtype;   /* SPARKATTN_BF16 or SPARKATTN_FP32                                 */
   int32_t per_head;       /* 0: weights [d], shared by the heads; 1: [heads, d] contiguous    */
-  float eps;              /* > 0                                                              */
+  float eps;              /* > 0, not a subnormal number                                      */
   uint32_t pad;           /* must be 0                                                        */
   const void* q_weight;   /* 16-byte aligned, or NULL: ones                                   */
   const void* k_weight;

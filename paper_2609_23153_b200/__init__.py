@@ -567,9 +567,9 @@ def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, page_table: t
     as the newest tokens of the sequences, and returns q bf16 [T, H, d] normalised and rotated (None without q; ``q_out`` may be q).  page_table int32 [B, max_pages]; kv_len int32 [B] with the
     new tokens; rows q_start[b] .. q_start[b+1] - 1 (int32 [B+1]) belong to sequence b, T / B each without it; max_new:
     no sequence has more new tokens (0: T with q_start, which is slow where many sequences share the rows, else T / B)."""
-    rc, q_out, workspace = _calls().cache_append(*cache, page_table, kv_len, q_start, max_new, k, v, q, q_out, *(_NO_ROTARY if rotary is None else rotary),
-                                                 *(_NO_NORM if norm is None else (True, *norm)), workspace,
-                                                 None if stream is None else stream.cuda_stream)
+    args = (*cache, page_table, kv_len, q_start, max_new, k, v, q, q_out, *(_NO_ROTARY if rotary is None else rotary))
+    last = (workspace, None if stream is None else stream.cuda_stream)
+    rc, q_out, workspace = _calls().cache_append(*args, *last) if norm is None else _calls().cache_append_norm(*args, True, *norm, *last)
     if rc != OK:
         _check(rc, "sparkattn_cache_append")
     if check_status:
@@ -586,8 +586,9 @@ def cache_fwd(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, kv_len:
     0: not), over the last ``window`` frames (0: all) and the sequence's first ``sink`` tokens.
     The batch as in :func:`cache_append`; kernel and split go by ``max_new`` and the width of ``page_table``, so both should be what the
     batch needs.  Returns out bf16 [T, H, d] (and lse float32 [T, H])."""
-    rc, out, lse, workspace = _calls().cache_fwd(*cache, page_table, kv_len, q_start, max_new, q, frame_tokens, window, sink, softmax_scale, out,
-                                                 return_lse, workspace, None if stream is None else stream.cuda_stream)
+    args = (*cache, page_table, kv_len, q_start, max_new, q, frame_tokens, window)
+    last = (softmax_scale, out, return_lse, workspace, None if stream is None else stream.cuda_stream)
+    rc, out, lse, workspace = _calls().cache_fwd(*args, *last) if sink == 0 else _calls().cache_fwd_sink(*args, sink, *last)
     if rc != OK:
         _check(rc, "sparkattn_cache_fwd")
     if check_status:

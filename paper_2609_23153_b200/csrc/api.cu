@@ -575,7 +575,7 @@ int check_norm(const sparkattn_norm_t* n) {
   if (n == nullptr) return SPARKATTN_OK;
   if (n->struct_size != sizeof(sparkattn_norm_t) || n->version != SPARKATTN_VERSION || n->pad != 0) return SPARKATTN_E_INVALID_ARG;
   if ((n->weight_dtype != SPARKATTN_BF16 && n->weight_dtype != SPARKATTN_FP32) || (n->per_head != 0 && n->per_head != 1)) return SPARKATTN_E_INVALID_ARG;
-  if (!(n->eps > 0.0f) || isinf(n->eps)) return SPARKATTN_E_INVALID_ARG;
+  if (!(n->eps >= 1.17549435e-38f) || isinf(n->eps)) return SPARKATTN_E_INVALID_ARG;
   return !aligned16(n->q_weight) || !aligned16(n->k_weight) ? SPARKATTN_E_MISALIGNED : SPARKATTN_OK;
 }
 // one tensor of sparkattn_norm_rotate

@@ -569,9 +569,9 @@ struct Rotation {
 };
 struct HeadNorm {
   at::Tensor q, k;
-  bool on;
+  bool on = false;
   sparkattn_norm_t n{};
-  explicit HeadNorm(Args& a) {
+  void take(Args& a) {
     on = a.truth();
     q = a.optional_tensor();
     k = a.optional_tensor();
@@ -599,16 +599,18 @@ struct HeadNorm {
 };
 
 // cache_append(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, k, v, q, q_out, cos, sin, positions, axis,
-// interleaved, norm, q_weight, k_weight, eps, workspace, stream) -> rc, q_out, workspace
+// interleaved, workspace, stream) -> rc, q_out, workspace; cache_append_norm has norm, q_weight, k_weight, eps behind interleaved
+template <bool NORM>
 PyObject* cache_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Args a(argv, n);
-  a.expect(23);
+  a.expect(NORM ? 23 : 19);
   Cache cache(a);
   const at::Tensor k = a.tensor(), v = a.tensor(), q = a.optional_tensor();
   at::Tensor q_out = a.optional_tensor();
   Rotation rotation(a);
-  HeadNorm norm(a);
+  HeadNorm norm;
+  if constexpr (NORM) norm.take(a);
   at::Tensor ws = a.optional_tensor();
   const Stream stream = a.stream();
   cache.describe(k);
@@ -644,7 +646,8 @@ PyObject* norm_rotate(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const at::Tensor q = a.tensor(), k = a.optional_tensor();
   at::Tensor q_out = a.optional_tensor(), k_out = a.optional_tensor();
   Rotation rotation(a);
-  HeadNorm norm(a);
+  HeadNorm norm;
+  norm.take(a);
   at::Tensor ws = a.optional_tensor();
   const Stream stream = a.stream();
   const int32_t block = q.dim() == 4 && q.size(3) == 64 ? 64 : 128;
@@ -674,15 +677,16 @@ PyObject* norm_rotate(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// cache_fwd(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, q, frame_tokens, window, sink, softmax_scale, out,
-// return_lse, workspace, stream) -> rc, out, lse, workspace
+// cache_fwd(k_cache, v_cache, k_scale, v_scale, page_table, kv_len, q_start, max_new, q, frame_tokens, window, softmax_scale, out, return_lse,
+// workspace, stream) -> rc, out, lse, workspace; cache_fwd_sink has sink behind window
+template <bool SINK>
 PyObject* cache_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Args a(argv, n);
-  a.expect(17);
+  a.expect(SINK ? 17 : 16);
   Cache cache(a);
   const at::Tensor q = a.tensor();
-  const int32_t frame_tokens = a.i32(), window = a.i32(), sink = a.i32();
+  const int32_t frame_tokens = a.i32(), window = a.i32(), sink = SINK ? a.i32() : 0;
   const float softmax_scale = a.number();
   at::Tensor out = a.optional_tensor(), lse;
   const bool return_lse = a.truth();
@@ -902,7 +906,8 @@ PyMethodDef g_methods[] = {method<bind>("bind"), method<select>("select"), metho
                            method<quant_fp8>("quant_fp8"), method<quant_fp8_pooled>("quant_fp8_pooled"),
                            method<quant_fp8_per_token>("quant_fp8_per_token"), method<fwd>("fwd"), method<gather_tokens>("gather_tokens"),
                            method<comp_state>("comp_state"), method<comp_apply>("comp_apply"), method<fwd_gated>("fwd_gated"),
-                           method<cache_append>("cache_append"), method<cache_fwd>("cache_fwd"),
+                           method<cache_append<false>>("cache_append"), method<cache_append<true>>("cache_append_norm"),
+                           method<cache_fwd<false>>("cache_fwd"), method<cache_fwd<true>>("cache_fwd_sink"),
                            method<norm_rotate>("norm_rotate"), method<pages_fork>("pages_fork"), method<pages_reserve>("pages_reserve"),
                            method<pages_trim>("pages_trim"), method<pages_compact>("pages_compact"), method<cache_copy_pages>("cache_copy_pages"),
                            {nullptr, nullptr, 0, nullptr}};

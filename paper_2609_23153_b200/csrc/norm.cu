@@ -2,16 +2,20 @@
 //
 // y = R(x / sqrt(mean x^2 + eps) * w), row by row; nothing is used twice but the tokens' cosines and sines, which all heads share, and the
 // weights, which all tokens share.  So a thread stays with 16 bytes of one token's rows: its pairs' phases and (per tensor) its weights are in
-// registers once, and it goes through the heads, kUnroll rows asked for at a time.  The sum of squares goes through the D / 8 lanes of a row.
+// registers once, and it goes through the heads, four rows asked for at a time.  The sum of squares goes through the D / 8 lanes of a row.
 // A CTA is 256 threads: 16 tokens (32 of 64 channels) by a run of the (sample, head) lines of both tensors.
+// Bandwidth bounds it, and instructions are near: 40 + 40 heads of 75,600 tokens, 128 channels, 3.10 GB in 498 us = 6.2 TB/s, 0.95 of a copy's rate
+// (541 with scalar instructions and the rotation's products rounded one by one, the SMs issuing in 0.78 of the clocks).  Small calls are latency:
+// phases, then rows; 8 heads of two samples of 1201 tokens, 64 channels, 3.5 us.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.cuh"
 #include "tmap.h"
 
 namespace sparkattn {
 
-constexpr int kNormThreads = 256, kNormUnroll = 4;
+constexpr int kNormThreads = 256;
 
 struct HeadRowsView {
   const __nv_bfloat16* in;
@@ -41,8 +45,9 @@ __device__ __forceinline__ uint32_t angle_row(const RotaryView& r, int n, int m)
   return r.positions != nullptr ? (uint32_t)r.positions[(int64_t)n * r.axes + axis] : (uint32_t)n;
 }
 
-template <int D, bool INTERLEAVED, bool NORM>
-__global__ void __launch_bounds__(kNormThreads, 4)
+// U: rows that a thread asks for at a time
+template <int D, bool INTERLEAVED, bool NORM, int U>
+__global__ void __launch_bounds__(kNormThreads, U == 4 ? 5 : 4)
 norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
   constexpr int kLanes = D / 8, kRows = kNormThreads / kLanes, kPairs = INTERLEAVED ? 4 : 8;
   const RotaryView& r = p.rotary;
@@ -63,21 +68,48 @@ norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
   for (int j = 0; j < kPairs; ++j) {
     c[j] = 1.0f;
     s[j] = 0.0f;
-    if (there && on) {
-      const uint32_t e = angle_row(r, n, m0 + j);
+  }
+  if (there && on) {
+    if (r.axis == nullptr) {
+      // one row of the tables, four pairs at a time
+      const uint32_t e = r.positions != nullptr ? (uint32_t)r.positions[(int64_t)n * r.axes] : (uint32_t)n;
       if (e < (uint32_t)r.rows) {
-        c[j] = r.cos[e * (r.rot / 2) + m0 + j];
-        s[j] = r.sin[e * (r.rot / 2) + m0 + j];
+#pragma unroll
+        for (int j = 0; j < kPairs; j += 4) {
+          const float4 cc = *reinterpret_cast<const float4*>(r.cos + (e * (r.rot / 2) + m0 + j));
+          const float4 ss = *reinterpret_cast<const float4*>(r.sin + (e * (r.rot / 2) + m0 + j));
+          c[j] = cc.x; c[j + 1] = cc.y; c[j + 2] = cc.z; c[j + 3] = cc.w;
+          s[j] = ss.x; s[j + 1] = ss.y; s[j + 2] = ss.z; s[j + 3] = ss.w;
+        }
       } else {
         any_bad = true;
         bad = (int)e;
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        const uint32_t e = angle_row(r, n, m0 + j);
+        if (e < (uint32_t)r.rows) {
+          c[j] = r.cos[e * (r.rot / 2) + m0 + j];
+          s[j] = r.sin[e * (r.rot / 2) + m0 + j];
+        } else {
+          any_bad = true;
+          bad = (int)e;
+        }
+      }
     }
-    if (!INTERLEAVED && !second) s[j] = -s[j];                    // a first side takes away what a second side adds
+  }
+  if (!INTERLEAVED && !second) {
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) s[j] = -s[j];                // a first side takes away what a second side adds
   }
   auto turned = [&](const Chunk& x) {
-    Chunk y;
-    if constexpr (INTERLEAVED) {
+    Chunk y{};
+    if constexpr (NORM && INTERLEAVED) {
+      y = turn_pairs_fused(c, s, x);
+    } else if constexpr (NORM) {
+      y = turn_halves_fused(c, s, x, chunk_of(x, partner));
+    } else if constexpr (INTERLEAVED) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         y.x[2 * j] = __fsub_rn(__fmul_rn(x.x[2 * j], c[j]), __fmul_rn(x.x[2 * j + 1], s[j]));
@@ -103,15 +135,15 @@ norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
     const __nv_bfloat16* in = v.in + (int64_t)n * v.in_n + chunk * 8;
     __nv_bfloat16* out = v.out + (int64_t)n * v.out_n + chunk * 8;
 #pragma unroll 1
-    for (int l0 = first; l0 < last; l0 += kNormUnroll) {
-      uint4 raw[kNormUnroll];
+    for (int l0 = first; l0 < last; l0 += U) {
+      uint4 raw[U];
 #pragma unroll
-      for (int u = 0; u < kNormUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int l = l0 + u, b = fast_div(l, v.by_H), h = l - b * v.H;
         raw[u] = l < last && there ? *reinterpret_cast<const uint4*>(in + (b * v.in_b + h * v.in_h)) : make_uint4(0u, 0u, 0u, 0u);
       }
 #pragma unroll
-      for (int u = 0; u < kNormUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int l = l0 + u, b = fast_div(l, v.by_H), h = l - b * v.H;
         Chunk x = widen(raw[u]);
         if constexpr (NORM) {
@@ -164,20 +196,27 @@ int launch_norm_rotate(const HeadRows& q, const HeadRows* k, const sparkattn_nor
   if (sms < 1) return SPARKATTN_E_CUDA;
   p.tiles = (s.N + rows - 1) / rows;
   p.by_tiles = make_fast_div(p.tiles);
-  // runs of lines: as many as give four CTAs for every place on the SMs, of at least two batches of rows each
+  // Four rows at a time where that gives every place on the SMs a CTA (40 heads of 75,600 tokens: 498 us by four, 564 by two, 501 by five on four CTAs
+  // an SM), else two, so that more CTAs share the work (8 heads of 1201 tokens of 64 channels: 3.5 us by two, 4.1 by four).
   const long long lines = (long long)p.x[0].lines + p.x[1].lines;
-  long long groups = std::min<long long>((16LL * sms + p.tiles - 1) / p.tiles, (lines + 2 * kNormUnroll - 1) / (2 * kNormUnroll));
+  const int u = (lines + 3) / 4 * p.tiles >= 5LL * sms ? 4 : 2;
+  // runs of lines: as many as give three CTAs for every place, of one batch of rows at least
+  long long groups = std::min<long long>((16LL * sms + p.tiles - 1) / p.tiles, (lines + u - 1) / u);
   p.each = (int)((lines + groups - 1) / groups);
   groups = (lines + p.each - 1) / p.each;
   if (groups * p.tiles > 0x7fffff00LL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
-  auto go = [&](auto kern) { return launch_kernel(kern, dim3((unsigned)(groups * p.tiles)), kNormThreads, 0, true, stream, p); };
-  const bool inter = p.rotary.interleaved != 0;
-  if (s.d == 128) {
-    if (norm) return inter ? go(norm_rotate_kernel<128, true, true>) : go(norm_rotate_kernel<128, false, true>);
-    return inter ? go(norm_rotate_kernel<128, true, false>) : go(norm_rotate_kernel<128, false, false>);
-  }
-  if (norm) return inter ? go(norm_rotate_kernel<64, true, true>) : go(norm_rotate_kernel<64, false, true>);
-  return inter ? go(norm_rotate_kernel<64, true, false>) : go(norm_rotate_kernel<64, false, false>);
+  auto go = [&](auto d, auto inter, auto normed) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool I = decltype(inter)::value, N = decltype(normed)::value;
+    return launch_kernel(u == 4 ? norm_rotate_kernel<D, I, N, 4> : norm_rotate_kernel<D, I, N, 2>, dim3((unsigned)(groups * p.tiles)), kNormThreads, 0, true,
+                         stream, p);
+  };
+  auto with = [&](auto d) {
+    using std::true_type, std::false_type;
+    if (p.rotary.interleaved) return norm ? go(d, true_type{}, true_type{}) : go(d, true_type{}, false_type{});
+    return norm ? go(d, false_type{}, true_type{}) : go(d, false_type{}, false_type{});
+  };
+  return s.d == 128 ? with(std::integral_constant<int, 128>{}) : with(std::integral_constant<int, 64>{});
 }
 
 }  // namespace sparkattn

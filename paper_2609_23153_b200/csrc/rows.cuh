@@ -70,19 +70,53 @@ __device__ __forceinline__ Chunk norm_weights(const NormView& n, const void* wei
   }
   return w;
 }
-// x / sqrt(mean x^2 + eps) * weight of a row whose chunks the D / 8 lanes hold.  Squares, their sum and both products are fp32; the order of the sum
-// is that of the lanes, so a row has the same bits whatever call it goes through.
+// x / sqrt(mean x^2 + eps) * weight of a row whose chunks the D / 8 lanes hold.  Squares, their sum and the products are fp32; the order of the sum
+// is that of the channels and lanes, so a row has the same bits whatever call it goes through.  In pairs of channels: with scalar instructions
+// (and the rotation's products rounded one by one) 40 + 40 heads of 75,600 tokens take 541 us instead of 514.
 template <int D>
 __device__ __forceinline__ Chunk normed(const Chunk& x, const Chunk& weight, float eps) {
-  float sum = __fmul_rn(x.x[0], x.x[0]);
+  uint64_t pair[4], sum2 = 0;
 #pragma unroll
-  for (int j = 1; j < 8; ++j) sum = __fmaf_rn(x.x[j], x.x[j], sum);
+  for (int j = 0; j < 4; ++j) {
+    pair[j] = pack_f32x2(x.x[2 * j], x.x[2 * j + 1]);
+    sum2 = j == 0 ? fmul2(pair[j], pair[j]) : ffma2(pair[j], pair[j], sum2);
+  }
+  const float2 two = unpack_f32x2(sum2);
+  float sum = two.x + two.y;
 #pragma unroll
   for (int o = 1; o < D / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  const float by = rsqrtf(__fmaf_rn(sum, 1.0f / D, eps));
+  float by;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(by) : "f"(__fmaf_rn(sum, 1.0f / D, eps)));      // (eps is a normal number)
+  const uint64_t by2 = pack_f32x2(by, by);
   Chunk r;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) r.x[j] = __fmul_rn(__fmul_rn(x.x[j], by), weight.x[j]);
+  for (int j = 0; j < 4; ++j) {
+    const float2 y = unpack_f32x2(fmul2(pair[j], fmul2(pack_f32x2(weight.x[2 * j], weight.x[2 * j + 1]), by2)));
+    r.x[2 * j] = y.x;
+    r.x[2 * j + 1] = y.y;
+  }
+  return r;
+}
+// The rotation behind a norm: a product rounded, the other one and the sum in one step.  Interleaved: the chunk's four pairs by c, s.
+__device__ __forceinline__ Chunk turn_pairs_fused(const float (&c)[4], const float (&s)[4], const Chunk& x) {
+  Chunk r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    r.x[2 * j] = __fmaf_rn(x.x[2 * j], c[j], -__fmul_rn(x.x[2 * j + 1], s[j]));
+    r.x[2 * j + 1] = __fmaf_rn(x.x[2 * j], s[j], __fmul_rn(x.x[2 * j + 1], c[j]));
+  }
+  return r;
+}
+// Halves: far holds the other sides, s is negative on the first side
+__device__ __forceinline__ Chunk turn_halves_fused(const float (&c)[8], const float (&s)[8], const Chunk& x, const Chunk& far) {
+  Chunk r;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const uint64_t other = fmul2(pack_f32x2(far.x[j], far.x[j + 1]), pack_f32x2(s[j], s[j + 1]));
+    const float2 y = unpack_f32x2(ffma2(pack_f32x2(x.x[j], x.x[j + 1]), pack_f32x2(c[j], c[j + 1]), other));
+    r.x[j] = y.x;
+    r.x[j + 1] = y.y;
+  }
   return r;
 }
 
