@@ -542,9 +542,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             dst[j] = make_uint4(x[0], x[1], x[2], x[3]);
           }
         } else if (past.there && tiles > 0) {
-          uint4* dst = reinterpret_cast<uint4*>(p.part_o + ((int64_t)past.slot * R + r) * D + ch * 32);
+          // (four channels of a warp's rows side by side: with a row's channels together every store had 32 lines, and an item's end took 4.5 us)
+          uint4* dst = reinterpret_cast<uint4*>(p.part_o + (((int64_t)past.slot * (D / 4) + ch * 8) * R + r) * 4);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) dst[j] = empty ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+          for (int j = 0; j < 8; ++j) dst[j * R] = empty ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
         }
       }
       tc_fence_before();
@@ -741,7 +742,7 @@ static int launch_chunk(const sparkattn_cache_t& c, CacheFwdParams& p, const voi
   auto kern = p.causal.sink > 0 ? cache_chunk_kernel<D, FP8, SPLIT, true> : cache_chunk_kernel<D, FP8, SPLIT, false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kChunkThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
-  return launch_kernel(combine_kernel<D, R>, dim3(p.workers - 1, R / 16), kCombineThreads, 0, true, stream, p);
+  return launch_kernel(combine_rows_kernel<D, R>, dim3(p.workers - 1, 4), kCombineRowsThreads, 0, true, stream, p);
 }
 
 int launch_cache_chunk(const sparkattn_cache_t& c, int rows, CacheFwdParams& p, const void* k_cache, const void* v_cache, cudaStream_t stream) {

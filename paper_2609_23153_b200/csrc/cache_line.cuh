@@ -43,7 +43,7 @@ struct CacheFwdParams {
   int32_t* status;
   struct Border* borders;        // [workers]
   float* part_ml;                // [2 workers][R][2] reference, sum
-  float* part_o;                 // [2 workers][R][d] unnormalised output
+  float* part_o;                 // [2 workers][R][d] unnormalised output (128 rows and more: [2 workers][d / 4][R][4])
 };
 
 // What the combining kernel needs to know of the border in front of a stretch: the item that it cuts, if it does.
@@ -91,10 +91,28 @@ struct Line {
     }
     return it;
   }
-  // units of the row tiles of one key head
+  // Units of the row tiles of one key head, every lane for a sequence of its own (n = 0: none).  Whole warps: few sequences of many row tiles are
+  // taken one after the other by all lanes (three frames of 1560 tokens, one sequence of 19 row tiles: 0.8 us instead of 3.8).
   static __device__ __forceinline__ int units_of(const CacheFwdParams& p, const Sequence& s) {
+    const int tiles = row_tiles(p, s);
     int sum = 0;
-    for (int rt = 0; rt < row_tiles(p, s); ++rt) sum += item_of(p, s, rt).units();
+    if constexpr (R >= 128) {
+      const int most = (int)__reduce_max_sync(0xffffffffu, (unsigned)tiles), lane = threadIdx.x & 31;
+      uint32_t long_ones = __ballot_sync(0xffffffffu, tiles > 1);
+      if (__popc(long_ones) * ((most + 31) / 32) < most) {
+        if (tiles == 1) sum = item_of(p, s, 0).units();
+        for (; long_ones != 0; long_ones &= long_ones - 1) {
+          const int l = __ffs(long_ones) - 1;
+          const Sequence its{__shfl_sync(0xffffffffu, s.start, l), __shfl_sync(0xffffffffu, s.n, l), __shfl_sync(0xffffffffu, s.len, l)};
+          int part = 0;
+          for (int rt = lane; rt < row_tiles(p, its); rt += 32) part += item_of(p, its, rt).units();
+          part = (int)__reduce_add_sync(0xffffffffu, (unsigned)part);
+          if (lane == l) sum = part;
+        }
+        return sum;
+      }
+    }
+    for (int rt = 0; rt < tiles; ++rt) sum += item_of(p, s, rt).units();
     return sum;
   }
   // all threads: prefix[b] = units in front of sequence b, prefix[B] = all (shared memory)
@@ -103,7 +121,7 @@ struct Line {
     int carry = 0;
     for (int base = 0; base < p.batch.B; base += blockDim.x) {
       const int b = base + threadIdx.x;
-      const int mine = b < p.batch.B ? units_of(p, sequence_of(p.batch, b)) * p.Hk : 0;
+      const int mine = units_of(p, b < p.batch.B ? sequence_of(p.batch, b) : Sequence{0, 0, 0}) * p.Hk;
       int x = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -451,6 +469,69 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
       dst[j] = *reinterpret_cast<const uint32_t*>(&v);
     }
     if (p.lse && lane == 0) p.lse[(int64_t)token * p.H + head] = sum == 0.0f ? -INFINITY : (top - kBase + log2f(sum)) * 0.6931471805599453f;
+  }
+}
+
+// The same for items of 128 rows and more: CTA (w, y) takes runs y, y + gridDim.y, ... of 32 rows.  A lane has a row and a warp every eighth group of four
+// channels, as the parts lie in memory (what a softmax thread has of its row in registers goes there a line at a time); rows of the
+// output come together in shared memory.
+constexpr int kCombineRowsThreads = 256;
+template <int D, int R>
+__global__ void __launch_bounds__(kCombineRowsThreads, 4)
+combine_rows_kernel(const __grid_constant__ CacheFwdParams p) {
+  constexpr int kWarps = kCombineRowsThreads / 32, kGroups = D / 4 / kWarps, kPitch = D + 8;
+  __shared__ __align__(16) __nv_bfloat16 s_out[32 * kPitch];
+  pdl_wait();
+  const int4 b0 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[0], b1 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[1];
+  const int before = b0.x, units = b0.y, share = b0.z, token0 = b0.w, row0 = b1.x, rows = b1.y, h = b1.z;
+  if (before == 0 || before > share) return;
+  const int w0 = blockIdx.x, parts = 1 + (units - before + share - 1) / share;
+  auto slot_of = [&](int i) { return 2 * (w0 + i) + (i > 0 || before == share ? 0 : 1); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int r0 = blockIdx.y * 32; r0 < rows; r0 += gridDim.y * 32) {
+    const int r = r0 + lane;      // (rows behind the item's last are parts' rows all the same, of no meaning)
+    float top = -INFINITY;
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) top = fmaxf(top, p.part_ml[((int64_t)slot_of(i) * R + r) * 2]);
+    float sum = 0.0f, acc[kGroups][4] = {};
+#pragma unroll 2
+    for (int i = 0; i < parts; ++i) {
+      const int slot = slot_of(i);
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((int64_t)slot * R + r) * 2);
+      float4 v[kGroups];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) v[g] = *reinterpret_cast<const float4*>(p.part_o + (((int64_t)slot * (D / 4) + warp + g * kWarps) * R + r) * 4);
+      const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
+      sum = fmaf(ml.y, f, sum);
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        const float x[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[g][j] = ml.x == -INFINITY ? acc[g][j] : fmaf(x[j], f, acc[g][j]);      // (a part without keys has left no output)
+      }
+    }
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const __nv_bfloat162 a = __floats2bfloat162_rn(acc[g][0] * inv, acc[g][1] * inv), b = __floats2bfloat162_rn(acc[g][2] * inv, acc[g][3] * inv);
+      *reinterpret_cast<uint2*>(s_out + lane * kPitch + (warp + g * kWarps) * 4) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    }
+    if (p.lse && warp == 0 && r < rows) {
+      const int row = row0 + r, of = fast_div(row, p.by_G);
+      p.lse[(int64_t)(token0 + of) * p.H + h * p.G + row - of * p.G] = sum == 0.0f ? -INFINITY : (top - kBase + log2f(sum)) * 0.6931471805599453f;
+    }
+    __syncthreads();
+    constexpr int kLanes = D / 8;      // 16 bytes each
+#pragma unroll 1
+    for (int i = threadIdx.x; i < 32 * kLanes; i += kCombineRowsThreads) {
+      const int mine = i / kLanes, c = i % kLanes;
+      if (r0 + mine >= rows) continue;
+      const int row = row0 + r0 + mine, of = fast_div(row, p.by_G);
+      *reinterpret_cast<uint4*>(p.out + (int64_t)(token0 + of) * p.out_stride_t + (h * p.G + row - of * p.G) * p.out_stride_h + c * 8) =
+          *reinterpret_cast<const uint4*>(s_out + mine * kPitch + c * 8);
+    }
+    __syncthreads();
   }
 }
 
