@@ -703,6 +703,14 @@ int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame
   const long long tiles = (keys + tile_keys - 1) / tile_keys;
   int n = items * 16 <= sms ? 16 : 8;
   while (n > 1 && (items * n > std::max(2 * sms, 16) || n / 2 >= tiles)) n /= 2;
+  if (sink > 0 && items <= 2 * sms && items * n >= sms) {
+    // What is seen of long sequences has one length, that of window and first tokens, so a wave of equal clusters ends together: 32 sequences of 8
+    // heads, window 4000, E4M3: one CTA an item 46.7 us, two 54.4, the line 55.6; 16 of 8: two 28.2, the line 34.3; 12 of 12, 8000, bf16: two
+    // 74.6, the line 82.6.  The line wins where the wave's CTAs are too few to keep the memory busy (some 1.7 an SM) for longer than its own
+    // beginning and second launch take: 20 of 8, 4000: one 42.6, the line 39.1; 24 of 8, 8000: 77.8 and 72.7; 10 of 8, 16,000: two 77.3, the line 61.7.
+    const double busy = items * n / (1.7 * sms);
+    return busy >= 1.0 || keys / n * (1.0 - busy) < (n == 1 ? 1200.0 : 600.0) ? n : 0;
+  }
   if (n == 1 && items <= 2 * sms && tiles >= 16) n = 2;
   if (items > 2 * sms ? tiles >= 32 : items * n < sms ? tiles > 12 * n : keys > 2304LL * n) return 0;
   return n;
