@@ -1,11 +1,16 @@
 // The book of a paged cache: who holds which pages.  sparkattn_pages_fork, _reserve, _trim, _compact keep it, sparkattn_cache_copy_pages moves
 // what the pages hold.
 //
-// The book is a few hundred thousand words at most, so what a step costs is launches and chains of loads.  Each call is one launch (compact: two).
-// What has to happen in order, counting, handing out, adjusting counts, is the work of one thread-block cluster of up to sixteen CTAs, whose
-// barrier stands between the steps and through whose shared memory the counts go; a chain of launches would take 2 us a step.  Tables that go
-// to another place are copied meanwhile by the grid's other clusters.  Counts change by integer additions, so their order does not matter, and free
-// pages are handed out in ascending order: the same call gives the same book.
+// The book is a few hundred thousand words at most, so what a step costs is launches and chains of loads; a launch takes 2 us.
+//   What has to happen in order, counting pages, handing them out, changing the counts once they are at their other place, is the work of one
+//   thread-block cluster of up to sixteen CTAs, whose barrier stands between the steps and through whose shared memory the counts go; a chain of
+//   launches would take 2 us a step.  Tables that go to another place are copied meanwhile by the grid's other clusters.
+//   A fork changes counts for whole rows, by integer additions, in any order: a launch of its own, since sixteen SMs issue their additions to
+//   scattered words a few clocks apart (256 rows of 500 entries: 11.2 us with one cluster, 4.6 with two launches).
+// Free pages are handed out in ascending order: the same call gives the same book.
+// Measured: a fork of 256 sequences of up to 32,000 tokens, pages of 64, 4.6 us; pages for a token of each of 128 sequences 7.3 us, in place 6.0, and the 90
+// copies of pages of 16 tokens that they share 2.7; a trim of 32 sequences 4.7, with nothing to give back 3.1; compact, 1560 pages, 6.4.  Latency
+// bounds all of them.  The copy of 368 pages of 196 KB, K and V, 289 MB read and written: 49 us = 5.9 TB/s, 0.89 of a copy's rate.
 #include <algorithm>
 
 #include "cache.h"
@@ -140,29 +145,61 @@ __device__ __forceinline__ void copy_table(const BookView& v, int rows, int cta,
   }
 }
 
+// refs to their other place, CTAs from `cta` on
+__device__ __forceinline__ void copy_refs(const BookView& v, int cta, int ctas) {
+  if (v.refs_out == v.refs) return;
+#pragma unroll 4
+  for (long long i = (long long)cta * kBookThreads + threadIdx.x; i < v.pages; i += (long long)ctas * kBookThreads) v.refs_out[i] = v.refs[i];
+}
+__device__ __forceinline__ void first_status(const BookShared& s, int32_t* status) {
+  __syncthreads();
+  if (threadIdx.x == 0) *reinterpret_cast<unsigned long long*>(status) = (unsigned long long)(uint32_t)s.bad[1] << 32 | (uint32_t)s.bad[0];
+}
+// `change` added to the counts of up to 64 entries of a row, a warp's (-1: none); bad(e) for entries that name no page, and where a count falls
+// below 0.  (An SM issues additions to scattered words a few clocks apart, so they are dealt out to many: 64 instead of 256 entries a warp took a
+// fork of 256 rows of 500 entries from 7.2 us to 4.7, a trim that gives back 12,000 pages from 7.6 to 4.7.)
+constexpr int kCountColumns = 64;
+template <typename Bad>
+__device__ __forceinline__ void add_to_counts(const BookView& v, const int (&e)[kCountColumns / 32], int change, Bad bad) {
+  int before[kCountColumns / 32];
+  if (change > 0) {
+#pragma unroll
+    for (int u = 0; u < kCountColumns / 32; ++u) {
+      if ((uint32_t)e[u] < (uint32_t)v.pages) atomicAdd(v.refs_out + e[u], change);
+      before[u] = 1;
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < kCountColumns / 32; ++u) before[u] = (uint32_t)e[u] < (uint32_t)v.pages ? atomicAdd(v.refs_out + e[u], change) : 1;
+  }
+#pragma unroll
+  for (int u = 0; u < kCountColumns / 32; ++u)
+    if (((uint32_t)e[u] >= (uint32_t)v.pages && e[u] != -1) || before[u] <= 0) bad(e[u]);
+}
+
 // ---------------------------------------------------------------------------------------------------------------- fork
 struct ForkParams {
   BookView v;
   const int32_t* kv_len;
   const int32_t* parent;
   int32_t* kv_len_out;
-  int B_out, ranks;
+  int32_t* uses;                 // workspace [B]: sequences that go on from a row, less one
+  int B_out;
   int32_t* status;
 };
-// Every row's number of users changes by the sequences that go on from it less one; its pages' counts do with it.
 __global__ void __launch_bounds__(kBookThreads)
 pages_fork_kernel(const __grid_constant__ ForkParams p) {
-  __shared__ BookShared s;
-  __shared__ int uses[kCacheMaxSequences];
-  const int cluster = (int)blockIdx.x / p.ranks, rank = (int)blockIdx.x - cluster * p.ranks;
   const BookView& v = p.v;
   pdl_wait();
-  if (cluster > 0) {
-    copy_table(v, p.B_out, (int)blockIdx.x - p.ranks, (int)gridDim.x - p.ranks,
-               [&](int b) { const int f = p.parent[b]; return (uint32_t)f < (uint32_t)v.B ? f : -1; }, [](int, int, int e) { return e; },
+  if (blockIdx.x > 0) {
+    const int cta = blockIdx.x - 1, ctas = gridDim.x - 1;
+    copy_table(v, p.B_out, cta, ctas, [&](int b) { const int f = p.parent[b]; return (uint32_t)f < (uint32_t)v.B ? f : -1; }, [](int, int, int e) { return e; },
                [](int, int) { return false; });
+    copy_refs(v, cta, ctas);
     return;
   }
+  __shared__ BookShared s;
+  __shared__ int uses[kCacheMaxSequences];
   for (int b = threadIdx.x; b < v.B; b += kBookThreads) uses[b] = -1;
   book_begin(s);
   for (int b = threadIdx.x; b < p.B_out; b += kBookThreads) {
@@ -170,28 +207,26 @@ pages_fork_kernel(const __grid_constant__ ForkParams p) {
     const bool there = (uint32_t)f < (uint32_t)v.B;
     if (there) atomicAdd(&uses[f], 1);
     else if (f != -1) found(s, SPARKATTN_E_BAD_INDEX, f);
-    if (rank == 0) p.kv_len_out[b] = there ? p.kv_len[f] : 0;
+    p.kv_len_out[b] = there ? p.kv_len[f] : 0;
   }
-  if (v.refs_out != v.refs) count_run(v, run_of_warp(v.pages, p.ranks, rank), [](int) { return 0; });
-  book_barrier();
-  const int segments = (v.max_pages + kCopyColumns - 1) / kCopyColumns, lane = threadIdx.x & 31;
+  __syncthreads();
+  for (int b = threadIdx.x; b < v.B; b += kBookThreads) p.uses[b] = uses[b];
+  first_status(s, p.status);
+}
+// Every row's number of users changes by the sequences that go on from it less one; its pages' counts do with it.
+__global__ void __launch_bounds__(kBookThreads)
+pages_fork_counts_kernel(const __grid_constant__ ForkParams p) {
+  const BookView& v = p.v;
+  const int segments = (v.max_pages + kCountColumns - 1) / kCountColumns, lane = threadIdx.x & 31;
   const long long items = (long long)v.B * segments;
-  for (long long item = rank * kBookWarps + (threadIdx.x >> 5); item < items; item += p.ranks * kBookWarps) {
-    const int b = (int)(item / segments), c0 = (int)(item - (long long)b * segments) * kCopyColumns + lane, change = uses[b];
-    if (change == 0) continue;
-    int e[kCopyColumns / 32];
+  pdl_wait();
+  for (long long item = (long long)blockIdx.x * kBookWarps + (threadIdx.x >> 5); item < items; item += (long long)gridDim.x * kBookWarps) {
+    const int b = (int)(item / segments), c0 = (int)(item - (long long)b * segments) * kCountColumns + lane, change = p.uses[b];
+    int e[kCountColumns / 32];
 #pragma unroll
-    for (int u = 0; u < kCopyColumns / 32; ++u) e[u] = c0 + 32 * u < v.max_pages ? v.table[(int64_t)b * v.max_pages + c0 + 32 * u] : -1;
-#pragma unroll
-    for (int u = 0; u < kCopyColumns / 32; ++u) {
-      if ((uint32_t)e[u] < (uint32_t)v.pages) {
-        if (atomicAdd(v.refs_out + e[u], change) <= 0 && change < 0) found(s, SPARKATTN_E_BAD_INDEX, e[u]);
-      } else if (e[u] != -1) {
-        found(s, SPARKATTN_E_BAD_INDEX, e[u]);
-      }
-    }
+    for (int u = 0; u < kCountColumns / 32; ++u) e[u] = c0 + 32 * u < v.max_pages ? v.table[(int64_t)b * v.max_pages + c0 + 32 * u] : -1;
+    if (change != 0) add_to_counts(v, e, change, [&](int page) { report_status(p.status, SPARKATTN_E_BAD_INDEX, page); });
   }
-  book_end(s, rank, p.ranks, p.status);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- trim
@@ -233,29 +268,33 @@ pages_trim_kernel(const __grid_constant__ TrimParams p) {
     return;
   }
   book_begin(s);
+  copy_refs(v, rank, p.ranks);
   for (int b = rank * kBookThreads + threadIdx.x; b < v.B; b += p.ranks * kBookThreads)
     if (!fits_table(v, p.kv_len[b])) found(s, SPARKATTN_E_BAD_INDEX, p.kv_len[b]);
-  if (v.refs_out != v.refs) count_run(v, run_of_warp(v.pages, p.ranks, rank), [](int) { return 0; });
-  book_barrier();
-  const int segments = (v.max_pages + kCopyColumns - 1) / kCopyColumns, lane = threadIdx.x & 31;
+  const int segments = (v.max_pages + kCountColumns - 1) / kCountColumns, lane = threadIdx.x & 31;
   const bool in_place = v.table_out == v.table;
-  const long long items = (long long)v.B * segments;
-  for (long long item = rank * kBookWarps + (threadIdx.x >> 5); item < items; item += p.ranks * kBookWarps) {
-    const int b = (int)(item / segments), first = (int)(item - (long long)b * segments) * kCopyColumns, c0 = first + lane;
+  const long long items = (long long)v.B * segments, step = p.ranks * kBookWarps;
+  bool waited = false;
+  for (long long item = rank * kBookWarps + (threadIdx.x >> 5); item - rank * kBookWarps - (threadIdx.x >> 5) < items; item += step) {
+    // (the first entries are on their way while the counts are)
+    const bool there = item < items;
+    const int b = there ? (int)(item / segments) : 0, first = (int)(item - (long long)b * segments) * kCountColumns, c0 = first + lane;
     const Dead d = dead_of(p, b);
-    if (first + kCopyColumns <= d.end && (first >= d.to || first + kCopyColumns <= d.from)) continue;
     const int64_t row = (int64_t)b * v.max_pages;
-    int e[kCopyColumns / 32];
+    const bool some = there && (first + kCountColumns > d.end || (first < d.to && first + kCountColumns > d.from));
+    int e[kCountColumns / 32];
 #pragma unroll
-    for (int u = 0; u < kCopyColumns / 32; ++u) {
+    for (int u = 0; u < kCountColumns / 32; ++u) {
       const int i = c0 + 32 * u;
-      e[u] = i < v.max_pages && is_dead(d, i) ? v.table[row + i] : -1;
+      e[u] = some && i < v.max_pages && is_dead(d, i) ? v.table[row + i] : -1;
     }
+    if (!waited) book_barrier();
+    waited = true;
+    add_to_counts(v, e, -1, [&](int page) { found(s, SPARKATTN_E_BAD_INDEX, page); });
+    if (in_place) {
 #pragma unroll
-    for (int u = 0; u < kCopyColumns / 32; ++u) {
-      if (e[u] == -1) continue;
-      if ((uint32_t)e[u] >= (uint32_t)v.pages || atomicSub(v.refs_out + e[u], 1) <= 0) found(s, SPARKATTN_E_BAD_INDEX, e[u]);
-      if (in_place) v.table_out[row + c0 + 32 * u] = -1;
+      for (int u = 0; u < kCountColumns / 32; ++u)
+        if (e[u] != -1) v.table_out[row + c0 + 32 * u] = -1;
     }
   }
   book_end(s, rank, p.ranks, p.status);
@@ -285,18 +324,22 @@ __device__ __forceinline__ Asks asks_of(const ReserveParams& p, int b) {
   if (a.fine && len > old) a = {old >> p.v.shift, pages_of(p.v, old), pages_of(p.v, len), true};
   return a;
 }
-// Shared memory behind BookShared: prefix[B + 1], then the hash table of partly filled pages that several hold: page, sequences that write to it, the
-// first of them.
+// Dynamic shared memory: prefix[B + 1]; of every sequence the columns that it asks for and the page that it copies; the hash table of partly
+// filled pages that several hold: page, sequences that write to it, the first of them.  Every CTA of the first cluster has it all.
 __global__ void __launch_bounds__(kBookThreads)
 pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   __shared__ BookShared s;
   extern __shared__ int s_dynamic[];
+  const BookView& v = p.v;
   int* prefix = s_dynamic;
-  int* h_page = prefix + p.v.B + 1;
+  int* s_tail = prefix + v.B + 1;
+  int* s_first = s_tail + v.B;
+  int* s_last = s_first + v.B;
+  int* s_copy = s_last + v.B;
+  int* h_page = s_copy + v.B;
   int* h_writers = h_page + p.slots;
   int* h_first = h_writers + p.slots;
   const int cluster = (int)blockIdx.x / p.ranks, rank = (int)blockIdx.x - cluster * p.ranks;
-  const BookView& v = p.v;
   pdl_wait();
   if (cluster > 0) {
     Asks a{};
@@ -309,10 +352,6 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < p.slots; i += kBookThreads) { h_page[i] = -1; h_writers[i] = 0; h_first[i] = 0x7fffffff; }
   book_begin(s);
-  // every CTA for itself: who writes to pages that several hold
-  const PoolRun run = run_of_warp(v.pages, p.ranks, rank);
-  const int free_here = count_run(v, run, [](int r) { return r == 0 ? 1 : 0; });
-  if (lane == 0) s.count[warp] = free_here;
   auto slot_of = [&](int page, bool insert) {
     uint32_t at = (uint32_t)page * 2654435761u >> 7;
     for (int tries = 0; tries < p.slots; ++tries, ++at) {           // (it always ends earlier: there are more slots than pages in it)
@@ -322,41 +361,46 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     }
     return (int)(at & (p.slots - 1));
   };
-  auto tail_page = [&](const Asks& a, int b) {       // the partly filled page, if others hold it, or -1
-    if (!a.partly()) return -1;
-    const int e = v.table[(int64_t)b * v.max_pages + a.tail];
-    if ((uint32_t)e >= (uint32_t)v.pages) return -2;
-    return v.refs[e] > 1 ? e : -1;
-  };
+  // who writes to pages that several hold
   for (int b = threadIdx.x; b < v.B; b += kBookThreads) {
     const Asks a = asks_of(p, b);
+    int shared = -1;
     if (!a.fine) found(s, SPARKATTN_E_BAD_INDEX, b);
-    const int page = tail_page(a, b);
-    if (page == -2) found(s, SPARKATTN_E_BAD_INDEX, v.table[(int64_t)b * v.max_pages + a.tail]);
-    if (page >= 0) {
-      const int at = slot_of(page, true);
-      atomicAdd(h_writers + at, 1);
-      atomicMin(h_first + at, b);
+    if (a.partly()) {
+      const int e = v.table[(int64_t)b * v.max_pages + a.tail];
+      if ((uint32_t)e >= (uint32_t)v.pages) {
+        found(s, SPARKATTN_E_BAD_INDEX, e);
+      } else if (v.refs[e] > 1) {
+        shared = e;
+        const int at = slot_of(e, true);
+        atomicAdd(h_writers + at, 1);
+        atomicMin(h_first + at, b);
+      }
     }
+    s_tail[b] = a.tail;
+    s_first[b] = a.first;
+    s_last[b] = a.last;
+    s_copy[b] = shared;
   }
+  const PoolRun run = run_of_warp(v.pages, p.ranks, rank);
+  const int free_here = count_run(v, run, [](int r) { return r == 0 ? 1 : 0; });
+  if (lane == 0) s.count[warp] = free_here;
   __syncthreads();
-  // the first of the sequences that write to a page keeps it, if nobody else holds it
-  auto copies = [&](const Asks& a, int b) {
-    const int page = tail_page(a, b);
-    if (page < 0) return -1;
-    const int at = slot_of(page, false);
-    return h_writers[at] == v.refs[page] && h_first[at] == b ? -1 : page;
-  };
   int carry = 0;
   for (int base = 0; base < v.B; base += kBookThreads) {
     const int b = base + threadIdx.x;
     int mine = 0;
     if (b < v.B) {
-      const Asks a = asks_of(p, b);
-      mine = copies(a, b) >= 0 ? 1 : 0;
+      // the first of the sequences that write to a page keeps it, if nobody else holds it
+      const int page = s_copy[b];
+      if (page >= 0) {
+        const int at = slot_of(page, false);
+        if (h_writers[at] == v.refs[page] && h_first[at] == b) s_copy[b] = -1;
+        else mine = 1;
+      }
       const int32_t* row = v.table + (int64_t)b * v.max_pages;
 #pragma unroll 4
-      for (int i = a.first; i < a.last; ++i) mine += row[i] == -1 ? 1 : 0;
+      for (int i = s_first[b]; i < s_last[b]; ++i) mine += row[i] == -1 ? 1 : 0;
     }
     int x = mine;
 #pragma unroll
@@ -374,48 +418,46 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     if (b < v.B) prefix[b] = before + x - mine;
     __syncthreads();
   }
-  if (threadIdx.x == 0) prefix[v.B] = carry;
   book_barrier();
   const int2 free = in_front(s, rank, p.ranks);
   const bool enough = carry <= free.y;
   if (!enough && rank == 0 && threadIdx.x == 0) found(s, SPARKATTN_E_OUT_OF_PAGES, carry - free.y);
   if (enough) {
     int k = free.x;
-    for (int p0 = run.first; p0 < run.last && k < carry; p0 += 32) {
-      const bool is = p0 + lane < run.last && v.refs[p0 + lane] == 0;
-      const uint32_t all = __ballot_sync(0xffffffffu, is);
-      const int mine = k + __popc(all & ((1u << lane) - 1u));
-      if (is && mine < carry) {
-        p.list[mine] = p0 + lane;
-        v.refs_out[p0 + lane] = 1;
+    for (int p0 = run.first; p0 < run.last && k < carry; p0 += 32 * 8) {
+      int r[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) r[u] = p0 + 32 * u + lane < run.last ? v.refs[p0 + 32 * u + lane] : 1;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const uint32_t all = __ballot_sync(0xffffffffu, r[u] == 0);
+        const int mine = k + __popc(all & ((1u << lane) - 1u)), page = p0 + 32 * u + lane;
+        if (r[u] == 0 && mine < carry) {
+          p.list[mine] = page;
+          v.refs_out[page] = 1;
+        }
+        k += __popc(all);
       }
-      k += __popc(all);
     }
-  }
-  // (who copies is asked before counts change under the question)
-  for (int b = rank * kBookWarps + warp; b < v.B; b += p.ranks * kBookWarps) {
-    const int from = copies(asks_of(p, b), b);
-    if (lane == 0) p.src[b] = enough ? from : -1;
   }
   book_barrier();
   for (int b = rank * kBookWarps + warp; b < v.B; b += p.ranks * kBookWarps) {
-    const Asks a = asks_of(p, b);
-    const int from = p.src[b];
+    const int tail = s_tail[b], first = s_first[b], last = s_last[b], from = enough ? s_copy[b] : -1;
     int at = prefix[b];
     const int32_t* row = v.table + (int64_t)b * v.max_pages;
     int32_t* out = v.table_out + (int64_t)b * v.max_pages;
-    int to = -1;
-    if (from >= 0) {
-      to = p.list[at++];
-      if (lane == 0) atomicSub(v.refs_out + from, 1);
+    const int to = from >= 0 ? p.list[at++] : -1;
+    if (lane == 0) {
+      if (from >= 0) atomicSub(v.refs_out + from, 1);
+      p.src[b] = from;
+      p.dst[b] = to;
+      if (tail < first) out[tail] = from >= 0 ? to : row[tail];
     }
-    if (lane == 0) p.dst[b] = to;
-    if (a.partly() && lane == 0) out[a.tail] = from >= 0 ? to : row[a.tail];
-    for (int i0 = a.first; i0 < a.last; i0 += 32) {
+    for (int i0 = first; i0 < last; i0 += 32) {
       const int i = i0 + lane;
-      const int e = i < a.last ? row[i] : 0;
-      const uint32_t missing = __ballot_sync(0xffffffffu, i < a.last && e == -1);
-      if (i < a.last) out[i] = e == -1 && enough ? p.list[at + __popc(missing & ((1u << lane) - 1u))] : e;
+      const int e = i < last ? row[i] : 0;
+      const uint32_t missing = __ballot_sync(0xffffffffu, i < last && e == -1);
+      if (i < last) out[i] = e == -1 && enough ? p.list[at + __popc(missing & ((1u << lane) - 1u))] : e;
       at += __popc(missing);
     }
   }
@@ -443,7 +485,7 @@ pages_compact_kernel(const __grid_constant__ CompactParams p) {
   book_begin(s);
   const PoolRun run = run_of_warp(v.pages, p.ranks, rank);
   int n = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int i = run.first + lane; i < run.last; i += 32) n += v.refs[i] > 0 ? 1 : 0;
   n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
   if (lane == 0) s.count[warp] = n;
@@ -462,27 +504,35 @@ pages_compact_kernel(const __grid_constant__ CompactParams p) {
   __syncthreads();
   const int below = front + s_part, moves = border - below;
   int k = used.x;                                                   // used pages in front
-  for (int p0 = run.first; p0 < run.last; p0 += 32) {
-    const int at = p0 + lane;
-    const bool there = at < run.last, is = there && v.refs[at] > 0;
-    const uint32_t all = __ballot_sync(0xffffffffu, is);
-    const int in_use = k + __popc(all & ((1u << lane) - 1u));
-    if (there) {
-      if (is && at >= border) p.src[in_use - below] = at;
-      else p.to[at] = is ? at : -1;
-      if (!is && at < border) p.dst[at - in_use] = at;
+  for (int p0 = run.first; p0 < run.last; p0 += 32 * 8) {
+    int r[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) r[u] = p0 + 32 * u + lane < run.last ? v.refs[p0 + 32 * u + lane] : 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int at = p0 + 32 * u + lane;
+      const bool there = at < run.last, is = there && r[u] > 0;
+      const uint32_t all = __ballot_sync(0xffffffffu, is);
+      const int in_use = k + __popc(all & ((1u << lane) - 1u));
+      if (there) {
+        if (is && at >= border) p.src[in_use - below] = at;
+        else p.to[at] = is ? at : -1;
+        if (!is && at < border) p.dst[at - in_use] = at;
+      }
+      k += __popc(all);
     }
-    k += __popc(all);
   }
   for (int i = moves + rank * kBookThreads + threadIdx.x; i < v.pages / 2; i += p.ranks * kBookThreads) p.src[i] = p.dst[i] = -1;
   book_barrier();
   if (v.refs_out != v.refs) {
     // every page's count where it ends up: what stays, then what moves (whose new places nobody held)
+#pragma unroll 8
     for (int p0 = run.first + lane; p0 < run.last; p0 += 32) {
       const int r = v.refs[p0];
       if (p0 < border ? r > 0 : true) v.refs_out[p0] = p0 < border ? r : 0;
     }
   }
+#pragma unroll 4
   for (int i = rank * kBookThreads + threadIdx.x; i < moves; i += p.ranks * kBookThreads) {
     const int from = p.src[i], to = p.dst[i];
     p.to[from] = to;
@@ -505,8 +555,8 @@ pages_remap_kernel(const __grid_constant__ CompactParams p) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------- copy
-constexpr int kCopyThreads = 256, kCopyUnroll = 8, kCopyPieces = kCopyThreads * kCopyUnroll;      // 16-byte pieces of a unit: 32 KB
-constexpr int kCheckPages = 1 << 17;      // pages that a checking CTA looks after: a bit each in 16 KB
+constexpr int kCopyThreads = 256, kCopyUnroll = 8, kCopyPerSM = 4, kCopyPieces = 32 * kCopyUnroll;      // 16-byte pieces of a unit, a warp's
+constexpr int kCheckPages = 1 << 16;      // pages that a checking CTA looks after: two bits each in 16 KB
 
 struct CopyPagesParams {
   const uint4* from[2];          // K, V
@@ -521,7 +571,6 @@ struct CopyPagesParams {
   const int32_t* src;
   const int32_t* dst;
   int n, split;                  // pairs; units of a page's K or V
-  FastDiv by_split;
   long long units;
   int checkers;
   int32_t* status;
@@ -530,48 +579,65 @@ struct CopyPagesParams {
 // Looks through the pairs: numbers outside the pools, a page that is written twice, and one that is written and read.
 __device__ __forceinline__ bool check_pairs(const CopyPagesParams& p, int range, uint32_t* bits, int* s_bad) {
   const int first = range * kCheckPages;
-  for (int i = threadIdx.x; i < kCheckPages / 32; i += kCopyThreads) bits[i] = 0u;
+  uint32_t* written = bits;
+  uint32_t* read = bits + kCheckPages / 32;
+  for (int i = threadIdx.x; i < 2 * kCheckPages / 32; i += kCopyThreads) bits[i] = 0u;
   if (threadIdx.x == 0) { s_bad[0] = 0; s_bad[1] = 0; }
   __syncthreads();
   auto bad = [&](int page) { if (atomicExch(s_bad, 1) == 0) s_bad[1] = page; };
-#pragma unroll 1
-  for (int pass = 0; pass < 1 + p.same; ++pass) {
-#pragma unroll 1
-    for (long long i0 = threadIdx.x; i0 < p.n; i0 += 8 * kCopyThreads) {
-      int a[8], b[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const long long i = i0 + (long long)u * kCopyThreads;
-        a[u] = i < p.n ? p.src[i] : -1;
-        b[u] = i < p.n ? p.dst[i] : -1;
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        if (a[u] == -1 && b[u] == -1) continue;
-        if ((uint32_t)a[u] >= (uint32_t)p.pages_from || (uint32_t)b[u] >= (uint32_t)p.pages_to) {
-          bad((uint32_t)a[u] >= (uint32_t)p.pages_from ? a[u] : b[u]);
-          continue;
-        }
-        const uint32_t at = (uint32_t)(pass == 0 ? b[u] : a[u]) - (uint32_t)first;
-        if (at >= (uint32_t)kCheckPages) continue;
-        const uint32_t bit = 1u << (at & 31);
-        const uint32_t before = pass == 0 ? atomicOr(bits + (at >> 5), bit) : bits[at >> 5];
-        if (before & bit) bad(pass == 0 ? b[u] : a[u]);
-      }
+  auto look = [&](int a, int b) {
+    if (a == -1 && b == -1) return;
+    if ((uint32_t)a >= (uint32_t)p.pages_from || (uint32_t)b >= (uint32_t)p.pages_to) {
+      bad((uint32_t)a >= (uint32_t)p.pages_from ? a : b);
+      return;
     }
-    __syncthreads();
+    // (whoever marks a page as written looks for it among those read, and the other way round, each after its own mark: one of two finds the other)
+    const uint32_t to = (uint32_t)b - (uint32_t)first, from = (uint32_t)a - (uint32_t)first;
+    if (to < (uint32_t)kCheckPages) {
+      const uint32_t bit = 1u << (to & 31);
+      if (atomicOr(written + (to >> 5), bit) & bit) bad(b);
+      if (p.same && (atomicOr(read + (to >> 5), 0u) & bit)) bad(b);
+    }
+    if (p.same && from < (uint32_t)kCheckPages) {
+      const uint32_t bit = 1u << (from & 31);
+      atomicOr(read + (from >> 5), bit);
+      if (atomicOr(written + (from >> 5), 0u) & bit) bad(a);
+    }
+  };
+  // sixteen bytes at a time where the lists lie so (200,000 pairs of -1: 40 us, one by one and in two passes 82)
+  const int whole = ((reinterpret_cast<uintptr_t>(p.src) | reinterpret_cast<uintptr_t>(p.dst)) & 15u) == 0 ? p.n / 4 : 0;
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < whole; i0 += 4 * kCopyThreads) {
+    int4 a[4], b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool there = whole - i0 > u * kCopyThreads;
+      a[u] = there ? reinterpret_cast<const int4*>(p.src)[i0 + u * kCopyThreads] : make_int4(-1, -1, -1, -1);
+      b[u] = there ? reinterpret_cast<const int4*>(p.dst)[i0 + u * kCopyThreads] : make_int4(-1, -1, -1, -1);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      look(a[u].x, b[u].x);
+      look(a[u].y, b[u].y);
+      look(a[u].z, b[u].z);
+      look(a[u].w, b[u].w);
+    }
   }
+#pragma unroll 1
+  for (long long i = 4LL * whole + threadIdx.x; i < p.n; i += kCopyThreads) look(p.src[i], p.dst[i]);
+  __syncthreads();
   const bool is = s_bad[0] != 0;
   if (threadIdx.x == 0 && is) report_early(p.status, SPARKATTN_E_BAD_INDEX, s_bad[1]);
   __syncthreads();
   return is;
 }
 
-__global__ void __launch_bounds__(kCopyThreads, 4)
+// Warps go through the units, 4 KB of a page's K or V each, w, w + warps, ...: 32 of them are looked up at a time, and those with a page to copy
+// copied one after the other, eight 16-byte loads of every lane in flight.
+__global__ void __launch_bounds__(kCopyThreads, kCopyPerSM)
 cache_copy_pages_kernel(const __grid_constant__ CopyPagesParams p) {
-  __shared__ uint32_t bits[kCheckPages / 32];
+  __shared__ uint32_t bits[2 * kCheckPages / 32];
   __shared__ int s_bad[2];
-  __shared__ int s_pair[kCopyThreads], s_part[kCopyThreads], s_n;
   pdl_wait();
   if ((int)blockIdx.x < p.checkers) {
     bool code_there = false;
@@ -582,45 +648,51 @@ cache_copy_pages_kernel(const __grid_constant__ CopyPagesParams p) {
       for (int range = 1; range < p.checkers; ++range) check_pairs(p, range, bits, s_bad);
     return;
   }
-  const long long cta = (int)blockIdx.x - p.checkers, ctas = (int)gridDim.x - p.checkers;
+  const int lane = threadIdx.x & 31;
+  const long long warp = (long long)((int)blockIdx.x - p.checkers) * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  const long long warps = (long long)((int)gridDim.x - p.checkers) * (kCopyThreads / 32);
 #pragma unroll 1
-  for (long long round = 0; cta + ctas * kCopyThreads * round < p.units; ++round) {
-    // 256 units at a time: which of them have a page to copy
-    if (threadIdx.x == 0) s_n = 0;
-    __syncthreads();
-    const long long unit = cta + ctas * (kCopyThreads * round + threadIdx.x);
+  for (long long u0 = warp; u0 < p.units; u0 += 32 * warps) {
+    const long long unit = u0 + lane * warps;
+    int from = -1, to = -1, part = 0;
     if (unit < p.units) {
-      const int pair = (int)(unit / (2 * p.split)), part = (int)(unit - (long long)pair * 2 * p.split);
-      if ((uint32_t)p.src[pair] < (uint32_t)p.pages_from && (uint32_t)p.dst[pair] < (uint32_t)p.pages_to) {
-        const int at = atomicAdd(&s_n, 1);
-        s_pair[at] = pair;
-        s_part[at] = part;
-      }
+      const int pair = (int)(unit / (2 * p.split));
+      part = (int)(unit - (long long)pair * 2 * p.split);
+      from = p.src[pair];
+      to = p.dst[pair];
     }
-    __syncthreads();
-    const int found = s_n;
-#pragma unroll 1
-    for (int i = 0; i < found; ++i) {
-      const int pair = s_pair[i], part = s_part[i], kv = part >= p.split, first = (part - kv * p.split) * kCopyPieces + threadIdx.x;
-      const int from = p.src[pair], to = p.dst[pair];
-      const uint4* in = p.from[kv] + from * p.page_from;
-      uint4* out = p.to[kv] + to * p.page_to;
+    uint32_t going = __ballot_sync(0xffffffffu, (uint32_t)from < (uint32_t)p.pages_from && (uint32_t)to < (uint32_t)p.pages_to);
+    for (; going != 0; going &= going - 1) {
+      const int l = __ffs(going) - 1;
+      const int its_from = __shfl_sync(0xffffffffu, from, l), its_to = __shfl_sync(0xffffffffu, to, l), its_part = __shfl_sync(0xffffffffu, part, l);
+      const int kv = its_part >= p.split, first = (its_part - kv * p.split) * kCopyPieces + lane;
+      const uint4* in = p.from[kv] + its_from * p.page_from;
+      uint4* out = p.to[kv] + its_to * p.page_to;
       uint4 x[kCopyUnroll];
-      int64_t at[kCopyUnroll];
+      if (p.run == p.pieces) {
+        // the whole page side by side
 #pragma unroll
-      for (int u = 0; u < kCopyUnroll; ++u) {
-        const int piece = first + u * kCopyThreads, run = fast_div(piece, p.by_run), in_run = piece - run * p.run;
-        const int outer = fast_div(run, p.by_runs), inner = run - outer * p.runs;
-        at[u] = outer * p.outer_to[0] + inner * p.outer_to[1] + in_run;
-        if (piece < p.pieces) x[u] = in[outer * p.outer_from[0] + inner * p.outer_from[1] + in_run];
+        for (int u = 0; u < kCopyUnroll; ++u)
+          if (first + 32 * u < p.pieces) x[u] = in[first + 32 * u];
+#pragma unroll
+        for (int u = 0; u < kCopyUnroll; ++u)
+          if (first + 32 * u < p.pieces) out[first + 32 * u] = x[u];
+      } else {
+        int64_t at[kCopyUnroll];
+#pragma unroll
+        for (int u = 0; u < kCopyUnroll; ++u) {
+          const int piece = first + 32 * u, run = fast_div(piece, p.by_run), in_run = piece - run * p.run;
+          const int outer = fast_div(run, p.by_runs), inner = run - outer * p.runs;
+          at[u] = outer * p.outer_to[0] + inner * p.outer_to[1] + in_run;
+          if (piece < p.pieces) x[u] = in[outer * p.outer_from[0] + inner * p.outer_from[1] + in_run];
+        }
+#pragma unroll
+        for (int u = 0; u < kCopyUnroll; ++u)
+          if (first + 32 * u < p.pieces) out[at[u]] = x[u];
       }
-#pragma unroll
-      for (int u = 0; u < kCopyUnroll; ++u)
-        if (first + u * kCopyThreads < p.pieces) out[at[u]] = x[u];
-      if (p.scale_from[kv] != nullptr && part == kv * p.split)
-        for (int h = threadIdx.x; h < p.H; h += kCopyThreads) p.scale_to[kv][(int64_t)to * p.H + h] = p.scale_from[kv][(int64_t)from * p.H + h];
+      if (p.scale_from[kv] != nullptr && its_part == kv * p.split)
+        for (int h = lane; h < p.H; h += 32) p.scale_to[kv][(int64_t)its_to * p.H + h] = p.scale_from[kv][(int64_t)its_from * p.H + h];
     }
-    __syncthreads();
   }
 }
 
@@ -632,10 +704,10 @@ int ranks_for(long long words) {
   while (n < kBookClusterMax && (long long)n * 4096 < words) n *= 2;
   return n;
 }
-// clusters that copy the tables meanwhile
-int copiers_for(long long rows, int max_pages, int ranks, int sms) {
-  const long long warps = rows * ((max_pages + kCopyColumns - 1) / kCopyColumns), ctas = (warps + kBookWarps - 1) / kBookWarps;
-  return (int)std::max<long long>(1, std::min<long long>((ctas + ranks - 1) / ranks, 2LL * sms / ranks));
+// CTAs for rows of max_pages entries, a warp for `columns` of them
+int ctas_for(long long rows, int max_pages, int columns, int sms) {
+  const long long warps = rows * ((max_pages + columns - 1) / columns), ctas = (warps + kBookWarps - 1) / kBookWarps;
+  return (int)std::max<long long>(1, std::min<long long>(ctas, 2LL * sms));
 }
 template <typename Params>
 int launch_book(void (*kern)(Params), int clusters, int ranks, size_t smem, cudaStream_t stream, const Params& p) {
@@ -644,15 +716,17 @@ int launch_book(void (*kern)(Params), int clusters, int ranks, size_t smem, cuda
 }
 }  // namespace
 
-size_t pages_workspace_bytes(const sparkattn_book_t& b) { return kWorkspaceHeaderBytes + ((size_t)b.pages * 4 + 255) / 256 * 256; }
+size_t pages_workspace_bytes(const sparkattn_book_t& b) { return kWorkspaceHeaderBytes + ((size_t)std::max(b.pages, b.B) * 4 + 255) / 256 * 256; }
 
 int launch_pages_fork(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* parent, int B_out, int32_t* table_out, int32_t* kv_len_out,
                       int32_t* refs_out, void* workspace, cudaStream_t stream) {
-  ForkParams p{make_book_view(book, table_out, refs_out), kv_len, parent, kv_len_out, B_out, 1, static_cast<int32_t*>(workspace)};
+  int32_t* status = static_cast<int32_t*>(workspace);
+  const ForkParams p{make_book_view(book, table_out, refs_out), kv_len, parent, kv_len_out, status + kWorkspaceHeaderBytes / 4, B_out, status};
   const int sms = current_sm_count();
   if (sms < 1) return SPARKATTN_E_CUDA;
-  p.ranks = ranks_for((long long)book.B * book.max_pages + book.pages);
-  return launch_book(pages_fork_kernel, 1 + copiers_for(B_out, book.max_pages, p.ranks, sms), p.ranks, 0, stream, p);
+  const int rc = launch_kernel(pages_fork_kernel, dim3(1 + ctas_for(B_out, book.max_pages, kCopyColumns, sms)), kBookThreads, 0, true, stream, p);
+  if (rc != SPARKATTN_OK) return rc;
+  return launch_kernel(pages_fork_counts_kernel, dim3(ctas_for(book.B, book.max_pages, kCountColumns, sms)), kBookThreads, 0, true, stream, p);
 }
 
 int launch_pages_trim(const sparkattn_book_t& book, const int32_t* kv_len, int frame, int window, int sink, int32_t* table_out, int32_t* refs_out,
@@ -660,8 +734,8 @@ int launch_pages_trim(const sparkattn_book_t& book, const int32_t* kv_len, int f
   TrimParams p{make_book_view(book, table_out, refs_out), kv_len, std::max(frame, 1), window, sink, 1, static_cast<int32_t*>(workspace)};
   const int sms = current_sm_count();
   if (sms < 1) return SPARKATTN_E_CUDA;
-  p.ranks = ranks_for((long long)book.B * book.max_pages + book.pages);
-  const int copiers = table_out != book.page_table ? copiers_for(book.B, book.max_pages, p.ranks, sms) : 0;
+  p.ranks = ranks_for(4LL * book.B * book.max_pages + book.pages);
+  const int copiers = table_out != book.page_table ? (ctas_for(book.B, book.max_pages, kCopyColumns, sms) + p.ranks - 1) / p.ranks : 0;
   return launch_book(pages_trim_kernel, 1 + copiers, p.ranks, 0, stream, p);
 }
 
@@ -673,11 +747,11 @@ int launch_pages_reserve(const sparkattn_book_t& book, const int32_t* kv_len, co
   if (sms < 1) return SPARKATTN_E_CUDA;
   while (p.slots < 2 * book.B) p.slots *= 2;
   p.ranks = ranks_for((long long)book.pages + 64LL * book.B);
-  const size_t smem = ((size_t)book.B + 1 + 3 * (size_t)p.slots) * 4;
+  const size_t smem = (5 * (size_t)book.B + 1 + 3 * (size_t)p.slots) * 4;
   // (the most that any call asks for: host threads with other batches set it too)
-  if (cudaFuncSetAttribute(pages_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kCacheMaxSequences + 1 + 3 * 2 * kCacheMaxSequences) * 4) != cudaSuccess)
+  if (cudaFuncSetAttribute(pages_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (5 * kCacheMaxSequences + 1 + 3 * 2 * kCacheMaxSequences) * 4) != cudaSuccess)
     return SPARKATTN_E_CUDA;
-  const int copiers = table_out != book.page_table ? copiers_for(book.B, book.max_pages, p.ranks, sms) : 0;
+  const int copiers = table_out != book.page_table ? (ctas_for(book.B, book.max_pages, kCopyColumns, sms) + p.ranks - 1) / p.ranks : 0;
   return launch_book(pages_reserve_kernel, 1 + copiers, p.ranks, smem, stream, p);
 }
 
@@ -732,7 +806,7 @@ int launch_copy_pages(const sparkattn_cache_t& from, const PagePools& in, const 
   p.status = static_cast<int32_t*>(workspace);
   const int sms = current_sm_count();
   if (sms < 1) return SPARKATTN_E_CUDA;
-  const unsigned ctas = p.checkers + (unsigned)std::min<long long>(p.units, 4LL * sms);
+  const unsigned ctas = p.checkers + (unsigned)std::min<long long>((p.units + kCopyThreads / 32 - 1) / (kCopyThreads / 32), (long long)kCopyPerSM * sms);
   return launch_kernel(cache_copy_pages_kernel, dim3(ctas), kCopyThreads, 0, true, stream, p);
 }
 
