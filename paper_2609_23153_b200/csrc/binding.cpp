@@ -146,6 +146,11 @@ void same_layout(const at::Tensor& a, const at::Tensor& b) {
   TORCH_CHECK_VALUE(a.sizes() == b.sizes() && a.strides() == b.strides(), "tensors of one call must share shape and strides");
 }
 
+// The library launches on the current device, in its current stream.
+void check_here(const at::Tensor& x) {
+  TORCH_CHECK_VALUE(x.is_cuda(), "tensors of a call must be on a CUDA device");
+  TORCH_CHECK_VALUE(x.device().index() == c10::cuda::current_device(), "tensors of a call must be on the current CUDA device");
+}
 void* ptr(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 int32_t* iptr(const at::Tensor& t) { return static_cast<int32_t*>(ptr(t)); }
 float* fptr(const at::Tensor& t) { return static_cast<float*>(ptr(t)); }
@@ -659,7 +664,7 @@ PyObject* norm_rotate(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const sparkattn_norm_t* normed = norm.describe(qs.H, k.defined() ? ks.H : -1, qs.d, q.device());
   for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&q, &k, &q_out, &k_out})
     TORCH_CHECK_VALUE(!x->defined() || (x->scalar_type() == at::kBFloat16 && x->device() == q.device()), "expected bfloat16 tensors on one device");
-  TORCH_CHECK_VALUE(q.is_cuda(), "tensors of a call must be on a CUDA device");
+  check_here(q);
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
@@ -733,12 +738,12 @@ struct Book {
     TORCH_CHECK_VALUE(refs.scalar_type() == at::kInt && refs.dim() == 1 && refs.is_contiguous() && refs.device() == table.device(),
                       "refs is a contiguous int32 [pages] on the table's device");
     if (needs_len) words(len, table.size(0), "kv_len is a contiguous int32 [B] on the table's device");
-    TORCH_CHECK_VALUE(table.is_cuda(), "tensors of a call must be on a CUDA device");
     b.struct_size = sizeof(b);
     b.version = SPARKATTN_VERSION;
     b.B = (int32_t)table.size(0); b.max_pages = (int32_t)table.size(1); b.pages = (int32_t)refs.size(0); b.page = page;
     b.page_table = iptr(table); b.refs = iptr(refs);
   }
+  void check_device() const { check_here(table); }
   void outputs(at::Tensor given_table, at::Tensor given_refs, at::Tensor given_ws, int64_t rows, const Stream& stream) {
     table_out = given_table.defined() ? given_table : stream.output({rows, table.size(1)}, at::kInt, table);
     refs_out = given_refs.defined() ? given_refs : stream.output({refs.size(0)}, at::kInt, refs);
@@ -773,6 +778,7 @@ PyObject* pages_fork(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   book.describe(16);      // (the call does not look at tokens)
   TORCH_CHECK_VALUE(parent.dim() == 1, "parent is a contiguous int32 [sequences] on the table's device");
   book.words(parent, parent.size(0), "parent is a contiguous int32 [sequences] on the table's device");
+  book.check_device();
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
@@ -800,6 +806,7 @@ PyObject* pages_reserve(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const Stream stream = a.stream();
   book.describe(page);
   book.words(kv_new, book.b.B, "kv_new is a contiguous int32 [B] on the table's device");
+  book.check_device();
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
@@ -823,6 +830,7 @@ PyObject* pages_trim(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const at::Tensor table_out = a.optional_tensor(), refs_out = a.optional_tensor(), ws = a.optional_tensor();
   const Stream stream = a.stream();
   book.describe(page);
+  book.check_device();
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
@@ -845,6 +853,7 @@ PyObject* pages_compact(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   const at::Tensor ws = a.optional_tensor();
   const Stream stream = a.stream();
   book.describe(16);
+  book.check_device();
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
@@ -873,7 +882,7 @@ PyObject* cache_copy_pages(PyObject*, PyObject* const* argv, Py_ssize_t n) {
                         src.sizes() == dst.sizes(), "src and dst are contiguous int32 of one length");
   for (const at::Tensor* x : std::initializer_list<const at::Tensor*>{&to.k, &src, &dst})
     TORCH_CHECK_VALUE(x->device() == from.k.device(), "tensors of one call must be on one device");
-  TORCH_CHECK_VALUE(from.k.is_cuda(), "tensors of a call must be on a CUDA device");
+  check_here(from.k);
   int rc;
   {
     pybind11::gil_scoped_release no_gil;

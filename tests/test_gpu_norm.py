@@ -287,3 +287,30 @@ def test_captured_and_on_another_stream():
     graph.replay()
     again = sa.norm_rotate(q, k, norm=norm, rotary=rotary)
     assert all(same_bits(a, b) for a, b in zip(outs, again)) and not same_bits(again[0], want[0])
+
+
+def test_more_than_2_to_the_32_bytes():
+    """Rows far apart: a sequence whose heads together pass 2^32 bytes."""
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    N, H = 300000, 60
+    q = torch.empty((1, H, N, 128), dtype=torch.bfloat16, device=DEV)
+    assert q.numel() * 2 > 2 ** 32
+    for h in range(H):
+        q[0, h] = torch.randn((N, 128), generator=gen, device=DEV, dtype=torch.bfloat16)
+    rotary = make_rotary(gen, 128, 128, N, N, 0, True)
+    want = {}
+    for h, n in ((0, 0), (0, N - 1), (H // 2, N // 2), (H - 1, 0), (H - 1, N - 1)):
+        want[h, n] = turned64(normed64(q[0, h, n:n + 1], None, 1e-6), rotary, torch.tensor([n], device=DEV))
+    sa.norm_rotate(q, norm=sa.Norm(), rotary=rotary, q_out=q, check_status=True)
+    for (h, n), (x, size) in want.items():
+        near(q[0, h, n:n + 1], x, size)
+
+
+def test_attention_and_norm_over_odd_strides():
+    """Heads of a larger tensor, every second token, both samples of a batch in one storage."""
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    big = torch.randn((2, 90, 7, 192), generator=gen, device=DEV).bfloat16()
+    x = big[:, ::2, 1:6, 64:].transpose(1, 2)
+    assert x.shape == (2, 5, 45, 128) and x.stride(3) == 1
+    got = sa.norm_rotate(x, norm=sa.Norm(), check_status=True)
+    near(got, normed64(x, None, 1e-6), normed64(x, None, 1e-6).abs())

@@ -461,3 +461,19 @@ def test_captured_with_counts_that_change():
             if a >= 0:
                 held[b] = held[a]
         assert torch.equal(cache.k.view(torch.uint8), held)
+
+
+def test_copy_far_apart():
+    """Pages whose places lie more than 2^32 bytes apart."""
+    pages, H = 36000, 8
+    cache = sa.KVCache(*(torch.zeros((pages, H, 64, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)))
+    assert cache.k[0].numel() * 2 * pages > 2 ** 32
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    far = (0, 1, pages // 2, pages - 2, pages - 1)
+    for p in far:
+        cache.k[p], cache.v[p] = (torch.randn((H, 64, 128), generator=gen, device=DEV).bfloat16() for _ in range(2))
+    want = {b: (cache.k[a].clone(), cache.v[a].clone()) for a, b in ((0, pages - 3), (pages - 1, 2), (pages - 2, 3), (pages // 2, pages - 4))}
+    src, dst = ints([0, pages - 1, pages - 2, pages // 2]), ints(list(want))
+    sa.cache_copy_pages(cache, src, dst, check_status=True)
+    for b, (k, v) in want.items():
+        assert same_bits(cache.k[b], k) and same_bits(cache.v[b], v)
