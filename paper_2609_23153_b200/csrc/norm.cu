@@ -4,9 +4,11 @@
 // weights, which all tokens share.  So a thread stays with 16 bytes of one token's rows: its pairs' phases and (per tensor) its weights are in
 // registers once, and it goes through the heads, four rows asked for at a time.  The sum of squares goes through the D / 8 lanes of a row.
 // A CTA is 256 threads: 16 tokens (32 of 64 channels) by a run of the (sample, head) lines of both tensors.
-// Bandwidth bounds it, and instructions are near: 40 + 40 heads of 75,600 tokens, 128 channels, 3.10 GB in 498 us = 6.2 TB/s, 0.95 of a copy's rate
-// (541 with scalar instructions and the rotation's products rounded one by one, the SMs issuing in 0.78 of the clocks).  Small calls are latency:
-// phases, then rows; 8 heads of two samples of 1201 tokens, 64 channels, 3.5 us.
+// Bandwidth bounds it, and instructions are near: 40 + 40 heads of 75,600 tokens, 128 channels, 3.10 GB in 505 us = 6.1 TB/s, 0.93 of a copy's rate,
+// called for seconds, under the power limit, 530-550; halves, whose other sides go through the lanes, 554 and 580-610.  Five CTAs an SM (48 registers)
+// take 499, but 540-565 for seconds, and halves spill (711).  Halves as eight bytes of either side a thread: 650.  With scalar instructions and the
+// rotation's products rounded one by one 541 us, the SMs issuing in 0.78 of the clocks.  Small calls are latency: phases, then rows; 8 heads
+// of two samples of 1201 tokens, 64 channels, 3.4 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -47,7 +49,7 @@ __device__ __forceinline__ uint32_t angle_row(const RotaryView& r, int n, int m)
 
 // U: rows that a thread asks for at a time
 template <int D, bool INTERLEAVED, bool NORM, int U>
-__global__ void __launch_bounds__(kNormThreads, U == 4 ? 5 : 4)
+__global__ void __launch_bounds__(kNormThreads, 4)
 norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
   constexpr int kLanes = D / 8, kRows = kNormThreads / kLanes, kPairs = INTERLEAVED ? 4 : 8;
   const RotaryView& r = p.rotary;
@@ -142,13 +144,21 @@ norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
         const int l = l0 + u, b = fast_div(l, v.by_H), h = l - b * v.H;
         raw[u] = l < last && there ? *reinterpret_cast<const uint4*>(in + (b * v.in_b + h * v.in_h)) : make_uint4(0u, 0u, 0u, 0u);
       }
+      [[maybe_unused]] float by[U];
+      constexpr bool kTogether = NORM && INTERLEAVED && U == 4;      // (halves have the registers' room taken up by the other sides' phases)
+      if constexpr (kTogether) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) by[u] = sum_of_squares(widen(raw[u]));
+        norm_factors<D>(by, p.norm.eps);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int l = l0 + u, b = fast_div(l, v.by_H), h = l - b * v.H;
         Chunk x = widen(raw[u]);
         if constexpr (NORM) {
           if (p.norm.stride != 0 && l < last) weight = norm_weights(p.norm, v.weight, h, chunk * 8);
-          x = normed<D>(x, weight, p.norm.eps);
+          if constexpr (kTogether) x = scaled(x, weight, by[u]);
+          else x = normed<D>(x, weight, p.norm.eps);
         }
         if (r.rot > 0) {
           const Chunk y = turned(x);
@@ -196,10 +206,9 @@ int launch_norm_rotate(const HeadRows& q, const HeadRows* k, const sparkattn_nor
   if (sms < 1) return SPARKATTN_E_CUDA;
   p.tiles = (s.N + rows - 1) / rows;
   p.by_tiles = make_fast_div(p.tiles);
-  // Four rows at a time where that gives every place on the SMs a CTA (40 heads of 75,600 tokens: 498 us by four, 564 by two, 501 by five on four CTAs
-  // an SM), else two, so that more CTAs share the work (8 heads of 1201 tokens of 64 channels: 3.5 us by two, 4.1 by four).
+  // Four rows at a time where that gives every place on the SMs a CTA (40 + 40 heads of 75,600 tokens: 504 us by four, 564 by two), else two, so that more CTAs share the work (8 heads of 1201 tokens of 64 channels: 3.5 us by two, 4.1 by four).
   const long long lines = (long long)p.x[0].lines + p.x[1].lines;
-  const int u = (lines + 3) / 4 * p.tiles >= 5LL * sms ? 4 : 2;
+  const int u = (lines + 3) / 4 * p.tiles >= 4LL * sms ? 4 : 2;
   // runs of lines: as many as give three CTAs for every place, of one batch of rows at least
   long long groups = std::min<long long>((16LL * sms + p.tiles - 1) / p.tiles, (lines + u - 1) / u);
   p.each = (int)((lines + groups - 1) / groups);

@@ -71,31 +71,59 @@ __device__ __forceinline__ Chunk norm_weights(const NormView& n, const void* wei
   return w;
 }
 // x / sqrt(mean x^2 + eps) * weight of a row whose chunks the D / 8 lanes hold.  Squares, their sum and the products are fp32; the order of the sum
-// is that of the channels and lanes, so a row has the same bits whatever call it goes through.  In pairs of channels: with scalar instructions
-// (and the rotation's products rounded one by one) 40 + 40 heads of 75,600 tokens take 541 us instead of 514.
-template <int D>
-__device__ __forceinline__ Chunk normed(const Chunk& x, const Chunk& weight, float eps) {
-  uint64_t pair[4], sum2 = 0;
+// is that of the channels, then of the lanes, those D / 16 apart first, so a row has the same bits whatever call it goes through.  In pairs of
+// channels: with scalar instructions (and the rotation's products rounded one by one) 40 + 40 heads of 75,600 tokens took 541 us instead of 514.
+__device__ __forceinline__ float sum_of_squares(const Chunk& x) {
+  uint64_t sum2 = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    pair[j] = pack_f32x2(x.x[2 * j], x.x[2 * j + 1]);
-    sum2 = j == 0 ? fmul2(pair[j], pair[j]) : ffma2(pair[j], pair[j], sum2);
+    const uint64_t pair = pack_f32x2(x.x[2 * j], x.x[2 * j + 1]);
+    sum2 = j == 0 ? fmul2(pair, pair) : ffma2(pair, pair, sum2);
   }
   const float2 two = unpack_f32x2(sum2);
-  float sum = two.x + two.y;
-#pragma unroll
-  for (int o = 1; o < D / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return two.x + two.y;
+}
+template <int D>
+__device__ __forceinline__ float norm_factor(float row_sum, float eps) {
   float by;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(by) : "f"(__fmaf_rn(sum, 1.0f / D, eps)));      // (eps is a normal number)
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(by) : "f"(__fmaf_rn(row_sum, 1.0f / D, eps)));      // (eps is a normal number)
+  return by;
+}
+__device__ __forceinline__ Chunk scaled(const Chunk& x, const Chunk& weight, float by) {
   const uint64_t by2 = pack_f32x2(by, by);
   Chunk r;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 y = unpack_f32x2(fmul2(pair[j], fmul2(pack_f32x2(weight.x[2 * j], weight.x[2 * j + 1]), by2)));
+    const float2 y = unpack_f32x2(fmul2(pack_f32x2(x.x[2 * j], x.x[2 * j + 1]), fmul2(pack_f32x2(weight.x[2 * j], weight.x[2 * j + 1]), by2)));
     r.x[2 * j] = y.x;
     r.x[2 * j + 1] = y.y;
   }
   return r;
+}
+template <int D>
+__device__ __forceinline__ Chunk normed(const Chunk& x, const Chunk& weight, float eps) {
+  float sum = sum_of_squares(x);
+#pragma unroll
+  for (int o = D / 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return scaled(x, weight, norm_factor<D>(sum, eps));
+}
+// The sums of four rows' chunks into the rows' factors: the lanes share the rows out, a quarter of them a row, and pass the factors round.  (Ten
+// instructions a row become six.)
+template <int D>
+__device__ __forceinline__ void norm_factors(float (&x)[4], float eps) {
+  constexpr int L = D / 8;
+  const int lane = threadIdx.x & 31;
+  const bool high = lane & (L / 2), odd = lane & (L / 4);
+  float a = high ? x[2] : x[0], b = high ? x[3] : x[1];
+  a += __shfl_xor_sync(0xffffffffu, high ? x[0] : x[2], L / 2);
+  b += __shfl_xor_sync(0xffffffffu, high ? x[1] : x[3], L / 2);
+  float mine = odd ? b : a;
+  mine += __shfl_xor_sync(0xffffffffu, odd ? a : b, L / 4);
+#pragma unroll
+  for (int o = L / 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  mine = norm_factor<D>(mine, eps);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) x[u] = __shfl_sync(0xffffffffu, mine, (lane & ~(L - 1)) + (u & 2 ? L / 2 : 0) + (u & 1 ? L / 4 : 0));
 }
 // The rotation behind a norm: a product rounded, the other one and the sum in one step.  Interleaved: the chunk's four pairs by c, s.
 __device__ __forceinline__ Chunk turn_pairs_fused(const float (&c)[4], const float (&s)[4], const Chunk& x) {
