@@ -494,22 +494,37 @@ combine_rows_kernel(const __grid_constant__ CacheFwdParams p) {
     float top = -INFINITY;
 #pragma unroll 4
     for (int i = 0; i < parts; ++i) top = fmaxf(top, p.part_ml[((int64_t)slot_of(i) * R + r) * 2]);
-    float sum = 0.0f, acc[kGroups][4] = {};
+    // (items of fewer than 16 rows: every n-th part by itself, then the sums of these, the order that calls of many sequences with few rows have had)
+    const int split = rows >= 16 ? 1 : 16 / rows;
+    auto add_up = [&](int k, float& sum, float (&acc)[kGroups][4]) {
 #pragma unroll 2
-    for (int i = 0; i < parts; ++i) {
-      const int slot = slot_of(i);
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((int64_t)slot * R + r) * 2);
-      float4 v[kGroups];
+      for (int i = k; i < parts; i += split) {
+        const int slot = slot_of(i);
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((int64_t)slot * R + r) * 2);
+        float4 v[kGroups];
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) v[g] = *reinterpret_cast<const float4*>(p.part_o + (((int64_t)slot * (D / 4) + warp + g * kWarps) * R + r) * 4);
-      const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
-      sum = fmaf(ml.y, f, sum);
+        for (int g = 0; g < kGroups; ++g) v[g] = *reinterpret_cast<const float4*>(p.part_o + (((int64_t)slot * (D / 4) + warp + g * kWarps) * R + r) * 4);
+        const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
+        sum = fmaf(ml.y, f, sum);
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        const float x[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
+        for (int g = 0; g < kGroups; ++g) {
+          const float x[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[g][j] = ml.x == -INFINITY ? acc[g][j] : fmaf(x[j], f, acc[g][j]);      // (a part without keys has left no output)
+          for (int j = 0; j < 4; ++j) acc[g][j] = ml.x == -INFINITY ? acc[g][j] : fmaf(x[j], f, acc[g][j]);      // (a part without keys has left no output)
+        }
       }
+    };
+    float sum = 0.0f, acc[kGroups][4] = {};
+    add_up(0, sum, acc);
+#pragma unroll 1
+    for (int k = 1; k < split; ++k) {
+      float sum_k = 0.0f, acc_k[kGroups][4] = {};
+      add_up(k, sum_k, acc_k);
+      sum += sum_k;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[g][j] += acc_k[g][j];
     }
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
