@@ -8,7 +8,7 @@
 // called for seconds, under the power limit, 530-550; halves, whose other sides go through the lanes, 554 and 580-610.  Five CTAs an SM (48 registers)
 // take 499, but 540-565 for seconds, and halves spill (711).  Halves as eight bytes of either side a thread: 650.  With scalar instructions and the
 // rotation's products rounded one by one 541 us, the SMs issuing in 0.78 of the clocks.  Small calls are latency: phases, then rows; 8 heads
-// of two samples of 1201 tokens, 64 channels, 3.4 us.
+// of two samples of 1201 tokens, 64 channels, 3.5 us.
 #include <algorithm>
 #include <type_traits>
 
