@@ -172,15 +172,32 @@ norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
   if (group == 0 && any_bad) report_early(p.status, SPARKATTN_E_BAD_INDEX, bad);
   if (blockIdx.x == 0 && __syncthreads_or(code_there)) {
     // the word held a code, which may have been one of this call's: see take_header
+    // (the positions of the axes that a pair turns by, each once, while the grid's other CTAs are at work: pair by pair 75,600 tokens took 20 ms)
     any_bad = false;
-    const long long all = (long long)p.N * (r.rot / 2);
-#pragma unroll 1
-    for (long long i = threadIdx.x; i < all; i += kNormThreads) {
-      const int row = (int)(i / (r.rot / 2));
-      const uint32_t e = angle_row(r, row, (int)(i - (long long)row * (r.rot / 2)));
-      if (e >= (uint32_t)r.rows) {
+    uint32_t used = r.axis == nullptr ? 1u : 0u;
+    for (int m = threadIdx.x & 31; r.axis != nullptr && m < r.rot / 2; m += 32) {
+      if ((uint32_t)r.axis[m] < (uint32_t)r.axes) {
+        used |= 1u << r.axis[m];
+      } else {
         any_bad = true;
-        bad = (int)e;
+        bad = -1;
+      }
+    }
+    used = __reduce_or_sync(0xffffffffu, used);
+    if (r.positions == nullptr) {
+      if (used != 0 && p.N > r.rows) {
+        any_bad = true;
+        bad = r.rows;
+      }
+    } else {
+      const int64_t all = (int64_t)p.N * r.axes;
+#pragma unroll 8
+      for (int64_t i = threadIdx.x; i < all; i += kNormThreads) {
+        const int e = r.positions[i];
+        if ((uint32_t)e >= (uint32_t)r.rows && (used >> (uint32_t)(i % r.axes) & 1u)) {
+          any_bad = true;
+          bad = e;
+        }
       }
     }
     if (any_bad) report_early(p.status, SPARKATTN_E_BAD_INDEX, bad);

@@ -314,3 +314,25 @@ def test_attention_and_norm_over_odd_strides():
     assert x.shape == (2, 5, 45, 128) and x.stride(3) == 1
     got = sa.norm_rotate(x, norm=sa.Norm(), check_status=True)
     near(got, normed64(x, None, 1e-6), normed64(x, None, 1e-6).abs())
+
+
+@pytest.mark.parametrize("word", [0, -7])
+def test_positions_of_many_tokens(word):
+    """What stands in the positions of an axis that no pair turns by is not looked at, and one number among many is found whatever the
+    workspace held."""
+    gen = torch.Generator(device=DEV).manual_seed(14)
+    N = 70001
+    x = torch.randn((1, 1, N, 64), generator=gen, device=DEV).bfloat16()
+    ws = torch.zeros(64, dtype=torch.int32, device=DEV)
+    rotary = make_rotary(gen, 64, 64, 50, N, 3, True)
+    positions, axis = rotary.positions.clone(), torch.where(rotary.axis == 1, 2, rotary.axis).int()
+    positions[:, 1] = 1000
+    want = sa.norm_rotate(x, norm=sa.Norm(), rotary=rotary._replace(axis=axis))
+    for token, ax, code in ((0, 1, sa.OK), (N - 1, 2, sa.E_BAD_INDEX), (12345, 0, sa.E_BAD_INDEX)):
+        bad = positions.clone()
+        bad[token, ax] = -5
+        ws[0] = word
+        got = sa.norm_rotate(x, norm=sa.Norm(), rotary=rotary._replace(positions=bad, axis=axis), workspace=ws.view(torch.uint8))
+        assert sa.read_status(ws.view(torch.uint8)) == code
+        rest = torch.arange(N, device=DEV) != token
+        assert same_bits(got[:, :, rest], want[:, :, rest])
