@@ -589,7 +589,7 @@ typedef struct {
   uint32_t struct_size; /* sizeof(sparkattn_book_t)                                           */
   uint32_t version;     /* SPARKATTN_VERSION                                                  */
   int32_t B;            /* sequences, at most 4096                                            */
-  int32_t max_pages;    /* columns of page_table; B * max_pages < 2^31                        */
+  int32_t max_pages;    /* columns of page_table; B * max_pages at most 2^31 - 256            */
   int32_t pages;        /* pages in the pool, at most 2^30                                    */
   int32_t page;         /* tokens per page: 16, 32, 64 or 128                                 */
   const int32_t* page_table; /* [B, max_pages]                                                */
@@ -618,11 +618,12 @@ int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, co
  * free pages (those that have one keep it).  Where the token kv_len[b] falls into a page that others hold as well, it is replaced
  * by a free one, and the pair (src, dst) says what has to be copied; of the sequences that go on in one page the first keeps it if nobody
  * else holds it.  All or nothing: where the pool has fewer free pages than that, the book stays as it was, and the status is
- * SPARKATTN_E_OUT_OF_PAGES, its detail the number of pages that are missing.  Nothing may be appended then.
+ * SPARKATTN_E_OUT_OF_PAGES, its detail the number of pages that are missing, whatever else was found.  Nothing may be appended then.
  * kv_len, kv_new : in,  int32 [B], 0 <= kv_len <= kv_new <= max_pages * page
  * src, dst   : out, int32 [B]: pages to copy for sequence b, or -1 and -1
  * table_out, refs_out : out, may be page_table and refs
- * Device errors (SPARKATTN_E_BAD_INDEX): lengths that are not so (the sequence is left out), a partly filled page that is none.
+ * Device errors (SPARKATTN_E_BAD_INDEX): lengths that are not so (the sequence is left out), a partly filled page that is none or
+ * that nobody holds.
  */
 int sparkattn_pages_reserve(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out,
                             int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream);

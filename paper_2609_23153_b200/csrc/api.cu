@@ -683,7 +683,7 @@ namespace {
 int check_book(const sparkattn_book_t* b) {
   if (b == nullptr || b->struct_size != sizeof(sparkattn_book_t) || b->version != SPARKATTN_VERSION) return SPARKATTN_E_INVALID_ARG;
   if (b->B < 1 || b->max_pages < 1 || b->pages < 1) return SPARKATTN_E_INVALID_ARG;
-  if (b->B > kCacheMaxSequences || (long long)b->B * b->max_pages > 0x7fffffffLL || b->pages > 1 << 30) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  if (b->B > kCacheMaxSequences || (long long)b->B * b->max_pages > 0x7fffff00LL || b->pages > 1 << 30) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   if (b->page != 16 && b->page != 32 && b->page != 64 && b->page != 128) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   return SPARKATTN_OK;
 }
@@ -711,7 +711,7 @@ int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, co
   const int rc = check_book_call(book, table_out, refs_out, workspace, workspace_bytes);
   if (rc != SPARKATTN_OK) return rc;
   if (!kv_len || !parent || !kv_len_out || B_out < 1 || table_out == book->page_table || kv_len_out == kv_len) return SPARKATTN_E_INVALID_ARG;
-  if (B_out > kCacheMaxSequences || (long long)B_out * book->max_pages > 0x7fffffffLL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
+  if (B_out > kCacheMaxSequences || (long long)B_out * book->max_pages > 0x7fffff00LL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   return launch_pages_fork(*book, kv_len, parent, B_out, table_out, kv_len_out, refs_out, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 

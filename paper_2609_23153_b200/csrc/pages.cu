@@ -8,10 +8,12 @@
 //   A fork changes counts for whole rows, by integer additions, in any order: a launch of its own, since sixteen SMs issue their additions to
 //   scattered words a few clocks apart (256 rows of 500 entries: 11.2 us with one cluster, 4.6 with two launches).
 // Free pages are handed out in ascending order: the same call gives the same book.
-// Measured: a fork of 256 sequences of up to 32,000 tokens, pages of 64, 4.6 us; pages for a token of each of 128 sequences 7.3 us, in place 6.0, and the 90
+// Measured: a fork of 256 sequences of up to 32,000 tokens, pages of 64, 4.6 us; pages for a token of each of 128 sequences 7.0 us, in place 5.8, for prompts of
+// 4000 tokens of each of 32, pages of 16, 9.7, for one of 65,536, whose 4096 entries one warp writes, 35; the 90
 // copies of pages of 16 tokens that they share 2.7; a trim of 32 sequences 4.7, with nothing to give back 3.1; compact, 1560 pages, 6.4.  Latency
 // bounds all of them.  The copy of 368 pages of 196 KB, K and V, 289 MB read and written: 49 us = 5.9 TB/s, 0.89 of a copy's rate.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
 #include "tmap.h"
@@ -311,6 +313,7 @@ struct ReserveParams {
   int ranks, slots;              // slots of the hash table: a power of two, twice the sequences or more
   int32_t* status;
 };
+constexpr int kOwnColumns = 32;      // a sequence that asks for more columns is looked through by the whole CTA
 // What a sequence asks for: pages for the columns [first, last) that have none, and another page in place of a partly filled one, `tail`, that
 // others hold as well.
 struct Asks {
@@ -361,22 +364,33 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     }
     return (int)(at & (p.slots - 1));
   };
-  // who writes to pages that several hold
+  // who writes to pages that several hold, and the columns that have no page
+  bool long_one = false;
   for (int b = threadIdx.x; b < v.B; b += kBookThreads) {
     const Asks a = asks_of(p, b);
     int shared = -1;
     if (!a.fine) found(s, SPARKATTN_E_BAD_INDEX, b);
+    const int32_t* row = v.table + (int64_t)b * v.max_pages;
+    const int e = a.partly() ? row[a.tail] : 0;
+    int missing = 0;
+    if (a.last - a.first <= kOwnColumns) {
+#pragma unroll 8
+      for (int i = a.first; i < a.last; ++i) missing += row[i] == -1 ? 1 : 0;
+    } else {
+      long_one = true;
+    }
     if (a.partly()) {
-      const int e = v.table[(int64_t)b * v.max_pages + a.tail];
-      if ((uint32_t)e >= (uint32_t)v.pages) {
+      const int holders = (uint32_t)e < (uint32_t)v.pages ? v.refs[e] : 0;
+      if (holders < 1) {
         found(s, SPARKATTN_E_BAD_INDEX, e);
-      } else if (v.refs[e] > 1) {
+      } else if (holders > 1) {
         shared = e;
         const int at = slot_of(e, true);
         atomicAdd(h_writers + at, 1);
         atomicMin(h_first + at, b);
       }
     }
+    prefix[b] = missing;
     s_tail[b] = a.tail;
     s_first[b] = a.first;
     s_last[b] = a.last;
@@ -385,22 +399,38 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   const PoolRun run = run_of_warp(v.pages, p.ranks, rank);
   const int free_here = count_run(v, run, [](int r) { return r == 0 ? 1 : 0; });
   if (lane == 0) s.count[warp] = free_here;
-  __syncthreads();
+  if (__syncthreads_or(long_one)) {
+    // 256 columns at a time, those of a sequence dealt out to the warps
+    for (int b0 = 0; b0 < v.B; b0 += 32) {
+      const int own = b0 + lane, columns = own < v.B ? s_last[own] - s_first[own] : 0;
+      const int chunks = columns > kOwnColumns ? (columns + kCopyColumns - 1) / kCopyColumns : 0;
+      for (uint32_t left = __ballot_sync(0xffffffffu, ((warp - own) & (kBookWarps - 1)) < chunks); left != 0; left &= left - 1) {
+        const int b = b0 + __ffs(left) - 1, last = s_last[b];
+        const int32_t* row = v.table + (int64_t)b * v.max_pages;
+        int n = 0;
+        for (long long i0 = s_first[b] + (long long)((warp - b) & (kBookWarps - 1)) * kCopyColumns; i0 < last; i0 += kBookWarps * kCopyColumns) {
+#pragma unroll
+          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && row[i0 + 32 * u + lane] == -1 ? 1 : 0;
+        }
+        n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+        if (lane == 0) atomicAdd(&prefix[b], n);
+      }
+    }
+    __syncthreads();
+  }
   int carry = 0;
   for (int base = 0; base < v.B; base += kBookThreads) {
     const int b = base + threadIdx.x;
     int mine = 0;
     if (b < v.B) {
+      mine = prefix[b];
       // the first of the sequences that write to a page keeps it, if nobody else holds it
       const int page = s_copy[b];
       if (page >= 0) {
         const int at = slot_of(page, false);
         if (h_writers[at] == v.refs[page] && h_first[at] == b) s_copy[b] = -1;
-        else mine = 1;
+        else ++mine;
       }
-      const int32_t* row = v.table + (int64_t)b * v.max_pages;
-#pragma unroll 4
-      for (int i = s_first[b]; i < s_last[b]; ++i) mine += row[i] == -1 ? 1 : 0;
     }
     int x = mine;
 #pragma unroll
@@ -421,7 +451,10 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   book_barrier();
   const int2 free = in_front(s, rank, p.ranks);
   const bool enough = carry <= free.y;
-  if (!enough && rank == 0 && threadIdx.x == 0) found(s, SPARKATTN_E_OUT_OF_PAGES, carry - free.y);
+  if (!enough && rank == 0 && threadIdx.x == 0) {      // (goes before what else has been found)
+    s.bad[0] = SPARKATTN_E_OUT_OF_PAGES;
+    s.bad[1] = carry - free.y;
+  }
   if (enough) {
     int k = free.x;
     for (int p0 = run.first; p0 < run.last && k < carry; p0 += 32 * 8) {
@@ -453,12 +486,25 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
       p.dst[b] = to;
       if (tail < first) out[tail] = from >= 0 ? to : row[tail];
     }
-    for (int i0 = first; i0 < last; i0 += 32) {
-      const int i = i0 + lane;
-      const int e = i < last ? row[i] : 0;
-      const uint32_t missing = __ballot_sync(0xffffffffu, i < last && e == -1);
-      if (i < last) out[i] = e == -1 && enough ? p.list[at + __popc(missing & ((1u << lane) - 1u))] : e;
-      at += __popc(missing);
+    auto fill = [&](int i0, auto many) {
+      constexpr int U = decltype(many)::value;
+      int e[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) e[u] = i0 + 32 * u + lane < last ? row[i0 + 32 * u + lane] : 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t missing = __ballot_sync(0xffffffffu, e[u] == -1);
+        if (e[u] == -1 && enough) e[u] = p.list[at + __popc(missing & ((1u << lane) - 1u))];
+        at += __popc(missing);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i0 + 32 * u + lane < last) out[i0 + 32 * u + lane] = e[u];
+    };
+    if (last - first <= 32) {
+      fill(first, std::integral_constant<int, 1>{});
+    } else {
+      for (int i0 = first; i0 < last; i0 += kCopyColumns) fill(i0, std::integral_constant<int, kCopyColumns / 32>{});
     }
   }
   book_end(s, rank, p.ranks, p.status);
@@ -802,7 +848,7 @@ int launch_copy_pages(const sparkattn_cache_t& from, const PagePools& in, const 
   p.src = src; p.dst = dst; p.n = n;
   p.split = (p.pieces + kCopyPieces - 1) / kCopyPieces;
   p.units = 2LL * p.split * n;
-  p.checkers = (to.pages + kCheckPages - 1) / kCheckPages;
+  p.checkers = (int)(((long long)to.pages + kCheckPages - 1) / kCheckPages);
   p.status = static_cast<int32_t*>(workspace);
   const int sms = current_sm_count();
   if (sms < 1) return SPARKATTN_E_CUDA;

@@ -196,6 +196,59 @@ def test_reserve(size, seed):
         assert same(again[0], after.table) and same(again[1], after.refs) and same(again[2], src)
 
 
+@pytest.mark.parametrize("B,most", [(1, 9000), (3, 5000), (40, 700), (1000, 9)])
+def test_reserve_many_pages_at_once(B, most):
+    """Prompts: columns by the thousand, some of which have a page already."""
+    rng = random.Random(B)
+    page, columns = 16, 9003
+    pages = B * most + 50
+    order = list(range(pages))
+    rng.shuffle(order)
+    table, refs, length, new = [], [0] * pages, [], []
+    for b in range(B):
+        had, wants = rng.randint(0, 20), most if b % 3 == 0 else rng.randint(0, most)
+        n = min(had, wants)
+        row = [order.pop() for _ in range(n)] + [-1] * (columns - n)
+        for i in range(n, wants):
+            if rng.random() < 0.1:
+                row[i] = order.pop()
+        for e in row:
+            if e >= 0:
+                refs[e] += 1
+        table.append(row)
+        length.append(max(0, n * page - rng.randint(0, 15)) if n else 0)
+        new.append(max(length[-1], wants * page - rng.randint(0, 15)))
+    for spare in (0, 1):
+        book = Book(table, refs, length, page)
+        if spare:                  # one page too few
+            free = [p for p, r in enumerate(refs) if r == 0]
+            needed = sum(row[i] == -1 for row, n in zip(table, new) for i in range(-(-n // page)))
+            for p in free[:len(free) - needed + 1]:
+                book.refs[p] = 1
+        want = book.copy()
+        src, dst, missing = want.reserve(new)
+        assert missing == spare
+        ws = workspace(pages)
+        got = sa.pages_reserve(*on_device(book), ints(new), page, workspace=ws)
+        assert sa.read_status(ws) == (sa.E_OUT_OF_PAGES if spare else sa.OK) and int(ws.view(torch.int32)[1]) == missing
+        assert same(got[0], want.table) and same(got[1], want.refs) and same(got[2], src) and same(got[3], dst)
+
+
+def test_too_few_pages_goes_before_other_reports():
+    book = Book([[0, -1, -1], [1, -1, -1], [2, -1, -1]], [1, 1, 1, 0], [16, 16, 10], 16)
+    ws = workspace(4)
+    got = sa.pages_reserve(*on_device(book), ints([48, 15, 10]), 16, workspace=ws)           # two pages; fewer tokens than there are
+    assert sa.read_status(ws) == sa.E_OUT_OF_PAGES and int(ws.view(torch.int32)[1]) == 1
+    assert same(got[0], book.table) and same(got[1], book.refs)
+
+
+def test_a_partly_filled_page_that_nobody_holds_is_reported():
+    book = Book([[0, -1], [1, -1]], [1, 0, 0], [10, 10], 16)
+    ws = workspace(3)
+    sa.pages_reserve(*on_device(book), ints([12, 12]), 16, workspace=ws)
+    assert sa.read_status(ws) == sa.E_BAD_INDEX
+
+
 def test_reserve_to_the_last_page():
     for spare in (0, 1, 2, 3, 4, 5):
         book = Book([[0, 1, -1, -1], [0, 1, -1, -1], [5, -1, -1, -1]], [2, 2, 0, 0, 0, 1] + [0] * spare, [24, 24, 16], 16)
