@@ -113,6 +113,27 @@ __device__ __noinline__ void mark_tile(const CacheFwdParams& p, const Marks<D, 8
   using S = DecodeShape<D, FP8, NT>;
   constexpr int kVWords = D / 8 * S::kElt / 4;
   const int g8 = (threadIdx.x & 31) >> 2, t4 = threadIdx.x & 3;
+  // mostly there is nothing to mark, which whole chunks tell in a tenth of the time: 9 sequences, four tokens each, window 3722, 4 heads, E4M3,
+  // 23.8 us without this look and 19.0 with it, with a first token to be seen, whose tile is another such, 34.0 and 19.7
+  const uint32_t s_v = smem_u32(tile);
+  bool odd = false;
+#pragma unroll
+  for (int u = 0; u < S::kPerWarp; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = tile_row0 + u * kGroupKeys + 4 * t4 + i;
+      if constexpr (kVWords == 2) {
+        const uint2 w = lds8(s_v + chunk_offset<S::kRowBytes, S::kTileKeys>(row, g8 >> 1) + (g8 & 1) * 8);
+        odd |= word_not_finite<FP8>(w.x) || word_not_finite<FP8>(w.y);
+      } else {
+#pragma unroll
+        for (int c = 0; c < kVWords / 4; ++c) {
+          const uint4 w = lds16(s_v + chunk_offset<S::kRowBytes, S::kTileKeys>(row, g8 * (kVWords / 4) + c));
+          odd |= word_not_finite<FP8>(w.x) || word_not_finite<FP8>(w.y) || word_not_finite<FP8>(w.z) || word_not_finite<FP8>(w.w);
+        }
+      }
+    }
+  if (!__any_sync(0xffffffffu, odd)) return;
 #pragma unroll 1
   for (int i = 0; i < S::kPerWarp * 4 * kVWords; ++i) {
     const int u = i / kVWords >> 2, in = u * kGroupKeys + 4 * t4 + (i / kVWords & 3), key = key0 + in, channel = g8 * (D / 8) + i % kVWords * (4 / S::kElt);
