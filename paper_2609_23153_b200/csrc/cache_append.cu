@@ -11,7 +11,7 @@
 // 8 sequences, 32 query and 8 key heads, bf16 pages of 64, half the channels rotated: 425 MB in 74 us = 5.8 TB/s, 0.89 of it.  4680
 // tokens of 12 heads (three frames of 1560), E4M3 pages of 128, positions of three axes: 74 MB in 19 us = 3.9 TB/s; the
 // SMs issue an instruction in six of ten clocks, rotating and encoding, and the one wave has its beginning and end to itself.  One token for each of 128 sequences
-// 5.2 us, for one 2.8: latency.  With the norm of keys and queries (NORM) the frames take 24.3 us, a line of a page 3.3 of them, and the tokens 6.2.
+// 5.0 us, for one 2.7: latency.  With the norm of keys and queries (NORM) the frames take 24.3 us, a line of a page 3.3 of them, and the tokens 6.05.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -141,6 +141,9 @@ struct UnitShape {
   // rows on their way, then cosines and sines
   static constexpr int kRowBytes = kThreads * C * 16;
   static size_t smem(int rot) { return kRowBytes + (size_t)(kThreads / U) * ROWS * rot * sizeof(float); }
+  // CTAs per SM: 64 registers a thread, or 80 where norm and codes of a page's 128 channels need them (8 prompts of up to 4706 tokens, 48 + 2 x 4 heads, pages of
+  // 32 and 64: 114 and 116 us by three, 127 and 126 by four; without the norm 108 and 102)
+  static constexpr int per_sm(bool fp8, bool norm) { return fp8 && norm && D == 128 && U > 32 && kThreads == 256 ? 3 : 1024 / kThreads; }
 };
 
 // Lines first, first + step, ... of a unit: the threads hold its up to ROWS new rows of one of them, 16 bytes of a row each at a time.
@@ -292,7 +295,7 @@ __device__ __forceinline__ void append_lines(const AppendParams& p, const Part& 
 }
 
 template <int D, bool FP8, int ROWS, bool NORM>
-__global__ void __launch_bounds__(UnitShape<D, ROWS>::kThreads, 1024 / UnitShape<D, ROWS>::kThreads)
+__global__ void __launch_bounds__(UnitShape<D, ROWS>::kThreads, UnitShape<D, ROWS>::per_sm(FP8, NORM))
 cache_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int kThreads = UnitShape<D, ROWS>::kThreads;
   __shared__ uint32_t s_max[2 * kThreads / 32];
@@ -329,7 +332,8 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
     return;
   }
   constexpr int U = UnitShape<D, ROWS>::U;
-  const int group = threadIdx.x / U;
+  // (the same in all lanes, which the compiler has to see: with the unit's numbers in vector registers pages of 32 and less spilled, 178 us instead of 127)
+  const int group = __shfl_sync(0xffffffffu, (int)threadIdx.x / U, 0);
   const int unit = (int)(blockIdx.x - 1) * (kThreads / U) + group;
   if (unit >= p.units) return;
   const int bj = fast_div(unit, p.by_groups), first = unit - bj * p.groups;
@@ -352,7 +356,7 @@ static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream)
     AppendParams p = given;
     p.lines = 2 * p.Hk + (p.q.data ? p.H : 0);
     // One wave of CTAs where that leaves a unit at most sixteen lines, else units of eight
-    const long long parts = (long long)p.batch.B * p.pages_each, slots = (long long)per * (1024 / kThreads) * current_sm_count();
+    const long long parts = (long long)p.batch.B * p.pages_each, slots = (long long)per * decltype(shape)::per_sm(FP8, NORM) * current_sm_count();
     // (a sequence reaches one page less than it could if its first new token begins one or its pieces are shorter: most do.  Three frames of 1560 tokens
     // by eight units a page instead of seven: 20.6 -> 19.1 us.)
     const long long likely = parts - (p.pages_each > 1 ? p.batch.B : 0);
