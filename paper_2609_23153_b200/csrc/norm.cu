@@ -4,8 +4,8 @@
 // weights, which all tokens share.  So a thread stays with 16 bytes of one token's rows: its pairs' phases and (per tensor) its weights are in
 // registers once, and it goes through the heads, four rows asked for at a time.  The sum of squares goes through the D / 8 lanes of a row.
 // A CTA is 256 threads: 16 tokens (32 of 64 channels) by a run of the (sample, head) lines of both tensors.
-// Bandwidth bounds it, and instructions are near: 40 + 40 heads of 75,600 tokens, 128 channels, 3.10 GB in 505 us = 6.1 TB/s, 0.93 of a copy's rate,
-// called for seconds, under the power limit, 530-550; halves, whose other sides go through the lanes, 554 and 580-610.  Five CTAs an SM (48 registers)
+// Bandwidth bounds it, and instructions are near: 40 + 40 heads of 75,600 tokens, 128 channels, 3.10 GB in 497 us = 6.2 TB/s, 0.95 of a copy's rate,
+// called for seconds, under the power limit, 530-550; halves, whose other sides go through the lanes, 585-600 and 615-630.  Five CTAs an SM (48 registers)
 // take 499, but 540-565 for seconds, and halves spill (711).  Halves as eight bytes of either side a thread: 650.  With scalar instructions and the
 // rotation's products rounded one by one 541 us, the SMs issuing in 0.78 of the clocks.  Small calls are latency: phases, then rows; 8 heads
 // of two samples of 1201 tokens, 64 channels, 3.5 us.
@@ -172,31 +172,17 @@ norm_rotate_kernel(const __grid_constant__ NormRotateParams p) {
   if (group == 0 && any_bad) report_early(p.status, SPARKATTN_E_BAD_INDEX, bad);
   if (blockIdx.x == 0 && __syncthreads_or(code_there)) {
     // the word held a code, which may have been one of this call's: see take_header
-    // (the positions of the axes that a pair turns by, each once, while the grid's other CTAs are at work: pair by pair 75,600 tokens took 20 ms)
     any_bad = false;
-    uint32_t used = r.axis == nullptr ? 1u : 0u;
-    for (int m = threadIdx.x & 31; r.axis != nullptr && m < r.rot / 2; m += 32) {
-      if ((uint32_t)r.axis[m] < (uint32_t)r.axes) {
-        used |= 1u << r.axis[m];
-      } else {
-        any_bad = true;
-        bad = -1;
-      }
-    }
-    used = __reduce_or_sync(0xffffffffu, used);
-    if (r.positions == nullptr) {
-      if (used != 0 && p.N > r.rows) {
-        any_bad = true;
-        bad = r.rows;
-      }
-    } else {
-      const int64_t all = (int64_t)p.N * r.axes;
-#pragma unroll 8
-      for (int64_t i = threadIdx.x; i < all; i += kNormThreads) {
-        const int e = r.positions[i];
-        if ((uint32_t)e >= (uint32_t)r.rows && (used >> (uint32_t)(i % r.axes) & 1u)) {
+    // (pair by pair only where neighbouring pairs turn by different axes: all pairs of 75,600 tokens took 20 ms)
+#pragma unroll 1
+    for (int m = 0; m < r.rot / 2; ++m) {
+      if (m > 0 && (r.axis == nullptr || r.axis[m] == r.axis[m - 1])) continue;
+#pragma unroll 4
+      for (int row = threadIdx.x; row < p.N; row += kNormThreads) {
+        const uint32_t e = angle_row(r, row, m);
+        if (e >= (uint32_t)r.rows) {
           any_bad = true;
-          bad = e;
+          bad = (int)e;
         }
       }
     }
@@ -226,9 +212,9 @@ int launch_norm_rotate(const HeadRows& q, const HeadRows* k, const sparkattn_nor
   // Four rows at a time where that gives every place on the SMs a CTA (40 + 40 heads of 75,600 tokens: 504 us by four, 564 by two), else two, so that more CTAs share the work (8 heads of 1201 tokens of 64 channels: 3.5 us by two, 4.1 by four).
   const long long lines = (long long)p.x[0].lines + p.x[1].lines;
   const int u = (lines + 3) / 4 * p.tiles >= 4LL * sms ? 4 : 2;
-  // runs of lines: as many as give three CTAs for every place, of one batch of rows at least
-  long long groups = std::min<long long>((16LL * sms + p.tiles - 1) / p.tiles, (lines + u - 1) / u);
-  p.each = (int)((lines + groups - 1) / groups);
+  // runs of lines: three CTAs for every place, whole batches of rows (56 + 8 heads of four samples of 715 tokens by four lines a CTA 22.5 us, by five 29.5)
+  long long groups = std::min<long long>((12LL * sms + p.tiles - 1) / p.tiles, (lines + u - 1) / u);
+  p.each = (int)((lines + groups - 1) / groups + u - 1) / u * u;
   groups = (lines + p.each - 1) / p.each;
   if (groups * p.tiles > 0x7fffff00LL) return SPARKATTN_E_UNSUPPORTED_SHAPE;
   auto go = [&](auto d, auto inter, auto normed) {
