@@ -336,3 +336,26 @@ def test_positions_of_many_tokens(word):
         assert sa.read_status(ws.view(torch.uint8)) == code
         rest = torch.arange(N, device=DEV) != token
         assert same_bits(got[:, :, rest], want[:, :, rest])
+
+
+@pytest.mark.parametrize("shift", range(4))
+@pytest.mark.parametrize("T", [1, 3, 700, 4999])
+def test_positions_that_begin_anywhere(shift, T):
+    """Positions whose first number lies 4, 8 or 12 bytes behind a 16-byte boundary: a bad one is reported wherever it stands."""
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    cache = sa.alloc_cache(-(-T // 64), 1, 64, 64, fp8=True, device=DEV)
+    k = torch.randn((T, 1, 64), generator=gen, device=DEV).bfloat16()
+    table = torch.arange(cache.k.shape[0], dtype=torch.int32, device=DEV)[None]
+    kv_len = torch.tensor([T], dtype=torch.int32, device=DEV)
+    rotary = make_rotary(gen, 64, 64, 50, T, 3, True)
+    whole = torch.full((shift + 3 * T + 8,), -1, dtype=torch.int32, device=DEV)           # (what lies around them is not looked at)
+    positions = whole[shift:shift + 3 * T].view(T, 3)
+    positions.copy_(rotary.positions)
+    ws = torch.empty(256, dtype=torch.uint8, device=DEV)
+    sa.cache_append(cache, k, k, table, kv_len, rotary=rotary._replace(positions=positions), workspace=ws)
+    assert sa.read_status(ws) == sa.OK
+    for at in sorted({0, 1, 3 * T // 2, 3 * T - 2, 3 * T - 1}):
+        positions.copy_(rotary.positions)
+        positions.view(-1)[at] = 50
+        sa.cache_append(cache, k, k, table, kv_len, rotary=rotary._replace(positions=positions), workspace=ws)
+        assert sa.read_status(ws) == sa.E_BAD_INDEX
