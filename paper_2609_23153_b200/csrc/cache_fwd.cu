@@ -4,7 +4,7 @@
 // A (sequence, key head) with G query heads and n new tokens has G n query rows over the same keys.  The work is reading
 // the keys and values once: 2 d bytes (E4M3) a token against 4 d G n flops, far below the tensor cores' rate, so what
 // counts is that every SM always has copies in flight, and that long and short sequences come out even.
-//   Work split: an item is a (sequence, key head); a tile is 128 of its keys (bf16 with 128 channels: 64).  Two CTAs per SM.  Either
+//   Work split: an item is a (sequence, key head), or up to 16 rows of one (row_tile_cluster); a tile is 128 of its keys (bf16 with 128 channels: 64).  Two CTAs per SM.  Either
 //     each item belongs to a thread-block cluster, whose CTAs take equal runs of its tiles and add up maximum, sum and
 //     unnormalised output through distributed shared memory; or the tiles of all items stand in one line (cache_line.cuh), which is
 //     cut into equal stretches, one per CTA: an item that lies in one stretch is finished there, one that several share leaves partial
@@ -145,7 +145,7 @@ __device__ __noinline__ void mark_tile(const CacheFwdParams& p, const Marks<D, 8
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the tile is released to the next copy
 }
 
-// CLUSTER: an item (it has one row tile) belongs to a cluster of CTAs, each takes an equal run of its key tiles, and the CTAs' results
+// CLUSTER: an item (a row tile; SINK only, a key head may have several) belongs to a cluster of CTAs, each takes an equal run of its key tiles, and the CTAs' results
 // are added up through distributed shared memory.  Otherwise the line, see cache_line.cuh; cluster_of has the rule.
 template <int D, bool FP8, int NT, bool CLUSTER, bool SINK>
 __global__ void __launch_bounds__(kDecodeThreads, kDecodePerSM)
@@ -189,8 +189,13 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       if (rank == 0) check_call<SINK>(p, s_bad);
       return;
     }
-    const int b = fast_div(cluster - 1, p.by_Hk);
-    if (!g.run_of(p, b, cluster - 1 - b * p.Hk, rank, p.cluster)) return;
+    int of = cluster - 1, rt = 0;
+    if constexpr (SINK) {
+      of = fast_div(cluster - 1, p.by_row_tiles);
+      rt = cluster - 1 - of * p.row_tiles;
+    }
+    const int b = fast_div(of, p.by_Hk);
+    if (!g.run_of(p, b, of - b * p.Hk, rt, rank, p.cluster)) return;
   } else {
   Line<R, kTileKeys, kDecodeOver, SINK>::lay_out(p, s_prefix, s_warp);
   const int total = s_prefix[p.batch.B], share = Line<R, kTileKeys, kDecodeOver, SINK>::share_of(p, total);
@@ -738,6 +743,20 @@ int cluster_of(const sparkattn_cache_t& c, const sparkattn_batch_t& b, int frame
   return n;
 }
 
+// Calls of 17 to 128 rows per key head through a window with first tokens, cut into row tiles of 16, each an item of this file's kernel with a cluster of the returned
+// number of CTAs; 0: they take the tensor cores' kernel, where an item's beginning and end take 15 us but its rows share every key tile.  By row tiles a call takes some
+// 9 us and the rows' keys at 12 a ns, else 19.5 and the items' keys at 13.6 a ns.  E4M3, 128 channels, key heads in all x row tiles, window: 8 x 3, 4000 keys 19 us and 25,
+// 16,000 42 and 34; 8 x 7, 1500 17 and 22, 4000 27 and 25; 64 x 3, 500 18 and 25, 1500 35 and 31; bf16 64 x 3, 500 17 and 23, 1500 32 and 27; 1 x 3 of 64 channels,
+// 16,000 13 and 51.  Not more items than a wave: 96 x 7, 32 keys 27 us and 24.  (Without first tokens such calls keep the kernel, and so the bits, that they have had.)
+int row_tile_cluster(const sparkattn_cache_t& c, const sparkattn_batch_t& b, const Causal& causal, int row_tiles, int sms) {
+  const long long heads = (long long)b.B * c.H, items = heads * row_tiles;
+  const long long keys = std::min((long long)b.max_pages * c.page, ((long long)causal.window + 1) * causal.frame + b.max_new + causal.sink), tiles = (keys + 63) / 64;
+  if (items > 2 * sms || (double)keys * (items / 12.0 - heads / 13.6) > 10500.0) return 0;
+  int n = items * 16 <= sms ? 16 : 8;
+  while (n > 1 && (items * n > std::max(2 * sms, 16) || n / 2 >= tiles)) n /= 2;
+  return keys <= 4000LL * n ? n : 0;
+}
+
 // rows of an item, and stretches of the line: up to 16 rows per key head take this file's kernel, more the tensor cores' (cache_chunk.cu)
 struct Plan {
   int R, workers;
@@ -781,8 +800,8 @@ static int launch_decode(const sparkattn_cache_t& c, const sparkattn_batch_t& b,
   p.boxes = S::kTileKeys / p.box_rows;
   if ((rc = make_page_map(&mk, k_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
   if ((rc = make_page_map(&mv, v_cache, S::kElt, c, p.box_rows)) != SPARKATTN_OK) return rc;
-  const long long items = (long long)b.B * c.H;
-  p.cluster = cluster_of(c, b, p.causal.frame, p.causal.window, p.causal.sink, S::kTileKeys, p.workers / kDecodePerSM);
+  const long long items = (long long)b.B * c.H * p.row_tiles;
+  if (p.row_tiles == 1) p.cluster = cluster_of(c, b, p.causal.frame, p.causal.window, p.causal.sink, S::kTileKeys, p.workers / kDecodePerSM);
   const bool cluster = p.cluster > 0;
   // as deep a ring as the CTAs of an SM leave each other, sixteen tiles at most; fewer CTAs where a great many sequences leave no room
   const int listed = cluster ? 0 : b.B;
@@ -810,7 +829,9 @@ int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, con
                      const sparkattn_rows_t& out, float* lse, void* workspace, cudaStream_t stream) {
   CacheFwdParams p{};
   p.batch = make_batch_view(c, b);
-  p.causal = {frame_tokens, window, make_fast_div(std::max(frame_tokens, 1)), window > 0 ? sink : 0};
+  // (a window as wide as the table leaves no key out)
+  const bool apart = window > 0 && (long long)window * frame_tokens < (long long)b.max_pages * c.page;
+  p.causal = {frame_tokens, window, make_fast_div(std::max(frame_tokens, 1)), apart ? sink : 0};
   p.q = static_cast<const __nv_bfloat16*>(q.data);
   p.out = static_cast<__nv_bfloat16*>(out.data);
   p.q_stride_t = q.stride_t; p.q_stride_h = q.stride_h;
@@ -833,10 +854,22 @@ int launch_cache_fwd(const sparkattn_cache_t& c, const sparkattn_batch_t& b, con
   p.part_ml = reinterpret_cast<float*>(base);
   base += plan.ml;
   p.part_o = reinterpret_cast<float*>(base);
-  if (plan.R >= 128) return launch_cache_chunk(c, plan.R, p, k_cache, v_cache, stream);
+  p.row_tiles = 1;
+  int R = plan.R;
+  if (R == 128 && p.causal.sink > 0) {
+    const int sms = plan.workers, tiles = (p.G * b.max_new + 15) / 16, n = row_tile_cluster(c, b, p.causal, tiles, sms);
+    if (n > 0) {
+      R = 16;
+      p.row_tiles = tiles;
+      p.cluster = n;
+      p.workers = sms * kDecodePerSM;
+    }
+  }
+  p.by_row_tiles = make_fast_div(p.row_tiles);
+  if (R >= 128) return launch_cache_chunk(c, R, p, k_cache, v_cache, stream);
   const bool fp8 = c.dtype == SPARKATTN_FP8_E4M3;
   auto go = [&](auto d, auto e4m3) {
-    return plan.R == 8 ? launch_decode<decltype(d)::value, decltype(e4m3)::value, 1>(c, b, p, k_cache, v_cache, stream)
+    return R == 8 ? launch_decode<decltype(d)::value, decltype(e4m3)::value, 1>(c, b, p, k_cache, v_cache, stream)
                        : launch_decode<decltype(d)::value, decltype(e4m3)::value, 2>(c, b, p, k_cache, v_cache, stream);
   };
   using std::integral_constant;

@@ -40,6 +40,8 @@ struct CacheFwdParams {
   int workers;                   // stretches
   int slots;                     // K and V tiles that a CTA's ring holds
   int cluster;                   // CTAs of an item's cluster; 0: the line
+  int row_tiles;                 // clusters, SINK: row tiles of a (sequence, key head), each an item
+  FastDiv by_row_tiles;
   int32_t* status;
   struct Border* borders;        // [workers]
   float* part_ml;                // [2 workers][R][2] reference, sum
@@ -233,20 +235,21 @@ struct Stretch {
     rows = min(R, c.seq.n * p.G - row0);
     x += until - c.at;
   }
-  // instead: run `rank` of `ranks` equal runs of the item (b, h), which has all its rows in one tile; false if it has none
-  __device__ __forceinline__ bool run_of(const CacheFwdParams& p, int b, int h, int rank, int ranks) {
+  // instead: run `rank` of `ranks` equal runs of row tile rt of (b, h), the only one but for SINK; false if it has no rows
+  __device__ __forceinline__ bool run_of(const CacheFwdParams& p, int b, int h, int rt, int rank, int ranks) {
     c.b = b;
     c.h = h;
-    c.rt = c.at = 0;
+    c.rt = SINK ? rt : 0;
+    c.at = 0;
     c.row_tiles = 1;
     c.seq = sequence_of(p.batch, b);
-    if (c.seq.n == 0) return false;
-    c.item = L::item_of(p, c.seq, 0);
+    if (SINK ? c.seq.n * p.G <= c.rt * R : c.seq.n == 0) return false;
+    c.item = L::item_of(p, c.seq, c.rt);
     const int each = (c.item.tiles + ranks - 1) / ranks, end_tile = c.item.first + c.item.tiles;
     t0 = min(c.item.first + rank * each, end_tile);
     t1 = min(t0 + each, end_tile);
-    row0 = 0;
-    rows = c.seq.n * p.G;
+    row0 = c.rt * R;
+    rows = SINK ? min(R, c.seq.n * p.G - row0) : c.seq.n * p.G;
     x = end = 0;
     first = true;
     whole = false;

@@ -202,3 +202,59 @@ def test_a_page_that_is_seen_and_is_not_there_is_reported():
             out = sa.cache_fwd(q, cache, table, kv_len, max_new=news, window=60, sink=20, workspace=ws)
             assert sa.read_status(ws) == (sa.E_BAD_INDEX if bad else sa.OK)
             assert torch.isfinite(out).all()
+
+
+ROW_TILES = [
+    # lens, news, H, Hk, d, page, fp8, frame, window, sink: 17 to 128 rows per key head
+    ([900, 907], [5, 5], 16, 2, 128, 64, True, 1, 90, 21),
+    ([900, 907], [5, 5], 16, 2, 128, 64, False, 1, 90, 21),
+    ([900, 0, 7, 300], [5, 0, 1, 3], 8, 1, 64, 16, True, 1, 70, 4),       # sequences with fewer row tiles, and with none
+    ([900, 0, 7, 300], [5, 0, 1, 3], 8, 1, 64, 16, False, 1, 70, 129),
+    ([700, 650, 700], [17, 2, 16], 2, 2, 128, 32, True, 1, 40, 1),        # tiles of one row, of sixteen
+    ([700, 650], [33, 32], 2, 2, 128, 128, False, 1, 300, 64),
+    ([1300, 5], [9, 4], 24, 2, 128, 16, True, 1, 200, 500),
+    ([900], [128], 3, 3, 64, 64, True, 1, 77, 10),
+    ([900, 800], [60, 20], 4, 2, 128, 64, True, 25, 2, 25),               # rows of several frames in a tile
+    ([6000], [7], 12, 1, 128, 64, True, 1, 3000, 4),
+    ([20000], [9], 5, 1, 64, 128, False, 1, 12000, 300),
+    ([3, 130, 513], [7, 30, 1], 14, 7, 128, 64, True, 1, 50, 3),          # more new tokens than the first sequence holds
+]
+
+
+@pytest.mark.parametrize("case", ROW_TILES, ids=lambda c: "-".join(str(x) for x in c[2:]) + f"-{len(c[0])}x{max(c[0])}")
+@pytest.mark.parametrize("spare", [1, 700])
+def test_row_tiles(case, spare):
+    test_window_and_first_tokens(case, spare)
+
+
+def test_row_tiles_captured():
+    """A graph that holds two such calls, replayed with other lengths and queries, some sequences without rows."""
+    gen = torch.Generator(device=DEV).manual_seed(21)
+    lens, news, Hk, G, page = [600, 444, 90], [6, 6, 6], 2, 6, 32
+    pages = sum(-(-n // page) for n in lens) + 2
+    cache = make_cache(gen, pages, Hk, page, 128, True)
+    table = make_table(gen, lens, page, pages)
+    kv_len, q_start = batch_of(lens, news)
+    q = torch.randn((sum(news), Hk * G, 128), generator=gen, device=DEV).bfloat16()
+    args = dict(q_start=q_start, max_new=6, return_lse=True)
+    outs = [None, None]
+
+    def step():
+        outs[0] = sa.cache_fwd(q, cache, table, kv_len, window=60, sink=5, **args)
+        outs[1] = sa.cache_fwd(q, cache, table, kv_len, window=200, sink=70, **args)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for lens, news in (([600, 444, 90], [6, 6, 6]), ([580, 0, 33], [3, 0, 6]), ([64, 100, 90], [1, 6, 0])):
+        a, b = batch_of(lens, news)
+        kv_len.copy_(a)
+        q_start.copy_(b)
+        q.copy_(torch.randn(q.shape, generator=gen, device=DEV))
+        graph.replay()
+        n = sum(news)
+        for (out, lse), (window, sink) in zip(outs, ((60, 5), (200, 70))):
+            want, want_lse = reference(q[:n], cache, table, lens, news, 1, window, sink)
+            check(out[:n], lse[:n], want, want_lse)
