@@ -618,7 +618,7 @@ struct CopyPagesParams {
   const int32_t* dst;
   int n, split;                  // pairs; units of a page's K or V
   long long units;
-  int checkers;
+  int check_ctas;
   int32_t* status;
 };
 
@@ -685,18 +685,18 @@ cache_copy_pages_kernel(const __grid_constant__ CopyPagesParams p) {
   __shared__ uint32_t bits[2 * kCheckPages / 32];
   __shared__ int s_bad[2];
   pdl_wait();
-  if ((int)blockIdx.x < p.checkers) {
+  if ((int)blockIdx.x < p.check_ctas) {
     bool code_there = false;
     if (blockIdx.x == 0 && threadIdx.x == 0) code_there = take_header(p.status);
     check_pairs(p, blockIdx.x, bits, s_bad);
     if (blockIdx.x == 0 && __syncthreads_or(code_there))
-      // the word held a code, which may have been another checker's: see take_header
-      for (int range = 1; range < p.checkers; ++range) check_pairs(p, range, bits, s_bad);
+      // the word held a code, which may have been another CTA's: see take_header
+      for (int range = 1; range < p.check_ctas; ++range) check_pairs(p, range, bits, s_bad);
     return;
   }
   const int lane = threadIdx.x & 31;
-  const long long warp = (long long)((int)blockIdx.x - p.checkers) * (kCopyThreads / 32) + (threadIdx.x >> 5);
-  const long long warps = (long long)((int)gridDim.x - p.checkers) * (kCopyThreads / 32);
+  const long long warp = (long long)((int)blockIdx.x - p.check_ctas) * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  const long long warps = (long long)((int)gridDim.x - p.check_ctas) * (kCopyThreads / 32);
 #pragma unroll 1
   for (long long u0 = warp; u0 < p.units; u0 += 32 * warps) {
     const long long unit = u0 + lane * warps;
@@ -848,11 +848,11 @@ int launch_copy_pages(const sparkattn_cache_t& from, const PagePools& in, const 
   p.src = src; p.dst = dst; p.n = n;
   p.split = (p.pieces + kCopyPieces - 1) / kCopyPieces;
   p.units = 2LL * p.split * n;
-  p.checkers = (int)(((long long)to.pages + kCheckPages - 1) / kCheckPages);
+  p.check_ctas = (int)(((long long)to.pages + kCheckPages - 1) / kCheckPages);
   p.status = static_cast<int32_t*>(workspace);
   const int sms = current_sm_count();
   if (sms < 1) return SPARKATTN_E_CUDA;
-  const unsigned ctas = p.checkers + (unsigned)std::min<long long>((p.units + kCopyThreads / 32 - 1) / (kCopyThreads / 32), (long long)kCopyPerSM * sms);
+  const unsigned ctas = p.check_ctas + (unsigned)std::min<long long>((p.units + kCopyThreads / 32 - 1) / (kCopyThreads / 32), (long long)kCopyPerSM * sms);
   return launch_kernel(cache_copy_pages_kernel, dim3(ctas), kCopyThreads, 0, true, stream, p);
 }
 
