@@ -601,8 +601,8 @@ size_t sparkattn_pages_workspace_bytes(const sparkattn_book_t* book);
 
 /*
  * Sequence b of the new batch goes on from sequence parent[b] of the old one: fork (the same parent several times), reorder, and drop (a sequence
- * that is nobody's parent gives its pages back).  Children share their parent's pages, the partly filled last one too, until
- * sparkattn_pages_reserve finds that both go on in it.
+ * that is nobody's parent gives its pages back).  Children share their parent's pages, the partly filled last one and those reserved ahead too,
+ * until sparkattn_pages_reserve finds that both go on in them.
  * kv_len     : in,  int32 [B]
  * parent     : in,  int32 [B_out], entries in [-1, B); -1: an empty sequence (so does any other number, which is reported)
  * B_out      : sequences of the new batch, at most 4096
@@ -615,9 +615,10 @@ int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, co
 
 /*
  * Pages for the tokens kv_len[b] .. kv_new[b] - 1 of every sequence, in front of sparkattn_cache_append: the columns that these tokens begin get
- * free pages (those that have one keep it).  Where the token kv_len[b] falls into a page that others hold as well, it is replaced
- * by a free one, and the pair (src, dst) says what has to be copied; of the sequences that go on in one page the first keeps it if nobody
- * else holds it.  All or nothing: where the pool has fewer free pages than that, the book stays as it was, and the status is
+ * free pages.  Those that have one, reserved ahead, keep it if nobody else holds it; if others do, since the sequence was forked behind that,
+ * the column gets another one.  Where the token kv_len[b] falls into a partly filled page that others hold as well, it is replaced
+ * by a free one, and the pair (src, dst) says what has to be copied; of the sequences that go on in one such page the first keeps it if nobody
+ * else holds it.  So no token of the call lies in a page that another sequence has.  All or nothing: where the pool has fewer free pages than that, the book stays as it was, and the status is
  * SPARKATTN_E_OUT_OF_PAGES, its detail the number of pages that are missing, whatever else was found.  Nothing may be appended then.
  * kv_len, kv_new : in,  int32 [B], 0 <= kv_len <= kv_new <= max_pages * page
  * src, dst   : out, int32 [B]: pages to copy for sequence b, or -1 and -1

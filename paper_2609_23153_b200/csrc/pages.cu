@@ -309,13 +309,14 @@ struct ReserveParams {
   const int32_t* kv_new;
   int32_t* src;
   int32_t* dst;
-  int32_t* list;                 // workspace: the free pages that are handed out, in order
+  int32_t* list;                 // workspace: the free pages that are handed out, in order; then what each has been given for (-1: nothing)
   int ranks, slots;              // slots of the hash table: a power of two, twice the sequences or more
   int32_t* status;
 };
 constexpr int kOwnColumns = 32;      // a sequence that asks for more columns is looked through by the whole CTA
-// What a sequence asks for: pages for the columns [first, last) that have none, and another page in place of a partly filled one, `tail`, that
-// others hold as well.
+// What a sequence asks for: pages for those of the columns [first, last) that have none, or one that others hold as well (reserved ahead, then
+// forked: whoever goes on there would write into the others' tokens, and there is nothing in it to copy), and another page in place of a
+// partly filled one, `tail`, that others hold as well.
 struct Asks {
   int tail, first, last;         // tail: column of the partly filled page, or first where there is none
   bool fine;                     // the numbers make sense
@@ -327,6 +328,7 @@ __device__ __forceinline__ Asks asks_of(const ReserveParams& p, int b) {
   if (a.fine && len > old) a = {old >> p.v.shift, pages_of(p.v, old), pages_of(p.v, len), true};
   return a;
 }
+__device__ __forceinline__ bool asks_for(const BookView& v, int e) { return e == -1 || ((uint32_t)e < (uint32_t)v.pages && v.refs[e] > 1); }
 // Dynamic shared memory: prefix[B + 1]; of every sequence the columns that it asks for and the page that it copies; the hash table of partly
 // filled pages that several hold: page, sequences that write to it, the first of them.  Every CTA of the first cluster has it all.
 __global__ void __launch_bounds__(kBookThreads)
@@ -364,7 +366,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     }
     return (int)(at & (p.slots - 1));
   };
-  // who writes to pages that several hold, and the columns that have no page
+  // who writes to pages that several hold, and the columns that ask for a page
   bool long_one = false;
   for (int b = threadIdx.x; b < v.B; b += kBookThreads) {
     const Asks a = asks_of(p, b);
@@ -375,7 +377,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     int missing = 0;
     if (a.last - a.first <= kOwnColumns) {
 #pragma unroll 8
-      for (int i = a.first; i < a.last; ++i) missing += row[i] == -1 ? 1 : 0;
+      for (int i = a.first; i < a.last; ++i) missing += asks_for(v, row[i]) ? 1 : 0;
     } else {
       long_one = true;
     }
@@ -410,7 +412,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
         int n = 0;
         for (long long i0 = s_first[b] + (long long)((warp - b) & (kBookWarps - 1)) * kCopyColumns; i0 < last; i0 += kBookWarps * kCopyColumns) {
 #pragma unroll
-          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && row[i0 + 32 * u + lane] == -1 ? 1 : 0;
+          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(v, row[i0 + 32 * u + lane]) ? 1 : 0;
         }
         n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
         if (lane == 0) atomicAdd(&prefix[b], n);
@@ -479,23 +481,34 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     int at = prefix[b];
     const int32_t* row = v.table + (int64_t)b * v.max_pages;
     int32_t* out = v.table_out + (int64_t)b * v.max_pages;
-    const int to = from >= 0 ? p.list[at++] : -1;
     if (lane == 0) {
-      if (from >= 0) atomicSub(v.refs_out + from, 1);
+      int to = -1;
+      if (from >= 0) {
+        to = p.list[at];
+        p.list[at] = from;
+      }
       p.src[b] = from;
       p.dst[b] = to;
       if (tail < first) out[tail] = from >= 0 ? to : row[tail];
     }
+    if (from >= 0) ++at;
     auto fill = [&](int i0, auto many) {
       constexpr int U = decltype(many)::value;
       int e[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) e[u] = i0 + 32 * u + lane < last ? row[i0 + 32 * u + lane] : 0;
+      for (int u = 0; u < U; ++u) e[u] = i0 + 32 * u + lane < last ? row[i0 + 32 * u + lane] : -1;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t missing = __ballot_sync(0xffffffffu, e[u] == -1);
-        if (e[u] == -1 && enough) e[u] = p.list[at + __popc(missing & ((1u << lane) - 1u))];
-        at += __popc(missing);
+        // (counts that are more than 1 are what they were: they change behind the last barrier)
+        const bool asks = enough && i0 + 32 * u + lane < last && asks_for(v, e[u]);
+        const uint32_t all = __ballot_sync(0xffffffffu, asks);
+        if (asks) {
+          int32_t* mine = p.list + at + __popc(all & ((1u << lane) - 1u));
+          const int to = *mine;
+          *mine = e[u];
+          e[u] = to;
+        }
+        at += __popc(all);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -508,6 +521,12 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     }
   }
   book_end(s, rank, p.ranks, p.status);
+  // what has been replaced has a user less (behind book_end's barrier: everybody has looked at the counts)
+  if (!enough) return;
+  for (int i = rank * kBookThreads + threadIdx.x; i < carry; i += p.ranks * kBookThreads) {
+    const int e = p.list[i];
+    if (e >= 0) atomicSub(v.refs_out + e, 1);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------- compact
