@@ -309,7 +309,7 @@ struct ReserveParams {
   const int32_t* kv_new;
   int32_t* src;
   int32_t* dst;
-  int32_t* list;                 // workspace: the free pages that are handed out, in order; then what each has been given for (-1: nothing)
+  int32_t* list;                 // workspace: the free pages that are handed out, in order; then (Asks::ahead) what each has been given for
   int ranks, slots;              // slots of the hash table: a power of two, twice the sequences or more
   int32_t* status;
 };
@@ -328,12 +328,19 @@ __device__ __forceinline__ Asks asks_of(const ReserveParams& p, int b) {
   if (a.fine && len > old) a = {old >> p.v.shift, pages_of(p.v, old), pages_of(p.v, len), true};
   return a;
 }
-__device__ __forceinline__ bool asks_for(const BookView& v, int e) { return e == -1 || ((uint32_t)e < (uint32_t)v.pages && v.refs[e] > 1); }
+// Whether a column with entry e asks for a page; `ahead` is set where it is in place of one that others hold.
+__device__ __forceinline__ bool asks_for(const BookView& v, int e, bool& ahead) {
+  if (e == -1) return true;
+  const bool shared = (uint32_t)e < (uint32_t)v.pages && v.refs[e] > 1;
+  ahead |= shared;
+  return shared;
+}
 // Dynamic shared memory: prefix[B + 1]; of every sequence the columns that it asks for and the page that it copies; the hash table of partly
 // filled pages that several hold: page, sequences that write to it, the first of them.  Every CTA of the first cluster has it all.
 __global__ void __launch_bounds__(kBookThreads)
 pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   __shared__ BookShared s;
+  __shared__ int s_ahead;              // some column asks for a page in place of one that others hold
   extern __shared__ int s_dynamic[];
   const BookView& v = p.v;
   int* prefix = s_dynamic;
@@ -356,6 +363,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < p.slots; i += kBookThreads) { h_page[i] = -1; h_writers[i] = 0; h_first[i] = 0x7fffffff; }
+  if (threadIdx.x == 0) s_ahead = 0;
   book_begin(s);
   auto slot_of = [&](int page, bool insert) {
     uint32_t at = (uint32_t)page * 2654435761u >> 7;
@@ -367,7 +375,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     return (int)(at & (p.slots - 1));
   };
   // who writes to pages that several hold, and the columns that ask for a page
-  bool long_one = false;
+  bool long_one = false, ahead = false;
   for (int b = threadIdx.x; b < v.B; b += kBookThreads) {
     const Asks a = asks_of(p, b);
     int shared = -1;
@@ -377,7 +385,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     int missing = 0;
     if (a.last - a.first <= kOwnColumns) {
 #pragma unroll 8
-      for (int i = a.first; i < a.last; ++i) missing += asks_for(v, row[i]) ? 1 : 0;
+      for (int i = a.first; i < a.last; ++i) missing += asks_for(v, row[i], ahead) ? 1 : 0;
     } else {
       long_one = true;
     }
@@ -398,10 +406,12 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     s_last[b] = a.last;
     s_copy[b] = shared;
   }
+  if (ahead) s_ahead = 1;
   const PoolRun run = run_of_warp(v.pages, p.ranks, rank);
   const int free_here = count_run(v, run, [](int r) { return r == 0 ? 1 : 0; });
   if (lane == 0) s.count[warp] = free_here;
   if (__syncthreads_or(long_one)) {
+    ahead = false;
     // 256 columns at a time, those of a sequence dealt out to the warps
     for (int b0 = 0; b0 < v.B; b0 += 32) {
       const int own = b0 + lane, columns = own < v.B ? s_last[own] - s_first[own] : 0;
@@ -412,12 +422,13 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
         int n = 0;
         for (long long i0 = s_first[b] + (long long)((warp - b) & (kBookWarps - 1)) * kCopyColumns; i0 < last; i0 += kBookWarps * kCopyColumns) {
 #pragma unroll
-          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(v, row[i0 + 32 * u + lane]) ? 1 : 0;
+          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(v, row[i0 + 32 * u + lane], ahead) ? 1 : 0;
         }
         n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
         if (lane == 0) atomicAdd(&prefix[b], n);
       }
     }
+    if (ahead) s_ahead = 1;
     __syncthreads();
   }
   int carry = 0;
@@ -476,16 +487,19 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     }
   }
   book_barrier();
+  // Counts of what is replaced fall at once, or, where columns are looked at for being shared, behind the last barrier, so that every
+  // look sees the same; until then the list holds what its pages take the place of.
+  const bool later = s_ahead != 0;
   for (int b = rank * kBookWarps + warp; b < v.B; b += p.ranks * kBookWarps) {
     const int tail = s_tail[b], first = s_first[b], last = s_last[b], from = enough ? s_copy[b] : -1;
     int at = prefix[b];
     const int32_t* row = v.table + (int64_t)b * v.max_pages;
     int32_t* out = v.table_out + (int64_t)b * v.max_pages;
     if (lane == 0) {
-      int to = -1;
+      const int to = from >= 0 ? p.list[at] : -1;
       if (from >= 0) {
-        to = p.list[at];
-        p.list[at] = from;
+        if (later) p.list[at] = from;
+        else atomicSub(v.refs_out + from, 1);
       }
       p.src[b] = from;
       p.dst[b] = to;
@@ -499,13 +513,13 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
       for (int u = 0; u < U; ++u) e[u] = i0 + 32 * u + lane < last ? row[i0 + 32 * u + lane] : -1;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        // (counts that are more than 1 are what they were: they change behind the last barrier)
-        const bool asks = enough && i0 + 32 * u + lane < last && asks_for(v, e[u]);
+        bool in_place = false;
+        const bool asks = enough && i0 + 32 * u + lane < last && (later ? asks_for(v, e[u], in_place) : e[u] == -1);
         const uint32_t all = __ballot_sync(0xffffffffu, asks);
         if (asks) {
           int32_t* mine = p.list + at + __popc(all & ((1u << lane) - 1u));
           const int to = *mine;
-          *mine = e[u];
+          if (later) *mine = e[u];
           e[u] = to;
         }
         at += __popc(all);
@@ -521,8 +535,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     }
   }
   book_end(s, rank, p.ranks, p.status);
-  // what has been replaced has a user less (behind book_end's barrier: everybody has looked at the counts)
-  if (!enough) return;
+  if (!later || !enough) return;
   for (int i = rank * kBookThreads + threadIdx.x; i < carry; i += p.ranks * kBookThreads) {
     const int e = p.list[i];
     if (e >= 0) atomicSub(v.refs_out + e, 1);
