@@ -330,8 +330,8 @@ __device__ __forceinline__ Asks asks_of(const ReserveParams& p, int b) {
 }
 // Whether a column with entry e asks for a page; `ahead` is set where it is in place of one that others hold.
 __device__ __forceinline__ bool asks_for(const BookView& v, int e, bool& ahead) {
-  if (e == -1) return true;
-  const bool shared = (uint32_t)e < (uint32_t)v.pages && v.refs[e] > 1;
+  if ((uint32_t)e >= (uint32_t)v.pages) return true;
+  const bool shared = v.refs[e] > 1;
   ahead |= shared;
   return shared;
 }
@@ -514,7 +514,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         bool in_place = false;
-        const bool asks = enough && i0 + 32 * u + lane < last && (later ? asks_for(v, e[u], in_place) : e[u] == -1);
+        const bool asks = enough && i0 + 32 * u + lane < last && (later ? asks_for(v, e[u], in_place) : (uint32_t)e[u] >= (uint32_t)v.pages);
         const uint32_t all = __ballot_sync(0xffffffffu, asks);
         if (asks) {
           int32_t* mine = p.list + at + __popc(all & ((1u << lane) - 1u));
@@ -538,7 +538,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   if (!later || !enough) return;
   for (int i = rank * kBookThreads + threadIdx.x; i < carry; i += p.ranks * kBookThreads) {
     const int e = p.list[i];
-    if (e >= 0) atomicSub(v.refs_out + e, 1);
+    if ((uint32_t)e < (uint32_t)v.pages) atomicSub(v.refs_out + e, 1);
   }
 }
 

@@ -192,3 +192,24 @@ def test_a_sequence_taken_back_leaves_what_others_go_on_in():
     for x, y, z in zip(cache[:2], (k, v), more):
         assert torch.equal(gathered(x, table[0], 41, P), torch.cat([y, z[:1]]))
         assert torch.equal(gathered(x, table[1], 45, P), torch.cat([y[:20], z[1:]]))
+
+
+@pytest.mark.parametrize("columns", [4, 500])
+def test_entries_that_name_no_page_count_as_none(columns):
+    """-1 or any other number outside the pool, in a column that is asked for."""
+    pages, P = 2 * columns + 10, 16
+    wrong = [-1, -2, pages, 2 ** 31 - 1, -2 ** 31, pages + 7, -1]
+    row = [0, 1] + [wrong[i % len(wrong)] for i in range(columns - 2)]
+    table, refs = [row, [2, -2] + row[2:]], [1, 1, 1] + [0] * (pages - 3)
+    length, new = [20, 16], [columns * P, (columns - 1) * P]
+    got = sa.pages_reserve(ints(table), ints(length), ints(refs), ints(new), P, check_status=True)
+    first = list(range(3, 3 + columns - 2))
+    second = list(range(3 + columns - 2, 3 + 2 * columns - 4))
+    assert got[0].tolist() == [[0, 1] + first, [2] + second + [row[-1]]]
+    assert got[1].tolist() == [1] * (3 + 2 * columns - 4) + [0] * (pages - 3 - 2 * columns + 4)
+    assert (got[2] == -1).all() and (got[3] == -1).all()
+    few = [1] * pages                                  # none is free: the book stays as it was
+    ws = workspace(pages)
+    got = sa.pages_reserve(ints(table), ints(length), ints(few), ints(new), P, workspace=ws)
+    assert sa.read_status(ws) == sa.E_OUT_OF_PAGES and int(ws.view(torch.int32)[1]) == 2 * columns - 4
+    assert same(got[0], table) and same(got[1], few)
