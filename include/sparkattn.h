@@ -624,7 +624,7 @@ int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, co
  * src, dst   : out, int32 [B]: pages to copy for sequence b, or -1 and -1
  * table_out, refs_out : out, may be page_table and refs
  * Device errors (SPARKATTN_E_BAD_INDEX): lengths that are not so (the sequence is left out), a partly filled page that is none or
- * that nobody holds.
+ * that nobody holds, a page that stands in a column that is asked for and that nobody holds (it stays there).
  */
 int sparkattn_pages_reserve(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out,
                             int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream);

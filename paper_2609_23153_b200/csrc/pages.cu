@@ -328,13 +328,6 @@ __device__ __forceinline__ Asks asks_of(const ReserveParams& p, int b) {
   if (a.fine && len > old) a = {old >> p.v.shift, pages_of(p.v, old), pages_of(p.v, len), true};
   return a;
 }
-// Whether a column with entry e asks for a page; `ahead` is set where it is in place of one that others hold.
-__device__ __forceinline__ bool asks_for(const BookView& v, int e, bool& ahead) {
-  if ((uint32_t)e >= (uint32_t)v.pages) return true;
-  const bool shared = v.refs[e] > 1;
-  ahead |= shared;
-  return shared;
-}
 // Dynamic shared memory: prefix[B + 1]; of every sequence the columns that it asks for and the page that it copies; the hash table of partly
 // filled pages that several hold: page, sequences that write to it, the first of them.  Every CTA of the first cluster has it all.
 __global__ void __launch_bounds__(kBookThreads)
@@ -376,6 +369,13 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   };
   // who writes to pages that several hold, and the columns that ask for a page
   bool long_one = false, ahead = false;
+  auto asks_for = [&](int e) {
+    if ((uint32_t)e >= (uint32_t)v.pages) return true;
+    const int holders = v.refs[e];
+    if (holders < 1) found(s, SPARKATTN_E_BAD_INDEX, e);
+    ahead |= holders > 1;
+    return holders > 1;
+  };
   for (int b = threadIdx.x; b < v.B; b += kBookThreads) {
     const Asks a = asks_of(p, b);
     int shared = -1;
@@ -385,7 +385,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     int missing = 0;
     if (a.last - a.first <= kOwnColumns) {
 #pragma unroll 8
-      for (int i = a.first; i < a.last; ++i) missing += asks_for(v, row[i], ahead) ? 1 : 0;
+      for (int i = a.first; i < a.last; ++i) missing += asks_for(row[i]) ? 1 : 0;
     } else {
       long_one = true;
     }
@@ -422,7 +422,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
         int n = 0;
         for (long long i0 = s_first[b] + (long long)((warp - b) & (kBookWarps - 1)) * kCopyColumns; i0 < last; i0 += kBookWarps * kCopyColumns) {
 #pragma unroll
-          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(v, row[i0 + 32 * u + lane], ahead) ? 1 : 0;
+          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(row[i0 + 32 * u + lane]) ? 1 : 0;
         }
         n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
         if (lane == 0) atomicAdd(&prefix[b], n);
@@ -513,8 +513,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
       for (int u = 0; u < U; ++u) e[u] = i0 + 32 * u + lane < last ? row[i0 + 32 * u + lane] : -1;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        bool in_place = false;
-        const bool asks = enough && i0 + 32 * u + lane < last && (later ? asks_for(v, e[u], in_place) : (uint32_t)e[u] >= (uint32_t)v.pages);
+        const bool asks = enough && i0 + 32 * u + lane < last && ((uint32_t)e[u] >= (uint32_t)v.pages || (later && v.refs[e[u]] > 1));
         const uint32_t all = __ballot_sync(0xffffffffu, asks);
         if (asks) {
           int32_t* mine = p.list + at + __popc(all & ((1u << lane) - 1u));

@@ -213,3 +213,18 @@ def test_entries_that_name_no_page_count_as_none(columns):
     got = sa.pages_reserve(ints(table), ints(length), ints(few), ints(new), P, workspace=ws)
     assert sa.read_status(ws) == sa.E_OUT_OF_PAGES and int(ws.view(torch.int32)[1]) == 2 * columns - 4
     assert same(got[0], table) and same(got[1], few)
+
+
+@pytest.mark.parametrize("columns,at", [(4, 2), (4, 3), (500, 2), (500, 499)])
+def test_a_page_ahead_that_nobody_holds_is_reported(columns, at):
+    """It stays where it is, and the rest of the call is as without it."""
+    pages, P = 2 * columns, 16
+    row = [0] + [-1] * (columns - 1)
+    row[at] = pages - 1
+    ws = workspace(pages)
+    got = sa.pages_reserve(ints([row]), ints([16]), ints([1] + [0] * (pages - 1)), ints([columns * P]), P, workspace=ws)
+    assert sa.read_status(ws) == sa.E_BAD_INDEX and int(ws.view(torch.int32)[1]) == pages - 1
+    free = iter(range(1, pages))
+    assert got[0].tolist() == [[e if e >= 0 else next(free) for e in row]]
+    sa.pages_reserve(ints([row]), ints([16]), ints([1] + [0] * (pages - 1)), ints([at * P]), P, workspace=ws)      # not asked for: not looked at
+    assert sa.read_status(ws) == sa.OK
