@@ -579,7 +579,7 @@ int sparkattn_cache_fwd_sink(const sparkattn_cache_t* cache, const sparkattn_bat
  * of tables name it (0: free); whoever keeps a page for another reason, a prompt that is asked for again for instance, adds 1 of its own.
  * Every layer has pools of its own; the book is one for all, and the calls that move pages leave (from, to) pairs that
  * sparkattn_cache_copy_pages takes once for each layer.  Nothing here waits for the host: a captured graph can reserve, append,
- * attend and trim step after step.
+ * attend and trim step after step, by the lengths that sparkattn_pages_reserve_len leaves, which stop a step whose pages do not suffice.
  *
  * An entry of a table is a page, or -1 where a sequence has none.  The calls write table, counts and lengths to where they are told, which
  * may be where they come from (but for sparkattn_pages_fork's tables and lengths); entries that name no page of the pool count as none.
@@ -619,7 +619,8 @@ int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, co
  * the column gets another one.  Where the token kv_len[b] falls into a partly filled page that others hold as well, it is replaced
  * by a free one, and the pair (src, dst) says what has to be copied; of the sequences that go on in one such page the first keeps it if nobody
  * else holds it.  So no token of the call lies in a page that another sequence has.  All or nothing: where the pool has fewer free pages than that, the book stays as it was, and the status is
- * SPARKATTN_E_OUT_OF_PAGES, its detail the number of pages that are missing, whatever else was found.  Nothing may be appended then.
+ * SPARKATTN_E_OUT_OF_PAGES, its detail the number of pages that are missing, whatever else was found.  Nothing may be appended then: sequences
+ * still share the page that they go on in.  Who does not read the status before the append takes sparkattn_pages_reserve_len.
  * kv_len, kv_new : in,  int32 [B], 0 <= kv_len <= kv_new <= max_pages * page
  * src, dst   : out, int32 [B]: pages to copy for sequence b, or -1 and -1
  * table_out, refs_out : out, may be page_table and refs
@@ -628,6 +629,16 @@ int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, co
  */
 int sparkattn_pages_reserve(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out,
                             int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The same, and the lengths for the calls of the step behind it, so that the host need not learn first how it went.
+ * kv_len_out : out, int32 [B], neither kv_len nor kv_new: kv_new[b]; -1 where sequence b has not got what it asked for, whether its own numbers
+ *              make no sense or the pages do not suffice (then every b with kv_new[b] > kv_len[b]).  By a length of -1 sparkattn_cache_append stores
+ *              nothing, sparkattn_cache_fwd gives rows of a sequence without keys, and sparkattn_pages_trim gives nothing back; all three
+ *              report it, and so does a reservation that takes it as kv_len.
+ */
+int sparkattn_pages_reserve_len(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* kv_len_out, int32_t* table_out,
+                                int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * Gives back the pages that no token from position kv_len[b] on reads, under the rules of sparkattn_cache_fwd_sink: those that lie

@@ -47,7 +47,7 @@ EXPORTS = (
     "sparkattn_quant_fp8_pooled", "sparkattn_select_pooled", "sparkattn_fwd_gated_workspace_bytes", "sparkattn_fwd_gated",
     "sparkattn_cache_workspace_bytes", "sparkattn_cache_append", "sparkattn_cache_fwd", "sparkattn_cache_fwd_sink",
     "sparkattn_cache_append_norm", "sparkattn_norm_rotate", "sparkattn_pages_workspace_bytes", "sparkattn_pages_fork",
-    "sparkattn_pages_reserve", "sparkattn_pages_trim", "sparkattn_pages_compact", "sparkattn_cache_copy_pages",
+    "sparkattn_pages_reserve", "sparkattn_pages_trim", "sparkattn_pages_compact", "sparkattn_cache_copy_pages", "sparkattn_pages_reserve_len",
 )
 
 
@@ -127,7 +127,7 @@ _BOUND = ("workspace_bytes", "select", "select_window", "select_padded", "select
           "quant_fp8_per_token", "fwd", "fwd_window", "fwd_padded", "gather_tokens", "comp_workspace_bytes", "comp_state", "comp_apply",
           "fwd_gated_workspace_bytes", "fwd_gated", "cache_workspace_bytes", "cache_append", "cache_fwd",
           "cache_fwd_sink", "cache_append_norm", "norm_rotate", "pages_workspace_bytes", "pages_fork", "pages_reserve", "pages_trim",
-          "pages_compact", "cache_copy_pages")
+          "pages_compact", "cache_copy_pages", "pages_reserve_len")
 _NO_WORKSPACE = 1        # the library does not serve the shape: the workspace query returned 0
 
 _lib = None
@@ -213,7 +213,7 @@ def lib() -> ctypes.CDLL:
         kp = ctypes.POINTER(BookShape)
         L.sparkattn_pages_workspace_bytes.restype = sz
         L.sparkattn_pages_workspace_bytes.argtypes = [kp]
-        for name, args in (("fork", [vp, vp, i32, vp, vp, vp]), ("reserve", [vp, vp, vp, vp, vp, vp]), ("trim", [vp, i32, i32, i32, vp, vp]),
+        for name, args in (("fork", [vp, vp, i32, vp, vp, vp]), ("reserve", [vp, vp, vp, vp, vp, vp]), ("reserve_len", [vp, vp, vp, vp, vp, vp, vp]), ("trim", [vp, i32, i32, i32, vp, vp]),
                            ("compact", [vp, vp, vp, vp])):
             call = getattr(L, "sparkattn_pages_" + name)
             call.restype = ctypes.c_int
@@ -617,13 +617,15 @@ def pages_fork(page_table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tenso
 
 def pages_reserve(page_table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor, kv_new: torch.Tensor, page: int, *,
                   page_table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, src: Optional[torch.Tensor] = None,
-                  dst: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
-                  check_status: bool = False):
-    """``sparkattn_pages_reserve``: pages for the tokens kv_len[b] .. kv_new[b] - 1 of every sequence, pages of ``page`` tokens, in front of
+                  dst: Optional[torch.Tensor] = None, kv_len_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None, check_status: bool = False):
+    """``sparkattn_pages_reserve`` (``sparkattn_pages_reserve_len`` with ``kv_len_out``): pages for the tokens kv_len[b] .. kv_new[b] - 1 of every sequence, pages of ``page`` tokens, in front of
     :func:`cache_append`.  Returns (page_table, refs, src, dst): src, dst int32 [B] go to :func:`cache_copy_pages`, for every layer's cache.  All
-    or nothing: with too few free pages the status is E_OUT_OF_PAGES and the book stays as it was.  The outputs may be the inputs."""
-    rc, table, refs, src, dst, workspace = _calls().pages_reserve(page_table, kv_len, refs, kv_new, page, page_table_out, refs_out, src, dst, workspace,
-                                                                  None if stream is None else stream.cuda_stream)
+    or nothing: with too few free pages the status is E_OUT_OF_PAGES, the book stays as it was, and nothing may be appended.  ``kv_len_out`` int32 [B]
+    gets the lengths for the calls of the step, kv_new[b], or -1 where sequence b has not got its pages, by which they leave it alone: for a captured
+    step, or any that does not read the status first.  The other outputs may be the inputs."""
+    rc, table, refs, src, dst, workspace = _calls().pages_reserve(page_table, kv_len, refs, kv_new, page, page_table_out, refs_out, src, dst, kv_len_out,
+                                                                  workspace, None if stream is None else stream.cuda_stream)
     _book(rc, "sparkattn_pages_reserve", workspace, stream, check_status)
     return table, refs, src, dst
 

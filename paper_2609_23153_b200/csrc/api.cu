@@ -715,12 +715,25 @@ int sparkattn_pages_fork(const sparkattn_book_t* book, const int32_t* kv_len, co
   return launch_pages_fork(*book, kv_len, parent, B_out, table_out, kv_len_out, refs_out, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
-int sparkattn_pages_reserve(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out,
-                            int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+namespace {
+int reserve_impl(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* kv_len_out, int32_t* table_out, int32_t* refs_out,
+                 int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   const int rc = check_book_call(book, table_out, refs_out, workspace, workspace_bytes);
   if (rc != SPARKATTN_OK) return rc;
   if (!kv_len || !kv_new || !src || !dst) return SPARKATTN_E_INVALID_ARG;
-  return launch_pages_reserve(*book, kv_len, kv_new, table_out, refs_out, src, dst, workspace, static_cast<cudaStream_t>(cuda_stream));
+  return launch_pages_reserve(*book, kv_len, kv_new, kv_len_out, table_out, refs_out, src, dst, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+}  // namespace
+
+int sparkattn_pages_reserve(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out,
+                            int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return reserve_impl(book, kv_len, kv_new, nullptr, table_out, refs_out, src, dst, workspace, workspace_bytes, cuda_stream);
+}
+
+int sparkattn_pages_reserve_len(const sparkattn_book_t* book, const int32_t* kv_len, const int32_t* kv_new, int32_t* kv_len_out, int32_t* table_out,
+                                int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!kv_len_out || kv_len_out == kv_len || kv_len_out == kv_new) return SPARKATTN_E_INVALID_ARG;
+  return reserve_impl(book, kv_len, kv_new, kv_len_out, table_out, refs_out, src, dst, workspace, workspace_bytes, cuda_stream);
 }
 
 int sparkattn_pages_trim(const sparkattn_book_t* book, const int32_t* kv_len, int32_t frame_tokens, int32_t window_frames, int32_t sink_tokens,

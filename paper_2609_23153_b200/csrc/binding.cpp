@@ -51,6 +51,7 @@ struct Library {
   decltype(&sparkattn_pages_trim) pages_trim;
   decltype(&sparkattn_pages_compact) pages_compact;
   decltype(&sparkattn_cache_copy_pages) cache_copy_pages;
+  decltype(&sparkattn_pages_reserve_len) pages_reserve_len;
 };
 Library g_lib{};
 
@@ -792,20 +793,22 @@ PyObject* pages_fork(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// pages_reserve(page_table, kv_len, refs, kv_new, page, table_out, refs_out, src, dst, workspace, stream) -> rc, table, refs, src, dst, workspace
+// pages_reserve(page_table, kv_len, refs, kv_new, page, table_out, refs_out, src, dst, kv_len_out, workspace, stream)
+// -> rc, table, refs, src, dst, workspace
 PyObject* pages_reserve(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Args a(argv, n);
-  a.expect(11);
+  a.expect(12);
   Book book(a, true);
   const at::Tensor kv_new = a.tensor();
   const int32_t page = a.i32();
   const at::Tensor table_out = a.optional_tensor(), refs_out = a.optional_tensor();
   at::Tensor src = a.optional_tensor(), dst = a.optional_tensor();
-  const at::Tensor ws = a.optional_tensor();
+  const at::Tensor len_out = a.optional_tensor(), ws = a.optional_tensor();
   const Stream stream = a.stream();
   book.describe(page);
   book.words(kv_new, book.b.B, "kv_new is a contiguous int32 [B] on the table's device");
+  if (len_out.defined()) book.words(len_out, book.b.B, "kv_len_out is a contiguous int32 [B] on the table's device");
   book.check_device();
   int rc;
   {
@@ -813,8 +816,10 @@ PyObject* pages_reserve(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     book.outputs(table_out, refs_out, ws, book.b.B, stream);
     src = book.pairs(src, book.b.B, stream);
     dst = book.pairs(dst, book.b.B, stream);
-    rc = g_lib.pages_reserve(&book.b, iptr(book.len), iptr(kv_new), iptr(book.table_out), iptr(book.refs_out), iptr(src), iptr(dst), ptr(book.ws),
-                             (size_t)book.ws.numel(), stream);
+    rc = len_out.defined() ? g_lib.pages_reserve_len(&book.b, iptr(book.len), iptr(kv_new), iptr(len_out), iptr(book.table_out), iptr(book.refs_out), iptr(src),
+                                                     iptr(dst), ptr(book.ws), (size_t)book.ws.numel(), stream)
+                           : g_lib.pages_reserve(&book.b, iptr(book.len), iptr(kv_new), iptr(book.table_out), iptr(book.refs_out), iptr(src), iptr(dst),
+                                                 ptr(book.ws), (size_t)book.ws.numel(), stream);
   }
   return result(rc, {book.table_out, book.refs_out, src, dst, book.ws});
   END_HANDLE_TH_ERRORS

@@ -128,8 +128,8 @@ int launch_pages_fork(const sparkattn_book_t& book, const int32_t* kv_len, const
                       int32_t* refs_out, void* workspace, cudaStream_t stream);
 int launch_pages_trim(const sparkattn_book_t& book, const int32_t* kv_len, int frame, int window, int sink, int32_t* table_out, int32_t* refs_out,
                       void* workspace, cudaStream_t stream);
-int launch_pages_reserve(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out, int32_t* src,
-                         int32_t* dst, void* workspace, cudaStream_t stream);
+int launch_pages_reserve(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* kv_new, int32_t* kv_len_out, int32_t* table_out,
+                         int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace, cudaStream_t stream);      // kv_len_out: NULL, or the lengths for the step
 int launch_pages_compact(const sparkattn_book_t& book, int32_t* table_out, int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace, cudaStream_t stream);
 struct PagePools {
   void* k;

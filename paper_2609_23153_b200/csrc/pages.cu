@@ -307,6 +307,7 @@ struct ReserveParams {
   BookView v;
   const int32_t* kv_len;
   const int32_t* kv_new;
+  int32_t* kv_len_out;           // NULL: not asked for
   int32_t* src;
   int32_t* dst;
   int32_t* list;                 // workspace: the free pages that are handed out, in order; then (Asks::ahead) what each has been given for
@@ -334,6 +335,7 @@ __global__ void __launch_bounds__(kBookThreads)
 pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   __shared__ BookShared s;
   __shared__ int s_ahead;              // some column asks for a page in place of one that others hold
+  __shared__ uint32_t s_wrong[kCacheMaxSequences / 32];      // a bit for every sequence whose numbers make no sense
   extern __shared__ int s_dynamic[];
   const BookView& v = p.v;
   int* prefix = s_dynamic;
@@ -357,6 +359,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < p.slots; i += kBookThreads) { h_page[i] = -1; h_writers[i] = 0; h_first[i] = 0x7fffffff; }
   if (threadIdx.x == 0) s_ahead = 0;
+  if (threadIdx.x < kCacheMaxSequences / 32) s_wrong[threadIdx.x] = 0u;
   book_begin(s);
   auto slot_of = [&](int page, bool insert) {
     uint32_t at = (uint32_t)page * 2654435761u >> 7;
@@ -369,30 +372,34 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
   };
   // who writes to pages that several hold, and the columns that ask for a page
   bool long_one = false, ahead = false;
-  auto asks_for = [&](int e) {
+  auto wrong = [&](int b, int detail) {
+    found(s, SPARKATTN_E_BAD_INDEX, detail);
+    atomicOr(s_wrong + b / 32, 1u << (b & 31));
+  };
+  auto asks_for = [&](int b, int e) {
     if ((uint32_t)e >= (uint32_t)v.pages) return true;
     const int holders = v.refs[e];
-    if (holders < 1) found(s, SPARKATTN_E_BAD_INDEX, e);
+    if (holders < 1) wrong(b, e);
     ahead |= holders > 1;
     return holders > 1;
   };
   for (int b = threadIdx.x; b < v.B; b += kBookThreads) {
     const Asks a = asks_of(p, b);
     int shared = -1;
-    if (!a.fine) found(s, SPARKATTN_E_BAD_INDEX, b);
+    if (!a.fine) wrong(b, b);
     const int32_t* row = v.table + (int64_t)b * v.max_pages;
     const int e = a.partly() ? row[a.tail] : 0;
     int missing = 0;
     if (a.last - a.first <= kOwnColumns) {
 #pragma unroll 8
-      for (int i = a.first; i < a.last; ++i) missing += asks_for(row[i]) ? 1 : 0;
+      for (int i = a.first; i < a.last; ++i) missing += asks_for(b, row[i]) ? 1 : 0;
     } else {
       long_one = true;
     }
     if (a.partly()) {
       const int holders = (uint32_t)e < (uint32_t)v.pages ? v.refs[e] : 0;
       if (holders < 1) {
-        found(s, SPARKATTN_E_BAD_INDEX, e);
+        wrong(b, e);
       } else if (holders > 1) {
         shared = e;
         const int at = slot_of(e, true);
@@ -422,7 +429,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
         int n = 0;
         for (long long i0 = s_first[b] + (long long)((warp - b) & (kBookWarps - 1)) * kCopyColumns; i0 < last; i0 += kBookWarps * kCopyColumns) {
 #pragma unroll
-          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(row[i0 + 32 * u + lane]) ? 1 : 0;
+          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(b, row[i0 + 32 * u + lane]) ? 1 : 0;
         }
         n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
         if (lane == 0) atomicAdd(&prefix[b], n);
@@ -501,6 +508,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
         if (later) p.list[at] = from;
         else atomicSub(v.refs_out + from, 1);
       }
+      if (p.kv_len_out != nullptr) p.kv_len_out[b] = (s_wrong[b / 32] >> (b & 31) & 1u) || (!enough && last > tail) ? -1 : p.kv_new[b];      // (last > tail: it asks)
       p.src[b] = from;
       p.dst[b] = to;
       if (tail < first) out[tail] = from >= 0 ? to : row[tail];
@@ -816,10 +824,10 @@ int launch_pages_trim(const sparkattn_book_t& book, const int32_t* kv_len, int f
   return launch_book(pages_trim_kernel, 1 + copiers, p.ranks, 0, stream, p);
 }
 
-int launch_pages_reserve(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* kv_new, int32_t* table_out, int32_t* refs_out, int32_t* src,
-                         int32_t* dst, void* workspace, cudaStream_t stream) {
+int launch_pages_reserve(const sparkattn_book_t& book, const int32_t* kv_len, const int32_t* kv_new, int32_t* kv_len_out, int32_t* table_out,
+                         int32_t* refs_out, int32_t* src, int32_t* dst, void* workspace, cudaStream_t stream) {
   int32_t* status = static_cast<int32_t*>(workspace);
-  ReserveParams p{make_book_view(book, table_out, refs_out), kv_len, kv_new, src, dst, status + kWorkspaceHeaderBytes / 4, 1, 64, status};
+  ReserveParams p{make_book_view(book, table_out, refs_out), kv_len, kv_new, kv_len_out, src, dst, status + kWorkspaceHeaderBytes / 4, 1, 64, status};
   const int sms = current_sm_count();
   if (sms < 1) return SPARKATTN_E_CUDA;
   while (p.slots < 2 * book.B) p.slots *= 2;

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2609_23153_b200 as sa
-from test_gpu_cache import DEV
+from test_gpu_cache import DEV, same_bits
 from test_gpu_pages import SIZES, Book, ints, make_book, on_device, same, workspace
 
 pytestmark = pytest.mark.gpu
@@ -228,3 +228,108 @@ def test_a_page_ahead_that_nobody_holds_is_reported(columns, at):
     assert got[0].tolist() == [[e if e >= 0 else next(free) for e in row]]
     sa.pages_reserve(ints([row]), ints([16]), ints([1] + [0] * (pages - 1)), ints([at * P]), P, workspace=ws)      # not asked for: not looked at
     assert sa.read_status(ws) == sa.OK
+
+
+def lengths_of_the_step(book, new, missing):
+    """... of a book whose numbers make sense."""
+    return [m if m == n or not missing else -1 for n, m in zip(book.len, new)]
+
+
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "-".join(str(x) for x in s))
+@pytest.mark.parametrize("seed", range(3))
+def test_lengths_for_the_step(size, seed):
+    rng = random.Random(300 + seed)
+    B, pages, page, columns, most = size
+    book = ahead_book(rng, size, 3)
+    new = [min(n + rng.choice((0, 1, page, 40 * page)[:seed + 2]), columns * page) for n in book.len]
+    if seed == 1:
+        book.refs = [max(r, 1) for r in book.refs]        # none is free
+    want = book.copy()
+    want.__class__ = Ahead
+    src, dst, missing = want.reserve(new)
+    for in_place in (False, True):
+        table, length, refs = on_device(book)
+        kv_len = torch.full((B,), 77, dtype=torch.int32, device=DEV)
+        there = dict(page_table_out=table, refs_out=refs) if in_place else {}
+        got = sa.pages_reserve(table, length, refs, ints(new), page, kv_len_out=kv_len, **there)
+        assert same(got[0], want.table) and same(got[1], want.refs) and same(got[2], src) and same(got[3], dst)
+        assert same(kv_len, lengths_of_the_step(book, new, missing))
+
+
+@pytest.mark.parametrize("columns", [5, 300])
+def test_a_sequence_that_has_not_got_its_pages_has_no_length(columns):
+    """By its own numbers, each in another way; the others have theirs."""
+    P, far = 16, 16 * columns
+    table = [[0] + [-1] * (columns - 1), [1] + [-1] * (columns - 1), [-1] * columns, [3] + [-1] * (columns - 1), [4, columns + 60] + [-1] * (columns - 2), [5] + [-1] * (columns - 1)]
+    refs = [1, 1, 0, 0, 1, 1] + [0] * (6 * columns + 200)
+    length, new = [16, 16, 10, 10, 16, 16], [far, 15, 12, 12, far, far + 1]
+    kv_len = ints([77] * 6)
+    ws = workspace(len(refs))
+    got = sa.pages_reserve(ints(table), ints(length), ints(refs), ints(new), P, kv_len_out=kv_len, workspace=ws)
+    assert sa.read_status(ws) == sa.E_BAD_INDEX
+    # fewer than there are; a partly filled page that is none, or nobody's; a page ahead that is nobody's; more than the table holds
+    assert kv_len.tolist() == [far, -1, -1, -1, -1, -1] and (got[0][0] >= 0).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new,G", [(1, 2), (5, 4), (40, 8)])
+def test_captured_step_whose_pages_do_not_suffice(fp8, new, G):
+    """Reserve, copy, append, attend and trim in one graph.  Two sequences share a partly filled page and the pool runs out: nothing that a page
+    holds changes, and the book stays; with pages given back the same graph goes on."""
+    P, H, d, B, columns = 16, 2, 64, 3, 12
+    need = -(-(20 + new) // P) - 2                        # further pages of each
+    pages = 2 + 4 + 2 * need                              # two shared, four of the third, and one too few for a copy and what is new
+    gen = torch.Generator(device=DEV).manual_seed(new)
+    cache = sa.alloc_cache(pages, H, P, d, fp8=fp8, device=DEV)
+    for x in cache:
+        if x is not None:
+            x.zero_() if x.element_size() != 4 else x.fill_(1.0)
+    rows = lambda n, h: torch.randn((n, h, d), generator=gen, device=DEV).bfloat16()
+    table, refs, lens = torch.full((2, columns), -1, dtype=torch.int32, device=DEV), torch.zeros(pages, dtype=torch.int32, device=DEV), ints([20, 64])
+    table, refs, _, _ = sa.pages_reserve(table, ints([0, 0]), refs, lens, P, check_status=True)
+    sa.cache_append(cache, rows(84, H), rows(84, H), table, lens, q_start=ints([0, 20, 84]), max_new=64, check_status=True)
+    table, lens, refs = sa.pages_fork(table, lens, refs, ints([0, 0, 1]), check_status=True)
+    want_new, kv_len, q_start = ints([20 + new, 20 + new, 64]), torch.empty_like(lens), ints([0, new, 2 * new, 2 * new])
+    src, dst = torch.empty_like(lens), torch.empty_like(lens)
+    k, v, q = rows(2 * new, H), rows(2 * new, H), rows(2 * new, H * G)
+    turned, out = torch.empty_like(q), torch.empty_like(q)
+    batch = dict(q_start=q_start, max_new=new)
+    ws = [torch.zeros(1 << 12, dtype=torch.uint8, device=DEV) for _ in range(4)] + [torch.zeros(1 << 28, dtype=torch.uint8, device=DEV)]
+
+    def step():
+        sa.pages_reserve(table, lens, refs, want_new, P, page_table_out=table, refs_out=refs, src=src, dst=dst, kv_len_out=kv_len, workspace=ws[0])
+        sa.cache_copy_pages(cache, src, dst, workspace=ws[1])
+        turned.copy_(q)
+        sa.cache_append(cache, k, v, table, kv_len, q=turned, q_out=turned, workspace=ws[2], **batch)
+        sa.cache_fwd(turned, cache, table, kv_len, out=out, workspace=ws[4], **batch)
+        sa.pages_trim(table, kv_len, refs, P, page_table_out=table, refs_out=refs, workspace=ws[3])
+
+    before = [x.clone() for x in (table, refs)] + [x.clone() for x in cache if x is not None]
+
+    def unchanged():
+        now = [table, refs] + [x for x in cache if x is not None]
+        return all(same_bits(x, y) for x, y in zip(now, before))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(2):
+        graph.replay()
+        assert [sa.read_status(w) for w in ws] == [sa.E_OUT_OF_PAGES, sa.OK, sa.E_BAD_INDEX, sa.E_BAD_INDEX, sa.E_BAD_INDEX]
+        assert kv_len.tolist() == [-1, -1, 64] and unchanged() and (out == 0).all()
+    # the third ends: there is room
+    t, _, r = sa.pages_fork(table, lens, refs, ints([0, 1, -1]), check_status=True)
+    table.copy_(t), refs.copy_(r), lens.copy_(ints([20, 20, 0])), want_new.copy_(ints([20 + new, 20 + new, 0]))
+    graph.replay()
+    assert [sa.read_status(w) for w in ws] == [sa.OK] * 5 and kv_len.tolist() == [20 + new, 20 + new, 0]
+    for x, y, s in ((cache.k, k, cache.k_scale), (cache.v, v, cache.v_scale)):
+        for b in range(2):
+            at = torch.arange(20, 20 + new, device=DEV)
+            pg = table[b][at // P].long()
+            got = x.view(torch.uint8)[pg, :, at % P].view(torch.float8_e4m3fn).double() * s[pg].double()[..., None] if fp8 else x[pg, :, at % P].double()
+            mine = y[b * new:(b + 1) * new].double()
+            # a code is off by half a step, 2^-4 of it, or 2^-10 scales among the smallest
+            assert ((got - mine).abs() <= (2.0 ** -4 * mine.abs() + (s[pg].double()[..., None] * 2.0 ** -10) if fp8 else torch.zeros_like(mine))).all()
+    assert (out != 0).any(-1).all()
