@@ -747,7 +747,7 @@ static int launch_chunk(const sparkattn_cache_t& c, CacheFwdParams& p, const voi
   auto kern = p.causal.sink > 0 ? cache_chunk_kernel<D, FP8, SPLIT, true> : cache_chunk_kernel<D, FP8, SPLIT, false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPARKATTN_E_CUDA;
   if ((rc = launch_kernel(kern, dim3(p.workers + 1), kChunkThreads, smem, true, stream, mk, mv, p)) != SPARKATTN_OK) return rc;
-  return launch_kernel(combine_rows_kernel<D, R>, dim3(p.workers - 1, 4), kCombineRowsThreads, 0, true, stream, p);
+  return launch_kernel(combine_rows_kernel<D, R>, dim3(p.workers - 1, kCombineRowsCtas), kCombineRowsThreads, 0, true, stream, p);
 }
 
 int launch_cache_chunk(const sparkattn_cache_t& c, int rows, CacheFwdParams& p, const void* k_cache, const void* v_cache, cudaStream_t stream) {

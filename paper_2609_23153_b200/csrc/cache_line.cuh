@@ -475,45 +475,67 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
   }
 }
 
-// The same for items of 128 rows and more: CTA (w, y) takes runs y, y + gridDim.y, ... of 32 rows.  A lane has a row and a warp every eighth group of four
-// channels, as the parts lie in memory (what a softmax thread has of its row in registers goes there a line at a time); rows of the
-// output come together in shared memory.
-constexpr int kCombineRowsThreads = 256;
+// The same for items of 128 rows and more.  A lane has a row and a warp two groups of four channels, as the parts lie in memory (what a softmax
+// thread has of its row in registers goes there a line at a time); rows of the output come together in shared memory.
+// Pieces are 32 rows by 64 channels, dealt out to the CTAs of all of an item's borders, gridDim.y each, so that an item of many parts has many CTAs; two parts (64
+// channels: three) are on their way at a time, and the code is one loop without a remainder, since it comes from memory at every call: five tokens of 8 heads of one
+// sequence of 131,072 keys, 148 parts, 57 us (whole rows by the first border's four CTAs 78; three or four parts at a time 53 and 51), five of 64
+// heads of 8 sequences, 3 parts, 69 (70; 69 and 69), a prompt of 5000 tokens of 4 heads 53 (54; 54 and 55); 64 channels, five of 32
+// heads over two of 131,072 keys, bf16, 38 by three and 42 by two, three pieces of 2000 tokens through a window 46 and 45.
+constexpr int kCombineRowsThreads = 256, kCombineRowsCtas = 6;
 template <int D, int R>
 __global__ void __launch_bounds__(kCombineRowsThreads, 4)
 combine_rows_kernel(const __grid_constant__ CacheFwdParams p) {
-  constexpr int kWarps = kCombineRowsThreads / 32, kGroups = D / 4 / kWarps, kPitch = D + 8;
+  constexpr int kWarps = kCombineRowsThreads / 32, kGroups = 2, kAtOnce = D == 64 ? 3 : 2, kPieces = D / 4 / (kWarps * kGroups), kPitch = kWarps * kGroups * 4 + 8;
   __shared__ __align__(16) __nv_bfloat16 s_out[32 * kPitch];
+  __shared__ float s_top[kWarps][32];
   pdl_wait();
   const int4 b0 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[0], b1 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[1];
-  const int before = b0.x, units = b0.y, share = b0.z, token0 = b0.w, row0 = b1.x, rows = b1.y, h = b1.z;
-  if (before == 0 || before > share) return;
-  const int w0 = blockIdx.x, parts = 1 + (units - before + share - 1) / share;
+  const int units = b0.y, share = b0.z, token0 = b0.w, row0 = b1.x, rows = b1.y, h = b1.z;
+  if (b0.x == 0) return;
+  const int border = (b0.x - 1) / share, before = b0.x - border * share;         // which of the item's this is; units in front of the first one
+  const int w0 = (int)blockIdx.x - border, parts = 1 + (units - before + share - 1) / share;
   auto slot_of = [&](int i) { return 2 * (w0 + i) + (i > 0 || before == share ? 0 : 1); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll 1
-  for (int r0 = blockIdx.y * 32; r0 < rows; r0 += gridDim.y * 32) {
+  for (int piece = border * (int)gridDim.y + (int)blockIdx.y; piece < (rows + 31) / 32 * kPieces; piece += (parts - 1) * (int)gridDim.y) {
+    const int r0 = piece / kPieces * 32, g0 = piece % kPieces * (kWarps * kGroups);         // first row, first group of four channels
     const int r = r0 + lane;      // (rows behind the item's last are parts' rows all the same, of no meaning)
     float top = -INFINITY;
 #pragma unroll 4
-    for (int i = 0; i < parts; ++i) top = fmaxf(top, p.part_ml[((int64_t)slot_of(i) * R + r) * 2]);
+    for (int i = warp; i < parts; i += kWarps) top = fmaxf(top, p.part_ml[((int64_t)slot_of(i) * R + r) * 2]);
+    s_top[warp][lane] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, s_top[i][lane]);
     // (items of fewer than 16 rows: every n-th part by itself, then the sums of these, the order that calls of many sequences with few rows have had)
     const int split = rows >= 16 ? 1 : 16 / rows;
     auto add_up = [&](int k, float& sum, float (&acc)[kGroups][4]) {
-#pragma unroll 2
-      for (int i = k; i < parts; i += split) {
-        const int slot = slot_of(i);
-        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((int64_t)slot * R + r) * 2);
-        float4 v[kGroups];
+#pragma unroll 1
+      for (int i0 = k; i0 < parts; i0 += kAtOnce * split) {
+        float2 ml[kAtOnce];
+        float4 v[kAtOnce][kGroups];
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) v[g] = *reinterpret_cast<const float4*>(p.part_o + (((int64_t)slot * (D / 4) + warp + g * kWarps) * R + r) * 4);
-        const float f = top == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
-        sum = fmaf(ml.y, f, sum);
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int i = i0 + u * split, slot = slot_of(i);
+          ml[u] = make_float2(-INFINITY, 0.0f);      // (adds nothing)
+          if (i < parts) ml[u] = *reinterpret_cast<const float2*>(p.part_ml + ((int64_t)slot * R + r) * 2);
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          const float x[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
+          for (int g = 0; g < kGroups; ++g) {
+            v[u][g] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (i < parts) v[u][g] = *reinterpret_cast<const float4*>(p.part_o + (((int64_t)slot * (D / 4) + g0 + warp + g * kWarps) * R + r) * 4);
+          }
+        }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[g][j] = ml.x == -INFINITY ? acc[g][j] : fmaf(x[j], f, acc[g][j]);      // (a part without keys has left no output)
+        for (int u = 0; u < kAtOnce; ++u) {
+          const float f = top == -INFINITY ? 0.0f : fast_exp2(ml[u].x - top);
+          sum = fmaf(ml[u].y, f, sum);
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            const float x[4] = {v[u][g].x, v[u][g].y, v[u][g].z, v[u][g].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[g][j] = ml[u].x == -INFINITY ? acc[g][j] : fmaf(x[j], f, acc[g][j]);      // (a part without keys has left no output)
+          }
         }
       }
     };
@@ -535,18 +557,18 @@ combine_rows_kernel(const __grid_constant__ CacheFwdParams p) {
       const __nv_bfloat162 a = __floats2bfloat162_rn(acc[g][0] * inv, acc[g][1] * inv), b = __floats2bfloat162_rn(acc[g][2] * inv, acc[g][3] * inv);
       *reinterpret_cast<uint2*>(s_out + lane * kPitch + (warp + g * kWarps) * 4) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
     }
-    if (p.lse && warp == 0 && r < rows) {
+    if (p.lse && g0 == 0 && warp == 0 && r < rows) {
       const int row = row0 + r, of = fast_div(row, p.by_G);
       p.lse[(int64_t)(token0 + of) * p.H + h * p.G + row - of * p.G] = sum == 0.0f ? -INFINITY : (top - kBase + log2f(sum)) * 0.6931471805599453f;
     }
     __syncthreads();
-    constexpr int kLanes = D / 8;      // 16 bytes each
+    constexpr int kLanes = kGroups * kWarps / 2;      // 16 bytes each
 #pragma unroll 1
     for (int i = threadIdx.x; i < 32 * kLanes; i += kCombineRowsThreads) {
       const int mine = i / kLanes, c = i % kLanes;
       if (r0 + mine >= rows) continue;
       const int row = row0 + r0 + mine, of = fast_div(row, p.by_G);
-      *reinterpret_cast<uint4*>(p.out + (int64_t)(token0 + of) * p.out_stride_t + (h * p.G + row - of * p.G) * p.out_stride_h + c * 8) =
+      *reinterpret_cast<uint4*>(p.out + (int64_t)(token0 + of) * p.out_stride_t + (h * p.G + row - of * p.G) * p.out_stride_h + g0 * 4 + c * 8) =
           *reinterpret_cast<const uint4*>(s_out + mine * kPitch + c * 8);
     }
     __syncthreads();
