@@ -407,12 +407,13 @@ __device__ __forceinline__ void note_border(const CacheFwdParams& p, int worker,
 }
 
 // Adds up what several stretches have left of an item, in the order of the line.  CTA w looks at the border in front of stretch
-// w + 1 and does the item if that is the first border inside it; gridDim.y CTAs share its rows.  A warp takes a row, or, of an item
-// of few rows, every n-th part of a row, since what this kernel spends is the time of a few loads one after the other.
+// w + 1 and does the item if that is the first border inside it.  A warp takes a row, or, of an item of few rows,
+// every n-th part of a row, since what this kernel spends is the time of a few loads one after the other.
 constexpr int kCombineThreads = 512;
 template <int D, int R>
 __global__ void __launch_bounds__(kCombineThreads)
 combine_kernel(const __grid_constant__ CacheFwdParams p) {
+  static_assert(R < 128, "parts of 128 rows and more lie in another order");
   constexpr int kVec = D / 32, kWarps = kCombineThreads / 32;
   __shared__ float s_acc[kWarps][D + 2];
   pdl_wait();
@@ -425,7 +426,7 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int split = rows >= kWarps ? 1 : kWarps / rows;           // warps of a row
   const int share_of_row = warp % split;
-  for (int r = blockIdx.y * (kWarps / split) + warp / split; r - warp / split < rows; r += gridDim.y * (kWarps / split)) {
+  for (int r = warp / split; r - warp / split < rows; r += kWarps / split) {
     const bool there = r < rows && warp / split < kWarps / split;
     float top = -INFINITY, sum = 0.0f, acc[kVec] = {};
     if (there) {
