@@ -70,8 +70,9 @@ __device__ __forceinline__ bool sees(const Causal& c, int2 seen, int key) {
 
 // One CTA looks through the numbers a call was given and leaves the status word: nobody else writes it but a wait that has run
 // out, seconds later, so that nothing has to be cleared in front.  reach: pages of the sequence that the call reaches, from the
-// first to behind the last; and those of the first `sink` tokens.
-template <typename Reach>
+// first to behind the last; SINK: and those of the first `sink` tokens.  (This CTA is what a call of hundreds of short sequences waits for, or one of long tables
+// of small pages: with the first tokens' places worked out in calls that have none, a token of each of 4000 sequences of 50 took 161 us instead of 143.)
+template <bool SINK, typename Reach>
 __device__ __forceinline__ void check_batch(const BatchView& v, int* s_bad /* [2], shared */, Reach reach, int sink = 0) {
   if (threadIdx.x == 0) { s_bad[0] = 0; s_bad[1] = 0; }
   __syncthreads();
@@ -94,13 +95,13 @@ __device__ __forceinline__ void check_batch(const BatchView& v, int* s_bad /* [2
     const int32_t* row = v.page_table + (int64_t)b * v.max_pages;
     const int last = min(pages.y, v.max_pages);
     // (the first tokens' pages stand in front of the others, `gap` pages nearer to them than they are)
-    const int front = sink > 0 ? min(((sink - 1) >> v.page_shift) + 1, pages.x) : 0, gap = pages.x - front;
+    const int front = SINK ? min(((sink - 1) >> v.page_shift) + 1, pages.x) : 0, gap = pages.x - front;
     for (int i = pages.x - front + lane; i < last; i += lanes * 8) {
       int page[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int at = i + lanes * u;
-        page[u] = at < last ? row[at < pages.x ? at - gap : at] : 0;
+        page[u] = at < last ? row[SINK && at < pages.x ? at - gap : at] : 0;
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)

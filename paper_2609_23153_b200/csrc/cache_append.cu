@@ -304,7 +304,7 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
   pdl_wait();
   if (blockIdx.x == 0) {
     const int shift = p.batch.page_shift;
-    check_batch(p.batch, s_bad, [&](const Sequence& s) { return make_int2(max(s.first_pos(), 0) >> shift, s.n == 0 ? 0 : (s.len + (1 << shift) - 1) >> shift); });
+    check_batch<false>(p.batch, s_bad, [&](const Sequence& s) { return make_int2(max(s.first_pos(), 0) >> shift, s.n == 0 ? 0 : (s.len + (1 << shift) - 1) >> shift); });
     if (p.rotary.rot > 0) {
       const RotaryView& r = p.rotary;
       auto bad = [&](int detail) { if (atomicExch(s_bad, 1) == 0) s_bad[1] = detail; };

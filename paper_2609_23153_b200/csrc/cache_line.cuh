@@ -391,11 +391,11 @@ __device__ __forceinline__ uint32_t mark_word(const CacheFwdParams& p, const Mar
 // the status of a call: the first CTA's work
 template <bool SINK>
 __device__ __forceinline__ void check_call(const CacheFwdParams& p, int* s_bad) {
-  check_batch(p.batch, s_bad, [&](const Sequence& s) {
+  check_batch<SINK>(p.batch, s_bad, [&](const Sequence& s) {
     if (s.n == 0) return make_int2(0, 0);
     const int lo = visible_keys(p.causal, s.first_pos(), s.len).x, hi = visible_keys(p.causal, s.len - 1, s.len).y;
     return make_int2(lo >> p.batch.page_shift, (hi + (1 << p.batch.page_shift) - 1) >> p.batch.page_shift);
-  }, SINK ? p.causal.sink : 0);
+  }, p.causal.sink);
   leave_status(p.status, s_bad);
 }
 template <int R, int TK, int OVER, bool SINK>
