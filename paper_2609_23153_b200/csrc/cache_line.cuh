@@ -478,16 +478,15 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
 
 // The same for items of 128 rows and more.  A lane has a row and a warp two groups of four channels, as the parts lie in memory (what a softmax
 // thread has of its row in registers goes there a line at a time); rows of the output come together in shared memory.
-// Pieces are 32 rows by 64 channels, dealt out to the CTAs of all of an item's borders, gridDim.y each, so that an item of many parts has many CTAs; two parts (64
-// channels: three) are on their way at a time, and the code is one loop without a remainder, since it comes from memory at every call: five tokens of 8 heads of one
-// sequence of 131,072 keys, 148 parts, 57 us (whole rows by the first border's four CTAs 78; three or four parts at a time 53 and 51), five of 64
-// heads of 8 sequences, 3 parts, 69 (70; 69 and 69), a prompt of 5000 tokens of 4 heads 53 (54; 54 and 55); 64 channels, five of 32
-// heads over two of 131,072 keys, bf16, 38 by three and 42 by two, three pieces of 2000 tokens through a window 46 and 45.
+// Pieces are 32 rows by 64 channels, dealt out to the CTAs of all of an item's borders, gridDim.y each, so that an item of many parts has many CTAs; three parts are
+// on their way at a time, and the code is one loop without a remainder, since it comes from memory at every call.  Five tokens of 8 heads of one sequence of
+// 131,072 keys, 148 parts: 53 us (whole rows by the first border's four CTAs 78; two or four parts at a time 57 and 51); five of 64 heads of 8 sequences,
+// 3 parts: 69 (70; 69 and 69); 52 of 8 heads over 2 of 6 sequences of up to 26,175, bf16: 40 (57; 41 and 40); a prompt of 5000 tokens of 4 heads 54 (54; 53 and 55).
 constexpr int kCombineRowsThreads = 256, kCombineRowsCtas = 6;
 template <int D, int R>
 __global__ void __launch_bounds__(kCombineRowsThreads, 4)
 combine_rows_kernel(const __grid_constant__ CacheFwdParams p) {
-  constexpr int kWarps = kCombineRowsThreads / 32, kGroups = 2, kAtOnce = D == 64 ? 3 : 2, kPieces = D / 4 / (kWarps * kGroups), kPitch = kWarps * kGroups * 4 + 8;
+  constexpr int kWarps = kCombineRowsThreads / 32, kGroups = 2, kAtOnce = 3, kPieces = D / 4 / (kWarps * kGroups), kPitch = kWarps * kGroups * 4 + 8;
   __shared__ __align__(16) __nv_bfloat16 s_out[32 * kPitch];
   __shared__ float s_top[kWarps][32];
   pdl_wait();
