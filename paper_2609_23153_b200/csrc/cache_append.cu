@@ -310,8 +310,8 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
       auto bad = [&](int detail) { if (atomicExch(s_bad, 1) == 0) s_bad[1] = detail; };
       if (r.positions) {
         // sixteen bytes at a time where they lie so: 105 sequences of up to 2784 tokens, three axes, 10 + 2 x 2 heads of 64 channels take 110 us, which number by
-        // number waited for this CTA, 200
-        const long long n = (long long)p.batch.T * r.axes, quads = reinterpret_cast<uintptr_t>(r.positions) % 16 == 0 ? n / 4 : 0;
+        // number waited for this CTA, 200.  (Those of one round of the other loop by that: a token of each of 100 sequences 3.9 us, and 4.8 by both loops.)
+        const long long n = (long long)p.batch.T * r.axes, quads = n > 8 * kThreads && reinterpret_cast<uintptr_t>(r.positions) % 16 == 0 ? n / 4 : 0;
 #pragma unroll 1
         for (long long first = threadIdx.x; first < quads; first += 8 * kThreads) {
           int4 at[8];
