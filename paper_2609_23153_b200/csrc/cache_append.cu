@@ -310,8 +310,8 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
       auto bad = [&](int detail) { if (atomicExch(s_bad, 1) == 0) s_bad[1] = detail; };
       if (r.positions) {
         // sixteen bytes at a time where they lie so: 105 sequences of up to 2784 tokens, three axes, 10 + 2 x 2 heads of 64 channels take 110 us, which number by
-        // number waited for this CTA, 200.  (Those of one round of the other loop by that: a token of each of 100 sequences 3.9 us, and 4.8 by both loops.)
-        const long long n = (long long)p.batch.T * r.axes, quads = n > 8 * kThreads && reinterpret_cast<uintptr_t>(r.positions) % 16 == 0 ? n / 4 : 0;
+        // number waited for this CTA, 200.  (A few rounds of the other loop by that: a token of each of 100 sequences 3.9 us, and 4.8 by both loops.)
+        const long long n = (long long)p.batch.T * r.axes, quads = n > 32 * kThreads && reinterpret_cast<uintptr_t>(r.positions) % 16 == 0 ? n / 4 : 0;
 #pragma unroll 1
         for (long long first = threadIdx.x; first < quads; first += 8 * kThreads) {
           int4 at[8];
@@ -371,11 +371,21 @@ static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream)
     p.lines = 2 * p.Hk + (p.q.data ? p.H : 0);
     // One wave of CTAs where that leaves a unit at most sixteen lines, else units of eight
     const long long parts = (long long)p.batch.B * p.pages_each, slots = (long long)per * decltype(shape)::per_sm(FP8, NORM) * current_sm_count();
-    // (a sequence reaches one page less than it could if its first new token begins one or its pieces are shorter: most do.  Three frames of 1560 tokens
-    // by eight units a page instead of seven: 20.6 -> 19.1 us.)
-    const long long likely = parts - (p.pages_each > 1 ? p.batch.B : 0);
-    p.groups = (int)std::min<long long>(std::max<long long>(slots / std::max<long long>(likely, 1), 1), p.lines);
-    if (p.lines > 16 * p.groups) p.groups = (p.lines + 7) / 8;
+    auto groups_for = [&](long long wave, long long pages) { return (int)std::min<long long>(std::max<long long>(wave / pages, 1), p.lines); };
+    auto lines_of = [&](int groups) { return (p.lines + groups - 1) / groups; };
+    p.groups = groups_for(slots, parts);
+    if (p.lines > 16 * p.groups) {
+      p.groups = (p.lines + 7) / 8;
+    } else {
+      // ... or a wave of the pages that T new tokens reach on average, wherever in a page they begin, and a little more, where that leaves a unit fewer lines.
+      // Three frames of 1560 tokens by eight units a page instead of seven 19.5 us for 20.9, and 20.3 for 21.0 where they reach a page more; 16 sequences of up to
+      // 400 tokens over pages of 128, 64 channels, 17.4 and 25.0.  The CTAs of pages that are not reached cost what they take to begin, so units of few lines or of four
+      // tokens have to get half as many by a third more CTAs at most: 34 sequences of up to 84 tokens, ten lines, 6.3 us otherwise and 5.7, two tokens
+      // of each of 186, 48 lines, 7.3 and 5.8.  (By one page of every sequence less than it could reach: 256 tokens of each of 8 over pages of 128 17.0 instead of 12.4.)
+      const int g = groups_for(slots + slots / 32, p.batch.B + (p.batch.T - p.batch.B + (1 << p.batch.page_shift) - 1) / (1 << p.batch.page_shift));
+      const int before = lines_of(p.groups), after = lines_of(g);
+      if (before >= 4 && rows > 4 ? after < before : 2 * after <= before && 3 * parts * g <= 4 * slots) p.groups = g;
+    }
     const long long units = parts * p.groups;
     if (units > 0x7fffff00LL) return (int)SPARKATTN_E_UNSUPPORTED_SHAPE;
     p.units = (int)units;
