@@ -481,7 +481,7 @@ combine_kernel(const __grid_constant__ CacheFwdParams p) {
 // Pieces are 32 rows by 64 channels, dealt out to the CTAs of all of an item's borders, gridDim.y each, so that an item of many parts has many CTAs; three parts are
 // on their way at a time, and the code is one loop without a remainder, since it comes from memory at every call.  Five tokens of 8 heads of one sequence of
 // 131,072 keys, 148 parts: 53 us (whole rows by the first border's four CTAs 78; two or four parts at a time 57 and 51); five of 64 heads of 8 sequences,
-// 3 parts: 69 (70; 69 and 69); 52 of 8 heads over 2 of 6 sequences of up to 26,175, bf16: 40 (57; 41 and 40); a prompt of 5000 tokens of 4 heads 54 (54; 53 and 55).
+// 3 parts: 68 (70; 69 and 69); 52 of 8 heads over 2 of 6 sequences of up to 26,175, bf16: 40 (57; 41 and 40); a prompt of 5000 tokens of 4 heads 54 (54; 53 and 55).
 constexpr int kCombineRowsThreads = 256, kCombineRowsCtas = 6;
 template <int D, int R>
 __global__ void __launch_bounds__(kCombineRowsThreads, 4)
@@ -493,23 +493,26 @@ combine_rows_kernel(const __grid_constant__ CacheFwdParams p) {
   const int4 b0 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[0], b1 = reinterpret_cast<const int4*>(p.borders + blockIdx.x + 1)[1];
   const int units = b0.y, share = b0.z, token0 = b0.w, row0 = b1.x, rows = b1.y, h = b1.z;
   if (b0.x == 0) return;
-  const int border = (b0.x - 1) / share, before = b0.x - border * share;         // which of the item's this is; units in front of the first one
+  const int border = b0.x > share ? (b0.x - 1) / share : 0, before = b0.x - border * share;         // which of the item's this is; units in front of the first one
   const int w0 = (int)blockIdx.x - border, parts = 1 + (units - before + share - 1) / share;
   auto slot_of = [&](int i) { return 2 * (w0 + i) + (i > 0 || before == share ? 0 : 1); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (items of fewer than 16 rows: every n-th part by itself, then the sums of these, the order that calls of many sequences with few rows have had)
+  const int split = rows >= 16 ? 1 : 16 / rows;
+  const bool few = split == 1 && parts <= kAtOnce;      // all on their way at once: what the largest is shows from them
 #pragma unroll 1
   for (int piece = border * (int)gridDim.y + (int)blockIdx.y; piece < (rows + 31) / 32 * kPieces; piece += (parts - 1) * (int)gridDim.y) {
     const int r0 = piece / kPieces * 32, g0 = piece % kPieces * (kWarps * kGroups);         // first row, first group of four channels
     const int r = r0 + lane;      // (rows behind the item's last are parts' rows all the same, of no meaning)
     float top = -INFINITY;
+    if (!few) {
 #pragma unroll 4
-    for (int i = warp; i < parts; i += kWarps) top = fmaxf(top, p.part_ml[((int64_t)slot_of(i) * R + r) * 2]);
-    s_top[warp][lane] = top;
-    __syncthreads();
+      for (int i = warp; i < parts; i += kWarps) top = fmaxf(top, p.part_ml[((int64_t)slot_of(i) * R + r) * 2]);
+      s_top[warp][lane] = top;
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) top = fmaxf(top, s_top[i][lane]);
-    // (items of fewer than 16 rows: every n-th part by itself, then the sums of these, the order that calls of many sequences with few rows have had)
-    const int split = rows >= 16 ? 1 : 16 / rows;
+      for (int i = 0; i < kWarps; ++i) top = fmaxf(top, s_top[i][lane]);
+    }
     auto add_up = [&](int k, float& sum, float (&acc)[kGroups][4]) {
 #pragma unroll 1
       for (int i0 = k; i0 < parts; i0 += kAtOnce * split) {
@@ -525,6 +528,10 @@ combine_rows_kernel(const __grid_constant__ CacheFwdParams p) {
             v[u][g] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (i < parts) v[u][g] = *reinterpret_cast<const float4*>(p.part_o + (((int64_t)slot * (D / 4) + g0 + warp + g * kWarps) * R + r) * 4);
           }
+        }
+        if (few) {
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) top = fmaxf(top, ml[u].x);
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
