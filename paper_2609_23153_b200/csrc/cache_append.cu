@@ -39,10 +39,11 @@ struct AppendParams {
   int64_t stride_page, stride_h, stride_n;
   int H, Hk;
   int pages_each;                // pages of a sequence that max_new tokens can reach
-  FastDiv by_pages_each, by_groups;
+  FastDiv by_pages_each, by_groups, by_B;
   int lines;                     // of a (sequence, page): K and V of every key head, then the queries
   int groups;                    // units that share them: unit g takes lines g, g + groups, ...
   int units;
+  int budget;                    // more than 0: units of a sequence, shared by the one or two pages that it reaches (see its_share)
   int32_t* status;
 };
 
@@ -116,11 +117,9 @@ struct Part {
   int page, held;              // the page, -1: nothing to do; tokens there before
   int rows, t0, pos0;          // new tokens; row of the call and position of the first
 };
-__device__ __forceinline__ Part part_of(const AppendParams& p, int bj) {
+__device__ __forceinline__ Part part_of(const AppendParams& p, int b, int j, const Sequence& s) {
   Part u{-1, 0, 0, 0, 0};
-  const int b = fast_div(bj, p.by_pages_each);
-  const Sequence s = sequence_of(p.batch, b);
-  const int first = max(s.first_pos(), 0), number = (first >> p.batch.page_shift) + bj - b * p.pages_each;
+  const int first = max(s.first_pos(), 0), number = (first >> p.batch.page_shift) + j;
   u.pos0 = max(number << p.batch.page_shift, first);
   u.rows = min((number + 1) << p.batch.page_shift, s.len) - u.pos0;
   if (u.rows <= 0 || number >= p.batch.max_pages) { u.rows = 0; return u; }
@@ -129,6 +128,20 @@ __device__ __forceinline__ Part part_of(const AppendParams& p, int bj) {
   u.page = p.batch.page_table[(int64_t)b * p.batch.max_pages + number];
   if ((uint32_t)u.page >= (uint32_t)p.batch.pages) u.page = -1;
   return u;
+}
+
+// Which page of its sequence a unit takes, and of its lines every groups-th from `first` on.
+struct Share {
+  int j, first, groups;
+};
+// Where sequences reach two pages at most, by where they begin in one, each has its units for those that it does reach.  108 tokens of each of 4 from the
+// first on, pages of 128, 32 + 2 x 8 heads: 5.5 us, with units for two pages of each 7.7; 60 of each of 20 that reach two, pages of 64, 8 + 2 x 8 heads: 9.6
+// and 10.4, where all units for one page of each take 13.7.
+__device__ __forceinline__ Share its_share(const AppendParams& p, int unit, const Sequence& s) {
+  const int first = max(s.first_pos(), 0);
+  const bool two = s.len > first && (s.len - 1) >> p.batch.page_shift > first >> p.batch.page_shift;
+  const int groups = min(max(two ? p.budget / 2 : p.budget, 1), p.lines), j = unit >= groups;
+  return {j + (unit >= 2 * groups), unit - j * groups, groups};
 }
 
 template <int D, int ROWS>
@@ -350,8 +363,12 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
   const int group = __shfl_sync(0xffffffffu, (int)threadIdx.x / U, 0);
   const int unit = (int)(blockIdx.x - 1) * (kThreads / U) + group;
   if (unit >= p.units) return;
-  const int bj = fast_div(unit, p.by_groups), first = unit - bj * p.groups;
-  const Part u = part_of(p, bj);
+  // (the sequences' first units, then their second ones and so on: those of less to do come last, and the SMs have as many of them each)
+  const bool budget = U > 32 && p.budget > 0;
+  const int of = fast_div(unit, budget ? p.by_B : p.by_groups), b = budget ? unit - of * p.batch.B : fast_div(of, p.by_pages_each);
+  const Sequence s = sequence_of(p.batch, b);
+  const Share share = budget ? its_share(p, of, s) : Share{of - b * p.pages_each, unit - of * p.groups, p.groups};
+  const Part u = part_of(p, b, share.j, s);
   if (u.rows <= 0) return;
   float* s_cos = reinterpret_cast<float*>(s_raw + UnitShape<D, ROWS>::kRowBytes) + group * ROWS * p.rotary.rot;
   float* s_sin = s_cos + ROWS * (p.rotary.rot / 2);
@@ -360,7 +377,7 @@ cache_append_kernel(const __grid_constant__ AppendParams p) {
     if constexpr (U > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(U) : "memory");
     else __syncwarp();
   }
-  append_lines<D, FP8, ROWS, NORM>(p, u, first, p.groups, group, s_max, s_cos, s_sin);
+  append_lines<D, FP8, ROWS, NORM>(p, u, share.first, share.groups, group, s_max, s_cos, s_sin);
 }
 
 template <int D, bool FP8, bool NORM>
@@ -376,21 +393,24 @@ static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream)
     p.groups = groups_for(slots, parts);
     if (p.lines > 16 * p.groups) {
       p.groups = (p.lines + 7) / 8;
+    } else if (rows > 4 && p.pages_each == 2 && slots >= 4 * parts) {
+      p.budget = (int)std::min(slots / p.batch.B, 2LL * p.lines);
     } else {
       // ... or a wave of the pages that T new tokens reach on average, wherever in a page they begin, and a little more, where that leaves a unit fewer lines.
       // Three frames of 1560 tokens by eight units a page instead of seven 19.5 us for 20.9, and 20.3 for 21.0 where they reach a page more; 16 sequences of up to
       // 400 tokens over pages of 128, 64 channels, 17.4 and 25.0.  The CTAs of pages that are not reached cost what they take to begin, so units of few lines or of four
-      // tokens have to get half as many by a third more CTAs at most: 34 sequences of up to 84 tokens, ten lines, 6.3 us otherwise and 5.7, two tokens
-      // of each of 186, 48 lines, 7.3 and 5.8.  (By one page of every sequence less than it could reach: 256 tokens of each of 8 over pages of 128 17.0 instead of 12.4.)
+      // tokens have to get half as many by a third more CTAs at most: two tokens of each of 186, 48 lines, 7.3 us
+      // otherwise and 5.8.  (By one page of every sequence less than it could reach: 256 tokens of each of 8 over pages of 128 17.0 instead of 12.4.)
       const int g = groups_for(slots + slots / 32, p.batch.B + (p.batch.T - p.batch.B + (1 << p.batch.page_shift) - 1) / (1 << p.batch.page_shift));
       const int before = lines_of(p.groups), after = lines_of(g);
       if (before >= 4 && rows > 4 ? after < before : 2 * after <= before && 3 * parts * g <= 4 * slots) p.groups = g;
     }
-    const long long units = parts * p.groups;
+    const long long units = p.budget > 0 ? (long long)p.budget * p.batch.B : parts * p.groups;
     if (units > 0x7fffff00LL) return (int)SPARKATTN_E_UNSUPPORTED_SHAPE;
     p.units = (int)units;
     p.by_pages_each = make_fast_div(p.pages_each);
     p.by_groups = make_fast_div(p.groups);
+    p.by_B = make_fast_div(p.batch.B);
     const unsigned ctas = 1 + (unsigned)((units + per - 1) / per);
     const size_t smem = decltype(shape)::smem(p.rotary.rot);
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)decltype(shape)::smem(D)) != cudaSuccess) return (int)SPARKATTN_E_CUDA;
