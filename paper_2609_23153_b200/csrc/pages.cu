@@ -376,8 +376,9 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     found(s, SPARKATTN_E_BAD_INDEX, detail);
     atomicOr(s_wrong + b / 32, 1u << (b & 31));
   };
-  auto asks_for = [&](int b, int e) {
-    if ((uint32_t)e >= (uint32_t)v.pages) return true;
+  // a page ahead that others hold as well
+  auto shared_ahead = [&](int b, int e) {
+    if ((uint32_t)e >= (uint32_t)v.pages) return false;
     const int holders = v.refs[e];
     if (holders < 1) wrong(b, e);
     ahead |= holders > 1;
@@ -391,8 +392,18 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     const int e = a.partly() ? row[a.tail] : 0;
     int missing = 0;
     if (a.last - a.first <= kOwnColumns) {
-#pragma unroll 8
-      for (int i = a.first; i < a.last; ++i) missing += asks_for(b, row[i]) ? 1 : 0;
+      // (eight on their way at a time; mostly none of them is a page)
+      for (int i0 = a.first; i0 < a.last; i0 += 8) {
+        int e8[8], pages = 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) e8[u] = i0 + u < a.last ? row[i0 + u] : -1;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) pages += (uint32_t)e8[u] < (uint32_t)v.pages ? 1 : 0;
+        missing += min(8, a.last - i0) - pages;
+        if (pages == 0) continue;
+#pragma unroll 1
+        for (int i = i0; i < min(i0 + 8, a.last); ++i) missing += shared_ahead(b, row[i]) ? 1 : 0;
+      }
     } else {
       long_one = true;
     }
@@ -428,8 +439,18 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
         const int32_t* row = v.table + (int64_t)b * v.max_pages;
         int n = 0;
         for (long long i0 = s_first[b] + (long long)((warp - b) & (kBookWarps - 1)) * kCopyColumns; i0 < last; i0 += kBookWarps * kCopyColumns) {
+          int e[kCopyColumns / 32], pages = 0;
 #pragma unroll
-          for (int u = 0; u < kCopyColumns / 32; ++u) n += i0 + 32 * u + lane < last && asks_for(b, row[i0 + 32 * u + lane]) ? 1 : 0;
+          for (int u = 0; u < kCopyColumns / 32; ++u) e[u] = i0 + 32 * u + lane < last ? row[i0 + 32 * u + lane] : -1;
+#pragma unroll
+          for (int u = 0; u < kCopyColumns / 32; ++u) {
+            const bool is = (uint32_t)e[u] < (uint32_t)v.pages;
+            pages += is ? 1 : 0;
+            n += i0 + 32 * u + lane < last && !is ? 1 : 0;
+          }
+          if (pages == 0) continue;
+#pragma unroll 1
+          for (long long i = i0 + lane; i < min(i0 + kCopyColumns, (long long)last); i += 32) n += shared_ahead(b, row[i]) ? 1 : 0;
         }
         n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
         if (lane == 0) atomicAdd(&prefix[b], n);
