@@ -43,7 +43,7 @@ struct AppendParams {
   int lines;                     // of a (sequence, page): K and V of every key head, then the queries
   int groups;                    // units that share them: unit g takes lines g, g + groups, ...
   int units;
-  int budget;                    // more than 0: units of a sequence, shared by the one or two pages that it reaches (see its_share)
+  int budget, one;               // budget more than 0: units of a sequence, by whether it reaches one page, of `one` units, or two, of `groups` each (see its_share)
   int32_t* status;
 };
 
@@ -134,13 +134,13 @@ __device__ __forceinline__ Part part_of(const AppendParams& p, int b, int j, con
 struct Share {
   int j, first, groups;
 };
-// Where sequences reach two pages at most, by where they begin in one, each has its units for those that it does reach.  108 tokens of each of 4 from the
-// first on, pages of 128, 32 + 2 x 8 heads: 5.5 us, with units for two pages of each 7.7; 60 of each of 20 that reach two, pages of 64, 8 + 2 x 8 heads: 9.6
-// and 10.4, where all units for one page of each take 13.7.
+// Where sequences reach two pages at most, by where they begin in one, each has its units for those that it does reach.  From the first token on: 108 tokens of
+// each of 4, pages of 128, 32 + 2 x 8 heads, 5.5 us, with units for two pages of each 7.7; up to 120 of each of 60, 8 + 2 x 8, bf16, 14.3 and 18.6.  From anywhere:
+// 60 of each of 20, pages of 64, 8 + 2 x 8 heads, 9.4 and 10.4, where units for one page of each take 13.7; up to 120 of each of 60 18.6 and 17.4 (18.4).
 __device__ __forceinline__ Share its_share(const AppendParams& p, int unit, const Sequence& s) {
   const int first = max(s.first_pos(), 0);
   const bool two = s.len > first && (s.len - 1) >> p.batch.page_shift > first >> p.batch.page_shift;
-  const int groups = min(max(two ? p.budget / 2 : p.budget, 1), p.lines), j = unit >= groups;
+  const int groups = two ? p.groups : p.one, j = unit >= groups;
   return {j + (unit >= 2 * groups), unit - j * groups, groups};
 }
 
@@ -393,8 +393,6 @@ static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream)
     p.groups = groups_for(slots, parts);
     if (p.lines > 16 * p.groups) {
       p.groups = (p.lines + 7) / 8;
-    } else if (rows > 4 && p.pages_each == 2 && slots >= 4 * parts) {
-      p.budget = (int)std::min(slots / p.batch.B, 2LL * p.lines);
     } else {
       // ... or a wave of the pages that T new tokens reach on average, wherever in a page they begin, and a little more, where that leaves a unit fewer lines.
       // Three frames of 1560 tokens by eight units a page instead of seven 19.5 us for 20.9, and 20.3 for 21.0 where they reach a page more; 16 sequences of up to
@@ -404,6 +402,13 @@ static int launch_rows(const AppendParams& given, int rows, cudaStream_t stream)
       const int g = groups_for(slots + slots / 32, p.batch.B + (p.batch.T - p.batch.B + (1 << p.batch.page_shift) - 1) / (1 << p.batch.page_shift));
       const int before = lines_of(p.groups), after = lines_of(g);
       if (before >= 4 && rows > 4 ? after < before : 2 * after <= before && 3 * parts * g <= 4 * slots) p.groups = g;
+    }
+    if (rows > 4 && p.pages_each == 2 && slots >= 4LL * p.batch.B) {
+      // a wave of one page of every sequence for those that reach one, and for the others half of that where it is enough
+      p.one = groups_for(slots, p.batch.B);
+      if (slots >= 4 * parts) p.groups = groups_for(slots / p.batch.B, 2);
+      else if (p.lines > 16 * p.one) p.one = p.groups;
+      p.budget = std::max(p.one, 2 * p.groups);
     }
     const long long units = p.budget > 0 ? (long long)p.budget * p.batch.B : parts * p.groups;
     if (units > 0x7fffff00LL) return (int)SPARKATTN_E_UNSUPPORTED_SHAPE;
