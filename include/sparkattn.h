@@ -466,7 +466,9 @@ typedef struct {
   const int32_t* axis;       /* [rot/2], entries in [0, axes); NULL: all 0                    */
 } sparkattn_rotary_t;
 
-/* RMS norm over the d channels of each head, in front of the rotation:  y_c = x_c / sqrt(mean(x^2) + eps) * weight_c.
+/* RMS norm over the d channels of each head, in front of the rotation:  y_c = x_c / sqrt(mean(x^2) + eps) * weight_c.  The mean is a head's, with
+ * weights of each head too: models whose norm takes one mean over all heads' channels (Wan2.1's, over 12 or 40 heads of 128) need theirs in front, and
+ * norm = NULL here.  weight / sqrt(mean + eps) has to be a finite fp32 number.
  * fp32 throughout (squares, their sum, the root, the products); no rounding to 16 bits between norm and rotation, whose products and sums may be
  * fused here.  A row whose sum of squares passes
  * fp32's range, which takes entries of 1e18, comes out as zeros; one with an infinity or a NaN gives NaN there. */

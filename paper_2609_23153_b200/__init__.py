@@ -524,7 +524,8 @@ class Rotary(NamedTuple):
 
 class Norm(NamedTuple):
     """RMS norm over the channels of each head of queries and keys, in front of their rotation: x / sqrt(mean(x^2) + eps) * weight.  Weights
-    ``q``, ``k`` float32 or bfloat16, [d] or [heads, d], both alike; None: ones."""
+    ``q``, ``k`` float32 or bfloat16, [d] or [heads, d], both alike; None: ones.  (Not the norm of models that take one mean over all heads'
+    channels, such as Wan2.1's: apply that in front, and rotate with ``norm=None``.)"""
     q: Optional[torch.Tensor] = None
     k: Optional[torch.Tensor] = None
     eps: float = 1e-6

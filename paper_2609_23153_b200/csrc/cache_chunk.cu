@@ -22,10 +22,10 @@
 // the second one in the other half of S's columns, give 1.7e-3, and half as many products again: three frames of 1560 tokens 851 -> 1184 us, four
 // prompts 550 -> 774, five drafted tokens of 8 sequences 69 -> 78.  So one part here, two with few rows, where the memory's time hides the second.
 // Measured (E4M3, 128 channels; a library product of bf16 matrices reaches 1704 TFLOP/s in a burst, 1439 for seconds): 4680 new tokens,
-// three frames, over 32,760, 12 heads, 897 GFLOP in 815-840 us = 1070-1100 TFLOP/s, called for seconds, at 1.6 GHz and less under the power limit, 897: tensor cores and
+// three frames, over 32,760, 12 heads, 897 GFLOP in 807-815 us = 1100-1110 TFLOP/s, called for seconds, at 1.6 GHz and less under the power limit, 897: tensor cores and
 // special-function unit are busy 52 % of the clocks each, the rest is the chain that a half goes through once a tile, S, maximum, exponentials, P V.
-// Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 515-540 us = 940-980 TFLOP/s; a causal
-// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 64-66 us;
+// Pieces of 2048 tokens of four prompts of up to 8000, 32 heads over 8, causal by token: 507 GFLOP in 500-540 us = 940-1010 TFLOP/s; a causal
+// tile at the border costs as much as a whole one.  SPLIT: five drafted tokens of 8 sequences of up to 16,383, 64 heads over 8: 145 MB in 63 us;
 // 1 us a tile per SM, a chain of copy, conversion, product, softmax and product that only two tiles at a time share.
 // Through a window with first tokens (SINK): the same three frames over five frames up to their own and the first, 269 GFLOP in 296 us = 910 TFLOP/s; pieces of
 // 2048 tokens of four prompts, window 1500 and 100 tokens, bf16, 145 GFLOP in 195 us: items are 14 tiles long, and what lies between two of them, 8 us, is a

@@ -8,8 +8,8 @@
 //   A fork changes counts for whole rows, by integer additions, in any order: a launch of its own, since sixteen SMs issue their additions to
 //   scattered words a few clocks apart (256 rows of 500 entries: 11.2 us with one cluster, 4.6 with two launches).
 // Free pages are handed out in ascending order: the same call gives the same book.
-// Measured: a fork of 256 sequences of up to 32,000 tokens, pages of 64, 4.6 us; pages for a token of each of 128 sequences 7.0 us, in place 5.8, for prompts of
-// 4000 tokens of each of 32, pages of 16, 9.7, for one of 65,536, whose 4096 entries one warp writes, 35; the 90
+// Measured: a fork of 256 sequences of up to 32,000 tokens, pages of 64, 4.6 us; pages for a token of each of 128 sequences 7.2 us, in place 6.3, with the step's
+// lengths 7.4, for prompts of 4000 tokens of each of 32, pages of 16, 10.3, for one of 65,536, whose 4096 entries one warp writes, 31; the 90
 // copies of pages of 16 tokens that they share 2.7; a trim of 32 sequences 4.7, with nothing to give back 3.1; compact, 1560 pages, 6.4.  Latency
 // bounds all of them.  The copy of 368 pages of 196 KB, K and V, 289 MB read and written: 49 us = 5.9 TB/s, 0.89 of a copy's rate.
 #include <algorithm>
