@@ -310,7 +310,7 @@ struct ReserveParams {
   int32_t* kv_len_out;           // NULL: not asked for
   int32_t* src;
   int32_t* dst;
-  int32_t* list;                 // workspace: the free pages that are handed out, in order; then (Asks::ahead) what each has been given for
+  int32_t* list;                 // workspace: the free pages that are handed out, in order; then, where columns ask in place of others' pages, the entry that each has taken the place of
   int ranks, slots;              // slots of the hash table: a power of two, twice the sequences or more
   int32_t* status;
 };
@@ -563,7 +563,7 @@ pages_reserve_kernel(const __grid_constant__ ReserveParams p) {
     }
   }
   book_end(s, rank, p.ranks, p.status);
-  if (!later || !enough) return;
+  if (!later || !enough) return;      // (its barrier stands between the last look at a count and what follows)
   for (int i = rank * kBookThreads + threadIdx.x; i < carry; i += p.ranks * kBookThreads) {
     const int e = p.list[i];
     if ((uint32_t)e < (uint32_t)v.pages) atomicSub(v.refs_out + e, 1);
